@@ -41,7 +41,7 @@ def listed():
         # chunked prefill of eight ragged requests on 28 / 4 heads, half of the head rotated, interleaved pairs
         _rope("rope ragged 8x511", 8, 28, 4, 511, 1024, 64, True, "linear", True, False),
         # two whole prompts of 16384 tokens
-        _rope("rope prompt 2x16384", 2, 32, 8, 16384, 16384, 128, False, "llama3", False, False),
+        _rope("rope prompt 2x16384", 2, 32, 8, 16384, 16384, 128, False, "bands", False, False),
         # the smallest decode step: one sequence, eight single-query heads, capped scores
         _scored("scored cap 1x8", 1, 8, 8, 4096, 8, 4, 64, 30.0, False, 0, 0, False),
         # 32 single-query heads with distance slopes over 32768 cached tokens, 128 selected pages
@@ -80,7 +80,7 @@ def draw(rng):
             max_new = max(1, max_new // 2)
         return dict(op=op, batch=batch, hq=hq, hkv=hkv, max_new=max_new, t_cap=max_new + rng.randint(0, 700),
                     rot=rng.choice([16, 32, 64, 96, 128]), interleaved=rng.random() < 0.5,
-                    scaling=rng.choice(["none", "linear", "yarn", "llama3"]), ragged=rng.random() < 0.6,
+                    scaling=rng.choice(["none", "linear", "yarn", "bands"]), ragged=rng.random() < 0.6,
                     far=rng.random() < 0.5)
     if op == "scored":
         t = _log(rng, 17, 131072)
@@ -124,7 +124,7 @@ def _i32(values):
 def _inv_freq(rot, scaling):
     """Radians per position of each pair, in 64 bits, and the factor on the rotated channels."""
     i = torch.arange(rot // 2, dtype=torch.float64)
-    if scaling == "llama3":                    # base 500000; wavelengths beyond the trained context / 1 slowed 8 times
+    if scaling == "bands":                    # base 500000; wavelengths beyond the trained context / 1 slowed 8 times
         f = 500000.0 ** (-2.0 * i / rot)
         wave, old = 2 * math.pi / f, 8192.0
         smooth = ((old / wave - 1.0) / (4.0 - 1.0)).clamp(0.0, 1.0)
