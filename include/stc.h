@@ -90,6 +90,32 @@ typedef struct stc_cache {
     int64_t cap_groups;        /* rows of v_packed per problem                        */
 } stc_cache;
 
+/* What stc_decode_attn_scored does to the scores besides sm_scale; zero / NULL
+ * switches an option off. */
+typedef struct stc_score {
+    float softcap;             /* > 0: s becomes softcap * tanh(s / softcap)          */
+    int32_t window;            /* > 0: a query sees its window most recent tokens     */
+    const float* slopes;       /* device f32 [Hq]: s += slopes[h] * (t - q_pos), after the cap */
+    const int32_t* q_pos;      /* device i32, one per query row: position of the query,
+                                  counted like t (cached token t stands at t); tokens
+                                  behind it are not seen                              */
+    const int32_t* tok_doc;    /* device i32 [B][t_cap]: document of each cached token,
+                                  < 0 = seen by every query                           */
+    const int32_t* q_doc;      /* device i32, one per query row: the query's document  */
+} stc_score;
+
+/* Rotary positions: pair i of the rotated channels is turned by the angle
+ * position * inv_freq[i]. */
+typedef struct stc_rope {
+    const double* inv_freq;    /* device f64 [rot_dim/2], radians per position        */
+    int32_t rot_dim;           /* leading channels that are rotated: multiple of 16, 0..128 */
+    int32_t interleaved;       /* 0: pair i = channels (i, i + rot_dim/2); 1: (2i, 2i+1) */
+    float scale;               /* factor on the rotated channels (1 unless the table's scaling asks for one) */
+    int32_t reserved;          /* must be 0 */
+} stc_rope;
+
+enum { STC_ROPE_NONE = 0, STC_ROPE_LINEAR = 1, STC_ROPE_BANDS = 2, STC_ROPE_YARN = 3 };
+
 const char* stc_status_string(int32_t status);
 int32_t stc_version(void);
 
@@ -297,6 +323,44 @@ int32_t stc_append_tokens(const stc_shape* shape, const stc_cache* cache, const 
                           const int32_t* old_len, int32_t max_new, int64_t* total_groups, int32_t* status,
                           void* stream);
 
+/* Frequency table of a stc_rope, by host arithmetic in double.  With f_i = base^(-2i/rot_dim):
+ *   STC_ROPE_NONE     f_i
+ *   STC_ROPE_LINEAR   f_i / factor (positions interpolated)
+ *   STC_ROPE_BANDS    by the turns n_i = original_len * f_i / 2 pi that the pair makes over the
+ *                     context it was trained on: f_i where n_i >= high, f_i / factor where
+ *                     n_i <= low, linear in n_i between (common: low 1, high 4)
+ *   STC_ROPE_YARN     f_i for pairs up to the one that makes `high` turns, f_i / factor from the one
+ *                     that makes `low` turns on, linear in the pair index between (bounds rounded
+ *                     outwards to whole pairs; common: low 1, high 32); scale = 0.1 ln(factor) + 1
+ * inv_freq_host: f64 [rot_dim/2]; scale_host: f32, 1 except for STC_ROPE_YARN.  factor >= 1;
+ * original_len, low, high are read by BANDS and YARN only. */
+int32_t stc_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double original_len,
+                             double low, double high, double* inv_freq_host, float* scale_host);
+
+/* Rotary positions on the way into the cache.  (The paper leaves q and k as the model produces them, Section 3.3;
+ * its models rotate them before they are cached, which every other call here presumes.)  For every
+ * sequence b the tokens old_len[b] <= t < len[b] (len = shape->seq_len AFTER the append, as in
+ * stc_append_tokens) are new; the i-th of them, t = old_len[b] + i, has its rows at token
+ * b * max_new + i of the projection's output:
+ *   q_in  bf16, q_stride elements from token to token, Hq rows of 128 per token -> rotated to
+ *   q_out bf16 [B][max_new][Hq][128]  (max_new = 1: the layout stc_quest_select / stc_decode_attn read)
+ *   k_in  likewise with Hkv rows -> rotated to k[b][hk][t][128]   (the cache's keys)
+ *   v_in  likewise -> copied to v[b][hk][t][128]   (what stc_route_pack / stc_append_tokens read)
+ * Each of the three may be absent (both of its pointers NULL).  Strides are multiples of 8 and at
+ * least one token's rows, so the three may be slices of one fused projection.  The rotation of token t uses
+ * positions_opt[b][i] (i32 [B][max_new]; tokens that survived an upstream reducer keep the positions they
+ * had), or t when positions_opt is NULL.  q_out may be q_in where the layouts agree
+ * (q_stride = Hq * 128); other outputs must not overlap inputs.
+ * Angles are formed modulo a whole turn in 64-bit fixed point, so they are exact to fp32 at any position;
+ * the products are fp32 with one rounding to bf16.  Channels from rot_dim on are copied.
+ * Rows of q_out behind a sequence's new tokens, and all other rows of the caches, are left as they were.
+ * status: i32 [B]: STC_OK, or STC_ERR_INVALID_ARG for a sequence whose lengths are inconsistent
+ * (old_len > len, or more than max_new new tokens), which is left untouched.  Needs no workspace. */
+int32_t stc_rope_write(const stc_shape* shape, const stc_rope* rope, const int32_t* old_len, int32_t max_new,
+                       const int32_t* positions_opt, const void* q_in, int64_t q_stride, const void* k_in,
+                       int64_t k_stride, const void* v_in, int64_t v_stride, void* q_out, void* k, void* v,
+                       int32_t* status, void* stream);
+
 /* Routing of the pages completed during decoding (Section 3.4: the budget is global over the
  * retained tokens, M = N*K in Appendix B.1, and the query region stays uncompressed; the paper
  * does not say when a generated token leaves the query region -- reading taken: while its
@@ -343,6 +407,23 @@ int32_t stc_decode_attn(const stc_shape* shape, const stc_cache* cache, const vo
                         const int32_t* page_ids, const int32_t* n_pages, int32_t max_pages,
                         float sm_scale, float* out, float* lse_opt, void* ws, size_t ws_bytes,
                         void* stream);
+
+/* stc_decode_attn with options on the scores, for models that cap them, bias them by distance or keep
+ * documents apart (the paper's attention equation, Section 3.3, has none of these; everything else is as there).
+ * Per query head h of sequence b with query position p = score->q_pos[b] (NULL: len - 1, the
+ * newest cached token), over the valid tokens t of the listed pages with
+ *     t <= p,   p - t < window (if set),   tok_doc[b][t] < 0 or tok_doc[b][t] == q_doc[b] (if set):
+ *     x_t = sm_scale * q_h.k_t;   x_t = softcap * tanh(x_t / softcap) (if set);
+ *     s_t = x_t + slopes[h] * (t - p) (if set)
+ * and softmax, values and lse as in stc_decode_attn.  A head with no token left gives out = 0 and
+ * lse = -inf.  Keys and values of tokens that are not seen are never used, whatever they hold.
+ * score NULL or all off: the same kernels, hence the same bits, as stc_decode_attn.  tanh is good to
+ * one fp32 unit.  Workspace, alignment and status word as in stc_decode_attn; page selection knows nothing
+ * of a distance bias (a cap is monotone and changes no ranking within a head). */
+int32_t stc_decode_attn_scored(const stc_shape* shape, const stc_cache* cache, const void* q,
+                               const int32_t* page_ids, const int32_t* n_pages, int32_t max_pages,
+                               float sm_scale, const stc_score* score, float* out, float* lse_opt, void* ws,
+                               size_t ws_bytes, void* stream);
 
 /* One decode step on the device: stc_quest_select followed by stc_decode_attn over the pages it
  * selected (Stage I per step, Section 3.2, then the routed attention of Section 3.3), as one call.

@@ -20,6 +20,7 @@ _LIB_PATH = _PKG / "libstc.so"
 OP_QUEST_SELECT, OP_ROUTE_PACK, OP_DECODE_ATTN = 1, 2, 3
 MODE_GLOBAL, MODE_PER_TOKEN = 0, 1
 CLS_DROP, CLS_ROUTED, CLS_FULL = 0, 1, 2
+ROPE_NONE, ROPE_LINEAR, ROPE_BANDS, ROPE_YARN = 0, 1, 2, 3
 STC_OK = 0
 STATIC_SCRATCH_BYTES = 8 << 20
 
@@ -27,6 +28,7 @@ EXPORTS = (
     "stc_status_string", "stc_version", "stc_workspace_bytes", "stc_build_page_meta",
     "stc_quest_select", "stc_route_pack", "stc_decode_attn", "stc_cache_bytes",
     "stc_pass_host_arena_bytes", "stc_pass_host", "stc_quest_select_static", "stc_route_mask", "stc_pack_values", "stc_append_tokens", "stc_router_logits", "stc_query_bias", "stc_quest_select_window", "stc_pages_to_class", "stc_route_new_pages", "stc_decode_step", "stc_decode_step_host_arena_bytes", "stc_decode_step_host",
+    "stc_rope_frequencies", "stc_rope_write", "stc_decode_attn_scored",
 )
 
 
@@ -47,6 +49,16 @@ class _Cache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("kmin", C.c_void_p), ("kmax", C.c_void_p),
                 ("v_packed", C.c_void_p), ("v_mask", C.c_void_p), ("v_offs", C.c_void_p),
                 ("cap_groups", C.c_int64)]
+
+
+class _Score(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("window", C.c_int32), ("slopes", C.c_void_p), ("q_pos", C.c_void_p),
+                ("tok_doc", C.c_void_p), ("q_doc", C.c_void_p)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_float),
+                ("reserved", C.c_int32)]
 
 
 _lib = None
@@ -95,6 +107,14 @@ def load_library():
         lib.stc_decode_attn.argtypes = [C.POINTER(_Shape), C.POINTER(_Cache), C.c_void_p, C.c_void_p, C.c_void_p,
                                         C.c_int32, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
                                         C.c_void_p]
+        lib.stc_decode_attn_scored.argtypes = [C.POINTER(_Shape), C.POINTER(_Cache), C.c_void_p, C.c_void_p,
+                                               C.c_void_p, C.c_int32, C.c_float, C.POINTER(_Score), C.c_void_p,
+                                               C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.stc_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double,
+                                             C.c_double, C.c_void_p, C.c_void_p]
+        lib.stc_rope_write.argtypes = [C.POINTER(_Shape), C.POINTER(_Rope), C.c_void_p, C.c_int32, C.c_void_p,
+                                       C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         lib.stc_decode_step.argtypes = [C.POINTER(_Shape), C.POINTER(_Cache), C.c_void_p, C.c_int32, C.c_int32,
                                         C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p,
                                         C.c_size_t, C.c_void_p, C.c_size_t, C.c_void_p]
@@ -180,6 +200,68 @@ class Cache:
             v_mask=torch.zeros(B, H, T, dtype=torch.int16, device=dev),
             v_offs=torch.zeros(B, H, T + 1, dtype=torch.int32, device=dev),
             cap_groups=cap_groups)
+
+
+@dataclass
+class Score:
+    """Options on the scores of decode_attn (stc_score): cap, window, distance slopes, document mask."""
+    softcap: float = 0.0
+    slopes: Optional[torch.Tensor] = None     # f32 [Hq]
+    q_pos: Optional[torch.Tensor] = None      # i32, one per query row
+    window: int = 0
+    tok_doc: Optional[torch.Tensor] = None    # i32 [B, T]
+    q_doc: Optional[torch.Tensor] = None      # i32, one per query row
+
+    def c(self, shape: Shape, rows: int) -> _Score:
+        _sized(self.slopes, (shape.n_q_heads,), "slopes")
+        _sized(self.q_pos, (rows,), "q_pos")
+        _sized(self.tok_doc, (shape.batch, shape.t_cap), "tok_doc")
+        _sized(self.q_doc, (rows,), "q_doc")
+        return _Score(self.softcap, self.window, _ptr(self.slopes, torch.float32, "slopes"),
+                      _ptr(self.q_pos, torch.int32, "q_pos"), _ptr(self.tok_doc, torch.int32, "tok_doc"),
+                      _ptr(self.q_doc, torch.int32, "q_doc"))
+
+
+@dataclass
+class Rope:
+    """Rotary table (stc_rope): inv_freq f64 [rot_dim/2] on the device, radians per position."""
+    inv_freq: torch.Tensor
+    interleaved: bool = False
+    scale: float = 1.0
+
+    def c(self) -> _Rope:
+        return _Rope(_ptr(self.inv_freq, torch.float64, "inv_freq"), 2 * self.inv_freq.numel(), int(self.interleaved),
+                     self.scale, 0)
+
+
+def _sized(t: Optional[torch.Tensor], size, name: str) -> None:
+    if t is not None and tuple(t.shape) != tuple(size):
+        raise ValueError(f"{name} must have shape {tuple(size)}, got {tuple(t.shape)}")
+
+
+def _on_current_device(*tensors) -> None:
+    """The call goes to the current device's stream: every tensor has to live there."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != here:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
+
+
+def _token_rows(t: Optional[torch.Tensor], shape: Shape, heads: int, name: str):
+    """(pointer, elements from token to token) of rows [B, n, heads, 128] that may be a slice of wider token rows."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.dtype != torch.bfloat16:
+        raise ValueError(f"{name} must be a CUDA tensor of torch.bfloat16")
+    if t.dim() != 4 or t.shape[0] != shape.batch or t.shape[2:] != (heads, shape.head_dim):
+        raise ValueError(f"{name} must have shape [{shape.batch}, n, {heads}, {shape.head_dim}], got {tuple(t.shape)}")
+    B, n = t.shape[:2]
+    if t.numel() == 0:
+        return C.c_void_p(t.data_ptr()), heads * shape.head_dim
+    step = t.stride(1) if n > 1 else t.stride(0) if B > 1 else heads * shape.head_dim
+    if t.stride(3) != 1 or (heads > 1 and t.stride(2) != shape.head_dim) or (B > 1 and t.stride(0) != n * step):
+        raise ValueError(f"{name}: a token's rows must be contiguous and tokens equally spaced, got strides {t.stride()}")
+    return C.c_void_p(t.data_ptr()), step
 
 
 def _check(rc: int, where: str):
@@ -290,6 +372,52 @@ def append_tokens(shape: Shape, cache: Cache, v: torch.Tensor, old_len: torch.Te
         "stc_append_tokens")
 
 
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = ROPE_NONE, factor: float = 1.0,
+                     original_len: float = 0.0, low: float = 1.0, high: float = 0.0):
+    """(inv_freq f64 [rot_dim/2] on the host, scale) of a rotary table; high 0 = 4 for ROPE_BANDS, 32 for ROPE_YARN."""
+    if not high:
+        high = 32.0 if scaling == ROPE_YARN else 4.0
+    inv_freq = torch.zeros(max(rot_dim, 0) // 2, dtype=torch.float64)
+    scale = C.c_float(1.0)
+    _check(load_library().stc_rope_frequencies(rot_dim, base, scaling, factor, original_len, low, high,
+                                               C.c_void_p(inv_freq.data_ptr() or 1), C.byref(scale)),
+           "stc_rope_frequencies")
+    return inv_freq, float(scale.value)
+
+
+def rope_write(shape: Shape, rope: Rope, old_len: torch.Tensor, status: torch.Tensor,
+               q_in: Optional[torch.Tensor] = None, k_in: Optional[torch.Tensor] = None,
+               v_in: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+               k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+               positions: Optional[torch.Tensor] = None) -> None:
+    """Rotates q and k of the tokens old_len[b] .. shape.seq_len[b] and writes them, and v, where the cache wants them.
+
+    q_in / k_in / v_in [B, n, heads, 128] (slices of one fused projection allowed) -> q_out [B, n, Hq, 128],
+    k, v [B, Hkv, T, 128]; n is the most new tokens of a sequence; positions i32 [B, n] or None (= cache index)."""
+    B, T, D = shape.batch, shape.t_cap, shape.head_dim
+    given = [x for x in (q_in, k_in, v_in) if x is not None]
+    if not given:
+        raise ValueError("rope_write needs at least one of q_in, k_in, v_in")
+    n = given[0].shape[1]
+    if any(x.shape[1] != n for x in given):
+        raise ValueError("q_in, k_in and v_in must hold the same number of tokens")
+    qp, qs = _token_rows(q_in, shape, shape.n_q_heads, "q_in")
+    kp, ks = _token_rows(k_in, shape, shape.n_kv_heads, "k_in")
+    vp, vs = _token_rows(v_in, shape, shape.n_kv_heads, "v_in")
+    _sized(q_out, (B, n, shape.n_q_heads, D), "q_out")
+    _sized(k, (B, shape.n_kv_heads, T, D), "k")
+    _sized(v, (B, shape.n_kv_heads, T, D), "v")
+    _sized(positions, (B, n), "positions")
+    _sized(old_len, (B,), "old_len")
+    _sized(status, (B,), "status")
+    _on_current_device(q_in, k_in, v_in, q_out, k, v, positions, old_len, status, rope.inv_freq, shape.seq_len)
+    cs, cr = shape.c(), rope.c()
+    _check(load_library().stc_rope_write(
+        C.byref(cs), C.byref(cr), _ptr(old_len, torch.int32, "old_len"), n, _ptr(positions, torch.int32, "positions"),
+        qp, qs, kp, ks, vp, vs, _ptr(q_out, torch.bfloat16, "q_out"), _ptr(k, torch.bfloat16, "k"),
+        _ptr(v, torch.bfloat16, "v"), _ptr(status, torch.int32, "status"), _stream()), "stc_rope_write")
+
+
 def route_new_pages(shape: Shape, cache: Cache, scores: torch.Tensor, first_page: torch.Tensor, k_nominal: int,
                     total_groups: torch.Tensor, status: torch.Tensor, min_per_token: int = 1,
                     mode: int = MODE_GLOBAL) -> None:
@@ -323,9 +451,19 @@ def query_bias(h_q: torch.Tensor, w_q: torch.Tensor, s_q: torch.Tensor, bias: to
 
 def decode_attn(shape: Shape, cache: Cache, q: torch.Tensor, page_ids: Optional[torch.Tensor],
                 n_pages: Optional[torch.Tensor], sm_scale: float, out: torch.Tensor, ws: torch.Tensor,
-                lse: Optional[torch.Tensor] = None) -> None:
+                lse: Optional[torch.Tensor] = None, score: Optional[Score] = None) -> None:
+    """score: capped / biased / windowed / per-document scores (stc_decode_attn_scored)."""
     max_pages = page_ids.shape[-1] if page_ids is not None else shape.n_pages
     cs, cc = shape.c(), cache.c()
+    if score is not None:
+        _on_current_device(q, out, ws, cache.k, score.slopes, score.q_pos, score.tok_doc, score.q_doc)
+        co = score.c(shape, shape.batch)
+        _check(load_library().stc_decode_attn_scored(
+            C.byref(cs), C.byref(cc), _ptr(q, torch.bfloat16, "q"), _ptr(page_ids, torch.int32, "page_ids"),
+            _ptr(n_pages, torch.int32, "n_pages"), max_pages, sm_scale, C.byref(co), _ptr(out, torch.float32, "out"),
+            _ptr(lse, torch.float32, "lse"), _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream()),
+            "stc_decode_attn_scored")
+        return
     _check(load_library().stc_decode_attn(
         C.byref(cs), C.byref(cc), _ptr(q, torch.bfloat16, "q"), _ptr(page_ids, torch.int32, "page_ids"),
         _ptr(n_pages, torch.int32, "n_pages"), max_pages, sm_scale, _ptr(out, torch.float32, "out"),

@@ -137,6 +137,41 @@ __device__ __forceinline__ uint32_t bmax2(uint32_t a, uint32_t b) {
     return *reinterpret_cast<uint32_t*>(&r);
 }
 
+// tanh to about one fp32 ulp.  |z| <= 0.55: odd polynomial z + z^3 P(z^2), P fitted by weighted least
+// squares at Chebyshev nodes (relative error 6.7e-8 against extended precision); above: 1 - 2 / (e^{2z} + 1), whose
+// absolute error of about 1.5e-7 is small against tanh >= 0.5.  The hardware tanh (error 2^-11) would
+// move a score capped at 50 by 0.02.
+__device__ __forceinline__ float tanh_f32(float z) {
+    const float u = z * z;
+    if (u <= 0.3025f) {
+        float p = -0.006272607482969761f;
+        p = fmaf(p, u, 0.02107025310397148f);
+        p = fmaf(p, u, -0.053851865231990814f);
+        p = fmaf(p, u, 0.13332580029964447f);
+        p = fmaf(p, u, -0.33333316445350647f);
+        return fmaf(z * u, p, z);
+    }
+    const float e = exp2f(fabsf(z) * 2.885390081777927f);           // e^{2|z|}, +inf from |z| = 44 on
+    return copysignf(1.f - __fdividef(2.f, fminf(e, 1e30f) + 1.f), z);
+}
+
+// Options of the scored attention calls (stc_score) as the kernels take them.
+struct ScoreArgs {
+    float softcap;               // 0 = none
+    int window;                  // 0 = none
+    const float* slopes;         // [Hq] or nullptr
+    const int32_t* q_pos;        // position of each query row, or nullptr
+    const int32_t* tok_doc;      // [B][T] or nullptr
+    const int32_t* q_doc;        // document of each query row (with tok_doc)
+};
+
+// Tokens a query at position `pos` may see: [lo, hi) of a sequence of `len` tokens.
+__device__ __forceinline__ void visible_range(int len, int pos, int window, int& lo, int& hi) {
+    hi = pos < len ? (pos < 0 ? 0 : pos + 1) : len;
+    lo = (window > 0 && pos >= window) ? pos - window + 1 : 0;
+    if (lo > hi) lo = hi;
+}
+
 // Multiprocessor count of the current device (queried per call: cheap next to a launch, and
 // right on every device of a multi-GPU process).
 inline cudaError_t device_sm_count(int* n) {
@@ -194,6 +229,11 @@ cudaError_t launch_router_logits(const Geom& g, const void* h, const void* w, co
 cudaError_t launch_query_bias(int B, int Lq, int d_model, int n_logits, const void* h_q, const int32_t* q_len,
                               const void* w_q, float* s_q, float* bias, cudaStream_t st);
 
+cudaError_t launch_rope_write(const Geom& g, const stc_rope& rope, const int32_t* old_len, int max_new,
+                              const int32_t* positions, const void* q_in, int64_t q_stride, const void* k_in,
+                              int64_t k_stride, const void* v_in, int64_t v_stride, void* q_out, void* k, void* v,
+                              int32_t* status, cudaStream_t st);
+
 struct AttnPlan { int n_workers, slots_cap; };   // warps that share the pages; partial slots per problem
 AttnPlan attn_plan(const Geom& g, int max_pages);
 size_t attn_ws_bytes(const Geom& g, int max_pages);
@@ -201,7 +241,7 @@ cudaError_t launch_decode_attn(const Geom& g, const void* k, const void* v_packe
                                const uint16_t* v_mask, const uint32_t* v_offs, int64_t cap_groups,
                                const void* q, const int32_t* page_ids, const int32_t* n_pages,
                                int max_pages, float sm_scale, float* out, float* lse, void* ws,
-                               cudaStream_t st, unsigned flags = 0);
+                               cudaStream_t st, unsigned flags = 0, const ScoreArgs* score = nullptr);
 cudaError_t clear_decode_attn_ws(const Geom& g, void* ws, cudaStream_t st);
 size_t decode_attn_clear_bytes(const Geom& g);     // leading bytes of the workspace a call needs zeroed
 

@@ -2,6 +2,8 @@
 // allocates device memory; every launch goes to the caller's stream.
 #include <nvtx3/nvToolsExt.h>
 
+#include <cmath>
+
 #include "common.cuh"
 
 using namespace stc;
@@ -244,6 +246,69 @@ int32_t stc_append_tokens(const stc_shape* shape, const stc_cache* cache, const 
                                  static_cast<cudaStream_t>(stream)));
 }
 
+int32_t stc_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double original_len,
+                             double low, double high, double* inv_freq_host, float* scale_host) {
+    if (rot_dim < 0 || rot_dim > kHeadDim || !inv_freq_host || !scale_host || !(base > 1.0) || !std::isfinite(base))
+        return STC_ERR_INVALID_ARG;
+    if (rot_dim % 16 != 0) return STC_ERR_UNSUPPORTED;
+    if (scaling < STC_ROPE_NONE || scaling > STC_ROPE_YARN) return STC_ERR_INVALID_ARG;
+    if (scaling != STC_ROPE_NONE && !(factor >= 1.0 && std::isfinite(factor))) return STC_ERR_INVALID_ARG;
+    if (scaling >= STC_ROPE_BANDS && !(original_len > 0.0 && low > 0.0 && high > low && std::isfinite(original_len) &&
+                                       std::isfinite(high)))
+        return STC_ERR_INVALID_ARG;
+    const double two_pi = 6.283185307179586476925;
+    // pair (as a real number) that makes `turns` turns over the original context
+    auto pair_of = [&](double turns) {
+        return rot_dim * std::log(original_len / (turns * two_pi)) / (2.0 * std::log(base));
+    };
+    double lo = 0.0, hi = 0.0;
+    if (scaling == STC_ROPE_YARN) {
+        lo = std::fmax(std::floor(pair_of(high)), 0.0);
+        hi = std::fmin(std::ceil(pair_of(low)), rot_dim - 1.0);
+    }
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / rot_dim);
+        double keep = 1.0;                          // share of the unscaled frequency; the rest is divided by factor
+        if (scaling == STC_ROPE_LINEAR) keep = 0.0;
+        if (scaling == STC_ROPE_BANDS) {
+            const double turns = original_len * f / two_pi;
+            keep = std::fmin(std::fmax((turns - low) / (high - low), 0.0), 1.0);
+        }
+        if (scaling == STC_ROPE_YARN)
+            keep = 1.0 - std::fmin(std::fmax((i - lo) / std::fmax(hi - lo, 1e-3), 0.0), 1.0);
+        inv_freq_host[i] = keep * f + (1.0 - keep) * f / factor;
+    }
+    *scale_host = scaling == STC_ROPE_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
+    return STC_OK;
+}
+
+int32_t stc_rope_write(const stc_shape* shape, const stc_rope* rope, const int32_t* old_len, int32_t max_new,
+                       const int32_t* positions_opt, const void* q_in, int64_t q_stride, const void* k_in,
+                       int64_t k_stride, const void* v_in, int64_t v_stride, void* q_out, void* k, void* v,
+                       int32_t* status, void* stream) {
+    Range nvtx_range("stc_rope_write");
+    Geom g;
+    int32_t rc = make_geom(shape, &g);
+    if (rc != STC_OK) return rc;
+    if (!rope || max_new < 0 || rope->rot_dim < 0 || rope->rot_dim > kHeadDim || rope->reserved != 0 ||
+        (rope->interleaved != 0 && rope->interleaved != 1))
+        return STC_ERR_INVALID_ARG;
+    if (rope->rot_dim % 16 != 0) return STC_ERR_UNSUPPORTED;
+    if (empty(g) || max_new == 0) return STC_OK;
+    if (!old_len || !status || (rope->rot_dim > 0 && !rope->inv_freq)) return STC_ERR_INVALID_ARG;
+    if ((!q_in) != (!q_out) || (!k_in) != (!k) || (!v_in) != (!v) || (!q_in && !k_in && !v_in))
+        return STC_ERR_INVALID_ARG;
+    if (!aligned16(q_in, q_out, k_in, k, v_in, v) || (reinterpret_cast<uintptr_t>(rope->inv_freq) & 7u) != 0)
+        return STC_ERR_INVALID_ARG;
+    auto stride_ok = [&](const void* in, int64_t stride, int heads) {
+        return !in || (stride >= (int64_t)heads * kHeadDim && stride % 8 == 0 && stride < ((int64_t)1 << 40));
+    };
+    if (!stride_ok(q_in, q_stride, g.Hq) || !stride_ok(k_in, k_stride, g.Hkv) || !stride_ok(v_in, v_stride, g.Hkv))
+        return STC_ERR_INVALID_ARG;
+    return cuda_rc(launch_rope_write(g, *rope, old_len, max_new, positions_opt, q_in, q_stride, k_in, k_stride,
+                                     v_in, v_stride, q_out, k, v, status, static_cast<cudaStream_t>(stream)));
+}
+
 int32_t stc_route_new_pages(const stc_shape* shape, const stc_cache* cache, const float* scores,
                             const int32_t* first_page, int32_t k_nominal, int32_t min_per_token,
                             int32_t mode, int64_t* total_groups, int32_t* status, void* stream) {
@@ -264,15 +329,31 @@ int32_t stc_route_new_pages(const stc_shape* shape, const stc_cache* cache, cons
                                           static_cast<cudaStream_t>(stream)));
 }
 
-int32_t stc_decode_attn(const stc_shape* shape, const stc_cache* cache, const void* q,
-                        const int32_t* page_ids, const int32_t* n_pages, int32_t max_pages,
-                        float sm_scale, float* out, float* lse_opt, void* ws, size_t ws_bytes,
-                        void* stream) {
-    Range nvtx_range("stc_decode_attn");
+namespace {
+// Checked options of the scored calls; *plain = nothing is set and the call is the unscored one.
+int32_t score_args(const stc_score* score, ScoreArgs* out, bool* plain) {
+    *out = ScoreArgs{};
+    *plain = true;
+    if (!score) return STC_OK;
+    if (!(score->softcap >= 0.f) || !std::isfinite(score->softcap) || score->window < 0) return STC_ERR_INVALID_ARG;
+    if ((!score->tok_doc) != (!score->q_doc)) return STC_ERR_INVALID_ARG;
+    out->softcap = score->softcap; out->window = score->window; out->slopes = score->slopes;
+    out->q_pos = score->q_pos; out->tok_doc = score->tok_doc; out->q_doc = score->q_doc;
+    *plain = score->softcap == 0.f && score->window == 0 && !score->slopes && !score->q_pos && !score->tok_doc;
+    return STC_OK;
+}
+
+int32_t decode_attn(const stc_shape* shape, const stc_cache* cache, const void* q, const int32_t* page_ids,
+                    const int32_t* n_pages, int32_t max_pages, float sm_scale, const stc_score* score, float* out,
+                    float* lse_opt, void* ws, size_t ws_bytes, void* stream) {
     Geom g;
     int32_t rc = make_geom(shape, &g);
     if (rc != STC_OK) return rc;
     if (!cache || max_pages < 0 || !(sm_scale == sm_scale)) return STC_ERR_INVALID_ARG;
+    ScoreArgs sc;
+    bool plain;
+    rc = score_args(score, &sc, &plain);
+    if (rc != STC_OK) return rc;
     if (g.problems == 0) return STC_OK;
     if (!q || !out) return STC_ERR_INVALID_ARG;
     if (page_ids && !n_pages) return STC_ERR_INVALID_ARG;
@@ -285,7 +366,26 @@ int32_t stc_decode_attn(const stc_shape* shape, const stc_cache* cache, const vo
     if (rc != STC_OK) return rc;
     return cuda_rc(launch_decode_attn(g, cache->k, cache->v_packed, cache->v_mask, cache->v_offs,
                                       cache->cap_groups, q, page_ids, n_pages, max_pages, sm_scale,
-                                      out, lse_opt, ws, static_cast<cudaStream_t>(stream)));
+                                      out, lse_opt, ws, static_cast<cudaStream_t>(stream), 0, plain ? nullptr : &sc));
+}
+}  // namespace
+
+int32_t stc_decode_attn(const stc_shape* shape, const stc_cache* cache, const void* q,
+                        const int32_t* page_ids, const int32_t* n_pages, int32_t max_pages,
+                        float sm_scale, float* out, float* lse_opt, void* ws, size_t ws_bytes,
+                        void* stream) {
+    Range nvtx_range("stc_decode_attn");
+    return decode_attn(shape, cache, q, page_ids, n_pages, max_pages, sm_scale, nullptr, out, lse_opt, ws, ws_bytes,
+                       stream);
+}
+
+int32_t stc_decode_attn_scored(const stc_shape* shape, const stc_cache* cache, const void* q,
+                               const int32_t* page_ids, const int32_t* n_pages, int32_t max_pages,
+                               float sm_scale, const stc_score* score, float* out, float* lse_opt, void* ws,
+                               size_t ws_bytes, void* stream) {
+    Range nvtx_range("stc_decode_attn_scored");
+    return decode_attn(shape, cache, q, page_ids, n_pages, max_pages, sm_scale, score, out, lse_opt, ws, ws_bytes,
+                       stream);
 }
 
 int32_t stc_decode_step(const stc_shape* shape, const stc_cache* cache, const void* q, int32_t token_budget,
