@@ -67,7 +67,7 @@ typedef enum {
 
 enum { STC_CLS_DROP = 0, STC_CLS_ROUTED = 1, STC_CLS_FULL = 2 };
 enum { STC_MODE_GLOBAL = 0, STC_MODE_PER_TOKEN = 1 };
-enum { STC_OP_QUEST_SELECT = 1, STC_OP_ROUTE_PACK = 2, STC_OP_DECODE_ATTN = 3 };
+enum { STC_OP_QUEST_SELECT = 1, STC_OP_ROUTE_PACK = 2, STC_OP_DECODE_ATTN = 3, STC_OP_PREFIX_ATTN = 4 };
 
 typedef struct stc_shape {
     int32_t batch, n_q_heads, n_kv_heads;
@@ -90,7 +90,7 @@ typedef struct stc_cache {
     int64_t cap_groups;        /* rows of v_packed per problem                        */
 } stc_cache;
 
-/* What stc_decode_attn_scored does to the scores besides sm_scale; zero / NULL
+/* What stc_decode_attn_scored and stc_prefix_attn do to the scores besides sm_scale; zero / NULL
  * switches an option off. */
 typedef struct stc_score {
     float softcap;             /* > 0: s becomes softcap * tanh(s / softcap)          */
@@ -120,7 +120,7 @@ const char* stc_status_string(int32_t status);
 int32_t stc_version(void);
 
 /* Bytes of workspace `op` (STC_OP_*) needs for `shape`; `arg` is max_pages for
- * STC_OP_DECODE_ATTN and ignored otherwise.  Workspaces must be 256-byte
+ * STC_OP_DECODE_ATTN, n_rows for STC_OP_PREFIX_ATTN and ignored otherwise.  Workspaces must be 256-byte
  * aligned.  A workspace may be reused by consecutive calls on one stream;
  * calls that share a workspace must not overlap on the device. */
 int32_t stc_workspace_bytes(const stc_shape* shape, int32_t op, int64_t arg, size_t* bytes_host);
@@ -424,6 +424,34 @@ int32_t stc_decode_attn_scored(const stc_shape* shape, const stc_cache* cache, c
                                const int32_t* page_ids, const int32_t* n_pages, int32_t max_pages,
                                float sm_scale, const stc_score* score, float* out, float* lse_opt, void* ws,
                                size_t ws_bytes, void* stream);
+
+/* Attention over shared prefixes (the attention equation of Section 3.3 for a batch whose sequences continue
+ * the same cached text: a common prompt, document or image; the paper serves one sequence at a time).
+ * `shape` and `cache` describe the prefixes: shape->batch of them, shape->seq_len their lengths, routed and
+ * packed like any cache.  Query rows r with row_start[g] <= r < row_start[g+1] attend ALL valid tokens of prefix g
+ * (page selection is per query; a prefix computed once for all is attended whole), each KV head's prefix being
+ * read once for all its rows:
+ *     s_t = sm_scale * q_r.k_t, with the options of stc_score as in stc_decode_attn_scored (q_pos and q_doc
+ *           per row, tok_doc [batch][t_cap] of the prefixes; prefix token t stands at position t),
+ *     out[r] = softmax(s) V~,   lse[r] = log sum exp s.
+ * With own_out / own_lse (f32 [n_rows][Hq][128] / [n_rows][Hq], e.g. stc_decode_attn's out and lse over the
+ * sequence's own tokens) the two are joined:
+ *     L = log(e^lse + e^own_lse),  out = e^{lse-L} out + e^{own_lse-L} own_out,  lse = L;
+ * out may be own_out and lse_opt own_lse.  A side with lse = -inf contributes nothing, whatever its out holds; with
+ * nothing on either side out = 0 and lse = -inf.  Keys of tokens that no row sees may hold anything; packed
+ * values of all valid tokens must be finite.
+ *   q          bf16 [n_rows][Hq][128]   one row per query token: several tokens of a sequence are several rows
+ *   row_start  device i32 [batch+1], 0 <= row_start[g] <= row_start[g+1] <= n_rows; else nothing is written
+ *              and the status word becomes STC_ERR_INVALID_ARG.  Rows before row_start[0] and from
+ *              row_start[batch] on are left as they were.
+ * slopes and window need q_pos (STC_ERR_INVALID_ARG without).  batch * n_kv_heads * t_cap and n_rows * n_q_heads
+ * must be below 2^31 (else STC_ERR_UNSUPPORTED).  Both products run on the tensor cores with fp32 accumulation; the
+ * weights enter the second as a bf16 pair.  ws: STC_OP_PREFIX_ATTN with arg = n_rows; its first int32 is a
+ * device status word the call writes: STC_OK, STC_ERR_INVALID_ARG (row_start), or STC_ERR_TIMEOUT if a bounded
+ * wait expired on the device (it never should; out / lse are then unspecified). */
+int32_t stc_prefix_attn(const stc_shape* shape, const stc_cache* cache, int32_t n_rows, const void* q,
+                        const int32_t* row_start, float sm_scale, const stc_score* score, const float* own_out,
+                        const float* own_lse, float* out, float* lse_opt, void* ws, size_t ws_bytes, void* stream);
 
 /* One decode step on the device: stc_quest_select followed by stc_decode_attn over the pages it
  * selected (Stage I per step, Section 3.2, then the routed attention of Section 3.3), as one call.

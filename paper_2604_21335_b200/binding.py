@@ -17,7 +17,7 @@ import torch
 _PKG = Path(__file__).resolve().parent
 _LIB_PATH = _PKG / "libstc.so"
 
-OP_QUEST_SELECT, OP_ROUTE_PACK, OP_DECODE_ATTN = 1, 2, 3
+OP_QUEST_SELECT, OP_ROUTE_PACK, OP_DECODE_ATTN, OP_PREFIX_ATTN = 1, 2, 3, 4
 MODE_GLOBAL, MODE_PER_TOKEN = 0, 1
 CLS_DROP, CLS_ROUTED, CLS_FULL = 0, 1, 2
 ROPE_NONE, ROPE_LINEAR, ROPE_BANDS, ROPE_YARN = 0, 1, 2, 3
@@ -28,7 +28,7 @@ EXPORTS = (
     "stc_status_string", "stc_version", "stc_workspace_bytes", "stc_build_page_meta",
     "stc_quest_select", "stc_route_pack", "stc_decode_attn", "stc_cache_bytes",
     "stc_pass_host_arena_bytes", "stc_pass_host", "stc_quest_select_static", "stc_route_mask", "stc_pack_values", "stc_append_tokens", "stc_router_logits", "stc_query_bias", "stc_quest_select_window", "stc_pages_to_class", "stc_route_new_pages", "stc_decode_step", "stc_decode_step_host_arena_bytes", "stc_decode_step_host",
-    "stc_rope_frequencies", "stc_rope_write", "stc_decode_attn_scored",
+    "stc_rope_frequencies", "stc_rope_write", "stc_decode_attn_scored", "stc_prefix_attn",
 )
 
 
@@ -110,6 +110,9 @@ def load_library():
         lib.stc_decode_attn_scored.argtypes = [C.POINTER(_Shape), C.POINTER(_Cache), C.c_void_p, C.c_void_p,
                                                C.c_void_p, C.c_int32, C.c_float, C.POINTER(_Score), C.c_void_p,
                                                C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.stc_prefix_attn.argtypes = [C.POINTER(_Shape), C.POINTER(_Cache), C.c_int32, C.c_void_p, C.c_void_p,
+                                        C.c_float, C.POINTER(_Score), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                        C.c_void_p, C.c_size_t, C.c_void_p]
         lib.stc_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double,
                                              C.c_double, C.c_void_p, C.c_void_p]
         lib.stc_rope_write.argtypes = [C.POINTER(_Shape), C.POINTER(_Rope), C.c_void_p, C.c_int32, C.c_void_p,
@@ -469,6 +472,31 @@ def decode_attn(shape: Shape, cache: Cache, q: torch.Tensor, page_ids: Optional[
         _ptr(n_pages, torch.int32, "n_pages"), max_pages, sm_scale, _ptr(out, torch.float32, "out"),
         _ptr(lse, torch.float32, "lse"), _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream()),
         "stc_decode_attn")
+
+
+def prefix_attn(shape: Shape, cache: Cache, q: torch.Tensor, row_start: torch.Tensor, sm_scale: float, out: torch.Tensor,
+                ws: torch.Tensor, lse: Optional[torch.Tensor] = None, score: Optional[Score] = None,
+                own_out: Optional[torch.Tensor] = None, own_lse: Optional[torch.Tensor] = None) -> None:
+    """Rows row_start[g] .. row_start[g+1] of q [n_rows, Hq, 128] attend prefix g (sequence g of shape / cache), read
+    once for all of them; own_out / own_lse (the rows' results over their own tokens) are joined by log-sum-exp."""
+    n = q.shape[0]
+    _sized(q, (n, shape.n_q_heads, shape.head_dim), "q")
+    _sized(row_start, (shape.batch + 1,), "row_start")
+    _sized(out, (n, shape.n_q_heads, shape.head_dim), "out")
+    _sized(lse, (n, shape.n_q_heads), "lse")
+    _sized(own_out, (n, shape.n_q_heads, shape.head_dim), "own_out")
+    _sized(own_lse, (n, shape.n_q_heads), "own_lse")
+    _on_current_device(q, row_start, out, ws, lse, own_out, own_lse, cache.k, cache.v_packed, shape.seq_len)
+    cs, cc = shape.c(), cache.c()
+    co = None
+    if score is not None:
+        _on_current_device(score.slopes, score.q_pos, score.tok_doc, score.q_doc)
+        co = C.byref(score.c(shape, n))
+    _check(load_library().stc_prefix_attn(
+        C.byref(cs), C.byref(cc), n, _ptr(q, torch.bfloat16, "q"), _ptr(row_start, torch.int32, "row_start"), sm_scale,
+        co, _ptr(own_out, torch.float32, "own_out"), _ptr(own_lse, torch.float32, "own_lse"),
+        _ptr(out, torch.float32, "out"), _ptr(lse, torch.float32, "lse"), _ptr(ws, torch.uint8, "ws"), ws.numel(),
+        _stream()), "stc_prefix_attn")
 
 
 def decode_step(shape: Shape, cache: Cache, q: torch.Tensor, token_budget: int, page_ids: torch.Tensor,

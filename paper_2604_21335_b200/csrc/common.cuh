@@ -234,6 +234,12 @@ cudaError_t launch_rope_write(const Geom& g, const stc_rope& rope, const int32_t
                               int64_t k_stride, const void* v_in, int64_t v_stride, void* q_out, void* k, void* v,
                               int32_t* status, cudaStream_t st);
 
+size_t prefix_ws_bytes(const Geom& g, int n_rows);
+cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packed, const uint16_t* v_mask,
+                               const uint32_t* v_offs, int64_t cap_groups, int n_rows, const void* q,
+                               const int32_t* row_start, float sm_scale, const ScoreArgs* score, const float* own_out,
+                               const float* own_lse, float* out, float* lse, void* ws, cudaStream_t st);
+
 struct AttnPlan { int n_workers, slots_cap; };   // warps that share the pages; partial slots per problem
 AttnPlan attn_plan(const Geom& g, int max_pages);
 size_t attn_ws_bytes(const Geom& g, int max_pages);

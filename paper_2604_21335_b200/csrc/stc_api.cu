@@ -75,6 +75,11 @@ int32_t stc_workspace_bytes(const stc_shape* shape, int32_t op, int64_t arg, siz
     int32_t rc = make_geom(shape, &g);
     if (rc != STC_OK) return rc;
     if (!bytes_host) return STC_ERR_INVALID_ARG;
+    if (op == STC_OP_PREFIX_ATTN) {                 // rows have outputs even where the prefixes have no tokens
+        if (arg < 0 || arg > 0x7FFFFFFF) return STC_ERR_INVALID_ARG;
+        *bytes_host = g.problems == 0 || arg == 0 ? 0 : prefix_ws_bytes(g, (int)arg);
+        return STC_OK;
+    }
     if (empty(g)) { *bytes_host = 0; return STC_OK; }
     switch (op) {
         case STC_OP_QUEST_SELECT: *bytes_host = select_ws_bytes(g); break;
@@ -386,6 +391,32 @@ int32_t stc_decode_attn_scored(const stc_shape* shape, const stc_cache* cache, c
     Range nvtx_range("stc_decode_attn_scored");
     return decode_attn(shape, cache, q, page_ids, n_pages, max_pages, sm_scale, score, out, lse_opt, ws, ws_bytes,
                        stream);
+}
+
+int32_t stc_prefix_attn(const stc_shape* shape, const stc_cache* cache, int32_t n_rows, const void* q,
+                        const int32_t* row_start, float sm_scale, const stc_score* score, const float* own_out,
+                        const float* own_lse, float* out, float* lse_opt, void* ws, size_t ws_bytes, void* stream) {
+    Range nvtx_range("stc_prefix_attn");
+    Geom g;
+    int32_t rc = make_geom(shape, &g);
+    if (rc != STC_OK) return rc;
+    if (!cache || n_rows < 0 || !(sm_scale == sm_scale)) return STC_ERR_INVALID_ARG;
+    ScoreArgs sc;
+    bool plain;
+    rc = score_args(score, &sc, &plain);
+    if (rc != STC_OK) return rc;
+    if ((sc.slopes || sc.window > 0) && !sc.q_pos) return STC_ERR_INVALID_ARG;    // no position to count from
+    if ((int64_t)g.problems * g.T > 0x7FFFFFFFLL || (int64_t)n_rows * g.Hq > 0x7FFFFFFFLL) return STC_ERR_UNSUPPORTED;
+    if (g.problems == 0 || n_rows == 0) return STC_OK;
+    if (!q || !row_start || !out || (!own_out) != (!own_lse)) return STC_ERR_INVALID_ARG;
+    if (g.T > 0 && (!cache->k || !cache->v_packed || !cache->v_mask || !cache->v_offs || cache->cap_groups < 0))
+        return STC_ERR_INVALID_ARG;
+    if (!aligned16(cache->k, cache->v_packed, q, own_out, out)) return STC_ERR_INVALID_ARG;
+    rc = check_ws(ws, ws_bytes, prefix_ws_bytes(g, n_rows));
+    if (rc != STC_OK) return rc;
+    return cuda_rc(launch_prefix_attn(g, cache->k, cache->v_packed, cache->v_mask, cache->v_offs, cache->cap_groups,
+                                      n_rows, q, row_start, sm_scale, plain ? nullptr : &sc, own_out, own_lse, out,
+                                      lse_opt, ws, static_cast<cudaStream_t>(stream)));
 }
 
 int32_t stc_decode_step(const stc_shape* shape, const stc_cache* cache, const void* q, int32_t token_budget,

@@ -96,3 +96,30 @@ def test_scored_attention_refusals(lib):
     assert call(Bd._Score(0.0, 0, None, None, fake, None)) == 1
     assert call(Bd._Score(0.0, 0, None, None, None, fake)) == 1
     assert call(Bd._Score(30.0, 64, fake, fake, fake, fake)) == 3      # reaches the workspace check
+
+
+def test_prefix_attention_refusals(lib):
+    cs = P.Shape(2, 8, 4, 8, 4096).c()
+    fake, odd = C.c_void_p(0x1000), C.c_void_p(0x1008)
+    full = Bd._Cache(fake, fake, fake, fake, fake, fake, 100)
+
+    def call(shp=cs, cache=full, n=4, q=fake, start=fake, scale=0.1, score=None, own=None, own_lse=None, out=fake, ws=fake,
+             ws_bytes=16):
+        return lib.stc_prefix_attn(C.byref(shp), C.byref(cache), n, q, start, scale, score and C.byref(score), own, own_lse, out,
+                                   None, ws, ws_bytes, None)
+
+    assert call() == 3                           # valid but for the workspace
+    assert call(ws=C.c_void_p(0x1010), ws_bytes=1 << 40) == 3
+    for kw, code in [(dict(n=-1), 1), (dict(q=None), 1), (dict(start=None), 1), (dict(out=None), 1), (dict(q=odd), 1),
+                     (dict(out=odd), 1), (dict(scale=float("nan")), 1), (dict(own=fake), 1), (dict(own_lse=fake), 1),
+                     (dict(cache=Bd._Cache()), 1), (dict(score=Bd._Score(0.0, 5)), 1),
+                     (dict(score=Bd._Score(0.0, 0, fake)), 1), (dict(score=Bd._Score(-1.0, 0)), 1),
+                     (dict(shp=P.Shape(200, 8, 8, 8, (1 << 27) - 16).c()), 2), (dict(n=1 << 29), 2),
+                     (dict(n=0), 0), (dict(shp=P.Shape(0, 8, 4, 8, 4096).c()), 0)]:
+        assert call(**kw) == code, kw
+    s = P.Shape(2, 8, 4, 8, 4096)
+    n = P.workspace_bytes(s, Bd.OP_PREFIX_ATTN, 4)
+    assert n > 0 and n % 256 == 0 and P.workspace_bytes(s, Bd.OP_PREFIX_ATTN, 0) == 0
+    assert P.workspace_bytes(P.Shape(2, 8, 4, 8, 0), Bd.OP_PREFIX_ATTN, 4) > 0
+    with pytest.raises(P.StcError):
+        P.workspace_bytes(s, Bd.OP_PREFIX_ATTN, -1)
