@@ -141,19 +141,21 @@ __device__ __forceinline__ uint32_t bmax2(uint32_t a, uint32_t b) {
 // squares at Chebyshev nodes (relative error 6.7e-8 against extended precision); above: 1 - 2 / (e^{2z} + 1), whose
 // absolute error of about 1.5e-7 is small against tanh >= 0.5.  The hardware tanh (error 2^-11) would
 // move a score capped at 50 by 0.02.
-__device__ __forceinline__ float tanh_f32(float z) {
+constexpr float kTanhSmall = 0.55f;
+__device__ __forceinline__ float tanh_small(float z) {
     const float u = z * z;
-    if (u <= 0.3025f) {
-        float p = -0.006272607482969761f;
-        p = fmaf(p, u, 0.02107025310397148f);
-        p = fmaf(p, u, -0.053851865231990814f);
-        p = fmaf(p, u, 0.13332580029964447f);
-        p = fmaf(p, u, -0.33333316445350647f);
-        return fmaf(z * u, p, z);
-    }
+    float p = -0.006272607482969761f;
+    p = fmaf(p, u, 0.02107025310397148f);
+    p = fmaf(p, u, -0.053851865231990814f);
+    p = fmaf(p, u, 0.13332580029964447f);
+    p = fmaf(p, u, -0.33333316445350647f);
+    return fmaf(z * u, p, z);
+}
+__device__ __forceinline__ float tanh_large(float z) {
     const float e = exp2f(fabsf(z) * 2.885390081777927f);           // e^{2|z|}, +inf from |z| = 44 on
     return copysignf(1.f - __fdividef(2.f, fminf(e, 1e30f) + 1.f), z);
 }
+__device__ __forceinline__ float tanh_f32(float z) { return fabsf(z) <= kTanhSmall ? tanh_small(z) : tanh_large(z); }
 
 // Options of the scored attention calls (stc_score) as the kernels take them.
 struct ScoreArgs {

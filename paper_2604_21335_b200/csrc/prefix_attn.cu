@@ -162,7 +162,28 @@ __device__ __forceinline__ float bias_shift(const PrefixArgs& a, int len, int se
     return a.sc.slopes[head] * (float)(hi - 1 - pos);
 }
 
-template <int S, bool SCORED>
+// Caps 32 scores of a row (raw products in, log2 units out).  Scores far below the cap, the usual case, need only the
+// polynomial of tanh_f32; the warp votes once per 32 instead of branching per score.
+__device__ __forceinline__ void cap_scores(uint32_t (&r)[32], float cap_in, float cap_log2) {
+    float big = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) big = fmaxf(big, fabsf(__uint_as_float(r[i])));
+    if (__all_sync(0xFFFFFFFFu, big * fabsf(cap_in) <= kTanhSmall)) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(cap_log2 * tanh_small(__uint_as_float(r[i]) * cap_in));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float z = __uint_as_float(r[i]) * cap_in;
+            const float lo = tanh_small(z), hi = tanh_large(z);
+            r[i] = __float_as_uint(cap_log2 * (fabsf(z) <= kTanhSmall ? lo : hi));
+        }
+    }
+}
+
+// CAP: capped scores; BIAS: finished scores are needed for the maximum (slopes, or a scale that is not positive).
+// The window, positions and documents of the rows are masks and looked at in every variant.
+template <int S, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1)
 prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                    const PrefixArgs a) {
@@ -255,6 +276,12 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     Segment s;
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
     auto wait = [&](int i, uint32_t parity) { return mbar_wait_or_abort(bar(i), parity & 1u, abort_flag, kWaitNs); };
+    // the same for a whole warp: lane 0 waits and hands the answer on
+    auto warp_wait = [&](int i, uint32_t parity) -> bool {
+        int got = 0;
+        if (lane == 0) got = wait(i, parity);
+        return __shfl_sync(0xFFFFFFFFu, got, 0) != 0;
+    };
     auto give_up = [&]() { *abort_flag = 1; atomicCAS(a.status, 0, (int)STC_ERR_TIMEOUT); };
 
     if (*abort_flag) {
@@ -367,58 +394,58 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const int seq = s.row0 + (live ? seq_i : 0), head = s.hk * a.Gq + row % a.Gq;
             int lo = 0, hi = s.len, my_doc = 0;
             float slope2 = 0.f;
-            if constexpr (SCORED) {
-                if (a.sc.q_pos) visible_range(s.len, a.sc.q_pos[seq], a.sc.window, lo, hi);
-                if (a.sc.slopes) slope2 = a.sc.slopes[head] * kLog2e;
-                if (a.sc.tok_doc) my_doc = a.sc.q_doc[seq];
-            }
+            if (a.sc.q_pos) visible_range(s.len, a.sc.q_pos[seq], a.sc.window, lo, hi);
+            if (BIAS && a.sc.slopes) slope2 = a.sc.slopes[head] * kLog2e;
+            const int32_t* doc = a.sc.tok_doc ? a.sc.tok_doc + (size_t)s.g * a.T : nullptr;
+            if (doc) my_doc = a.sc.q_doc[seq];
+            // -inf for the tokens t .. t + 31 that the row does not see
+            auto hide = [&](uint32_t (&r)[32], int t) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (t + i < lo || t + i >= hi) r[i] = __float_as_uint(-INFINITY);
+                if (doc) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const int d = __ldg(doc + min(t + i, a.T - 1));
+                        if (d >= 0 && d != my_doc) r[i] = __float_as_uint(-INFINITY);
+                    }
+                }
+            };
             float m = -INFINITY, l = 0.f;
             for (int n = 0; n < mine; ++n) {
-                ok = __all_sync(0xFFFFFFFFu, wait(kSFull + w, n_s));
+                ok = warp_wait(kSFull + w, n_s);
                 if (!ok) break;
                 tc_after();
                 const int t0 = (first + n * stride) * kTok;
                 // does every row of the warp see the whole tile?
-                const bool open = __all_sync(0xFFFFFFFFu, lo <= t0 && hi >= t0 + kTok) && !(SCORED && a.sc.tok_doc);
-                // pass 1: the tile's maximum (SCORED: the finished scores go back to tensor memory)
+                const bool open = __all_sync(0xFFFFFFFFu, lo <= t0 && hi >= t0 + kTok) && !doc;
+                // pass 1: the tile's maximum.  A cap alone keeps the order, so the raw products do; with a bias the finished
+                // scores are compared, and kept if capping them again would cost more than tensor memory
                 float top = -INFINITY;
 #pragma unroll 1
                 for (int c = 0; c < 4; ++c) {
                     uint32_t r[32];
                     tmem_ld32(ts + 32 * c, r);
                     tmem_wait_ld();
-                    if constexpr (SCORED) {
+                    if constexpr (BIAS) {
                         const float far = (float)(t0 + 32 * c - (hi - 1));
+                        if constexpr (CAP) cap_scores(r, a.cap_in, a.cap_log2);
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
-                            float x = __uint_as_float(r[i]);
-                            x = a.sc.softcap > 0.f ? a.cap_log2 * tanh_f32(x * a.cap_in) : x * a.scale_log2;
+                            const float x = CAP ? __uint_as_float(r[i]) : __uint_as_float(r[i]) * a.scale_log2;
                             r[i] = __float_as_uint(fmaf(slope2, far + (float)i, x));
                         }
-                        if (!open) {
-                            const int32_t* doc = a.sc.tok_doc ? a.sc.tok_doc + (size_t)s.g * a.T : nullptr;
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                const int t = t0 + 32 * c + i;
-                                bool see = t >= lo && t < hi;
-                                if (see && doc) { const int d = __ldg(doc + t); see = d < 0 || d == my_doc; }
-                                if (!see) r[i] = __float_as_uint(-INFINITY);
-                            }
-                        }
-                        tmem_st32(ts + 32 * c, r);
-                    } else if (!open) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (t0 + 32 * c + i >= hi) r[i] = __float_as_uint(-INFINITY);
                     }
+                    if (!open) hide(r, t0 + 32 * c);
+                    if constexpr (CAP && BIAS) tmem_st32(ts + 32 * c, r);
                     float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                     for (int i = 0; i < 32; ++i) t4[i & 3] = fmaxf(t4[i & 3], __uint_as_float(r[i]));
                     top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
                 }
-                if constexpr (SCORED) tmem_wait_st();
-                const float mul = SCORED ? 1.f : a.scale_log2;
-                if constexpr (!SCORED) top *= mul;                    // sm_scale > 0 (others go the scored way)
+                if constexpr (CAP && BIAS) tmem_wait_st();
+                if constexpr (!BIAS)
+                    if (top > -INFINITY) top = CAP ? a.cap_log2 * tanh_f32(top * a.cap_in) : top * a.scale_log2;
                 // move the maximum only if it is exceeded by much; the accumulator follows
                 const bool move = top > m + kSlack || (m == -INFINITY && top > -INFINITY);
                 if (__any_sync(0xFFFFFFFFu, move)) {
@@ -447,16 +474,22 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     uint32_t r[32];
                     tmem_ld32(ts + 32 * c, r);
                     tmem_wait_ld();
-                    if (!SCORED && !open) {
+                    if constexpr (CAP && !BIAS) cap_scores(r, a.cap_in, a.cap_log2);
+                    const float far = (float)(t0 + 32 * c - (hi - 1));
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (t0 + 32 * c + i >= hi) r[i] = __float_as_uint(-INFINITY);
+                    for (int i = 0; i < 32; ++i) {
+                        const float x = __uint_as_float(r[i]);
+                        float y;
+                        if constexpr (CAP) y = x - ref;
+                        else if constexpr (BIAS) y = fmaf(x, a.scale_log2, fmaf(slope2, far + (float)i, -ref));
+                        else y = fmaf(x, a.scale_log2, -ref);
+                        r[i] = __float_as_uint(y);
                     }
+                    if (!(CAP && BIAS) && !open) hide(r, t0 + 32 * c);
                     uint32_t o[32];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const float p0 = ex2(fmaf(__uint_as_float(r[2 * i]), mul, -ref));
-                        const float p1 = ex2(fmaf(__uint_as_float(r[2 * i + 1]), mul, -ref));
+                        const float p0 = ex2(__uint_as_float(r[2 * i])), p1 = ex2(__uint_as_float(r[2 * i + 1]));
                         l4[(2 * i) & 3] += p0;
                         l4[(2 * i + 1) & 3] += p1;
                         const __nv_bfloat162 h2 = __floats2bfloat162_rn(p0, p1);
@@ -475,7 +508,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (!ok) break;
             // ---- end of the segment -----------------------------------------------------------------------
             if (mine > 0) {
-                ok = __all_sync(0xFFFFFFFFu, wait(kOFull + w, n_s - 1));
+                ok = warp_wait(kOFull + w, n_s - 1);
                 if (!ok) break;
                 tc_after();
             }
@@ -487,7 +520,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 ml[w * kRows + row] = make_float2(m, l);
                 tc_before();
                 mbar_arrive(bar(kXchg));
-                ok = __all_sync(0xFFFFFFFFu, wait(kXchg, n_x++));
+                ok = warp_wait(kXchg, n_x++);
                 if (!ok) break;
                 tc_after();
                 const float2 a0 = ml[row], a1 = ml[kRows + row];
@@ -506,7 +539,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const float* own = nullptr;
             float* dst;
             if (s.slot < 0) {
-                const Join j = join(mo, lo_sum, SCORED ? bias_shift(a, s.len, seq, head) : 0.f, a.own_lse != nullptr,
+                const Join j = join(mo, lo_sum, BIAS ? bias_shift(a, s.len, seq, head) : 0.f, a.own_lse != nullptr,
                                     a.own_lse ? a.own_lse[out_row] : 0.f);
                 fo = j.fo;
                 fown = j.fown;
@@ -547,7 +580,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (!two) {                              // the other group's accumulator and the exchange are free again
                 tc_before();
                 mbar_arrive(bar(kXchg));
-                ok = __all_sync(0xFFFFFFFFu, wait(kXchg, n_x++));
+                ok = warp_wait(kXchg, n_x++);
                 tc_after();
             }
         }
@@ -586,7 +619,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 const int st = vc % kVStages;
                 if (vc >= kVStages) {
-                    ok = __all_sync(0xFFFFFFFFu, wait(kVEmpty + st, (uint32_t)(vc / kVStages - 1)));
+                    ok = warp_wait(kVEmpty + st, (uint32_t)(vc / kVStages - 1));
                     if (!ok) break;
                 }
                 const uint32_t dst = base + kOffV + st * kTile + (uint32_t)(oct >> 3) * kHalf;
@@ -614,7 +647,6 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
 // Joins the partials of units that more than one CTA worked on, and answers the rows whose prefix is empty.
 // One warp per (row, query head), a lane four channels; partials in CTA order.
-template <bool SCORED>
 __global__ void __launch_bounds__(256)
 prefix_merge_kernel(const PrefixArgs a, int n_cta) {
     const long long task = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -658,7 +690,7 @@ prefix_merge_kernel(const PrefixArgs a, int n_cta) {
         }
     }
     const size_t out_row = (size_t)seq * a.Hq + head;
-    const Join j = join(m, l, SCORED ? bias_shift(a, grp.len, seq, head) : 0.f, a.own_lse != nullptr,
+    const Join j = join(m, l, bias_shift(a, grp.len, seq, head), a.own_lse != nullptr,
                         a.own_lse ? a.own_lse[out_row] : 0.f);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (j.fo != 0.f) v = make_float4(o.x * j.fo, o.y * j.fo, o.z * j.fo, o.w * j.fo);
@@ -741,18 +773,20 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
     }
     e = cudaMemsetAsync(a.status, 0, 4, st);
     if (e != cudaSuccess) return e;
-    // a scale that is not positive does not keep the order of the raw products: the scored kernel looks at finished scores
-    const bool scored = score != nullptr || !(sm_scale > 0.f);
-#define STC_PREFIX_LAUNCH(S_, SC_)                                                                               \
+    const bool cap = a.sc.softcap > 0.f, bias = a.sc.slopes || !(sm_scale > 0.f);
+#define STC_PREFIX_LAUNCH(S_, C_, B_)                                                                            \
     do {                                                                                                         \
-        e = cudaFuncSetAttribute(prefix_attn_kernel<S_, SC_>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem); \
+        e = cudaFuncSetAttribute(prefix_attn_kernel<S_, C_, B_>, cudaFuncAttributeMaxDynamicSharedMemorySize,    \
+                                 (int)kSmem);                                                                    \
         if (e != cudaSuccess) return e;                                                                          \
-        prefix_attn_kernel<S_, SC_><<<n_cta, kThreads, kSmem, st>>>(map_q, map_k, a);                            \
+        prefix_attn_kernel<S_, C_, B_><<<n_cta, kThreads, kSmem, st>>>(map_q, map_k, a);                         \
     } while (0)
 #define STC_PREFIX(S_)                                                                                           \
     case S_:                                                                                                     \
-        if (scored) STC_PREFIX_LAUNCH(S_, true);                                                                 \
-        else STC_PREFIX_LAUNCH(S_, false);                                                                       \
+        if (cap && bias) STC_PREFIX_LAUNCH(S_, true, true);                                                      \
+        else if (cap) STC_PREFIX_LAUNCH(S_, true, false);                                                        \
+        else if (bias) STC_PREFIX_LAUNCH(S_, false, true);                                                       \
+        else STC_PREFIX_LAUNCH(S_, false, false);                                                                \
         break;
     switch (g.S) {
         STC_PREFIX(4) STC_PREFIX(8) STC_PREFIX(16)
@@ -764,8 +798,7 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
     if (e != cudaSuccess) return e;
     const long long tasks = (long long)n_rows * g.Hq;
     const unsigned grid = (unsigned)((tasks + 7) / 8);
-    if (scored) prefix_merge_kernel<true><<<grid, 256, 0, st>>>(a, n_cta);
-    else prefix_merge_kernel<false><<<grid, 256, 0, st>>>(a, n_cta);
+    prefix_merge_kernel<<<grid, 256, 0, st>>>(a, n_cta);
     return cudaGetLastError();
 }
 
