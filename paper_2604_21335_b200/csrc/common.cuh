@@ -142,13 +142,15 @@ __device__ __forceinline__ uint32_t bmax2(uint32_t a, uint32_t b) {
 // absolute error of about 1.5e-7 is small against tanh >= 0.5.  The hardware tanh (error 2^-11) would
 // move a score capped at 50 by 0.02.
 constexpr float kTanhSmall = 0.55f;
+constexpr float kTanh0 = -0.33333316445350647f, kTanh1 = 0.13332580029964447f, kTanh2 = -0.053851865231990814f,
+                kTanh3 = 0.02107025310397148f, kTanh4 = -0.006272607482969761f;
 __device__ __forceinline__ float tanh_small(float z) {
     const float u = z * z;
-    float p = -0.006272607482969761f;
-    p = fmaf(p, u, 0.02107025310397148f);
-    p = fmaf(p, u, -0.053851865231990814f);
-    p = fmaf(p, u, 0.13332580029964447f);
-    p = fmaf(p, u, -0.33333316445350647f);
+    float p = kTanh4;
+    p = fmaf(p, u, kTanh3);
+    p = fmaf(p, u, kTanh2);
+    p = fmaf(p, u, kTanh1);
+    p = fmaf(p, u, kTanh0);
     return fmaf(z * u, p, z);
 }
 __device__ __forceinline__ float tanh_large(float z) {

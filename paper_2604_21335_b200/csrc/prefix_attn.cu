@@ -25,8 +25,8 @@
 // accumulator) which a second small kernel joins in CTA order: no atomics, bitwise repeatable.
 //
 // Roles (16 warps): warp 0 = TMA producer of Q and K; warp 1 = MMA issuer; warps 4..7 and 8..11 = two softmax
-// groups, thread = row; warps 12..15 rebuild the value tiles, thread = 16-byte chunks, straight from global
-// memory into the swizzled tile (16 loads in flight per thread).  Two row tiles: group w owns row tile w and
+// groups, thread = row; warps 12..15 rebuild the value tiles with 16-byte
+// asynchronous copies straight from the packed store into the swizzled tile.  Two row tiles: group w owns row tile w and
 // both see every token tile.  One row tile: the groups take the token tiles in turn, each with its own running
 // maximum, sum and accumulator, joined at the end of the segment: the products of one overlap the softmax of the
 // other in both modes.
@@ -44,10 +44,13 @@ namespace {
 constexpr int kRows = 128;                        // rows per tile = tensor-memory lanes
 constexpr int kTok = 128;                         // tokens per tile
 constexpr int kThreads = 512;
-constexpr int kKStages = 3, kVStages = 2;
+constexpr int kKStages = 3;                       // key tiles of 128 tokens
+constexpr int kVStages = 4;                       // value tiles of 64 tokens: finer, so that more of the ring is in flight
+constexpr int kVTok = 64;
 constexpr uint32_t kHalf = kRows * 128;           // 64 columns of a tile: 128 rows of 128 bytes
 constexpr uint32_t kTile = 2 * kHalf;             // 32 KiB
-constexpr uint32_t kOffK = 2 * kTile, kOffV = kOffK + kKStages * kTile, kOffCtl = kOffV + kVStages * kTile;
+constexpr uint32_t kVHalf = kVTok * 128, kVTile = 2 * kVHalf;
+constexpr uint32_t kOffK = 2 * kTile, kOffV = kOffK + kKStages * kTile, kOffCtl = kOffV + kVStages * kVTile;
 constexpr uint32_t kCtlBytes = 512 + 2 * kRows * 8;
 constexpr uint32_t kSmem = kOffCtl + kCtlBytes;
 static_assert(kSmem <= 232448, "shared memory of a block");
@@ -162,22 +165,29 @@ __device__ __forceinline__ float bias_shift(const PrefixArgs& a, int len, int se
     return a.sc.slopes[head] * (float)(hi - 1 - pos);
 }
 
-// Caps 32 scores of a row (raw products in, log2 units out).  Scores far below the cap, the usual case, need only the
-// polynomial of tanh_f32; the warp votes once per 32 instead of branching per score.
-__device__ __forceinline__ void cap_scores(uint32_t (&r)[32], float cap_in, float cap_log2) {
+// Caps 16 scores of a row (raw products in, log2 units out).  Scores far below the cap, the usual case, need only the
+// polynomial of tanh_f32; the warp votes once per 16 instead of branching per score.
+__device__ __forceinline__ void cap_scores(uint32_t (&r)[16], float cap_in, float cap_log2) {
     float big = 0.f;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) big = fmaxf(big, fabsf(__uint_as_float(r[i])));
-    if (__all_sync(0xFFFFFFFFu, big * fabsf(cap_in) <= kTanhSmall)) {
+    for (int i = 0; i < 16; ++i) big = fmaxf(big, fabsf(__uint_as_float(r[i])));
+    const bool small = __all_sync(0xFFFFFFFFu, big * fabsf(cap_in) <= kTanhSmall);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(cap_log2 * tanh_small(__uint_as_float(r[i]) * cap_in));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const float z = __uint_as_float(r[i]) * cap_in;
-            const float lo = tanh_small(z), hi = tanh_large(z);
-            r[i] = __float_as_uint(cap_log2 * (fabsf(z) <= kTanhSmall ? lo : hi));
+    for (int i = 0; i < 16; i += 2) {                // tanh_small, two at a time
+        const float2 z = mul2(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), both(cap_in));
+        const float2 u = mul2(z, z);
+        float2 p = fma2(both(kTanh4), u, both(kTanh3));
+        p = fma2(p, u, both(kTanh2));
+        p = fma2(p, u, both(kTanh1));
+        p = fma2(p, u, both(kTanh0));
+        const float2 t = fma2(mul2(z, u), p, z);
+        float2 y = mul2(t, both(cap_log2));
+        if (!small) {                                // uniform
+            if (fabsf(z.x) > kTanhSmall) y.x = cap_log2 * tanh_large(z.x);
+            if (fabsf(z.y) > kTanhSmall) y.y = cap_log2 * tanh_large(z.y);
         }
+        r[i] = __float_as_uint(y.x);
+        r[i + 1] = __float_as_uint(y.y);
     }
 }
 
@@ -203,7 +213,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         mbar_init(bars + 8 * kQFull, 1);
         mbar_init(bars + 8 * kQEmpty, 1);
         for (int i = 0; i < kKStages; ++i) { mbar_init(bars + 8 * (kKFull + i), 1); mbar_init(bars + 8 * (kKEmpty + i), 1); }
-        for (int i = 0; i < kVStages; ++i) { mbar_init(bars + 8 * (kVFull + i), 4); mbar_init(bars + 8 * (kVEmpty + i), 1); }
+        for (int i = 0; i < kVStages; ++i) { mbar_init(bars + 8 * (kVFull + i), 2); mbar_init(bars + 8 * (kVEmpty + i), 1); }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bars + 8 * (kSFull + i), 1);
             mbar_init(bars + 8 * (kPFull + i), kRows);
@@ -317,65 +327,77 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
         }
     } else if (warp == 1) {
-        // ---- MMA issuer --------------------------------------------------------------------------------
+        // ---- MMA issuer ----------------------------------------------------------------------------------
+        // (loops are kept rolled here and in the other roles: the roles of an SM partition share its small first-level
+        // instruction cache, and unrolled they evict each other; the issuer then took 3200 cycles per step)
         if (lane == 0) {
             constexpr uint32_t id_qk = idesc_bf16(kRows, kTok, false), id_pv = idesc_bf16(kRows, kHeadDim, true);
             int kc0 = 0, seg = 0;                    // tiles of the segments before; segments before
-            uint32_t n_s[2] = {0u, 0u};              // S tiles issued per group (= P consumed + at most one)
-            uint32_t n_o[2] = {0u, 0u};
+            uint32_t n_o0 = 0, n_o1 = 0;             // P tiles consumed per group
             bool ok = true;
             while (ok && walk.next(a, s)) {
                 const int tiles = s.tile1 - s.tile0;
                 const bool two = s.n_seq > a.seqs;   // two row tiles: every token tile goes to both groups
                 const int steps = two ? 2 * tiles : tiles;
-                if (!wait(kQFull, (uint32_t)seg)) { give_up(); break; }
-                tc_after();
-                const uint32_t seg_o[2] = {n_o[0], n_o[1]};
-                auto qk = [&](int i) -> bool {
-                    const int w = i & 1, j = kc0 + (two ? i >> 1 : i), st = j % kKStages;
-                    if ((!two || w == 0) && !wait(kKFull + st, (uint32_t)(j / kKStages))) return false;
-                    // S and P share their columns: the product that read the group's last P has to be through
-                    if (n_o[w] > 0 && !wait(kOFull + w, n_o[w] - 1)) return false;
-                    tc_after();
-                    const uint64_t dq = smem_desc_128(base + (two ? w * kTile : 0u), 16);
-                    const uint64_t dk = smem_desc_128(base + kOffK + st * kTile, 16);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {    // 16 dims = 32 bytes = 2 units; 64 dims = one half tile
-                        const uint64_t step = (uint64_t)((k >> 2) * (kHalf >> 4) + (k & 3) * 2);
-                        tc_mma_ss(tmem + w * 128, dq + step, dk + step, id_qk, k != 0);
+                if (!wait(kQFull, (uint32_t)seg)) { ok = false; break; }
+                // step i belongs to group w = i & 1; it is S = Q K^T now, and O += P V two iterations on
+#pragma unroll 1
+                for (int n = 0; n < steps + 2; ++n) {
+                    const int w = n & 1;
+                    const uint32_t n_o = w ? n_o1 : n_o0;
+                    const uint32_t ts = tmem + (uint32_t)w * 128u;
+                    if (n >= 2) {                    // O += P V of step n - 2
+                        const int j = kc0 + (two ? (n - 2) >> 1 : n - 2);
+                        ok = wait(kPFull + w, n_o);
+                        uint32_t acc = n >= 4;       // the group's first product of a segment starts O anew
+#pragma unroll 1
+                        for (int jv = 2 * j; ok && jv < 2 * j + 2; ++jv) {   // two value tiles of 64 tokens
+                            const int st = jv % kVStages;
+                            if (!two || w == 0) ok = wait(kVFull + st, (uint32_t)(jv / kVStages));
+                            tc_after();
+                            uint64_t dv = smem_desc_128(base + kOffV + st * kVTile, kVHalf);
+                            uint32_t pk = ts + 64u * (jv & 1);
+#pragma unroll 1
+                            for (int k = 0; k < 4; ++k) {    // 16 tokens: 16 rows of 128 bytes; P: 8 columns high, 8 residual
+                                tc_mma_ts(ts + 256, pk, dv, id_pv, acc);
+                                tc_mma_ts(ts + 256, pk + 8, dv, id_pv, 1);
+                                acc = 1;
+                                pk += 16;
+                                dv += 2048 >> 4;
+                            }
+                            if (!two || w == 1) tc_commit_to(bar(kVEmpty + st));
+                        }
+                        if (!ok) break;
+                        tc_commit_to(bar(kOFull + w));
+                        if (w) ++n_o1; else ++n_o0;
                     }
-                    tc_commit_to(bar(kSFull + w));
-                    if (!two || w == 1) tc_commit_to(bar(kKEmpty + st));
-                    if (i == steps - 1) tc_commit_to(bar(kQEmpty));
-                    ++n_s[w];
-                    return true;
-                };
-                auto pv = [&](int i) -> bool {
-                    const int w = i & 1, j = kc0 + (two ? i >> 1 : i), st = j % kVStages;
-                    if ((!two || w == 0) && !wait(kVFull + st, (uint32_t)(j / kVStages))) return false;
-                    if (!wait(kPFull + w, n_o[w])) return false;
-                    tc_after();
-                    const uint64_t dv = smem_desc_128(base + kOffV + st * kTile, kHalf);
-                    const uint32_t p = tmem + w * 128, o = tmem + 256 + w * 128;
-                    const bool fresh = n_o[w] == seg_o[w];
+                    if (n < steps) {                 // S = Q K^T of step n
+                        const int j = kc0 + (two ? n >> 1 : n), st = j % kKStages;
+                        if (!two || w == 0) ok = wait(kKFull + st, (uint32_t)(j / kKStages));
+                        // S and P share their columns: the product that read the group's last P has to be through
+                        const uint32_t done = w ? n_o1 : n_o0;
+                        if (ok && done > 0) ok = wait(kOFull + w, done - 1);
+                        if (!ok) break;
+                        tc_after();
+                        uint64_t dq = smem_desc_128(base + (two ? w * kTile : 0u), 16);
+                        uint64_t dk = smem_desc_128(base + kOffK + st * kTile, 16);
+#pragma unroll 1
+                        for (int k = 0; k < 2; ++k) {        // 64 dims: one half tile
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {    // 16 tokens = 16 rows of 128 bytes; P: 8 columns high, 8 residual
-                        const uint32_t pk = p + 32 * (k >> 1) + 8 * (k & 1);
-                        const uint64_t dvk = dv + (uint64_t)(k * (2048 >> 4));
-                        tc_mma_ts(o, pk, dvk, id_pv, !(fresh && k == 0));
-                        tc_mma_ts(o, pk + 16, dvk, id_pv, 1);
+                            for (int e = 0; e < 4; ++e)      // 16 dims: 32 bytes, 2 units
+                                tc_mma_ss(ts, dq + 2 * e, dk + 2 * e, id_qk, k + e != 0);
+                            dq += kHalf >> 4;
+                            dk += kHalf >> 4;
+                        }
+                        tc_commit_to(bar(kSFull + w));
+                        if (!two || w == 1) tc_commit_to(bar(kKEmpty + st));
+                        if (n == steps - 1) tc_commit_to(bar(kQEmpty));
                     }
-                    tc_commit_to(bar(kOFull + w));
-                    if (!two || w == 1) tc_commit_to(bar(kVEmpty + st));
-                    ++n_o[w];
-                    return true;
-                };
-                ok = qk(0) && (steps < 2 || qk(1));
-                for (int i = 0; ok && i < steps; ++i) ok = pv(i) && (i + 2 >= steps || qk(i + 2));
-                if (!ok) give_up();
+                }
                 kc0 += tiles;
                 ++seg;
             }
+            if (!ok) give_up();
         }
     } else if (warp >= 4 && warp < 12) {
         // ---- softmax: thread = row -----------------------------------------------------------------------
@@ -398,14 +420,14 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (BIAS && a.sc.slopes) slope2 = a.sc.slopes[head] * kLog2e;
             const int32_t* doc = a.sc.tok_doc ? a.sc.tok_doc + (size_t)s.g * a.T : nullptr;
             if (doc) my_doc = a.sc.q_doc[seq];
-            // -inf for the tokens t .. t + 31 that the row does not see
-            auto hide = [&](uint32_t (&r)[32], int t) {
+            // -inf for the tokens t .. t + 15 that the row does not see
+            auto hide = [&](uint32_t (&r)[16], int t) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
+                for (int i = 0; i < 16; ++i)
                     if (t + i < lo || t + i >= hi) r[i] = __float_as_uint(-INFINITY);
                 if (doc) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
+                    for (int i = 0; i < 16; ++i) {
                         const int d = __ldg(doc + min(t + i, a.T - 1));
                         if (d >= 0 && d != my_doc) r[i] = __float_as_uint(-INFINITY);
                     }
@@ -423,25 +445,26 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 // scores are compared, and kept if capping them again would cost more than tensor memory
                 float top = -INFINITY;
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t r[32];
-                    tmem_ld32(ts + 32 * c, r);
+                for (int c = 0; c < kTok; c += 16) {
+                    uint32_t r[16];
+                    tmem_ld16(ts + c, r);
                     tmem_wait_ld();
                     if constexpr (BIAS) {
-                        const float far = (float)(t0 + 32 * c - (hi - 1));
+                        const float far = (float)(t0 + c - (hi - 1));
                         if constexpr (CAP) cap_scores(r, a.cap_in, a.cap_log2);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
+                        for (int i = 0; i < 16; ++i) {
                             const float x = CAP ? __uint_as_float(r[i]) : __uint_as_float(r[i]) * a.scale_log2;
                             r[i] = __float_as_uint(fmaf(slope2, far + (float)i, x));
                         }
                     }
-                    if (!open) hide(r, t0 + 32 * c);
-                    if constexpr (CAP && BIAS) tmem_st32(ts + 32 * c, r);
-                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    if (!open) hide(r, t0 + c);
+                    if constexpr (CAP && BIAS) tmem_st16(ts + c, r);
+                    float t2[2] = {top, -INFINITY};
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) t4[i & 3] = fmaxf(t4[i & 3], __uint_as_float(r[i]));
-                    top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
+                    for (int i = 0; i < 16; i += 2)
+                        t2[(i >> 1) & 1] = fmaxf(fmaxf(t2[(i >> 1) & 1], __uint_as_float(r[i])), __uint_as_float(r[i + 1]));
+                    top = fmaxf(t2[0], t2[1]);
                 }
                 if constexpr (CAP && BIAS) tmem_wait_st();
                 if constexpr (!BIAS)
@@ -454,52 +477,54 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     l *= f;
                     if (n > 0) {
 #pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            uint32_t r[32];
-                            tmem_ld32(to + 32 * c, r);
+                        for (int c = 0; c < kHeadDim; c += 16) {
+                            uint32_t r[16];
+                            tmem_ld16(to + c, r);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i)
+                            for (int i = 0; i < 16; ++i)
                                 r[i] = move ? __float_as_uint(__uint_as_float(r[i]) * f) : r[i];
-                            tmem_st32(to + 32 * c, r);
+                            tmem_st16(to + c, r);
                         }
                     }
                     m = to_m;
                 }
-                // pass 2: weights, their sum, and P over S: 16 columns of bf16 pairs high, 16 residual, per 32 tokens
+                // pass 2: weights, their sum, and P over S: per 16 tokens 8 columns of bf16 pairs high, 8 residual
                 const float ref = m == -INFINITY ? 0.f : m;
-                float l4[4] = {0.f, 0.f, 0.f, 0.f};
+                float2 la = make_float2(0.f, 0.f), lb = la;
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t r[32];
-                    tmem_ld32(ts + 32 * c, r);
+                for (int c = 0; c < kTok; c += 16) {
+                    uint32_t r[16];
+                    tmem_ld16(ts + c, r);
                     tmem_wait_ld();
                     if constexpr (CAP && !BIAS) cap_scores(r, a.cap_in, a.cap_log2);
-                    const float far = (float)(t0 + 32 * c - (hi - 1));
+                    const float far = (float)(t0 + c - (hi - 1));
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const float x = __uint_as_float(r[i]);
-                        float y;
-                        if constexpr (CAP) y = x - ref;
-                        else if constexpr (BIAS) y = fmaf(x, a.scale_log2, fmaf(slope2, far + (float)i, -ref));
-                        else y = fmaf(x, a.scale_log2, -ref);
-                        r[i] = __float_as_uint(y);
+                    for (int i = 0; i < 16; i += 2) {
+                        const float2 x = make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+                        float2 y;
+                        if constexpr (CAP) y = add2(x, both(-ref));
+                        else if constexpr (BIAS)
+                            y = fma2(x, both(a.scale_log2), fma2(both(slope2), make_float2(far + (float)i, far + (float)(i + 1)), both(-ref)));
+                        else y = fma2(x, both(a.scale_log2), both(-ref));
+                        r[i] = __float_as_uint(y.x);
+                        r[i + 1] = __float_as_uint(y.y);
                     }
-                    if (!(CAP && BIAS) && !open) hide(r, t0 + 32 * c);
-                    uint32_t o[32];
+                    if (!(CAP && BIAS) && !open) hide(r, t0 + c);
+                    uint32_t o[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float p0 = ex2(__uint_as_float(r[2 * i])), p1 = ex2(__uint_as_float(r[2 * i + 1]));
-                        l4[(2 * i) & 3] += p0;
-                        l4[(2 * i + 1) & 3] += p1;
-                        const __nv_bfloat162 h2 = __floats2bfloat162_rn(p0, p1);
+                    for (int i = 0; i < 8; ++i) {
+                        const float2 p = make_float2(ex2(__uint_as_float(r[2 * i])), ex2(__uint_as_float(r[2 * i + 1])));
+                        if (i & 1) lb = add2(lb, p); else la = add2(la, p);
+                        const __nv_bfloat162 h2 = __floats2bfloat162_rn(p.x, p.y);
                         o[i] = *reinterpret_cast<const uint32_t*>(&h2);
-                        const __nv_bfloat162 r2 = __floats2bfloat162_rn(p0 - bf16lo(o[i]), p1 - bf16hi(o[i]));
-                        o[16 + i] = *reinterpret_cast<const uint32_t*>(&r2);
+                        const float2 d = fma2(make_float2(bf16lo(o[i]), bf16hi(o[i])), both(-1.f), p);
+                        const __nv_bfloat162 r2 = __floats2bfloat162_rn(d.x, d.y);
+                        o[8 + i] = *reinterpret_cast<const uint32_t*>(&r2);
                     }
-                    tmem_st32(ts + 32 * c, o);
+                    tmem_st16(ts + c, o);
                 }
-                l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+                l += (la.x + lb.x) + (la.y + lb.y);
                 tmem_wait_st();
                 tc_before();
                 mbar_arrive(bar(kPFull + w));
@@ -513,8 +538,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 tc_after();
             }
             float mo = m, lo_sum = l, f0 = 1.f, f1 = 0.f;   // joined maximum and sum; factors of accumulator 0 / 1
-            bool has0 = true, has1 = false;
-            int c_lo = 0, c_hi = 4;                          // 32-column chunks this thread writes
+            bool has1 = false;
+            int c_lo = 0, c_hi = kHeadDim;                   // dims this thread writes
             uint32_t acc0 = to, acc1 = to;
             if (!two) {                              // both groups hold part of the same rows: join, half the dims each
                 ml[w * kRows + row] = make_float2(m, l);
@@ -531,8 +556,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 has1 = tiles > 1;
                 acc0 = lane_base + 256;
                 acc1 = lane_base + 384;
-                c_lo = 2 * w;
-                c_hi = c_lo + 2;
+                c_lo = 64 * w;
+                c_hi = c_lo + 64;
             }
             const size_t out_row = (size_t)seq * a.Hq + head;
             float fo = 1.f, fown = 0.f;
@@ -552,14 +577,14 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if (live && c_lo == 0) a.part_ml[slot] = make_float2(mo, lo_sum);
             }
 #pragma unroll 1
-            for (int c = c_lo; c < c_hi; ++c) {
-                uint32_t r0[32], r1[32];
-                if (has0) tmem_ld32(acc0 + 32 * c, r0);
-                if (has1) tmem_ld32(acc1 + 32 * c, r1);
+            for (int c = c_lo; c < c_hi; c += 16) {
+                uint32_t r0[16], r1[16];
+                tmem_ld16(acc0 + c, r0);
+                if (has1) tmem_ld16(acc1 + c, r1);
                 tmem_wait_ld();
                 if (live) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
+                    for (int i = 0; i < 16; i += 4) {
                         float v[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
@@ -569,11 +594,11 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         }
                         float4 v4 = make_float4(v[0], v[1], v[2], v[3]);
                         if (own) {
-                            const float4 w4 = *reinterpret_cast<const float4*>(own + 32 * c + i);
+                            const float4 w4 = *reinterpret_cast<const float4*>(own + c + i);
                             v4.x = fmaf(w4.x, fown, v4.x); v4.y = fmaf(w4.y, fown, v4.y);
                             v4.z = fmaf(w4.z, fown, v4.z); v4.w = fmaf(w4.w, fown, v4.w);
                         }
-                        *reinterpret_cast<float4*>(dst + 32 * c + i) = v4;
+                        *reinterpret_cast<float4*>(dst + c + i) = v4;
                     }
                 }
             }
@@ -587,54 +612,69 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         if (!ok) give_up();
     } else if (warp >= 12) {
         // ---- value tiles: packed groups -> swizzled rows ---------------------------------------------------
-        const int wv = warp - 12, oct = lane & 15, grp = oct / OPG, sub = oct % OPG;
+        // Warps 12, 13 build the even tiles of 64 tokens and 14, 15 the odd ones, 32 tokens each.  A lane owns one
+        // 16-byte column of every other token; a kept group is one asynchronous 16-byte copy, a dropped one a
+        // zero-filled copy that reads nothing.  The copies of a warp's next tile are under way before the last
+        // one's are waited for, unless its stage is still being read.
+        const int pair = (warp - 12) >> 1, tok0 = (warp & 1) * 32, oct = lane & 15, grp = oct / OPG, sub = oct % OPG;
         const uint32_t below = (1u << grp) - 1u;
-        int vc = 0;
+        int vc = 0;                                  // tiles of 64 tokens so far, both pairs'
+        int pending = -1;                            // stage whose copies are not waited for yet
         bool ok = true;
+        auto publish = [&]() {                       // this warp's copies into `pending` have landed
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kVFull + pending));
+            pending = -1;
+        };
         while (ok && walk.next(a, s)) {
             const size_t problem = (size_t)s.g * a.Hkv + s.hk;
             const uint16_t* mask_row = a.v_mask + problem * a.T;
             const uint32_t* offs = a.v_offs + problem * (a.T + 1);
             const uint4* packed = a.v_packed + problem * a.cap_groups * OPG;
             const int64_t limit = a.cap_groups;
-            auto fetch = [&](int t0, uint32_t& m, uint32_t& first) {       // this lane's token mask, the warp's first group
-                const int t = t0 + wv * 32;
-                m = t + lane < s.len ? mask_row[t + lane] : 0u;
-                first = t < s.len ? offs[t] : 0u;
+            const int n_half = 2 * (s.tile1 - s.tile0), first_tok = s.tile0 * kTok + tok0;
+            auto fetch = [&](int h, uint32_t& m, uint32_t& first) {        // this lane's token mask, the warp's first group
+                const int t = first_tok + h * kVTok;
+                m = h < n_half && t + lane < s.len ? mask_row[t + lane] : 0u;
+                first = h < n_half && t < s.len ? offs[t] : 0u;
             };
             uint32_t m_next, first_next;
-            fetch(s.tile0 * kTok, m_next, first_next);
-            for (int t = s.tile0; t < s.tile1; ++t, ++vc) {
+            fetch(pair, m_next, first_next);         // a segment is an even number of tiles of 64 tokens
+            for (int h = pair; h < n_half; h += 2) {
                 const uint32_t m = m_next & ((1u << S) - 1u), first = first_next;
-                if (t + 1 < s.tile1) fetch((t + 1) * kTok, m_next, first_next);
+                fetch(h + 2, m_next, first_next);
                 const uint32_t cnt = __popc(m);
                 const uint32_t pre = warp_incl_scan(cnt, lane) - cnt;
-                uint4 v[16];
-#pragma unroll
+                const int j = vc + h, st = j % kVStages;
+                if (j >= kVStages) {
+                    const uint32_t par = (uint32_t)(j / kVStages - 1) & 1u;
+                    int free = 0;
+                    if (lane == 0) free = mbar_try_wait(bar(kVEmpty + st), par);
+                    if (!__shfl_sync(0xFFFFFFFFu, free, 0)) {
+                        if (pending >= 0) { cp_async_wait<0>(); publish(); }
+                        ok = warp_wait(kVEmpty + st, par);
+                        if (!ok) break;
+                    }
+                }
+                const uint32_t dst = base + kOffV + st * kVTile + (uint32_t)(oct >> 3) * kVHalf;
+#pragma unroll 4
                 for (int i = 0; i < 16; ++i) {
                     const int tok = 2 * i + (lane >> 4);
                     const uint32_t mt = __shfl_sync(0xFFFFFFFFu, m, tok), pt = __shfl_sync(0xFFFFFFFFu, pre, tok);
                     const int64_t at = (int64_t)first + pt + __popc(mt & below);
-                    v[i] = ((mt >> grp) & 1u) && at < limit ? ldg_nc16(packed + at * OPG + sub) : make_uint4(0, 0, 0, 0);
+                    const bool kept = ((mt >> grp) & 1u) && at < limit;
+                    cp_async16_zfill(dst + (uint32_t)(tok0 + tok) * 128u + (uint32_t)(((oct & 7) ^ (tok & 7)) * 16),
+                                     kept ? packed + at * OPG + sub : packed, kept ? 16 : 0);
                 }
-                const int st = vc % kVStages;
-                if (vc >= kVStages) {
-                    ok = warp_wait(kVEmpty + st, (uint32_t)(vc / kVStages - 1));
-                    if (!ok) break;
-                }
-                const uint32_t dst = base + kOffV + st * kTile + (uint32_t)(oct >> 3) * kHalf;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int tok = wv * 32 + 2 * i + (lane >> 4);
-                    const uint32_t at = dst + (uint32_t)tok * 128u + (uint32_t)(((oct & 7) ^ (tok & 7)) * 16);
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};"
-                                 ::"r"(at), "r"(v[i].x), "r"(v[i].y), "r"(v[i].z), "r"(v[i].w) : "memory");
-                }
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(kVFull + st));
+                cp_async_commit();
+                if (pending >= 0) { cp_async_wait<1>(); publish(); }
+                pending = st;
             }
+            vc += n_half;
         }
+        cp_async_wait<0>();
+        if (ok && pending >= 0) publish();
         if (!ok) give_up();
     }
     tc_before();
