@@ -6,17 +6,18 @@
 //     out_r = sum_t p_t v~_t   (v~: routed values, dropped groups zero),  lse_r = log sum exp s
 //   optionally joined with (own_out, own_lse) of the sequence's own tokens by their log-sum-exps.
 //
-// Rows of one KV head form tiles of 128, tokens tiles of 128; both products run on the 5th-generation tensor
+// Rows of one KV head form tiles of 128, tokens tiles of 64; both products run on the 5th-generation tensor
 // cores with their accumulators in tensor memory:
-//   S[row][token] = Q . K^T     Q, K tiles by TMA (128-byte swizzle), M = N = 128, K = 128
+//   S[row][token] = Q . K^T     Q, K tiles by TMA (128-byte swizzle), M = 128, N = 64, K = 128
 //   O[row][dim]  += P . V~      P from tensor memory, written over S by the softmax; V~ rebuilt from the packed
 //                               groups in shared memory, token rows of 128 dims = N-major operand
 // P enters as a bf16 high part plus a bf16 residual (two MMAs): the output is fp32, and one bf16 weight alone would
-// leave it 2^-9 off; the pair leaves 2^-17.
+// leave it 2^-9 off; the pair leaves 2^-17.  The tensor core truncates when it adds to an accumulator (measured:
+// 4e-8 of its value per product), so an accumulator is emptied into fp32 sums after kFlush tiles.
 //
-// What bounds it.  Up to 128 rows per KV head the two products of a token tile take 1536 cycles of the tensor pipe
-// and its bytes (K 32 KiB, V up to 32 KiB) 2100 to 2800 cycles of an SM's share of HBM: memory-bound; at 256 rows
-// the pipe needs 3072 cycles and binds, so a work unit is at most two row tiles (one pass over K and V for 256
+// What bounds it.  Up to 128 rows per KV head the two products of 128 tokens take about 1800 cycles of the tensor pipe
+// and their bytes (K 32 KiB, V up to 32 KiB) 2100 to 2800 cycles of an SM's share of HBM: memory-bound; at 256 rows
+// the pipe and the softmax bind, so a work unit is at most two row tiles (one pass over K and V for 256
 // rows) and larger batches take more units, whose K and V come from L2.
 //
 // Work split.  Unit = (prefix, KV head, block of up to two row tiles); the token tiles of all units form one flat
@@ -24,15 +25,18 @@
 // range; a segment that is a whole unit is finished in place, another one leaves a partial (max, sum,
 // accumulator) which a second small kernel joins in CTA order: no atomics, bitwise repeatable.
 //
-// Roles (16 warps): warp 0 = TMA producer of Q and K; warp 1 = MMA issuer; warps 4..7 and 8..11 = two softmax
-// groups, thread = row; warps 12..15 rebuild the value tiles with 16-byte
-// asynchronous copies straight from the packed store into the swizzled tile.  Two row tiles: group w owns row tile w and
-// both see every token tile.  One row tile: the groups take the token tiles in turn, each with its own running
-// maximum, sum and accumulator, joined at the end of the segment: the products of one overlap the softmax of the
-// other in both modes.
+// Roles (16 warps): warp 0 = TMA producer of Q and K; warps 1, 2 = MMA issuers of the two groups; warps 4..7 and
+// 8..11 = softmax of the two groups, thread = row; warps 12..15 rebuild the value tiles with 16-byte asynchronous
+// copies straight from the packed store into the swizzled tile.  Two row tiles: group w owns row tile w and both see
+// every token tile.  One row tile: the groups take the token tiles in turn, each with its own running
+// maximum, sum and accumulator, joined at the end of the segment.  A group has two S buffers: the product for its next
+// tile runs while it works on this one, and its softmax waits for nothing else unless the maximum moves.
 //
 // The running maximum only moves when a tile exceeds it by more than 2^8, so the accumulator in tensor memory is
 // rescaled a few times per segment and not per tile; weights are then at most 2^8, far from fp32's limits.
+//
+// Loops are kept rolled (16 scores at a time): the roles of an SM partition share its small first-level instruction
+// cache and evict each other where they are unrolled.
 //
 // Every wait is bounded (about a second); one that expires raises a CTA-wide flag and STC_ERR_TIMEOUT in the
 // status word, the roles leave, the producer waits (bounded) for its copies, tensor memory is freed.
@@ -42,15 +46,15 @@ namespace stc {
 namespace {
 
 constexpr int kRows = 128;                        // rows per tile = tensor-memory lanes
-constexpr int kTok = 128;                         // tokens per tile
+constexpr int kTok = 64;                          // tokens per tile
 constexpr int kThreads = 512;
-constexpr int kKStages = 3;                       // key tiles of 128 tokens
-constexpr int kVStages = 4;                       // value tiles of 64 tokens: finer, so that more of the ring is in flight
-constexpr int kVTok = 64;
-constexpr uint32_t kHalf = kRows * 128;           // 64 columns of a tile: 128 rows of 128 bytes
-constexpr uint32_t kTile = 2 * kHalf;             // 32 KiB
-constexpr uint32_t kVHalf = kVTok * 128, kVTile = 2 * kVHalf;
-constexpr uint32_t kOffK = 2 * kTile, kOffV = kOffK + kKStages * kTile, kOffCtl = kOffV + kVStages * kVTile;
+constexpr int kKStages = 6, kVStages = 4;
+constexpr int kFlush = 16;                        // tiles an accumulator takes: 128 products, 3e-6 of truncation
+constexpr uint32_t kQHalf = kRows * 128;          // 64 channels of a row tile: 128 rows of 128 bytes
+constexpr uint32_t kQTile = 2 * kQHalf;           // 32 KiB
+constexpr uint32_t kHalf = kTok * 128;            // 64 channels of a token tile
+constexpr uint32_t kTile = 2 * kHalf;             // 16 KiB
+constexpr uint32_t kOffK = 2 * kQTile, kOffV = kOffK + kKStages * kTile, kOffCtl = kOffV + kVStages * kTile;
 constexpr uint32_t kCtlBytes = 512 + 2 * kRows * 8;
 constexpr uint32_t kSmem = kOffCtl + kCtlBytes;
 static_assert(kSmem <= 232448, "shared memory of a block");
@@ -58,10 +62,12 @@ constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;                     // log2 units the maximum may be exceeded by
 
-// barriers, in 8-byte words of the control block
-enum { kQFull, kQEmpty, kKFull, kKEmpty = kKFull + kKStages, kVFull = kKEmpty + kKStages, kVEmpty = kVFull + kVStages,
-       kSFull = kVEmpty + kVStages, kPFull = kSFull + 2, kOFull = kPFull + 2, kXchg = kOFull + 2, kBars };
-static_assert(kBars * 8 <= 256, "control block");
+// barriers, in 8-byte words of the control block; [2] = per group, empties [stage][group]
+enum { kQFull, kQEmpty, kKFull = kQEmpty + 2, kKEmpty = kKFull + kKStages, kVFull = kKEmpty + 2 * kKStages,
+       kVEmpty = kVFull + kVStages, kSFull = kVEmpty + 2 * kVStages, kPFull = kSFull + 4, kOFull = kPFull + 4,
+       kXchg = kOFull + 2, kBars };
+static_assert(kBars * 8 <= 448, "control block");
+constexpr uint32_t kCtlTmem = 448, kCtlAbort = 452, kCtlPlan = 456;    // tensor-memory address, abort flag, 4 x 8 bytes
 
 struct PrefixArgs {
     const int32_t* row_start;    // [G + 1]
@@ -73,10 +79,12 @@ struct PrefixArgs {
     const float* own_lse;
     float* out;
     float* lse;                  // or nullptr
-    int32_t* status;
+    int32_t* cta_status;         // [grid], one word per CTA
+    int32_t* status;             // the call's status word, written by the second kernel
     long long* base;             // [G + 2]: first flat tile of each prefix; [G] = total; [G + 1] = 1 if row_start is bad
-    float* part_o;               // [2 * grid][slot_rows][128]
+    float4* part_o;              // [2 * grid][32 chunks of 4 dims][slot_rows]
     float2* part_ml;             // [2 * grid][slot_rows]
+    float4* flush;               // [grid][2 groups][32][128 rows]: sums of emptied accumulators
     int64_t cap_groups;
     int G, Hq, Hkv, Gq, T, n_rows, slot_rows;
     int seqs;                    // sequences per row tile = 128 / Gq
@@ -202,35 +210,25 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const uint32_t base = smem_u32(smem);
     const uint32_t bars = base + kOffCtl;
     unsigned char* ctl = smem + kOffCtl;
-    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctl + 256);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + 260);
-    volatile long long* plan = reinterpret_cast<volatile long long*>(ctl + 272);      // x, x_end, off, g
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctl + kCtlTmem);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + kCtlAbort);
+    volatile long long* plan = reinterpret_cast<volatile long long*>(ctl + kCtlPlan);  // x, x_end, off, g
     float2* ml = reinterpret_cast<float2*>(ctl + 512);                                // [2][128]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     // ---- set-up: barriers, tensor memory, this CTA's range ------------------------------------------
     if (threadIdx.x == 0) {
-        mbar_init(bars + 8 * kQFull, 1);
-        mbar_init(bars + 8 * kQEmpty, 1);
-        for (int i = 0; i < kKStages; ++i) { mbar_init(bars + 8 * (kKFull + i), 1); mbar_init(bars + 8 * (kKEmpty + i), 1); }
-        for (int i = 0; i < kVStages; ++i) { mbar_init(bars + 8 * (kVFull + i), 2); mbar_init(bars + 8 * (kVEmpty + i), 1); }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(bars + 8 * (kSFull + i), 1);
-            mbar_init(bars + 8 * (kPFull + i), kRows);
-            mbar_init(bars + 8 * (kOFull + i), 1);
-        }
-        mbar_init(bars + 8 * kXchg, 2 * kRows);
-        *abort_flag = (base & 1023u) != 0;           // swizzled tiles need 1024-byte aligned bases
-        if (base & 1023u) atomicExch(a.status, (int)STC_ERR_CUDA);
+        for (int i = 0; i < kBars; ++i)
+            mbar_init(bars + 8 * i, i >= kPFull && i < kOFull ? kRows : i == kXchg ? 2 * kRows : i >= kVFull && i < kVEmpty ? 2 : 1);
+        *abort_flag = (base & 1023u) != 0 ? (int)STC_ERR_CUDA : 0;      // swizzled tiles need 1024-byte aligned bases
         fence_mbar_init();
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     ::"r"(bars + 256), "r"(512u) : "memory");
+                     ::"r"(bars + kCtlTmem), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    if (warp == 2) {                                 // flat tile sequence: prefix sums over the prefixes, 32 at a time
-        long long total = 0;
+    if (warp == 3) {                                 // flat tile sequence: prefix sums over the prefixes, 32 at a time
         bool bad = false;
         auto scan = [&](auto&& use) {
             long long run = 0;
@@ -253,25 +251,26 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
             return run;
         };
-        total = scan([&](int g, long long lo, long long) {
+        long long total = scan([&](int g, long long lo, long long) {
             if (blockIdx.x == 0 && g < a.G) a.base[g] = lo;
         });
         bad = __any_sync(0xFFFFFFFFu, bad);
         if (bad) total = 0;
-        const long long lo = total * blockIdx.x / gridDim.x, hi = total * (blockIdx.x + 1) / gridDim.x;
+        const long long n_cta = min(total, (long long)gridDim.x);         // with fewer tiles than CTAs the rest stay idle
+        long long lo = 0, hi = 0;
+        if (blockIdx.x < n_cta) { lo = total * blockIdx.x / n_cta; hi = total * (blockIdx.x + 1) / n_cta; }
         if (lane == 0) {
             plan[0] = lo; plan[1] = hi; plan[2] = 0; plan[3] = 0;
-            if (blockIdx.x == 0) {
-                a.base[a.G] = total;
-                a.base[a.G + 1] = bad;
-                if (bad) atomicExch(a.status, (int)STC_ERR_INVALID_ARG);
-            }
+            if (blockIdx.x == 0) { a.base[a.G] = total; a.base[a.G + 1] = bad; }
         }
         __syncwarp();
-        if (hi > lo)
-            scan([&](int g, long long first, long long end) {
-                if (g < a.G && first <= lo && lo < end) { plan[2] = lo - first; plan[3] = g; }
-            });
+        if (hi > lo) {
+            if (a.G == 1) { if (lane == 0) plan[2] = lo; }
+            else
+                scan([&](int g, long long first, long long end) {
+                    if (g < a.G && first <= lo && lo < end) { plan[2] = lo - first; plan[3] = g; }
+                });
+        }
     }
     tc_before();
     __syncthreads();
@@ -292,7 +291,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         if (lane == 0) got = wait(i, parity);
         return __shfl_sync(0xFFFFFFFFu, got, 0) != 0;
     };
-    auto give_up = [&]() { *abort_flag = 1; atomicCAS(a.status, 0, (int)STC_ERR_TIMEOUT); };
+    auto give_up = [&]() { *abort_flag = (int)STC_ERR_TIMEOUT; };
 
     if (*abort_flag) {
         // nothing was started
@@ -300,25 +299,39 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // ---- producer of Q and K ---------------------------------------------------------------------
         if (lane == 0) {
             int kc = 0, seg = 0;
+            uint32_t used[2] = {0u, 0u}, par[2] = {0u, 0u};    // per group, bit = stage: its last tile was read; parity to wait for
             bool ok = true;
             const uint32_t q_bytes = 2u * 128u * (uint32_t)(a.Gq * a.seqs);       // per row tile
             while (ok && walk.next(a, s)) {
-                const int row_tiles = s.n_seq > a.seqs ? 2 : 1;
-                if (seg > 0 && !wait(kQEmpty, (uint32_t)(seg - 1))) { give_up(); break; }
-                mbar_expect_tx(bar(kQFull), q_bytes * row_tiles);
-                for (int i = 0; i < row_tiles; ++i)
+                const bool two = s.n_seq > a.seqs;
+                if (seg > 0 && !(wait(kQEmpty, (uint32_t)(seg - 1)) && wait(kQEmpty + 1, (uint32_t)(seg - 1)))) { ok = false; break; }
+                mbar_expect_tx(bar(kQFull), two ? 2 * q_bytes : q_bytes);
+                for (int i = 0; i < (two ? 2 : 1); ++i)
                     for (int h = 0; h < 2; ++h)
-                        tma_3d(base + i * kTile + h * kHalf, &map_q, 64 * h, s.hk * a.Gq, s.row0 + i * a.seqs, bar(kQFull));
+                        tma_3d(base + i * kQTile + h * kQHalf, &map_q, 64 * h, s.hk * a.Gq, s.row0 + i * a.seqs, bar(kQFull));
                 ++seg;
                 const int row = (s.g * a.Hkv + s.hk) * a.T;
+                int st = kc % kKStages;
+#pragma unroll 1
                 for (int t = s.tile0; t < s.tile1; ++t, ++kc) {
-                    const int st = kc % kKStages;
-                    if (kc >= kKStages && !wait(kKEmpty + st, (uint32_t)(kc / kKStages - 1))) { give_up(); ok = false; break; }
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        if (!((used[w] >> st) & 1u)) continue;
+                        ok = ok && wait(kKEmpty + 2 * st + w, par[w] >> st);
+                        par[w] ^= 1u << st;
+                        used[w] &= ~(1u << st);
+                    }
+                    if (!ok) break;
                     mbar_expect_tx(bar(kKFull + st), kTile);
                     for (int h = 0; h < 2; ++h)
                         tma_2d(base + kOffK + st * kTile + h * kHalf, &map_k, 64 * h, row + t * kTok, bar(kKFull + st));
+                    const uint32_t odd = (uint32_t)(t - s.tile0) & 1u;
+                    if (two || odd == 0) used[0] |= 1u << st;
+                    if (two || odd == 1) used[1] |= 1u << st;
+                    if (++st == kKStages) st = 0;
                 }
             }
+            if (!ok) give_up();
             if (*abort_flag) {                       // copies still in flight get one more bounded wait each
                 int none = 0;
                 if (seg > 0) mbar_wait_or_abort(bar(kQFull), (uint32_t)(seg - 1) & 1u, &none, kWaitNs);
@@ -326,75 +339,63 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     mbar_wait_or_abort(bar(kKFull + i % kKStages), (uint32_t)(i / kKStages) & 1u, &none, kWaitNs);
             }
         }
-    } else if (warp == 1) {
-        // ---- MMA issuer ----------------------------------------------------------------------------------
-        // (loops are kept rolled here and in the other roles: the roles of an SM partition share its small first-level
-        // instruction cache, and unrolled they evict each other; the issuer then took 3200 cycles per step)
+    } else if (warp == 1 || warp == 2) {
+        // ---- MMA issuer of group w ------------------------------------------------------------------------
         if (lane == 0) {
             constexpr uint32_t id_qk = idesc_bf16(kRows, kTok, false), id_pv = idesc_bf16(kRows, kHeadDim, true);
-            int kc0 = 0, seg = 0;                    // tiles of the segments before; segments before
-            uint32_t n_o0 = 0, n_o1 = 0;             // P tiles consumed per group
+            const int w = warp - 1;
+            const uint32_t to = tmem + 256 + (uint32_t)w * 128u;
+            uint32_t kc0 = 0, seg = 0;               // tiles of the segments before; segments before
+            uint32_t n_s = 0, n_o = 0;               // products issued by this group
             bool ok = true;
             while (ok && walk.next(a, s)) {
                 const int tiles = s.tile1 - s.tile0;
                 const bool two = s.n_seq > a.seqs;   // two row tiles: every token tile goes to both groups
-                const int steps = two ? 2 * tiles : tiles;
-                if (!wait(kQFull, (uint32_t)seg)) { ok = false; break; }
-                // step i belongs to group w = i & 1; it is S = Q K^T now, and O += P V two iterations on
+                const int mine = two ? tiles : (tiles + 1 - w) >> 1;
+                const uint32_t first = kc0 + (two ? 0 : w), stride = two ? 1 : 2;
+                ok = wait(kQFull, seg);
+                if (ok && mine == 0) mbar_arrive(bar(kQEmpty + w));
+                const uint64_t dq = smem_desc_128(base + (two ? w * kQTile : 0u), 16);
+                // iteration n: O += P V of tile n - 2, whose S buffer then takes S = Q K^T of tile n
 #pragma unroll 1
-                for (int n = 0; n < steps + 2; ++n) {
-                    const int w = n & 1;
-                    const uint32_t n_o = w ? n_o1 : n_o0;
-                    const uint32_t ts = tmem + (uint32_t)w * 128u;
-                    if (n >= 2) {                    // O += P V of step n - 2
-                        const int j = kc0 + (two ? (n - 2) >> 1 : n - 2);
-                        ok = wait(kPFull + w, n_o);
-                        uint32_t acc = n >= 4;       // the group's first product of a segment starts O anew
-#pragma unroll 1
-                        for (int jv = 2 * j; ok && jv < 2 * j + 2; ++jv) {   // two value tiles of 64 tokens
-                            const int st = jv % kVStages;
-                            if (!two || w == 0) ok = wait(kVFull + st, (uint32_t)(jv / kVStages));
-                            tc_after();
-                            uint64_t dv = smem_desc_128(base + kOffV + st * kVTile, kVHalf);
-                            uint32_t pk = ts + 64u * (jv & 1);
-#pragma unroll 1
-                            for (int k = 0; k < 4; ++k) {    // 16 tokens: 16 rows of 128 bytes; P: 8 columns high, 8 residual
-                                tc_mma_ts(ts + 256, pk, dv, id_pv, acc);
-                                tc_mma_ts(ts + 256, pk + 8, dv, id_pv, 1);
-                                acc = 1;
-                                pk += 16;
-                                dv += 2048 >> 4;
-                            }
-                            if (!two || w == 1) tc_commit_to(bar(kVEmpty + st));
-                        }
-                        if (!ok) break;
-                        tc_commit_to(bar(kOFull + w));
-                        if (w) ++n_o1; else ++n_o0;
-                    }
-                    if (n < steps) {                 // S = Q K^T of step n
-                        const int j = kc0 + (two ? n >> 1 : n), st = j % kKStages;
-                        if (!two || w == 0) ok = wait(kKFull + st, (uint32_t)(j / kKStages));
-                        // S and P share their columns: the product that read the group's last P has to be through
-                        const uint32_t done = w ? n_o1 : n_o0;
-                        if (ok && done > 0) ok = wait(kOFull + w, done - 1);
+                for (int n = 0; ok && mine > 0 && n < mine + 2; ++n) {
+                    if (n >= 2) {
+                        const uint32_t j = first + (uint32_t)(n - 2) * stride, st = j % kVStages, buf = n_o & 1u;
+                        ok = wait(kPFull + 2 * w + buf, n_o >> 1) && wait(kVFull + st, j / kVStages);
                         if (!ok) break;
                         tc_after();
-                        uint64_t dq = smem_desc_128(base + (two ? w * kTile : 0u), 16);
-                        uint64_t dk = smem_desc_128(base + kOffK + st * kTile, 16);
-#pragma unroll 1
-                        for (int k = 0; k < 2; ++k) {        // 64 dims: one half tile
+                        const uint64_t dv = smem_desc_128(base + kOffV + st * kTile, kHalf);
+                        const uint32_t p = tmem + (uint32_t)w * 128u + buf * 64u;
+                        const uint32_t more = (n - 2) % kFlush != 0;          // else O starts anew
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)      // 16 dims: 32 bytes, 2 units
-                                tc_mma_ss(ts, dq + 2 * e, dk + 2 * e, id_qk, k + e != 0);
-                            dq += kHalf >> 4;
-                            dk += kHalf >> 4;
+                        for (int k = 0; k < 4; ++k) {        // 16 tokens: 16 rows of 128 bytes; P: 8 columns high, 8 residual
+                            tc_mma_ts(to, p + 16 * k, dv + (uint64_t)(k * (2048 >> 4)), id_pv, k ? 1u : more);
+                            tc_mma_ts(to, p + 16 * k + 8, dv + (uint64_t)(k * (2048 >> 4)), id_pv, 1);
                         }
-                        tc_commit_to(bar(kSFull + w));
-                        if (!two || w == 1) tc_commit_to(bar(kKEmpty + st));
-                        if (n == steps - 1) tc_commit_to(bar(kQEmpty));
+                        tc_commit_to(bar(kOFull + w));
+                        tc_commit_to(bar(kVEmpty + 2 * st + w));
+                        ++n_o;
+                    }
+                    if (n < mine) {
+                        const uint32_t j = first + (uint32_t)n * stride, st = j % kKStages, buf = n_s & 1u;
+                        ok = wait(kKFull + st, j / kKStages);
+                        // the buffer holds the P of the group's last but one tile until that product is through
+                        // (at a segment's start both of its predecessors may be through: the later one is asked for)
+                        if (ok && n_s >= 2) ok = wait(kOFull + w, n == 0 ? n_s - 1 : n_s - 2);
+                        if (!ok) break;
+                        tc_after();
+                        const uint64_t dk = smem_desc_128(base + kOffK + st * kTile, 16);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)          // 16 dims = 32 bytes = 2 units; 64 dims = one half tile
+                            tc_mma_ss(tmem + (uint32_t)w * 128u + buf * 64u, dq + (uint64_t)((k >> 2) * (kQHalf >> 4) + (k & 3) * 2),
+                                      dk + (uint64_t)((k >> 2) * (kHalf >> 4) + (k & 3) * 2), id_qk, k != 0);
+                        tc_commit_to(bar(kSFull + 2 * w + buf));
+                        tc_commit_to(bar(kKEmpty + 2 * st + w));
+                        if (n == mine - 1) tc_commit_to(bar(kQEmpty + w));
+                        ++n_s;
                     }
                 }
-                kc0 += tiles;
+                kc0 += (uint32_t)tiles;
                 ++seg;
             }
             if (!ok) give_up();
@@ -403,8 +404,9 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // ---- softmax: thread = row -----------------------------------------------------------------------
         const int w = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t ts = lane_base + w * 128, to = lane_base + 256 + w * 128;
-        uint32_t n_s = 0, n_x = 0;
+        const uint32_t to = lane_base + 256 + w * 128;
+        float4* const my_flush = a.flush + ((size_t)blockIdx.x * 2 + w) * 32 * kRows + row;
+        uint32_t n_s = 0, n_x = 0;                   // tiles of this group; uses of the exchange barrier
         bool ok = true;
         while (ok && walk.next(a, s)) {
             const int tiles = s.tile1 - s.tile0;
@@ -433,9 +435,11 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     }
                 }
             };
-            float m = -INFINITY, l = 0.f;
+            float m = -INFINITY, l = 0.f, m_flush = -INFINITY;
+#pragma unroll 1
             for (int n = 0; n < mine; ++n) {
-                ok = warp_wait(kSFull + w, n_s);
+                const uint32_t buf = n_s & 1u, ts = lane_base + w * 128 + buf * 64;
+                ok = warp_wait(kSFull + 2 * w + buf, n_s >> 1);
                 if (!ok) break;
                 tc_after();
                 const int t0 = (first + n * stride) * kTok;
@@ -469,13 +473,42 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if constexpr (CAP && BIAS) tmem_wait_st();
                 if constexpr (!BIAS)
                     if (top > -INFINITY) top = CAP ? a.cap_log2 * tanh_f32(top * a.cap_in) : top * a.scale_log2;
-                // move the maximum only if it is exceeded by much; the accumulator follows
+                // move the maximum only if it is exceeded by much; the accumulator follows.  After kFlush tiles it is
+                // emptied first (with the maximum it was built with), and the issuer starts it anew
                 const bool move = top > m + kSlack || (m == -INFINITY && top > -INFINITY);
-                if (__any_sync(0xFFFFFFFFu, move)) {
+                const bool any_move = __any_sync(0xFFFFFFFFu, move), empty_now = n > 0 && n % kFlush == 0;
+                if (n > 0 && (any_move || empty_now)) {
+                    ok = warp_wait(kOFull + w, n_s - 1);
+                    if (!ok) break;
+                    tc_after();
+                }
+                if (empty_now) {
+                    const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
+#pragma unroll 1
+                    for (int c = 0; c < kHeadDim; c += 16) {
+                        uint32_t r[16];
+                        tmem_ld16(to + c, r);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float4* dst = my_flush + (size_t)(c / 4 + i) * kRows;
+                            float4 v = make_float4(__uint_as_float(r[4 * i]), __uint_as_float(r[4 * i + 1]),
+                                                   __uint_as_float(r[4 * i + 2]), __uint_as_float(r[4 * i + 3]));
+                            if (n > kFlush) {
+                                const float4 o = __ldcg(dst);
+                                v.x = fmaf(o.x, keep, v.x); v.y = fmaf(o.y, keep, v.y);
+                                v.z = fmaf(o.z, keep, v.z); v.w = fmaf(o.w, keep, v.w);
+                            }
+                            __stcg(dst, v);
+                        }
+                    }
+                    m_flush = m;
+                }
+                if (any_move) {
                     const float to_m = move ? top : m;
                     const float f = (m == -INFINITY) ? 0.f : exp2f(m - to_m);
                     l *= f;
-                    if (n > 0) {
+                    if (n > 0 && !empty_now) {
 #pragma unroll 1
                         for (int c = 0; c < kHeadDim; c += 16) {
                             uint32_t r[16];
@@ -527,7 +560,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 l += (la.x + lb.x) + (la.y + lb.y);
                 tmem_wait_st();
                 tc_before();
-                mbar_arrive(bar(kPFull + w));
+                mbar_arrive(bar(kPFull + 2 * w + buf));
                 ++n_s;
             }
             if (!ok) break;
@@ -537,6 +570,28 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if (!ok) break;
                 tc_after();
             }
+            if (mine > kFlush) {                     // take back what the accumulator was emptied of
+                const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
+#pragma unroll 1
+                for (int c = 0; c < kHeadDim; c += 16) {
+                    uint32_t r[16];
+                    tmem_ld16(to + c, r);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float4 o = __ldcg(my_flush + (size_t)(c / 4 + i) * kRows);
+                        r[4 * i] = __float_as_uint(fmaf(o.x, keep, __uint_as_float(r[4 * i])));
+                        r[4 * i + 1] = __float_as_uint(fmaf(o.y, keep, __uint_as_float(r[4 * i + 1])));
+                        r[4 * i + 2] = __float_as_uint(fmaf(o.z, keep, __uint_as_float(r[4 * i + 2])));
+                        r[4 * i + 3] = __float_as_uint(fmaf(o.w, keep, __uint_as_float(r[4 * i + 3])));
+                    }
+                    tmem_st16(to + c, r);
+                }
+                tmem_wait_st();
+            }
+            const size_t out_row = (size_t)seq * a.Hq + head;
+            // read before the exchange: own_lse and lse may be one array, and the other group writes lse behind it
+            const float own_l = s.slot < 0 && a.own_lse ? a.own_lse[out_row] : 0.f;
             float mo = m, lo_sum = l, f0 = 1.f, f1 = 0.f;   // joined maximum and sum; factors of accumulator 0 / 1
             bool has1 = false;
             int c_lo = 0, c_hi = kHeadDim;                   // dims this thread writes
@@ -559,22 +614,23 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 c_lo = 64 * w;
                 c_hi = c_lo + 64;
             }
-            const size_t out_row = (size_t)seq * a.Hq + head;
             float fo = 1.f, fown = 0.f;
-            const float* own = nullptr;
-            float* dst;
+            const float4* own = nullptr;
+            float4* dst;
+            size_t step;                             // from one chunk of four dims to the next
             if (s.slot < 0) {
-                const Join j = join(mo, lo_sum, BIAS ? bias_shift(a, s.len, seq, head) : 0.f, a.own_lse != nullptr,
-                                    a.own_lse ? a.own_lse[out_row] : 0.f);
+                const Join j = join(mo, lo_sum, BIAS ? bias_shift(a, s.len, seq, head) : 0.f, a.own_lse != nullptr, own_l);
                 fo = j.fo;
                 fown = j.fown;
-                if (a.own_out && fown != 0.f) own = a.own_out + out_row * kHeadDim;
-                dst = a.out + out_row * kHeadDim;
+                if (a.own_out && fown != 0.f) own = reinterpret_cast<const float4*>(a.own_out + out_row * kHeadDim);
+                dst = reinterpret_cast<float4*>(a.out + out_row * kHeadDim);
+                step = 1;
                 if (live && a.lse && c_lo == 0) a.lse[out_row] = j.lse;
             } else {
-                const size_t slot = (size_t)s.slot * a.slot_rows + (two ? w * a.seqs * a.Gq : 0) + row;
-                dst = a.part_o + slot * kHeadDim;
-                if (live && c_lo == 0) a.part_ml[slot] = make_float2(mo, lo_sum);
+                const int part_row = (two ? w * a.seqs * a.Gq : 0) + row;
+                dst = a.part_o + (size_t)s.slot * 32 * a.slot_rows + part_row;
+                step = a.slot_rows;
+                if (live && c_lo == 0) a.part_ml[(size_t)s.slot * a.slot_rows + part_row] = make_float2(mo, lo_sum);
             }
 #pragma unroll 1
             for (int c = c_lo; c < c_hi; c += 16) {
@@ -594,11 +650,11 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         }
                         float4 v4 = make_float4(v[0], v[1], v[2], v[3]);
                         if (own) {
-                            const float4 w4 = *reinterpret_cast<const float4*>(own + c + i);
+                            const float4 w4 = own[(c + i) / 4];
                             v4.x = fmaf(w4.x, fown, v4.x); v4.y = fmaf(w4.y, fown, v4.y);
                             v4.z = fmaf(w4.z, fown, v4.z); v4.w = fmaf(w4.w, fown, v4.w);
                         }
-                        *reinterpret_cast<float4*>(dst + c + i) = v4;
+                        dst[(size_t)((c + i) / 4) * step] = v4;
                     }
                 }
             }
@@ -612,13 +668,14 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         if (!ok) give_up();
     } else if (warp >= 12) {
         // ---- value tiles: packed groups -> swizzled rows ---------------------------------------------------
-        // Warps 12, 13 build the even tiles of 64 tokens and 14, 15 the odd ones, 32 tokens each.  A lane owns one
-        // 16-byte column of every other token; a kept group is one asynchronous 16-byte copy, a dropped one a
+        // Warps 12, 13 build the even tiles and 14, 15 the odd ones (counted over the CTA), 32 tokens each.  A lane owns
+        // one 16-byte column of every other token; a kept group is one asynchronous 16-byte copy, a dropped one a
         // zero-filled copy that reads nothing.  The copies of a warp's next tile are under way before the last
         // one's are waited for, unless its stage is still being read.
         const int pair = (warp - 12) >> 1, tok0 = (warp & 1) * 32, oct = lane & 15, grp = oct / OPG, sub = oct % OPG;
         const uint32_t below = (1u << grp) - 1u;
-        int vc = 0;                                  // tiles of 64 tokens so far, both pairs'
+        uint32_t used[2] = {0u, 0u}, par[2] = {0u, 0u};    // as the producer's, for the value stages
+        int vc = 0;                                  // tiles of the segments before
         int pending = -1;                            // stage whose copies are not waited for yet
         bool ok = true;
         auto publish = [&]() {                       // this warp's copies into `pending` have landed
@@ -628,36 +685,44 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             pending = -1;
         };
         while (ok && walk.next(a, s)) {
+            const bool two = s.n_seq > a.seqs;
             const size_t problem = (size_t)s.g * a.Hkv + s.hk;
             const uint16_t* mask_row = a.v_mask + problem * a.T;
             const uint32_t* offs = a.v_offs + problem * (a.T + 1);
             const uint4* packed = a.v_packed + problem * a.cap_groups * OPG;
             const int64_t limit = a.cap_groups;
-            const int n_half = 2 * (s.tile1 - s.tile0), first_tok = s.tile0 * kTok + tok0;
+            const int tiles = s.tile1 - s.tile0, first_tok = s.tile0 * kTok + tok0;
             auto fetch = [&](int h, uint32_t& m, uint32_t& first) {        // this lane's token mask, the warp's first group
-                const int t = first_tok + h * kVTok;
-                m = h < n_half && t + lane < s.len ? mask_row[t + lane] : 0u;
-                first = h < n_half && t < s.len ? offs[t] : 0u;
+                const int t = first_tok + h * kTok;
+                m = h < tiles && t + lane < s.len ? mask_row[t + lane] : 0u;
+                first = h < tiles && t < s.len ? offs[t] : 0u;
             };
+            const int h0 = (vc + pair) & 1;          // the pair's first tile of the segment
             uint32_t m_next, first_next;
-            fetch(pair, m_next, first_next);         // a segment is an even number of tiles of 64 tokens
-            for (int h = pair; h < n_half; h += 2) {
+            fetch(h0, m_next, first_next);
+#pragma unroll 1
+            for (int h = h0; h < tiles; h += 2) {
                 const uint32_t m = m_next & ((1u << S) - 1u), first = first_next;
                 fetch(h + 2, m_next, first_next);
                 const uint32_t cnt = __popc(m);
                 const uint32_t pre = warp_incl_scan(cnt, lane) - cnt;
-                const int j = vc + h, st = j % kVStages;
-                if (j >= kVStages) {
-                    const uint32_t par = (uint32_t)(j / kVStages - 1) & 1u;
+                const int st = (vc + h) % kVStages;
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    if (!((used[w] >> st) & 1u)) continue;
+                    const uint32_t p = (par[w] >> st) & 1u;
+                    par[w] ^= 1u << st;
+                    used[w] &= ~(1u << st);
                     int free = 0;
-                    if (lane == 0) free = mbar_try_wait(bar(kVEmpty + st), par);
-                    if (!__shfl_sync(0xFFFFFFFFu, free, 0)) {
-                        if (pending >= 0) { cp_async_wait<0>(); publish(); }
-                        ok = warp_wait(kVEmpty + st, par);
-                        if (!ok) break;
-                    }
+                    if (lane == 0) free = mbar_try_wait(bar(kVEmpty + 2 * st + w), p);
+                    if (__shfl_sync(0xFFFFFFFFu, free, 0)) continue;
+                    if (pending >= 0) { cp_async_wait<0>(); publish(); }
+                    ok = ok && warp_wait(kVEmpty + 2 * st + w, p);
                 }
-                const uint32_t dst = base + kOffV + st * kVTile + (uint32_t)(oct >> 3) * kVHalf;
+                if (!ok) break;
+                if (two || !(h & 1)) used[0] |= 1u << st;
+                if (two || (h & 1)) used[1] |= 1u << st;
+                const uint32_t dst = base + kOffV + st * kTile + (uint32_t)(oct >> 3) * kHalf;
 #pragma unroll 4
                 for (int i = 0; i < 16; ++i) {
                     const int tok = 2 * i + (lane >> 4);
@@ -671,7 +736,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if (pending >= 0) { cp_async_wait<1>(); publish(); }
                 pending = st;
             }
-            vc += n_half;
+            vc += tiles;
         }
         cp_async_wait<0>();
         if (ok && pending >= 0) publish();
@@ -679,67 +744,94 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     }
     tc_before();
     __syncthreads();
+    if (threadIdx.x == 0) a.cta_status[blockIdx.x] = *abort_flag;
     if (warp == 1) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
 }
 
-// Joins the partials of units that more than one CTA worked on, and answers the rows whose prefix is empty.
-// One warp per (row, query head), a lane four channels; partials in CTA order.
+// Joins the partials of units that more than one CTA worked on, answers the rows whose prefix is empty, and gathers the
+// CTAs' status.  A block owns eight consecutive rows of a KV head (row = sequence * Gq + head within the KV
+// head), a thread four channels of one of them: 8 rows x 16 bytes are one 128-byte line of a partial, and 4 x 16
+// bytes of a row are written together.  Partials are taken in CTA order, four loads in flight.
 __global__ void __launch_bounds__(256)
-prefix_merge_kernel(const PrefixArgs a, int n_cta) {
-    const long long task = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    if (task >= (long long)a.n_rows * a.Hq || a.base[a.G + 1] != 0) return;
-    const int seq = (int)(task / a.Hq), head = (int)(task - (long long)seq * a.Hq);
-    if (seq < a.row_start[0] || seq >= a.row_start[a.G]) return;
-    int g = 0, g_hi = a.G;                           // last prefix that starts at or before the row
-    while (g_hi - g > 1) {
-        const int mid = (g + g_hi) >> 1;
-        if (a.row_start[mid] <= seq) g = mid; else g_hi = mid;
+prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
+    const bool bad = a.base[a.G + 1] != 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        int st = bad ? (int)STC_ERR_INVALID_ARG : (int)STC_OK;
+        for (int c = 0; c < grid; ++c)
+            if (a.cta_status[c] != 0) st = a.cta_status[c];
+        *a.status = st;
     }
-    const Group grp = load_group(a, g);
-    const int hk = head / a.Gq, in_group = seq - grp.row0, blk = in_group / (2 * a.seqs);
-    const int row = (in_group - blk * 2 * a.seqs) * a.Gq + head % a.Gq;
-    float m = -INFINITY, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (grp.tiles > 0) {
-        const long long total = a.base[a.G];
-        const long long x0 = a.base[g] + ((long long)hk * grp.blocks + blk) * grp.tiles, x1 = x0 + grp.tiles;
-        const long long c0 = ((x0 + 1) * n_cta + total - 1) / total - 1, c1 = (x1 * n_cta + total - 1) / total - 1;
-        if (c0 == c1) return;                        // a whole unit: done where it was computed
-        // a range that begins inside the unit used its first slot; with fewer tiles than CTAs some ranges are empty
-        auto slot_of = [&](long long c) -> long long {
-            const long long lo = total * c / n_cta, hi = total * (c + 1) / n_cta;
-            return lo < hi ? (2 * c + (lo >= x0 ? 0 : 1)) * a.slot_rows + row : -1;
-        };
-        for (long long c = c0; c <= c1; ++c) {
-            const long long slot = slot_of(c);
-            if (slot >= 0) m = fmaxf(m, a.part_ml[slot].x);
-        }
-        for (long long c = c0; c <= c1; ++c) {
-            const long long slot = slot_of(c);
-            if (slot < 0) continue;
-            const float2 p = a.part_ml[slot];
-            if (p.x == -INFINITY) continue;
-            const float f = exp2f(p.x - m);
-            const float4 v = reinterpret_cast<const float4*>(a.part_o + slot * kHeadDim)[lane];
-            l = fmaf(p.y, f, l);
-            o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
-        }
-    }
+    const int hk = blockIdx.x / chunks;
+    const long long flat = (long long)(blockIdx.x - hk * chunks) * 8 + ((threadIdx.x & 31) >> 2);
+    const int d4 = (threadIdx.x >> 5) * 4 + (threadIdx.x & 3);
+    const int seq = (int)(flat / a.Gq), head = hk * a.Gq + (int)(flat - (long long)seq * a.Gq);
+    bool mine = !bad && seq < a.n_rows && seq >= a.row_start[0] && seq < a.row_start[a.G];
+    float m = -INFINITY, l = 0.f, shift = 0.f, own_l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f), own = o;
     const size_t out_row = (size_t)seq * a.Hq + head;
-    const Join j = join(m, l, bias_shift(a, grp.len, seq, head), a.own_lse != nullptr,
-                        a.own_lse ? a.own_lse[out_row] : 0.f);
+    if (mine) {
+        int g = 0, g_hi = a.G;                       // last prefix that starts at or before the row
+        while (g_hi - g > 1) {
+            const int mid = (g + g_hi) >> 1;
+            if (a.row_start[mid] <= seq) g = mid; else g_hi = mid;
+        }
+        const Group grp = load_group(a, g);
+        const int in_group = seq - grp.row0, blk = in_group / (2 * a.seqs);
+        const int row = (in_group - blk * 2 * a.seqs) * a.Gq + (head - hk * a.Gq);
+        int c0 = 0, c1 = -1, late = 0;
+        if (grp.tiles > 0) {
+            const long long total = a.base[a.G], n = min(total, (long long)grid);
+            const long long x0 = a.base[g] + ((long long)hk * grp.blocks + blk) * grp.tiles, x1 = x0 + grp.tiles;
+            // the CTA whose range holds tile x is ceil((x + 1) * n / total) - 1; only the first of a unit's CTAs can
+            // have begun before the unit, and then used its second slot for it
+            c0 = (int)(((x0 + 1) * n + total - 1) / total - 1);
+            c1 = (int)((x1 * n + total - 1) / total - 1);
+            late = total * c0 / n < x0 ? 1 : 0;
+            mine = c0 != c1;                         // a whole unit was finished where it was computed
+        }
+        if (mine) {
+            if (a.own_lse) {
+                own_l = a.own_lse[out_row];
+                own = reinterpret_cast<const float4*>(a.own_out + out_row * kHeadDim)[d4];
+            }
+            shift = bias_shift(a, grp.len, seq, head);
+        }
+#pragma unroll 1
+        for (int c = c0; mine && c <= c1; c += 4) {
+            float2 p[4];
+            float4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int cc = min(c + i, c1);
+                const size_t slot = 2 * (size_t)cc + (cc == c0 ? late : 0);
+                p[i] = __ldcg(a.part_ml + slot * a.slot_rows + row);
+                v[i] = __ldcg(a.part_o + (slot * 32 + d4) * a.slot_rows + row);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (c + i > c1 || p[i].x == -INFINITY) continue;
+                const float top = fmaxf(m, p[i].x), fm = m == -INFINITY ? 0.f : exp2f(m - top), fp = exp2f(p[i].x - top);
+                l = fmaf(p[i].y, fp, l * fm);
+                o.x = fmaf(v[i].x, fp, o.x * fm); o.y = fmaf(v[i].y, fp, o.y * fm);
+                o.z = fmaf(v[i].z, fp, o.z * fm); o.w = fmaf(v[i].w, fp, o.w * fm);
+                m = top;
+            }
+        }
+    }
+    __syncthreads();                                 // own_lse and lse may be one array: every thread of a row has read the former
+    if (!mine) return;
+    const Join j = join(m, l, shift, a.own_lse != nullptr, own_l);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (j.fo != 0.f) v = make_float4(o.x * j.fo, o.y * j.fo, o.z * j.fo, o.w * j.fo);
-    if (a.own_out && j.fown != 0.f) {
-        const float4 w = reinterpret_cast<const float4*>(a.own_out + out_row * kHeadDim)[lane];
-        v.x = fmaf(w.x, j.fown, v.x); v.y = fmaf(w.y, j.fown, v.y); v.z = fmaf(w.z, j.fown, v.z); v.w = fmaf(w.w, j.fown, v.w);
+    if (j.fown != 0.f) {
+        v.x = fmaf(own.x, j.fown, v.x); v.y = fmaf(own.y, j.fown, v.y);
+        v.z = fmaf(own.z, j.fown, v.z); v.w = fmaf(own.w, j.fown, v.w);
     }
-    reinterpret_cast<float4*>(a.out + out_row * kHeadDim)[lane] = v;
-    if (a.lse && lane == 0) a.lse[out_row] = j.lse;
+    reinterpret_cast<float4*>(a.out + out_row * kHeadDim)[d4] = v;
+    if (a.lse && d4 == 0) a.lse[out_row] = j.lse;
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -756,7 +848,8 @@ int slot_rows(const Geom& g, int n_rows) {
 
 size_t prefix_ws_bytes(const Geom& g, int n_rows) {
     const size_t slots = 2 * (size_t)kPlanSms * slot_rows(g, n_rows);
-    return 256 + align256(((size_t)g.B + 2) * 8) + align256(slots * 8) + align256(slots * kHeadDim * 4);
+    return 256 + align256(kPlanSms * 4) + align256(((size_t)g.B + 2) * 8) + align256(slots * 8) + slots * kHeadDim * 4 +
+           2 * (size_t)kPlanSms * kRows * kHeadDim * 4;
 }
 
 cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packed, const uint16_t* v_mask,
@@ -768,14 +861,19 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
     a.row_start = row_start; a.seq_len = g.seq_len;
     a.v_mask = v_mask; a.v_offs = v_offs; a.v_packed = static_cast<const uint4*>(v_packed);
     a.own_out = own_out; a.own_lse = own_lse; a.out = out; a.lse = lse;
+    a.slot_rows = slot_rows(g, n_rows);
+    const size_t slots = 2 * (size_t)kPlanSms * a.slot_rows;
     a.status = reinterpret_cast<int32_t*>(w);
     w += 256;
+    a.cta_status = reinterpret_cast<int32_t*>(w);
+    w += align256(kPlanSms * 4);
     a.base = reinterpret_cast<long long*>(w);
     w += align256(((size_t)g.B + 2) * 8);
-    a.slot_rows = slot_rows(g, n_rows);
     a.part_ml = reinterpret_cast<float2*>(w);
-    w += align256(2 * (size_t)kPlanSms * a.slot_rows * 8);
-    a.part_o = reinterpret_cast<float*>(w);
+    w += align256(slots * 8);
+    a.part_o = reinterpret_cast<float4*>(w);
+    w += slots * kHeadDim * 4;
+    a.flush = reinterpret_cast<float4*>(w);
     a.cap_groups = cap_groups;
     a.G = g.B; a.Hq = g.Hq; a.Hkv = g.Hkv; a.Gq = g.Gq; a.T = g.T; a.n_rows = n_rows;
     a.seqs = kRows / g.Gq;
@@ -811,8 +909,6 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return cudaErrorInvalidValue;
     }
-    e = cudaMemsetAsync(a.status, 0, 4, st);
-    if (e != cudaSuccess) return e;
     const bool cap = a.sc.softcap > 0.f, bias = a.sc.slopes || !(sm_scale > 0.f);
 #define STC_PREFIX_LAUNCH(S_, C_, B_)                                                                            \
     do {                                                                                                         \
@@ -836,9 +932,8 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
 #undef STC_PREFIX_LAUNCH
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    const long long tasks = (long long)n_rows * g.Hq;
-    const unsigned grid = (unsigned)((tasks + 7) / 8);
-    prefix_merge_kernel<<<grid, 256, 0, st>>>(a, n_cta);
+    const int chunks = (int)(((long long)n_rows * g.Gq + 7) / 8);    // times Hkv: below 2^31, as n_rows * Hq is
+    prefix_merge_kernel<<<(unsigned)(chunks * g.Hkv), 256, 0, st>>>(a, n_cta, chunks);
     return cudaGetLastError();
 }
 
