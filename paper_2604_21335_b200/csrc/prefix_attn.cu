@@ -35,8 +35,8 @@
 // The running maximum only moves when a tile exceeds it by more than 2^8, so the accumulator in tensor memory is
 // rescaled a few times per segment and not per tile; weights are then at most 2^8, far from fp32's limits.
 //
-// Loops are kept rolled (16 scores at a time): the roles of an SM partition share its small first-level instruction
-// cache and evict each other where they are unrolled.
+// The token tiles of a segment are taken from the last to the first: with a distance bias the largest scores come
+// first and the maximum hardly moves afterwards.
 //
 // Every wait is bounded (about a second); one that expires raises a CTA-wide flag and STC_ERR_TIMEOUT in the
 // status word, the roles leave, the producer waits (bounded) for its copies, tensor memory is freed.
@@ -173,29 +173,31 @@ __device__ __forceinline__ float bias_shift(const PrefixArgs& a, int len, int se
     return a.sc.slopes[head] * (float)(hi - 1 - pos);
 }
 
-// Caps 16 scores of a row (raw products in, log2 units out).  Scores far below the cap, the usual case, need only the
-// polynomial of tanh_f32; the warp votes once per 16 instead of branching per score.
-__device__ __forceinline__ void cap_scores(uint32_t (&r)[16], float cap_in, float cap_log2) {
+// Caps the 64 scores of a row (raw products in, log2 units out).  Scores far below the cap, the usual case, need only the
+// polynomial of tanh_f32, two at a time; the warp votes once per tile instead of branching per score.
+__device__ __forceinline__ void cap_scores(uint32_t (&r)[kTok], float cap_in, float cap_log2) {
     float big = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) big = fmaxf(big, fabsf(__uint_as_float(r[i])));
-    const bool small = __all_sync(0xFFFFFFFFu, big * fabsf(cap_in) <= kTanhSmall);
+    for (int i = 0; i < kTok; ++i) big = fmaxf(big, fabsf(__uint_as_float(r[i])));
+    if (__all_sync(0xFFFFFFFFu, big * fabsf(cap_in) <= kTanhSmall)) {
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {                // tanh_small, two at a time
-        const float2 z = mul2(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), both(cap_in));
-        const float2 u = mul2(z, z);
-        float2 p = fma2(both(kTanh4), u, both(kTanh3));
-        p = fma2(p, u, both(kTanh2));
-        p = fma2(p, u, both(kTanh1));
-        p = fma2(p, u, both(kTanh0));
-        const float2 t = fma2(mul2(z, u), p, z);
-        float2 y = mul2(t, both(cap_log2));
-        if (!small) {                                // uniform
-            if (fabsf(z.x) > kTanhSmall) y.x = cap_log2 * tanh_large(z.x);
-            if (fabsf(z.y) > kTanhSmall) y.y = cap_log2 * tanh_large(z.y);
+        for (int i = 0; i < kTok; i += 2) {          // tanh_small
+            const float2 z = mul2(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), both(cap_in));
+            const float2 u = mul2(z, z);
+            float2 p = fma2(both(kTanh4), u, both(kTanh3));
+            p = fma2(p, u, both(kTanh2));
+            p = fma2(p, u, both(kTanh1));
+            p = fma2(p, u, both(kTanh0));
+            const float2 y = mul2(fma2(mul2(z, u), p, z), both(cap_log2));
+            r[i] = __float_as_uint(y.x);
+            r[i + 1] = __float_as_uint(y.y);
         }
-        r[i] = __float_as_uint(y.x);
-        r[i + 1] = __float_as_uint(y.y);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kTok; ++i) {
+            const float z = __uint_as_float(r[i]) * cap_in, lo = tanh_small(z), hi = tanh_large(z);
+            r[i] = __float_as_uint(cap_log2 * (fabsf(z) <= kTanhSmall ? lo : hi));
+        }
     }
 }
 
@@ -313,7 +315,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const int row = (s.g * a.Hkv + s.hk) * a.T;
                 int st = kc % kKStages;
 #pragma unroll 1
-                for (int t = s.tile0; t < s.tile1; ++t, ++kc) {
+                for (int t = s.tile1 - 1; t >= s.tile0; --t, ++kc) {
 #pragma unroll
                     for (int w = 0; w < 2; ++w) {
                         if (!((used[w] >> st) & 1u)) continue;
@@ -325,7 +327,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     mbar_expect_tx(bar(kKFull + st), kTile);
                     for (int h = 0; h < 2; ++h)
                         tma_2d(base + kOffK + st * kTile + h * kHalf, &map_k, 64 * h, row + t * kTok, bar(kKFull + st));
-                    const uint32_t odd = (uint32_t)(t - s.tile0) & 1u;
+                    const uint32_t odd = (uint32_t)(s.tile1 - 1 - t) & 1u;
                     if (two || odd == 0) used[0] |= 1u << st;
                     if (two || odd == 1) used[1] |= 1u << st;
                     if (++st == kKStages) st = 0;
@@ -411,7 +413,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         while (ok && walk.next(a, s)) {
             const int tiles = s.tile1 - s.tile0;
             const bool two = s.n_seq > a.seqs;
-            const int mine = two ? tiles : (tiles + 1 - w) >> 1, stride = two ? 1 : 2, first = s.tile0 + (two ? 0 : w);
+            const int mine = two ? tiles : (tiles + 1 - w) >> 1, stride = two ? 1 : 2, first = s.tile1 - 1 - (two ? 0 : w);
             // this thread's row: sequence and head
             const int in_tile = row / a.Gq, seq_i = (two ? w * a.seqs : 0) + in_tile;
             const bool live = in_tile < a.seqs && seq_i < s.n_seq;
@@ -422,14 +424,14 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (BIAS && a.sc.slopes) slope2 = a.sc.slopes[head] * kLog2e;
             const int32_t* doc = a.sc.tok_doc ? a.sc.tok_doc + (size_t)s.g * a.T : nullptr;
             if (doc) my_doc = a.sc.q_doc[seq];
-            // -inf for the tokens t .. t + 15 that the row does not see
-            auto hide = [&](uint32_t (&r)[16], int t) {
+            // -inf for the tokens t .. t + 63 that the row does not see
+            auto hide = [&](uint32_t (&r)[kTok], int t) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
+                for (int i = 0; i < kTok; ++i)
                     if (t + i < lo || t + i >= hi) r[i] = __float_as_uint(-INFINITY);
                 if (doc) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
+                    for (int i = 0; i < kTok; ++i) {
                         const int d = __ldg(doc + min(t + i, a.T - 1));
                         if (d >= 0 && d != my_doc) r[i] = __float_as_uint(-INFINITY);
                     }
@@ -442,37 +444,34 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 ok = warp_wait(kSFull + 2 * w + buf, n_s >> 1);
                 if (!ok) break;
                 tc_after();
-                const int t0 = (first + n * stride) * kTok;
-                // does every row of the warp see the whole tile?
-                const bool open = __all_sync(0xFFFFFFFFu, lo <= t0 && hi >= t0 + kTok) && !doc;
-                // pass 1: the tile's maximum.  A cap alone keeps the order, so the raw products do; with a bias the finished
-                // scores are compared, and kept if capping them again would cost more than tensor memory
-                float top = -INFINITY;
-#pragma unroll 1
-                for (int c = 0; c < kTok; c += 16) {
-                    uint32_t r[16];
-                    tmem_ld16(ts + c, r);
-                    tmem_wait_ld();
-                    if constexpr (BIAS) {
-                        const float far = (float)(t0 + c - (hi - 1));
-                        if constexpr (CAP) cap_scores(r, a.cap_in, a.cap_log2);
+                const int t0 = (first - n * stride) * kTok;
+                uint32_t r[kTok];
+                tmem_ld16<0>(ts, r);
+                tmem_ld16<16>(ts + 16, r);
+                tmem_ld16<32>(ts + 32, r);
+                tmem_ld16<48>(ts + 48, r);
+                tmem_wait_ld();
+                // scores in log2 units where they are not the raw products times a positive scale
+                if constexpr (CAP) cap_scores(r, a.cap_in, a.cap_log2);
+                if constexpr (BIAS) {
+                    const float far = (float)(t0 - (hi - 1));
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float x = CAP ? __uint_as_float(r[i]) : __uint_as_float(r[i]) * a.scale_log2;
-                            r[i] = __float_as_uint(fmaf(slope2, far + (float)i, x));
-                        }
+                    for (int i = 0; i < kTok; i += 2) {
+                        float2 x = make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+                        if constexpr (!CAP) x = mul2(x, both(a.scale_log2));
+                        x = fma2(both(slope2), add2(both(far), make_float2((float)i, (float)(i + 1))), x);
+                        r[i] = __float_as_uint(x.x);
+                        r[i + 1] = __float_as_uint(x.y);
                     }
-                    if (!open) hide(r, t0 + c);
-                    if constexpr (CAP && BIAS) tmem_st16(ts + c, r);
-                    float t2[2] = {top, -INFINITY};
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2)
-                        t2[(i >> 1) & 1] = fmaxf(fmaxf(t2[(i >> 1) & 1], __uint_as_float(r[i])), __uint_as_float(r[i + 1]));
-                    top = fmaxf(t2[0], t2[1]);
                 }
-                if constexpr (CAP && BIAS) tmem_wait_st();
-                if constexpr (!BIAS)
-                    if (top > -INFINITY) top = CAP ? a.cap_log2 * tanh_f32(top * a.cap_in) : top * a.scale_log2;
+                // does every row of the warp see the whole tile?
+                if (doc || !__all_sync(0xFFFFFFFFu, lo <= t0 && hi >= t0 + kTok)) hide(r, t0);
+                float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int i = 0; i < kTok; i += 2)
+                    t4[(i >> 1) & 3] = fmaxf(fmaxf(t4[(i >> 1) & 3], __uint_as_float(r[i])), __uint_as_float(r[i + 1]));
+                float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+                if constexpr (!CAP && !BIAS) top *= a.scale_log2;     // (-inf stays -inf: the scale is positive)
                 // move the maximum only if it is exceeded by much; the accumulator follows.  After kFlush tiles it is
                 // emptied first (with the maximum it was built with), and the issuer starts it anew
                 const bool move = top > m + kSlack || (m == -INFINITY && top > -INFINITY);
@@ -483,17 +482,23 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     tc_after();
                 }
                 if (empty_now) {
+                    // (uniform maxima: the sums only grow by this accumulator, and nothing has to be read back)
                     const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
+                    const bool grow = n > kFlush && __all_sync(0xFFFFFFFFu, keep == 1.f);
 #pragma unroll 1
                     for (int c = 0; c < kHeadDim; c += 16) {
-                        uint32_t r[16];
-                        tmem_ld16(to + c, r);
+                        uint32_t q[16];
+                        tmem_ld16(to + c, q);
                         tmem_wait_ld();
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             float4* dst = my_flush + (size_t)(c / 4 + i) * kRows;
-                            float4 v = make_float4(__uint_as_float(r[4 * i]), __uint_as_float(r[4 * i + 1]),
-                                                   __uint_as_float(r[4 * i + 2]), __uint_as_float(r[4 * i + 3]));
+                            float4 v = make_float4(__uint_as_float(q[4 * i]), __uint_as_float(q[4 * i + 1]),
+                                                   __uint_as_float(q[4 * i + 2]), __uint_as_float(q[4 * i + 3]));
+                            if (grow) {
+                                red_add4(dst, v.x, v.y, v.z, v.w);
+                                continue;
+                            }
                             if (n > kFlush) {
                                 const float4 o = __ldcg(dst);
                                 v.x = fmaf(o.x, keep, v.x); v.y = fmaf(o.y, keep, v.y);
@@ -511,43 +516,30 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     if (n > 0 && !empty_now) {
 #pragma unroll 1
                         for (int c = 0; c < kHeadDim; c += 16) {
-                            uint32_t r[16];
-                            tmem_ld16(to + c, r);
+                            uint32_t q[16];
+                            tmem_ld16(to + c, q);
                             tmem_wait_ld();
 #pragma unroll
                             for (int i = 0; i < 16; ++i)
-                                r[i] = move ? __float_as_uint(__uint_as_float(r[i]) * f) : r[i];
-                            tmem_st16(to + c, r);
+                                q[i] = move ? __float_as_uint(__uint_as_float(q[i]) * f) : q[i];
+                            tmem_st16(to + c, q);
                         }
                     }
                     m = to_m;
                 }
-                // pass 2: weights, their sum, and P over S: per 16 tokens 8 columns of bf16 pairs high, 8 residual
+                // weights, their sum, and P over S: per 16 tokens 8 columns of bf16 pairs high, 8 residual
                 const float ref = m == -INFINITY ? 0.f : m;
                 float2 la = make_float2(0.f, 0.f), lb = la;
-#pragma unroll 1
-                for (int c = 0; c < kTok; c += 16) {
-                    uint32_t r[16];
-                    tmem_ld16(ts + c, r);
-                    tmem_wait_ld();
-                    if constexpr (CAP && !BIAS) cap_scores(r, a.cap_in, a.cap_log2);
-                    const float far = (float)(t0 + c - (hi - 1));
 #pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const float2 x = make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
-                        float2 y;
-                        if constexpr (CAP) y = add2(x, both(-ref));
-                        else if constexpr (BIAS)
-                            y = fma2(x, both(a.scale_log2), fma2(both(slope2), make_float2(far + (float)i, far + (float)(i + 1)), both(-ref)));
-                        else y = fma2(x, both(a.scale_log2), both(-ref));
-                        r[i] = __float_as_uint(y.x);
-                        r[i + 1] = __float_as_uint(y.y);
-                    }
-                    if (!(CAP && BIAS) && !open) hide(r, t0 + c);
+                for (int c = 0; c < kTok; c += 16) {
                     uint32_t o[16];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float2 p = make_float2(ex2(__uint_as_float(r[2 * i])), ex2(__uint_as_float(r[2 * i + 1])));
+                        float2 p = make_float2(__uint_as_float(r[c + 2 * i]), __uint_as_float(r[c + 2 * i + 1]));
+                        if constexpr (CAP || BIAS) p = add2(p, both(-ref));
+                        else p = fma2(p, both(a.scale_log2), both(-ref));
+                        p.x = ex2(p.x);
+                        p.y = ex2(p.y);
                         if (i & 1) lb = add2(lb, p); else la = add2(la, p);
                         const __nv_bfloat162 h2 = __floats2bfloat162_rn(p.x, p.y);
                         o[i] = *reinterpret_cast<const uint32_t*>(&h2);
@@ -691,9 +683,9 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const uint32_t* offs = a.v_offs + problem * (a.T + 1);
             const uint4* packed = a.v_packed + problem * a.cap_groups * OPG;
             const int64_t limit = a.cap_groups;
-            const int tiles = s.tile1 - s.tile0, first_tok = s.tile0 * kTok + tok0;
+            const int tiles = s.tile1 - s.tile0, last_tok = (s.tile1 - 1) * kTok + tok0;
             auto fetch = [&](int h, uint32_t& m, uint32_t& first) {        // this lane's token mask, the warp's first group
-                const int t = first_tok + h * kTok;
+                const int t = last_tok - h * kTok;
                 m = h < tiles && t + lane < s.len ? mask_row[t + lane] : 0u;
                 first = h < tiles && t < s.len ? offs[t] : 0u;
             };
