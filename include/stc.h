@@ -437,7 +437,7 @@ int32_t stc_decode_attn_scored(const stc_shape* shape, const stc_cache* cache, c
  * With own_out / own_lse (f32 [n_rows][Hq][128] / [n_rows][Hq], e.g. stc_decode_attn's out and lse over the
  * sequence's own tokens) the two are joined:
  *     L = log(e^lse + e^own_lse),  out = e^{lse-L} out + e^{own_lse-L} own_out,  lse = L;
- * out may be own_out and lse_opt own_lse.  A side with lse = -inf contributes nothing, whatever its out holds; with
+ * out and lse_opt must not overlap own_out and own_lse.  A side with lse = -inf contributes nothing, whatever its out holds; with
  * nothing on either side out = 0 and lse = -inf.  Keys of tokens that no row sees may hold anything; packed
  * values of all valid tokens must be finite.
  *   q          bf16 [n_rows][Hq][128]   one row per query token: several tokens of a sequence are several rows

@@ -28,9 +28,14 @@
 // Roles (16 warps): warp 0 = TMA producer of Q and K; warps 1, 2 = MMA issuers of the two groups; warps 4..7 and
 // 8..11 = softmax of the two groups, thread = row; warps 12..15 rebuild the value tiles with 16-byte asynchronous
 // copies straight from the packed store into the swizzled tile.  Two row tiles: group w owns row tile w and both see
-// every token tile.  One row tile: the groups take the token tiles in turn, each with its own running
-// maximum, sum and accumulator, joined at the end of the segment.  A group has two S buffers: the product for its next
-// tile runs while it works on this one, and its softmax waits for nothing else unless the maximum moves.
+// every token tile.  One row tile: the groups take the token tiles in turn.  A group has two S buffers: the product for
+// its next tile runs while it works on this one, and its softmax waits for nothing else unless the maximum moves.
+// Few rows: a row tile is four quarters of 32 lanes (the lanes of one warp), and the softmax of a row is 64 scores of
+// one thread, so half-empty tiles would cost as much as full ones.  With at most two quarters of rows the tile holds
+// them twice, with at most one four times (rep = 2, 4); copy i weighs columns [i, i + 1) * 64 / rep and
+// writes zeros for the others, so each thread has 64 / rep scores and its own part of the sums.
+// Every (group, copy) thus keeps a running maximum, sum and accumulator of its own; they are joined like the
+// partials of different CTAs.
 //
 // The running maximum only moves when a tile exceeds it by more than 2^8, so the accumulator in tensor memory is
 // rescaled a few times per segment and not per tile; weights are then at most 2^8, far from fp32's limits.
@@ -40,6 +45,8 @@
 //
 // Every wait is bounded (about a second); one that expires raises a CTA-wide flag and STC_ERR_TIMEOUT in the
 // status word, the roles leave, the producer waits (bounded) for its copies, tensor memory is freed.
+#include <type_traits>
+
 #include "umma.cuh"
 
 namespace stc {
@@ -55,17 +62,19 @@ constexpr uint32_t kQTile = 2 * kQHalf;           // 32 KiB
 constexpr uint32_t kHalf = kTok * 128;            // 64 channels of a token tile
 constexpr uint32_t kTile = 2 * kHalf;             // 16 KiB
 constexpr uint32_t kOffK = 2 * kQTile, kOffV = kOffK + kKStages * kTile, kOffCtl = kOffV + kVStages * kTile;
-constexpr uint32_t kCtlBytes = 512 + 2 * kRows * 8;
+constexpr uint32_t kCtlBytes = 512;
 constexpr uint32_t kSmem = kOffCtl + kCtlBytes;
 static_assert(kSmem <= 232448, "shared memory of a block");
 constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;                     // log2 units the maximum may be exceeded by
 
-// barriers, in 8-byte words of the control block; [2] = per group, empties [stage][group]
+// barriers, in 8-byte words of the control block; [2] = per group, empties [stage][group], S / P / O [group][buffer].
+// A waiter may be two products behind (its group has two buffers), which one barrier's parity could not tell from none:
+// hence one O barrier per buffer, whose earlier use the waiter always knows to be through.
 enum { kQFull, kQEmpty, kKFull = kQEmpty + 2, kKEmpty = kKFull + kKStages, kVFull = kKEmpty + 2 * kKStages,
        kVEmpty = kVFull + kVStages, kSFull = kVEmpty + 2 * kVStages, kPFull = kSFull + 4, kOFull = kPFull + 4,
-       kXchg = kOFull + 2, kBars };
+       kXchg = kOFull + 4, kBars };
 static_assert(kBars * 8 <= 448, "control block");
 constexpr uint32_t kCtlTmem = 448, kCtlAbort = 452, kCtlPlan = 456;    // tensor-memory address, abort flag, 4 x 8 bytes
 
@@ -82,12 +91,13 @@ struct PrefixArgs {
     int32_t* cta_status;         // [grid], one word per CTA
     int32_t* status;             // the call's status word, written by the second kernel
     long long* base;             // [G + 2]: first flat tile of each prefix; [G] = total; [G + 1] = 1 if row_start is bad
-    float4* part_o;              // [2 * grid][32 chunks of 4 dims][slot_rows]
-    float2* part_ml;             // [2 * grid][slot_rows]
+    float4* part_o;              // [3 * grid][2 groups][32 chunks of 4 dims][128 lanes]
+    float2* part_ml;             // [3 * grid][2][128]
     float4* flush;               // [grid][2 groups][32][128 rows]: sums of emptied accumulators
     int64_t cap_groups;
-    int G, Hq, Hkv, Gq, T, n_rows, slot_rows;
-    int seqs;                    // sequences per row tile = 128 / Gq
+    int G, Hq, Hkv, Gq, T, n_rows;
+    int quarter;                 // sequences per quarter of a row tile = 32 / Gq
+    int seqs;                    // sequences per row tile = 4 * quarter
     float scale_log2, cap_in, cap_log2;
     ScoreArgs sc;
 };
@@ -120,6 +130,14 @@ struct Segment {
     int g, hk, row0, n_seq, len, tile0, tile1;
     int slot;                    // partial slot, -1 = the whole unit
 };
+// Copies of its rows that the row tile of a segment holds.
+__device__ __forceinline__ int copies(const PrefixArgs& a, int n_seq) {
+    return n_seq <= a.quarter ? 4 : n_seq <= 2 * a.quarter ? 2 : 1;
+}
+__device__ __forceinline__ long long div_small(long long x, int d) {        // x >= 0, d > 0
+    return (x >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)d) : x / d;
+}
+
 // Walks the segments of the CTA's range [x, x_end).
 struct Walker {
     long long x, x_end, x_begin, off;  // off = x - base of group g
@@ -133,11 +151,11 @@ struct Walker {
             off -= group_tiles(a, grp);
             grp = load_group(a, ++g);
         }
-        const long long unit = off / grp.tiles;
+        const long long unit = div_small(off, grp.tiles);
         s.tile0 = (int)(off - unit * grp.tiles);
         const long long left = x_end - x;
         s.tile1 = (int)min((long long)grp.tiles, s.tile0 + left);
-        s.hk = (int)(unit / grp.blocks);
+        s.hk = (int)div_small(unit, grp.blocks);
         const int blk = (int)(unit - (long long)s.hk * grp.blocks);
         s.g = g;
         s.row0 = grp.row0 + blk * 2 * a.seqs;
@@ -173,15 +191,16 @@ __device__ __forceinline__ float bias_shift(const PrefixArgs& a, int len, int se
     return a.sc.slopes[head] * (float)(hi - 1 - pos);
 }
 
-// Caps the 64 scores of a row (raw products in, log2 units out).  Scores far below the cap, the usual case, need only the
+// Caps N scores of a row (raw products in, log2 units out).  Scores far below the cap, the usual case, need only the
 // polynomial of tanh_f32, two at a time; the warp votes once per tile instead of branching per score.
-__device__ __forceinline__ void cap_scores(uint32_t (&r)[kTok], float cap_in, float cap_log2) {
+template <int N>
+__device__ __forceinline__ void cap_scores(uint32_t (&r)[N], float cap_in, float cap_log2) {
     float big = 0.f;
 #pragma unroll
-    for (int i = 0; i < kTok; ++i) big = fmaxf(big, fabsf(__uint_as_float(r[i])));
+    for (int i = 0; i < N; ++i) big = fmaxf(big, fabsf(__uint_as_float(r[i])));
     if (__all_sync(0xFFFFFFFFu, big * fabsf(cap_in) <= kTanhSmall)) {
 #pragma unroll
-        for (int i = 0; i < kTok; i += 2) {          // tanh_small
+        for (int i = 0; i < N; i += 2) {          // tanh_small
             const float2 z = mul2(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), both(cap_in));
             const float2 u = mul2(z, z);
             float2 p = fma2(both(kTanh4), u, both(kTanh3));
@@ -194,7 +213,7 @@ __device__ __forceinline__ void cap_scores(uint32_t (&r)[kTok], float cap_in, fl
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < kTok; ++i) {
+        for (int i = 0; i < N; ++i) {
             const float z = __uint_as_float(r[i]) * cap_in, lo = tanh_small(z), hi = tanh_large(z);
             r[i] = __float_as_uint(cap_log2 * (fabsf(z) <= kTanhSmall ? lo : hi));
         }
@@ -215,7 +234,6 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctl + kCtlTmem);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + kCtlAbort);
     volatile long long* plan = reinterpret_cast<volatile long long*>(ctl + kCtlPlan);  // x, x_end, off, g
-    float2* ml = reinterpret_cast<float2*>(ctl + 512);                                // [2][128]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     // ---- set-up: barriers, tensor memory, this CTA's range ------------------------------------------
@@ -308,9 +326,13 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const bool two = s.n_seq > a.seqs;
                 if (seg > 0 && !(wait(kQEmpty, (uint32_t)(seg - 1)) && wait(kQEmpty + 1, (uint32_t)(seg - 1)))) { ok = false; break; }
                 mbar_expect_tx(bar(kQFull), two ? 2 * q_bytes : q_bytes);
-                for (int i = 0; i < (two ? 2 : 1); ++i)
-                    for (int h = 0; h < 2; ++h)
-                        tma_3d(base + i * kQTile + h * kQHalf, &map_q, 64 * h, s.hk * a.Gq, s.row0 + i * a.seqs, bar(kQFull));
+                const int quarters = 4 / copies(a, s.n_seq);
+#pragma unroll 1
+                for (int i = 0; i < (two ? 16 : 8); ++i) {                         // (row tile, half, quarter)
+                    const int q = i & 3, h = (i >> 2) & 1, tile = i >> 3;
+                    tma_3d(base + tile * kQTile + h * kQHalf + q * (kQHalf / 4), &map_q, 64 * h, s.hk * a.Gq,
+                           s.row0 + tile * a.seqs + (q % quarters) * a.quarter, bar(kQFull));
+                }
                 ++seg;
                 const int row = (s.g * a.Hkv + s.hk) * a.T;
                 int st = kc % kKStages;
@@ -374,7 +396,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             tc_mma_ts(to, p + 16 * k, dv + (uint64_t)(k * (2048 >> 4)), id_pv, k ? 1u : more);
                             tc_mma_ts(to, p + 16 * k + 8, dv + (uint64_t)(k * (2048 >> 4)), id_pv, 1);
                         }
-                        tc_commit_to(bar(kOFull + w));
+                        tc_commit_to(bar(kOFull + 2 * w + buf));
                         tc_commit_to(bar(kVEmpty + 2 * st + w));
                         ++n_o;
                     }
@@ -382,8 +404,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         const uint32_t j = first + (uint32_t)n * stride, st = j % kKStages, buf = n_s & 1u;
                         ok = wait(kKFull + st, j / kKStages);
                         // the buffer holds the P of the group's last but one tile until that product is through
-                        // (at a segment's start both of its predecessors may be through: the later one is asked for)
-                        if (ok && n_s >= 2) ok = wait(kOFull + w, n == 0 ? n_s - 1 : n_s - 2);
+                        if (ok && n_s >= 2) ok = wait(kOFull + 2 * w + buf, (n_s - 2) >> 1);
                         if (!ok) break;
                         tc_after();
                         const uint64_t dk = smem_desc_128(base + kOffK + st * kTile, 16);
@@ -403,35 +424,40 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (!ok) give_up();
         }
     } else if (warp >= 4 && warp < 12) {
-        // ---- softmax: thread = row -----------------------------------------------------------------------
-        const int w = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
-        const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        // ---- softmax: thread = row of the tile's lanes --------------------------------------------------------
+        const int w = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
         const uint32_t to = lane_base + 256 + w * 128;
         float4* const my_flush = a.flush + ((size_t)blockIdx.x * 2 + w) * 32 * kRows + row;
         uint32_t n_s = 0, n_x = 0;                   // tiles of this group; uses of the exchange barrier
         bool ok = true;
-        while (ok && walk.next(a, s)) {
+
+        // One segment with 64 / COLS copies of the rows; this thread weighs COLS of a tile's 64 scores.
+        auto segment = [&](auto cols) {
+            constexpr int COLS = decltype(cols)::value, REP = kTok / COLS;
             const int tiles = s.tile1 - s.tile0;
             const bool two = s.n_seq > a.seqs;
-            const int mine = two ? tiles : (tiles + 1 - w) >> 1, stride = two ? 1 : 2, first = s.tile1 - 1 - (two ? 0 : w);
-            // this thread's row: sequence and head
-            const int in_tile = row / a.Gq, seq_i = (two ? w * a.seqs : 0) + in_tile;
-            const bool live = in_tile < a.seqs && seq_i < s.n_seq;
-            const int seq = s.row0 + (live ? seq_i : 0), head = s.hk * a.Gq + row % a.Gq;
+            const int mine = two ? tiles : (tiles + 1 - w) >> 1, stride = two ? 1 : 2, last = s.tile1 - 1 - (two ? 0 : w);
+            // this thread's row: sequence, head, copy
+            const int copy = quarter / (4 / REP), c0 = copy * COLS;
+            const int in_quarter = lane / a.Gq, seq_i = (two ? w * a.seqs : 0) + (quarter % (4 / REP)) * a.quarter + in_quarter;
+            const bool live = in_quarter < a.quarter && seq_i < s.n_seq;
+            const bool warp_live = __any_sync(0xFFFFFFFFu, live);
+            const int seq = s.row0 + (live ? seq_i : 0), head = s.hk * a.Gq + lane % a.Gq;
             int lo = 0, hi = s.len, my_doc = 0;
             float slope2 = 0.f;
             if (a.sc.q_pos) visible_range(s.len, a.sc.q_pos[seq], a.sc.window, lo, hi);
             if (BIAS && a.sc.slopes) slope2 = a.sc.slopes[head] * kLog2e;
             const int32_t* doc = a.sc.tok_doc ? a.sc.tok_doc + (size_t)s.g * a.T : nullptr;
             if (doc) my_doc = a.sc.q_doc[seq];
-            // -inf for the tokens t .. t + 63 that the row does not see
-            auto hide = [&](uint32_t (&r)[kTok], int t) {
+            // -inf for the tokens t .. t + COLS - 1 that the row does not see
+            auto hide = [&](uint32_t (&r)[COLS], int t) {
 #pragma unroll
-                for (int i = 0; i < kTok; ++i)
+                for (int i = 0; i < COLS; ++i)
                     if (t + i < lo || t + i >= hi) r[i] = __float_as_uint(-INFINITY);
                 if (doc) {
 #pragma unroll
-                    for (int i = 0; i < kTok; ++i) {
+                    for (int i = 0; i < COLS; ++i) {
                         const int d = __ldg(doc + min(t + i, a.T - 1));
                         if (d >= 0 && d != my_doc) r[i] = __float_as_uint(-INFINITY);
                     }
@@ -441,22 +467,63 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll 1
             for (int n = 0; n < mine; ++n) {
                 const uint32_t buf = n_s & 1u, ts = lane_base + w * 128 + buf * 64;
+                if (!warp_live) {                    // a quarter without rows: its P may be anything
+                    ok = warp_wait(kSFull + 2 * w + buf, n_s >> 1);
+                    if (!ok) return;
+                    mbar_arrive(bar(kPFull + 2 * w + buf));
+                    ++n_s;
+                    continue;
+                }
+                // After kFlush tiles the accumulator is emptied into fp32 sums (with the maximum it was built with), and
+                // the issuer starts it anew
+                const bool empty_now = n > 0 && n % kFlush == 0;
+                if (empty_now) {
+                    ok = warp_wait(kOFull + 2 * w + ((n_s - 1) & 1u), (n_s - 1) >> 1);
+                    if (!ok) return;
+                    tc_after();
+                    const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
+#pragma unroll 1
+                    for (int c = 0; c < kHeadDim; c += 32) {
+                        float4 old[8];
+                        if (n > kFlush) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) old[i] = __ldcg(my_flush + (size_t)(c / 4 + i) * kRows);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) old[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        }
+                        uint32_t q[32];
+                        tmem_ld16<0>(to + c, q);
+                        tmem_ld16<16>(to + c + 16, q);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            __stcg(my_flush + (size_t)(c / 4 + i) * kRows,
+                                   make_float4(fmaf(old[i].x, keep, __uint_as_float(q[4 * i])),
+                                               fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1])),
+                                               fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2])),
+                                               fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3]))));
+                    }
+                    m_flush = m;
+                }
                 ok = warp_wait(kSFull + 2 * w + buf, n_s >> 1);
-                if (!ok) break;
+                if (!ok) return;
                 tc_after();
-                const int t0 = (first - n * stride) * kTok;
-                uint32_t r[kTok];
-                tmem_ld16<0>(ts, r);
-                tmem_ld16<16>(ts + 16, r);
-                tmem_ld16<32>(ts + 32, r);
-                tmem_ld16<48>(ts + 48, r);
+                const int t0 = (last - n * stride) * kTok + c0;
+                uint32_t r[COLS];
+                tmem_ld16<0>(ts + c0, r);
+                if constexpr (COLS > 16) tmem_ld16<16>(ts + c0 + 16, r);
+                if constexpr (COLS > 32) {
+                    tmem_ld16<32>(ts + c0 + 32, r);
+                    tmem_ld16<48>(ts + c0 + 48, r);
+                }
                 tmem_wait_ld();
                 // scores in log2 units where they are not the raw products times a positive scale
                 if constexpr (CAP) cap_scores(r, a.cap_in, a.cap_log2);
                 if constexpr (BIAS) {
                     const float far = (float)(t0 - (hi - 1));
 #pragma unroll
-                    for (int i = 0; i < kTok; i += 2) {
+                    for (int i = 0; i < COLS; i += 2) {
                         float2 x = make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
                         if constexpr (!CAP) x = mul2(x, both(a.scale_log2));
                         x = fma2(both(slope2), add2(both(far), make_float2((float)i, (float)(i + 1))), x);
@@ -464,56 +531,24 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         r[i + 1] = __float_as_uint(x.y);
                     }
                 }
-                // does every row of the warp see the whole tile?
-                if (doc || !__all_sync(0xFFFFFFFFu, lo <= t0 && hi >= t0 + kTok)) hide(r, t0);
+                // does every row of the warp see all the tokens?
+                if (doc || !__all_sync(0xFFFFFFFFu, lo <= t0 && hi >= t0 + COLS)) hide(r, t0);
                 float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int i = 0; i < kTok; i += 2)
+                for (int i = 0; i < COLS; i += 2)
                     t4[(i >> 1) & 3] = fmaxf(fmaxf(t4[(i >> 1) & 3], __uint_as_float(r[i])), __uint_as_float(r[i + 1]));
                 float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
                 if constexpr (!CAP && !BIAS) top *= a.scale_log2;     // (-inf stays -inf: the scale is positive)
-                // move the maximum only if it is exceeded by much; the accumulator follows.  After kFlush tiles it is
-                // emptied first (with the maximum it was built with), and the issuer starts it anew
+                // move the maximum only if it is exceeded by much; the accumulator follows
                 const bool move = top > m + kSlack || (m == -INFINITY && top > -INFINITY);
-                const bool any_move = __any_sync(0xFFFFFFFFu, move), empty_now = n > 0 && n % kFlush == 0;
-                if (n > 0 && (any_move || empty_now)) {
-                    ok = warp_wait(kOFull + w, n_s - 1);
-                    if (!ok) break;
-                    tc_after();
-                }
-                if (empty_now) {
-                    // (uniform maxima: the sums only grow by this accumulator, and nothing has to be read back)
-                    const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
-                    const bool grow = n > kFlush && __all_sync(0xFFFFFFFFu, keep == 1.f);
-#pragma unroll 1
-                    for (int c = 0; c < kHeadDim; c += 16) {
-                        uint32_t q[16];
-                        tmem_ld16(to + c, q);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float4* dst = my_flush + (size_t)(c / 4 + i) * kRows;
-                            float4 v = make_float4(__uint_as_float(q[4 * i]), __uint_as_float(q[4 * i + 1]),
-                                                   __uint_as_float(q[4 * i + 2]), __uint_as_float(q[4 * i + 3]));
-                            if (grow) {
-                                red_add4(dst, v.x, v.y, v.z, v.w);
-                                continue;
-                            }
-                            if (n > kFlush) {
-                                const float4 o = __ldcg(dst);
-                                v.x = fmaf(o.x, keep, v.x); v.y = fmaf(o.y, keep, v.y);
-                                v.z = fmaf(o.z, keep, v.z); v.w = fmaf(o.w, keep, v.w);
-                            }
-                            __stcg(dst, v);
-                        }
-                    }
-                    m_flush = m;
-                }
-                if (any_move) {
+                if (__any_sync(0xFFFFFFFFu, move)) {
                     const float to_m = move ? top : m;
-                    const float f = (m == -INFINITY) ? 0.f : exp2f(m - to_m);
+                    const float f = (m == -INFINITY) ? 0.f : ex2(m - to_m);
                     l *= f;
                     if (n > 0 && !empty_now) {
+                        ok = warp_wait(kOFull + 2 * w + ((n_s - 1) & 1u), (n_s - 1) >> 1);
+                        if (!ok) return;
+                        tc_after();
 #pragma unroll 1
                         for (int c = 0; c < kHeadDim; c += 16) {
                             uint32_t q[16];
@@ -531,7 +566,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const float ref = m == -INFINITY ? 0.f : m;
                 float2 la = make_float2(0.f, 0.f), lb = la;
 #pragma unroll
-                for (int c = 0; c < kTok; c += 16) {
+                for (int c = 0; c < COLS; c += 16) {
                     uint32_t o[16];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -547,7 +582,14 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         const __nv_bfloat162 r2 = __floats2bfloat162_rn(d.x, d.y);
                         o[8 + i] = *reinterpret_cast<const uint32_t*>(&r2);
                     }
-                    tmem_st16(ts + c, o);
+                    tmem_st16(ts + c0 + c, o);
+                }
+                if constexpr (REP > 1) {             // the columns of the other copies
+                    uint32_t zero[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) zero[i] = 0u;
+#pragma unroll
+                    for (int c = 0; c < kTok - COLS; c += 16) tmem_st16(ts + ((c0 + COLS + c) & (kTok - 1)), zero);
                 }
                 l += (la.x + lb.x) + (la.y + lb.y);
                 tmem_wait_st();
@@ -555,107 +597,125 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 mbar_arrive(bar(kPFull + 2 * w + buf));
                 ++n_s;
             }
-            if (!ok) break;
-            // ---- end of the segment -----------------------------------------------------------------------
-            if (mine > 0) {
-                ok = warp_wait(kOFull + w, n_s - 1);
-                if (!ok) break;
-                tc_after();
-            }
-            if (mine > kFlush) {                     // take back what the accumulator was emptied of
-                const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
-#pragma unroll 1
-                for (int c = 0; c < kHeadDim; c += 16) {
-                    uint32_t r[16];
-                    tmem_ld16(to + c, r);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float4 o = __ldcg(my_flush + (size_t)(c / 4 + i) * kRows);
-                        r[4 * i] = __float_as_uint(fmaf(o.x, keep, __uint_as_float(r[4 * i])));
-                        r[4 * i + 1] = __float_as_uint(fmaf(o.y, keep, __uint_as_float(r[4 * i + 1])));
-                        r[4 * i + 2] = __float_as_uint(fmaf(o.z, keep, __uint_as_float(r[4 * i + 2])));
-                        r[4 * i + 3] = __float_as_uint(fmaf(o.w, keep, __uint_as_float(r[4 * i + 3])));
-                    }
-                    tmem_st16(to + c, r);
-                }
-                tmem_wait_st();
-            }
+            // ---- end of the segment: this thread's (m, l, accumulator) ------------------------------------------
+            const bool whole = s.slot < 0, finish = whole && two;      // a row of a whole unit that is complete here
             const size_t out_row = (size_t)seq * a.Hq + head;
-            // read before the exchange: own_lse and lse may be one array, and the other group writes lse behind it
-            const float own_l = s.slot < 0 && a.own_lse ? a.own_lse[out_row] : 0.f;
-            float mo = m, lo_sum = l, f0 = 1.f, f1 = 0.f;   // joined maximum and sum; factors of accumulator 0 / 1
-            bool has1 = false;
-            int c_lo = 0, c_hi = kHeadDim;                   // dims this thread writes
-            uint32_t acc0 = to, acc1 = to;
-            if (!two) {                              // both groups hold part of the same rows: join, half the dims each
-                ml[w * kRows + row] = make_float2(m, l);
-                tc_before();
-                mbar_arrive(bar(kXchg));
-                ok = warp_wait(kXchg, n_x++);
-                if (!ok) break;
+            const float own_l = whole && a.own_lse && live ? a.own_lse[out_row] : -INFINITY;
+            const Join j = finish ? join(m, l, BIAS ? bias_shift(a, s.len, seq, head) : 0.f, a.own_lse != nullptr, own_l)
+                                  : Join{1.f, 0.f, 0.f};
+            const size_t slot = (size_t)(whole ? 2 * (int)gridDim.x + (int)blockIdx.x : s.slot) * 2;
+            if (!finish) __stcg(a.part_ml + (slot + w) * kRows + row, make_float2(m, l));
+            else if (live && a.lse) a.lse[out_row] = j.lse;
+            if (mine > 0 && warp_live) {
+                ok = warp_wait(kOFull + 2 * w + ((n_s - 1) & 1u), (n_s - 1) >> 1);
+                if (!ok) return;
                 tc_after();
-                const float2 a0 = ml[row], a1 = ml[kRows + row];
-                mo = fmaxf(a0.x, a1.x);
-                f0 = a0.x == -INFINITY ? 0.f : exp2f(a0.x - mo);
-                f1 = a1.x == -INFINITY ? 0.f : exp2f(a1.x - mo);
-                lo_sum = a0.y * f0 + a1.y * f1;
-                has1 = tiles > 1;
-                acc0 = lane_base + 256;
-                acc1 = lane_base + 384;
-                c_lo = 64 * w;
-                c_hi = c_lo + 64;
-            }
-            float fo = 1.f, fown = 0.f;
-            const float4* own = nullptr;
-            float4* dst;
-            size_t step;                             // from one chunk of four dims to the next
-            if (s.slot < 0) {
-                const Join j = join(mo, lo_sum, BIAS ? bias_shift(a, s.len, seq, head) : 0.f, a.own_lse != nullptr, own_l);
-                fo = j.fo;
-                fown = j.fown;
-                if (a.own_out && fown != 0.f) own = reinterpret_cast<const float4*>(a.own_out + out_row * kHeadDim);
-                dst = reinterpret_cast<float4*>(a.out + out_row * kHeadDim);
-                step = 1;
-                if (live && a.lse && c_lo == 0) a.lse[out_row] = j.lse;
-            } else {
-                const int part_row = (two ? w * a.seqs * a.Gq : 0) + row;
-                dst = a.part_o + (size_t)s.slot * 32 * a.slot_rows + part_row;
-                step = a.slot_rows;
-                if (live && c_lo == 0) a.part_ml[(size_t)s.slot * a.slot_rows + part_row] = make_float2(mo, lo_sum);
-            }
+                const bool flushed = mine > kFlush;
+                const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
+                const bool add_own = finish && live && a.own_out && j.fown != 0.f;
+                const float4* own = reinterpret_cast<const float4*>(a.own_out) + out_row * 32;
+                float4* dst = finish ? reinterpret_cast<float4*>(a.out) + out_row * 32 : a.part_o + (slot + w) * 32 * kRows + row;
+                const int step = finish ? 1 : kRows;
 #pragma unroll 1
-            for (int c = c_lo; c < c_hi; c += 16) {
-                uint32_t r0[16], r1[16];
-                tmem_ld16(acc0 + c, r0);
-                if (has1) tmem_ld16(acc1 + c, r1);
-                tmem_wait_ld();
-                if (live) {
+                for (int c = 0; c < kHeadDim; c += 32) {
+                    float4 old[8];
+                    if (flushed) {
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        float v[4];
+                        for (int i = 0; i < 8; ++i) old[i] = __ldcg(my_flush + (size_t)(c / 4 + i) * kRows);
+                    }
+                    uint32_t q[32];
+                    tmem_ld16<0>(to + c, q);
+                    tmem_ld16<16>(to + c + 16, q);
+                    tmem_wait_ld();
+                    if (flushed) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            v[e] = f0 != 0.f ? __uint_as_float(r0[i + e]) * f0 : 0.f;
-                            if (has1 && f1 != 0.f) v[e] = fmaf(__uint_as_float(r1[i + e]), f1, v[e]);
-                            v[e] = fo != 0.f ? v[e] * fo : 0.f;
+                        for (int i = 0; i < 8; ++i) {
+                            q[4 * i] = __float_as_uint(fmaf(old[i].x, keep, __uint_as_float(q[4 * i])));
+                            q[4 * i + 1] = __float_as_uint(fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1])));
+                            q[4 * i + 2] = __float_as_uint(fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2])));
+                            q[4 * i + 3] = __float_as_uint(fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3])));
                         }
-                        float4 v4 = make_float4(v[0], v[1], v[2], v[3]);
-                        if (own) {
-                            const float4 w4 = own[(c + i) / 4];
-                            v4.x = fmaf(w4.x, fown, v4.x); v4.y = fmaf(w4.y, fown, v4.y);
-                            v4.z = fmaf(w4.z, fown, v4.z); v4.w = fmaf(w4.w, fown, v4.w);
+                    }
+                    if (add_own) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) old[i] = own[c / 4 + i];
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) old[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+                    if (live || !finish) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            float4 v = make_float4(__uint_as_float(q[4 * i]), __uint_as_float(q[4 * i + 1]),
+                                                   __uint_as_float(q[4 * i + 2]), __uint_as_float(q[4 * i + 3]));
+                            if (finish) {            // (a factor 0 stands for "nothing seen", whatever was summed)
+                                if (j.fo == 0.f) v = make_float4(0.f, 0.f, 0.f, 0.f);
+                                v.x = fmaf(old[i].x, j.fown, v.x * j.fo); v.y = fmaf(old[i].y, j.fown, v.y * j.fo);
+                                v.z = fmaf(old[i].z, j.fown, v.z * j.fo); v.w = fmaf(old[i].w, j.fown, v.w * j.fo);
+                            }
+                            dst[(size_t)(c / 4 + i) * step] = v;
                         }
-                        dst[(size_t)((c + i) / 4) * step] = v4;
                     }
                 }
-            }
-            if (!two) {                              // the other group's accumulator and the exchange are free again
                 tc_before();
-                mbar_arrive(bar(kXchg));
-                ok = warp_wait(kXchg, n_x++);
-                tc_after();
             }
+            if (!whole || two) return;
+            // ---- a whole unit of one row tile: the 2 * REP threads of a row join their parts, 16 / REP chunks of four dims each
+            __threadfence();
+            mbar_arrive(bar(kXchg));
+            ok = warp_wait(kXchg, n_x++);
+            if (!ok) return;
+            constexpr int E = 2 * REP, CH = 32 / E;
+            const int lane0 = (quarter % (4 / REP)) * 32 + lane, d0 = (w * REP + copy) * CH;
+            if (live) {
+                float fe[E], top = -INFINITY, sum = 0.f;
+                float2 p[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) p[e] = __ldcg(a.part_ml + (slot + e / REP) * kRows + lane0 + (e % REP) * (kRows / REP));
+#pragma unroll
+                for (int e = 0; e < E; ++e) top = fmaxf(top, p[e].x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    fe[e] = p[e].x == -INFINITY ? 0.f : ex2(p[e].x - top);
+                    sum = fmaf(p[e].y, fe[e], sum);
+                }
+                const Join jj = join(top, sum, BIAS ? bias_shift(a, s.len, seq, head) : 0.f, a.own_lse != nullptr, own_l);
+                float4* dst = reinterpret_cast<float4*>(a.out) + out_row * 32 + d0;
+                const float4* own = reinterpret_cast<const float4*>(a.own_out) + out_row * 32 + d0;
+                constexpr int BATCH = E == 8 ? 2 : 4;
+#pragma unroll 1
+                for (int d = 0; d < CH; d += BATCH) {
+                    float4 v[BATCH][E], o[BATCH];
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            v[i][e] = fe[e] == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                                   : __ldcg(a.part_o + ((slot + e / REP) * 32 + d0 + d + i) * kRows + lane0 + (e % REP) * (kRows / REP));
+                        o[i] = a.own_out && jj.fown != 0.f ? own[d + i] : make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+                        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            x.x = fmaf(v[i][e].x, fe[e], x.x); x.y = fmaf(v[i][e].y, fe[e], x.y);
+                            x.z = fmaf(v[i][e].z, fe[e], x.z); x.w = fmaf(v[i][e].w, fe[e], x.w);
+                        }
+                        dst[d + i] = make_float4(fmaf(o[i].x, jj.fown, x.x * jj.fo), fmaf(o[i].y, jj.fown, x.y * jj.fo),
+                                                 fmaf(o[i].z, jj.fown, x.z * jj.fo), fmaf(o[i].w, jj.fown, x.w * jj.fo));
+                    }
+                }
+                if (a.lse && d0 == 0) a.lse[out_row] = jj.lse;
+            }
+            mbar_arrive(bar(kXchg));                 // the scratch slot is free again
+            ok = warp_wait(kXchg, n_x++);
+        };
+        while (ok && walk.next(a, s)) {
+            const int n_copies = copies(a, s.n_seq);
+            if (n_copies == 1) segment(std::integral_constant<int, 64>{});
+            else if (n_copies == 2) segment(std::integral_constant<int, 32>{});
+            else segment(std::integral_constant<int, 16>{});
         }
         if (!ok) give_up();
     } else if (warp >= 12) {
@@ -745,21 +805,23 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
 // Joins the partials of units that more than one CTA worked on, answers the rows whose prefix is empty, and gathers the
 // CTAs' status.  A block owns eight consecutive rows of a KV head (row = sequence * Gq + head within the KV
-// head), a thread four channels of one of them: 8 rows x 16 bytes are one 128-byte line of a partial, and 4 x 16
-// bytes of a row are written together.  Partials are taken in CTA order, four loads in flight.
+// head) and four chunks of four dims, a thread one of each (8 rows x 16 bytes are mostly one 128-byte line of a partial);
+// its eight warps share the partials of the rows, in a fixed order, four loads in flight.
 __global__ void __launch_bounds__(256)
 prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
+    __shared__ float4 sh_o[8][32];
+    __shared__ float2 sh_ml[8][32];
     const bool bad = a.base[a.G + 1] != 0;
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-        int st = bad ? (int)STC_ERR_INVALID_ARG : (int)STC_OK;
-        for (int c = 0; c < grid; ++c)
-            if (a.cta_status[c] != 0) st = a.cta_status[c];
-        *a.status = st;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 32) {
+        int st = 0;
+        for (int c = threadIdx.x; c < grid; c += 32) st = max(st, a.cta_status[c]);
+        st = __reduce_max_sync(0xFFFFFFFFu, st);
+        if (threadIdx.x == 0) *a.status = bad ? (int)STC_ERR_INVALID_ARG : st;
     }
-    const int hk = blockIdx.x / chunks;
-    const long long flat = (long long)(blockIdx.x - hk * chunks) * 8 + ((threadIdx.x & 31) >> 2);
-    const int d4 = (threadIdx.x >> 5) * 4 + (threadIdx.x & 3);
-    const int seq = (int)(flat / a.Gq), head = hk * a.Gq + (int)(flat - (long long)seq * a.Gq);
+    const int hk = blockIdx.x / chunks, part = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long flat = (long long)(blockIdx.x - hk * chunks) * 8 + (lane >> 2);
+    const int d4 = blockIdx.y * 4 + (lane & 3);
+    const int seq = (int)(flat / a.Gq), in_head = (int)(flat - (long long)seq * a.Gq), head = hk * a.Gq + in_head;
     bool mine = !bad && seq < a.n_rows && seq >= a.row_start[0] && seq < a.row_start[a.G];
     float m = -INFINITY, l = 0.f, shift = 0.f, own_l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f), own = o;
@@ -771,18 +833,24 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
             if (a.row_start[mid] <= seq) g = mid; else g_hi = mid;
         }
         const Group grp = load_group(a, g);
-        const int in_group = seq - grp.row0, blk = in_group / (2 * a.seqs);
-        const int row = (in_group - blk * 2 * a.seqs) * a.Gq + (head - hk * a.Gq);
-        int c0 = 0, c1 = -1, late = 0;
+        const int in_group = seq - grp.row0, blk = in_group / (2 * a.seqs), in_blk = in_group - blk * 2 * a.seqs;
+        const int n_seq = min(2 * a.seqs, grp.n_seq - blk * 2 * a.seqs);
+        const bool two = n_seq > a.seqs;
+        // where the row's parts stand in a slot: lane of its first copy, copies, groups
+        const int tile = two ? in_blk / a.seqs : 0, in_tile = in_blk - tile * a.seqs, qr = in_tile / a.quarter;
+        const int row = qr * 32 + (in_tile - qr * a.quarter) * a.Gq + in_head;
+        const int n_copies = copies(a, n_seq), per_slot = two ? 1 : 2 * n_copies;
+        int c0 = 0, n_parts = 0, late = 0;
         if (grp.tiles > 0) {
             const long long total = a.base[a.G], n = min(total, (long long)grid);
             const long long x0 = a.base[g] + ((long long)hk * grp.blocks + blk) * grp.tiles, x1 = x0 + grp.tiles;
             // the CTA whose range holds tile x is ceil((x + 1) * n / total) - 1; only the first of a unit's CTAs can
             // have begun before the unit, and then used its second slot for it
             c0 = (int)(((x0 + 1) * n + total - 1) / total - 1);
-            c1 = (int)((x1 * n + total - 1) / total - 1);
+            const int c1 = (int)((x1 * n + total - 1) / total - 1);
             late = total * c0 / n < x0 ? 1 : 0;
             mine = c0 != c1;                         // a whole unit was finished where it was computed
+            if (mine) n_parts = (c1 - c0 + 1) * per_slot;
         }
         if (mine) {
             if (a.own_lse) {
@@ -792,20 +860,21 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
             shift = bias_shift(a, grp.len, seq, head);
         }
 #pragma unroll 1
-        for (int c = c0; mine && c <= c1; c += 4) {
+        for (int e0 = part; e0 < n_parts; e0 += 32) {
             float2 p[4];
             float4 v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int cc = min(c + i, c1);
-                const size_t slot = 2 * (size_t)cc + (cc == c0 ? late : 0);
-                p[i] = __ldcg(a.part_ml + slot * a.slot_rows + row);
-                v[i] = __ldcg(a.part_o + (slot * 32 + d4) * a.slot_rows + row);
+                const int e = min(e0 + 8 * i, n_parts - 1), c = e / per_slot, k = e - c * per_slot;
+                const int w = two ? tile : k / n_copies, at = row + (two ? 0 : (k % n_copies) * (kRows / n_copies));
+                const size_t slot = (2 * (size_t)(c0 + c) + (c == 0 ? late : 0)) * 2 + w;
+                p[i] = __ldcg(a.part_ml + slot * kRows + at);
+                v[i] = __ldcg(a.part_o + (slot * 32 + d4) * kRows + at);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (c + i > c1 || p[i].x == -INFINITY) continue;
-                const float top = fmaxf(m, p[i].x), fm = m == -INFINITY ? 0.f : exp2f(m - top), fp = exp2f(p[i].x - top);
+                if (e0 + 8 * i >= n_parts || p[i].x == -INFINITY) continue;
+                const float top = fmaxf(m, p[i].x), fm = m == -INFINITY ? 0.f : ex2(m - top), fp = ex2(p[i].x - top);
                 l = fmaf(p[i].y, fp, l * fm);
                 o.x = fmaf(v[i].x, fp, o.x * fm); o.y = fmaf(v[i].y, fp, o.y * fm);
                 o.z = fmaf(v[i].z, fp, o.z * fm); o.w = fmaf(v[i].w, fp, o.w * fm);
@@ -813,8 +882,21 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
             }
         }
     }
-    __syncthreads();                                 // own_lse and lse may be one array: every thread of a row has read the former
-    if (!mine) return;
+    sh_o[part][lane] = o;
+    sh_ml[part][lane] = make_float2(m, l);
+    __syncthreads();
+    if (part != 0 || !mine) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+        const float2 p = sh_ml[i][lane];
+        const float4 v = sh_o[i][lane];
+        if (p.x == -INFINITY) continue;
+        const float top = fmaxf(m, p.x), fm = m == -INFINITY ? 0.f : ex2(m - top), fp = ex2(p.x - top);
+        l = fmaf(p.y, fp, l * fm);
+        o.x = fmaf(v.x, fp, o.x * fm); o.y = fmaf(v.y, fp, o.y * fm);
+        o.z = fmaf(v.z, fp, o.z * fm); o.w = fmaf(v.w, fp, o.w * fm);
+        m = top;
+    }
     const Join j = join(m, l, shift, a.own_lse != nullptr, own_l);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (j.fo != 0.f) v = make_float4(o.x * j.fo, o.y * j.fo, o.z * j.fo, o.w * j.fo);
@@ -831,16 +913,12 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // The workspace has to be sized without a device, so the partial slots are counted for this many CTAs.
 constexpr int kPlanSms = 148;
 
-int slot_rows(const Geom& g, int n_rows) {
-    const long long rows = (long long)n_rows * g.Gq, most = 2LL * (kRows / g.Gq) * g.Gq;
-    return (int)(rows < most ? rows : most);
-}
+constexpr size_t kSlots = 3 * (size_t)kPlanSms * 2;          // first and last partial and a scratch slot, two groups
 
 }  // namespace
 
-size_t prefix_ws_bytes(const Geom& g, int n_rows) {
-    const size_t slots = 2 * (size_t)kPlanSms * slot_rows(g, n_rows);
-    return 256 + align256(kPlanSms * 4) + align256(((size_t)g.B + 2) * 8) + align256(slots * 8) + slots * kHeadDim * 4 +
+size_t prefix_ws_bytes(const Geom& g, int) {
+    return 256 + align256(kPlanSms * 4) + align256(((size_t)g.B + 2) * 8) + kSlots * kRows * 8 + kSlots * kRows * kHeadDim * 4 +
            2 * (size_t)kPlanSms * kRows * kHeadDim * 4;
 }
 
@@ -853,8 +931,6 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
     a.row_start = row_start; a.seq_len = g.seq_len;
     a.v_mask = v_mask; a.v_offs = v_offs; a.v_packed = static_cast<const uint4*>(v_packed);
     a.own_out = own_out; a.own_lse = own_lse; a.out = out; a.lse = lse;
-    a.slot_rows = slot_rows(g, n_rows);
-    const size_t slots = 2 * (size_t)kPlanSms * a.slot_rows;
     a.status = reinterpret_cast<int32_t*>(w);
     w += 256;
     a.cta_status = reinterpret_cast<int32_t*>(w);
@@ -862,13 +938,14 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
     a.base = reinterpret_cast<long long*>(w);
     w += align256(((size_t)g.B + 2) * 8);
     a.part_ml = reinterpret_cast<float2*>(w);
-    w += align256(slots * 8);
+    w += kSlots * kRows * 8;
     a.part_o = reinterpret_cast<float4*>(w);
-    w += slots * kHeadDim * 4;
+    w += kSlots * kRows * kHeadDim * 4;
     a.flush = reinterpret_cast<float4*>(w);
     a.cap_groups = cap_groups;
     a.G = g.B; a.Hq = g.Hq; a.Hkv = g.Hkv; a.Gq = g.Gq; a.T = g.T; a.n_rows = n_rows;
-    a.seqs = kRows / g.Gq;
+    a.quarter = 32 / g.Gq;
+    a.seqs = 4 * a.quarter;
     a.sc = score ? *score : ScoreArgs{};
     a.scale_log2 = sm_scale * kLog2e;
     a.cap_in = a.sc.softcap > 0.f ? sm_scale / a.sc.softcap : 0.f;
@@ -884,7 +961,7 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
     {
         const cuuint64_t dims[3] = {kHeadDim, (cuuint64_t)g.Hq, (cuuint64_t)n_rows};
         const cuuint64_t strides[2] = {kRowBytes, (cuuint64_t)g.Hq * kRowBytes};
-        const cuuint32_t box[3] = {64, (cuuint32_t)g.Gq, (cuuint32_t)a.seqs}, step[3] = {1, 1, 1};
+        const cuuint32_t box[3] = {64, (cuuint32_t)g.Gq, (cuuint32_t)a.quarter}, step[3] = {1, 1, 1};
         if (enc(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides, box, step,
                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
@@ -925,7 +1002,7 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const int chunks = (int)(((long long)n_rows * g.Gq + 7) / 8);    // times Hkv: below 2^31, as n_rows * Hq is
-    prefix_merge_kernel<<<(unsigned)(chunks * g.Hkv), 256, 0, st>>>(a, n_cta, chunks);
+    prefix_merge_kernel<<<dim3((unsigned)(chunks * g.Hkv), 8), 256, 0, st>>>(a, n_cta, chunks);
     return cudaGetLastError();
 }
 

@@ -409,6 +409,7 @@ int32_t stc_prefix_attn(const stc_shape* shape, const stc_cache* cache, int32_t 
     if ((int64_t)g.problems * g.T > 0x7FFFFFFFLL || (int64_t)n_rows * g.Hq > 0x7FFFFFFFLL) return STC_ERR_UNSUPPORTED;
     if (g.problems == 0 || n_rows == 0) return STC_OK;
     if (!q || !row_start || !out || (!own_out) != (!own_lse)) return STC_ERR_INVALID_ARG;
+    if (own_out == out || (own_lse && own_lse == lse_opt)) return STC_ERR_INVALID_ARG;
     if (g.T > 0 && (!cache->k || !cache->v_packed || !cache->v_mask || !cache->v_offs || cache->cap_groups < 0))
         return STC_ERR_INVALID_ARG;
     if (!aligned16(cache->k, cache->v_packed, q, own_out, out)) return STC_ERR_INVALID_ARG;

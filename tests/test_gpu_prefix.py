@@ -13,7 +13,7 @@ SCALE = 1 / math.sqrt(128)
 
 
 def run_case(seed, lens, T, starts, n_rows, Hq, Hkv, S=8, keep=4, softcap=0.0, alibi=False, window=0, docs=None, q_pos=None,
-             own=True, poison_keys=False, in_place=False, scale=SCALE, stream=None):
+             own=True, poison_keys=False, scale=SCALE, stream=None):
     G = len(lens)
     g = torch.Generator().manual_seed(seed + 1)
     c = R.make_cache(seed, G, Hkv, T, S, keep, lens)
@@ -46,8 +46,8 @@ def run_case(seed, lens, T, starts, n_rows, Hq, Hkv, S=8, keep=4, softcap=0.0, a
     shape = P.Shape(G, Hq, Hkv, S, T, torch.tensor(lens, dtype=torch.int32, device="cuda"))
     cache = P.Cache(k=dev["k"], v_packed=dev["v_packed"], v_mask=dev["v_mask"], v_offs=dev["v_offs"], cap_groups=c["cap"])
     d_own, d_lse = cu(own_out), cu(own_lse)
-    out = d_own if in_place else torch.full((n_rows, Hq, 128), 7.0, device="cuda")
-    lse = d_lse if in_place else torch.full((n_rows, Hq), 7.0, device="cuda")
+    out = torch.full((n_rows, Hq, 128), 7.0, device="cuda")
+    lse = torch.full((n_rows, Hq), 7.0, device="cuda")
     ws = Bd.new_workspace(shape, Bd.OP_PREFIX_ATTN, n_rows)
     ws.fill_(0xEF)
     optioned = softcap or alibi or window or docs is not None or q_pos is not None
@@ -61,8 +61,7 @@ def run_case(seed, lens, T, starts, n_rows, Hq, Hkv, S=8, keep=4, softcap=0.0, a
     got_o, got_l = out.double().cpu(), lse.double().cpu()
     inside = torch.zeros(n_rows, dtype=torch.bool)
     inside[starts[0]:starts[-1]] = True
-    if not in_place:
-        assert (got_o[~inside] == 7).all() and (got_l[~inside] == 7).all()
+    assert (got_o[~inside] == 7).all() and (got_l[~inside] == 7).all()
     for i, n in enumerate(lens):
         a, b = starts[i], starts[i + 1]
         if a == b:
@@ -106,6 +105,21 @@ def test_row_tiles_of_every_head_layout(heads, seqs):
     run_case(seqs, [300], 300, [0, seqs], seqs, *heads, own=seqs == 19)
 
 
+@pytest.mark.parametrize("rows", [16, 17, 32, 33, 64, 65, 128])
+@pytest.mark.parametrize("options", [dict(), dict(softcap=30.0), dict(alibi=True), dict(softcap=30.0, alibi=True, window=700, docs=3)],
+                         ids=lambda o: "+".join(o) or "plain")
+def test_copies_of_few_rows(rows, options):
+    """The row counts at which a tile holds its rows four times, twice, once, and the next tile begins; several CTAs and one."""
+    run_case(rows, [2000], 2000, [0, rows], rows, 2, 1, **options)
+    run_case(rows, [130, 60], 130, [0, rows, 2 * rows - 1], 2 * rows - 1, 48, 48, keep=2, **options)
+
+
+def test_accumulators_that_are_emptied():
+    """More tiles per CTA than an accumulator takes, and a maximum that moves afterwards."""
+    run_case(23, [64 * 36] * 15, 64 * 36, [9 * i for i in range(16)], 135, 48, 48, S=4, keep=1)
+    run_case(24, [64 * 40] * 12, 64 * 40, [9 * i for i in range(13)], 108, 48, 48, alibi=True, q_pos=[100 + 290 * (i % 9) for i in range(108)])
+
+
 def test_more_rows_than_a_unit_and_one_more():
     run_case(3, [200], 200, [0, 257], 257, 1, 1)
     run_case(4, [200], 200, [0, 129], 129, 2, 1, S=4, keep=2)
@@ -146,9 +160,9 @@ def test_scales(scale):
     run_case(16, [200], 200, [0, 4], 4, 4, 2, scale=scale)
 
 
-def test_in_place_join_and_another_stream():
+def test_another_stream():
     a = run_case(17, [333], 333, [0, 20], 20, 8, 2)
-    b = run_case(17, [333], 333, [0, 20], 20, 8, 2, in_place=True, stream=torch.cuda.Stream())
+    b = run_case(17, [333], 333, [0, 20], 20, 8, 2, stream=torch.cuda.Stream())
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 

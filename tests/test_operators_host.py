@@ -113,7 +113,7 @@ def test_prefix_attention_refusals(lib):
     for kw, code in [(dict(n=-1), 1), (dict(q=None), 1), (dict(start=None), 1), (dict(out=None), 1), (dict(q=odd), 1),
                      (dict(out=odd), 1), (dict(scale=float("nan")), 1), (dict(own=fake), 1), (dict(own_lse=fake), 1),
                      (dict(cache=Bd._Cache()), 1), (dict(score=Bd._Score(0.0, 5)), 1),
-                     (dict(score=Bd._Score(0.0, 0, fake)), 1), (dict(score=Bd._Score(-1.0, 0)), 1),
+                     (dict(score=Bd._Score(0.0, 0, fake)), 1), (dict(score=Bd._Score(-1.0, 0)), 1), (dict(own=fake, own_lse=C.c_void_p(0x2000)), 1),
                      (dict(shp=P.Shape(200, 8, 8, 8, (1 << 27) - 16).c()), 2), (dict(n=1 << 29), 2),
                      (dict(n=0), 0), (dict(shp=P.Shape(0, 8, 4, 8, 4096).c()), 0)]:
         assert call(**kw) == code, kw
