@@ -25,7 +25,8 @@
 // range; a segment that is a whole unit is finished in place, another one leaves a partial (max, sum,
 // accumulator) which a second small kernel joins in CTA order: no atomics, bitwise repeatable.
 //
-// Roles (16 warps): warp 0 = TMA producer of Q and K; warps 1, 2 = MMA issuers of the two groups; warps 4..7 and
+// Roles (16 warps): warp 0 = TMA producer of Q and K; warps 1, 2 = MMA issuers of the two groups; warp 3 = scheduler
+// (walks the segments for all roles, a few ahead); warps 4..7 and
 // 8..11 = softmax of the two groups, thread = row; warps 12..15 rebuild the value tiles with 16-byte asynchronous
 // copies straight from the packed store into the swizzled tile.  Two row tiles: group w owns row tile w and both see
 // every token tile.  One row tile: the groups take the token tiles in turn.  A group has two S buffers: the product for
@@ -56,13 +57,15 @@ constexpr int kRows = 128;                        // rows per tile = tensor-memo
 constexpr int kTok = 64;                          // tokens per tile
 constexpr int kThreads = 512;
 constexpr int kKStages = 6, kVStages = 4;
-constexpr int kFlush = 16;                        // tiles an accumulator takes: 128 products, 3e-6 of truncation
+constexpr int kFlush = 32;                        // tiles an accumulator takes: 256 products, 5e-6 of truncation (16 halve it and
+                                                  // cost a 32768-token, 128-sequence call a tenth of its time)
+constexpr int kSegs = 8;                          // segments the scheduler may be ahead
 constexpr uint32_t kQHalf = kRows * 128;          // 64 channels of a row tile: 128 rows of 128 bytes
 constexpr uint32_t kQTile = 2 * kQHalf;           // 32 KiB
 constexpr uint32_t kHalf = kTok * 128;            // 64 channels of a token tile
 constexpr uint32_t kTile = 2 * kHalf;             // 16 KiB
 constexpr uint32_t kOffK = 2 * kQTile, kOffV = kOffK + kKStages * kTile, kOffCtl = kOffV + kVStages * kTile;
-constexpr uint32_t kCtlBytes = 512;
+constexpr uint32_t kCtlBytes = 1024;
 constexpr uint32_t kSmem = kOffCtl + kCtlBytes;
 static_assert(kSmem <= 232448, "shared memory of a block");
 constexpr unsigned long long kWaitNs = 1000000000ull;
@@ -74,9 +77,10 @@ constexpr float kSlack = 8.f;                     // log2 units the maximum may 
 // hence one O barrier per buffer, whose earlier use the waiter always knows to be through.
 enum { kQFull, kQEmpty, kKFull = kQEmpty + 2, kKEmpty = kKFull + kKStages, kVFull = kKEmpty + 2 * kKStages,
        kVEmpty = kVFull + kVStages, kSFull = kVEmpty + 2 * kVStages, kPFull = kSFull + 4, kOFull = kPFull + 4,
-       kXchg = kOFull + 4, kBars };
-static_assert(kBars * 8 <= 448, "control block");
-constexpr uint32_t kCtlTmem = 448, kCtlAbort = 452, kCtlPlan = 456;    // tensor-memory address, abort flag, 4 x 8 bytes
+       kXchg = kOFull + 4, kSegFull, kSegEmpty = kSegFull + kSegs, kBars = kSegEmpty + kSegs };
+static_assert(kBars * 8 <= 512, "control block");
+constexpr uint32_t kCtlTmem = 512, kCtlAbort = 516, kCtlSegs = 544;    // tensor-memory address, abort flag, kSegs x 32 bytes
+constexpr int kSegReaders = 15;                   // warps that follow the segments: all but the scheduler
 
 struct PrefixArgs {
     const int32_t* row_start;    // [G + 1]
@@ -233,13 +237,13 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     unsigned char* ctl = smem + kOffCtl;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctl + kCtlTmem);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + kCtlAbort);
-    volatile long long* plan = reinterpret_cast<volatile long long*>(ctl + kCtlPlan);  // x, x_end, off, g
+    volatile int* const segs = reinterpret_cast<volatile int*>(ctl + kCtlSegs);        // [kSegs][8]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     // ---- set-up: barriers, tensor memory, this CTA's range ------------------------------------------
     if (threadIdx.x == 0) {
         for (int i = 0; i < kBars; ++i)
-            mbar_init(bars + 8 * i, i >= kPFull && i < kOFull ? kRows : i == kXchg ? 2 * kRows : i >= kVFull && i < kVEmpty ? 2 : 1);
+            mbar_init(bars + 8 * i, i >= kPFull && i < kOFull ? kRows : i == kXchg ? 2 * kRows : i >= kVFull && i < kVEmpty ? 2 : i >= kSegEmpty ? kSegReaders : 1);
         *abort_flag = (base & 1023u) != 0 ? (int)STC_ERR_CUDA : 0;      // swizzled tiles need 1024-byte aligned bases
         fence_mbar_init();
     }
@@ -248,60 +252,10 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                      ::"r"(bars + kCtlTmem), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    if (warp == 3) {                                 // flat tile sequence: prefix sums over the prefixes, 32 at a time
-        bool bad = false;
-        auto scan = [&](auto&& use) {
-            long long run = 0;
-            for (int g0 = 0; g0 < a.G; g0 += 32) {
-                const int g = g0 + lane;
-                long long n = 0;
-                if (g < a.G) {
-                    const int r0 = a.row_start[g], r1 = a.row_start[g + 1];
-                    if (r0 < 0 || r1 < r0 || r1 > a.n_rows) bad = true;
-                    else n = group_tiles(a, load_group(a, g));
-                }
-                long long incl = n;
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const long long o = __shfl_up_sync(0xFFFFFFFFu, incl, d);
-                    if (lane >= d) incl += o;
-                }
-                use(g, run + incl - n, run + incl);
-                run += __shfl_sync(0xFFFFFFFFu, incl, 31);
-            }
-            return run;
-        };
-        long long total = scan([&](int g, long long lo, long long) {
-            if (blockIdx.x == 0 && g < a.G) a.base[g] = lo;
-        });
-        bad = __any_sync(0xFFFFFFFFu, bad);
-        if (bad) total = 0;
-        const long long n_cta = min(total, (long long)gridDim.x);         // with fewer tiles than CTAs the rest stay idle
-        long long lo = 0, hi = 0;
-        if (blockIdx.x < n_cta) { lo = total * blockIdx.x / n_cta; hi = total * (blockIdx.x + 1) / n_cta; }
-        if (lane == 0) {
-            plan[0] = lo; plan[1] = hi; plan[2] = 0; plan[3] = 0;
-            if (blockIdx.x == 0) { a.base[a.G] = total; a.base[a.G + 1] = bad; }
-        }
-        __syncwarp();
-        if (hi > lo) {
-            if (a.G == 1) { if (lane == 0) plan[2] = lo; }
-            else
-                scan([&](int g, long long first, long long end) {
-                    if (g < a.G && first <= lo && lo < end) { plan[2] = lo - first; plan[3] = g; }
-                });
-        }
-    }
     tc_before();
     __syncthreads();
     tc_after();
     const uint32_t tmem = *tmem_slot;
-    Walker walk;
-    walk.x = walk.x_begin = plan[0];
-    walk.x_end = plan[1];
-    walk.off = plan[2];
-    walk.g = (int)plan[3];
-    walk.loaded = false;
     Segment s;
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
     auto wait = [&](int i, uint32_t parity) { return mbar_wait_or_abort(bar(i), parity & 1u, abort_flag, kWaitNs); };
@@ -312,6 +266,29 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         return __shfl_sync(0xFFFFFFFFu, got, 0) != 0;
     };
     auto give_up = [&]() { *abort_flag = (int)STC_ERR_TIMEOUT; };
+    // The next segment, for a role that is one lane / a whole warp.  False: none left, or given up (`good` cleared).
+    int n_seg = 0;
+    auto read_segment = [&]() {
+        const volatile int* e = segs + (n_seg % kSegs) * 8;
+        s = Segment{e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]};
+    };
+    auto next_lane = [&](bool& good) -> bool {
+        good = wait(kSegFull + n_seg % kSegs, (uint32_t)(n_seg / kSegs));
+        if (!good) return false;
+        read_segment();
+        mbar_arrive(bar(kSegEmpty + n_seg % kSegs));
+        ++n_seg;
+        return s.tile1 >= 0;
+    };
+    auto next_warp = [&](bool& good) -> bool {
+        good = warp_wait(kSegFull + n_seg % kSegs, (uint32_t)(n_seg / kSegs));
+        if (!good) return false;
+        read_segment();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kSegEmpty + n_seg % kSegs));
+        ++n_seg;
+        return s.tile1 >= 0;
+    };
 
     if (*abort_flag) {
         // nothing was started
@@ -322,7 +299,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             uint32_t used[2] = {0u, 0u}, par[2] = {0u, 0u};    // per group, bit = stage: its last tile was read; parity to wait for
             bool ok = true;
             const uint32_t q_bytes = 2u * 128u * (uint32_t)(a.Gq * a.seqs);       // per row tile
-            while (ok && walk.next(a, s)) {
+            while (ok && next_lane(ok)) {
                 const bool two = s.n_seq > a.seqs;
                 if (seg > 0 && !(wait(kQEmpty, (uint32_t)(seg - 1)) && wait(kQEmpty + 1, (uint32_t)(seg - 1)))) { ok = false; break; }
                 mbar_expect_tx(bar(kQFull), two ? 2 * q_bytes : q_bytes);
@@ -372,7 +349,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             uint32_t kc0 = 0, seg = 0;               // tiles of the segments before; segments before
             uint32_t n_s = 0, n_o = 0;               // products issued by this group
             bool ok = true;
-            while (ok && walk.next(a, s)) {
+            while (ok && next_lane(ok)) {
                 const int tiles = s.tile1 - s.tile0;
                 const bool two = s.n_seq > a.seqs;   // two row tiles: every token tile goes to both groups
                 const int mine = two ? tiles : (tiles + 1 - w) >> 1;
@@ -420,6 +397,71 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 kc0 += (uint32_t)tiles;
                 ++seg;
+            }
+            if (!ok) give_up();
+        }
+    } else if (warp == 3) {
+        // ---- scheduler: flat tile sequence by prefix sums over the prefixes, 32 at a time; this CTA's range; its segments ----
+        bool bad = false;
+        auto scan = [&](auto&& use) {
+            long long run = 0;
+            for (int g0 = 0; g0 < a.G; g0 += 32) {
+                const int g = g0 + lane;
+                long long n = 0;
+                if (g < a.G) {
+                    const int r0 = a.row_start[g], r1 = a.row_start[g + 1];
+                    if (r0 < 0 || r1 < r0 || r1 > a.n_rows) bad = true;
+                    else n = group_tiles(a, load_group(a, g));
+                }
+                long long incl = n;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const long long o = __shfl_up_sync(0xFFFFFFFFu, incl, d);
+                    if (lane >= d) incl += o;
+                }
+                use(g, run + incl - n, run + incl);
+                run += __shfl_sync(0xFFFFFFFFu, incl, 31);
+            }
+            return run;
+        };
+        long long total = scan([&](int g, long long lo, long long) {
+            if (blockIdx.x == 0 && g < a.G) a.base[g] = lo;
+        });
+        bad = __any_sync(0xFFFFFFFFu, bad);
+        if (bad) total = 0;
+        const long long n_cta = min(total, (long long)gridDim.x);         // with fewer tiles than CTAs the rest stay idle
+        long long lo = 0, hi = 0;
+        if (blockIdx.x < n_cta) { lo = total * blockIdx.x / n_cta; hi = total * (blockIdx.x + 1) / n_cta; }
+        if (blockIdx.x == 0 && lane == 0) { a.base[a.G] = total; a.base[a.G + 1] = bad; }
+        long long off = lo;
+        int g_first = 0;
+        if (hi > lo && a.G > 1) {
+            scan([&](int g, long long first, long long end) {
+                const bool here = g < a.G && first <= lo && lo < end;
+                const uint32_t who = __ballot_sync(0xFFFFFFFFu, here);
+                if (who) {
+                    off = __shfl_sync(0xFFFFFFFFu, lo - first, __ffs(who) - 1);
+                    g_first = __shfl_sync(0xFFFFFFFFu, g, __ffs(who) - 1);
+                }
+            });
+        }
+        if (lane == 0) {
+            Walker walk;
+            walk.x = walk.x_begin = lo;
+            walk.x_end = hi;
+            walk.off = off;
+            walk.g = g_first;
+            walk.loaded = false;
+            bool ok = true, more = true;
+            for (int i = 0; ok && more; ++i) {
+                more = walk.next(a, s);
+                if (i >= kSegs) ok = wait(kSegEmpty + i % kSegs, (uint32_t)(i / kSegs - 1));
+                if (!ok) break;
+                volatile int* e = segs + (i % kSegs) * 8;
+                e[0] = s.g; e[1] = s.hk; e[2] = s.row0; e[3] = s.n_seq; e[4] = s.len; e[5] = s.tile0;
+                e[6] = more ? s.tile1 : -1;
+                e[7] = s.slot;
+                mbar_arrive(bar(kSegFull + i % kSegs));
             }
             if (!ok) give_up();
         }
@@ -482,27 +524,26 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     if (!ok) return;
                     tc_after();
                     const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
+                    const bool grow = n > kFlush && __all_sync(0xFFFFFFFFu, keep == 1.f);   // nothing to read back
 #pragma unroll 1
                     for (int c = 0; c < kHeadDim; c += 32) {
                         float4 old[8];
-                        if (n > kFlush) {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) old[i] = __ldcg(my_flush + (size_t)(c / 4 + i) * kRows);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) old[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                        }
+                        for (int i = 0; i < 8; ++i)
+                            old[i] = n > kFlush && !grow ? __ldcg(my_flush + (size_t)(c / 4 + i) * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
                         uint32_t q[32];
                         tmem_ld16<0>(to + c, q);
                         tmem_ld16<16>(to + c + 16, q);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            __stcg(my_flush + (size_t)(c / 4 + i) * kRows,
-                                   make_float4(fmaf(old[i].x, keep, __uint_as_float(q[4 * i])),
-                                               fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1])),
-                                               fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2])),
-                                               fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3]))));
+                        for (int i = 0; i < 8; ++i) {
+                            float4* dst = my_flush + (size_t)(c / 4 + i) * kRows;
+                            const float4 v = make_float4(
+                                fmaf(old[i].x, keep, __uint_as_float(q[4 * i])), fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1])),
+                                fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2])), fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3])));
+                            if (grow) red_add4(dst, v.x, v.y, v.z, v.w);
+                            else __stcg(dst, v);
+                        }
                     }
                     m_flush = m;
                 }
@@ -610,50 +651,63 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 ok = warp_wait(kOFull + 2 * w + ((n_s - 1) & 1u), (n_s - 1) >> 1);
                 if (!ok) return;
                 tc_after();
-                const bool flushed = mine > kFlush;
-                const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
-                const bool add_own = finish && live && a.own_out && j.fown != 0.f;
-                const float4* own = reinterpret_cast<const float4*>(a.own_out) + out_row * 32;
-                float4* dst = finish ? reinterpret_cast<float4*>(a.out) + out_row * 32 : a.part_o + (slot + w) * 32 * kRows + row;
-                const int step = finish ? 1 : kRows;
+                if (mine > kFlush) {                 // take back what the accumulator was emptied of
+                    const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
 #pragma unroll 1
-                for (int c = 0; c < kHeadDim; c += 32) {
-                    float4 old[8];
-                    if (flushed) {
+                    for (int c = 0; c < kHeadDim; c += 16) {
+                        float4 old[4];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) old[i] = __ldcg(my_flush + (size_t)(c / 4 + i) * kRows);
-                    }
-                    uint32_t q[32];
-                    tmem_ld16<0>(to + c, q);
-                    tmem_ld16<16>(to + c + 16, q);
-                    tmem_wait_ld();
-                    if (flushed) {
+                        for (int i = 0; i < 4; ++i) old[i] = __ldcg(my_flush + (size_t)(c / 4 + i) * kRows);
+                        uint32_t q[16];
+                        tmem_ld16(to + c, q);
+                        tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
+                        for (int i = 0; i < 4; ++i) {
                             q[4 * i] = __float_as_uint(fmaf(old[i].x, keep, __uint_as_float(q[4 * i])));
                             q[4 * i + 1] = __float_as_uint(fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1])));
                             q[4 * i + 2] = __float_as_uint(fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2])));
                             q[4 * i + 3] = __float_as_uint(fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3])));
                         }
+                        tmem_st16(to + c, q);
                     }
-                    if (add_own) {
+                    tmem_wait_st();
+                }
+                if (!finish) {                       // a part as it stands
+                    float4* dst = a.part_o + (slot + w) * 32 * kRows + row;
+#pragma unroll 1
+                    for (int c = 0; c < kHeadDim; c += 64) {
+                        uint32_t q[64];
+                        tmem_ld16<0>(to + c, q);
+                        tmem_ld16<16>(to + c + 16, q);
+                        tmem_ld16<32>(to + c + 32, q);
+                        tmem_ld16<48>(to + c + 48, q);
+                        tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) old[i] = own[c / 4 + i];
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) old[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        for (int i = 0; i < 16; ++i)
+                            __stcg(dst + (size_t)(c / 4 + i) * kRows,
+                                   make_float4(__uint_as_float(q[4 * i]), __uint_as_float(q[4 * i + 1]),
+                                               __uint_as_float(q[4 * i + 2]), __uint_as_float(q[4 * i + 3])));
                     }
-                    if (live || !finish) {
+                } else {                             // the row's output
+                    const bool add_own = live && a.own_out && j.fown != 0.f;
+                    const float4* own = reinterpret_cast<const float4*>(a.own_out) + out_row * 32;
+                    float4* dst = reinterpret_cast<float4*>(a.out) + out_row * 32;
+#pragma unroll 1
+                    for (int c = 0; c < kHeadDim; c += 16) {
+                        float4 mix[4];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            float4 v = make_float4(__uint_as_float(q[4 * i]), __uint_as_float(q[4 * i + 1]),
-                                                   __uint_as_float(q[4 * i + 2]), __uint_as_float(q[4 * i + 3]));
-                            if (finish) {            // (a factor 0 stands for "nothing seen", whatever was summed)
-                                if (j.fo == 0.f) v = make_float4(0.f, 0.f, 0.f, 0.f);
-                                v.x = fmaf(old[i].x, j.fown, v.x * j.fo); v.y = fmaf(old[i].y, j.fown, v.y * j.fo);
-                                v.z = fmaf(old[i].z, j.fown, v.z * j.fo); v.w = fmaf(old[i].w, j.fown, v.w * j.fo);
-                            }
-                            dst[(size_t)(c / 4 + i) * step] = v;
+                        for (int i = 0; i < 4; ++i) mix[i] = add_own ? own[c / 4 + i] : make_float4(0.f, 0.f, 0.f, 0.f);
+                        uint32_t q[16];
+                        tmem_ld16(to + c, q);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {        // (a factor 0 stands for "nothing seen", whatever was summed)
+                            const float4 v = j.fo == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                                         : make_float4(__uint_as_float(q[4 * i]) * j.fo, __uint_as_float(q[4 * i + 1]) * j.fo,
+                                                                       __uint_as_float(q[4 * i + 2]) * j.fo, __uint_as_float(q[4 * i + 3]) * j.fo);
+                            if (live)
+                                dst[c / 4 + i] = make_float4(fmaf(mix[i].x, j.fown, v.x), fmaf(mix[i].y, j.fown, v.y),
+                                                             fmaf(mix[i].z, j.fown, v.z), fmaf(mix[i].w, j.fown, v.w));
                         }
                     }
                 }
@@ -682,7 +736,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const Join jj = join(top, sum, BIAS ? bias_shift(a, s.len, seq, head) : 0.f, a.own_lse != nullptr, own_l);
                 float4* dst = reinterpret_cast<float4*>(a.out) + out_row * 32 + d0;
                 const float4* own = reinterpret_cast<const float4*>(a.own_out) + out_row * 32 + d0;
-                constexpr int BATCH = E == 8 ? 2 : 4;
+                constexpr int BATCH = 8 / E;
 #pragma unroll 1
                 for (int d = 0; d < CH; d += BATCH) {
                     float4 v[BATCH][E], o[BATCH];
@@ -711,7 +765,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             mbar_arrive(bar(kXchg));                 // the scratch slot is free again
             ok = warp_wait(kXchg, n_x++);
         };
-        while (ok && walk.next(a, s)) {
+        while (ok && next_warp(ok)) {
             const int n_copies = copies(a, s.n_seq);
             if (n_copies == 1) segment(std::integral_constant<int, 64>{});
             else if (n_copies == 2) segment(std::integral_constant<int, 32>{});
@@ -736,7 +790,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (lane == 0) mbar_arrive(bar(kVFull + pending));
             pending = -1;
         };
-        while (ok && walk.next(a, s)) {
+        while (ok && next_warp(ok)) {
             const bool two = s.n_seq > a.seqs;
             const size_t problem = (size_t)s.g * a.Hkv + s.hk;
             const uint16_t* mask_row = a.v_mask + problem * a.T;
