@@ -259,12 +259,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     Segment s;
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
     auto wait = [&](int i, uint32_t parity) { return mbar_wait_or_abort(bar(i), parity & 1u, abort_flag, kWaitNs); };
-    // the same for a whole warp: lane 0 waits and hands the answer on
-    auto warp_wait = [&](int i, uint32_t parity) -> bool {
-        int got = 0;
-        if (lane == 0) got = wait(i, parity);
-        return __shfl_sync(0xFFFFFFFFu, got, 0) != 0;
-    };
+    auto warp_wait = [&](int i, uint32_t parity) { return mbar_warp_wait_or_abort(bar(i), parity & 1u, abort_flag, kWaitNs); };
     auto give_up = [&]() { *abort_flag = (int)STC_ERR_TIMEOUT; };
     // The next segment, for a role that is one lane / a whole warp.  False: none left, or given up (`good` cleared).
     int n_seg = 0;
@@ -341,33 +336,33 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
         }
     } else if (warp == 1 || warp == 2) {
-        // ---- MMA issuer of group w ------------------------------------------------------------------------
-        if (lane == 0) {
-            constexpr uint32_t id_qk = idesc_bf16(kRows, kTok, false), id_pv = idesc_bf16(kRows, kHeadDim, true);
-            const int w = warp - 1;
-            const uint32_t to = tmem + 256 + (uint32_t)w * 128u;
-            uint32_t kc0 = 0, seg = 0;               // tiles of the segments before; segments before
-            uint32_t n_s = 0, n_o = 0;               // products issued by this group
-            bool ok = true;
-            while (ok && next_lane(ok)) {
-                const int tiles = s.tile1 - s.tile0;
-                const bool two = s.n_seq > a.seqs;   // two row tiles: every token tile goes to both groups
-                const int mine = two ? tiles : (tiles + 1 - w) >> 1;
-                const uint32_t first = kc0 + (two ? 0 : w), stride = two ? 1 : 2;
-                ok = wait(kQFull, seg);
-                if (ok && mine == 0) mbar_arrive(bar(kQEmpty + w));
-                const uint64_t dq = smem_desc_128(base + (two ? w * kQTile : 0u), 16);
-                // iteration n: O += P V of tile n - 2, whose S buffer then takes S = Q K^T of tile n
+        // ---- MMA issuer of group w: the warp stays together, an elected lane issues ---------------------------
+        constexpr uint32_t id_qk = idesc_bf16(kRows, kTok, false), id_pv = idesc_bf16(kRows, kHeadDim, true);
+        const int w = uniform(warp) - 1;
+        const uint32_t sm = uniform(base), ts = uniform(tmem) + (uint32_t)w * 128u, to = uniform(tmem) + 256 + (uint32_t)w * 128u;
+        uint32_t kc0 = 0, seg = 0;                   // tiles of the segments before; segments before
+        uint32_t n_s = 0, n_o = 0;                   // products issued by this group
+        bool ok = true;
+        while (ok && next_warp(ok)) {
+            const int tiles = uniform(s.tile1 - s.tile0);
+            const bool two = uniform((int)(s.n_seq > a.seqs)) != 0;       // two row tiles: every token tile goes to both groups
+            const int mine = two ? tiles : (tiles + 1 - w) >> 1;
+            const uint32_t first = kc0 + (two ? 0 : w), stride = two ? 1 : 2;
+            ok = warp_wait(kQFull, seg);
+            if (ok && mine == 0 && lane == 0) mbar_arrive(bar(kQEmpty + w));
+            const uint32_t q_at = sm + (two ? w * kQTile : 0u);
+            // iteration n: O += P V of tile n - 2, whose S buffer then takes S = Q K^T of tile n
 #pragma unroll 1
-                for (int n = 0; ok && mine > 0 && n < mine + 2; ++n) {
-                    if (n >= 2) {
-                        const uint32_t j = first + (uint32_t)(n - 2) * stride, st = j % kVStages, buf = n_o & 1u;
-                        ok = wait(kPFull + 2 * w + buf, n_o >> 1) && wait(kVFull + st, j / kVStages);
-                        if (!ok) break;
-                        tc_after();
-                        const uint64_t dv = smem_desc_128(base + kOffV + st * kTile, kHalf);
-                        const uint32_t p = tmem + (uint32_t)w * 128u + buf * 64u;
-                        const uint32_t more = (n - 2) % kFlush != 0;          // else O starts anew
+            for (int n = 0; ok && mine > 0 && n < mine + 2; ++n) {
+                if (n >= 2) {
+                    const uint32_t j = first + (uint32_t)(n - 2) * stride, st = j % kVStages, buf = n_o & 1u;
+                    ok = warp_wait(kPFull + 2 * w + buf, n_o >> 1) && warp_wait(kVFull + st, j / kVStages);
+                    if (!ok) break;
+                    tc_after();
+                    const uint64_t dv = smem_desc_128(sm + kOffV + st * kTile, kHalf);
+                    const uint32_t p = ts + buf * 64u;
+                    const uint32_t more = (n - 2) % kFlush != 0;          // else O starts anew
+                    if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {        // 16 tokens: 16 rows of 128 bytes; P: 8 columns high, 8 residual
                             tc_mma_ts(to, p + 16 * k, dv + (uint64_t)(k * (2048 >> 4)), id_pv, k ? 1u : more);
@@ -375,31 +370,35 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         }
                         tc_commit_to(bar(kOFull + 2 * w + buf));
                         tc_commit_to(bar(kVEmpty + 2 * st + w));
-                        ++n_o;
                     }
-                    if (n < mine) {
-                        const uint32_t j = first + (uint32_t)n * stride, st = j % kKStages, buf = n_s & 1u;
-                        ok = wait(kKFull + st, j / kKStages);
-                        // the buffer holds the P of the group's last but one tile until that product is through
-                        if (ok && n_s >= 2) ok = wait(kOFull + 2 * w + buf, (n_s - 2) >> 1);
-                        if (!ok) break;
-                        tc_after();
-                        const uint64_t dk = smem_desc_128(base + kOffK + st * kTile, 16);
+                    __syncwarp();
+                    ++n_o;
+                }
+                if (n < mine) {
+                    const uint32_t j = first + (uint32_t)n * stride, st = j % kKStages, buf = n_s & 1u;
+                    ok = warp_wait(kKFull + st, j / kKStages);
+                    // the buffer holds the P of the group's last but one tile until that product is through
+                    if (ok && n_s >= 2) ok = warp_wait(kOFull + 2 * w + buf, (n_s - 2) >> 1);
+                    if (!ok) break;
+                    tc_after();
+                    const uint64_t dq = smem_desc_128(q_at, 16), dk = smem_desc_128(sm + kOffK + st * kTile, 16);
+                    if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k)          // 16 dims = 32 bytes = 2 units; 64 dims = one half tile
-                            tc_mma_ss(tmem + (uint32_t)w * 128u + buf * 64u, dq + (uint64_t)((k >> 2) * (kQHalf >> 4) + (k & 3) * 2),
+                            tc_mma_ss(ts + buf * 64u, dq + (uint64_t)((k >> 2) * (kQHalf >> 4) + (k & 3) * 2),
                                       dk + (uint64_t)((k >> 2) * (kHalf >> 4) + (k & 3) * 2), id_qk, k != 0);
                         tc_commit_to(bar(kSFull + 2 * w + buf));
                         tc_commit_to(bar(kKEmpty + 2 * st + w));
                         if (n == mine - 1) tc_commit_to(bar(kQEmpty + w));
-                        ++n_s;
                     }
+                    __syncwarp();
+                    ++n_s;
                 }
-                kc0 += (uint32_t)tiles;
-                ++seg;
             }
-            if (!ok) give_up();
+            kc0 += (uint32_t)tiles;
+            ++seg;
         }
+        if (!ok) give_up();
     } else if (warp == 3) {
         // ---- scheduler: flat tile sequence by prefix sums over the prefixes, 32 at a time; this CTA's range; its segments ----
         bool bad = false;
@@ -810,8 +809,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             for (int h = h0; h < tiles; h += 2) {
                 const uint32_t m = m_next & ((1u << S) - 1u), first = first_next;
                 fetch(h + 2, m_next, first_next);
-                const uint32_t cnt = __popc(m);
-                const uint32_t pre = warp_incl_scan(cnt, lane) - cnt;
+                // per token: groups of the warp's tokens before it << 16 | its mask
+                const uint32_t cnt = __popc(m), tok_word = (warp_incl_scan(cnt, lane) - cnt) << 16 | m;
                 const int st = (vc + h) % kVStages;
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
@@ -819,24 +818,26 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     const uint32_t p = (par[w] >> st) & 1u;
                     par[w] ^= 1u << st;
                     used[w] &= ~(1u << st);
-                    int free = 0;
-                    if (lane == 0) free = mbar_try_wait(bar(kVEmpty + 2 * st + w), p);
-                    if (__shfl_sync(0xFFFFFFFFu, free, 0)) continue;
+                    if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar(kVEmpty + 2 * st + w), p))) continue;
                     if (pending >= 0) { cp_async_wait<0>(); publish(); }
                     ok = ok && warp_wait(kVEmpty + 2 * st + w, p);
                 }
                 if (!ok) break;
                 if (two || !(h & 1)) used[0] |= 1u << st;
                 if (two || (h & 1)) used[1] |= 1u << st;
-                const uint32_t dst = base + kOffV + st * kTile + (uint32_t)(oct >> 3) * kHalf;
+                // token tok0 + 2 i + (lane >> 4), chunk oct of its row: 16-byte chunks of a row are swizzled by the token
+                const uint32_t dst = base + kOffV + st * kTile + (uint32_t)(oct >> 3) * kHalf + (uint32_t)(tok0 + (lane >> 4)) * 128u;
+                const uint32_t chunk = (uint32_t)((oct & 7) ^ (lane >> 4));
+                const int64_t room = limit - (int64_t)first;
+                const uint32_t most = room <= 0 ? 0u : room > 1024 ? 1024u : (uint32_t)room;   // groups left in the store
+                const uint4* src = packed + (int64_t)first * OPG + sub;
 #pragma unroll 4
                 for (int i = 0; i < 16; ++i) {
-                    const int tok = 2 * i + (lane >> 4);
-                    const uint32_t mt = __shfl_sync(0xFFFFFFFFu, m, tok), pt = __shfl_sync(0xFFFFFFFFu, pre, tok);
-                    const int64_t at = (int64_t)first + pt + __popc(mt & below);
-                    const bool kept = ((mt >> grp) & 1u) && at < limit;
-                    cp_async16_zfill(dst + (uint32_t)(tok0 + tok) * 128u + (uint32_t)(((oct & 7) ^ (tok & 7)) * 16),
-                                     kept ? packed + at * OPG + sub : packed, kept ? 16 : 0);
+                    const uint32_t tw = __shfl_sync(0xFFFFFFFFu, tok_word, 2 * i + (lane >> 4));
+                    const uint32_t at = (tw >> 16) + __popc(tw & below);
+                    const bool kept = ((tw >> grp) & 1u) && at < most;
+                    cp_async16_zfill(dst + (uint32_t)i * 256u + ((chunk ^ (uint32_t)(2 * (i & 3))) << 4),
+                                     kept ? src + at * OPG : packed, kept ? 16 : 0);
                 }
                 cp_async_commit();
                 if (pending >= 0) { cp_async_wait<1>(); publish(); }

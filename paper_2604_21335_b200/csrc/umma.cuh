@@ -23,6 +23,32 @@ __device__ __forceinline__ bool mbar_wait_or_abort(uint32_t bar, uint32_t parity
     }
 }
 
+// The same for a converged warp: every lane asks and the answer is a vote, so the warp stays converged and the branches
+// are uniform.  (One lane waiting for the others costs some 200 cycles of coming together again.)
+__device__ __forceinline__ bool mbar_warp_wait_or_abort(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                                        unsigned long long limit_ns) {
+    if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity))) return true;
+    const unsigned long long t0 = global_ns();
+#pragma unroll 1
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i)
+            if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity))) return true;
+        if (__any_sync(0xFFFFFFFFu, *abort_flag != 0 || global_ns() - t0 > limit_ns)) return false;
+    }
+}
+// One lane of a converged warp.  The operands of tcgen05.mma live in uniform registers: issued by an elected lane
+// of a warp whose control flow is uniform they cost little, issued inside `if (lane == 0)` every operand
+// is moved over by itself (measured: 20 against 85 cycles per instruction).  To be asked directly in the condition
+// of the block that issues.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+template <typename T>
+__device__ __forceinline__ T uniform(T v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
+
 // Tiled TMA loads.  The innermost coordinate is a multiple of 64 bf16 = 128 bytes (a copy must start on a
 // 16-byte boundary).
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
