@@ -195,33 +195,42 @@ __device__ __forceinline__ float bias_shift(const PrefixArgs& a, int len, int se
     return a.sc.slopes[head] * (float)(hi - 1 - pos);
 }
 
-// Caps N scores of a row (raw products in, log2 units out).  Scores far below the cap, the usual case, need only the
-// polynomial of tanh_f32, two at a time; the warp votes once per tile instead of branching per score.
+// Two raw products capped, in log2 units, where both are small against the cap (tanh_small).
+__device__ __forceinline__ float2 cap_small(float2 x, float cap_in, float cap_log2) {
+    const float2 z = mul2(x, both(cap_in)), u = mul2(z, z);
+    float2 p = fma2(both(kTanh4), u, both(kTanh3));
+    p = fma2(p, u, both(kTanh2));
+    p = fma2(p, u, both(kTanh1));
+    p = fma2(p, u, both(kTanh0));
+    return mul2(fma2(mul2(z, u), p, z), both(cap_log2));
+}
+__device__ __forceinline__ float cap_any(float x, float cap_in, float cap_log2) {
+    const float z = x * cap_in, lo = tanh_small(z), hi = tanh_large(z);
+    return cap_log2 * (fabsf(z) <= kTanhSmall ? lo : hi);
+}
+// Caps N scores of a row.  Scores far below the cap are the usual case; the warp votes once per tile instead of branching
+// per score.  `big`: largest magnitude among them.
 template <int N>
-__device__ __forceinline__ void cap_scores(uint32_t (&r)[N], float cap_in, float cap_log2) {
-    float big = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) big = fmaxf(big, fabsf(__uint_as_float(r[i])));
+__device__ __forceinline__ void cap_scores(uint32_t (&r)[N], float big, float cap_in, float cap_log2) {
     if (__all_sync(0xFFFFFFFFu, big * fabsf(cap_in) <= kTanhSmall)) {
 #pragma unroll
-        for (int i = 0; i < N; i += 2) {          // tanh_small
-            const float2 z = mul2(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), both(cap_in));
-            const float2 u = mul2(z, z);
-            float2 p = fma2(both(kTanh4), u, both(kTanh3));
-            p = fma2(p, u, both(kTanh2));
-            p = fma2(p, u, both(kTanh1));
-            p = fma2(p, u, both(kTanh0));
-            const float2 y = mul2(fma2(mul2(z, u), p, z), both(cap_log2));
+        for (int i = 0; i < N; i += 2) {
+            const float2 y = cap_small(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), cap_in, cap_log2);
             r[i] = __float_as_uint(y.x);
             r[i + 1] = __float_as_uint(y.y);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float z = __uint_as_float(r[i]) * cap_in, lo = tanh_small(z), hi = tanh_large(z);
-            r[i] = __float_as_uint(cap_log2 * (fabsf(z) <= kTanhSmall ? lo : hi));
-        }
+        for (int i = 0; i < N; ++i) r[i] = __float_as_uint(cap_any(__uint_as_float(r[i]), cap_in, cap_log2));
     }
+}
+template <int N>
+__device__ __forceinline__ float magnitude(const uint32_t (&r)[N]) {
+    float b[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < N; i += 2)
+        b[(i >> 1) & 3] = fmaxf(fmaxf(b[(i >> 1) & 3], fabsf(__uint_as_float(r[i]))), fabsf(__uint_as_float(r[i + 1])));
+    return fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3]));
 }
 
 // CAP: capped scores; BIAS: finished scores are needed for the maximum (slopes, or a scale that is not positive).
@@ -239,6 +248,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + kCtlAbort);
     volatile int* const segs = reinterpret_cast<volatile int*>(ctl + kCtlSegs);        // [kSegs][8]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    asm volatile("griddepcontrol.launch_dependents;");
 
     // ---- set-up: barriers, tensor memory, this CTA's range ------------------------------------------
     if (threadIdx.x == 0) {
@@ -559,7 +569,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 tmem_wait_ld();
                 // scores in log2 units where they are not the raw products times a positive scale
-                if constexpr (CAP) cap_scores(r, a.cap_in, a.cap_log2);
+                if constexpr (CAP) cap_scores(r, magnitude(r), a.cap_in, a.cap_log2);
                 if constexpr (BIAS) {
                     const float far = (float)(t0 - (hi - 1));
 #pragma unroll
@@ -773,12 +783,13 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         if (!ok) give_up();
     } else if (warp >= 12) {
         // ---- value tiles: packed groups -> swizzled rows ---------------------------------------------------
-        // Warps 12, 13 build the even tiles and 14, 15 the odd ones (counted over the CTA), 32 tokens each.  A lane owns
-        // one 16-byte column of every other token; a kept group is one asynchronous 16-byte copy, a dropped one a
-        // zero-filled copy that reads nothing.  The copies of a warp's next tile are under way before the last
-        // one's are waited for, unless its stage is still being read.
-        const int pair = (warp - 12) >> 1, tok0 = (warp & 1) * 32, oct = lane & 15, grp = oct / OPG, sub = oct % OPG;
-        const uint32_t below = (1u << grp) - 1u;
+        // Warps 12, 13 build the even tiles and 14, 15 the odd ones (counted over the CTA), 32 tokens each.  LPT
+        // neighbouring lanes copy 16-byte chunks of one token (a whole group of 32 or 64 bytes; two groups of 16), so a
+        // token's mask stays with its lanes and the place of a kept group is a running count.  A kept group is one
+        // asynchronous 16-byte copy per chunk, a dropped one a zero-filled copy that reads nothing.  The copies of a
+        // warp's next tile are under way before the last one's are waited for, unless its stage is still being read.
+        constexpr int LPT = OPG < 2 ? 2 : OPG, GPL = LPT / OPG;           // lanes per token, groups they span
+        const int pair = (warp - 12) >> 1, tok0 = (warp & 1) * 32, sub = lane % LPT;
         uint32_t used[2] = {0u, 0u}, par[2] = {0u, 0u};    // as the producer's, for the value stages
         int vc = 0;                                  // tiles of the segments before
         int pending = -1;                            // stage whose copies are not waited for yet
@@ -825,19 +836,32 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if (!ok) break;
                 if (two || !(h & 1)) used[0] |= 1u << st;
                 if (two || (h & 1)) used[1] |= 1u << st;
-                // token tok0 + 2 i + (lane >> 4), chunk oct of its row: 16-byte chunks of a row are swizzled by the token
-                const uint32_t dst = base + kOffV + st * kTile + (uint32_t)(oct >> 3) * kHalf + (uint32_t)(tok0 + (lane >> 4)) * 128u;
-                const uint32_t chunk = (uint32_t)((oct & 7) ^ (lane >> 4));
                 const int64_t room = limit - (int64_t)first;
                 const uint32_t most = room <= 0 ? 0u : room > 1024 ? 1024u : (uint32_t)room;   // groups left in the store
-                const uint4* src = packed + (int64_t)first * OPG + sub;
-#pragma unroll 4
-                for (int i = 0; i < 16; ++i) {
-                    const uint32_t tw = __shfl_sync(0xFFFFFFFFu, tok_word, 2 * i + (lane >> 4));
-                    const uint32_t at = (tw >> 16) + __popc(tw & below);
-                    const bool kept = ((tw >> grp) & 1u) && at < most;
-                    cp_async16_zfill(dst + (uint32_t)i * 256u + ((chunk ^ (uint32_t)(2 * (i & 3))) << 4),
-                                     kept ? src + at * OPG : packed, kept ? 16 : 0);
+                const uint4* src = packed + (int64_t)first * OPG + sub % OPG;
+#pragma unroll 1
+                for (int pass = 0; pass < LPT; ++pass) {
+                    const int tok = pass * (32 / LPT) + lane / LPT;      // of the warp's 32
+                    const uint32_t tw = __shfl_sync(0xFFFFFFFFu, tok_word, tok);
+                    uint32_t at = tw >> 16;          // place of the next kept group of the token
+                    const uint32_t row = base + kOffV + st * kTile + (uint32_t)(tok0 + tok) * 128u, swz = (uint32_t)(tok & 7);
+#pragma unroll
+                    for (int k = 0; k < 16 / LPT; ++k) {
+                        const uint32_t oct = (uint32_t)(k * LPT + sub);  // chunk of the row: half oct >> 3, swizzled by the token
+                        uint32_t mine_at = at;
+                        bool kept;
+                        if constexpr (GPL == 1) {
+                            kept = (tw >> k) & 1u;
+                            at += kept;
+                        } else {
+                            kept = (tw >> (2 * k + sub)) & 1u;
+                            if (sub) mine_at += (tw >> (2 * k)) & 1u;
+                            at += ((tw >> (2 * k)) & 1u) + ((tw >> (2 * k + 1)) & 1u);
+                        }
+                        kept = kept && mine_at < most;
+                        cp_async16_zfill(row + (oct >> 3) * kHalf + (((oct & 7u) ^ swz) << 4), kept ? src + mine_at * OPG : packed,
+                                         kept ? 16 : 0);
+                    }
                 }
                 cp_async_commit();
                 if (pending >= 0) { cp_async_wait<1>(); publish(); }
@@ -859,13 +883,16 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 }
 
 // Joins the partials of units that more than one CTA worked on, answers the rows whose prefix is empty, and gathers the
-// CTAs' status.  A block owns eight consecutive rows of a KV head (row = sequence * Gq + head within the KV
-// head) and four chunks of four dims, a thread one of each (8 rows x 16 bytes are mostly one 128-byte line of a partial);
-// its eight warps share the partials of the rows, in a fixed order, four loads in flight.
+// CTAs' status.  A thread owns four channels of one row (row = sequence * Gq + head within the KV head); a warp eight
+// consecutive rows by four such chunks (8 rows x 16 bytes are mostly one 128-byte line of a partial).  SPLIT = 1: the
+// eight warps take the row's 32 chunks and each thread all partials; SPLIT = 8: the warps share the partials of four
+// chunks, for calls with so few KV heads that a row has dozens of partials.  Eight loads in flight, a fixed order.
+template <int SPLIT>
 __global__ void __launch_bounds__(256)
 prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
-    __shared__ float4 sh_o[8][32];
-    __shared__ float2 sh_ml[8][32];
+    __shared__ float4 sh_o[SPLIT][32];
+    __shared__ float2 sh_ml[SPLIT][32];
+    asm volatile("griddepcontrol.wait;" ::: "memory");       // launched while the first kernel still runs
     const bool bad = a.base[a.G + 1] != 0;
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 32) {
         int st = 0;
@@ -873,10 +900,10 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
         st = __reduce_max_sync(0xFFFFFFFFu, st);
         if (threadIdx.x == 0) *a.status = bad ? (int)STC_ERR_INVALID_ARG : st;
     }
-    const int hk = blockIdx.x / chunks, part = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long long flat = (long long)(blockIdx.x - hk * chunks) * 8 + (lane >> 2);
-    const int d4 = blockIdx.y * 4 + (lane & 3);
-    const int seq = (int)(flat / a.Gq), in_head = (int)(flat - (long long)seq * a.Gq), head = hk * a.Gq + in_head;
+    const int hk = blockIdx.x / chunks, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = SPLIT == 1 ? 0 : warp;
+    const uint32_t flat = (uint32_t)(blockIdx.x - hk * chunks) * 8u + (uint32_t)(lane >> 2);     // below 2^31 + 8
+    const int d4 = (SPLIT == 1 ? warp : (int)blockIdx.y) * 4 + (lane & 3);
+    const int seq = (int)(flat / (uint32_t)a.Gq), in_head = (int)(flat - (uint32_t)seq * (uint32_t)a.Gq), head = hk * a.Gq + in_head;
     bool mine = !bad && seq < a.n_rows && seq >= a.row_start[0] && seq < a.row_start[a.G];
     float m = -INFINITY, l = 0.f, shift = 0.f, own_l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f), own = o;
@@ -891,21 +918,29 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
         const int in_group = seq - grp.row0, blk = in_group / (2 * a.seqs), in_blk = in_group - blk * 2 * a.seqs;
         const int n_seq = min(2 * a.seqs, grp.n_seq - blk * 2 * a.seqs);
         const bool two = n_seq > a.seqs;
-        // where the row's parts stand in a slot: lane of its first copy, copies, groups
+        // where the row's parts stand in a slot: lane of its first copy, copies and parts per slot (powers of two)
         const int tile = two ? in_blk / a.seqs : 0, in_tile = in_blk - tile * a.seqs, qr = in_tile / a.quarter;
         const int row = qr * 32 + (in_tile - qr * a.quarter) * a.Gq + in_head;
-        const int n_copies = copies(a, n_seq), per_slot = two ? 1 : 2 * n_copies;
+        const int n_copies = copies(a, n_seq), lg_copies = n_copies >> 1, lg_parts = two ? 0 : lg_copies + 1;
         int c0 = 0, n_parts = 0, late = 0;
         if (grp.tiles > 0) {
             const long long total = a.base[a.G], n = min(total, (long long)grid);
             const long long x0 = a.base[g] + ((long long)hk * grp.blocks + blk) * grp.tiles, x1 = x0 + grp.tiles;
             // the CTA whose range holds tile x is ceil((x + 1) * n / total) - 1; only the first of a unit's CTAs can
             // have begun before the unit, and then used its second slot for it
-            c0 = (int)(((x0 + 1) * n + total - 1) / total - 1);
-            const int c1 = (int)((x1 * n + total - 1) / total - 1);
-            late = total * c0 / n < x0 ? 1 : 0;
+            int c1;
+            if (total < (1 << 24)) {                 // everything below 2^32
+                const uint32_t t = (uint32_t)total, k = (uint32_t)n;
+                c0 = (int)((((uint32_t)x0 + 1u) * k + t - 1u) / t) - 1;
+                c1 = (int)(((uint32_t)x1 * k + t - 1u) / t) - 1;
+                late = t * (uint32_t)c0 / k < (uint32_t)x0 ? 1 : 0;
+            } else {
+                c0 = (int)(((x0 + 1) * n + total - 1) / total - 1);
+                c1 = (int)((x1 * n + total - 1) / total - 1);
+                late = total * c0 / n < x0 ? 1 : 0;
+            }
             mine = c0 != c1;                         // a whole unit was finished where it was computed
-            if (mine) n_parts = (c1 - c0 + 1) * per_slot;
+            if (mine) n_parts = (c1 - c0 + 1) << lg_parts;
         }
         if (mine) {
             if (a.own_lse) {
@@ -915,43 +950,54 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
             shift = bias_shift(a, grp.len, seq, head);
         }
 #pragma unroll 1
-        for (int e0 = part; e0 < n_parts; e0 += 32) {
-            float2 p[4];
-            float4 v[4];
+        for (int e0 = part; e0 < n_parts; e0 += 8 * SPLIT) {
+            float2 p[8];
+            float4 v[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int e = min(e0 + 8 * i, n_parts - 1), c = e / per_slot, k = e - c * per_slot;
-                const int w = two ? tile : k / n_copies, at = row + (two ? 0 : (k % n_copies) * (kRows / n_copies));
+            for (int i = 0; i < 8; ++i) {
+                const int e = min(e0 + SPLIT * i, n_parts - 1), c = e >> lg_parts, k = e - (c << lg_parts);
+                const int w = two ? tile : k >> lg_copies, at = row + (two ? 0 : (k & (n_copies - 1)) * (kRows >> lg_copies));
                 const size_t slot = (2 * (size_t)(c0 + c) + (c == 0 ? late : 0)) * 2 + w;
                 p[i] = __ldcg(a.part_ml + slot * kRows + at);
                 v[i] = __ldcg(a.part_o + (slot * 32 + d4) * kRows + at);
             }
+            float top = m;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (e0 + 8 * i >= n_parts || p[i].x == -INFINITY) continue;
-                const float top = fmaxf(m, p[i].x), fm = m == -INFINITY ? 0.f : ex2(m - top), fp = ex2(p[i].x - top);
-                l = fmaf(p[i].y, fp, l * fm);
-                o.x = fmaf(v[i].x, fp, o.x * fm); o.y = fmaf(v[i].y, fp, o.y * fm);
-                o.z = fmaf(v[i].z, fp, o.z * fm); o.w = fmaf(v[i].w, fp, o.w * fm);
-                m = top;
+            for (int i = 0; i < 8; ++i) {
+                if (e0 + SPLIT * i >= n_parts) p[i].x = -INFINITY;
+                top = fmaxf(top, p[i].x);
             }
+            if (top == -INFINITY) continue;
+            const float fm = m == -INFINITY ? 0.f : ex2(m - top);
+            l *= fm; o.x *= fm; o.y *= fm; o.z *= fm; o.w *= fm;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (p[i].x == -INFINITY) continue;   // (its sums may never have been written)
+                const float f = ex2(p[i].x - top);
+                l = fmaf(p[i].y, f, l);
+                o.x = fmaf(v[i].x, f, o.x); o.y = fmaf(v[i].y, f, o.y); o.z = fmaf(v[i].z, f, o.z); o.w = fmaf(v[i].w, f, o.w);
+            }
+            m = top;
         }
     }
-    sh_o[part][lane] = o;
-    sh_ml[part][lane] = make_float2(m, l);
-    __syncthreads();
-    if (part != 0 || !mine) return;
+    if constexpr (SPLIT > 1) {
+        sh_o[part][lane] = o;
+        sh_ml[part][lane] = make_float2(m, l);
+        __syncthreads();
+        if (part != 0) return;
 #pragma unroll
-    for (int i = 1; i < 8; ++i) {
-        const float2 p = sh_ml[i][lane];
-        const float4 v = sh_o[i][lane];
-        if (p.x == -INFINITY) continue;
-        const float top = fmaxf(m, p.x), fm = m == -INFINITY ? 0.f : ex2(m - top), fp = ex2(p.x - top);
-        l = fmaf(p.y, fp, l * fm);
-        o.x = fmaf(v.x, fp, o.x * fm); o.y = fmaf(v.y, fp, o.y * fm);
-        o.z = fmaf(v.z, fp, o.z * fm); o.w = fmaf(v.w, fp, o.w * fm);
-        m = top;
+        for (int i = 1; i < SPLIT; ++i) {
+            const float2 p = sh_ml[i][lane];
+            const float4 v = sh_o[i][lane];
+            if (p.x == -INFINITY) continue;
+            const float top = fmaxf(m, p.x), fm = m == -INFINITY ? 0.f : ex2(m - top), fp = ex2(p.x - top);
+            l = fmaf(p.y, fp, l * fm);
+            o.x = fmaf(v.x, fp, o.x * fm); o.y = fmaf(v.y, fp, o.y * fm);
+            o.z = fmaf(v.z, fp, o.z * fm); o.w = fmaf(v.w, fp, o.w * fm);
+            m = top;
+        }
     }
+    if (!mine) return;
     const Join j = join(m, l, shift, a.own_lse != nullptr, own_l);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (j.fo != 0.f) v = make_float4(o.x * j.fo, o.y * j.fo, o.z * j.fo, o.w * j.fo);
@@ -1057,8 +1103,21 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const int chunks = (int)(((long long)n_rows * g.Gq + 7) / 8);    // times Hkv: below 2^31, as n_rows * Hq is
-    prefix_merge_kernel<<<dim3((unsigned)(chunks * g.Hkv), 8), 256, 0, st>>>(a, n_cta, chunks);
-    return cudaGetLastError();
+    // about how many parts a row has: CTAs per unit (if the prefixes are alike) times copies and groups
+    const int most_copies = n_rows <= a.quarter ? 4 : n_rows <= 2 * a.quarter ? 2 : 1;
+    const long long parts = (long long)(n_cta / g.problems + 1) * (n_rows > a.seqs ? 1 : 2 * most_copies);
+    const bool split = parts > 24;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(chunks * g.Hkv), split ? 8 : 1);
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cudaLaunchAttribute early;                       // its blocks wait in place instead of behind a launch
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    return split ? cudaLaunchKernelEx(&cfg, prefix_merge_kernel<8>, a, n_cta, chunks)
+                 : cudaLaunchKernelEx(&cfg, prefix_merge_kernel<1>, a, n_cta, chunks);
 }
 
 }  // namespace stc
