@@ -33,10 +33,9 @@
 // its next tile runs while it works on this one, and its softmax waits for nothing else unless the maximum moves.
 // Few rows: a row tile is four quarters of 32 lanes (the lanes of one warp), and the softmax of a row is 64 scores of
 // one thread, so half-empty tiles would cost as much as full ones.  With at most two quarters of rows the tile holds
-// them twice, with at most one four times (rep = 2, 4); copy i weighs columns [i, i + 1) * 64 / rep and
-// writes zeros for the others, so each thread has 64 / rep scores and its own part of the sums.
-// Every (group, copy) thus keeps a running maximum, sum and accumulator of its own; they are joined like the
-// partials of different CTAs.
+// them twice; copy i weighs columns [32 i, 32 i + 32) and writes zeros for the others, so each thread has 32 scores.
+// At the end of a segment the groups join their accumulators (each reads both, for half of the channels); copies are joined
+// like the partials of different CTAs.
 //
 // The running maximum only moves when a tile exceeds it by more than 2^8, so the accumulator in tensor memory is
 // rescaled a few times per segment and not per tile; weights are then at most 2^8, far from fp32's limits.
@@ -65,7 +64,8 @@ constexpr uint32_t kQTile = 2 * kQHalf;           // 32 KiB
 constexpr uint32_t kHalf = kTok * 128;            // 64 channels of a token tile
 constexpr uint32_t kTile = 2 * kHalf;             // 16 KiB
 constexpr uint32_t kOffK = 2 * kQTile, kOffV = kOffK + kKStages * kTile, kOffCtl = kOffV + kVStages * kTile;
-constexpr uint32_t kCtlBytes = 1024;
+constexpr uint32_t kCtlMl = 1024;                 // [2 groups][128 lanes] maximum and sum, exchanged at a segment's end
+constexpr uint32_t kCtlBytes = kCtlMl + 2 * kRows * 8;
 constexpr uint32_t kSmem = kOffCtl + kCtlBytes;
 static_assert(kSmem <= 232448, "shared memory of a block");
 constexpr unsigned long long kWaitNs = 1000000000ull;
@@ -116,14 +116,17 @@ __device__ __forceinline__ float ex2(float x) {
 struct Group {
     int row0, n_seq, len, tiles, blocks;
 };
-__device__ __forceinline__ Group load_group(const PrefixArgs& a, int g) {
+__device__ __forceinline__ Group make_group(const PrefixArgs& a, int row0, int row1, int len) {
     Group r;
-    r.row0 = a.row_start[g];
-    r.n_seq = a.row_start[g + 1] - r.row0;
-    r.len = clamp_len(a.seq_len, g, a.T);
-    r.tiles = (r.len + kTok - 1) / kTok;
+    r.row0 = row0;
+    r.n_seq = row1 - row0;
+    r.len = len;
+    r.tiles = (len + kTok - 1) / kTok;
     r.blocks = (r.n_seq + 2 * a.seqs - 1) / (2 * a.seqs);
     return r;
+}
+__device__ __forceinline__ Group load_group(const PrefixArgs& a, int g) {
+    return make_group(a, a.row_start[g], a.row_start[g + 1], clamp_len(a.seq_len, g, a.T));
 }
 __device__ __forceinline__ long long group_tiles(const PrefixArgs& a, const Group& g) {
     return (long long)g.tiles * g.blocks * a.Hkv;
@@ -136,7 +139,7 @@ struct Segment {
 };
 // Copies of its rows that the row tile of a segment holds.
 __device__ __forceinline__ int copies(const PrefixArgs& a, int n_seq) {
-    return n_seq <= a.quarter ? 4 : n_seq <= 2 * a.quarter ? 2 : 1;
+    return n_seq <= 2 * a.quarter ? 2 : 1;
 }
 __device__ __forceinline__ long long div_small(long long x, int d) {        // x >= 0, d > 0
     return (x >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)d) : x / d;
@@ -146,11 +149,9 @@ __device__ __forceinline__ long long div_small(long long x, int d) {        // x
 struct Walker {
     long long x, x_end, x_begin, off;  // off = x - base of group g
     int g;
-    Group grp;
-    bool loaded;
+    Group grp;                   // group g
     __device__ __forceinline__ bool next(const PrefixArgs& a, Segment& s) {
         if (x >= x_end) return false;
-        if (!loaded) { grp = load_group(a, g); loaded = true; }
         while (off >= group_tiles(a, grp)) {
             off -= group_tiles(a, grp);
             grp = load_group(a, ++g);
@@ -246,11 +247,19 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     unsigned char* ctl = smem + kOffCtl;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctl + kCtlTmem);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + kCtlAbort);
+    float2* const ml = reinterpret_cast<float2*>(ctl + kCtlMl);
     volatile int* const segs = reinterpret_cast<volatile int*>(ctl + kCtlSegs);        // [kSegs][8]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     asm volatile("griddepcontrol.launch_dependents;");
 
-    // ---- set-up: barriers, tensor memory, this CTA's range ------------------------------------------
+    // ---- set-up: barriers, tensor memory; the scheduler's and the producer's first reads are under way meanwhile ------------
+    int first_r0 = 0, first_r1 = 0, first_len = 0;   // scheduler: prefix `lane`
+    if (warp == 3 && lane < a.G) {
+        first_r0 = a.row_start[lane];
+        first_r1 = a.row_start[lane + 1];
+        first_len = clamp_len(a.seq_len, lane, a.T);
+    }
+    if (warp == 0 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &map_k : &map_q) : "memory");
     if (threadIdx.x == 0) {
         for (int i = 0; i < kBars; ++i)
             mbar_init(bars + 8 * i, i >= kPFull && i < kOFull ? kRows : i == kXchg ? 2 * kRows : i >= kVFull && i < kVEmpty ? 2 : i >= kSegEmpty ? kSegReaders : 1);
@@ -416,42 +425,57 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             long long run = 0;
             for (int g0 = 0; g0 < a.G; g0 += 32) {
                 const int g = g0 + lane;
-                long long n = 0;
+                Group grp = {};
                 if (g < a.G) {
-                    const int r0 = a.row_start[g], r1 = a.row_start[g + 1];
+                    const int r0 = g0 ? a.row_start[g] : first_r0, r1 = g0 ? a.row_start[g + 1] : first_r1;
                     if (r0 < 0 || r1 < r0 || r1 > a.n_rows) bad = true;
-                    else n = group_tiles(a, load_group(a, g));
+                    else grp = make_group(a, r0, r1, g0 ? clamp_len(a.seq_len, g, a.T) : first_len);
                 }
+                const long long n = group_tiles(a, grp);
                 long long incl = n;
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) {
                     const long long o = __shfl_up_sync(0xFFFFFFFFu, incl, d);
                     if (lane >= d) incl += o;
                 }
-                use(g, run + incl - n, run + incl);
+                use(g, grp, run + incl - n, run + incl);
                 run += __shfl_sync(0xFFFFFFFFu, incl, 31);
             }
             return run;
         };
-        long long total = scan([&](int g, long long lo, long long) {
+        long long total = scan([&](int g, const Group&, long long lo, long long) {
             if (blockIdx.x == 0 && g < a.G) a.base[g] = lo;
         });
         bad = __any_sync(0xFFFFFFFFu, bad);
         if (bad) total = 0;
-        const long long n_cta = min(total, (long long)gridDim.x);         // with fewer tiles than CTAs the rest stay idle
+        // this CTA's range; with fewer tiles than CTAs the rest stay idle
+        const int n_cta = (int)min(total, (long long)gridDim.x), cta = (int)blockIdx.x;
         long long lo = 0, hi = 0;
-        if (blockIdx.x < n_cta) { lo = total * blockIdx.x / n_cta; hi = total * (blockIdx.x + 1) / n_cta; }
-        if (blockIdx.x == 0 && lane == 0) { a.base[a.G] = total; a.base[a.G + 1] = bad; }
-        long long off = lo;
+        if (cta < n_cta) {
+            if (total < (1 << 24)) {                 // everything below 2^32
+                lo = (uint32_t)total * (uint32_t)cta / (uint32_t)n_cta;
+                hi = (uint32_t)total * (uint32_t)(cta + 1) / (uint32_t)n_cta;
+            } else {
+                lo = total * cta / n_cta;
+                hi = total * (cta + 1) / n_cta;
+            }
+        }
+        if (cta == 0 && lane == 0) { a.base[a.G] = total; a.base[a.G + 1] = bad; }
+        long long off = 0;
         int g_first = 0;
-        if (hi > lo && a.G > 1) {
-            scan([&](int g, long long first, long long end) {
-                const bool here = g < a.G && first <= lo && lo < end;
-                const uint32_t who = __ballot_sync(0xFFFFFFFFu, here);
-                if (who) {
-                    off = __shfl_sync(0xFFFFFFFFu, lo - first, __ffs(who) - 1);
-                    g_first = __shfl_sync(0xFFFFFFFFu, g, __ffs(who) - 1);
-                }
+        Group at_first = {};
+        if (hi > lo) {
+            scan([&](int g, const Group& grp, long long first, long long end) {
+                const uint32_t who = __ballot_sync(0xFFFFFFFFu, g < a.G && first <= lo && lo < end);
+                if (!who) return;
+                const int from = __ffs(who) - 1;
+                off = lo - __shfl_sync(0xFFFFFFFFu, first, from);
+                g_first = __shfl_sync(0xFFFFFFFFu, g, from);
+                at_first.row0 = __shfl_sync(0xFFFFFFFFu, grp.row0, from);
+                at_first.n_seq = __shfl_sync(0xFFFFFFFFu, grp.n_seq, from);
+                at_first.len = __shfl_sync(0xFFFFFFFFu, grp.len, from);
+                at_first.tiles = __shfl_sync(0xFFFFFFFFu, grp.tiles, from);
+                at_first.blocks = __shfl_sync(0xFFFFFFFFu, grp.blocks, from);
             });
         }
         if (lane == 0) {
@@ -460,7 +484,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             walk.x_end = hi;
             walk.off = off;
             walk.g = g_first;
-            walk.loaded = false;
+            walk.grp = at_first;
             bool ok = true, more = true;
             for (int i = 0; ok && more; ++i) {
                 more = walk.next(a, s);
@@ -647,15 +671,10 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 mbar_arrive(bar(kPFull + 2 * w + buf));
                 ++n_s;
             }
-            // ---- end of the segment: this thread's (m, l, accumulator) ------------------------------------------
-            const bool whole = s.slot < 0, finish = whole && two;      // a row of a whole unit that is complete here
+            // ---- end of the segment -----------------------------------------------------------------------------
+            const bool whole = s.slot < 0;
             const size_t out_row = (size_t)seq * a.Hq + head;
             const float own_l = whole && a.own_lse && live ? a.own_lse[out_row] : -INFINITY;
-            const Join j = finish ? join(m, l, BIAS ? bias_shift(a, s.len, seq, head) : 0.f, a.own_lse != nullptr, own_l)
-                                  : Join{1.f, 0.f, 0.f};
-            const size_t slot = (size_t)(whole ? 2 * (int)gridDim.x + (int)blockIdx.x : s.slot) * 2;
-            if (!finish) __stcg(a.part_ml + (slot + w) * kRows + row, make_float2(m, l));
-            else if (live && a.lse) a.lse[out_row] = j.lse;
             if (mine > 0 && warp_live) {
                 ok = warp_wait(kOFull + 2 * w + ((n_s - 1) & 1u), (n_s - 1) >> 1);
                 if (!ok) return;
@@ -681,104 +700,107 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     }
                     tmem_wait_st();
                 }
-                if (!finish) {                       // a part as it stands
-                    float4* dst = a.part_o + (slot + w) * 32 * kRows + row;
+            }
+            // one row tile: both groups hold part of its rows; each joins them for half of the channels
+            float f0 = 1.f, f1 = 0.f;
+            uint32_t acc0 = to, acc1 = to;
+            int c_lo = 0, c_hi = kHeadDim;
+            if (!two) {
+                ml[w * kRows + row] = make_float2(m, l);
+                tc_before();
+                mbar_arrive(bar(kXchg));
+                ok = warp_wait(kXchg, n_x++);
+                if (!ok) return;
+                tc_after();
+                const float2 a0 = ml[row], a1 = ml[kRows + row];
+                m = fmaxf(a0.x, a1.x);
+                f0 = a0.x == -INFINITY ? 0.f : ex2(a0.x - m);
+                f1 = a1.x == -INFINITY ? 0.f : ex2(a1.x - m);
+                l = a0.y * f0 + a1.y * f1;
+                acc0 = lane_base + 256;
+                acc1 = lane_base + 384;
+                c_lo = 64 * w;
+                c_hi = c_lo + 64;
+            }
+            const bool part = !whole || REP > 1;     // one of several parts of the row: as it stands; else the row's output
+            const size_t slot = ((size_t)(whole ? 2 * (int)gridDim.x + (int)blockIdx.x : s.slot) * 2 + (two ? w : 0));
+            const Join j = part ? Join{1.f, 0.f, 0.f}
+                                : join(m, l, BIAS ? bias_shift(a, s.len, seq, head) : 0.f, a.own_lse != nullptr, own_l);
+            if (c_lo == 0) {
+                if (part) __stcg(a.part_ml + slot * kRows + row, make_float2(m, l));
+                else if (live && a.lse) a.lse[out_row] = j.lse;
+            }
+            if (warp_live) {
+                const bool add_own = !part && live && a.own_out && j.fown != 0.f, both_acc = f1 != 0.f;
+                const float4* own = reinterpret_cast<const float4*>(a.own_out) + out_row * 32;
+                float4* dst = part ? a.part_o + slot * 32 * kRows + row : reinterpret_cast<float4*>(a.out) + out_row * 32;
+                const int step = part ? kRows : 1;
 #pragma unroll 1
-                    for (int c = 0; c < kHeadDim; c += 64) {
-                        uint32_t q[64];
-                        tmem_ld16<0>(to + c, q);
-                        tmem_ld16<16>(to + c + 16, q);
-                        tmem_ld16<32>(to + c + 32, q);
-                        tmem_ld16<48>(to + c + 48, q);
-                        tmem_wait_ld();
+                for (int c = c_lo; c < c_hi; c += 16) {
+                    float4 mix[4];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            __stcg(dst + (size_t)(c / 4 + i) * kRows,
-                                   make_float4(__uint_as_float(q[4 * i]), __uint_as_float(q[4 * i + 1]),
-                                               __uint_as_float(q[4 * i + 2]), __uint_as_float(q[4 * i + 3])));
-                    }
-                } else {                             // the row's output
-                    const bool add_own = live && a.own_out && j.fown != 0.f;
-                    const float4* own = reinterpret_cast<const float4*>(a.own_out) + out_row * 32;
-                    float4* dst = reinterpret_cast<float4*>(a.out) + out_row * 32;
-#pragma unroll 1
-                    for (int c = 0; c < kHeadDim; c += 16) {
-                        float4 mix[4];
+                    for (int i = 0; i < 4; ++i) mix[i] = add_own ? own[c / 4 + i] : make_float4(0.f, 0.f, 0.f, 0.f);
+                    uint32_t q[16], q1[16];
+                    tmem_ld16(acc0 + c, q);
+                    tmem_ld16(acc1 + c, q1);
+                    tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) mix[i] = add_own ? own[c / 4 + i] : make_float4(0.f, 0.f, 0.f, 0.f);
-                        uint32_t q[16];
-                        tmem_ld16(to + c, q);
-                        tmem_wait_ld();
+                    for (int i = 0; i < 4; ++i) {
+                        float v[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {        // (a factor 0 stands for "nothing seen", whatever was summed)
-                            const float4 v = j.fo == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                                         : make_float4(__uint_as_float(q[4 * i]) * j.fo, __uint_as_float(q[4 * i + 1]) * j.fo,
-                                                                       __uint_as_float(q[4 * i + 2]) * j.fo, __uint_as_float(q[4 * i + 3]) * j.fo);
-                            if (live)
-                                dst[c / 4 + i] = make_float4(fmaf(mix[i].x, j.fown, v.x), fmaf(mix[i].y, j.fown, v.y),
-                                                             fmaf(mix[i].z, j.fown, v.z), fmaf(mix[i].w, j.fown, v.w));
+                        for (int e = 0; e < 4; ++e) {        // (a factor 0 stands for "nothing seen", whatever was summed)
+                            const float x = f0 != 0.f ? __uint_as_float(q[4 * i + e]) * f0 : 0.f;
+                            v[e] = both_acc ? fmaf(__uint_as_float(q1[4 * i + e]), f1, x) : x;
+                            v[e] = j.fo != 0.f ? v[e] * j.fo : 0.f;
                         }
+                        if (live || part)
+                            dst[(size_t)(c / 4 + i) * step] =
+                                make_float4(fmaf(mix[i].x, j.fown, v[0]), fmaf(mix[i].y, j.fown, v[1]),
+                                            fmaf(mix[i].z, j.fown, v[2]), fmaf(mix[i].w, j.fown, v[3]));
                     }
                 }
                 tc_before();
             }
-            if (!whole || two) return;
-            // ---- a whole unit of one row tile: the 2 * REP threads of a row join their parts, 16 / REP chunks of four dims each
-            __threadfence();
-            mbar_arrive(bar(kXchg));
-            ok = warp_wait(kXchg, n_x++);
-            if (!ok) return;
-            constexpr int E = 2 * REP, CH = 32 / E;
-            const int lane0 = (quarter % (4 / REP)) * 32 + lane, d0 = (w * REP + copy) * CH;
-            if (live) {
-                float fe[E], top = -INFINITY, sum = 0.f;
-                float2 p[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e) p[e] = __ldcg(a.part_ml + (slot + e / REP) * kRows + lane0 + (e % REP) * (kRows / REP));
-#pragma unroll
-                for (int e = 0; e < E; ++e) top = fmaxf(top, p[e].x);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    fe[e] = p[e].x == -INFINITY ? 0.f : ex2(p[e].x - top);
-                    sum = fmaf(p[e].y, fe[e], sum);
-                }
-                const Join jj = join(top, sum, BIAS ? bias_shift(a, s.len, seq, head) : 0.f, a.own_lse != nullptr, own_l);
-                float4* dst = reinterpret_cast<float4*>(a.out) + out_row * 32 + d0;
-                const float4* own = reinterpret_cast<const float4*>(a.own_out) + out_row * 32 + d0;
-                constexpr int BATCH = 8 / E;
-#pragma unroll 1
-                for (int d = 0; d < CH; d += BATCH) {
-                    float4 v[BATCH][E], o[BATCH];
-#pragma unroll
-                    for (int i = 0; i < BATCH; ++i) {
-#pragma unroll
-                        for (int e = 0; e < E; ++e)
-                            v[i][e] = fe[e] == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                                   : __ldcg(a.part_o + ((slot + e / REP) * 32 + d0 + d + i) * kRows + lane0 + (e % REP) * (kRows / REP));
-                        o[i] = a.own_out && jj.fown != 0.f ? own[d + i] : make_float4(0.f, 0.f, 0.f, 0.f);
-                    }
-#pragma unroll
-                    for (int i = 0; i < BATCH; ++i) {
-                        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            x.x = fmaf(v[i][e].x, fe[e], x.x); x.y = fmaf(v[i][e].y, fe[e], x.y);
-                            x.z = fmaf(v[i][e].z, fe[e], x.z); x.w = fmaf(v[i][e].w, fe[e], x.w);
+            if (two) return;
+            if constexpr (REP > 1) {
+                // a whole unit whose tile held its rows twice: the four threads of a row join the copies, 32 channels each
+                if (whole) {
+                    __threadfence();
+                    mbar_arrive(bar(kXchg));
+                    ok = warp_wait(kXchg, n_x++);
+                    if (!ok) return;
+                    const int lane0 = (quarter % (4 / REP)) * 32 + lane, d0 = (w * REP + copy) * (32 / (2 * REP));
+                    if (live) {
+                        const float2 p0 = __ldcg(a.part_ml + slot * kRows + lane0), p1 = __ldcg(a.part_ml + slot * kRows + lane0 + kRows / 2);
+                        const float top = fmaxf(p0.x, p1.x);
+                        const float e0 = p0.x == -INFINITY ? 0.f : ex2(p0.x - top), e1 = p1.x == -INFINITY ? 0.f : ex2(p1.x - top);
+                        const Join jj = join(top, p0.y * e0 + p1.y * e1, BIAS ? bias_shift(a, s.len, seq, head) : 0.f,
+                                             a.own_lse != nullptr, own_l);
+                        const float g0 = e0 * jj.fo, g1 = e1 * jj.fo;
+                        const float4* src = a.part_o + (slot * 32 + d0) * kRows + lane0;
+                        const float4* own = reinterpret_cast<const float4*>(a.own_out) + out_row * 32 + d0;
+                        float4* dst = reinterpret_cast<float4*>(a.out) + out_row * 32 + d0;
+                        const bool add_own = a.own_out && jj.fown != 0.f;
+#pragma unroll 4
+                        for (int i = 0; i < 32 / (2 * REP); ++i) {
+                            const float4 x = g0 != 0.f ? __ldcg(src + i * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            const float4 y = g1 != 0.f ? __ldcg(src + i * kRows + kRows / 2) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            const float4 z = add_own ? own[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+                            dst[i] = make_float4(fmaf(x.x, g0, fmaf(y.x, g1, z.x * jj.fown)), fmaf(x.y, g0, fmaf(y.y, g1, z.y * jj.fown)),
+                                                 fmaf(x.z, g0, fmaf(y.z, g1, z.z * jj.fown)), fmaf(x.w, g0, fmaf(y.w, g1, z.w * jj.fown)));
                         }
-                        dst[d + i] = make_float4(fmaf(o[i].x, jj.fown, x.x * jj.fo), fmaf(o[i].y, jj.fown, x.y * jj.fo),
-                                                 fmaf(o[i].z, jj.fown, x.z * jj.fo), fmaf(o[i].w, jj.fown, x.w * jj.fo));
+                        if (a.lse && d0 == 0) a.lse[out_row] = jj.lse;
                     }
                 }
-                if (a.lse && d0 == 0) a.lse[out_row] = jj.lse;
             }
-            mbar_arrive(bar(kXchg));                 // the scratch slot is free again
+            mbar_arrive(bar(kXchg));                 // the accumulators, the exchange and the scratch slot are free again
             ok = warp_wait(kXchg, n_x++);
+            tc_after();
         };
         while (ok && next_warp(ok)) {
             const int n_copies = copies(a, s.n_seq);
             if (n_copies == 1) segment(std::integral_constant<int, 64>{});
-            else if (n_copies == 2) segment(std::integral_constant<int, 32>{});
-            else segment(std::integral_constant<int, 16>{});
+            else segment(std::integral_constant<int, 32>{});
         }
         if (!ok) give_up();
     } else if (warp >= 12) {
@@ -893,6 +915,19 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
     __shared__ float4 sh_o[SPLIT][32];
     __shared__ float2 sh_ml[SPLIT][32];
     asm volatile("griddepcontrol.wait;" ::: "memory");       // launched while the first kernel still runs
+    const int lane = threadIdx.x & 31;
+    // everything that finds a row's unit in one round of loads: lane = prefix (more than 32: searched below)
+    const bool few = a.G <= 32;
+    int my_r0 = 0x7FFFFFFF, my_r1 = 0, my_len = 0;
+    long long my_base = 0;
+    if (few && lane < a.G) {
+        my_r0 = a.row_start[lane];
+        my_r1 = a.row_start[lane + 1];
+        my_len = clamp_len(a.seq_len, lane, a.T);
+        my_base = a.base[lane];
+    }
+    const long long total = a.base[a.G];
+    const int row_begin = a.row_start[0], row_end = a.row_start[a.G];
     const bool bad = a.base[a.G + 1] != 0;
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 32) {
         int st = 0;
@@ -900,32 +935,48 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
         st = __reduce_max_sync(0xFFFFFFFFu, st);
         if (threadIdx.x == 0) *a.status = bad ? (int)STC_ERR_INVALID_ARG : st;
     }
-    const int hk = blockIdx.x / chunks, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = SPLIT == 1 ? 0 : warp;
+    const int hk = blockIdx.x / chunks, warp = threadIdx.x >> 5, part = SPLIT == 1 ? 0 : warp;
     const uint32_t flat = (uint32_t)(blockIdx.x - hk * chunks) * 8u + (uint32_t)(lane >> 2);     // below 2^31 + 8
     const int d4 = (SPLIT == 1 ? warp : (int)blockIdx.y) * 4 + (lane & 3);
     const int seq = (int)(flat / (uint32_t)a.Gq), in_head = (int)(flat - (uint32_t)seq * (uint32_t)a.Gq), head = hk * a.Gq + in_head;
-    bool mine = !bad && seq < a.n_rows && seq >= a.row_start[0] && seq < a.row_start[a.G];
+    bool mine = !bad && seq < a.n_rows && seq >= row_begin && seq < row_end;
     float m = -INFINITY, l = 0.f, shift = 0.f, own_l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f), own = o;
     const size_t out_row = (size_t)seq * a.Hq + head;
-    if (mine) {
-        int g = 0, g_hi = a.G;                       // last prefix that starts at or before the row
+    if (mine && a.own_lse) {
+        own_l = a.own_lse[out_row];
+        own = reinterpret_cast<const float4*>(a.own_out + out_row * kHeadDim)[d4];
+    }
+    // last prefix that starts at or before the row
+    int g = 0;
+    Group grp = {};
+    long long base_g = 0;
+    if (few) {
+        for (int i = 1; i < a.G; ++i)
+            if (__shfl_sync(0xFFFFFFFFu, my_r0, i) <= seq) g = i;
+        grp = make_group(a, __shfl_sync(0xFFFFFFFFu, my_r0, g), __shfl_sync(0xFFFFFFFFu, my_r1, g), __shfl_sync(0xFFFFFFFFu, my_len, g));
+        base_g = __shfl_sync(0xFFFFFFFFu, my_base, g);
+    } else if (mine) {
+        int g_hi = a.G;
         while (g_hi - g > 1) {
             const int mid = (g + g_hi) >> 1;
             if (a.row_start[mid] <= seq) g = mid; else g_hi = mid;
         }
-        const Group grp = load_group(a, g);
+        grp = load_group(a, g);
+        base_g = a.base[g];
+    }
+    if (mine) {
         const int in_group = seq - grp.row0, blk = in_group / (2 * a.seqs), in_blk = in_group - blk * 2 * a.seqs;
         const int n_seq = min(2 * a.seqs, grp.n_seq - blk * 2 * a.seqs);
         const bool two = n_seq > a.seqs;
-        // where the row's parts stand in a slot: lane of its first copy, copies and parts per slot (powers of two)
+        // where the row's parts stand in a slot: row tile, lane of the first copy, log2 of the copies
         const int tile = two ? in_blk / a.seqs : 0, in_tile = in_blk - tile * a.seqs, qr = in_tile / a.quarter;
         const int row = qr * 32 + (in_tile - qr * a.quarter) * a.Gq + in_head;
-        const int n_copies = copies(a, n_seq), lg_copies = n_copies >> 1, lg_parts = two ? 0 : lg_copies + 1;
+        const int lg_copies = copies(a, n_seq) >> 1;         // (two row tiles: one copy)
         int c0 = 0, n_parts = 0, late = 0;
         if (grp.tiles > 0) {
-            const long long total = a.base[a.G], n = min(total, (long long)grid);
-            const long long x0 = a.base[g] + ((long long)hk * grp.blocks + blk) * grp.tiles, x1 = x0 + grp.tiles;
+            const long long n = min(total, (long long)grid);
+            const long long x0 = base_g + ((long long)hk * grp.blocks + blk) * grp.tiles, x1 = x0 + grp.tiles;
             // the CTA whose range holds tile x is ceil((x + 1) * n / total) - 1; only the first of a unit's CTAs can
             // have begun before the unit, and then used its second slot for it
             int c1;
@@ -940,24 +991,17 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
                 late = total * c0 / n < x0 ? 1 : 0;
             }
             mine = c0 != c1;                         // a whole unit was finished where it was computed
-            if (mine) n_parts = (c1 - c0 + 1) << lg_parts;
+            if (mine) n_parts = (c1 - c0 + 1) << lg_copies;
         }
-        if (mine) {
-            if (a.own_lse) {
-                own_l = a.own_lse[out_row];
-                own = reinterpret_cast<const float4*>(a.own_out + out_row * kHeadDim)[d4];
-            }
-            shift = bias_shift(a, grp.len, seq, head);
-        }
+        if (mine) shift = bias_shift(a, grp.len, seq, head);
 #pragma unroll 1
         for (int e0 = part; e0 < n_parts; e0 += 8 * SPLIT) {
             float2 p[8];
             float4 v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int e = min(e0 + SPLIT * i, n_parts - 1), c = e >> lg_parts, k = e - (c << lg_parts);
-                const int w = two ? tile : k >> lg_copies, at = row + (two ? 0 : (k & (n_copies - 1)) * (kRows >> lg_copies));
-                const size_t slot = (2 * (size_t)(c0 + c) + (c == 0 ? late : 0)) * 2 + w;
+                const int e = min(e0 + SPLIT * i, n_parts - 1), c = e >> lg_copies, at = row + (e - (c << lg_copies)) * (kRows / 2);
+                const size_t slot = (2 * (size_t)(c0 + c) + (c == 0 ? late : 0)) * 2 + tile;
                 p[i] = __ldcg(a.part_ml + slot * kRows + at);
                 v[i] = __ldcg(a.part_o + (slot * 32 + d4) * kRows + at);
             }
@@ -1103,10 +1147,8 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const int chunks = (int)(((long long)n_rows * g.Gq + 7) / 8);    // times Hkv: below 2^31, as n_rows * Hq is
-    // about how many parts a row has: CTAs per unit (if the prefixes are alike) times copies and groups
-    const int most_copies = n_rows <= a.quarter ? 4 : n_rows <= 2 * a.quarter ? 2 : 1;
-    const long long parts = (long long)(n_cta / g.problems + 1) * (n_rows > a.seqs ? 1 : 2 * most_copies);
-    const bool split = parts > 24;
+    // about how many parts a row has: CTAs per unit (if the prefixes are alike) times copies
+    const bool split = (n_cta / g.problems + 1) * (n_rows <= 2 * a.quarter ? 2 : 1) > 24;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(chunks * g.Hkv), split ? 8 : 1);
     cfg.blockDim = dim3(256);
