@@ -8,6 +8,7 @@ the shared library is missing the import of the library fails loudly.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from dataclasses import dataclass
 from pathlib import Path
 from typing import Optional
@@ -107,15 +108,16 @@ def load_library():
         lib.stc_decode_attn.argtypes = [C.POINTER(_Shape), C.POINTER(_Cache), C.c_void_p, C.c_void_p, C.c_void_p,
                                         C.c_int32, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
                                         C.c_void_p]
-        lib.stc_decode_attn_scored.argtypes = [C.POINTER(_Shape), C.POINTER(_Cache), C.c_void_p, C.c_void_p,
-                                               C.c_void_p, C.c_int32, C.c_float, C.POINTER(_Score), C.c_void_p,
-                                               C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
-        lib.stc_prefix_attn.argtypes = [C.POINTER(_Shape), C.POINTER(_Cache), C.c_int32, C.c_void_p, C.c_void_p,
-                                        C.c_float, C.POINTER(_Score), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
-                                        C.c_void_p, C.c_size_t, C.c_void_p]
+        # (structures of these calls: C.byref of the ctypes ones, or their bytes)
+        lib.stc_decode_attn_scored.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                               C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                               C.c_void_p]
+        lib.stc_prefix_attn.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p,
+                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                        C.c_void_p]
         lib.stc_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double,
                                              C.c_double, C.c_void_p, C.c_void_p]
-        lib.stc_rope_write.argtypes = [C.POINTER(_Shape), C.POINTER(_Rope), C.c_void_p, C.c_int32, C.c_void_p,
+        lib.stc_rope_write.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
                                        C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         lib.stc_decode_step.argtypes = [C.POINTER(_Shape), C.POINTER(_Cache), C.c_void_p, C.c_int32, C.c_int32,
@@ -142,11 +144,48 @@ def _ptr(t: Optional[torch.Tensor], dtype=None, name="tensor"):
         raise ValueError(f"{name} must be contiguous")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    return C.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
-def _stream() -> C.c_void_p:
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+def _stream() -> int:
+    return _raw_stream(_current_device())
+
+
+# The current device and its current stream without the objects torch.cuda wraps around them: a decode step's calls
+# take a few microseconds on the device, and the host's share of them is this module.
+_current_device = torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _at(t: Optional[torch.Tensor], dtype, device: int, name: str) -> int:
+    """Address of a contiguous tensor of `dtype` on CUDA device `device`; 0 for None."""
+    if t is None:
+        return 0
+    if t.get_device() == device and t.dtype is dtype and t.is_contiguous():
+        return t.data_ptr()
+    if t.is_cuda and t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, but the current device is cuda:{device}")
+    return _ptr(t, dtype, name)
+
+
+# Structures as the bytes the library reads (native layout of stc_shape, stc_cache, stc_score, stc_rope).
+_PACK_SHAPE = struct.Struct("8iP").pack
+_PACK_CACHE = struct.Struct("6Pq").pack
+_PACK_SCORE = struct.Struct("fi4P").pack
+_PACK_ROPE = struct.Struct("Piifi").pack
+
+
+def _pack_shape(s: "Shape", device: int) -> bytes:
+    return _PACK_SHAPE(s.batch, s.n_q_heads, s.n_kv_heads, s.head_dim, s.page_size, s.n_groups, s.t_cap, 0,
+                       _at(s.seq_len, torch.int32, device, "seq_len"))
+
+
+def _pack_cache(c: "Cache", device: int) -> bytes:
+    bf16 = torch.bfloat16
+    return _PACK_CACHE(_at(c.k, bf16, device, "k"), 0, 0, _at(c.v_packed, bf16, device, "v_packed"),
+                       0 if c.v_mask is None else _at(c.v_mask, c.v_mask.dtype, device, "v_mask"),
+                       0 if c.v_offs is None else _at(c.v_offs, c.v_offs.dtype, device, "v_offs"), c.cap_groups)
 
 
 @dataclass
@@ -215,14 +254,15 @@ class Score:
     tok_doc: Optional[torch.Tensor] = None    # i32 [B, T]
     q_doc: Optional[torch.Tensor] = None      # i32, one per query row
 
-    def c(self, shape: Shape, rows: int) -> _Score:
+    def packed(self, shape: Shape, rows: int, device: int) -> bytes:
         _sized(self.slopes, (shape.n_q_heads,), "slopes")
         _sized(self.q_pos, (rows,), "q_pos")
         _sized(self.tok_doc, (shape.batch, shape.t_cap), "tok_doc")
         _sized(self.q_doc, (rows,), "q_doc")
-        return _Score(self.softcap, self.window, _ptr(self.slopes, torch.float32, "slopes"),
-                      _ptr(self.q_pos, torch.int32, "q_pos"), _ptr(self.tok_doc, torch.int32, "tok_doc"),
-                      _ptr(self.q_doc, torch.int32, "q_doc"))
+        return _PACK_SCORE(self.softcap, self.window, _at(self.slopes, torch.float32, device, "slopes"),
+                           _at(self.q_pos, torch.int32, device, "q_pos"),
+                           _at(self.tok_doc, torch.int32, device, "tok_doc"),
+                           _at(self.q_doc, torch.int32, device, "q_doc"))
 
 
 @dataclass
@@ -232,39 +272,32 @@ class Rope:
     interleaved: bool = False
     scale: float = 1.0
 
-    def c(self) -> _Rope:
-        return _Rope(_ptr(self.inv_freq, torch.float64, "inv_freq"), 2 * self.inv_freq.numel(), int(self.interleaved),
-                     self.scale, 0)
+    def packed(self, device: int) -> bytes:
+        return _PACK_ROPE(_at(self.inv_freq, torch.float64, device, "inv_freq"), 2 * self.inv_freq.numel(),
+                          int(self.interleaved), self.scale, 0)
 
 
-def _sized(t: Optional[torch.Tensor], size, name: str) -> None:
-    if t is not None and tuple(t.shape) != tuple(size):
-        raise ValueError(f"{name} must have shape {tuple(size)}, got {tuple(t.shape)}")
+def _sized(t: Optional[torch.Tensor], size: tuple, name: str) -> None:
+    if t is not None and t.shape != size:
+        raise ValueError(f"{name} must have shape {size}, got {tuple(t.shape)}")
 
 
-def _on_current_device(*tensors) -> None:
-    """The call goes to the current device's stream: every tensor has to live there."""
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != here:
-            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
-
-
-def _token_rows(t: Optional[torch.Tensor], shape: Shape, heads: int, name: str):
-    """(pointer, elements from token to token) of rows [B, n, heads, 128] that may be a slice of wider token rows."""
+def _token_rows(t: Optional[torch.Tensor], B: int, n: int, heads: int, dim: int, device: int, name: str):
+    """(address, elements from token to token) of rows [B, n, heads, dim] that may be a slice of wider token rows."""
     if t is None:
-        return None, 0
-    if not t.is_cuda or t.dtype != torch.bfloat16:
-        raise ValueError(f"{name} must be a CUDA tensor of torch.bfloat16")
-    if t.dim() != 4 or t.shape[0] != shape.batch or t.shape[2:] != (heads, shape.head_dim):
-        raise ValueError(f"{name} must have shape [{shape.batch}, n, {heads}, {shape.head_dim}], got {tuple(t.shape)}")
-    B, n = t.shape[:2]
-    if t.numel() == 0:
-        return C.c_void_p(t.data_ptr()), heads * shape.head_dim
-    step = t.stride(1) if n > 1 else t.stride(0) if B > 1 else heads * shape.head_dim
-    if t.stride(3) != 1 or (heads > 1 and t.stride(2) != shape.head_dim) or (B > 1 and t.stride(0) != n * step):
+        return 0, 0
+    if t.get_device() != device or t.dtype is not torch.bfloat16:
+        raise ValueError(f"{name} must be a tensor of torch.bfloat16 on cuda:{device}, got {t.dtype} on {t.device}")
+    if t.shape != (B, n, heads, dim):
+        raise ValueError(f"{name} must have shape {(B, n, heads, dim)}, got {tuple(t.shape)}")
+    at, width = t.data_ptr(), heads * dim
+    if B == 0 or n == 0:
+        return at, width
+    sb, sn, sh, sd = t.stride()
+    step = sn if n > 1 else sb if B > 1 else width
+    if sd != 1 or (heads > 1 and sh != dim) or (B > 1 and sb != n * step):
         raise ValueError(f"{name}: a token's rows must be contiguous and tokens equally spaced, got strides {t.stride()}")
-    return C.c_void_p(t.data_ptr()), step
+    return at, step
 
 
 def _check(rc: int, where: str):
@@ -397,28 +430,26 @@ def rope_write(shape: Shape, rope: Rope, old_len: torch.Tensor, status: torch.Te
 
     q_in / k_in / v_in [B, n, heads, 128] (slices of one fused projection allowed) -> q_out [B, n, Hq, 128],
     k, v [B, Hkv, T, 128]; n is the most new tokens of a sequence; positions i32 [B, n] or None (= cache index)."""
-    B, T, D = shape.batch, shape.t_cap, shape.head_dim
-    given = [x for x in (q_in, k_in, v_in) if x is not None]
-    if not given:
+    B, T, D, Hq, Hkv = shape.batch, shape.t_cap, shape.head_dim, shape.n_q_heads, shape.n_kv_heads
+    first = q_in if q_in is not None else k_in if k_in is not None else v_in
+    if first is None:
         raise ValueError("rope_write needs at least one of q_in, k_in, v_in")
-    n = given[0].shape[1]
-    if any(x.shape[1] != n for x in given):
-        raise ValueError("q_in, k_in and v_in must hold the same number of tokens")
-    qp, qs = _token_rows(q_in, shape, shape.n_q_heads, "q_in")
-    kp, ks = _token_rows(k_in, shape, shape.n_kv_heads, "k_in")
-    vp, vs = _token_rows(v_in, shape, shape.n_kv_heads, "v_in")
-    _sized(q_out, (B, n, shape.n_q_heads, D), "q_out")
-    _sized(k, (B, shape.n_kv_heads, T, D), "k")
-    _sized(v, (B, shape.n_kv_heads, T, D), "v")
+    n, dev, bf16 = first.shape[1], _current_device(), torch.bfloat16
+    qp, qs = _token_rows(q_in, B, n, Hq, D, dev, "q_in")
+    kp, ks = _token_rows(k_in, B, n, Hkv, D, dev, "k_in")
+    vp, vs = _token_rows(v_in, B, n, Hkv, D, dev, "v_in")
+    _sized(q_out, (B, n, Hq, D), "q_out")
+    _sized(k, (B, Hkv, T, D), "k")
+    _sized(v, (B, Hkv, T, D), "v")
     _sized(positions, (B, n), "positions")
     _sized(old_len, (B,), "old_len")
     _sized(status, (B,), "status")
-    _on_current_device(q_in, k_in, v_in, q_out, k, v, positions, old_len, status, rope.inv_freq, shape.seq_len)
-    cs, cr = shape.c(), rope.c()
-    _check(load_library().stc_rope_write(
-        C.byref(cs), C.byref(cr), _ptr(old_len, torch.int32, "old_len"), n, _ptr(positions, torch.int32, "positions"),
-        qp, qs, kp, ks, vp, vs, _ptr(q_out, torch.bfloat16, "q_out"), _ptr(k, torch.bfloat16, "k"),
-        _ptr(v, torch.bfloat16, "v"), _ptr(status, torch.int32, "status"), _stream()), "stc_rope_write")
+    rc = load_library().stc_rope_write(
+        _pack_shape(shape, dev), rope.packed(dev), _at(old_len, torch.int32, dev, "old_len"), n,
+        _at(positions, torch.int32, dev, "positions"), qp, qs, kp, ks, vp, vs, _at(q_out, bf16, dev, "q_out"),
+        _at(k, bf16, dev, "k"), _at(v, bf16, dev, "v"), _at(status, torch.int32, dev, "status"), _raw_stream(dev))
+    if rc:
+        raise StcError(rc, "stc_rope_write")
 
 
 def route_new_pages(shape: Shape, cache: Cache, scores: torch.Tensor, first_page: torch.Tensor, k_nominal: int,
@@ -457,16 +488,17 @@ def decode_attn(shape: Shape, cache: Cache, q: torch.Tensor, page_ids: Optional[
                 lse: Optional[torch.Tensor] = None, score: Optional[Score] = None) -> None:
     """score: capped / biased / windowed / per-document scores (stc_decode_attn_scored)."""
     max_pages = page_ids.shape[-1] if page_ids is not None else shape.n_pages
-    cs, cc = shape.c(), cache.c()
     if score is not None:
-        _on_current_device(q, out, ws, cache.k, score.slopes, score.q_pos, score.tok_doc, score.q_doc)
-        co = score.c(shape, shape.batch)
-        _check(load_library().stc_decode_attn_scored(
-            C.byref(cs), C.byref(cc), _ptr(q, torch.bfloat16, "q"), _ptr(page_ids, torch.int32, "page_ids"),
-            _ptr(n_pages, torch.int32, "n_pages"), max_pages, sm_scale, C.byref(co), _ptr(out, torch.float32, "out"),
-            _ptr(lse, torch.float32, "lse"), _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream()),
-            "stc_decode_attn_scored")
+        dev = _current_device()
+        rc = load_library().stc_decode_attn_scored(
+            _pack_shape(shape, dev), _pack_cache(cache, dev), _at(q, torch.bfloat16, dev, "q"),
+            _at(page_ids, torch.int32, dev, "page_ids"), _at(n_pages, torch.int32, dev, "n_pages"), max_pages, sm_scale,
+            score.packed(shape, shape.batch, dev), _at(out, torch.float32, dev, "out"), _at(lse, torch.float32, dev, "lse"),
+            _at(ws, torch.uint8, dev, "ws"), ws.numel(), _raw_stream(dev))
+        if rc:
+            raise StcError(rc, "stc_decode_attn_scored")
         return
+    cs, cc = shape.c(), cache.c()
     _check(load_library().stc_decode_attn(
         C.byref(cs), C.byref(cc), _ptr(q, torch.bfloat16, "q"), _ptr(page_ids, torch.int32, "page_ids"),
         _ptr(n_pages, torch.int32, "n_pages"), max_pages, sm_scale, _ptr(out, torch.float32, "out"),
@@ -479,24 +511,21 @@ def prefix_attn(shape: Shape, cache: Cache, q: torch.Tensor, row_start: torch.Te
                 own_out: Optional[torch.Tensor] = None, own_lse: Optional[torch.Tensor] = None) -> None:
     """Rows row_start[g] .. row_start[g+1] of q [n_rows, Hq, 128] attend prefix g (sequence g of shape / cache), read
     once for all of them; own_out / own_lse (the rows' results over their own tokens) are joined by log-sum-exp."""
-    n = q.shape[0]
-    _sized(q, (n, shape.n_q_heads, shape.head_dim), "q")
+    n, Hq, dev, f32 = q.shape[0], shape.n_q_heads, _current_device(), torch.float32
+    rows = (n, Hq, shape.head_dim)
+    _sized(q, rows, "q")
     _sized(row_start, (shape.batch + 1,), "row_start")
-    _sized(out, (n, shape.n_q_heads, shape.head_dim), "out")
-    _sized(lse, (n, shape.n_q_heads), "lse")
-    _sized(own_out, (n, shape.n_q_heads, shape.head_dim), "own_out")
-    _sized(own_lse, (n, shape.n_q_heads), "own_lse")
-    _on_current_device(q, row_start, out, ws, lse, own_out, own_lse, cache.k, cache.v_packed, shape.seq_len)
-    cs, cc = shape.c(), cache.c()
-    co = None
-    if score is not None:
-        _on_current_device(score.slopes, score.q_pos, score.tok_doc, score.q_doc)
-        co = C.byref(score.c(shape, n))
-    _check(load_library().stc_prefix_attn(
-        C.byref(cs), C.byref(cc), n, _ptr(q, torch.bfloat16, "q"), _ptr(row_start, torch.int32, "row_start"), sm_scale,
-        co, _ptr(own_out, torch.float32, "own_out"), _ptr(own_lse, torch.float32, "own_lse"),
-        _ptr(out, torch.float32, "out"), _ptr(lse, torch.float32, "lse"), _ptr(ws, torch.uint8, "ws"), ws.numel(),
-        _stream()), "stc_prefix_attn")
+    _sized(out, rows, "out")
+    _sized(lse, (n, Hq), "lse")
+    _sized(own_out, rows, "own_out")
+    _sized(own_lse, (n, Hq), "own_lse")
+    rc = load_library().stc_prefix_attn(
+        _pack_shape(shape, dev), _pack_cache(cache, dev), n, _at(q, torch.bfloat16, dev, "q"),
+        _at(row_start, torch.int32, dev, "row_start"), sm_scale, score.packed(shape, n, dev) if score is not None else None,
+        _at(own_out, f32, dev, "own_out"), _at(own_lse, f32, dev, "own_lse"), _at(out, f32, dev, "out"),
+        _at(lse, f32, dev, "lse"), _at(ws, torch.uint8, dev, "ws"), ws.numel(), _raw_stream(dev))
+    if rc:
+        raise StcError(rc, "stc_prefix_attn")
 
 
 def decode_step(shape: Shape, cache: Cache, q: torch.Tensor, token_budget: int, page_ids: torch.Tensor,
