@@ -238,6 +238,11 @@ cudaError_t launch_rope_write(const Geom& g, const stc_rope& rope, const int32_t
                               int64_t k_stride, const void* v_in, int64_t v_stride, void* q_out, void* k, void* v,
                               int32_t* status, cudaStream_t st);
 
+cudaError_t launch_scored_attn(const Geom& g, const void* k, const void* v_packed, const uint16_t* v_mask,
+                               const uint32_t* v_offs, int64_t cap_groups, const void* q, const int32_t* page_ids,
+                               const int32_t* n_pages, int max_pages, float sm_scale, const ScoreArgs& score, float* out,
+                               float* lse, void* ws, cudaStream_t st);
+
 size_t prefix_ws_bytes(const Geom& g, int n_rows);
 cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packed, const uint16_t* v_mask,
                                const uint32_t* v_offs, int64_t cap_groups, int n_rows, const void* q,
@@ -251,7 +256,7 @@ cudaError_t launch_decode_attn(const Geom& g, const void* k, const void* v_packe
                                const uint16_t* v_mask, const uint32_t* v_offs, int64_t cap_groups,
                                const void* q, const int32_t* page_ids, const int32_t* n_pages,
                                int max_pages, float sm_scale, float* out, float* lse, void* ws,
-                               cudaStream_t st, unsigned flags = 0, const ScoreArgs* score = nullptr);
+                               cudaStream_t st, unsigned flags = 0);
 cudaError_t clear_decode_attn_ws(const Geom& g, void* ws, cudaStream_t st);
 size_t decode_attn_clear_bytes(const Geom& g);     // leading bytes of the workspace a call needs zeroed
 

@@ -41,7 +41,7 @@
 // Every wait on an mbarrier is bounded (about a second); a wait that expires
 // records STC_ERR_TIMEOUT in the workspace status word and the warp stops issuing
 // copies, skips its arithmetic and leaves without touching the outputs.
-#include "common.cuh"
+#include "warp_mma.cuh"
 
 namespace stc {
 namespace {
@@ -65,29 +65,6 @@ __host__ __device__ constexpr uint32_t smem_bytes(int stages) {      // ring + z
 }
 constexpr unsigned long long kWaitLimitNs = 1000000000ull;
 
-// ---- PTX wrappers -----------------------------------------------------------------------
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                         uint32_t b0, uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
-        "{%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a) {
-    uint32_t d;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
-    return d;
-}
-__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2,
-                                                  uint32_t& r3) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<uint32_t*>(&v);
-}
 // Bounded wait for a stage's copies.  False = gave up.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
     return mbar_wait_bounded(bar, parity, kWaitLimitNs);
@@ -114,9 +91,6 @@ struct AttnArgs {
     int slots_cap;
     int Hq, Hkv, Gq, T, max_pages;
     float scale_log2;    // sm_scale * log2(e)
-    ScoreArgs sc;        // read by the scored kernels only
-    float cap_in;        // sm_scale / softcap
-    float cap_log2;      // softcap * log2(e)
 };
 
 // What a lane remembers about one page of the 32-page lookahead window.
@@ -127,11 +101,7 @@ struct PageRef {
     uint32_t groups;     // packed groups of the page actually stored
 };
 
-// SCORED: capped scores, a bias linear in the distance, a window and a document mask (stc_score).
-// Per page and lane that is a handful of fp32 operations on at most four scores, under copies that take
-// ten times as long, so the scored kernels run at the pace of the plain ones; pages that the window
-// hides from the query are not copied at all.
-template <int S, bool MMA, int kStages, bool SCORED>
+template <int S, bool MMA, int kStages>
 __global__ void __launch_bounds__(kThreads, kStages == kStagesLean ? 3 : (kStages == kStagesWide ? kCtasPerSm : 1))
 decode_attn_kernel(const AttnArgs a) {
     constexpr uint32_t kRingBytes = ring_bytes(kStages);
@@ -173,14 +143,7 @@ decode_attn_kernel(const AttnArgs a) {
                 n_list = min(max(a.n_pages[p], 0), mp);
                 id = a.page_ids[(size_t)p * mp + slot];
             }
-            bool seen = slot < n_list && id >= 0 && id < np;
-            if constexpr (SCORED) {
-                const int b = p / a.Hkv;
-                int lo, hi;
-                visible_range(len, a.sc.q_pos ? a.sc.q_pos[b] : len - 1, a.sc.window, lo, hi);
-                seen = seen && id * kPage < hi && (id + 1) * kPage > lo;
-            }
-            if (seen) {
+            if (slot < n_list && id >= 0 && id < np) {
                 const int t0 = id * kPage, nv = min(kPage, len - t0);
                 const uint32_t* o = a.v_offs + (size_t)p * (a.T + 1) + t0;
                 const long long ob = min((long long)o[0], (long long)a.cap_groups);
@@ -196,8 +159,6 @@ decode_attn_kernel(const AttnArgs a) {
         int nv;              // valid tokens; 0 = nothing to attend at this position
         uint32_t chunks;     // 16-byte chunks of the value span present in the stage
         uint32_t mask;       // lanes 0..15: group mask of token `lane`
-        int t0;              // SCORED: first token of the page
-        int doc;             // SCORED: lanes 0..15: document of token `lane`
     };
     uint32_t phase = 0;                          // bit s = parity to wait for on stage s
 
@@ -208,7 +169,7 @@ decode_attn_kernel(const AttnArgs a) {
     int slot_issue = (int)(x_lo - (long long)p_issue * mp);
 
     auto issue = [&](int s, bool reuse) -> InFlight {   // bring position x_issue into stage s
-        InFlight f{0, 0u, 0u, 0, -1};
+        InFlight f{0, 0u, 0u};
         if (x_issue >= x_hi) return f;
         if (x_issue - win_base >= 32) { win_base = x_issue; fill_window(win_base); }
         const int src = (int)(x_issue - win_base);
@@ -219,11 +180,6 @@ decode_attn_kernel(const AttnArgs a) {
         if (page >= 0) {
             const size_t row0 = (size_t)p_issue * a.T + (size_t)page * kPage;
             if (lane < nv) f.mask = a.v_mask[row0 + lane];
-            if constexpr (SCORED) {
-                f.t0 = page * kPage;
-                if (a.sc.tok_doc && lane < nv)
-                    f.doc = a.sc.tok_doc[(size_t)(p_issue / a.Hkv) * a.T + (size_t)f.t0 + lane];
-            }
             f.nv = nv;
             f.chunks = groups * OPG;
             if (lane == 0) {
@@ -246,26 +202,8 @@ decode_attn_kernel(const AttnArgs a) {
     // MMA: lane (r, c) holds chunks c, c+4, c+8, c+12 of head r (zeros past Gq) = B fragments.
     // FMA: the same chunks of the single head.
     uint4 qa[4];
-    // SCORED: the tokens [lo, hi) the problem's query may see, its document, and per head of the lane
-    // the slope in log2 units.  The bias is taken against token hi - 1 instead of the query, which
-    // cancels in the softmax and keeps it small for the tokens that count even if the query stands far
-    // behind them; lse gets the difference back.
-    int see_lo = 0, see_hi = 0, my_doc = 0;
-    float slope2[2] = {0.f, 0.f};
     auto load_q = [&](int problem) {
         const int b = problem / a.Hkv, hk = problem - b * a.Hkv;
-        if constexpr (SCORED) {
-            const int len = clamp_len(a.seq_len, b, a.T);
-            visible_range(len, a.sc.q_pos ? a.sc.q_pos[b] : len - 1, a.sc.window, see_lo, see_hi);
-            if (a.sc.tok_doc) my_doc = a.sc.q_doc[b];
-            if (a.sc.slopes) {
-#pragma unroll
-                for (int e = 0; e < (MMA ? 2 : 1); ++e) {
-                    const int h = MMA ? 2 * c + e : 0;
-                    slope2[e] = h < a.Gq ? a.sc.slopes[hk * a.Gq + h] * 1.4426950408889634f : 0.f;
-                }
-            }
-        }
         const int head = MMA ? r : 0;
         const bool ok = head < a.Gq;
         const uint4* qrow = a.q + ((size_t)b * a.Hq + (size_t)hk * a.Gq + (ok ? head : 0)) * kOctets;
@@ -286,37 +224,10 @@ decode_attn_kernel(const AttnArgs a) {
         l_run[0] = l_run[1] = 0.f;
     };
 
-    // score in log2 units of token t from the raw product (SCORED)
-    auto scored = [&](float qk, int t, float slope) {
-        const float x = a.sc.softcap > 0.f ? a.cap_log2 * tanh_f32(qk * a.cap_in) : qk * a.scale_log2;
-        return fmaf(slope, (float)(t - (see_hi - 1)), x);
-    };
-    // what lse of head h (of the problem) lacks: slope * (hi - 1 - position of the query)
-    auto lse_shift = [&](int problem, int h) -> float {
-        if constexpr (!SCORED) return 0.f;
-        if (!a.sc.slopes) return 0.f;
-        const int b = problem / a.Hkv, hk = problem - b * a.Hkv;
-        const int len = clamp_len(a.seq_len, b, a.T), pos = a.sc.q_pos ? a.sc.q_pos[b] : len - 1;
-        int lo, hi;
-        visible_range(len, pos, a.sc.window, lo, hi);
-        return a.sc.slopes[hk * a.Gq + h] * (float)(hi - 1 - pos);
-    };
-
     // ---- one page -----------------------------------------------------------------------------
     auto compute = [&](int s, const InFlight& f) {
         const uint32_t kst = ring + (uint32_t)s * kStageBytes, vst = kst + kKeyBytes;
         const int nv = f.nv;
-        uint32_t vis = 0;                        // SCORED: bit i = token i of the page is visible
-        uint32_t mask = f.mask;                  // groups that may be read: none of a token that is not visible,
-        if constexpr (SCORED) {                  // whose stored values may be anything
-            const int t = f.t0 + lane;
-            const bool ok = lane < nv && t >= see_lo && t < see_hi &&
-                            (!a.sc.tok_doc || f.doc < 0 || f.doc == my_doc);
-            vis = __ballot_sync(0xFFFFFFFFu, ok);
-            if (vis == 0) return;
-            if (!ok) mask = 0;
-        }
-        auto valid = [&](int i) { return SCORED ? ((vis >> i) & 1u) != 0 : i < nv; };
         // exclusive prefix (in groups) of the page's token masks, lanes 0..15
         const uint32_t cnt = __popc(f.mask);
         uint32_t pre = cnt;
@@ -337,25 +248,19 @@ decode_attn_kernel(const AttnArgs a) {
                 mma_bf16(s0, k0.x, k1.x, k0.y, k1.y, qa[j].x, qa[j].y);
                 mma_bf16(s1, k0.z, k1.z, k0.w, k1.w, qa[j].z, qa[j].w);
             }
-            const bool v0 = valid(r), v1 = valid(r + 8);
+            const bool v0 = r < nv, v1 = r + 8 < nv;
             float sv[4];
-            if constexpr (SCORED) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    sv[i] = (i < 2 ? v0 : v1) ? scored(s0[i] + s1[i], f.t0 + r + (i < 2 ? 0 : 8), slope2[i & 1]) : -INFINITY;
-            } else {
-                sv[0] = v0 ? (s0[0] + s1[0]) * a.scale_log2 : -INFINITY;
-                sv[1] = v0 ? (s0[1] + s1[1]) * a.scale_log2 : -INFINITY;
-                sv[2] = v1 ? (s0[2] + s1[2]) * a.scale_log2 : -INFINITY;
-                sv[3] = v1 ? (s0[3] + s1[3]) * a.scale_log2 : -INFINITY;
-            }
+            sv[0] = v0 ? (s0[0] + s1[0]) * a.scale_log2 : -INFINITY;
+            sv[1] = v0 ? (s0[1] + s1[1]) * a.scale_log2 : -INFINITY;
+            sv[2] = v1 ? (s0[2] + s1[2]) * a.scale_log2 : -INFINITY;
+            sv[3] = v1 ? (s0[3] + s1[3]) * a.scale_log2 : -INFINITY;
             float pm0 = fmaxf(sv[0], sv[2]), pm1 = fmaxf(sv[1], sv[3]);
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) {
                 pm0 = fmaxf(pm0, __shfl_xor_sync(0xFFFFFFFFu, pm0, d));
                 pm1 = fmaxf(pm1, __shfl_xor_sync(0xFFFFFFFFu, pm1, d));
             }
-            const float mn0 = fmaxf(m_run[0], pm0), mn1 = fmaxf(m_run[1], pm1);   // finite: a token is valid
+            const float mn0 = fmaxf(m_run[0], pm0), mn1 = fmaxf(m_run[1], pm1);   // finite: token 0 is valid
             const float al0 = exp2f(m_run[0] - mn0), al1 = exp2f(m_run[1] - mn1);
             const float p0 = exp2f(sv[0] - mn0), p1 = exp2f(sv[1] - mn1);
             const float p2 = exp2f(sv[2] - mn0), p3 = exp2f(sv[3] - mn1);
@@ -370,7 +275,7 @@ decode_attn_kernel(const AttnArgs a) {
             const uint32_t bl0 = movmatrix_trans(wl0), bl1 = movmatrix_trans(wl1);
             // value rows: this lane addresses token tau, chunk 2dt + hb of every dim tile
             const int tau = (lane & 7) + 8 * (lane >> 4), hb = (lane >> 3) & 1;
-            const uint32_t m = __shfl_sync(0xFFFFFFFFu, mask, tau);
+            const uint32_t m = __shfl_sync(0xFFFFFFFFu, f.mask, tau);
             const uint32_t base = __shfl_sync(0xFFFFFFFFu, pre, tau) * OPG;
             const uint32_t limit = f.chunks;
 #pragma unroll
@@ -410,7 +315,7 @@ decode_attn_kernel(const AttnArgs a) {
                 float d = d0 + d1;
                 d += __shfl_xor_sync(0xFFFFFFFFu, d, 1);
                 d += __shfl_xor_sync(0xFFFFFFFFu, d, 2);
-                sd[hf] = !valid(r + 8 * hf) ? -INFINITY : SCORED ? scored(d, f.t0 + r + 8 * hf, slope2[0]) : d * a.scale_log2;
+                sd[hf] = (r + 8 * hf < nv) ? d * a.scale_log2 : -INFINITY;
             }
             float pm = fmaxf(sd[0], sd[1]);
 #pragma unroll
@@ -424,7 +329,7 @@ decode_attn_kernel(const AttnArgs a) {
             uint4 vr[2][4];
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-                const uint32_t m = __shfl_sync(0xFFFFFFFFu, mask, r + 8 * hf);
+                const uint32_t m = __shfl_sync(0xFFFFFFFFu, f.mask, r + 8 * hf);
                 const uint32_t base = __shfl_sync(0xFFFFFFFFu, pre, r + 8 * hf) * OPG;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -491,7 +396,7 @@ decode_attn_kernel(const AttnArgs a) {
                         o[16 * dt + r + 8] = acc[dt][2 + e] * inv;
                     }
                     if (a.lse && r == 0)
-                        a.lse[row_base + h] = l_run[e] > 0.f ? (m_run[e] + log2f(l_run[e])) * ln2 + lse_shift(problem, h) : -INFINITY;
+                        a.lse[row_base + h] = l_run[e] > 0.f ? (m_run[e] + log2f(l_run[e])) * ln2 : -INFINITY;
                 } else {
                     float* o = a.part_acc + (slot + h) * kHeadDim;
 #pragma unroll
@@ -517,7 +422,7 @@ decode_attn_kernel(const AttnArgs a) {
                 }
                 if (c == 0) {
                     if (whole) {
-                        if (a.lse) a.lse[row_base] = l_run[0] > 0.f ? (m_run[0] + log2f(l_run[0])) * ln2 + lse_shift(problem, 0) : -INFINITY;
+                        if (a.lse) a.lse[row_base] = l_run[0] > 0.f ? (m_run[0] + log2f(l_run[0])) * ln2 : -INFINITY;
                     } else {
                         a.part_ml[slot * 2] = m_run[0];
                         a.part_ml[slot * 2 + 1] = l_run[0];
@@ -591,7 +496,7 @@ decode_attn_kernel(const AttnArgs a) {
                 const float inv = L[i] > 0.f ? 1.f / L[i] : 0.f;
                 reinterpret_cast<float4*>(a.out + (row_base + h) * kHeadDim)[lane] =
                     make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv);
-                if (a.lse && lane == 0) a.lse[row_base + h] = L[i] > 0.f ? (M[i] + log2f(L[i])) * ln2 + lse_shift(problem, h) : -INFINITY;
+                if (a.lse && lane == 0) a.lse[row_base + h] = L[i] > 0.f ? (M[i] + log2f(L[i])) * ln2 : -INFINITY;
             }
         }
     };
@@ -692,7 +597,7 @@ cudaError_t launch_decode_attn(const Geom& g, const void* k, const void* v_packe
                                const uint16_t* v_mask, const uint32_t* v_offs, int64_t cap_groups,
                                const void* q, const int32_t* page_ids, const int32_t* n_pages,
                                int max_pages, float sm_scale, float* out, float* lse, void* ws,
-                               cudaStream_t st, unsigned flags, const ScoreArgs* score) {
+                               cudaStream_t st, unsigned flags) {
     if (g.problems == 0) return cudaSuccess;
     const int rows = g.B * g.Hq;
     char* wsp = static_cast<char*>(ws);
@@ -728,9 +633,6 @@ cudaError_t launch_decode_attn(const Geom& g, const void* k, const void* v_packe
     a.Hq = g.Hq; a.Hkv = g.Hkv; a.Gq = g.Gq; a.T = g.T;
     a.max_pages = max_pages;
     a.scale_log2 = sm_scale * 1.4426950408889634f;
-    a.sc = score ? *score : ScoreArgs{};
-    a.cap_in = a.sc.softcap > 0.f ? sm_scale / a.sc.softcap : 0.f;
-    a.cap_log2 = a.sc.softcap * 1.4426950408889634f;
     // status word + page counters start at zero
     cudaError_t e = cudaSuccess;
     if (!(flags & kLaunchNoClear)) e = clear_decode_attn_ws(g, ws, st);
@@ -740,16 +642,11 @@ cudaError_t launch_decode_attn(const Geom& g, const void* k, const void* v_packe
     e = device_sm_count(&sms);
     if (e != cudaSuccess) return e;
     const bool mma = g.Gq > 1, deep = n_cta <= sms;      // a call that fits one CTA per SM takes the deeper ring
-#define STC_ATTN_LAUNCH2(S_, MMA_, ST_, SC_)                                                            \
-    do {                                                                                                \
-        cudaFuncSetAttribute(decode_attn_kernel<S_, MMA_, ST_, SC_>,                                    \
-                             cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(ST_));        \
-        decode_attn_kernel<S_, MMA_, ST_, SC_><<<n_cta, kThreads, smem_bytes(ST_), st>>>(a);            \
-    } while (0)
 #define STC_ATTN_LAUNCH(S_, MMA_, ST_)                                                                  \
     do {                                                                                                \
-        if (score) STC_ATTN_LAUNCH2(S_, MMA_, ST_, true);                                               \
-        else STC_ATTN_LAUNCH2(S_, MMA_, ST_, false);                                                    \
+        cudaFuncSetAttribute(decode_attn_kernel<S_, MMA_, ST_>, cudaFuncAttributeMaxDynamicSharedMemorySize, \
+                             (int)smem_bytes(ST_));                                                     \
+        decode_attn_kernel<S_, MMA_, ST_><<<n_cta, kThreads, smem_bytes(ST_), st>>>(a);                 \
     } while (0)
 #define STC_ATTN(S_)                                                                                    \
     case S_:                                                                                            \
@@ -764,7 +661,6 @@ cudaError_t launch_decode_attn(const Geom& g, const void* k, const void* v_packe
         default: return cudaErrorInvalidValue;
     }
 #undef STC_ATTN_LAUNCH
-#undef STC_ATTN_LAUNCH2
 #undef STC_ATTN
     return cudaGetLastError();
 }

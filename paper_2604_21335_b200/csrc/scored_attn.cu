@@ -1,0 +1,554 @@
+// Scored decode attention: the routed decode attention with capped scores, a bias linear in the distance, a sliding
+// window and a document mask (stc_score).  Per query head h of sequence b with position p, over the valid tokens t
+// of the listed pages that the query sees (t <= p, p - t < window, document of t shared or the query's):
+//     x_t = sm_scale q_h.k_t,   x_t <- cap tanh(x_t / cap),   s_t = x_t + slope_h (t - p),
+//     out = softmax(s) V~ (dropped value groups add zero),   lse = log sum exp s.
+//
+// What bounds it.  HBM for large calls (256 bytes of key and the kept groups per token); the chain of dependent steps
+// for small ones: a decode step of one sequence moves a few MB, half a microsecond's worth, and what counts is how few
+// round trips stand between the launch and the result.
+//
+// Work split.  One cluster of C CTAs (4 warps each) per (sequence, KV head); warp i of the cluster takes the listed
+// pages i, i + 4 C, ...  C is chosen so that the clusters fill the machine (plan below).  Each warp keeps its own
+// running maximum, sum and accumulator; the four of a CTA are joined in shared memory and the CTAs of a cluster through
+// each other's shared memory (distributed shared memory), each CTA finishing its share of the outputs: one launch,
+// nothing in global memory, no atomics, and the same order of additions every time.
+//
+// Which pages a warp needs at all is settled before any copy: 32 listed pages at a time, one per lane, the lane
+// works out which of the page's 16 tokens the query sees (window and documents included) and drops the page from the
+// work if none; what is left streams through a ring of bulk asynchronous copies (a page's keys and its packed values)
+// on the warp's own mbarriers.  Values of tokens that are not seen are never used, whatever they hold.
+//
+// Arithmetic as in the plain decode attention: several query heads per KV head on mma.sync tiles (16 tokens x 8 heads,
+// softmax weights as a bf16 pair), a single head on the fp32 pipes.  The options are a handful of fp32 operations
+// on at most four scores per lane and page.  The bias is taken against the last visible token instead of the query, which
+// cancels in the softmax and keeps it small for the tokens that count even if the query stands far behind them;
+// lse gets the difference back.
+//
+// Waits for copies are bounded (about a second); one that expires raises STC_ERR_TIMEOUT in the workspace status word
+// and the warp goes on without the rest of its pages (outputs are then unspecified).
+#include "warp_mma.cuh"
+
+namespace stc {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
+constexpr int kMaxGq = 8;
+constexpr int kMaxCluster = 8;
+constexpr uint32_t kKeyBytes = kPage * kRowBytes;          // 4096
+constexpr uint32_t kStageBytes = 2 * kKeyBytes;            // keys + worst-case value span
+constexpr int kHeadStride = kHeadDim + 4;                  // floats from head to head of an exchanged accumulator (banks)
+constexpr unsigned long long kWaitLimitNs = 1000000000ull;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+__host__ __device__ constexpr uint32_t ring_bytes(int stages) { return kWarps * stages * kStageBytes; }
+__host__ __device__ constexpr uint32_t smem_bytes(int stages) { return ring_bytes(stages) + 64 + kWarps * stages * 8; }   // + zero row, mbarriers
+// the exchange buffers reuse the ring: [warps][Gq][kHeadStride] accumulators, then [Gq][kHeadStride] of the CTA
+static_assert((kWarps + 1) * kMaxGq * kHeadStride * 4 <= ring_bytes(2), "exchange buffers fit the ring");
+
+struct ScoredArgs {
+    const unsigned char* k;
+    const unsigned char* v_packed;
+    const uint16_t* v_mask;
+    const uint32_t* v_offs;
+    const uint4* q;
+    const int32_t* page_ids;
+    const int32_t* n_pages;
+    const int32_t* seq_len;
+    float* out;
+    float* lse;
+    int32_t* status;
+    int64_t cap_groups;
+    int Hq, Hkv, Gq, T, max_pages, cluster;
+    float scale_log2, cap_in, cap_log2;    // sm_scale log2(e); sm_scale / cap; cap log2(e)
+    ScoreArgs sc;
+};
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+// fp32 at `addr` of this CTA's shared memory, but of CTA `rank` of the cluster.
+__device__ __forceinline__ float ld_cluster(uint32_t addr, int rank) {
+    float v;
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}"
+                 : "=f"(v) : "r"(addr), "r"(rank) : "memory");
+    return v;
+}
+
+template <int S, bool MMA, int kStages, int kPerSm>
+__global__ void __launch_bounds__(kThreads, kPerSm)
+scored_attn_kernel(const ScoredArgs a) {
+    constexpr uint32_t kRingBytes = ring_bytes(kStages);
+    constexpr int OPG = kOctets / S;             // 16-byte chunks per value group
+    constexpr uint32_t kGroupBytes = OPG * 16;
+    constexpr int HEADS = MMA ? kMaxGq : 1;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ float2 sh_ml[kWarps][kMaxGq];     // maximum (log2 units) and sum per warp and head
+    __shared__ float sh_m[kMaxGq], sh_l[kMaxGq]; // of the CTA
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int r = lane >> 2, c = lane & 3;
+    const int rank = (int)(blockIdx.x % (unsigned)a.cluster), problem = (int)(blockIdx.x / (unsigned)a.cluster);
+    const int b = problem / a.Hkv, hk = problem - b * a.Hkv;
+    const uint32_t ring = smem_u32(smem) + (uint32_t)warp * kStages * kStageBytes;
+    const uint32_t zero_row = smem_u32(smem) + kRingBytes;
+    const uint32_t bars = smem_u32(smem) + kRingBytes + 64 + (uint32_t)warp * kStages * 8;
+
+    // the query and what it sees
+    const int len = clamp_len(a.seq_len, b, a.T), pos = a.sc.q_pos ? a.sc.q_pos[b] : len - 1;
+    const int my_doc = a.sc.tok_doc ? a.sc.q_doc[b] : 0;
+    const int n_list = a.page_ids ? min(max(a.n_pages[problem], 0), a.max_pages) : (len + kPage - 1) / kPage;
+    uint4 qa[4];                                 // lane (r, c): chunks c, c + 4, c + 8, c + 12 of head r (zeros past Gq; FMA: head 0)
+    float slope2[2] = {0.f, 0.f};                // log2 units; heads 2 c, 2 c + 1 (FMA: head 0)
+    {
+        const int head = MMA ? r : 0;
+        const bool ok = head < a.Gq;
+        const uint4* qrow = a.q + ((size_t)b * a.Hq + (size_t)hk * a.Gq + (ok ? head : 0)) * kOctets;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) qa[j] = ok ? __ldg(qrow + c + 4 * j) : make_uint4(0, 0, 0, 0);
+        if (a.sc.slopes) {
+#pragma unroll
+            for (int e = 0; e < (MMA ? 2 : 1); ++e) {
+                const int h = MMA ? 2 * c + e : 0;
+                slope2[e] = h < a.Gq ? a.sc.slopes[hk * a.Gq + h] * kLog2e : 0.f;
+            }
+        }
+    }
+    if (tid < 4) reinterpret_cast<uint32_t*>(smem + kRingBytes)[tid] = 0u;
+    if (lane == 0) {
+#pragma unroll
+        for (int s = 0; s < kStages; ++s) mbar_init(bars + 8 * s, 1);
+        fence_mbar_init();
+    }
+    if (blockIdx.x == 0 && tid == 0) *a.status = STC_OK;
+    int see_lo, see_hi;
+    visible_range(len, pos, a.sc.window, see_lo, see_hi);
+    __syncthreads();
+
+    // ---- lookahead window: lane i describes the i-th of the warp's next 32 listed pages -----------------------
+    const int W = a.cluster * kWarps, first_slot = rank * kWarps + warp;
+    int page = -1;                               // page id of this lane's entry
+    uint32_t seen = 0, first = 0, groups = 0;    // bit t = token t of the page is seen; its span of the packed store
+    uint32_t todo = 0;                           // entries with something to attend, not issued yet (same in all lanes)
+    long long next_slot = first_slot;
+    auto fill = [&]() {
+        const long long slot = next_slot + (long long)W * lane;
+        page = -1;
+        if (slot < n_list) page = a.page_ids ? a.page_ids[(size_t)problem * a.max_pages + slot] : (int)slot;
+        seen = 0;
+        // (an id outside the sequence is skipped; see_hi <= len)
+        if (page >= 0 && page < (len + kPage - 1) / kPage) {
+            const int t0 = page * kPage, lo = max(see_lo - t0, 0), hi = min(see_hi - t0, kPage);
+            if (lo < hi) seen = (0xFFFFu >> (kPage - hi)) & ~((1u << lo) - 1u);
+            if (seen) {
+                const int nv = min(kPage, len - t0);
+                const uint32_t* o = a.v_offs + (size_t)problem * (a.T + 1) + t0;
+                const long long ob = min((long long)o[0], (long long)a.cap_groups);
+                const long long oe = min((long long)o[nv], (long long)a.cap_groups);
+                first = (uint32_t)ob;
+                groups = (uint32_t)min(oe > ob ? oe - ob : 0LL, (long long)(kPage * S));       // never past the stage
+                if (a.sc.tok_doc) {
+                    const int32_t* doc = a.sc.tok_doc + (size_t)b * a.T + t0;
+                    uint32_t keep = 0;
+#pragma unroll
+                    for (int t = 0; t < kPage; ++t) {
+                        const int d = t < nv ? __ldg(doc + t) : 0;
+                        if (d < 0 || d == my_doc) keep |= 1u << t;
+                    }
+                    seen &= keep;
+                }
+            }
+        }
+        todo = __ballot_sync(0xFFFFFFFFu, seen != 0);
+        next_slot += 32 * W;
+    };
+
+    // ---- the pages in flight: a register FIFO, oldest first -----------------------------------------------------
+    struct InFlight {
+        uint32_t seen;       // 0 = empty
+        uint32_t chunks;     // 16-byte chunks of the value span present in the stage
+        uint32_t mask;       // lanes 0..15: group mask of token `lane`
+        int t0;
+    };
+    auto issue = [&](int s, bool reuse) -> InFlight {
+        InFlight f{0u, 0u, 0u, 0};
+        while (todo == 0) {
+            if (next_slot >= n_list) return f;
+            fill();
+        }
+        const int src = __ffs(todo) - 1;
+        todo &= todo - 1;
+        const int id = __shfl_sync(0xFFFFFFFFu, page, src);
+        f.seen = __shfl_sync(0xFFFFFFFFu, seen, src);
+        const uint32_t at = __shfl_sync(0xFFFFFFFFu, first, src), n = __shfl_sync(0xFFFFFFFFu, groups, src);
+        f.t0 = id * kPage;
+        f.chunks = n * OPG;
+        const int nv = min(kPage, len - f.t0);
+        const size_t row0 = (size_t)problem * a.T + (size_t)f.t0;
+        if (lane < nv) f.mask = a.v_mask[row0 + lane];
+        if (lane == 0) {
+            const uint32_t kb = (uint32_t)nv * kRowBytes, vb = n * kGroupBytes;
+            const uint32_t bar = bars + 8 * s, dst = ring + (uint32_t)s * kStageBytes;
+            if (reuse) fence_proxy_async();      // the stage's earlier reads precede the new writes
+            mbar_expect_tx(bar, kb + vb);
+            bulk_g2s(dst, a.k + row0 * kRowBytes, kb, bar);
+            if (vb) bulk_g2s(dst + kKeyBytes, a.v_packed + ((size_t)problem * a.cap_groups + at) * kGroupBytes, vb, bar);
+        }
+        return f;
+    };
+
+    // ---- running state ----------------------------------------------------------------------------------------------
+    // MMA: acc[dt][0..3] = (dim 16dt+r, head 2c), (16dt+r, 2c+1), (16dt+r+8, 2c), (16dt+r+8, 2c+1);
+    //      m_run/l_run[e] belong to head 2c+e (l_run summed over the lane's own tokens only).
+    // FMA: acc[j][2q2+e] -> dim 8(c+4j)+2q2+e, summed over the lane's own two tokens; m_run[0], l_run[0].
+    float acc[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+    float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+
+    // N raw products of tokens t[i] -> scores in log2 units (one branch per page, not per score)
+    auto score = [&](auto& x, const int* t, const int* e, int n) {
+        if (a.sc.softcap > 0.f) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < n) x[i] = a.cap_log2 * tanh_f32(x[i] * a.cap_in);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < n) x[i] *= a.scale_log2;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) x[i] = fmaf(slope2[e[i]], (float)(t[i] - (see_hi - 1)), x[i]);
+    };
+
+    auto compute = [&](int s, const InFlight& f) {
+        const uint32_t kst = ring + (uint32_t)s * kStageBytes, vst = kst + kKeyBytes;
+        // exclusive prefix (in groups) of the page's token masks, lanes 0..15
+        const uint32_t cnt = __popc(f.mask);
+        uint32_t pre = cnt;
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) {
+            const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, pre, d);
+            if (lane >= d) pre += o;
+        }
+        pre -= cnt;
+        const uint32_t mask = (f.seen >> (lane & 15)) & 1u ? f.mask : 0u;     // groups that may be read
+        const bool v0 = (f.seen >> r) & 1u, v1 = (f.seen >> (r + 8)) & 1u;
+
+        if constexpr (MMA) {
+            // S^T = K . Q^T : rows = tokens (r, r+8), columns = heads (2c, 2c+1)
+            float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint4 k0 = lds16(kst + (uint32_t)r * kRowBytes + (uint32_t)(c + 4 * j) * 16u);
+                const uint4 k1 = lds16(kst + (uint32_t)(r + 8) * kRowBytes + (uint32_t)(c + 4 * j) * 16u);
+                mma_bf16(s0, k0.x, k1.x, k0.y, k1.y, qa[j].x, qa[j].y);
+                mma_bf16(s1, k0.z, k1.z, k0.w, k1.w, qa[j].z, qa[j].w);
+            }
+            float sv[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sv[i] = s0[i] + s1[i];
+            const int t[4] = {f.t0 + r, f.t0 + r, f.t0 + r + 8, f.t0 + r + 8}, e[4] = {0, 1, 0, 1};
+            score(sv, t, e, 4);
+            sv[0] = v0 ? sv[0] : -INFINITY; sv[1] = v0 ? sv[1] : -INFINITY;
+            sv[2] = v1 ? sv[2] : -INFINITY; sv[3] = v1 ? sv[3] : -INFINITY;
+            float pm0 = fmaxf(sv[0], sv[2]), pm1 = fmaxf(sv[1], sv[3]);
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) {
+                pm0 = fmaxf(pm0, __shfl_xor_sync(0xFFFFFFFFu, pm0, d));
+                pm1 = fmaxf(pm1, __shfl_xor_sync(0xFFFFFFFFu, pm1, d));
+            }
+            const float mn0 = fmaxf(m_run[0], pm0), mn1 = fmaxf(m_run[1], pm1);   // finite: a token is seen
+            const float al0 = exp2f(m_run[0] - mn0), al1 = exp2f(m_run[1] - mn1);
+            const float p0 = exp2f(sv[0] - mn0), p1 = exp2f(sv[1] - mn1);
+            const float p2 = exp2f(sv[2] - mn0), p3 = exp2f(sv[3] - mn1);
+            l_run[0] = fmaf(l_run[0], al0, p0 + p2);
+            l_run[1] = fmaf(l_run[1], al1, p1 + p3);
+            m_run[0] = mn0; m_run[1] = mn1;
+            // P^T as B fragments: high bf16 part and bf16 residual
+            const uint32_t wh0 = pack_bf16(p0, p1), wh1 = pack_bf16(p2, p3);
+            const uint32_t wl0 = pack_bf16(p0 - bf16lo(wh0), p1 - bf16hi(wh0));
+            const uint32_t wl1 = pack_bf16(p2 - bf16lo(wh1), p3 - bf16hi(wh1));
+            const uint32_t bh0 = movmatrix_trans(wh0), bh1 = movmatrix_trans(wh1);
+            const uint32_t bl0 = movmatrix_trans(wl0), bl1 = movmatrix_trans(wl1);
+            // value rows: this lane addresses token tau, chunk 2dt + hb of every dim tile
+            const int tau = (lane & 7) + 8 * (lane >> 4), hb = (lane >> 3) & 1;
+            const uint32_t m = __shfl_sync(0xFFFFFFFFu, mask, tau);
+            const uint32_t base = __shfl_sync(0xFFFFFFFFu, pre, tau) * OPG;
+            // the low half of a masked token's own groups does not matter: its prefix counts all of them
+            const uint32_t all = __shfl_sync(0xFFFFFFFFu, f.mask, tau);
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) {
+                const int oct = 2 * dt + hb, grp = oct / OPG;
+                const uint32_t idx = base + __popc(all & ((1u << grp) - 1u)) * OPG + (uint32_t)(oct % OPG);
+                const bool kept = ((m >> grp) & 1u) && idx < f.chunks;
+                uint32_t a0, a1, a2, a3;
+                ldmatrix_x4_trans(kept ? vst + idx * 16u : zero_row, a0, a1, a2, a3);
+                acc[dt][0] *= al0; acc[dt][1] *= al1; acc[dt][2] *= al0; acc[dt][3] *= al1;
+                mma_bf16(acc[dt], a0, a1, a2, a3, bh0, bh1);
+                mma_bf16(acc[dt], a0, a1, a2, a3, bl0, bl1);
+            }
+        } else {
+            // one head on the fp32 pipes: lane = tokens r, r+8 x chunks c, c+4, c+8, c+12
+            float sd[4];
+            uint4 kr[2][4];
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    kr[hf][j] = lds16(kst + (uint32_t)(r + 8 * hf) * kRowBytes + (uint32_t)(c + 4 * j) * 16u);
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                float d0 = 0.f, d1 = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    d0 = fmaf(bf16lo(qa[j].x), bf16lo(kr[hf][j].x), d0);
+                    d1 = fmaf(bf16hi(qa[j].x), bf16hi(kr[hf][j].x), d1);
+                    d0 = fmaf(bf16lo(qa[j].y), bf16lo(kr[hf][j].y), d0);
+                    d1 = fmaf(bf16hi(qa[j].y), bf16hi(kr[hf][j].y), d1);
+                    d0 = fmaf(bf16lo(qa[j].z), bf16lo(kr[hf][j].z), d0);
+                    d1 = fmaf(bf16hi(qa[j].z), bf16hi(kr[hf][j].z), d1);
+                    d0 = fmaf(bf16lo(qa[j].w), bf16lo(kr[hf][j].w), d0);
+                    d1 = fmaf(bf16hi(qa[j].w), bf16hi(kr[hf][j].w), d1);
+                }
+                float d = d0 + d1;
+                d += __shfl_xor_sync(0xFFFFFFFFu, d, 1);
+                d += __shfl_xor_sync(0xFFFFFFFFu, d, 2);
+                sd[hf] = d;
+            }
+            const int t[4] = {f.t0 + r, f.t0 + r + 8, 0, 0}, e[4] = {0, 0, 0, 0};
+            score(sd, t, e, 2);
+            sd[0] = v0 ? sd[0] : -INFINITY;
+            sd[1] = v1 ? sd[1] : -INFINITY;
+            float pm = fmaxf(sd[0], sd[1]);
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) pm = fmaxf(pm, __shfl_xor_sync(0xFFFFFFFFu, pm, d));
+            const float mn = fmaxf(m_run[0], pm);
+            const float al = exp2f(m_run[0] - mn);
+            const float p0 = exp2f(sd[0] - mn), p1 = exp2f(sd[1] - mn);
+            l_run[0] = fmaf(l_run[0], al, p0 + p1);
+            m_run[0] = mn;
+            uint4 vr[2][4];
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                const uint32_t m = __shfl_sync(0xFFFFFFFFu, mask, r + 8 * hf);
+                const uint32_t base = __shfl_sync(0xFFFFFFFFu, pre, r + 8 * hf) * OPG;
+                const uint32_t all = __shfl_sync(0xFFFFFFFFu, f.mask, r + 8 * hf);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int oct = c + 4 * j, grp = oct / OPG;
+                    const uint32_t idx = base + __popc(all & ((1u << grp) - 1u)) * OPG + (uint32_t)(oct % OPG);
+                    const bool kept = ((m >> grp) & 1u) && idx < f.chunks;
+                    vr[hf][j] = kept ? lds16(vst + idx * 16u) : make_uint4(0, 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t u0[4] = {vr[0][j].x, vr[0][j].y, vr[0][j].z, vr[0][j].w};
+                const uint32_t u1[4] = {vr[1][j].x, vr[1][j].y, vr[1][j].z, vr[1][j].w};
+#pragma unroll
+                for (int q2 = 0; q2 < 4; ++q2) {
+                    float& lo = acc[2 * j + (q2 >> 1)][2 * (q2 & 1)];
+                    float& hi = acc[2 * j + (q2 >> 1)][2 * (q2 & 1) + 1];
+                    lo = fmaf(p1, bf16lo(u1[q2]), fmaf(p0, bf16lo(u0[q2]), lo * al));
+                    hi = fmaf(p1, bf16hi(u1[q2]), fmaf(p0, bf16hi(u0[q2]), hi * al));
+                }
+            }
+        }
+    };
+
+    // ---- main loop ----------------------------------------------------------------------------------------------
+    {
+        InFlight f[kStages];                     // f[0] = oldest page in flight, in stage s
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) f[i] = issue(i, false);
+        uint32_t phase = 0;                      // bit s = parity to wait for on stage s
+        int s = 0;
+#pragma unroll 1
+        while (f[0].seen) {
+            const uint32_t par = (phase >> s) & 1u;
+            phase ^= 1u << s;
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(bars + 8 * s, par, kWaitLimitNs))) {
+                // A copy did not land in time.  Report it and give the copies still in flight one more bounded wait each, so
+                // that they do not land in the exchange buffers or a dead CTA's memory.
+                if (lane == 0) atomicExch(a.status, (int)STC_ERR_TIMEOUT);
+                int s2 = s;
+#pragma unroll
+                for (int i = 1; i < kStages; ++i) {
+                    s2 = s2 + 1 == kStages ? 0 : s2 + 1;
+                    if (f[i].seen) mbar_wait_bounded(bars + 8 * s2, (phase >> s2) & 1u, kWaitLimitNs);
+                }
+                break;
+            }
+            compute(s, f[0]);
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i + 1 < kStages; ++i) f[i] = f[i + 1];
+            f[kStages - 1] = issue(s, true);
+            s = s + 1 == kStages ? 0 : s + 1;
+        }
+    }
+
+    // ---- join: the warps of the CTA, then the CTAs of the cluster --------------------------------------------------
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1) {
+        l_run[0] += __shfl_xor_sync(0xFFFFFFFFu, l_run[0], d);
+        if (MMA) l_run[1] += __shfl_xor_sync(0xFFFFFFFFu, l_run[1], d);
+    }
+    if constexpr (!MMA) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][e] += __shfl_xor_sync(0xFFFFFFFFu, acc[i][e], d);
+    }
+    __syncthreads();                             // every warp is through with its ring
+    float* const ex = reinterpret_cast<float*>(smem);                    // [kWarps][HEADS][kHeadStride]
+    float* const cta = ex + kWarps * HEADS * kHeadStride;                // [HEADS][kHeadStride]
+    {
+        float* mine = ex + warp * HEADS * kHeadStride;
+        if constexpr (MMA) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int h = 2 * c + e;
+                if (r == 0) sh_ml[warp][h] = make_float2(m_run[e], l_run[e]);
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) {
+                    mine[h * kHeadStride + 16 * dt + r] = acc[dt][e];
+                    mine[h * kHeadStride + 16 * dt + r + 8] = acc[dt][2 + e];
+                }
+            }
+        } else if (r == 0) {                     // lanes 0..3 hold the reduced 128 channels
+            if (c == 0) sh_ml[warp][0] = make_float2(m_run[0], l_run[0]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) mine[8 * (c + 4 * j) + e] = acc[2 * j + (e >> 2)][e & 3];
+        }
+    }
+    __syncthreads();
+    const int share = a.cluster;
+    const size_t row_base = (size_t)b * a.Hq + (size_t)hk * a.Gq;
+    // what lse lacks: slope * (last visible token - position of the query)
+    auto lse_of = [&](int h, float m, float l) {
+        const float shift = a.sc.slopes ? a.sc.slopes[hk * a.Gq + h] * (float)(see_hi - 1 - pos) : 0.f;
+        return l > 0.f ? (m + log2f(l)) * kLn2 + shift : -INFINITY;
+    };
+#pragma unroll 1
+    for (int h = 0; h < a.Gq; ++h) {             // thread = channel
+        float2 p[kWarps];
+        float m = -INFINITY, l = 0.f, o = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) { p[w] = sh_ml[w][h]; m = fmaxf(m, p[w].x); }
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float f = p[w].x == -INFINITY ? 0.f : exp2f(p[w].x - m);
+            l = fmaf(p[w].y, f, l);
+            o = fmaf(ex[(w * HEADS + h) * kHeadStride + tid], f, o);
+        }
+        if (share == 1) {
+            a.out[(row_base + h) * kHeadDim + tid] = l > 0.f ? o / l : 0.f;
+            if (a.lse && tid == 0) a.lse[row_base + h] = lse_of(h, m, l);
+        } else {
+            cta[h * kHeadStride + tid] = o;
+            if (tid == 0) { sh_m[h] = m; sh_l[h] = l; }
+        }
+    }
+    if (share == 1) return;
+    cluster_sync();
+    const uint32_t at_m = smem_u32(sh_m), at_l = smem_u32(sh_l), at_o = smem_u32(cta);
+#pragma unroll 1
+    for (int i = rank * kThreads + tid; i < a.Gq * kHeadDim; i += share * kThreads) {
+        const int h = i >> 7, d = i & (kHeadDim - 1);
+        float pm[kMaxCluster], pl[kMaxCluster], po[kMaxCluster], m = -INFINITY, l = 0.f, o = 0.f;
+#pragma unroll
+        for (int k = 0; k < kMaxCluster; ++k) {
+            if (k >= share) { pm[k] = -INFINITY; continue; }
+            pm[k] = ld_cluster(at_m + 4u * h, k);
+            pl[k] = ld_cluster(at_l + 4u * h, k);
+            po[k] = ld_cluster(at_o + 4u * (uint32_t)(h * kHeadStride + d), k);
+            m = fmaxf(m, pm[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kMaxCluster; ++k) {
+            if (pm[k] == -INFINITY) continue;
+            const float f = exp2f(pm[k] - m);
+            l = fmaf(pl[k], f, l);
+            o = fmaf(po[k], f, o);
+        }
+        a.out[(row_base + h) * kHeadDim + d] = l > 0.f ? o / l : 0.f;
+        if (a.lse && d == 0) a.lse[row_base + h] = lse_of(h, m, l);
+    }
+    cluster_sync();                              // no CTA leaves while another still reads its shared memory
+}
+
+// CTAs per problem.  A call takes waves x (pages of a warp + 3) page times: CTAs resident at once, and about
+// three page times to start, to fill the ring and to join.
+int cluster_size(int problems, int max_pages, int resident) {
+    int best = 1;
+    double least = 0.0;
+    for (int c = 1; c <= kMaxCluster; ++c) {
+        const double waves = (double)(((long long)problems * c + resident - 1) / resident);
+        const double cost = waves * ((max_pages + kWarps * c - 1) / (kWarps * c) + 3.0);
+        if (c == 1 || cost < least) { least = cost; best = c; }
+    }
+    return best;
+}
+
+template <int S, bool MMA, int kStages, int kPerSm>
+cudaError_t launch(const ScoredArgs& a, int problems, cudaStream_t st) {
+    auto kernel = scored_attn_kernel<S, MMA, kStages, kPerSm>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(kStages));
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(problems * a.cluster));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem_bytes(kStages);
+    cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = (unsigned)a.cluster;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+}  // namespace
+
+cudaError_t launch_scored_attn(const Geom& g, const void* k, const void* v_packed, const uint16_t* v_mask,
+                               const uint32_t* v_offs, int64_t cap_groups, const void* q, const int32_t* page_ids,
+                               const int32_t* n_pages, int max_pages, float sm_scale, const ScoreArgs& score, float* out,
+                               float* lse, void* ws, cudaStream_t st) {
+    if (g.problems == 0) return cudaSuccess;
+    ScoredArgs a;
+    a.k = static_cast<const unsigned char*>(k);
+    a.v_packed = static_cast<const unsigned char*>(v_packed);
+    a.v_mask = v_mask; a.v_offs = v_offs;
+    a.q = static_cast<const uint4*>(q);
+    a.page_ids = page_ids; a.n_pages = n_pages; a.seq_len = g.seq_len;
+    a.out = out; a.lse = lse;
+    a.status = static_cast<int32_t*>(ws);
+    a.cap_groups = cap_groups;
+    a.Hq = g.Hq; a.Hkv = g.Hkv; a.Gq = g.Gq; a.T = g.T; a.max_pages = max_pages;
+    a.sc = score;
+    a.scale_log2 = sm_scale * kLog2e;
+    a.cap_in = score.softcap > 0.f ? sm_scale / score.softcap : 0.f;
+    a.cap_log2 = score.softcap * kLog2e;
+    int sms = 0;
+    cudaError_t e = device_sm_count(&sms);
+    if (e != cudaSuccess) return e;
+    // two CTAs per SM with three stages, three with two for the single-head path, whose arithmetic per page outlasts a copy
+    a.cluster = cluster_size(g.problems, max_pages, sms * (g.Gq > 1 ? 2 : 3));
+#define STC_SCORED(S_) \
+    case S_: return g.Gq > 1 ? launch<S_, true, 3, 2>(a, g.problems, st) : launch<S_, false, 2, 3>(a, g.problems, st);
+    switch (g.S) {
+        STC_SCORED(4) STC_SCORED(8) STC_SCORED(16)
+        default: return cudaErrorInvalidValue;
+    }
+#undef STC_SCORED
+}
+
+}  // namespace stc

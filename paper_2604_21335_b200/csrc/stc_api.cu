@@ -369,9 +369,11 @@ int32_t decode_attn(const stc_shape* shape, const stc_cache* cache, const void* 
     if (!aligned16(cache->k, cache->v_packed, q, out)) return STC_ERR_INVALID_ARG;
     rc = check_ws(ws, ws_bytes, attn_ws_bytes(g, max_pages));
     if (rc != STC_OK) return rc;
-    return cuda_rc(launch_decode_attn(g, cache->k, cache->v_packed, cache->v_mask, cache->v_offs,
-                                      cache->cap_groups, q, page_ids, n_pages, max_pages, sm_scale,
-                                      out, lse_opt, ws, static_cast<cudaStream_t>(stream), 0, plain ? nullptr : &sc));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return cuda_rc(plain ? launch_decode_attn(g, cache->k, cache->v_packed, cache->v_mask, cache->v_offs, cache->cap_groups,
+                                              q, page_ids, n_pages, max_pages, sm_scale, out, lse_opt, ws, st)
+                         : launch_scored_attn(g, cache->k, cache->v_packed, cache->v_mask, cache->v_offs, cache->cap_groups,
+                                              q, page_ids, n_pages, max_pages, sm_scale, sc, out, lse_opt, ws, st));
 }
 }  // namespace
 
