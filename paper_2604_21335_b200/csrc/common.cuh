@@ -137,6 +137,13 @@ __device__ __forceinline__ uint32_t bmax2(uint32_t a, uint32_t b) {
     return *reinterpret_cast<uint32_t*>(&r);
 }
 
+// 2^x to 2 units of fp32; results below the normal range become zero.
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // tanh to about one fp32 ulp.  |z| <= 0.55: odd polynomial z + z^3 P(z^2), P fitted by weighted least
 // squares at Chebyshev nodes (relative error 6.7e-8 against extended precision); above: 1 - 2 / (e^{2z} + 1), whose
 // absolute error of about 1.5e-7 is small against tanh >= 0.5.  The hardware tanh (error 2^-11) would

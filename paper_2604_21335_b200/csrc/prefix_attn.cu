@@ -106,13 +106,6 @@ struct PrefixArgs {
     ScoreArgs sc;
 };
 
-// 2^x to 2 units of fp32; results below the normal range become zero.
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 struct Group {
     int row0, n_seq, len, tiles, blocks;
 };

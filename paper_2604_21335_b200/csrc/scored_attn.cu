@@ -25,6 +25,9 @@
 // cancels in the softmax and keeps it small for the tokens that count even if the query stands far behind them;
 // lse gets the difference back.
 //
+// The running maximum only moves when a page exceeds it by more than 2^8 (a vote instead of a reduction, and no
+// rescaling of the accumulator, on most pages); weights are then at most 2^8, far from fp32's limits.
+//
 // Waits for copies are bounded (about a second); one that expires raises STC_ERR_TIMEOUT in the workspace status word
 // and the warp goes on without the rest of its pages (outputs are then unspecified).
 #include "warp_mma.cuh"
@@ -40,6 +43,7 @@ constexpr uint32_t kKeyBytes = kPage * kRowBytes;          // 4096
 constexpr uint32_t kStageBytes = 2 * kKeyBytes;            // keys + worst-case value span
 constexpr int kHeadStride = kHeadDim + 4;                  // floats from head to head of an exchanged accumulator (banks)
 constexpr unsigned long long kWaitLimitNs = 1000000000ull;
+constexpr float kSlack = 8.f;                              // log2 units the maximum may be exceeded by
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __host__ __device__ constexpr uint32_t ring_bytes(int stages) { return kWarps * stages * kStageBytes; }
 __host__ __device__ constexpr uint32_t smem_bytes(int stages) { return ring_bytes(stages) + 64 + kWarps * stages * 8; }   // + zero row, mbarriers
@@ -94,6 +98,13 @@ scored_attn_kernel(const ScoredArgs a) {
     const uint32_t zero_row = smem_u32(smem) + kRingBytes;
     const uint32_t bars = smem_u32(smem) + kRingBytes + 64 + (uint32_t)warp * kStages * 8;
 
+    // The reads the first window needs go out together: the page list does not wait for the lengths (a listed slot below
+    // max_pages is readable whatever it holds).
+    const int W = a.cluster * kWarps, first_slot = rank * kWarps + warp;
+    const int32_t* const list = a.page_ids ? a.page_ids + (size_t)problem * a.max_pages : nullptr;
+    const long long slot0 = first_slot + (long long)W * lane;
+    int listed = list && slot0 < a.max_pages ? list[slot0] : -1;             // this lane's entry of the next window
+
     // the query and what it sees
     const int len = clamp_len(a.seq_len, b, a.T), pos = a.sc.q_pos ? a.sc.q_pos[b] : len - 1;
     const int my_doc = a.sc.tok_doc ? a.sc.q_doc[b] : 0;
@@ -126,7 +137,6 @@ scored_attn_kernel(const ScoredArgs a) {
     __syncthreads();
 
     // ---- lookahead window: lane i describes the i-th of the warp's next 32 listed pages -----------------------
-    const int W = a.cluster * kWarps, first_slot = rank * kWarps + warp;
     int page = -1;                               // page id of this lane's entry
     uint32_t seen = 0, first = 0, groups = 0;    // bit t = token t of the page is seen; its span of the packed store
     uint32_t todo = 0;                           // entries with something to attend, not issued yet (same in all lanes)
@@ -134,7 +144,7 @@ scored_attn_kernel(const ScoredArgs a) {
     auto fill = [&]() {
         const long long slot = next_slot + (long long)W * lane;
         page = -1;
-        if (slot < n_list) page = a.page_ids ? a.page_ids[(size_t)problem * a.max_pages + slot] : (int)slot;
+        if (slot < n_list) page = list ? listed : (int)slot;
         seen = 0;
         // (an id outside the sequence is skipped; see_hi <= len)
         if (page >= 0 && page < (len + kPage - 1) / kPage) {
@@ -161,6 +171,8 @@ scored_attn_kernel(const ScoredArgs a) {
         }
         todo = __ballot_sync(0xFFFFFFFFu, seen != 0);
         next_slot += 32 * W;
+        const long long ahead = next_slot + (long long)W * lane;
+        listed = list && ahead < n_list ? list[ahead] : -1;
     };
 
     // ---- the pages in flight: a register FIFO, oldest first -----------------------------------------------------
@@ -168,10 +180,12 @@ scored_attn_kernel(const ScoredArgs a) {
         uint32_t seen;       // 0 = empty
         uint32_t chunks;     // 16-byte chunks of the value span present in the stage
         uint32_t mask;       // lanes 0..15: group mask of token `lane`
+        uint32_t at;         // lanes 0..15: its first group in the packed store
+        uint32_t first;      // the page's first group
         int t0;
     };
     auto issue = [&](int s, bool reuse) -> InFlight {
-        InFlight f{0u, 0u, 0u, 0};
+        InFlight f{0u, 0u, 0u, 0u, 0u, 0};
         while (todo == 0) {
             if (next_slot >= n_list) return f;
             fill();
@@ -185,7 +199,11 @@ scored_attn_kernel(const ScoredArgs a) {
         f.chunks = n * OPG;
         const int nv = min(kPage, len - f.t0);
         const size_t row0 = (size_t)problem * a.T + (size_t)f.t0;
-        if (lane < nv) f.mask = a.v_mask[row0 + lane];
+        f.first = at;
+        if (lane < nv) {
+            f.mask = a.v_mask[row0 + lane];
+            f.at = a.v_offs[(size_t)problem * (a.T + 1) + (size_t)f.t0 + lane];
+        }
         if (lane == 0) {
             const uint32_t kb = (uint32_t)nv * kRowBytes, vb = n * kGroupBytes;
             const uint32_t bar = bars + 8 * s, dst = ring + (uint32_t)s * kStageBytes;
@@ -224,15 +242,7 @@ scored_attn_kernel(const ScoredArgs a) {
 
     auto compute = [&](int s, const InFlight& f) {
         const uint32_t kst = ring + (uint32_t)s * kStageBytes, vst = kst + kKeyBytes;
-        // exclusive prefix (in groups) of the page's token masks, lanes 0..15
-        const uint32_t cnt = __popc(f.mask);
-        uint32_t pre = cnt;
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) {
-            const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, pre, d);
-            if (lane >= d) pre += o;
-        }
-        pre -= cnt;
+        const uint32_t pre = f.at - f.first;     // groups of the page before the token (lanes 0..15)
         const uint32_t mask = (f.seen >> (lane & 15)) & 1u ? f.mask : 0u;     // groups that may be read
         const bool v0 = (f.seen >> r) & 1u, v1 = (f.seen >> (r + 8)) & 1u;
 
@@ -253,19 +263,28 @@ scored_attn_kernel(const ScoredArgs a) {
             score(sv, t, e, 4);
             sv[0] = v0 ? sv[0] : -INFINITY; sv[1] = v0 ? sv[1] : -INFINITY;
             sv[2] = v1 ? sv[2] : -INFINITY; sv[3] = v1 ? sv[3] : -INFINITY;
-            float pm0 = fmaxf(sv[0], sv[2]), pm1 = fmaxf(sv[1], sv[3]);
+            float al0 = 1.f, al1 = 1.f;
+            bool moved = false;
+            if (__any_sync(0xFFFFFFFFu, fmaxf(sv[0], sv[2]) > m_run[0] + kSlack || fmaxf(sv[1], sv[3]) > m_run[1] + kSlack)) {
+                float pm0 = fmaxf(sv[0], sv[2]), pm1 = fmaxf(sv[1], sv[3]);
 #pragma unroll
-            for (int d = 4; d < 32; d <<= 1) {
-                pm0 = fmaxf(pm0, __shfl_xor_sync(0xFFFFFFFFu, pm0, d));
-                pm1 = fmaxf(pm1, __shfl_xor_sync(0xFFFFFFFFu, pm1, d));
+                for (int d = 4; d < 32; d <<= 1) {
+                    pm0 = fmaxf(pm0, __shfl_xor_sync(0xFFFFFFFFu, pm0, d));
+                    pm1 = fmaxf(pm1, __shfl_xor_sync(0xFFFFFFFFu, pm1, d));
+                }
+                const float mn0 = fmaxf(m_run[0], pm0), mn1 = fmaxf(m_run[1], pm1);   // finite: a token is seen
+                al0 = ex2(m_run[0] - mn0); al1 = ex2(m_run[1] - mn1);
+                m_run[0] = mn0; m_run[1] = mn1;
+                moved = true;
             }
-            const float mn0 = fmaxf(m_run[0], pm0), mn1 = fmaxf(m_run[1], pm1);   // finite: a token is seen
-            const float al0 = exp2f(m_run[0] - mn0), al1 = exp2f(m_run[1] - mn1);
-            const float p0 = exp2f(sv[0] - mn0), p1 = exp2f(sv[1] - mn1);
-            const float p2 = exp2f(sv[2] - mn0), p3 = exp2f(sv[3] - mn1);
+            const float p0 = ex2(sv[0] - m_run[0]), p1 = ex2(sv[1] - m_run[1]);
+            const float p2 = ex2(sv[2] - m_run[0]), p3 = ex2(sv[3] - m_run[1]);
             l_run[0] = fmaf(l_run[0], al0, p0 + p2);
             l_run[1] = fmaf(l_run[1], al1, p1 + p3);
-            m_run[0] = mn0; m_run[1] = mn1;
+            if (moved) {
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) { acc[dt][0] *= al0; acc[dt][1] *= al1; acc[dt][2] *= al0; acc[dt][3] *= al1; }
+            }
             // P^T as B fragments: high bf16 part and bf16 residual
             const uint32_t wh0 = pack_bf16(p0, p1), wh1 = pack_bf16(p2, p3);
             const uint32_t wl0 = pack_bf16(p0 - bf16lo(wh0), p1 - bf16hi(wh0));
@@ -285,7 +304,6 @@ scored_attn_kernel(const ScoredArgs a) {
                 const bool kept = ((m >> grp) & 1u) && idx < f.chunks;
                 uint32_t a0, a1, a2, a3;
                 ldmatrix_x4_trans(kept ? vst + idx * 16u : zero_row, a0, a1, a2, a3);
-                acc[dt][0] *= al0; acc[dt][1] *= al1; acc[dt][2] *= al0; acc[dt][3] *= al1;
                 mma_bf16(acc[dt], a0, a1, a2, a3, bh0, bh1);
                 mma_bf16(acc[dt], a0, a1, a2, a3, bl0, bl1);
             }
@@ -321,14 +339,17 @@ scored_attn_kernel(const ScoredArgs a) {
             score(sd, t, e, 2);
             sd[0] = v0 ? sd[0] : -INFINITY;
             sd[1] = v1 ? sd[1] : -INFINITY;
-            float pm = fmaxf(sd[0], sd[1]);
+            float al = 1.f;
+            if (__any_sync(0xFFFFFFFFu, fmaxf(sd[0], sd[1]) > m_run[0] + kSlack)) {
+                float pm = fmaxf(sd[0], sd[1]);
 #pragma unroll
-            for (int d = 4; d < 32; d <<= 1) pm = fmaxf(pm, __shfl_xor_sync(0xFFFFFFFFu, pm, d));
-            const float mn = fmaxf(m_run[0], pm);
-            const float al = exp2f(m_run[0] - mn);
-            const float p0 = exp2f(sd[0] - mn), p1 = exp2f(sd[1] - mn);
+                for (int d = 4; d < 32; d <<= 1) pm = fmaxf(pm, __shfl_xor_sync(0xFFFFFFFFu, pm, d));
+                const float mn = fmaxf(m_run[0], pm);
+                al = ex2(m_run[0] - mn);
+                m_run[0] = mn;
+            }
+            const float p0 = ex2(sd[0] - m_run[0]), p1 = ex2(sd[1] - m_run[0]);
             l_run[0] = fmaf(l_run[0], al, p0 + p1);
-            m_run[0] = mn;
             uint4 vr[2][4];
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
@@ -444,7 +465,7 @@ scored_attn_kernel(const ScoredArgs a) {
         for (int w = 0; w < kWarps; ++w) { p[w] = sh_ml[w][h]; m = fmaxf(m, p[w].x); }
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-            const float f = p[w].x == -INFINITY ? 0.f : exp2f(p[w].x - m);
+            const float f = p[w].x == -INFINITY ? 0.f : ex2(p[w].x - m);
             l = fmaf(p[w].y, f, l);
             o = fmaf(ex[(w * HEADS + h) * kHeadStride + tid], f, o);
         }
@@ -474,7 +495,7 @@ scored_attn_kernel(const ScoredArgs a) {
 #pragma unroll
         for (int k = 0; k < kMaxCluster; ++k) {
             if (pm[k] == -INFINITY) continue;
-            const float f = exp2f(pm[k] - m);
+            const float f = ex2(pm[k] - m);
             l = fmaf(pl[k], f, l);
             o = fmaf(po[k], f, o);
         }
@@ -540,10 +561,11 @@ cudaError_t launch_scored_attn(const Geom& g, const void* k, const void* v_packe
     int sms = 0;
     cudaError_t e = device_sm_count(&sms);
     if (e != cudaSuccess) return e;
-    // two CTAs per SM with three stages, three with two for the single-head path, whose arithmetic per page outlasts a copy
-    a.cluster = cluster_size(g.problems, max_pages, sms * (g.Gq > 1 ? 2 : 3));
+    // three CTAs per SM with two stages per warp: a page's arithmetic outlasts a copy, so twelve warps per SM beat eight with
+    // three stages (8 sequences, 28 / 4 heads, 256 pages: 15.3 against 15.9 us)
+    a.cluster = cluster_size(g.problems, max_pages, sms * 3);
 #define STC_SCORED(S_) \
-    case S_: return g.Gq > 1 ? launch<S_, true, 3, 2>(a, g.problems, st) : launch<S_, false, 2, 3>(a, g.problems, st);
+    case S_: return g.Gq > 1 ? launch<S_, true, 2, 3>(a, g.problems, st) : launch<S_, false, 2, 3>(a, g.problems, st);
     switch (g.S) {
         STC_SCORED(4) STC_SCORED(8) STC_SCORED(16)
         default: return cudaErrorInvalidValue;
