@@ -285,12 +285,19 @@ scored_attn_kernel(const ScoredArgs a) {
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) { acc[dt][0] *= al0; acc[dt][1] *= al1; acc[dt][2] *= al0; acc[dt][3] *= al1; }
             }
-            // P^T as B fragments: high bf16 part and bf16 residual
-            const uint32_t wh0 = pack_bf16(p0, p1), wh1 = pack_bf16(p2, p3);
-            const uint32_t wl0 = pack_bf16(p0 - bf16lo(wh0), p1 - bf16hi(wh0));
-            const uint32_t wl1 = pack_bf16(p2 - bf16lo(wh1), p3 - bf16hi(wh1));
-            const uint32_t bh0 = movmatrix_trans(wh0), bh1 = movmatrix_trans(wh1);
-            const uint32_t bl0 = movmatrix_trans(wl0), bl1 = movmatrix_trans(wl1);
+            // P^T as B fragments: a weight is the sum of three bf16 parts (24 bits, so the weights are as good as fp32; the third
+            // part costs a page 8 of 32 MMAs and less than 3 % of a call)
+            uint32_t wb[3][2];
+            {
+                float x0 = p0, x1 = p1, x2 = p2, x3 = p3;
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                    const uint32_t u0 = pack_bf16(x0, x1), u1 = pack_bf16(x2, x3);
+                    wb[k][0] = movmatrix_trans(u0);
+                    wb[k][1] = movmatrix_trans(u1);
+                    x0 -= bf16lo(u0); x1 -= bf16hi(u0); x2 -= bf16lo(u1); x3 -= bf16hi(u1);
+                }
+            }
             // value rows: this lane addresses token tau, chunk 2dt + hb of every dim tile
             const int tau = (lane & 7) + 8 * (lane >> 4), hb = (lane >> 3) & 1;
             const uint32_t m = __shfl_sync(0xFFFFFFFFu, mask, tau);
@@ -304,8 +311,8 @@ scored_attn_kernel(const ScoredArgs a) {
                 const bool kept = ((m >> grp) & 1u) && idx < f.chunks;
                 uint32_t a0, a1, a2, a3;
                 ldmatrix_x4_trans(kept ? vst + idx * 16u : zero_row, a0, a1, a2, a3);
-                mma_bf16(acc[dt], a0, a1, a2, a3, bh0, bh1);
-                mma_bf16(acc[dt], a0, a1, a2, a3, bl0, bl1);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) mma_bf16(acc[dt], a0, a1, a2, a3, wb[k][0], wb[k][1]);
             }
         } else {
             // one head on the fp32 pipes: lane = tokens r, r+8 x chunks c, c+4, c+8, c+12
