@@ -153,7 +153,8 @@ def _stream() -> int:
 
 # The current device and its current stream without the objects torch.cuda wraps around them: a decode step's calls
 # take a few microseconds on the device, and the host's share of them is this module.
-_current_device = torch.cuda.current_device
+# (the tensors of a call have initialised CUDA)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
 
@@ -169,23 +170,27 @@ def _at(t: Optional[torch.Tensor], dtype, device: int, name: str) -> int:
     return _ptr(t, dtype, name)
 
 
+try:
+    from ._tensor_args import addresses as _native_addresses, sizes_are as _sizes_are, token_rows as _native_token_rows
+except ImportError:                              # not built: the same checks in Python
+    _native_addresses = _sizes_are = _native_token_rows = None
+_CODES = {"b": torch.bfloat16, "f": torch.float32, "d": torch.float64, "i": torch.int32, "u": torch.uint8}
+
+
+def _addresses(device: int, codes: str, names: tuple, *tensors) -> tuple:
+    """Address of each tensor (0 for None), checked to be a contiguous one of type codes[i] ('*': any) on CUDA `device`."""
+    got = _native_addresses(device, codes, *tensors) if _native_addresses is not None else None
+    if got is None:                              # something is wrong: find it and say what
+        got = tuple(_at(t, _CODES[c] if c != "*" else None if t is None else t.dtype, device, n)
+                    for t, c, n in zip(tensors, codes, names))
+    return got
+
+
 # Structures as the bytes the library reads (native layout of stc_shape, stc_cache, stc_score, stc_rope).
 _PACK_SHAPE = struct.Struct("8iP").pack
 _PACK_CACHE = struct.Struct("6Pq").pack
 _PACK_SCORE = struct.Struct("fi4P").pack
 _PACK_ROPE = struct.Struct("Piifi").pack
-
-
-def _pack_shape(s: "Shape", device: int) -> bytes:
-    return _PACK_SHAPE(s.batch, s.n_q_heads, s.n_kv_heads, s.head_dim, s.page_size, s.n_groups, s.t_cap, 0,
-                       _at(s.seq_len, torch.int32, device, "seq_len"))
-
-
-def _pack_cache(c: "Cache", device: int) -> bytes:
-    bf16 = torch.bfloat16
-    return _PACK_CACHE(_at(c.k, bf16, device, "k"), 0, 0, _at(c.v_packed, bf16, device, "v_packed"),
-                       0 if c.v_mask is None else _at(c.v_mask, c.v_mask.dtype, device, "v_mask"),
-                       0 if c.v_offs is None else _at(c.v_offs, c.v_offs.dtype, device, "v_offs"), c.cap_groups)
 
 
 @dataclass
@@ -254,15 +259,9 @@ class Score:
     tok_doc: Optional[torch.Tensor] = None    # i32 [B, T]
     q_doc: Optional[torch.Tensor] = None      # i32, one per query row
 
-    def packed(self, shape: Shape, rows: int, device: int) -> bytes:
-        _sized(self.slopes, (shape.n_q_heads,), "slopes")
-        _sized(self.q_pos, (rows,), "q_pos")
-        _sized(self.tok_doc, (shape.batch, shape.t_cap), "tok_doc")
-        _sized(self.q_doc, (rows,), "q_doc")
-        return _PACK_SCORE(self.softcap, self.window, _at(self.slopes, torch.float32, device, "slopes"),
-                           _at(self.q_pos, torch.int32, device, "q_pos"),
-                           _at(self.tok_doc, torch.int32, device, "tok_doc"),
-                           _at(self.q_doc, torch.int32, device, "q_doc"))
+    def check(self, shape: Shape, rows: int) -> None:
+        _sizes(("slopes", "q_pos", "tok_doc", "q_doc"), self.slopes, (shape.n_q_heads,), self.q_pos, (rows,), self.tok_doc,
+               (shape.batch, shape.t_cap), self.q_doc, (rows,))
 
 
 @dataclass
@@ -272,9 +271,13 @@ class Rope:
     interleaved: bool = False
     scale: float = 1.0
 
-    def packed(self, device: int) -> bytes:
-        return _PACK_ROPE(_at(self.inv_freq, torch.float64, device, "inv_freq"), 2 * self.inv_freq.numel(),
-                          int(self.interleaved), self.scale, 0)
+
+def _sizes(names: tuple, *pairs) -> None:
+    """Checks tensor, size, tensor, size, ..."""
+    if _sizes_are is not None and _sizes_are(*pairs):
+        return
+    for i, name in enumerate(names):
+        _sized(pairs[2 * i], pairs[2 * i + 1], name)
 
 
 def _sized(t: Optional[torch.Tensor], size: tuple, name: str) -> None:
@@ -286,6 +289,9 @@ def _token_rows(t: Optional[torch.Tensor], B: int, n: int, heads: int, dim: int,
     """(address, elements from token to token) of rows [B, n, heads, dim] that may be a slice of wider token rows."""
     if t is None:
         return 0, 0
+    got = _native_token_rows(device, t, B, n, heads, dim) if _native_token_rows is not None else None
+    if got is not None:
+        return got
     if t.get_device() != device or t.dtype is not torch.bfloat16:
         raise ValueError(f"{name} must be a tensor of torch.bfloat16 on cuda:{device}, got {t.dtype} on {t.device}")
     if t.shape != (B, n, heads, dim):
@@ -421,6 +427,9 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = ROPE_NO
     return inv_freq, float(scale.value)
 
 
+_ROPE_NAMES = ("seq_len", "inv_freq", "old_len", "positions", "q_out", "k", "v", "status")
+
+
 def rope_write(shape: Shape, rope: Rope, old_len: torch.Tensor, status: torch.Tensor,
                q_in: Optional[torch.Tensor] = None, k_in: Optional[torch.Tensor] = None,
                v_in: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
@@ -434,20 +443,19 @@ def rope_write(shape: Shape, rope: Rope, old_len: torch.Tensor, status: torch.Te
     first = q_in if q_in is not None else k_in if k_in is not None else v_in
     if first is None:
         raise ValueError("rope_write needs at least one of q_in, k_in, v_in")
-    n, dev, bf16 = first.shape[1], _current_device(), torch.bfloat16
+    n, dev = first.shape[1], _current_device()
     qp, qs = _token_rows(q_in, B, n, Hq, D, dev, "q_in")
     kp, ks = _token_rows(k_in, B, n, Hkv, D, dev, "k_in")
     vp, vs = _token_rows(v_in, B, n, Hkv, D, dev, "v_in")
-    _sized(q_out, (B, n, Hq, D), "q_out")
-    _sized(k, (B, Hkv, T, D), "k")
-    _sized(v, (B, Hkv, T, D), "v")
-    _sized(positions, (B, n), "positions")
-    _sized(old_len, (B,), "old_len")
-    _sized(status, (B,), "status")
+    cache, per_seq = (B, Hkv, T, D), (B,)
+    _sizes(("q_out", "k", "v", "positions", "old_len", "status"), q_out, (B, n, Hq, D), k, cache, v, cache, positions, (B, n),
+           old_len, per_seq, status, per_seq)
+    lp, fp, op, pp, qo, ko, vo, sp = _addresses(dev, "idiibbbi", _ROPE_NAMES, shape.seq_len, rope.inv_freq, old_len,
+                                                positions, q_out, k, v, status)
     rc = load_library().stc_rope_write(
-        _pack_shape(shape, dev), rope.packed(dev), _at(old_len, torch.int32, dev, "old_len"), n,
-        _at(positions, torch.int32, dev, "positions"), qp, qs, kp, ks, vp, vs, _at(q_out, bf16, dev, "q_out"),
-        _at(k, bf16, dev, "k"), _at(v, bf16, dev, "v"), _at(status, torch.int32, dev, "status"), _raw_stream(dev))
+        _PACK_SHAPE(B, Hq, Hkv, D, shape.page_size, shape.n_groups, T, 0, lp),
+        _PACK_ROPE(fp, 2 * rope.inv_freq.numel(), int(rope.interleaved), rope.scale, 0), op, n, pp, qp, qs, kp, ks, vp, vs,
+        qo, ko, vo, sp, _raw_stream(dev))
     if rc:
         raise StcError(rc, "stc_rope_write")
 
@@ -483,6 +491,10 @@ def query_bias(h_q: torch.Tensor, w_q: torch.Tensor, s_q: torch.Tensor, bias: to
         _stream()), "stc_query_bias")
 
 
+_SCORED_NAMES = ("seq_len", "k", "v_packed", "v_mask", "v_offs", "slopes", "q_pos", "tok_doc", "q_doc", "q", "page_ids",
+                 "n_pages", "out", "lse", "ws")
+
+
 def decode_attn(shape: Shape, cache: Cache, q: torch.Tensor, page_ids: Optional[torch.Tensor],
                 n_pages: Optional[torch.Tensor], sm_scale: float, out: torch.Tensor, ws: torch.Tensor,
                 lse: Optional[torch.Tensor] = None, score: Optional[Score] = None) -> None:
@@ -490,11 +502,15 @@ def decode_attn(shape: Shape, cache: Cache, q: torch.Tensor, page_ids: Optional[
     max_pages = page_ids.shape[-1] if page_ids is not None else shape.n_pages
     if score is not None:
         dev = _current_device()
+        score.check(shape, shape.batch)
+        lp, kp, vp, mp, op, slp, pop, tdp, qdp, qp, ip, np_, outp, lsep, wsp = _addresses(
+            dev, "ibb**fiiibiiffu", _SCORED_NAMES, shape.seq_len, cache.k, cache.v_packed, cache.v_mask, cache.v_offs,
+            score.slopes, score.q_pos, score.tok_doc, score.q_doc, q, page_ids, n_pages, out, lse, ws)
         rc = load_library().stc_decode_attn_scored(
-            _pack_shape(shape, dev), _pack_cache(cache, dev), _at(q, torch.bfloat16, dev, "q"),
-            _at(page_ids, torch.int32, dev, "page_ids"), _at(n_pages, torch.int32, dev, "n_pages"), max_pages, sm_scale,
-            score.packed(shape, shape.batch, dev), _at(out, torch.float32, dev, "out"), _at(lse, torch.float32, dev, "lse"),
-            _at(ws, torch.uint8, dev, "ws"), ws.numel(), _raw_stream(dev))
+            _PACK_SHAPE(shape.batch, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.page_size, shape.n_groups,
+                        shape.t_cap, 0, lp),
+            _PACK_CACHE(kp, 0, 0, vp, mp, op, cache.cap_groups), qp, ip, np_, max_pages, sm_scale,
+            _PACK_SCORE(score.softcap, score.window, slp, pop, tdp, qdp), outp, lsep, wsp, ws.numel(), _raw_stream(dev))
         if rc:
             raise StcError(rc, "stc_decode_attn_scored")
         return
@@ -506,24 +522,29 @@ def decode_attn(shape: Shape, cache: Cache, q: torch.Tensor, page_ids: Optional[
         "stc_decode_attn")
 
 
+_PREFIX_NAMES = ("seq_len", "k", "v_packed", "v_mask", "v_offs", "slopes", "q_pos", "tok_doc", "q_doc", "q", "row_start",
+                 "own_out", "own_lse", "out", "lse", "ws")
+_PLAIN = Score()
+
+
 def prefix_attn(shape: Shape, cache: Cache, q: torch.Tensor, row_start: torch.Tensor, sm_scale: float, out: torch.Tensor,
                 ws: torch.Tensor, lse: Optional[torch.Tensor] = None, score: Optional[Score] = None,
                 own_out: Optional[torch.Tensor] = None, own_lse: Optional[torch.Tensor] = None) -> None:
     """Rows row_start[g] .. row_start[g+1] of q [n_rows, Hq, 128] attend prefix g (sequence g of shape / cache), read
     once for all of them; own_out / own_lse (the rows' results over their own tokens) are joined by log-sum-exp."""
-    n, Hq, dev, f32 = q.shape[0], shape.n_q_heads, _current_device(), torch.float32
-    rows = (n, Hq, shape.head_dim)
-    _sized(q, rows, "q")
-    _sized(row_start, (shape.batch + 1,), "row_start")
-    _sized(out, rows, "out")
-    _sized(lse, (n, Hq), "lse")
-    _sized(own_out, rows, "own_out")
-    _sized(own_lse, (n, Hq), "own_lse")
+    n, Hq, dev = q.shape[0], shape.n_q_heads, _current_device()
+    rows, heads = (n, Hq, shape.head_dim), (n, Hq)
+    _sizes(("q", "row_start", "out", "lse", "own_out", "own_lse"), q, rows, row_start, (shape.batch + 1,), out, rows, lse, heads,
+           own_out, rows, own_lse, heads)
+    co = score if score is not None else _PLAIN
+    co.check(shape, n)
+    lp, kp, vp, mp, op, slp, pop, tdp, qdp, qp, sp, oop, olp, outp, lsep, wsp = _addresses(
+        dev, "ibb**fiiibiffffu", _PREFIX_NAMES, shape.seq_len, cache.k, cache.v_packed, cache.v_mask, cache.v_offs,
+        co.slopes, co.q_pos, co.tok_doc, co.q_doc, q, row_start, own_out, own_lse, out, lse, ws)
     rc = load_library().stc_prefix_attn(
-        _pack_shape(shape, dev), _pack_cache(cache, dev), n, _at(q, torch.bfloat16, dev, "q"),
-        _at(row_start, torch.int32, dev, "row_start"), sm_scale, score.packed(shape, n, dev) if score is not None else None,
-        _at(own_out, f32, dev, "own_out"), _at(own_lse, f32, dev, "own_lse"), _at(out, f32, dev, "out"),
-        _at(lse, f32, dev, "lse"), _at(ws, torch.uint8, dev, "ws"), ws.numel(), _raw_stream(dev))
+        _PACK_SHAPE(shape.batch, Hq, shape.n_kv_heads, shape.head_dim, shape.page_size, shape.n_groups, shape.t_cap, 0, lp),
+        _PACK_CACHE(kp, 0, 0, vp, mp, op, cache.cap_groups), n, qp, sp, sm_scale,
+        _PACK_SCORE(co.softcap, co.window, slp, pop, tdp, qdp), oop, olp, outp, lsep, wsp, ws.numel(), _raw_stream(dev))
     if rc:
         raise StcError(rc, "stc_prefix_attn")
 

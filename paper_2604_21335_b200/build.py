@@ -18,6 +18,27 @@ NVCC_FLAGS = [
 ]
 
 
+ARGS_SRC = CSRC / "tensor_args.cpp"
+ARGS_LIB = PKG / "_tensor_args.so"
+
+
+def _build_args(force: bool = False) -> None:
+    """The binding's argument check (a CPython module against the headers of the installed torch), in-tree."""
+    if not force and ARGS_LIB.exists() and ARGS_LIB.stat().st_mtime >= ARGS_SRC.stat().st_mtime:
+        return
+    import sysconfig
+
+    import torch
+    root = Path(torch.__file__).resolve().parent
+    include = [root / "include", root / "include" / "torch" / "csrc" / "api" / "include", sysconfig.get_paths()["include"]]
+    tmp = ARGS_LIB.with_suffix(f".{os.getpid()}.tmp")
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                           *[f"-I{p}" for p in include], str(ARGS_SRC), "-o", str(tmp), f"-L{root / 'lib'}",
+                           "-ltorch_python", "-ltorch_cpu", "-lc10"])
+    os.replace(tmp, ARGS_LIB)
+
+
 def _stale() -> bool:
     if not LIB.exists():
         return True
@@ -28,6 +49,7 @@ def _stale() -> bool:
 
 def build(force: bool = False, verbose: bool = False) -> Path:
     """Compile every CUDA source into one shared library; returns its path."""
+    _build_args(force)
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
