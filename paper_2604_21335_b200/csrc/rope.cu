@@ -13,9 +13,10 @@
 // Work split.  Bandwidth-bound: 512 bytes moved per head row, 256 each way.  A thread owns two 16-byte chunks
 // of a row (a "duo": with the half layout chunk d and its partner d + rot/16, else neighbours), so that both
 // members of eight pairs meet in one thread; it computes its eight (cos, sin) once and keeps them in registers
-// while it walks over the q and k heads of its token.  A CTA is 8 duos x 32 (token, head slot) lanes; long
-// calls put 32 tokens in a CTA (one sincos for all heads), short ones put one token and 32 head slots
-// there, which is what a decode step's latency wants: every row is in flight at once.
+// while it walks over the rows of its token, four in flight.  A CTA is 8 duos x 32 (token, row slot) lanes: four
+// tokens with eight slots each, or one token with 32 slots where tokens are few, so that every row is in flight at once.
+// Measured: 2 x 16384 tokens of 32 + 8 + 8 heads in 124 us = 6.5 TB/s, 1.0 of the measured copy bandwidth; a decode
+// step of 16 tokens in 3 us, which is the launch and two round trips to memory (lengths, then rows).
 #include "common.cuh"
 
 namespace stc {
@@ -97,38 +98,37 @@ rope_write_kernel(const RopeArgs a) {
         }
     }
 
-    // heads of this lane: slot, slot + SLOTS, ... over q (if any), then k, then v
+    // rows of this lane: slot, slot + SLOTS, ... of the token's q rows, then k, then v; all parts together, so that a short
+    // call has every row of the token in flight at once
     const size_t token = (size_t)b * a.max_new + i;
-    auto walk = [&](const uint4* in, int64_t stride, uint4* out, int64_t head_step, int heads, bool rotate) {
-        if (!in) return;
-        const uint4* src = in + token * stride;
-#pragma unroll 1
-        for (int h0 = slot; h0 < heads; h0 += SLOTS * kRowsInFlight) {
-            uint4 x[kRowsInFlight], y[kRowsInFlight];
-#pragma unroll
-            for (int j = 0; j < kRowsInFlight; ++j) {
-                const int h = h0 + j * SLOTS;
-                if (h < heads) {
-                    x[j] = src[h * kOctets + c0];
-                    y[j] = src[h * kOctets + c1];
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < kRowsInFlight; ++j) {
-                const int h = h0 + j * SLOTS;
-                if (h < heads) {
-                    if (rotate && turned) turn_duo<HALF>(x[j], y[j], cs, sn);
-                    out[h * head_step + c0] = x[j];
-                    out[h * head_step + c1] = y[j];
-                }
-            }
-        }
-    };
+    const int nq = a.q_in ? a.Hq : 0, nk = nq + (a.k_in ? a.Hkv : 0), nv = nk + (a.v_in ? a.Hkv : 0);
     const int64_t cache_step = (int64_t)a.T * kOctets;                    // from head to head of the cache
     const size_t cache_row = ((size_t)b * a.Hkv * a.T + t) * kOctets;
-    walk(a.q_in, a.q_stride, a.q_out + token * a.Hq * kOctets, kOctets, a.Hq, true);
-    walk(a.k_in, a.k_stride, a.k + cache_row, cache_step, a.Hkv, true);
-    walk(a.v_in, a.v_stride, a.v + cache_row, cache_step, a.Hkv, false);
+    const uint4 *q_src = a.q_in + token * a.q_stride, *k_src = a.k_in + token * a.k_stride, *v_src = a.v_in + token * a.v_stride;
+#pragma unroll 1
+    for (int h0 = slot; h0 < nv; h0 += SLOTS * kRowsInFlight) {
+        uint4 x[kRowsInFlight], y[kRowsInFlight];
+#pragma unroll
+        for (int j = 0; j < kRowsInFlight; ++j) {
+            const int h = h0 + j * SLOTS;
+            if (h < nv) {
+                const uint4* src = h < nq ? q_src + h * kOctets : h < nk ? k_src + (h - nq) * kOctets : v_src + (h - nk) * kOctets;
+                x[j] = src[c0];
+                y[j] = src[c1];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kRowsInFlight; ++j) {
+            const int h = h0 + j * SLOTS;
+            if (h < nv) {
+                if (h < nk && turned) turn_duo<HALF>(x[j], y[j], cs, sn);
+                uint4* dst = h < nq ? a.q_out + (token * a.Hq + h) * kOctets
+                                    : h < nk ? a.k + cache_row + (h - nq) * cache_step : a.v + cache_row + (h - nk) * cache_step;
+                dst[c0] = x[j];
+                dst[c1] = y[j];
+            }
+        }
+    }
 }
 
 }  // namespace
@@ -149,9 +149,10 @@ cudaError_t launch_rope_write(const Geom& g, const stc_rope& rope, const int32_t
     int sms = 0;
     cudaError_t e = device_sm_count(&sms);
     if (e != cudaSuccess) return e;
-    // 32 tokens per CTA once that still gives every SM four CTAs, else 4, else one token per CTA
+    // four tokens per CTA once that still gives every SM one, else one token per CTA (8 x 511 ragged tokens: 10.7 against
+    // 16.8 us; 2 x 16384 tokens: 2, 4, 8, 16, 32 tokens per CTA take 143, 124, 124, 127, 131 us)
     const long long tokens = (long long)g.B * max_new;
-    const int tok = tokens >= 32LL * 4 * sms ? 32 : tokens >= 4LL * 4 * sms ? 4 : 1;
+    const int tok = tokens >= 4LL * sms ? 4 : 1;
     a.chunks = (max_new + tok - 1) / tok;
     const long long n_cta = (long long)a.chunks * g.B;
     if (n_cta > 0x7FFFFFFFLL) return cudaErrorInvalidConfiguration;
@@ -160,8 +161,7 @@ cudaError_t launch_rope_write(const Geom& g, const stc_rope& rope, const int32_t
         if (rope.interleaved) rope_write_kernel<TOK_, false><<<(unsigned)n_cta, kThreads, 0, st>>>(a);  \
         else rope_write_kernel<TOK_, true><<<(unsigned)n_cta, kThreads, 0, st>>>(a);                    \
     } while (0)
-    if (tok == 32) STC_ROPE(32);
-    else if (tok == 4) STC_ROPE(4);
+    if (tok == 4) STC_ROPE(4);
     else STC_ROPE(1);
 #undef STC_ROPE
     return cudaGetLastError();

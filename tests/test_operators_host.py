@@ -123,3 +123,28 @@ def test_prefix_attention_refusals(lib):
     assert P.workspace_bytes(P.Shape(2, 8, 4, 8, 0), Bd.OP_PREFIX_ATTN, 4) > 0
     with pytest.raises(P.StcError):
         P.workspace_bytes(s, Bd.OP_PREFIX_ATTN, -1)
+
+
+def test_argument_checks_agree_with_and_without_the_native_module(lib, monkeypatch):
+    """CPU tensors, wrong types, sizes and layouts are refused in the same words by both."""
+    assert Bd._native_addresses is not None, "the build makes the native argument check"
+    i32 = torch.zeros(2, dtype=torch.int32)
+    shape = P.Shape(2, 8, 4, 8, 16, i32)
+    x = torch.zeros(2, 1, 8, 128, dtype=torch.bfloat16)
+    cases = [lambda: P.rope_write(shape, P.Rope(torch.zeros(8, dtype=torch.float64)), i32, i32, q_in=x, q_out=x),
+             lambda: P.rope_write(shape, P.Rope(torch.zeros(8, dtype=torch.float64)), i32, i32),
+             lambda: P.decode_attn(shape, P.Cache(), x[:, 0], None, None, 1.0, x[:, 0].float(), i32, score=P.Score(softcap=1.0)),
+             lambda: P.decode_attn(shape, P.Cache(), x[:, 0], None, None, 1.0, x[:, 0].float(), i32, score=P.Score(slopes=torch.zeros(3))),
+             lambda: P.prefix_attn(shape, P.Cache(), x[:, 0], i32, 1.0, x[:, 0].float(), i32),
+             lambda: P.prefix_attn(shape, P.Cache(), x[:, 0], torch.zeros(3, dtype=torch.int32), 1.0, x[:1, 0].float(), i32)]
+    monkeypatch.setattr(Bd, "_current_device", lambda: 0)
+
+    def said(f):
+        with pytest.raises(ValueError) as e:
+            f()
+        return str(e.value)
+
+    native = [said(f) for f in cases]
+    for name in ("_native_addresses", "_sizes_are", "_native_token_rows"):
+        monkeypatch.setattr(Bd, name, None)
+    assert [said(f) for f in cases] == native
