@@ -21,8 +21,9 @@
 // rows) and larger batches take more units, whose K and V come from L2.
 //
 // Work split.  Unit = (prefix, KV head, block of up to two row tiles); the token tiles of all units form one flat
-// sequence that is cut into equal contiguous ranges, one per CTA (one CTA per SM).  A CTA walks the segments of its
-// range; a segment that is a whole unit is finished in place, another one leaves a partial (max, sum,
+// sequence, each as long as it takes (2, 3 or 4 for a tile whose softmax has 32 scores per thread, 64, or 64 in both
+// groups), that is cut into equal contiguous ranges, one per CTA (one CTA per SM).  A CTA takes the tiles that begin in its
+// range and walks them unit by unit, segment by segment; a segment that is a whole unit is finished in place, another one leaves a partial (max, sum,
 // accumulator) which a second small kernel joins in CTA order: no atomics, bitwise repeatable.
 //
 // Roles (16 warps): warp 0 = TMA producer of Q and K; warps 1, 2 = MMA issuers of the two groups; warp 3 = scheduler
@@ -94,7 +95,8 @@ struct PrefixArgs {
     float* lse;                  // or nullptr
     int32_t* cta_status;         // [grid], one word per CTA
     int32_t* status;             // the call's status word, written by the second kernel
-    long long* base;             // [G + 2]: first flat tile of each prefix; [G] = total; [G + 1] = 1 if row_start is bad
+    long long* base;             // [G + 3]: where each prefix begins in the flat sequence; [G] = its length; [G + 1] = CTAs that
+                                 // share it; [G + 2] = 1 if row_start is bad
     float4* part_o;              // [3 * grid][2 groups][32 chunks of 4 dims][128 lanes]
     float2* part_ml;             // [3 * grid][2][128]
     float4* flush;               // [grid][2 groups][32][128 rows]: sums of emptied accumulators
@@ -102,12 +104,19 @@ struct PrefixArgs {
     int G, Hq, Hkv, Gq, T, n_rows;
     int quarter;                 // sequences per quarter of a row tile = 32 / Gq
     int seqs;                    // sequences per row tile = 4 * quarter
+    int q_box;                   // quarters a load of Q brings: 2 where their rows are contiguous (Gq divides 32), else 1
     float scale_log2, cap_in, cap_log2;
     ScoreArgs sc;
 };
 
+// Copies of its rows that the row tile of a segment holds.
+__device__ __forceinline__ int copies(const PrefixArgs& a, int n_seq) {
+    return n_seq <= 2 * a.quarter ? 2 : 1;
+}
+
 struct Group {
     int row0, n_seq, len, tiles, blocks;
+    int weight;                  // length of a tile of its first block in the flat sequence
 };
 __device__ __forceinline__ Group make_group(const PrefixArgs& a, int row0, int row1, int len) {
     Group r;
@@ -116,13 +125,14 @@ __device__ __forceinline__ Group make_group(const PrefixArgs& a, int row0, int r
     r.len = len;
     r.tiles = (len + kTok - 1) / kTok;
     r.blocks = (r.n_seq + 2 * a.seqs - 1) / (2 * a.seqs);
+    r.weight = r.n_seq > a.seqs ? 4 : copies(a, r.n_seq) == 2 ? 2 : 3;
     return r;
 }
 __device__ __forceinline__ Group load_group(const PrefixArgs& a, int g) {
     return make_group(a, a.row_start[g], a.row_start[g + 1], clamp_len(a.seq_len, g, a.T));
 }
-__device__ __forceinline__ long long group_tiles(const PrefixArgs& a, const Group& g) {
-    return (long long)g.tiles * g.blocks * a.Hkv;
+__device__ __forceinline__ long long group_length(const PrefixArgs& a, const Group& g) {
+    return (long long)g.tiles * g.weight * g.blocks * a.Hkv;
 }
 
 // One segment: tiles [tile0, tile1) of one unit.
@@ -130,41 +140,48 @@ struct Segment {
     int g, hk, row0, n_seq, len, tile0, tile1;
     int slot;                    // partial slot, -1 = the whole unit
 };
-// Copies of its rows that the row tile of a segment holds.
-__device__ __forceinline__ int copies(const PrefixArgs& a, int n_seq) {
-    return n_seq <= 2 * a.quarter ? 2 : 1;
-}
 __device__ __forceinline__ long long div_small(long long x, int d) {        // x >= 0, d > 0
     return (x >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)d) : x / d;
 }
+// CTA `c` of `n` takes the positions [total * c / n, total * (c + 1) / n) of the flat sequence.
+__device__ __forceinline__ long long range_begin(long long total, int c, int n) {
+    return total < (1 << 24) ? (long long)((uint32_t)total * (uint32_t)c / (uint32_t)n) : total * c / n;
+}
+__device__ __forceinline__ int cta_of(long long total, long long x, int n) {
+    return total < (1 << 24) ? (int)((((uint32_t)x + 1u) * (uint32_t)n + (uint32_t)total - 1u) / (uint32_t)total) - 1
+                             : (int)(((x + 1) * n + total - 1) / total - 1);
+}
 
-// Walks the segments of the CTA's range [x, x_end).
+// Walks the segments of the CTA's range.
 struct Walker {
-    long long x, x_end, x_begin, off;  // off = x - base of group g
+    long long x, x_end, off;     // positions; off = x - begin of group g
     int g;
     Group grp;                   // group g
     __device__ __forceinline__ bool next(const PrefixArgs& a, Segment& s) {
-        if (x >= x_end) return false;
-        while (off >= group_tiles(a, grp)) {
-            off -= group_tiles(a, grp);
-            grp = load_group(a, ++g);
+        while (x < x_end) {
+            while (off >= group_length(a, grp)) {
+                off -= group_length(a, grp);
+                grp = load_group(a, ++g);
+            }
+            const int length = grp.tiles * grp.weight;                     // of a unit (below 2^25)
+            const long long unit = div_small(off, length);
+            const int from = (int)(off - unit * length), to = (int)min((long long)length, from + (x_end - x));
+            x += to - from;
+            off += to - from;
+            s.tile0 = (int)((uint32_t)(from + grp.weight - 1) / (uint32_t)grp.weight);
+            s.tile1 = (int)((uint32_t)(to + grp.weight - 1) / (uint32_t)grp.weight);
+            if (s.tile0 >= s.tile1) continue;                              // the rest of a tile that began before the range
+            s.hk = (int)div_small(unit, grp.blocks);
+            const int blk = (int)(unit - (long long)s.hk * grp.blocks);
+            s.g = g;
+            s.row0 = grp.row0 + blk * 2 * a.seqs;
+            s.n_seq = min(2 * a.seqs, grp.n_seq - blk * 2 * a.seqs);
+            s.len = grp.len;
+            // a CTA continues at most one unit (slot 0) and leaves at most one that it begins (slot 1)
+            s.slot = s.tile1 - s.tile0 == grp.tiles ? -1 : 2 * (int)blockIdx.x + (s.tile0 == 0 ? 1 : 0);
+            return true;
         }
-        const long long unit = div_small(off, grp.tiles);
-        s.tile0 = (int)(off - unit * grp.tiles);
-        const long long left = x_end - x;
-        s.tile1 = (int)min((long long)grp.tiles, s.tile0 + left);
-        s.hk = (int)div_small(unit, grp.blocks);
-        const int blk = (int)(unit - (long long)s.hk * grp.blocks);
-        s.g = g;
-        s.row0 = grp.row0 + blk * 2 * a.seqs;
-        s.n_seq = min(2 * a.seqs, grp.n_seq - blk * 2 * a.seqs);
-        s.len = grp.len;
-        const bool whole = s.tile0 == 0 && s.tile1 == grp.tiles;
-        s.slot = whole ? -1 : 2 * (int)blockIdx.x + (x == x_begin ? 0 : 1);
-        const int n = s.tile1 - s.tile0;
-        x += n;
-        off += n;
-        return true;
+        return false;
     }
 };
 
@@ -306,18 +323,27 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             uint32_t used[2] = {0u, 0u}, par[2] = {0u, 0u};    // per group, bit = stage: its last tile was read; parity to wait for
             bool ok = true;
             const uint32_t q_bytes = 2u * 128u * (uint32_t)(a.Gq * a.seqs);       // per row tile
+            const int loads = 4 / a.q_box, box_seqs = a.q_box * a.quarter;         // per half of a row tile
             while (ok && next_lane(ok)) {
                 const bool two = s.n_seq > a.seqs;
-                if (seg > 0 && !(wait(kQEmpty, (uint32_t)(seg - 1)) && wait(kQEmpty + 1, (uint32_t)(seg - 1)))) { ok = false; break; }
-                mbar_expect_tx(bar(kQFull), two ? 2 * q_bytes : q_bytes);
-                const int quarters = 4 / copies(a, s.n_seq);
+                auto bring_q = [&]() -> bool {
+                    if (seg > 0 && !(wait(kQEmpty, (uint32_t)(seg - 1)) && wait(kQEmpty + 1, (uint32_t)(seg - 1)))) return false;
+                    mbar_expect_tx(bar(kQFull), two ? 2 * q_bytes : q_bytes);
+                    const int distinct = loads / copies(a, s.n_seq);
 #pragma unroll 1
-                for (int i = 0; i < (two ? 16 : 8); ++i) {                         // (row tile, half, quarter)
-                    const int q = i & 3, h = (i >> 2) & 1, tile = i >> 3;
-                    tma_3d(base + tile * kQTile + h * kQHalf + q * (kQHalf / 4), &map_q, 64 * h, s.hk * a.Gq,
-                           s.row0 + tile * a.seqs + (q % quarters) * a.quarter, bar(kQFull));
-                }
-                ++seg;
+                    for (int tile = 0; tile < (two ? 2 : 1); ++tile)
+#pragma unroll 1
+                        for (int i = 0; i < loads; ++i) {
+                            const uint32_t dst = base + tile * kQTile + i * (uint32_t)a.q_box * (kQHalf / 4);
+                            const int first = s.row0 + tile * a.seqs + (i < distinct ? i : i - distinct) * box_seqs;
+                            tma_3d(dst, &map_q, 0, s.hk * a.Gq, first, bar(kQFull));
+                            tma_3d(dst + kQHalf, &map_q, 64, s.hk * a.Gq, first, bar(kQFull));
+                        }
+                    ++seg;
+                    return true;
+                };
+                // the queries behind the first key tile: both are wanted at once, and the keys come from farther away
+                bool q_due = true;
                 const int row = (s.g * a.Hkv + s.hk) * a.T;
                 int st = kc % kKStages;
 #pragma unroll 1
@@ -337,6 +363,11 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     if (two || odd == 0) used[0] |= 1u << st;
                     if (two || odd == 1) used[1] |= 1u << st;
                     if (++st == kKStages) st = 0;
+                    if (q_due) {
+                        q_due = false;
+                        ok = bring_q();
+                        if (!ok) { ++kc; break; }
+                    }
                 }
             }
             if (!ok) give_up();
@@ -412,72 +443,82 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
         if (!ok) give_up();
     } else if (warp == 3) {
-        // ---- scheduler: flat tile sequence by prefix sums over the prefixes, 32 at a time; this CTA's range; its segments ----
+        // ---- scheduler: the flat sequence by prefix sums over the prefixes, this CTA's range, its segments ----------------------
+        // (32 prefixes at a time; straight through for up to 32, since this stands before everything else)
+        Group grp = {};                              // of prefix `lane`
         bool bad = false;
-        auto scan = [&](auto&& use) {
-            long long run = 0;
-            for (int g0 = 0; g0 < a.G; g0 += 32) {
-                const int g = g0 + lane;
-                Group grp = {};
-                if (g < a.G) {
-                    const int r0 = g0 ? a.row_start[g] : first_r0, r1 = g0 ? a.row_start[g + 1] : first_r1;
-                    if (r0 < 0 || r1 < r0 || r1 > a.n_rows) bad = true;
-                    else grp = make_group(a, r0, r1, g0 ? clamp_len(a.seq_len, g, a.T) : first_len);
-                }
-                const long long n = group_tiles(a, grp);
-                long long incl = n;
+        if (lane < a.G) {
+            bad = first_r0 < 0 || first_r1 < first_r0 || first_r1 > a.n_rows;
+            if (!bad) grp = make_group(a, first_r0, first_r1, first_len);
+        }
+        auto sums = [&](long long n) {               // inclusive over the lanes
+            if (a.G == 1) return __shfl_sync(0xFFFFFFFFu, n, 0);
 #pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const long long o = __shfl_up_sync(0xFFFFFFFFu, incl, d);
-                    if (lane >= d) incl += o;
-                }
-                use(g, grp, run + incl - n, run + incl);
-                run += __shfl_sync(0xFFFFFFFFu, incl, 31);
+            for (int d = 1; d < 32; d <<= 1) {
+                const long long o = __shfl_up_sync(0xFFFFFFFFu, n, d);
+                if (lane >= d) n += o;
             }
-            return run;
+            return n;
         };
-        long long total = scan([&](int g, const Group&, long long lo, long long) {
-            if (blockIdx.x == 0 && g < a.G) a.base[g] = lo;
-        });
+        long long mine = group_length(a, grp), end = sums(mine), total = __shfl_sync(0xFFFFFFFFu, end, 31);
+        int weight = __reduce_max_sync(0xFFFFFFFFu, mine > 0 ? grp.weight : 0);
+        auto some = [&](const Group& g) { return g.tiles > 0 ? (int)min((long long)g.blocks * a.Hkv, 1LL << 20) : 0; };
+        const int units = __reduce_add_sync(0xFFFFFFFFu, some(grp));
+        const int longest = __reduce_max_sync(0xFFFFFFFFu, grp.tiles * grp.weight);
+        const bool alike = a.G <= 32 && __all_sync(0xFFFFFFFFu, grp.tiles == 0 || grp.tiles * grp.weight == longest);
+        if (blockIdx.x == 0 && lane < a.G) a.base[lane] = end - mine;
+        for (int g0 = 32; g0 < a.G; g0 += 32) {
+            Group more = {};
+            if (g0 + lane < a.G) {
+                const int r0 = a.row_start[g0 + lane], r1 = a.row_start[g0 + lane + 1];
+                if (r0 < 0 || r1 < r0 || r1 > a.n_rows) bad = true;
+                else more = load_group(a, g0 + lane);
+            }
+            const long long n = group_length(a, more), e = total + sums(n);
+            if (blockIdx.x == 0 && g0 + lane < a.G) a.base[g0 + lane] = e - n;
+            total = __shfl_sync(0xFFFFFFFFu, e, 31);
+            weight = max(weight, __reduce_max_sync(0xFFFFFFFFu, n > 0 ? more.weight : 0));
+        }
         bad = __any_sync(0xFFFFFFFFu, bad);
         if (bad) total = 0;
-        // this CTA's range; with fewer tiles than CTAs the rest stay idle
-        const int n_cta = (int)min(total, (long long)gridDim.x), cta = (int)blockIdx.x;
-        long long lo = 0, hi = 0;
+        // with fewer tiles than CTAs the rest stay idle: every range holds the beginning of a tile
+        const int cta = (int)blockIdx.x;
+        int n_cta = total > 0 ? (int)min(div_small(total, weight), (long long)gridDim.x) : 0;
+        if (alike && units > 0 && units < n_cta) {
+            // Units of one length: the same number of CTAs for each, so that units end where ranges end, if the CTAs that this
+            // leaves idle cost the others less than three tiles, about what a second segment costs a CTA.
+            const int even = n_cta / units * units;
+            if (total / even - total / n_cta < 3 * weight) n_cta = even;
+        }
+        Walker walk;
+        walk.x = walk.x_end = walk.off = 0;
+        walk.g = 0;
         if (cta < n_cta) {
-            if (total < (1 << 24)) {                 // everything below 2^32
-                lo = (uint32_t)total * (uint32_t)cta / (uint32_t)n_cta;
-                hi = (uint32_t)total * (uint32_t)(cta + 1) / (uint32_t)n_cta;
-            } else {
-                lo = total * cta / n_cta;
-                hi = total * (cta + 1) / n_cta;
+            walk.x = range_begin(total, cta, n_cta);
+            walk.x_end = range_begin(total, cta + 1, n_cta);
+            // the prefix that holds x
+            long long before = 0;
+            int g0 = 0;
+            for (;;) {
+                const uint32_t who = __ballot_sync(0xFFFFFFFFu, end - mine <= walk.x && walk.x < end);
+                if (who) {
+                    const int from = __ffs(who) - 1;
+                    walk.off = walk.x - __shfl_sync(0xFFFFFFFFu, end - mine, from);
+                    walk.g = g0 + from;
+                    walk.grp = Group{__shfl_sync(0xFFFFFFFFu, grp.row0, from), __shfl_sync(0xFFFFFFFFu, grp.n_seq, from),
+                                     __shfl_sync(0xFFFFFFFFu, grp.len, from), __shfl_sync(0xFFFFFFFFu, grp.tiles, from),
+                                     __shfl_sync(0xFFFFFFFFu, grp.blocks, from), __shfl_sync(0xFFFFFFFFu, grp.weight, from)};
+                    break;
+                }
+                before = __shfl_sync(0xFFFFFFFFu, end, 31);
+                g0 += 32;                            // (x < total: there is a next 32)
+                grp = Group{};
+                if (g0 + lane < a.G) grp = load_group(a, g0 + lane);
+                mine = group_length(a, grp);
+                end = before + sums(mine);
             }
         }
-        if (cta == 0 && lane == 0) { a.base[a.G] = total; a.base[a.G + 1] = bad; }
-        long long off = 0;
-        int g_first = 0;
-        Group at_first = {};
-        if (hi > lo) {
-            scan([&](int g, const Group& grp, long long first, long long end) {
-                const uint32_t who = __ballot_sync(0xFFFFFFFFu, g < a.G && first <= lo && lo < end);
-                if (!who) return;
-                const int from = __ffs(who) - 1;
-                off = lo - __shfl_sync(0xFFFFFFFFu, first, from);
-                g_first = __shfl_sync(0xFFFFFFFFu, g, from);
-                at_first.row0 = __shfl_sync(0xFFFFFFFFu, grp.row0, from);
-                at_first.n_seq = __shfl_sync(0xFFFFFFFFu, grp.n_seq, from);
-                at_first.len = __shfl_sync(0xFFFFFFFFu, grp.len, from);
-                at_first.tiles = __shfl_sync(0xFFFFFFFFu, grp.tiles, from);
-                at_first.blocks = __shfl_sync(0xFFFFFFFFu, grp.blocks, from);
-            });
-        }
         if (lane == 0) {
-            Walker walk;
-            walk.x = walk.x_begin = lo;
-            walk.x_end = hi;
-            walk.off = off;
-            walk.g = g_first;
-            walk.grp = at_first;
             bool ok = true, more = true;
             for (int i = 0; ok && more; ++i) {
                 more = walk.next(a, s);
@@ -490,6 +531,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 mbar_arrive(bar(kSegFull + i % kSegs));
             }
             if (!ok) give_up();
+            if (cta == 0) { a.base[a.G] = total; a.base[a.G + 1] = n_cta; a.base[a.G + 2] = bad; }
         }
     } else if (warp >= 4 && warp < 12) {
         // ---- softmax: thread = row of the tile's lanes --------------------------------------------------------
@@ -675,21 +717,25 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if (mine > kFlush) {                 // take back what the accumulator was emptied of
                     const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
 #pragma unroll 1
-                    for (int c = 0; c < kHeadDim; c += 16) {
-                        float4 old[4];
+                    for (int c = 0; c < kHeadDim; c += 64) {
+                        float4 old[16];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) old[i] = __ldcg(my_flush + (size_t)(c / 4 + i) * kRows);
-                        uint32_t q[16];
-                        tmem_ld16(to + c, q);
-                        tmem_wait_ld();
+                        for (int i = 0; i < 16; ++i) old[i] = __ldcg(my_flush + (size_t)(c / 4 + i) * kRows);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            q[4 * i] = __float_as_uint(fmaf(old[i].x, keep, __uint_as_float(q[4 * i])));
-                            q[4 * i + 1] = __float_as_uint(fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1])));
-                            q[4 * i + 2] = __float_as_uint(fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2])));
-                            q[4 * i + 3] = __float_as_uint(fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3])));
+                        for (int k = 0; k < 4; ++k) {
+                            uint32_t q[16];
+                            tmem_ld16(to + c + 16 * k, q);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float4 o = old[4 * k + i];
+                                q[4 * i] = __float_as_uint(fmaf(o.x, keep, __uint_as_float(q[4 * i])));
+                                q[4 * i + 1] = __float_as_uint(fmaf(o.y, keep, __uint_as_float(q[4 * i + 1])));
+                                q[4 * i + 2] = __float_as_uint(fmaf(o.z, keep, __uint_as_float(q[4 * i + 2])));
+                                q[4 * i + 3] = __float_as_uint(fmaf(o.w, keep, __uint_as_float(q[4 * i + 3])));
+                            }
+                            tmem_st16(to + c + 16 * k, q);
                         }
-                        tmem_st16(to + c, q);
                     }
                     tmem_wait_st();
                 }
@@ -919,9 +965,9 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
         my_len = clamp_len(a.seq_len, lane, a.T);
         my_base = a.base[lane];
     }
-    const long long total = a.base[a.G];
+    const long long total = a.base[a.G], n_cta = a.base[a.G + 1];
     const int row_begin = a.row_start[0], row_end = a.row_start[a.G];
-    const bool bad = a.base[a.G + 1] != 0;
+    const bool bad = a.base[a.G + 2] != 0;
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 32) {
         int st = 0;
         for (int c = threadIdx.x; c < grid; c += 32) st = max(st, a.cta_status[c]);
@@ -966,23 +1012,11 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
         const int tile = two ? in_blk / a.seqs : 0, in_tile = in_blk - tile * a.seqs, qr = in_tile / a.quarter;
         const int row = qr * 32 + (in_tile - qr * a.quarter) * a.Gq + in_head;
         const int lg_copies = copies(a, n_seq) >> 1;         // (two row tiles: one copy)
-        int c0 = 0, n_parts = 0, late = 0;
-        if (grp.tiles > 0) {
-            const long long n = min(total, (long long)grid);
-            const long long x0 = base_g + ((long long)hk * grp.blocks + blk) * grp.tiles, x1 = x0 + grp.tiles;
-            // the CTA whose range holds tile x is ceil((x + 1) * n / total) - 1; only the first of a unit's CTAs can
-            // have begun before the unit, and then used its second slot for it
-            int c1;
-            if (total < (1 << 24)) {                 // everything below 2^32
-                const uint32_t t = (uint32_t)total, k = (uint32_t)n;
-                c0 = (int)((((uint32_t)x0 + 1u) * k + t - 1u) / t) - 1;
-                c1 = (int)(((uint32_t)x1 * k + t - 1u) / t) - 1;
-                late = t * (uint32_t)c0 / k < (uint32_t)x0 ? 1 : 0;
-            } else {
-                c0 = (int)(((x0 + 1) * n + total - 1) / total - 1);
-                c1 = (int)((x1 * n + total - 1) / total - 1);
-                late = total * c0 / n < x0 ? 1 : 0;
-            }
+        int c0 = 0, n_parts = 0;
+        if (grp.tiles > 0) {                         // CTAs that the unit's first and last tile begin in
+            const long long x0 = base_g + ((long long)hk * grp.blocks + blk) * grp.tiles * grp.weight;
+            c0 = cta_of(total, x0, (int)n_cta);
+            const int c1 = cta_of(total, x0 + (long long)(grp.tiles - 1) * grp.weight, (int)n_cta);
             mine = c0 != c1;                         // a whole unit was finished where it was computed
             if (mine) n_parts = (c1 - c0 + 1) << lg_copies;
         }
@@ -994,7 +1028,7 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int e = min(e0 + SPLIT * i, n_parts - 1), c = e >> lg_copies, at = row + (e - (c << lg_copies)) * (kRows / 2);
-                const size_t slot = (2 * (size_t)(c0 + c) + (c == 0 ? late : 0)) * 2 + tile;
+                const size_t slot = (2 * (size_t)(c0 + c) + (c == 0 ? 1 : 0)) * 2 + tile;
                 p[i] = __ldcg(a.part_ml + slot * kRows + at);
                 v[i] = __ldcg(a.part_o + (slot * 32 + d4) * kRows + at);
             }
@@ -1056,7 +1090,7 @@ constexpr size_t kSlots = 3 * (size_t)kPlanSms * 2;          // first and last p
 }  // namespace
 
 size_t prefix_ws_bytes(const Geom& g, int) {
-    return 256 + align256(kPlanSms * 4) + align256(((size_t)g.B + 2) * 8) + kSlots * kRows * 8 + kSlots * kRows * kHeadDim * 4 +
+    return 256 + align256(kPlanSms * 4) + align256(((size_t)g.B + 3) * 8) + kSlots * kRows * 8 + kSlots * kRows * kHeadDim * 4 +
            2 * (size_t)kPlanSms * kRows * kHeadDim * 4;
 }
 
@@ -1074,7 +1108,7 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
     a.cta_status = reinterpret_cast<int32_t*>(w);
     w += align256(kPlanSms * 4);
     a.base = reinterpret_cast<long long*>(w);
-    w += align256(((size_t)g.B + 2) * 8);
+    w += align256(((size_t)g.B + 3) * 8);
     a.part_ml = reinterpret_cast<float2*>(w);
     w += kSlots * kRows * 8;
     a.part_o = reinterpret_cast<float4*>(w);
@@ -1084,6 +1118,7 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
     a.G = g.B; a.Hq = g.Hq; a.Hkv = g.Hkv; a.Gq = g.Gq; a.T = g.T; a.n_rows = n_rows;
     a.quarter = 32 / g.Gq;
     a.seqs = 4 * a.quarter;
+    a.q_box = 32 % g.Gq == 0 ? 2 : 1;
     a.sc = score ? *score : ScoreArgs{};
     a.scale_log2 = sm_scale * kLog2e;
     a.cap_in = a.sc.softcap > 0.f ? sm_scale / a.sc.softcap : 0.f;
@@ -1099,7 +1134,7 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
     {
         const cuuint64_t dims[3] = {kHeadDim, (cuuint64_t)g.Hq, (cuuint64_t)n_rows};
         const cuuint64_t strides[2] = {kRowBytes, (cuuint64_t)g.Hq * kRowBytes};
-        const cuuint32_t box[3] = {64, (cuuint32_t)g.Gq, (cuuint32_t)a.quarter}, step[3] = {1, 1, 1};
+        const cuuint32_t box[3] = {64, (cuuint32_t)g.Gq, (cuuint32_t)(a.q_box * a.quarter)}, step[3] = {1, 1, 1};
         if (enc(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides, box, step,
                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
