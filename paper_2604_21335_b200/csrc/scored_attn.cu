@@ -12,7 +12,8 @@
 // pages i, i + 4 C, ...  C is chosen so that the clusters fill the machine (plan below).  Each warp keeps its own
 // running maximum, sum and accumulator; the four of a CTA are joined in shared memory and the CTAs of a cluster through
 // each other's shared memory (distributed shared memory), each CTA finishing its share of the outputs: one launch,
-// nothing in global memory, no atomics, and the same order of additions every time.
+// nothing in global memory, no atomics, and the same order of additions every time.  Few problems with long lists (one
+// sequence that attends all of its cache) take several clusters each, whose results a second small kernel joins.
 //
 // Which pages a warp needs at all is settled before any copy: 32 listed pages at a time, one per lane, the lane
 // works out which of the page's 16 tokens the query sees (window and documents included) and drops the page from the
@@ -63,7 +64,9 @@ struct ScoredArgs {
     float* lse;
     int32_t* status;
     int64_t cap_groups;
-    int Hq, Hkv, Gq, T, max_pages, cluster;
+    float* part_o;               // splits > 1: [problems][splits][Gq][128] sums, as they stand
+    float2* part_ml;             // [problems][splits][Gq] maximum (log2 units) and sum
+    int Hq, Hkv, Gq, T, max_pages, cluster, splits;
     float scale_log2, cap_in, cap_log2;    // sm_scale log2(e); sm_scale / cap; cap log2(e)
     ScoreArgs sc;
 };
@@ -92,7 +95,9 @@ scored_attn_kernel(const ScoredArgs a) {
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int r = lane >> 2, c = lane & 3;
-    const int rank = (int)(blockIdx.x % (unsigned)a.cluster), problem = (int)(blockIdx.x / (unsigned)a.cluster);
+    const int rank = (int)(blockIdx.x % (unsigned)a.cluster), cluster_id = (int)(blockIdx.x / (unsigned)a.cluster);
+    const int problem = cluster_id / a.splits, split = cluster_id - problem * a.splits;
+    if (a.splits > 1) asm volatile("griddepcontrol.launch_dependents;");
     const int b = problem / a.Hkv, hk = problem - b * a.Hkv;
     const uint32_t ring = smem_u32(smem) + (uint32_t)warp * kStages * kStageBytes;
     const uint32_t zero_row = smem_u32(smem) + kRingBytes;
@@ -100,7 +105,7 @@ scored_attn_kernel(const ScoredArgs a) {
 
     // The reads the first window needs go out together: the page list does not wait for the lengths (a listed slot below
     // max_pages is readable whatever it holds).
-    const int W = a.cluster * kWarps, first_slot = rank * kWarps + warp;
+    const int W = a.splits * a.cluster * kWarps, first_slot = (split * a.cluster + rank) * kWarps + warp;
     const int32_t* const list = a.page_ids ? a.page_ids + (size_t)problem * a.max_pages : nullptr;
     const long long slot0 = first_slot + (long long)W * lane;
     int listed = list && slot0 < a.max_pages ? list[slot0] : -1;             // this lane's entry of the next window
@@ -464,6 +469,17 @@ scored_attn_kernel(const ScoredArgs a) {
         const float shift = a.sc.slopes ? a.sc.slopes[hk * a.Gq + h] * (float)(see_hi - 1 - pos) : 0.f;
         return l > 0.f ? (m + log2f(l)) * kLn2 + shift : -INFINITY;
     };
+    // channel d of head h is finished (or this cluster's part of it)
+    const size_t part_row = (size_t)cluster_id * a.Gq;
+    auto put = [&](int h, int d, float m, float l, float o) {
+        if (a.splits > 1) {
+            a.part_o[(part_row + h) * kHeadDim + d] = o;
+            if (d == 0) a.part_ml[part_row + h] = make_float2(m, l);
+        } else {
+            a.out[(row_base + h) * kHeadDim + d] = l > 0.f ? o / l : 0.f;
+            if (a.lse && d == 0) a.lse[row_base + h] = lse_of(h, m, l);
+        }
+    };
 #pragma unroll 1
     for (int h = 0; h < a.Gq; ++h) {             // thread = channel
         float2 p[kWarps];
@@ -477,8 +493,7 @@ scored_attn_kernel(const ScoredArgs a) {
             o = fmaf(ex[(w * HEADS + h) * kHeadStride + tid], f, o);
         }
         if (share == 1) {
-            a.out[(row_base + h) * kHeadDim + tid] = l > 0.f ? o / l : 0.f;
-            if (a.lse && tid == 0) a.lse[row_base + h] = lse_of(h, m, l);
+            put(h, tid, m, l, o);
         } else {
             cta[h * kHeadStride + tid] = o;
             if (tid == 0) { sh_m[h] = m; sh_l[h] = l; }
@@ -506,23 +521,70 @@ scored_attn_kernel(const ScoredArgs a) {
             l = fmaf(pl[k], f, l);
             o = fmaf(po[k], f, o);
         }
-        a.out[(row_base + h) * kHeadDim + d] = l > 0.f ? o / l : 0.f;
-        if (a.lse && d == 0) a.lse[row_base + h] = lse_of(h, m, l);
+        put(h, d, m, l, o);
     }
     cluster_sync();                              // no CTA leaves while another still reads its shared memory
 }
 
-// CTAs per problem.  A call takes waves x (pages of a warp + 3) page times: CTAs resident at once, and about
-// three page times to start, to fill the ring and to join.
-int cluster_size(int problems, int max_pages, int resident) {
-    int best = 1;
+// Joins the clusters of a problem: one warp per (problem, head), a lane four channels; lane = cluster for the weights.
+__global__ void __launch_bounds__(128)
+scored_join_kernel(const ScoredArgs a, int rows) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int task = (int)blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (task >= rows) return;
+    const int problem = task / a.Gq, h = task - problem * a.Gq, b = problem / a.Hkv, hk = problem - b * a.Hkv;
+    const size_t first = (size_t)problem * a.splits * a.Gq + h;
+    const float2 p = lane < a.splits ? a.part_ml[first + (size_t)lane * a.Gq] : make_float2(-INFINITY, 0.f);
+    float m = p.x;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+    const float f = p.x == -INFINITY ? 0.f : ex2(p.x - m);
+    float l = p.y * f;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, d);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int k = 0; k < a.splits; ++k) {
+        const float4 v = reinterpret_cast<const float4*>(a.part_o + (first + (size_t)k * a.Gq) * kHeadDim)[lane];
+        const float w = __shfl_sync(0xFFFFFFFFu, f, k);
+        o.x = fmaf(v.x, w, o.x); o.y = fmaf(v.y, w, o.y); o.z = fmaf(v.z, w, o.z); o.w = fmaf(v.w, w, o.w);
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const size_t row = (size_t)b * a.Hq + (size_t)hk * a.Gq + h;
+    reinterpret_cast<float4*>(a.out + row * kHeadDim)[lane] = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if (a.lse && lane == 0) {
+        float shift = 0.f;
+        if (a.sc.slopes) {
+            const int len = clamp_len(a.seq_len, b, a.T), pos = a.sc.q_pos ? a.sc.q_pos[b] : len - 1;
+            int lo, hi;
+            visible_range(len, pos, a.sc.window, lo, hi);
+            shift = a.sc.slopes[hk * a.Gq + h] * (float)(hi - 1 - pos);
+        }
+        a.lse[row] = l > 0.f ? (m + log2f(l)) * kLn2 + shift : -INFINITY;
+    }
+}
+
+// CTAs per cluster and clusters per problem.  A call takes waves x (pages of a warp + 3) page times: CTAs resident at
+// once, and about three page times to start, to fill the ring and to join; several clusters cost three more for the second
+// kernel and are looked at where a warp of the largest cluster would have 16 pages or more, up to as many as the
+// workspace has partial slots for.  (Single-head and 4-head problems of 2048 to 8192 pages: 20 to 84 us against 74 to
+// 290 with one cluster or the plain kernel's split.)
+void plan(int problems, int max_pages, int resident, int slots, int* cluster, int* splits) {
     double least = 0.0;
+    *splits = 1;
     for (int c = 1; c <= kMaxCluster; ++c) {
+        if (c == 5 || c == 7) continue;          // they pack badly into the machine's groups of SMs
         const double waves = (double)(((long long)problems * c + resident - 1) / resident);
         const double cost = waves * ((max_pages + kWarps * c - 1) / (kWarps * c) + 3.0);
-        if (c == 1 || cost < least) { least = cost; best = c; }
+        if (c == 1 || cost < least) { least = cost; *cluster = c; }
     }
-    return best;
+    if (max_pages < kWarps * kMaxCluster * 16) return;
+    for (int n = 2; n <= 32 && n <= slots && (long long)problems * n <= resident; ++n) {
+        const int room = resident / (problems * n);
+        const int c = room >= 8 ? 8 : room >= 4 ? 4 : room >= 2 ? 2 : 1;     // (seven CTAs to a cluster: 125 us where eight take 84)
+        const double cost = (max_pages + kWarps * c * n - 1) / (kWarps * c * n) + 6.0;
+        if (cost < least) { least = cost; *cluster = c; *splits = n; }
+    }
 }
 
 template <int S, bool MMA, int kStages, int kPerSm>
@@ -531,7 +593,7 @@ cudaError_t launch(const ScoredArgs& a, int problems, cudaStream_t st) {
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(kStages));
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(problems * a.cluster));
+    cfg.gridDim = dim3((unsigned)(problems * a.splits * a.cluster));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem_bytes(kStages);
     cfg.stream = st;
@@ -541,7 +603,19 @@ cudaError_t launch(const ScoredArgs& a, int problems, cudaStream_t st) {
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a);
+    e = cudaLaunchKernelEx(&cfg, kernel, a);
+    if (e != cudaSuccess || a.splits == 1) return e;
+    const int rows = problems * a.Gq;
+    cudaLaunchConfig_t join = {};
+    join.gridDim = dim3((unsigned)((rows + 3) / 4));
+    join.blockDim = dim3(128);
+    join.stream = st;
+    cudaLaunchAttribute early;                       // its blocks wait in place instead of behind a launch
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    join.attrs = &early;
+    join.numAttrs = 1;
+    return cudaLaunchKernelEx(&join, scored_join_kernel, a, rows);
 }
 
 }  // namespace
@@ -570,7 +644,9 @@ cudaError_t launch_scored_attn(const Geom& g, const void* k, const void* v_packe
     if (e != cudaSuccess) return e;
     // three CTAs per SM with two stages per warp: a page's arithmetic outlasts a copy, so twelve warps per SM beat eight with
     // three stages (8 sequences, 28 / 4 heads, 256 pages: 15.3 against 15.9 us)
-    a.cluster = cluster_size(g.problems, max_pages, sms * 3);
+    plan(g.problems, max_pages, sms * 3, attn_plan(g, max_pages).slots_cap, &a.cluster, &a.splits);
+    a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + 256);
+    a.part_o = reinterpret_cast<float*>(a.part_ml) + ((size_t)g.problems * a.splits * g.Gq * 2 + 63) / 64 * 64;
 #define STC_SCORED(S_) \
     case S_: return g.Gq > 1 ? launch<S_, true, 2, 3>(a, g.problems, st) : launch<S_, false, 2, 3>(a, g.problems, st);
     switch (g.S) {

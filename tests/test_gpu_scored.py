@@ -92,6 +92,12 @@ def test_many_problems_and_a_full_wave():
     run_case(6, 24, 24, 24, 260, 16, 5, [260] * 24, alibi=True, docs=2)
 
 
+@pytest.mark.parametrize("heads", [(1, 1), (8, 1), (6, 2)])
+def test_few_problems_with_long_lists_take_several_clusters(heads):
+    run_case(7, 1, *heads, 16 * 1300 + 5, 8, 4, [16 * 1300 + 5], alibi=True, softcap=40.0)
+    run_case(8, 2, *heads, 16 * 600, 16, 4, [16 * 600, 40], window=3000, docs=2)
+
+
 @pytest.mark.parametrize("heads", [(4, 4), (12, 2)])
 def test_positions_empty_rows_and_poison(heads):
     """Queries that see nothing, one token, the middle of the cache; NaN and infinities in everything unseen."""
