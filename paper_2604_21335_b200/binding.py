@@ -501,8 +501,11 @@ def decode_attn(shape: Shape, cache: Cache, q: torch.Tensor, page_ids: Optional[
     """score: capped / biased / windowed / per-document scores (stc_decode_attn_scored)."""
     max_pages = page_ids.shape[-1] if page_ids is not None else shape.n_pages
     if score is not None:
-        dev = _current_device()
-        score.check(shape, shape.batch)
+        dev, B, Hq, Hkv = _current_device(), shape.batch, shape.n_q_heads, shape.n_kv_heads
+        rows = (B, Hq, shape.head_dim)
+        _sizes(("q", "out", "lse", "page_ids", "n_pages"), q, rows, out, rows, lse, (B, Hq), page_ids, (B, Hkv, max_pages),
+               n_pages, (B, Hkv))
+        score.check(shape, B)
         lp, kp, vp, mp, op, slp, pop, tdp, qdp, qp, ip, np_, outp, lsep, wsp = _addresses(
             dev, "ibb**fiiibiiffu", _SCORED_NAMES, shape.seq_len, cache.k, cache.v_packed, cache.v_mask, cache.v_offs,
             score.slopes, score.q_pos, score.tok_doc, score.q_doc, q, page_ids, n_pages, out, lse, ws)

@@ -336,11 +336,12 @@ int32_t stc_route_new_pages(const stc_shape* shape, const stc_cache* cache, cons
 
 namespace {
 // Checked options of the scored calls; *plain = nothing is set and the call is the unscored one.
-int32_t score_args(const stc_score* score, ScoreArgs* out, bool* plain) {
+int32_t score_args(const stc_score* score, float sm_scale, ScoreArgs* out, bool* plain) {
     *out = ScoreArgs{};
     *plain = true;
     if (!score) return STC_OK;
     if (!(score->softcap >= 0.f) || !std::isfinite(score->softcap) || score->window < 0) return STC_ERR_INVALID_ARG;
+    if (score->softcap > 0.f && !std::isfinite(sm_scale / score->softcap)) return STC_ERR_INVALID_ARG;    // the kernels multiply by it
     if ((!score->tok_doc) != (!score->q_doc)) return STC_ERR_INVALID_ARG;
     out->softcap = score->softcap; out->window = score->window; out->slopes = score->slopes;
     out->q_pos = score->q_pos; out->tok_doc = score->tok_doc; out->q_doc = score->q_doc;
@@ -357,7 +358,7 @@ int32_t decode_attn(const stc_shape* shape, const stc_cache* cache, const void* 
     if (!cache || max_pages < 0 || !(sm_scale == sm_scale)) return STC_ERR_INVALID_ARG;
     ScoreArgs sc;
     bool plain;
-    rc = score_args(score, &sc, &plain);
+    rc = score_args(score, sm_scale, &sc, &plain);
     if (rc != STC_OK) return rc;
     if (g.problems == 0) return STC_OK;
     if (!q || !out) return STC_ERR_INVALID_ARG;
@@ -405,7 +406,7 @@ int32_t stc_prefix_attn(const stc_shape* shape, const stc_cache* cache, int32_t 
     if (!cache || n_rows < 0 || !(sm_scale == sm_scale)) return STC_ERR_INVALID_ARG;
     ScoreArgs sc;
     bool plain;
-    rc = score_args(score, &sc, &plain);
+    rc = score_args(score, sm_scale, &sc, &plain);
     if (rc != STC_OK) return rc;
     if ((sc.slopes || sc.window > 0) && !sc.q_pos) return STC_ERR_INVALID_ARG;    // no position to count from
     if ((int64_t)g.problems * g.T > 0x7FFFFFFFLL || (int64_t)n_rows * g.Hq > 0x7FFFFFFFLL) return STC_ERR_UNSUPPORTED;

@@ -93,6 +93,8 @@ def test_scored_attention_refusals(lib):
     assert call(Bd._Score(-1.0, 0)) == 1
     assert call(Bd._Score(float("nan"), 0)) == 1
     assert call(Bd._Score(0.0, -3)) == 1
+    assert call(Bd._Score(1e-40, 0)) == 1                              # sm_scale / softcap overflows
+    assert call(Bd._Score(1e-30, 0)) == 3
     assert call(Bd._Score(0.0, 0, None, None, fake, None)) == 1
     assert call(Bd._Score(0.0, 0, None, None, None, fake)) == 1
     assert call(Bd._Score(30.0, 64, fake, fake, fake, fake)) == 3      # reaches the workspace check
