@@ -93,7 +93,7 @@ typedef struct stc_cache {
 /* What stc_decode_attn_scored and stc_prefix_attn do to the scores besides sm_scale; zero / NULL
  * switches an option off. */
 typedef struct stc_score {
-    float softcap;             /* > 0: s becomes softcap * tanh(s / softcap)          */
+    float softcap;             /* > 0: s becomes softcap * tanh(s / softcap); sm_scale / softcap must be finite */
     int32_t window;            /* > 0: a query sees its window most recent tokens     */
     const float* slopes;       /* device f32 [Hq]: s += slopes[h] * (t - q_pos), after the cap */
     const int32_t* q_pos;      /* device i32, one per query row: position of the query,
@@ -416,7 +416,8 @@ int32_t stc_decode_attn(const stc_shape* shape, const stc_cache* cache, const vo
  *     x_t = sm_scale * q_h.k_t;   x_t = softcap * tanh(x_t / softcap) (if set);
  *     s_t = x_t + slopes[h] * (t - p) (if set)
  * and softmax, values and lse as in stc_decode_attn.  A head with no token left gives out = 0 and
- * lse = -inf.  Keys and values of tokens that are not seen are never used, whatever they hold.
+ * lse = -inf.  Keys and values of tokens that are not seen are never used, whatever they hold; a NaN score of a token
+ * that is seen makes the head's out and lse NaN.
  * score NULL or all off: the same kernels, hence the same bits, as stc_decode_attn.  tanh is good to
  * one fp32 unit.  Workspace, alignment and status word as in stc_decode_attn; page selection knows nothing
  * of a distance bias (a cap is monotone and changes no ranking within a head). */
@@ -438,8 +439,8 @@ int32_t stc_decode_attn_scored(const stc_shape* shape, const stc_cache* cache, c
  * sequence's own tokens) the two are joined:
  *     L = log(e^lse + e^own_lse),  out = e^{lse-L} out + e^{own_lse-L} own_out,  lse = L;
  * out and lse_opt must not overlap own_out and own_lse.  A side with lse = -inf contributes nothing, whatever its out holds; with
- * nothing on either side out = 0 and lse = -inf.  Keys of tokens that no row sees may hold anything; packed
- * values of all valid tokens must be finite.
+ * nothing on either side out = 0 and lse = -inf.  Keys of tokens that a row does not see may hold anything (a NaN score
+ * of one that it sees makes its out and lse NaN); packed values of all valid tokens must be finite.
  *   q          bf16 [n_rows][Hq][128]   one row per query token: several tokens of a sequence are several rows
  *   row_start  device i32 [batch+1], 0 <= row_start[g] <= row_start[g+1] <= n_rows; else nothing is written
  *              and the status word becomes STC_ERR_INVALID_ARG.  Rows before row_start[0] and from

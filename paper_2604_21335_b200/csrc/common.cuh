@@ -162,7 +162,7 @@ __device__ __forceinline__ float tanh_small(float z) {
 }
 __device__ __forceinline__ float tanh_large(float z) {
     const float e = exp2f(fabsf(z) * 2.885390081777927f);           // e^{2|z|}, +inf from |z| = 44 on
-    return copysignf(1.f - __fdividef(2.f, fminf(e, 1e30f) + 1.f), z);
+    return copysignf(1.f - __fdividef(2.f, (e > 1e30f ? 1e30f : e) + 1.f), z);           // (NaN stays NaN)
 }
 __device__ __forceinline__ float tanh_f32(float z) { return fabsf(z) <= kTanhSmall ? tanh_small(z) : tanh_large(z); }
 

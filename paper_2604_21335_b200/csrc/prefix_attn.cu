@@ -189,6 +189,8 @@ struct Walker {
 // for o and own, and the joined lse.  An empty side gets the factor 0 and is not to be multiplied.
 struct Join { float fo, fown, lse; };
 __device__ __forceinline__ Join join(float m, float l, float shift, bool has_own, float own_lse) {
+    const float nan = __int_as_float(0x7FFFFFFF);
+    if (l != l || (has_own && own_lse != own_lse)) return Join{nan, nan, nan};      // a NaN among the seen is an answer
     const float a2 = l > 0.f ? m + log2f(l) + shift * kLog2e : -INFINITY;
     const float b2 = has_own ? own_lse * kLog2e : -INFINITY;
     const float top = fmaxf(a2, b2);
@@ -1038,12 +1040,14 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
                 if (e0 + SPLIT * i >= n_parts) p[i].x = -INFINITY;
                 top = fmaxf(top, p[i].x);
             }
-            if (top == -INFINITY) continue;
             const float fm = m == -INFINITY ? 0.f : ex2(m - top);
             l *= fm; o.x *= fm; o.y *= fm; o.z *= fm; o.w *= fm;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (p[i].x == -INFINITY) continue;   // (its sums may never have been written)
+                if (p[i].x == -INFINITY) {           // (its sums may never have been written; a sum of weights is 0 or NaN)
+                    if (e0 + SPLIT * i < n_parts) l += p[i].y;
+                    continue;
+                }
                 const float f = ex2(p[i].x - top);
                 l = fmaf(p[i].y, f, l);
                 o.x = fmaf(v[i].x, f, o.x); o.y = fmaf(v[i].y, f, o.y); o.z = fmaf(v[i].z, f, o.z); o.w = fmaf(v[i].w, f, o.w);
@@ -1060,7 +1064,10 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
         for (int i = 1; i < SPLIT; ++i) {
             const float2 p = sh_ml[i][lane];
             const float4 v = sh_o[i][lane];
-            if (p.x == -INFINITY) continue;
+            if (p.x == -INFINITY) {
+                l += p.y;
+                continue;
+            }
             const float top = fmaxf(m, p.x), fm = m == -INFINITY ? 0.f : ex2(m - top), fp = ex2(p.x - top);
             l = fmaf(p.y, fp, l * fm);
             o.x = fmaf(v.x, fp, o.x * fm); o.y = fmaf(v.y, fp, o.y * fm);

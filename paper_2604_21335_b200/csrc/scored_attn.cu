@@ -82,6 +82,9 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr, int rank) {
     return v;
 }
 
+// What scores are weighed against: the running maximum, or 0 as long as all of them were -inf (a seen key may hold one).
+__device__ __forceinline__ float above(float m) { return m == -INFINITY ? 0.f : m; }
+
 template <int S, bool MMA, int kStages, int kPerSm>
 __global__ void __launch_bounds__(kThreads, kPerSm)
 scored_attn_kernel(const ScoredArgs a) {
@@ -277,13 +280,13 @@ scored_attn_kernel(const ScoredArgs a) {
                     pm0 = fmaxf(pm0, __shfl_xor_sync(0xFFFFFFFFu, pm0, d));
                     pm1 = fmaxf(pm1, __shfl_xor_sync(0xFFFFFFFFu, pm1, d));
                 }
-                const float mn0 = fmaxf(m_run[0], pm0), mn1 = fmaxf(m_run[1], pm1);   // finite: a token is seen
-                al0 = ex2(m_run[0] - mn0); al1 = ex2(m_run[1] - mn1);
+                const float mn0 = fmaxf(m_run[0], pm0), mn1 = fmaxf(m_run[1], pm1);
+                al0 = ex2(m_run[0] - above(mn0)); al1 = ex2(m_run[1] - above(mn1));
                 m_run[0] = mn0; m_run[1] = mn1;
                 moved = true;
             }
-            const float p0 = ex2(sv[0] - m_run[0]), p1 = ex2(sv[1] - m_run[1]);
-            const float p2 = ex2(sv[2] - m_run[0]), p3 = ex2(sv[3] - m_run[1]);
+            const float ref0 = above(m_run[0]), ref1 = above(m_run[1]);
+            const float p0 = ex2(sv[0] - ref0), p1 = ex2(sv[1] - ref1), p2 = ex2(sv[2] - ref0), p3 = ex2(sv[3] - ref1);
             l_run[0] = fmaf(l_run[0], al0, p0 + p2);
             l_run[1] = fmaf(l_run[1], al1, p1 + p3);
             if (moved) {
@@ -357,10 +360,10 @@ scored_attn_kernel(const ScoredArgs a) {
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) pm = fmaxf(pm, __shfl_xor_sync(0xFFFFFFFFu, pm, d));
                 const float mn = fmaxf(m_run[0], pm);
-                al = ex2(m_run[0] - mn);
+                al = ex2(m_run[0] - above(mn));
                 m_run[0] = mn;
             }
-            const float p0 = ex2(sd[0] - m_run[0]), p1 = ex2(sd[1] - m_run[0]);
+            const float ref = above(m_run[0]), p0 = ex2(sd[0] - ref), p1 = ex2(sd[1] - ref);
             l_run[0] = fmaf(l_run[0], al, p0 + p1);
             uint4 vr[2][4];
 #pragma unroll
@@ -467,7 +470,7 @@ scored_attn_kernel(const ScoredArgs a) {
     // what lse lacks: slope * (last visible token - position of the query)
     auto lse_of = [&](int h, float m, float l) {
         const float shift = a.sc.slopes ? a.sc.slopes[hk * a.Gq + h] * (float)(see_hi - 1 - pos) : 0.f;
-        return l > 0.f ? (m + log2f(l)) * kLn2 + shift : -INFINITY;
+        return l != 0.f ? (m + log2f(l)) * kLn2 + shift : -INFINITY;
     };
     // channel d of head h is finished (or this cluster's part of it)
     const size_t part_row = (size_t)cluster_id * a.Gq;
@@ -476,7 +479,7 @@ scored_attn_kernel(const ScoredArgs a) {
             a.part_o[(part_row + h) * kHeadDim + d] = o;
             if (d == 0) a.part_ml[part_row + h] = make_float2(m, l);
         } else {
-            a.out[(row_base + h) * kHeadDim + d] = l > 0.f ? o / l : 0.f;
+            a.out[(row_base + h) * kHeadDim + d] = l != 0.f ? o / l : 0.f;     // (a NaN among the seen is an answer)
             if (a.lse && d == 0) a.lse[row_base + h] = lse_of(h, m, l);
         }
     };
@@ -488,7 +491,7 @@ scored_attn_kernel(const ScoredArgs a) {
         for (int w = 0; w < kWarps; ++w) { p[w] = sh_ml[w][h]; m = fmaxf(m, p[w].x); }
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-            const float f = p[w].x == -INFINITY ? 0.f : ex2(p[w].x - m);
+            const float f = ex2(p[w].x - above(m));
             l = fmaf(p[w].y, f, l);
             o = fmaf(ex[(w * HEADS + h) * kHeadStride + tid], f, o);
         }
@@ -508,7 +511,7 @@ scored_attn_kernel(const ScoredArgs a) {
         float pm[kMaxCluster], pl[kMaxCluster], po[kMaxCluster], m = -INFINITY, l = 0.f, o = 0.f;
 #pragma unroll
         for (int k = 0; k < kMaxCluster; ++k) {
-            if (k >= share) { pm[k] = -INFINITY; continue; }
+            if (k >= share) { pm[k] = -INFINITY; pl[k] = po[k] = 0.f; continue; }
             pm[k] = ld_cluster(at_m + 4u * h, k);
             pl[k] = ld_cluster(at_l + 4u * h, k);
             po[k] = ld_cluster(at_o + 4u * (uint32_t)(h * kHeadStride + d), k);
@@ -516,8 +519,7 @@ scored_attn_kernel(const ScoredArgs a) {
         }
 #pragma unroll
         for (int k = 0; k < kMaxCluster; ++k) {
-            if (pm[k] == -INFINITY) continue;
-            const float f = ex2(pm[k] - m);
+            const float f = ex2(pm[k] - above(m));
             l = fmaf(pl[k], f, l);
             o = fmaf(po[k], f, o);
         }
@@ -538,7 +540,7 @@ scored_join_kernel(const ScoredArgs a, int rows) {
     float m = p.x;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-    const float f = p.x == -INFINITY ? 0.f : ex2(p.x - m);
+    const float f = ex2(p.x - above(m));
     float l = p.y * f;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, d);
@@ -549,7 +551,7 @@ scored_join_kernel(const ScoredArgs a, int rows) {
         const float w = __shfl_sync(0xFFFFFFFFu, f, k);
         o.x = fmaf(v.x, w, o.x); o.y = fmaf(v.y, w, o.y); o.z = fmaf(v.z, w, o.z); o.w = fmaf(v.w, w, o.w);
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l != 0.f ? 1.f / l : 0.f;
     const size_t row = (size_t)b * a.Hq + (size_t)hk * a.Gq + h;
     reinterpret_cast<float4*>(a.out + row * kHeadDim)[lane] = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
     if (a.lse && lane == 0) {
@@ -560,7 +562,7 @@ scored_join_kernel(const ScoredArgs a, int rows) {
             visible_range(len, pos, a.sc.window, lo, hi);
             shift = a.sc.slopes[hk * a.Gq + h] * (float)(hi - 1 - pos);
         }
-        a.lse[row] = l > 0.f ? (m + log2f(l)) * kLn2 + shift : -INFINITY;
+        a.lse[row] = l != 0.f ? (m + log2f(l)) * kLn2 + shift : -INFINITY;
     }
 }
 
