@@ -272,12 +272,12 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         first_len = clamp_len(a.seq_len, lane, a.T);
     }
     if (warp == 0 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &map_k : &map_q) : "memory");
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < kBars; ++i)
-            mbar_init(bars + 8 * i, i >= kPFull && i < kOFull ? kRows : i == kXchg ? 2 * kRows : i >= kVFull && i < kVEmpty ? 2 : i >= kSegEmpty ? kSegReaders : 1);
-        *abort_flag = (base & 1023u) != 0 ? (int)STC_ERR_CUDA : 0;      // swizzled tiles need 1024-byte aligned bases
+    if (threadIdx.x >= 128 && threadIdx.x < 128 + kBars) {       // one barrier per thread
+        const int i = (int)threadIdx.x - 128;
+        mbar_init(bars + 8 * i, i >= kPFull && i < kOFull ? kRows : i == kXchg ? 2 * kRows : i >= kVFull && i < kVEmpty ? 2 : i >= kSegEmpty ? kSegReaders : 1);
         fence_mbar_init();
     }
+    if (threadIdx.x == 128) *abort_flag = (base & 1023u) != 0 ? (int)STC_ERR_CUDA : 0;      // swizzled tiles need 1024-byte aligned bases
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      ::"r"(bars + kCtlTmem), "r"(512u) : "memory");
