@@ -956,32 +956,23 @@ __global__ void __launch_bounds__(256)
 prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
     __shared__ float4 sh_o[SPLIT][32];
     __shared__ float2 sh_ml[SPLIT][32];
-    asm volatile("griddepcontrol.wait;" ::: "memory");       // launched while the first kernel still runs
+    // Launched while the first kernel still runs: what the call was given is read before the wait (what came before the
+    // first kernel is complete), the first kernel's results after it.
     const int lane = threadIdx.x & 31;
-    // everything that finds a row's unit in one round of loads: lane = prefix (more than 32: searched below)
+    // lane = prefix (more than 32: searched below)
     const bool few = a.G <= 32;
     int my_r0 = 0x7FFFFFFF, my_r1 = 0, my_len = 0;
-    long long my_base = 0;
     if (few && lane < a.G) {
         my_r0 = a.row_start[lane];
         my_r1 = a.row_start[lane + 1];
         my_len = clamp_len(a.seq_len, lane, a.T);
-        my_base = a.base[lane];
     }
-    const long long total = a.base[a.G], n_cta = a.base[a.G + 1];
     const int row_begin = a.row_start[0], row_end = a.row_start[a.G];
-    const bool bad = a.base[a.G + 2] != 0;
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 32) {
-        int st = 0;
-        for (int c = threadIdx.x; c < grid; c += 32) st = max(st, a.cta_status[c]);
-        st = __reduce_max_sync(0xFFFFFFFFu, st);
-        if (threadIdx.x == 0) *a.status = bad ? (int)STC_ERR_INVALID_ARG : st;
-    }
     const int hk = blockIdx.x / chunks, warp = threadIdx.x >> 5, part = SPLIT == 1 ? 0 : warp;
     const uint32_t flat = (uint32_t)(blockIdx.x - hk * chunks) * 8u + (uint32_t)(lane >> 2);     // below 2^31 + 8
     const int d4 = (SPLIT == 1 ? warp : (int)blockIdx.y) * 4 + (lane & 3);
     const int seq = (int)(flat / (uint32_t)a.Gq), in_head = (int)(flat - (uint32_t)seq * (uint32_t)a.Gq), head = hk * a.Gq + in_head;
-    bool mine = !bad && seq < a.n_rows && seq >= row_begin && seq < row_end;
+    bool mine = seq < a.n_rows && seq >= row_begin && seq < row_end;
     float m = -INFINITY, l = 0.f, shift = 0.f, own_l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f), own = o;
     const size_t out_row = (size_t)seq * a.Hq + head;
@@ -989,15 +980,13 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
         own_l = a.own_lse[out_row];
         own = reinterpret_cast<const float4*>(a.own_out + out_row * kHeadDim)[d4];
     }
-    // last prefix that starts at or before the row
+    // last prefix that starts at or before the row (row_start that does not fit gives some prefix, and nothing is written)
     int g = 0;
     Group grp = {};
-    long long base_g = 0;
     if (few) {
         for (int i = 1; i < a.G; ++i)
             if (__shfl_sync(0xFFFFFFFFu, my_r0, i) <= seq) g = i;
         grp = make_group(a, __shfl_sync(0xFFFFFFFFu, my_r0, g), __shfl_sync(0xFFFFFFFFu, my_r1, g), __shfl_sync(0xFFFFFFFFu, my_len, g));
-        base_g = __shfl_sync(0xFFFFFFFFu, my_base, g);
     } else if (mine) {
         int g_hi = a.G;
         while (g_hi - g > 1) {
@@ -1005,8 +994,18 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
             if (a.row_start[mid] <= seq) g = mid; else g_hi = mid;
         }
         grp = load_group(a, g);
-        base_g = a.base[g];
     }
+    if (mine) shift = bias_shift(a, grp.len, seq, head);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const long long base_g = a.base[g], total = a.base[a.G], n_cta = a.base[a.G + 1];
+    const bool bad = a.base[a.G + 2] != 0;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 32) {
+        int st = 0;
+        for (int c = threadIdx.x; c < grid; c += 32) st = max(st, a.cta_status[c]);
+        st = __reduce_max_sync(0xFFFFFFFFu, st);
+        if (threadIdx.x == 0) *a.status = bad ? (int)STC_ERR_INVALID_ARG : st;
+    }
+    if (bad) mine = false;
     if (mine) {
         const int in_group = seq - grp.row0, blk = in_group / (2 * a.seqs), in_blk = in_group - blk * 2 * a.seqs;
         const int n_seq = min(2 * a.seqs, grp.n_seq - blk * 2 * a.seqs);
@@ -1023,7 +1022,6 @@ prefix_merge_kernel(const PrefixArgs a, int grid, int chunks) {
             mine = c0 != c1;                         // a whole unit was finished where it was computed
             if (mine) n_parts = (c1 - c0 + 1) << lg_copies;
         }
-        if (mine) shift = bias_shift(a, grp.len, seq, head);
 #pragma unroll 1
         for (int e0 = part; e0 < n_parts; e0 += 8 * SPLIT) {
             float2 p[8];
