@@ -250,7 +250,7 @@ cudaError_t launch_scored_attn(const Geom& g, const void* k, const void* v_packe
                                const int32_t* n_pages, int max_pages, float sm_scale, const ScoreArgs& score, float* out,
                                float* lse, void* ws, cudaStream_t st);
 
-size_t prefix_ws_bytes(const Geom& g, int n_rows);
+size_t prefix_ws_bytes(const Geom& g);
 cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packed, const uint16_t* v_mask,
                                const uint32_t* v_offs, int64_t cap_groups, int n_rows, const void* q,
                                const int32_t* row_start, float sm_scale, const ScoreArgs* score, const float* own_out,

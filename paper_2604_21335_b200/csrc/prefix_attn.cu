@@ -16,9 +16,13 @@
 // 4e-8 of its value per product), so an accumulator is emptied into fp32 sums after kFlush tiles.
 //
 // What bounds it.  Up to 128 rows per KV head the two products of 128 tokens take about 1800 cycles of the tensor pipe
-// and their bytes (K 32 KiB, V up to 32 KiB) 2100 to 2800 cycles of an SM's share of HBM: memory-bound; at 256 rows
-// the pipe and the softmax bind, so a work unit is at most two row tiles (one pass over K and V for 256
-// rows) and larger batches take more units, whose K and V come from L2.
+// and their bytes (K 32 KiB, V up to 32 KiB) 2100 to 2800 cycles of an SM's share of HBM; the loop product -> softmax ->
+// product of a group takes about 3000 for its 64 of them, so a long prefix runs at 0.55 of the copy rate (131072 tokens, 16 x
+// 32/8 heads: 110 us for 405 MB).  Halving the softmax's work or the second product alone gains 5 % each, halving the value
+// warps' 1 %: it is the chain, not one of its links.  At 256 rows the tensor pipe is busy 0.8 of the time, so a work unit is at most
+// two row tiles (one pass over K and V for 256 rows) and larger batches take more units, whose K and V come from L2
+// (32768 tokens, 128 x 32/8 heads: 103 us for 69 GFLOP).  A short call pays 4.5 us to its first scores, 2 us for a segment's end
+// and 4 us for the second kernel (272 tokens, 8 x 32 heads: 14.4 us).
 //
 // Work split.  Unit = (prefix, KV head, block of up to two row tiles); the token tiles of all units form one flat
 // sequence, each as long as it takes (2, 3 or 4 for a tile whose softmax has 32 scores per thread, 64, or 64 in both
@@ -163,7 +167,7 @@ struct Walker {
                 off -= group_length(a, grp);
                 grp = load_group(a, ++g);
             }
-            const int length = grp.tiles * grp.weight;                     // of a unit (below 2^25)
+            const int length = grp.tiles * grp.weight;                     // of a unit (below 2^27)
             const long long unit = div_small(off, length);
             const int from = (int)(off - unit * length), to = (int)min((long long)length, from + (x_end - x));
             x += to - from;
@@ -1095,7 +1099,7 @@ constexpr size_t kSlots = 3 * (size_t)kPlanSms * 2;          // first and last p
 
 }  // namespace
 
-size_t prefix_ws_bytes(const Geom& g, int) {
+size_t prefix_ws_bytes(const Geom& g) {
     return 256 + align256(kPlanSms * 4) + align256(((size_t)g.B + 3) * 8) + kSlots * kRows * 8 + kSlots * kRows * kHeadDim * 4 +
            2 * (size_t)kPlanSms * kRows * kHeadDim * 4;
 }

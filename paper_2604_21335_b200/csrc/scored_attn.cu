@@ -4,7 +4,8 @@
 //     x_t = sm_scale q_h.k_t,   x_t <- cap tanh(x_t / cap),   s_t = x_t + slope_h (t - p),
 //     out = softmax(s) V~ (dropped value groups add zero),   lse = log sum exp s.
 //
-// What bounds it.  HBM for large calls (256 bytes of key and the kept groups per token); the chain of dependent steps
+// What bounds it.  HBM for large calls (256 bytes of key and the kept groups per token; 8 x 28/4 heads, 256 pages of 16 groups:
+// 15 us, of which 5.5 are the start and the join and the rest runs at 0.7 of the copy rate); the chain of dependent steps
 // for small ones: a decode step of one sequence moves a few MB, half a microsecond's worth, and what counts is how few
 // round trips stand between the launch and the result.
 //
@@ -645,7 +646,8 @@ cudaError_t launch_scored_attn(const Geom& g, const void* k, const void* v_packe
     cudaError_t e = device_sm_count(&sms);
     if (e != cudaSuccess) return e;
     // three CTAs per SM with two stages per warp: a page's arithmetic outlasts a copy, so twelve warps per SM beat eight with
-    // three stages (8 sequences, 28 / 4 heads, 256 pages: 15.3 against 15.9 us)
+    // three stages (8 sequences, 28 / 4 heads, 256 pages: 15.3 against 15.9 us); six or twelve warps per CTA take 14.4 us there,
+    // but 5.9 and 6.3 instead of 5.6 for one sequence of 8 heads, and clusters of 9 to 16 CTAs 16.8 to 27 us
     plan(g.problems, max_pages, sms * 3, attn_plan(g, max_pages).slots_cap, &a.cluster, &a.splits);
     a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + 256);
     a.part_o = reinterpret_cast<float*>(a.part_ml) + ((size_t)g.problems * a.splits * g.Gq * 2 + 63) / 64 * 64;

@@ -77,7 +77,7 @@ int32_t stc_workspace_bytes(const stc_shape* shape, int32_t op, int64_t arg, siz
     if (!bytes_host) return STC_ERR_INVALID_ARG;
     if (op == STC_OP_PREFIX_ATTN) {                 // rows have outputs even where the prefixes have no tokens
         if (arg < 0 || arg > 0x7FFFFFFF) return STC_ERR_INVALID_ARG;
-        *bytes_host = g.problems == 0 || arg == 0 ? 0 : prefix_ws_bytes(g, (int)arg);
+        *bytes_host = g.problems == 0 || arg == 0 ? 0 : prefix_ws_bytes(g);
         return STC_OK;
     }
     if (empty(g)) { *bytes_host = 0; return STC_OK; }
@@ -416,7 +416,7 @@ int32_t stc_prefix_attn(const stc_shape* shape, const stc_cache* cache, int32_t 
     if (g.T > 0 && (!cache->k || !cache->v_packed || !cache->v_mask || !cache->v_offs || cache->cap_groups < 0))
         return STC_ERR_INVALID_ARG;
     if (!aligned16(cache->k, cache->v_packed, q, own_out, out)) return STC_ERR_INVALID_ARG;
-    rc = check_ws(ws, ws_bytes, prefix_ws_bytes(g, n_rows));
+    rc = check_ws(ws, ws_bytes, prefix_ws_bytes(g));
     if (rc != STC_OK) return rc;
     return cuda_rc(launch_prefix_attn(g, cache->k, cache->v_packed, cache->v_mask, cache->v_offs, cache->cap_groups,
                                       n_rows, q, row_start, sm_scale, plain ? nullptr : &sc, own_out, own_lse, out,
