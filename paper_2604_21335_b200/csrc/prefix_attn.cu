@@ -61,8 +61,13 @@ constexpr int kRows = 128;                        // rows per tile = tensor-memo
 constexpr int kTok = 64;                          // tokens per tile
 constexpr int kThreads = 512;
 constexpr int kKStages = 6, kVStages = 4;
-constexpr int kFlush = 32;                        // tiles an accumulator takes: 256 products, 5e-6 of truncation (16 halve it and
-                                                  // cost a 32768-token, 128-sequence call a tenth of its time)
+// Tiles an accumulator takes before it is emptied, eight products each.  A product truncates the accumulator by 4e-8, so 32 tiles
+// leave up to 5e-6 of it and 16 half of that.  With one row tile a group sees every other tile and the weights' own error (2^-18
+// each, 1.2e-6 to 2e-6 of a result) is the larger part; emptying every 16 would cost 7 % there.  With two row tiles accumulators
+// see twice the tiles: 16 cost 7 % (32768 tokens, 128 sequences of 32/8 heads: 103 -> 111 us) and leave 3.2e-6 instead of 4.9e-6,
+// the plain fp32 form 2.3e-6.
+constexpr int kFlush = 32, kFlushTwo = 16;
+__device__ __forceinline__ bool empties(int n, bool two) { return n > 0 && (two ? n % kFlushTwo : n % kFlush) == 0; }
 constexpr int kSegs = 8;                          // segments the scheduler may be ahead
 constexpr uint32_t kQHalf = kRows * 128;          // 64 channels of a row tile: 128 rows of 128 bytes
 constexpr uint32_t kQTile = 2 * kQHalf;           // 32 KiB
@@ -411,7 +416,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     tc_after();
                     const uint64_t dv = smem_desc_128(sm + kOffV + st * kTile, kHalf);
                     const uint32_t p = ts + buf * 64u;
-                    const uint32_t more = (n - 2) % kFlush != 0;          // else O starts anew
+                    const uint32_t more = n > 2 && !empties(n - 2, two);  // else O starts anew
                     if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {        // 16 tokens: 16 rows of 128 bytes; P: 8 columns high, 8 residual
@@ -580,6 +585,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     }
                 }
             };
+            const int first_flush = two ? kFlushTwo : kFlush;
             float m = -INFINITY, l = 0.f, m_flush = -INFINITY;
 #pragma unroll 1
             for (int n = 0; n < mine; ++n) {
@@ -591,37 +597,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     ++n_s;
                     continue;
                 }
-                // After kFlush tiles the accumulator is emptied into fp32 sums (with the maximum it was built with), and
-                // the issuer starts it anew
-                const bool empty_now = n > 0 && n % kFlush == 0;
-                if (empty_now) {
-                    ok = warp_wait(kOFull + 2 * w + ((n_s - 1) & 1u), (n_s - 1) >> 1);
-                    if (!ok) return;
-                    tc_after();
-                    const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
-                    const bool grow = n > kFlush && __all_sync(0xFFFFFFFFu, keep == 1.f);   // nothing to read back
-#pragma unroll 1
-                    for (int c = 0; c < kHeadDim; c += 32) {
-                        float4 old[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            old[i] = n > kFlush && !grow ? __ldcg(my_flush + (size_t)(c / 4 + i) * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
-                        uint32_t q[32];
-                        tmem_ld16<0>(to + c, q);
-                        tmem_ld16<16>(to + c + 16, q);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            float4* dst = my_flush + (size_t)(c / 4 + i) * kRows;
-                            const float4 v = make_float4(
-                                fmaf(old[i].x, keep, __uint_as_float(q[4 * i])), fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1])),
-                                fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2])), fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3])));
-                            if (grow) red_add4(dst, v.x, v.y, v.z, v.w);
-                            else __stcg(dst, v);
-                        }
-                    }
-                    m_flush = m;
-                }
+                const bool empty_now = empties(n, two);
+                const float m_acc = m;               // maximum the accumulator was built with
                 ok = warp_wait(kSFull + 2 * w + buf, n_s >> 1);
                 if (!ok) return;
                 tc_after();
@@ -708,6 +685,36 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     for (int c = 0; c < kTok - COLS; c += 16) tmem_st16(ts + ((c0 + COLS + c) & (kTok - 1)), zero);
                 }
                 l += (la.x + lb.x) + (la.y + lb.y);
+                // After kFlush tiles the accumulator is emptied into fp32 sums and the issuer starts it anew.  Here the product it
+                // waits for is long through, and the product of the next scores runs meanwhile.
+                if (empty_now) {
+                    ok = warp_wait(kOFull + 2 * w + ((n_s - 1) & 1u), (n_s - 1) >> 1);
+                    if (!ok) return;
+                    tc_after();
+                    const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m_acc);
+                    const bool grow = n > first_flush && __all_sync(0xFFFFFFFFu, keep == 1.f);   // nothing to read back
+#pragma unroll 1
+                    for (int c = 0; c < kHeadDim; c += 32) {
+                        float4 old[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            old[i] = n > first_flush && !grow ? __ldcg(my_flush + (size_t)(c / 4 + i) * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
+                        uint32_t q[32];
+                        tmem_ld16<0>(to + c, q);
+                        tmem_ld16<16>(to + c + 16, q);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            float4* dst = my_flush + (size_t)(c / 4 + i) * kRows;
+                            const float4 v = make_float4(
+                                fmaf(old[i].x, keep, __uint_as_float(q[4 * i])), fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1])),
+                                fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2])), fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3])));
+                            if (grow) red_add4(dst, v.x, v.y, v.z, v.w);
+                            else __stcg(dst, v);
+                        }
+                    }
+                    m_flush = m_acc;
+                }
                 tmem_wait_st();
                 tc_before();
                 mbar_arrive(bar(kPFull + 2 * w + buf));
@@ -721,7 +728,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 ok = warp_wait(kOFull + 2 * w + ((n_s - 1) & 1u), (n_s - 1) >> 1);
                 if (!ok) return;
                 tc_after();
-                if (mine > kFlush) {                 // take back what the accumulator was emptied of
+                if (mine > first_flush) {                 // take back what the accumulator was emptied of
                     const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
 #pragma unroll 1
                     for (int c = 0; c < kHeadDim; c += 64) {
