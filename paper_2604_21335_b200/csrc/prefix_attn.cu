@@ -12,16 +12,16 @@
 //   O[row][dim]  += P . V~      P from tensor memory, written over S by the softmax; V~ rebuilt from the packed
 //                               groups in shared memory, token rows of 128 dims = N-major operand
 // P enters as a bf16 high part plus a bf16 residual (two MMAs): the output is fp32, and one bf16 weight alone would
-// leave it 2^-9 off; the pair leaves 2^-17.  The tensor core truncates when it adds to an accumulator (measured:
-// 4e-8 of its value per product), so an accumulator is emptied into fp32 sums after kFlush tiles.
+// leave it 2^-8 off; the pair leaves 2^-16.  The tensor core truncates when it adds to an accumulator (measured:
+// 4e-8 of its value per product), so an accumulator is emptied into fp32 sums now and then (kFlush).
 //
 // What bounds it.  Up to 128 rows per KV head the two products of 128 tokens take about 1800 cycles of the tensor pipe
 // and their bytes (K 32 KiB, V up to 32 KiB) 2100 to 2800 cycles of an SM's share of HBM; the loop product -> softmax ->
 // product of a group takes about 3000 for its 64 of them, so a long prefix runs at 0.55 of the copy rate (131072 tokens, 16 x
-// 32/8 heads: 110 us for 405 MB).  Halving the softmax's work or the second product alone gains 5 % each, halving the value
+// 32/8 heads: 107 us for 405 MB).  Halving the softmax's work or the second product alone gains 5 % each, halving the value
 // warps' 1 %: it is the chain, not one of its links.  At 256 rows the tensor pipe is busy 0.8 of the time, so a work unit is at most
 // two row tiles (one pass over K and V for 256 rows) and larger batches take more units, whose K and V come from L2
-// (32768 tokens, 128 x 32/8 heads: 103 us for 69 GFLOP).  A short call pays 4.5 us to its first scores, 2 us for a segment's end
+// (32768 tokens, 128 x 32/8 heads: 112 us for 69 GFLOP).  A short call pays 4.5 us to its first scores, 2 us for a segment's end
 // and 4 us for the second kernel (272 tokens, 8 x 32 heads: 14.4 us).
 //
 // Work split.  Unit = (prefix, KV head, block of up to two row tiles); the token tiles of all units form one flat
@@ -62,8 +62,8 @@ constexpr int kTok = 64;                          // tokens per tile
 constexpr int kThreads = 512;
 constexpr int kKStages = 6, kVStages = 4;
 // Tiles an accumulator takes before it is emptied, eight products each.  A product truncates the accumulator by 4e-8, so 32 tiles
-// leave up to 5e-6 of it and 16 half of that.  With one row tile a group sees every other tile and the weights' own error (2^-18
-// each, 1.2e-6 to 2e-6 of a result) is the larger part; emptying every 16 would cost 7 % there.  With two row tiles accumulators
+// leave up to 5e-6 of it and 16 half of that.  With one row tile a group sees every other tile and the weights' own error (up to
+// 2^-16 each, 1.2e-6 to 2e-6 of a result) is the larger part; emptying every 16 would cost 7 % there.  With two row tiles accumulators
 // see twice the tiles: 16 cost 7 % (32768 tokens, 128 sequences of 32/8 heads: 103 -> 111 us) and leave 3.2e-6 instead of 4.9e-6,
 // the plain fp32 form 2.3e-6.
 constexpr int kFlush = 32, kFlushTwo = 16;
@@ -685,7 +685,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     for (int c = 0; c < kTok - COLS; c += 16) tmem_st16(ts + ((c0 + COLS + c) & (kTok - 1)), zero);
                 }
                 l += (la.x + lb.x) + (la.y + lb.y);
-                // After kFlush tiles the accumulator is emptied into fp32 sums and the issuer starts it anew.  Here the product it
+                // The accumulator is emptied into fp32 sums and the issuer starts it anew.  Here the product it
                 // waits for is long through, and the product of the next scores runs meanwhile.
                 if (empty_now) {
                     ok = warp_wait(kOFull + 2 * w + ((n_s - 1) & 1u), (n_s - 1) >> 1);

@@ -22,7 +22,7 @@
 // on the warp's own mbarriers.  Values of tokens that are not seen are never used, whatever they hold.
 //
 // Arithmetic as in the plain decode attention: several query heads per KV head on mma.sync tiles (16 tokens x 8 heads,
-// softmax weights as a bf16 pair), a single head on the fp32 pipes.  The options are a handful of fp32 operations
+// softmax weights as three bf16 parts), a single head on the fp32 pipes.  The options are a handful of fp32 operations
 // on at most four scores per lane and page.  The bias is taken against the last visible token instead of the query, which
 // cancels in the softmax and keeps it small for the tokens that count even if the query stands far behind them;
 // lse gets the difference back.
