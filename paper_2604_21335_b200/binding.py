@@ -509,6 +509,8 @@ def decode_attn(shape: Shape, cache: Cache, q: torch.Tensor, page_ids: Optional[
         lp, kp, vp, mp, op, slp, pop, tdp, qdp, qp, ip, np_, outp, lsep, wsp = _addresses(
             dev, "ibb**fiiibiiffu", _SCORED_NAMES, shape.seq_len, cache.k, cache.v_packed, cache.v_mask, cache.v_offs,
             score.slopes, score.q_pos, score.tok_doc, score.q_doc, q, page_ids, n_pages, out, lse, ws)
+        if page_ids is not None and not ip:                # lists of no pages have no address, but are not "all pages"
+            ip = np_
         rc = load_library().stc_decode_attn_scored(
             _PACK_SHAPE(shape.batch, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.page_size, shape.n_groups,
                         shape.t_cap, 0, lp),

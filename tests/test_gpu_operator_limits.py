@@ -204,6 +204,19 @@ def test_calls_on_two_streams_at_once():
         assert all(torch.equal(s[name], alone[name]) for name in ("own", "lse", "out"))
 
 
+@pytest.mark.parametrize("heads", [(8, 8), (8, 2)])
+def test_scored_lists_without_pages_attend_nothing(heads):
+    c, q = setup(8, [64, 30], 64, *heads, 2)
+    shape, cache = on_device(c, [64, 30], 64, *heads)
+    out, lse = torch.ones(2, heads[0], 128, device="cuda"), torch.ones(2, heads[0], device="cuda")
+    for pages in (0, 3):
+        ids = torch.zeros(2, heads[1], pages, dtype=torch.int32, device="cuda")
+        n = torch.zeros(2, heads[1], dtype=torch.int32, device="cuda")
+        P.decode_attn(shape, cache, q.cuda(), ids, n, SCALE, out.fill_(1), Bd.new_workspace(shape, Bd.OP_DECODE_ATTN, pages),
+                      lse=lse.fill_(1), score=P.Score(softcap=5.0))
+        assert (out == 0).all() and (lse == -math.inf).all()
+
+
 def test_scored_sizes_that_do_not_fit_are_refused():
     c, q = setup(7, [64], 64, 8, 8, 1)
     shape, cache = on_device(c, [64], 64, 8, 8)
