@@ -134,7 +134,7 @@ def test_prefixes_of_all_kinds_side_by_side():
     """Empty prefixes, prefixes nobody continues, rows outside, tiny next to long, more units than CTAs."""
     run_case(7, [300, 0, 17, 1, 700, 128], 700, [2, 5, 9, 9, 40, 41, 60], 66, 8, 4)
     n = 40
-    run_case(8, [(37 * i) % 150 for i in range(n)], 150, [i * 2 for i in range(n + 1)], 2 * n, 24, 8)
+    run_case(8, [(37 * i) % 150 for i in range(n)], 150, [i * 2 for i in range(n + 1)], 2 * n, 21, 7)
 
 
 def test_long_prefix_on_all_ctas_one_unit():

@@ -62,7 +62,7 @@ def test_every_cta_shape_and_ragged_lengths(n, B):
 
 
 def test_nothing_new_and_lengths_that_do_not_fit():
-    run_case(5, 8, 8, 4, 64, 128, True, [0, 4, 5, 2, 1], [10, 60, 3, -1, 63])
+    run_case(5, 8, 4, 4, 64, 128, True, [0, 4, 5, 2, 1], [10, 60, 3, -1, 63])
 
 
 @pytest.mark.parametrize("first", [131072 - 8, (1 << 20) - 8, (1 << 24) + 1, 2**31 - 8, -5])

@@ -89,7 +89,7 @@ def test_lengths_and_page_lists(S, T, pages):
 
 def test_many_problems_and_a_full_wave():
     run_case(5, 16, 32, 8, 700, 8, 3, [700 - 31 * i for i in range(16)], softcap=50.0, window=300)
-    run_case(6, 24, 24, 24, 260, 16, 5, [260] * 24, alibi=True, docs=2)
+    run_case(6, 24, 20, 20, 260, 16, 5, [260] * 24, alibi=True, docs=2)
 
 
 @pytest.mark.parametrize("heads", [(1, 1), (8, 1), (6, 2)])
