@@ -612,7 +612,8 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 tmem_wait_ld();
                 // scores in log2 units where they are not the raw products times a positive scale
-                if constexpr (CAP) cap_scores(r, magnitude(r), a.cap_in, a.cap_log2, a.scale_log2);
+                // (lanes without a row hold whatever was in shared memory: they have no vote)
+                if constexpr (CAP) cap_scores(r, live ? magnitude(r) : 0.f, a.cap_in, a.cap_log2, a.scale_log2);
                 if constexpr (BIAS) {
                     const float far = (float)(t0 - (hi - 1));
 #pragma unroll

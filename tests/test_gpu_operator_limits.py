@@ -116,6 +116,24 @@ def test_prefix_nan_in_a_seen_key_and_in_a_query(rows, T, cap):
         assert a[~keep].isnan().all() and torch.equal(a[keep], b[keep])
 
 
+@pytest.mark.parametrize("heads", [(28, 4), (12, 2), (8, 1)])
+@pytest.mark.parametrize("options", [dict(), dict(softcap=30.0), dict(softcap=30.0, slopes=True)], ids=lambda o: "+".join(o) or "plain")
+def test_prefix_bits_do_not_depend_on_what_ran_before(heads, options):
+    """Tiles that rows do not fill keep what an earlier call left in shared memory; none of it may reach a result."""
+    Hq, Hkv = heads
+    lens, T, starts, n = [900, 333], 900, [0, 6, 25], 25
+    c, q = setup(9, lens, T, Hq, Hkv, n)
+    q = torch.randn(n, Hq, 128, generator=torch.Generator().manual_seed(9)).to(torch.bfloat16)
+    score = P.Score(options.get("softcap", 0.0), q_pos=torch.full((n,), T, dtype=torch.int32, device="cuda"),
+                    slopes=torch.full((Hq,), 0.01, device="cuda") if "slopes" in options else None)
+    first = prefix(c, q, lens, T, Hq, Hkv, starts, score)
+    other, other_q = setup(10, [900], 900, 32, 4, 64)
+    for scale in (0.0, 1e4, math.nan):
+        prefix(other, other_q * scale, [900], 900, 32, 4, [0, 64], P.Score(softcap=20.0))
+        again = prefix(c, q, lens, T, Hq, Hkv, starts, score)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
 def test_prefix_keys_that_give_minus_infinity_are_tokens_without_weight():
     lens, T, starts = [700, 64, 300], 700, [0, 5, 7, 40]
     c, q = setup(4, lens, T, 8, 4, 40)
