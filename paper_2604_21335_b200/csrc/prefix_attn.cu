@@ -231,21 +231,21 @@ __device__ __forceinline__ float cap_any(float x, float cap_in, float cap_log2) 
     const float z = x * cap_in, lo = tanh_small(z), hi = tanh_large(z);
     return cap_log2 * (fabsf(z) <= kTanhSmall ? lo : hi);
 }
-// Caps N scores of a row.  Scores far below the cap are the usual case; the warp votes once per tile instead of branching
-// per score.  `big`: largest magnitude among them.
+// Cap the N scores of a row: far below the cap (the usual case; the warp votes once per tile instead of branching per
+// score), and of any size.
 template <int N>
-__device__ __forceinline__ void cap_scores(uint32_t (&r)[N], float big, float cap_in, float cap_log2, float scale_log2) {
-    if (__all_sync(0xFFFFFFFFu, big * fabsf(cap_in) <= kCapSmall)) {
+__device__ __forceinline__ void cap_scores_low(uint32_t (&r)[N], float cap_in, float scale_log2) {
 #pragma unroll
-        for (int i = 0; i < N; i += 2) {
-            const float2 y = cap_small(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), cap_in, scale_log2);
-            r[i] = __float_as_uint(y.x);
-            r[i + 1] = __float_as_uint(y.y);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) r[i] = __float_as_uint(cap_any(__uint_as_float(r[i]), cap_in, cap_log2));
+    for (int i = 0; i < N; i += 2) {
+        const float2 y = cap_small(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), cap_in, scale_log2);
+        r[i] = __float_as_uint(y.x);
+        r[i + 1] = __float_as_uint(y.y);
     }
+}
+template <int N>
+__device__ __forceinline__ void cap_scores_any(uint32_t (&r)[N], float cap_in, float cap_log2) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = __float_as_uint(cap_any(__uint_as_float(r[i]), cap_in, cap_log2));
 }
 template <int N>
 __device__ __forceinline__ float magnitude(const uint32_t (&r)[N]) {
@@ -572,16 +572,16 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (BIAS && a.sc.slopes) slope2 = a.sc.slopes[head] * kLog2e;
             const int32_t* doc = a.sc.tok_doc ? a.sc.tok_doc + (size_t)s.g * a.T : nullptr;
             if (doc) my_doc = a.sc.q_doc[seq];
-            // -inf for the tokens t .. t + COLS - 1 that the row does not see
-            auto hide = [&](uint32_t (&r)[COLS], int t) {
+            // `v` for the tokens t .. t + COLS - 1 that the row does not see
+            auto hide = [&](uint32_t (&r)[COLS], int t, float v) {
 #pragma unroll
                 for (int i = 0; i < COLS; ++i)
-                    if (t + i < lo || t + i >= hi) r[i] = __float_as_uint(-INFINITY);
+                    if (t + i < lo || t + i >= hi) r[i] = __float_as_uint(v);
                 if (doc) {
 #pragma unroll
                     for (int i = 0; i < COLS; ++i) {
                         const int d = __ldg(doc + min(t + i, a.T - 1));
-                        if (d >= 0 && d != my_doc) r[i] = __float_as_uint(-INFINITY);
+                        if (d >= 0 && d != my_doc) r[i] = __float_as_uint(v);
                     }
                 }
             };
@@ -611,9 +611,26 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     tmem_ld16<48>(ts + c0 + 48, r);
                 }
                 tmem_wait_ld();
+                // does every row of the warp see all the tokens?
+                auto all_seen = [&]() { return !doc && __all_sync(0xFFFFFFFFu, lo <= t0 && hi >= t0 + COLS); };
                 // scores in log2 units where they are not the raw products times a positive scale
-                // (lanes without a row hold whatever was in shared memory: they have no vote)
-                if constexpr (CAP) cap_scores(r, live ? magnitude(r) : 0.f, a.cap_in, a.cap_log2, a.scale_log2);
+                if constexpr (CAP) {
+                    // Tokens that are not seen, and lanes without a row, hold whatever was in memory and have no say in how
+                    // the others are capped.  If everything is small, so is what is seen; else it is asked by itself (looking
+                    // at seen tokens only from the start costs 4 % of 131072 tokens, 18 % with a window).
+                    auto small = [&]() { return __all_sync(0xFFFFFFFFu, (live ? magnitude(r) : 0.f) * fabsf(a.cap_in) <= kCapSmall); };
+                    if (__builtin_expect(small(), 1)) {
+                        cap_scores_low(r, a.cap_in, a.scale_log2);
+                    } else {
+                        bool low = false;
+                        if (!all_seen()) {
+                            hide(r, t0, 0.f);
+                            low = small();
+                        }
+                        if (low) cap_scores_low(r, a.cap_in, a.scale_log2);
+                        else cap_scores_any(r, a.cap_in, a.cap_log2);
+                    }
+                }
                 if constexpr (BIAS) {
                     const float far = (float)(t0 - (hi - 1));
 #pragma unroll
@@ -625,8 +642,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         r[i + 1] = __float_as_uint(x.y);
                     }
                 }
-                // does every row of the warp see all the tokens?
-                if (doc || !__all_sync(0xFFFFFFFFu, lo <= t0 && hi >= t0 + COLS)) hide(r, t0);
+                if (!all_seen()) hide(r, t0, -INFINITY);
                 float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int i = 0; i < COLS; i += 2)
