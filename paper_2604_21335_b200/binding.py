@@ -491,6 +491,12 @@ def query_bias(h_q: torch.Tensor, w_q: torch.Tensor, s_q: torch.Tensor, bias: to
         _stream()), "stc_query_bias")
 
 
+def _list_address(page_ids: Optional[torch.Tensor], address, other):
+    """Address of the page lists for the attention calls, where NULL means every page.  Lists of no pages are an empty tensor,
+    which has no address: `other` (that of any tensor) stands for it, nothing is read there."""
+    return other if page_ids is not None and not address else address
+
+
 _SCORED_NAMES = ("seq_len", "k", "v_packed", "v_mask", "v_offs", "slopes", "q_pos", "tok_doc", "q_doc", "q", "page_ids",
                  "n_pages", "out", "lse", "ws")
 
@@ -509,8 +515,7 @@ def decode_attn(shape: Shape, cache: Cache, q: torch.Tensor, page_ids: Optional[
         lp, kp, vp, mp, op, slp, pop, tdp, qdp, qp, ip, np_, outp, lsep, wsp = _addresses(
             dev, "ibb**fiiibiiffu", _SCORED_NAMES, shape.seq_len, cache.k, cache.v_packed, cache.v_mask, cache.v_offs,
             score.slopes, score.q_pos, score.tok_doc, score.q_doc, q, page_ids, n_pages, out, lse, ws)
-        if page_ids is not None and not ip:                # lists of no pages have no address, but are not "all pages"
-            ip = np_
+        ip = _list_address(page_ids, ip, qp)
         rc = load_library().stc_decode_attn_scored(
             _PACK_SHAPE(shape.batch, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.page_size, shape.n_groups,
                         shape.t_cap, 0, lp),
@@ -520,8 +525,9 @@ def decode_attn(shape: Shape, cache: Cache, q: torch.Tensor, page_ids: Optional[
             raise StcError(rc, "stc_decode_attn_scored")
         return
     cs, cc = shape.c(), cache.c()
+    qp = _ptr(q, torch.bfloat16, "q")
     _check(load_library().stc_decode_attn(
-        C.byref(cs), C.byref(cc), _ptr(q, torch.bfloat16, "q"), _ptr(page_ids, torch.int32, "page_ids"),
+        C.byref(cs), C.byref(cc), qp, _list_address(page_ids, _ptr(page_ids, torch.int32, "page_ids"), qp),
         _ptr(n_pages, torch.int32, "n_pages"), max_pages, sm_scale, _ptr(out, torch.float32, "out"),
         _ptr(lse, torch.float32, "lse"), _ptr(ws, torch.uint8, "ws"), ws.numel(), _stream()),
         "stc_decode_attn")
