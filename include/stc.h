@@ -93,7 +93,8 @@ typedef struct stc_cache {
 /* What stc_decode_attn_scored and stc_prefix_attn do to the scores besides sm_scale; zero / NULL
  * switches an option off. */
 typedef struct stc_score {
-    float softcap;             /* > 0: s becomes softcap * tanh(s / softcap); sm_scale / softcap must be finite */
+    float softcap;             /* > 0: s becomes softcap * tanh(s / softcap); in fp32 sm_scale / softcap
+                                  must be finite and not subnormal, softcap * log2(e) finite */
     int32_t window;            /* > 0: a query sees its window most recent tokens     */
     const float* slopes;       /* device f32 [Hq]: s += slopes[h] * (t - q_pos), after the cap */
     const int32_t* q_pos;      /* device i32, one per query row: position of the query,

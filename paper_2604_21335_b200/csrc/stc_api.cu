@@ -341,7 +341,11 @@ int32_t score_args(const stc_score* score, float sm_scale, ScoreArgs* out, bool*
     *plain = true;
     if (!score) return STC_OK;
     if (!(score->softcap >= 0.f) || !std::isfinite(score->softcap) || score->window < 0) return STC_ERR_INVALID_ARG;
-    if (score->softcap > 0.f && !std::isfinite(sm_scale / score->softcap)) return STC_ERR_INVALID_ARG;    // the kernels multiply by it
+    // the kernels multiply by sm_scale / softcap (a subnormal one has lost bits) and by softcap log2(e)
+    if (score->softcap > 0.f) {
+        const float in = sm_scale / score->softcap;
+        if (!(std::isnormal(in) || sm_scale == 0.f) || !std::isfinite(score->softcap * 1.4426950408889634f)) return STC_ERR_INVALID_ARG;
+    }
     if ((!score->tok_doc) != (!score->q_doc)) return STC_ERR_INVALID_ARG;
     out->softcap = score->softcap; out->window = score->window; out->slopes = score->slopes;
     out->q_pos = score->q_pos; out->tok_doc = score->tok_doc; out->q_doc = score->q_doc;
