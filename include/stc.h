@@ -420,7 +420,7 @@ int32_t stc_decode_attn(const stc_shape* shape, const stc_cache* cache, const vo
  * lse = -inf.  Keys and values of tokens that are not seen are never used, whatever they hold; a NaN score of a token
  * that is seen makes the head's out and lse NaN.
  * score NULL or all off: the same kernels, hence the same bits, as stc_decode_attn.  tanh is good to
- * one fp32 unit.  Workspace, alignment and status word as in stc_decode_attn; page selection knows nothing
+ * one fp32 unit below 0.55 of the cap and to 3e-7 of the cap above.  Workspace, alignment and status word as in stc_decode_attn; page selection knows nothing
  * of a distance bias (a cap is monotone and changes no ranking within a head). */
 int32_t stc_decode_attn_scored(const stc_shape* shape, const stc_cache* cache, const void* q,
                                const int32_t* page_ids, const int32_t* n_pages, int32_t max_pages,

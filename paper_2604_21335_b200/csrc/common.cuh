@@ -144,10 +144,11 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
-// tanh to about one fp32 ulp.  |z| <= 0.55: odd polynomial z + z^3 P(z^2), P fitted by weighted least
-// squares at Chebyshev nodes (relative error 6.7e-8 against extended precision); above: 1 - 2 / (e^{2z} + 1), whose
-// absolute error of about 1.5e-7 is small against tanh >= 0.5.  The hardware tanh (error 2^-11) would
-// move a score capped at 50 by 0.02.
+// tanh.  |z| <= 0.55: odd polynomial z + z^3 P(z^2), P fitted by weighted least squares at Chebyshev nodes (relative error
+// 6.7e-8 against extended precision, about one fp32 unit with its roundings); above: 1 - 2 / (e^{2z} + 1).  There e^{2z} (2 units
+// of exp2f, 1.1 of its argument's rounding), the sum and the quotient (2 units) leave at most 2.7e-7 absolute just above the border,
+// under five units of a result of 0.5, and less farther out.  The hardware tanh (error 2^-11) would move a score capped at 50 by
+// 0.02.
 constexpr float kTanhSmall = 0.55f;
 constexpr float kTanh0 = -0.33333316445350647f, kTanh1 = 0.13332580029964447f, kTanh2 = -0.053851865231990814f,
                 kTanh3 = 0.02107025310397148f, kTanh4 = -0.006272607482969761f;
