@@ -8,7 +8,9 @@ the shared library is missing the import of the library fails loudly.
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import struct
+import sysconfig
 from dataclasses import dataclass
 from pathlib import Path
 from typing import Optional
@@ -132,6 +134,8 @@ def load_library():
         lib.stc_decode_step_host.argtypes = [C.POINTER(_Shape), C.POINTER(_Cache), C.c_void_p, C.c_int32, C.c_float,
                                              C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p]
         _lib = lib
+        if _native_addresses is None:            # built since the import
+            _take_native()
     return _lib
 
 
@@ -170,10 +174,33 @@ def _at(t: Optional[torch.Tensor], dtype, device: int, name: str) -> int:
     return _ptr(t, dtype, name)
 
 
-try:
-    from ._tensor_args import addresses as _native_addresses, sizes_are as _sizes_are, token_rows as _native_token_rows
-except ImportError:                              # not built: the same checks in Python
-    _native_addresses = _sizes_are = _native_token_rows = None
+def args_library() -> Path:
+    """Where the native argument check stands: it reads tensors by torch's own headers, so its name holds the versions of the torch
+    and the Python it was built for, and another one's is not found."""
+    return _PKG / f"_tensor_args.torch-{torch.__version__}{sysconfig.get_config_var('EXT_SUFFIX')}"
+
+
+def _native_module():
+    """The argument check built for this torch and this Python, or None: the same checks in Python."""
+    path = args_library()
+    if not path.exists():
+        return None
+    spec = importlib.util.spec_from_file_location(__package__ + "._tensor_args", path)
+    try:
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError:
+        return None
+    return module
+
+
+def _take_native() -> None:
+    global _native_addresses, _sizes_are, _native_token_rows
+    m = _native_module()
+    _native_addresses, _sizes_are, _native_token_rows = (m.addresses, m.sizes_are, m.token_rows) if m else (None, None, None)
+
+
+_take_native()
 _CODES = {"b": torch.bfloat16, "f": torch.float32, "d": torch.float64, "i": torch.int32, "u": torch.uint8}
 
 

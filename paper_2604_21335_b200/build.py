@@ -19,24 +19,34 @@ NVCC_FLAGS = [
 
 
 ARGS_SRC = CSRC / "tensor_args.cpp"
-ARGS_LIB = PKG / "_tensor_args.so"
 
 
 def _build_args(force: bool = False) -> None:
-    """The binding's argument check (a CPython module against the headers of the installed torch), in-tree."""
-    if not force and ARGS_LIB.exists() and ARGS_LIB.stat().st_mtime >= ARGS_SRC.stat().st_mtime:
+    """The binding's argument check (a CPython module against the headers of the installed torch), in-tree.  It is optional: where it
+    does not compile the binding checks in Python."""
+    if str(ROOT) not in sys.path:                # run by its path
+        sys.path.insert(0, str(ROOT))
+    from paper_2604_21335_b200 import binding
+    lib = binding.args_library()
+    if not force and lib.exists() and lib.stat().st_mtime >= ARGS_SRC.stat().st_mtime:
         return
     import sysconfig
 
     import torch
     root = Path(torch.__file__).resolve().parent
     include = [root / "include", root / "include" / "torch" / "csrc" / "api" / "include", sysconfig.get_paths()["include"]]
-    tmp = ARGS_LIB.with_suffix(f".{os.getpid()}.tmp")
-    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
-                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-                           *[f"-I{p}" for p in include], str(ARGS_SRC), "-o", str(tmp), f"-L{root / 'lib'}",
-                           "-ltorch_python", "-ltorch_cpu", "-lc10"])
-    os.replace(tmp, ARGS_LIB)
+    tmp = lib.with_name(f"{lib.name}.{os.getpid()}.tmp")
+    try:
+        subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+                               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                               *[f"-I{p}" for p in include], str(ARGS_SRC), "-o", str(tmp), f"-L{root / 'lib'}",
+                               "-ltorch_python", "-ltorch_cpu", "-lc10"])
+    except (OSError, subprocess.CalledProcessError) as e:
+        sys.stderr.write(f"the native argument check was not built, the binding checks in Python: {e}\n")
+        tmp.unlink(missing_ok=True)
+        lib.unlink(missing_ok=True)              # of an older source
+        return
+    os.replace(tmp, lib)
 
 
 def _stale() -> bool:
