@@ -151,9 +151,11 @@ cudaError_t launch_rope_write(const Geom& g, const stc_rope& rope, const int32_t
     if (e != cudaSuccess) return e;
     // four tokens per CTA once that still gives every SM one, else one token per CTA (8 x 511 ragged tokens: 10.7 against
     // 16.8 us; 2 x 16384 tokens: 2, 4, 8, 16, 32 tokens per CTA take 143, 124, 124, 127, 131 us)
-    const long long tokens = (long long)g.B * max_new;
+    // (max_new is a bound and a row stride: no sequence has more than T new tokens, and none of a CTA's token numbers overflows)
+    const int most = max_new < g.T ? max_new : g.T;
+    const long long tokens = (long long)g.B * most;
     const int tok = tokens >= 4LL * sms ? 4 : 1;
-    a.chunks = (max_new + tok - 1) / tok;
+    a.chunks = (most + tok - 1) / tok;
     const long long n_cta = (long long)a.chunks * g.B;
     if (n_cta > 0x7FFFFFFFLL) return cudaErrorInvalidConfiguration;
 #define STC_ROPE(TOK_)                                                                                  \
