@@ -313,23 +313,28 @@ scored_attn_kernel(const ScoredArgs a) {
             const uint32_t base = __shfl_sync(0xFFFFFFFFu, pre, tau) * OPG;
             // the low half of a masked token's own groups does not matter: its prefix counts all of them
             const uint32_t all = __shfl_sync(0xFFFFFFFFu, f.mask, tau);
+            // The page's product starts from zero and is added by the fp32 pipes, which round to nearest: mma.sync truncates the sum
+            // it adds to, and over hundreds of pages that takes a share of the result away (683 pages per warp, 16 x 32/8 heads:
+            // error 5.5e-5 when acc itself was the sum, 1.4e-7 now).  Small parts first, so that only the last product truncates
+            // at the sum's full size; the eight tiles' chains side by side (8 x 28/4 heads: acc as the sum 17.6 us, one chain
+            // after the other 18.9, side by side 18.3).
+            uint32_t vr[8][4];
 #pragma unroll
             for (int dt = 0; dt < 8; ++dt) {
                 const int oct = 2 * dt + hb, grp = oct / OPG;
                 const uint32_t idx = base + __popc(all & ((1u << grp) - 1u)) * OPG + (uint32_t)(oct % OPG);
                 const bool kept = ((m >> grp) & 1u) && idx < f.chunks;
-                uint32_t a0, a1, a2, a3;
-                ldmatrix_x4_trans(kept ? vst + idx * 16u : zero_row, a0, a1, a2, a3);
-                // The page's product starts from zero and is added by the fp32 pipes, which round to nearest: mma.sync truncates
-                // the sum it adds to, and over hundreds of pages that takes a share of the result away (683 pages per warp,
-                // 16 x 32/8 heads: error 5.5e-5 when acc itself was the sum, 1.4e-7 now; 8 x 28/4 heads 17.8 -> 18.6 us).  Small
-                // parts first, so that only the last product truncates at the sum's full size.
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int k = 2; k >= 0; --k) mma_bf16(sum, a0, a1, a2, a3, wb[k][0], wb[k][1]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[dt][i] += sum[i];
+                ldmatrix_x4_trans(kept ? vst + idx * 16u : zero_row, vr[dt][0], vr[dt][1], vr[dt][2], vr[dt][3]);
             }
+            float sum[8][4] = {};
+#pragma unroll
+            for (int k = 2; k >= 0; --k)
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) mma_bf16(sum[dt], vr[dt][0], vr[dt][1], vr[dt][2], vr[dt][3], wb[k][0], wb[k][1]);
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[dt][i] += sum[dt][i];
         } else {
             // one head on the fp32 pipes: lane = tokens r, r+8 x chunks c, c+4, c+8, c+12
             float sd[4];
