@@ -356,7 +356,8 @@ int32_t stc_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, doub
  * the products are fp32 with one rounding to bf16.  Channels from rot_dim on are copied.
  * Rows of q_out behind a sequence's new tokens, and all other rows of the caches, are left as they were.
  * status: i32 [B]: STC_OK, or STC_ERR_INVALID_ARG for a sequence whose lengths are inconsistent
- * (old_len > len, or more than max_new new tokens), which is left untouched.  Needs no workspace. */
+ * (old_len > len, or more than max_new new tokens), which is left untouched.  max_new is a bound and the row
+ * stride, and may exceed t_cap; 0 enqueues nothing and leaves status unwritten.  Needs no workspace. */
 int32_t stc_rope_write(const stc_shape* shape, const stc_rope* rope, const int32_t* old_len, int32_t max_new,
                        const int32_t* positions_opt, const void* q_in, int64_t q_stride, const void* k_in,
                        int64_t k_stride, const void* v_in, int64_t v_stride, void* q_out, void* k, void* v,
@@ -418,7 +419,8 @@ int32_t stc_decode_attn(const stc_shape* shape, const stc_cache* cache, const vo
  *     s_t = x_t + slopes[h] * (t - p) (if set)
  * and softmax, values and lse as in stc_decode_attn.  A head with no token left gives out = 0 and
  * lse = -inf.  Keys and values of tokens that are not seen are never used, whatever they hold; a NaN score of a token
- * that is seen makes the head's out and lse NaN.
+ * that is seen makes the head's out and lse NaN.  Values of seen tokens are to be finite: a weight enters the product in parts,
+ * one of which may be 0 or negative, so an infinite value can make its channel NaN.
  * score NULL or all off: the same kernels, hence the same bits, as stc_decode_attn.  tanh is good to
  * one fp32 unit below 0.55 of the cap and to 3e-7 of the cap above.  Workspace, alignment and status word as in stc_decode_attn; page selection knows nothing
  * of a distance bias (a cap is monotone and changes no ranking within a head). */
@@ -450,7 +452,12 @@ int32_t stc_decode_attn_scored(const stc_shape* shape, const stc_cache* cache, c
  * must be below 2^31 (else STC_ERR_UNSUPPORTED).  Both products run on the tensor cores with fp32 accumulation; the
  * weights enter the second as a bf16 pair.  ws: STC_OP_PREFIX_ATTN with arg = n_rows; its first int32 is a
  * device status word the call writes: STC_OK, STC_ERR_INVALID_ARG (row_start), or STC_ERR_TIMEOUT if a bounded
- * wait expired on the device (it never should; out / lse are then unspecified). */
+ * wait expired on the device (it never should; out / lse are then unspecified); without rows nothing is
+ * written.  The workspace is 78 MB for any n_rows (partial results of every SM); calls that may overlap need one each.
+ * A window, q_pos inside the prefix and documents hide tokens and save no work: all of a prefix is read.
+ * Repeatable bit for bit: the same call gives the same bits, whatever stands in tokens that no row sees.  The
+ * last bits of a row may depend on the other rows of the call, by which the prefix is split, and the rows of
+ * one KV head choose together between two forms of the cap that agree to fp32 accuracy. */
 int32_t stc_prefix_attn(const stc_shape* shape, const stc_cache* cache, int32_t n_rows, const void* q,
                         const int32_t* row_start, float sm_scale, const stc_score* score, const float* own_out,
                         const float* own_lse, float* out, float* lse_opt, void* ws, size_t ws_bytes, void* stream);

@@ -17,12 +17,17 @@
 //
 // What bounds it.  Up to 128 rows per KV head the two products of 128 tokens take about 1800 cycles of the tensor pipe
 // and their bytes (K 32 KiB, V up to 32 KiB) 2100 to 2800 cycles of an SM's share of HBM; the loop product -> softmax ->
-// product of a group takes about 3000 for its 64 of them, so a long prefix runs at 0.55 of the copy rate (131072 tokens, 16 x
+// product of a group takes about 2850 for its 64 of them, so a long prefix runs at 0.6 of the copy rate (131072 tokens, 16 x
 // 32/8 heads: 107 us for 405 MB).  Halving the softmax's work or the second product alone gains 5 % each, halving the value
-// warps' 1 %: it is the chain, not one of its links.  At 256 rows the tensor pipe is busy 0.8 of the time, so a work unit is at most
-// two row tiles (one pass over K and V for 256 rows) and larger batches take more units, whose K and V come from L2
+// warps' 1 %: it is the chain, not one of its links.  At 256 rows 64 tokens take 3020 cycles (start and end included), of which
+// the products are 1792: 1536 at the pipe's rate, 256 because an S product of N = 64 takes 1.5 times its share.  A work unit is
+// at most two row tiles (one pass over K and V for 256 rows); larger batches take more units, whose K and V come from L2
 // (32768 tokens, 128 x 32/8 heads: 112 us for 69 GFLOP).  A short call pays 4.5 us to its first scores, 2 us for a segment's end
-// and 4 us for the second kernel (272 tokens, 8 x 32 heads: 14.4 us).
+// and 4 us for the second kernel (272 tokens, 8 x 32 heads: 14.6 us).
+//
+// A window, positions inside the prefix and documents are masks on the scores: every tile of a prefix is loaded and multiplied,
+// whatever its rows see of it (131072 tokens, 16 x 32/8 heads: 105 us; with a window of 4096 100 us; with documents 135 to 138 us,
+// each thread then reads its tile's document words and hides scores one by one).
 //
 // Work split.  Unit = (prefix, KV head, block of up to two row tiles); the token tiles of all units form one flat
 // sequence, each as long as it takes (2, 3 or 4 for a tile whose softmax has 32 scores per thread, 64, or 64 in both

@@ -4,10 +4,11 @@
 //     x_t = sm_scale q_h.k_t,   x_t <- cap tanh(x_t / cap),   s_t = x_t + slope_h (t - p),
 //     out = softmax(s) V~ (dropped value groups add zero),   lse = log sum exp s.
 //
-// What bounds it.  HBM for large calls (256 bytes of key and the kept groups per token; 8 x 28/4 heads, 256 pages of 16 groups:
-// 15 us, of which 5.5 are the start and the join and the rest runs at 0.7 of the copy rate); the chain of dependent steps
-// for small ones: a decode step of one sequence moves a few MB, half a microsecond's worth, and what counts is how few
-// round trips stand between the launch and the result.
+// What bounds it.  HBM for the largest calls (256 bytes of key and the kept groups per token; 16 x 32/8 heads over whole caches of
+// 131072 tokens: 1.13 ms, 0.89 of the copy rate).  A few hundred pages per problem leave a warp few pages and the machine few warps: 8 x
+// 28/4 heads, 256 pages of 16 groups, take 18.2 us for 6.6 us' worth of bytes (21 to 22 us with cold caches; DRAM at a quarter of its rate),
+// 5.5 of them the start and the join.  Small calls are the chain of dependent steps: a decode step of one sequence moves half a
+// microsecond's worth, and what counts is how few round trips stand between the launch and the result (1 x 8 heads: 5.9 us).
 //
 // Work split.  One cluster of C CTAs (4 warps each) per (sequence, KV head); warp i of the cluster takes the listed
 // pages i, i + 4 C, ...  C is chosen so that the clusters fill the machine (plan below).  Each warp keeps its own
@@ -15,6 +16,8 @@
 // each other's shared memory (distributed shared memory), each CTA finishing its share of the outputs: one launch,
 // nothing in global memory, no atomics, and the same order of additions every time.  Few problems with long lists (one
 // sequence that attends all of its cache) take several clusters each, whose results a second small kernel joins.
+//
+// (One KV head, 131072 tokens: 20.7 us for one query head, 23.4 for eight, 7.8 us' worth of bytes; 263 with one cluster.)
 //
 // Which pages a warp needs at all is settled before any copy: 32 listed pages at a time, one per lane, the lane
 // works out which of the page's 16 tokens the query sees (window and documents included) and drops the page from the
@@ -295,7 +298,7 @@ scored_attn_kernel(const ScoredArgs a) {
                 for (int dt = 0; dt < 8; ++dt) { acc[dt][0] *= al0; acc[dt][1] *= al1; acc[dt][2] *= al0; acc[dt][3] *= al1; }
             }
             // P^T as B fragments: a weight is the sum of three bf16 parts (24 bits, so the weights are as good as fp32; the third
-            // part costs a page 8 of 32 MMAs and less than 3 % of a call)
+            // part costs a page 8 of 32 MMAs)
             uint32_t wb[3][2];
             {
                 float x0 = p0, x1 = p1, x2 = p2, x3 = p3;
@@ -658,8 +661,8 @@ cudaError_t launch_scored_attn(const Geom& g, const void* k, const void* v_packe
     cudaError_t e = device_sm_count(&sms);
     if (e != cudaSuccess) return e;
     // three CTAs per SM with two stages per warp: a page's arithmetic outlasts a copy, so twelve warps per SM beat eight with
-    // three stages (8 sequences, 28 / 4 heads, 256 pages: 15.3 against 15.9 us); six or twelve warps per CTA take 14.4 us there,
-    // but 5.9 and 6.3 instead of 5.6 for one sequence of 8 heads, and clusters of 9 to 16 CTAs 16.8 to 27 us
+    // three stages (8 sequences, 28 / 4 heads, 256 pages, their state in L2: 15.3 against 15.9 us); six or twelve warps per CTA took
+    // 14.4 us there, but 5.9 and 6.3 instead of 5.6 for one sequence of 8 heads, and clusters of 9 to 16 CTAs 16.8 to 27 us
     plan(g.problems, max_pages, sms * 3, attn_plan(g, max_pages).slots_cap, &a.cluster, &a.splits);
     a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + 256);
     a.part_o = reinterpret_cast<float*>(a.part_ml) + ((size_t)g.problems * a.splits * g.Gq * 2 + 63) / 64 * 64;

@@ -1,4 +1,4 @@
-// Wrappers of the tcgen05 / tensor-map instructions shared by the tensor-memory kernels.
+// Wrappers of the tcgen05 / tensor-map instructions of the shared-prefix attention (router.cu, older, has its own).
 #pragma once
 #include <cuda.h>
 
