@@ -280,7 +280,8 @@ def prepare(case, seed):
     s["page_ids"], s["n_pages"] = _selection(g, s, B, hkv, t, c["pages"]) if c["pages"] else (None, None)
     hq = c["hq"]
     s |= dict(q=_normal(g, B, n, hq, D), slopes=None, tok_doc=None, q_doc=None,
-              out=torch.zeros(B, n, hq, D, dtype=torch.float32, device=DEV), lse=torch.zeros(B, n, hq, dtype=torch.float32, device=DEV))
+              out=torch.zeros(B, n, hq, D, dtype=torch.float32, device=DEV), lse=torch.zeros(B, n, hq, dtype=torch.float32, device=DEV),
+              status=torch.zeros(B, dtype=torch.int32, device=DEV))
     if c["alibi"]:
         s["slopes"] = torch.tensor([2.0 ** (-8.0 * (h + 1) / hq) for h in range(hq)], dtype=torch.float32, device=DEV)
     if c["docs"]:                              # documents in a row; the last belongs to the sequence, the first (-1) to all
@@ -481,16 +482,14 @@ def _own_tree(s):
     if "ws" not in s:                          # the workspace that a serving program allocates once
         s["ws"] = P.binding.new_workspace(shape, P.binding.OP_TREE_ATTN, c["nodes"])
     score = P.Score(softcap=c["cap"], slopes=s["slopes"], window=c["window"], tok_doc=s["tok_doc"], q_doc=s["q_doc"])
-    P.tree_attn(shape, _own_cache(P, s), tree, s["q"], s["page_ids"], s["n_pages"], 1 / math.sqrt(D), s["out"], s["ws"],
-                lse=s["lse"], score=score)
+    P.tree_attn(shape, _own_cache(P, s), tree, s["q"], s["page_ids"], s["n_pages"], 1 / math.sqrt(D), s["out"], s["status"],
+                s["ws"], lse=s["lse"], score=score)
     return s["out"], s["lse"]
 
 
 def _own_accept(s):
     import paper_2604_21335_b200 as P
-    if "ws" not in s:
-        s["ws"] = P.binding.tree_accept_workspace(*s["logits"].shape)
-    P.tree_accept(s["logits"], s["tokens"], s["path"], s["n_accepted"], s["next"], s["ws"], parent=s["parent"])
+    P.tree_accept(s["logits"], s["tokens"], s["path"], s["n_accepted"], s["next"], parent=s["parent"])
     return s["path"], s["n_accepted"], s["next"]
 
 
