@@ -67,7 +67,8 @@ typedef enum {
 
 enum { STC_CLS_DROP = 0, STC_CLS_ROUTED = 1, STC_CLS_FULL = 2 };
 enum { STC_MODE_GLOBAL = 0, STC_MODE_PER_TOKEN = 1 };
-enum { STC_OP_QUEST_SELECT = 1, STC_OP_ROUTE_PACK = 2, STC_OP_DECODE_ATTN = 3, STC_OP_PREFIX_ATTN = 4 };
+enum { STC_OP_QUEST_SELECT = 1, STC_OP_ROUTE_PACK = 2, STC_OP_DECODE_ATTN = 3, STC_OP_PREFIX_ATTN = 4,
+       STC_OP_TREE_ATTN = 5 };
 
 typedef struct stc_shape {
     int32_t batch, n_q_heads, n_kv_heads;
@@ -115,13 +116,30 @@ typedef struct stc_rope {
     int32_t reserved;          /* must be 0 */
 } stc_rope;
 
+/* Drafted tokens of every sequence, in a tree (speculative decoding): several continuations of a
+ * sequence are put to the model at once.  Their rows stand in buffers of their own until some of them
+ * are accepted (stc_rope_write with t_cap = n_cap, old_len 0 and explicit positions fills them). */
+#define STC_TREE_MAX_NODES 128
+typedef struct stc_tree {
+    const void* k;             /* bf16 [B][Hkv][n_cap][128]: keys of the nodes         */
+    const void* v;             /* bf16 [B][Hkv][n_cap][128]: values, full width        */
+    const int32_t* parent;     /* device i32 [B][n_cap]: the node a node continues, lower than the
+                                  node itself; -1: it continues the cached sequence.
+                                  NULL: a chain, parent[i] = i - 1                     */
+    const int32_t* n_nodes;    /* device i32 [B], clamped to [0, n_cap]; NULL = n_cap for all */
+    int32_t n_cap;             /* nodes per sequence in all buffers: 1..STC_TREE_MAX_NODES */
+    int32_t reserved;          /* must be 0 */
+} stc_tree;
+
+enum { STC_LOGITS_BF16 = 0, STC_LOGITS_F32 = 1 };
+
 enum { STC_ROPE_NONE = 0, STC_ROPE_LINEAR = 1, STC_ROPE_BANDS = 2, STC_ROPE_YARN = 3 };
 
 const char* stc_status_string(int32_t status);
 int32_t stc_version(void);
 
 /* Bytes of workspace `op` (STC_OP_*) needs for `shape`; `arg` is max_pages for
- * STC_OP_DECODE_ATTN, n_rows for STC_OP_PREFIX_ATTN and ignored otherwise.  Workspaces must be 256-byte
+ * STC_OP_DECODE_ATTN, n_rows for STC_OP_PREFIX_ATTN, n_cap for STC_OP_TREE_ATTN and ignored otherwise.  Workspaces must be 256-byte
  * aligned.  A workspace may be reused by consecutive calls on one stream;
  * calls that share a workspace must not overlap on the device. */
 int32_t stc_workspace_bytes(const stc_shape* shape, int32_t op, int64_t arg, size_t* bytes_host);
@@ -461,6 +479,98 @@ int32_t stc_decode_attn_scored(const stc_shape* shape, const stc_cache* cache, c
 int32_t stc_prefix_attn(const stc_shape* shape, const stc_cache* cache, int32_t n_rows, const void* q,
                         const int32_t* row_start, float sm_scale, const stc_score* score, const float* own_out,
                         const float* own_lse, float* out, float* lse_opt, void* ws, size_t ws_bytes, void* stream);
+
+/* Attention for trees of drafted tokens over a routed cache (the attention equation of Section 3.3 for the verification
+ * step of speculative decoding, which the paper does not have): every node of a sequence's tree attends the valid tokens
+ * of the sequence's listed pages -- read once for all nodes and query heads of a KV head -- and its own ancestors:
+ *   N_i = node i, its parent, the parent's parent, ...;   position of node i: p_i = score->q_pos[b][i], or
+ *         len + |N_i| - 1 where q_pos is NULL (cached token t stands at t, the tree continues the sequence)
+ *     s_t = sm_scale * q_i.k_t over the listed tokens t and, over j in N_i, s_j = sm_scale * q_i.k_j (k_j: tree->k),
+ *           with the options of stc_score as in stc_decode_attn_scored, t and p_j being the positions;
+ *     out[b][i] = softmax(s) (V~, tree->v),   lse[b][i] = log sum exp s.
+ *   q         bf16 [B][n_cap][Hq][128]         out  f32 [B][n_cap][Hq][128]       lse_opt  f32 [B][n_cap][Hq] or NULL
+ *   score     NULL or options: q_pos i32 [B][n_cap], q_doc i32 [B] (a tree belongs to one document; the nodes of a tree
+ *             see each other whatever it is)
+ *   page_ids  as in stc_decode_attn (NULL = all; e.g. stc_quest_select's for the newest token's query); ids outside
+ *             the sequence are skipped, a page listed twice counts twice
+ * Without a window or q_pos a node sees at least itself; a row that sees nothing gives out = 0, lse = -inf.  Rows from
+ * n_nodes[b] on are left as they were.  A NaN score of a token that a row sees makes the row NaN; what the row
+ * does not see of the keys, and what no node of the sequence sees of the values, may hold anything; other values are to be
+ * finite.  status i32 [B]: STC_OK, or STC_ERR_INVALID_ARG for a sequence one of whose parents is not in
+ * [-1, node), which is left untouched.  batch * n_cap * n_q_heads and batch * n_kv_heads * t_cap must be below 2^31
+ * (else STC_ERR_UNSUPPORTED).  Both products run on the tensor cores with fp32 accumulation, the weights enter
+ * the second as a bf16 pair.  The same call gives the same bits.
+ * ws: STC_OP_TREE_ATTN with arg = n_cap; its first int32 is a device status word the call writes: STC_OK, or
+ * STC_ERR_TIMEOUT if a bounded wait expired on the device (it never should; out / lse are then unspecified). */
+int32_t stc_tree_attn(const stc_shape* shape, const stc_cache* cache, const stc_tree* tree, const void* q,
+                      const int32_t* page_ids, const int32_t* n_pages, int32_t max_pages, float sm_scale,
+                      const stc_score* score, float* out, float* lse_opt, int32_t* status, void* ws, size_t ws_bytes,
+                      void* stream);
+
+/* Greedy verification of drafted trees (not in the paper).  Node 0 of a tree is its root, the token chosen last, which
+ * is accepted; node i holds the token tokens[b][i].  From the root on, with c = the last accepted node and
+ *     x = argmax_v logits[b][c][v]     (the lowest index of equal values; NaN counts as the largest)
+ * the lowest node i in (c, n_nodes[b]) with parent[b][i] == c and tokens[b][i] == x is accepted; where there is none the walk ends
+ * and x is the sequence's next token.
+ *   logits       bf16 or f32 (logits_type STC_LOGITS_*) [batch][n_cap] rows of `vocab`, row_stride elements from row to row;
+ *                only the rows of accepted nodes are read
+ *   tokens, parent, n_nodes_opt   i32 [batch][n_cap] (parent NULL: a chain), i32 [batch] or NULL, as in stc_tree
+ *   path         i32 [batch][n_cap]: the accepted nodes, ascending; entries behind them are left as they were
+ *   n_accepted   i32 [batch]: their number, at least 1; 0 for a tree without nodes
+ *   next_token   i32 [batch]: x, or -1 for a tree without nodes
+ * vocab >= 1, 1 <= n_cap <= STC_TREE_MAX_NODES, row_stride >= vocab.  Needs no workspace. */
+int32_t stc_tree_accept(int32_t batch, int32_t n_cap, int32_t vocab, const void* logits, int32_t logits_type,
+                        int64_t row_stride, const int32_t* tokens, const int32_t* parent, const int32_t* n_nodes_opt,
+                        int32_t* path, int32_t* n_accepted, int32_t* next_token, void* stream);
+
+/* Accepted nodes become cached tokens (the query region stays at full width, Section 3.4, as in stc_append_tokens).
+ * shape->seq_len holds the lengths BEFORE the call.  For every sequence b the rows path[b][0 .. n_accepted[b]) of tree->k and
+ * tree->v become the tokens len .. len + n_accepted[b] - 1: keys go to cache->k (which this call writes), values with all S
+ * groups behind the packed groups, v_mask and v_offs follow, and kmin / kmax of every page that holds a new token are
+ * recomputed (both may be NULL).
+ *   new_len       i32 [B]: len + n_accepted[b]; must not be shape->seq_len
+ *   total_groups  i64 [B][Hkv], status i32 [B][Hkv] as in stc_append_tokens (STC_ERR_CAPACITY: groups past cap_groups were
+ *                 not stored).  A sequence with n_accepted outside [0, n_cap], a path entry outside [0, n_nodes[b])
+ *                 or more tokens than t_cap is left untouched, total_groups too, with new_len = len and STC_ERR_INVALID_ARG.
+ * tree->parent is not read.  Needs no workspace. */
+int32_t stc_tree_commit(const stc_shape* shape, const stc_cache* cache, const stc_tree* tree, const int32_t* path,
+                        const int32_t* n_accepted, int32_t* new_len, int64_t* total_groups, int32_t* status,
+                        void* stream);
+
+/* Copies of whole cached sequences (several answers to one prompt, beams, hand-over to another cache; not in the paper).
+ * For every pair i the sequence src_row[i] of `src` becomes the sequence dst_row[i] of `dst`: keys, page metadata, masks,
+ * offsets and packed groups up to its length.  The shapes agree in everything but batch, t_cap and seq_len
+ * (dst_shape->seq_len is not read); `dst` may be `src` (the same k), whose rows that are not a dst_row are left alone.
+ *   src_row, dst_row  device i32 [n_pairs]; pairs of one source next to each other share its reading
+ *   new_len           i32 [dst batch]: entry dst_row[i] receives the length
+ *   total_groups      i64 [dst batch][Hkv]: row dst_row[i] receives the groups
+ *   status            i32 [n_pairs][Hkv]: STC_OK; STC_ERR_CAPACITY (groups past dst's cap_groups were not stored);
+ *                     STC_ERR_INVALID_ARG for a pair that is left out whole: a row outside its cache, a dst_row that an
+ *                     earlier pair has, more tokens than dst's t_cap, or, within one cache, a dst_row that is
+ *                     the src_row of a pair (a pair of a row with itself is fine and moves nothing)
+ * dst->kmin and kmax may be NULL (metadata is not copied), and are NULL where src's are.  Buffers of different caches must not
+ * overlap.  n_pairs <= 4096, n_kv_heads <= 65535.  Needs no workspace. */
+int32_t stc_cache_fork(const stc_shape* src_shape, const stc_cache* src, const stc_shape* dst_shape, const stc_cache* dst,
+                       int32_t n_pairs, const int32_t* src_row, const int32_t* dst_row, int32_t* new_len,
+                       int64_t* total_groups, int32_t* status, void* stream);
+
+/* Drops the pages that are not listed and closes the gaps (a cache shrunk for good to what a selection kept; Section 3.2
+ * selects per step and keeps everything).  For every sequence and KV head the listed pages, ascending, become the pages
+ * 0 .. n_pages - 1 of `dst`: keys, metadata, masks, offsets and packed groups move together.  Tokens keep their rotation but no
+ * longer stand at their positions: later calls are given q_pos or positions where they matter.
+ *   page_ids, n_pages  as written by stc_quest_select (row stride max_pages): strictly ascending ids below ceil(len/16),
+ *                      the same number for all KV heads of a sequence; a last page that is not full is listed by all of
+ *                      them or by none (stc_quest_select_window with n_recent_pages >= 1 always lists it)
+ *   dst                another cache, whose shape agrees in everything but t_cap and seq_len (not read), or `src` itself
+ *                      (equal shapes, the same pointers): then the pages are moved in place
+ *   new_len            i32 [B]: tokens kept; must not be src_shape->seq_len
+ *   total_groups       i64 [B][Hkv];   status i32 [B][Hkv]: STC_OK; STC_ERR_CAPACITY (groups past dst's cap_groups were not
+ *                      stored); STC_ERR_INVALID_ARG in all heads of a sequence whose lists are not as above or do
+ *                      not fit dst's t_cap: new_len = len, nothing else is written
+ * kmin / kmax as in stc_cache_fork.  Needs no workspace. */
+int32_t stc_cache_compact(const stc_shape* src_shape, const stc_cache* src, const int32_t* page_ids,
+                          const int32_t* n_pages, int32_t max_pages, const stc_shape* dst_shape, const stc_cache* dst,
+                          int32_t* new_len, int64_t* total_groups, int32_t* status, void* stream);
 
 /* One decode step on the device: stc_quest_select followed by stc_decode_attn over the pages it
  * selected (Stage I per step, Section 3.2, then the routed attention of Section 3.3), as one call.

@@ -20,7 +20,7 @@ import torch
 _PKG = Path(__file__).resolve().parent
 _LIB_PATH = _PKG / "libstc.so"
 
-OP_QUEST_SELECT, OP_ROUTE_PACK, OP_DECODE_ATTN, OP_PREFIX_ATTN = 1, 2, 3, 4
+OP_QUEST_SELECT, OP_ROUTE_PACK, OP_DECODE_ATTN, OP_PREFIX_ATTN, OP_TREE_ATTN = 1, 2, 3, 4, 5
 MODE_GLOBAL, MODE_PER_TOKEN = 0, 1
 CLS_DROP, CLS_ROUTED, CLS_FULL = 0, 1, 2
 ROPE_NONE, ROPE_LINEAR, ROPE_BANDS, ROPE_YARN = 0, 1, 2, 3
@@ -32,6 +32,7 @@ EXPORTS = (
     "stc_quest_select", "stc_route_pack", "stc_decode_attn", "stc_cache_bytes",
     "stc_pass_host_arena_bytes", "stc_pass_host", "stc_quest_select_static", "stc_route_mask", "stc_pack_values", "stc_append_tokens", "stc_router_logits", "stc_query_bias", "stc_quest_select_window", "stc_pages_to_class", "stc_route_new_pages", "stc_decode_step", "stc_decode_step_host_arena_bytes", "stc_decode_step_host",
     "stc_rope_frequencies", "stc_rope_write", "stc_decode_attn_scored", "stc_prefix_attn",
+    "stc_tree_attn", "stc_tree_accept", "stc_tree_commit", "stc_cache_fork", "stc_cache_compact",
 )
 
 
@@ -117,6 +118,17 @@ def load_library():
         lib.stc_prefix_attn.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p,
                                         C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
                                         C.c_void_p]
+        lib.stc_tree_attn.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                      C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                      C.c_void_p]
+        lib.stc_tree_accept.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p,
+                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        lib.stc_tree_commit.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                        C.c_void_p, C.c_void_p]
+        lib.stc_cache_fork.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
+                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        lib.stc_cache_compact.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
+                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         lib.stc_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double,
                                              C.c_double, C.c_void_p, C.c_void_p]
         lib.stc_rope_write.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
@@ -201,7 +213,7 @@ def _take_native() -> None:
 
 
 _take_native()
-_CODES = {"b": torch.bfloat16, "f": torch.float32, "d": torch.float64, "i": torch.int32, "u": torch.uint8}
+_CODES = {"b": torch.bfloat16, "f": torch.float32, "d": torch.float64, "i": torch.int32, "l": torch.int64, "u": torch.uint8}
 
 
 def _addresses(device: int, codes: str, names: tuple, *tensors) -> tuple:
@@ -213,11 +225,12 @@ def _addresses(device: int, codes: str, names: tuple, *tensors) -> tuple:
     return got
 
 
-# Structures as the bytes the library reads (native layout of stc_shape, stc_cache, stc_score, stc_rope).
+# Structures as the bytes the library reads (native layout of stc_shape, stc_cache, stc_score, stc_rope, stc_tree).
 _PACK_SHAPE = struct.Struct("8iP").pack
 _PACK_CACHE = struct.Struct("6Pq").pack
 _PACK_SCORE = struct.Struct("fi4P").pack
 _PACK_ROPE = struct.Struct("Piifi").pack
+_PACK_TREE = struct.Struct("4Pii").pack
 
 
 @dataclass
@@ -297,6 +310,15 @@ class Rope:
     inv_freq: torch.Tensor
     interleaved: bool = False
     scale: float = 1.0
+
+
+@dataclass
+class Tree:
+    """Drafted tokens (stc_tree): their keys and values, and the node each continues (None: a chain)."""
+    k: torch.Tensor                           # bf16 [B,Hkv,n,128]
+    v: torch.Tensor
+    parent: Optional[torch.Tensor] = None     # i32 [B,n], parent[i] < i, -1 = the cached sequence
+    n_nodes: Optional[torch.Tensor] = None    # i32 [B], None = n for all
 
 
 def _sizes(names: tuple, *pairs) -> None:
@@ -585,6 +607,160 @@ def prefix_attn(shape: Shape, cache: Cache, q: torch.Tensor, row_start: torch.Te
         _PACK_SCORE(co.softcap, co.window, slp, pop, tdp, qdp), oop, olp, outp, lsep, wsp, ws.numel(), _raw_stream(dev))
     if rc:
         raise StcError(rc, "stc_prefix_attn")
+
+
+def _shape_bytes(shape: Shape, seq_len: int) -> bytes:
+    return _PACK_SHAPE(shape.batch, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.page_size, shape.n_groups,
+                       shape.t_cap, 0, seq_len)
+
+
+_CACHE_NAMES = ("k", "kmin", "kmax", "v_packed", "v_mask", "v_offs")
+_TREE_NAMES = ("seq_len", "k", "v_packed", "v_mask", "v_offs", "tree.k", "tree.v", "tree.parent", "tree.n_nodes", "slopes", "q_pos",
+               "tok_doc", "q_doc", "q", "page_ids", "n_pages", "out", "lse", "status", "ws")
+
+
+def _check_cache(shape: Shape, cache: Cache, what: str = "") -> None:
+    """Sizes of a cache's buffers against its shape."""
+    B, H, T, P, D = shape.batch, shape.n_kv_heads, shape.t_cap, shape.n_pages, shape.head_dim
+    names = _CACHE_NAMES if not what else tuple(f"{what}.{n}" for n in _CACHE_NAMES)
+    store = (B, H, cache.cap_groups, D // shape.n_groups)
+    if cache.v_packed is not None and cache.cap_groups == 0:          # (allocate() gives an empty store one row)
+        store = tuple(cache.v_packed.shape)
+    _sizes(names, cache.k, (B, H, T, D), cache.kmin, (B, H, P, D), cache.kmax, (B, H, P, D), cache.v_packed, store,
+           cache.v_mask, (B, H, T), cache.v_offs, (B, H, T + 1))
+    if cache.v_mask is not None and cache.v_mask.element_size() != 2 or cache.v_offs is not None and cache.v_offs.element_size() != 4:
+        raise ValueError("v_mask must hold 16-bit and v_offs 32-bit integers")
+
+
+def _check_tree(shape: Shape, tree: Tree) -> int:
+    n = tree.k.shape[2] if tree.k.dim() == 4 else -1
+    rows = (shape.batch, shape.n_kv_heads, n, shape.head_dim)
+    _sizes(("tree.k", "tree.v", "tree.parent", "tree.n_nodes"), tree.k, rows, tree.v, rows, tree.parent, (shape.batch, n),
+           tree.n_nodes, (shape.batch,))
+    return n
+
+
+def tree_attn(shape: Shape, cache: Cache, tree: Tree, q: torch.Tensor, page_ids: Optional[torch.Tensor],
+              n_pages: Optional[torch.Tensor], sm_scale: float, out: torch.Tensor, status: torch.Tensor, ws: torch.Tensor,
+              lse: Optional[torch.Tensor] = None, score: Optional[Score] = None) -> None:
+    """Every node of every sequence's tree attends the listed pages (None: all) of the sequence and its own ancestors.
+
+    q [B, n, Hq, 128] -> out f32 [B, n, Hq, 128], lse f32 [B, n, Hq]; score.q_pos i32 [B, n] or None (cache length + depth),
+    score.q_doc i32 [B]; status i32 [B]."""
+    dev, B, Hq, Hkv = _current_device(), shape.batch, shape.n_q_heads, shape.n_kv_heads
+    n = _check_tree(shape, tree)
+    max_pages = page_ids.shape[-1] if page_ids is not None else shape.n_pages
+    rows = (B, n, Hq, shape.head_dim)
+    _sizes(("q", "out", "lse", "page_ids", "n_pages", "status"), q, rows, out, rows, lse, (B, n, Hq), page_ids, (B, Hkv, max_pages),
+           n_pages, (B, Hkv), status, (B,))
+    co = score if score is not None else _PLAIN
+    _sizes(("slopes", "q_pos", "tok_doc", "q_doc"), co.slopes, (Hq,), co.q_pos, (B, n), co.tok_doc, (B, shape.t_cap), co.q_doc, (B,))
+    lp, kp, vp, mp, op, tkp, tvp, tpp, tnp, slp, pop, tdp, qdp, qp, ip, np_, outp, lsep, stp, wsp = _addresses(
+        dev, "ibb**bbiifiiibiiffiu", _TREE_NAMES, shape.seq_len, cache.k, cache.v_packed, cache.v_mask, cache.v_offs, tree.k, tree.v,
+        tree.parent, tree.n_nodes, co.slopes, co.q_pos, co.tok_doc, co.q_doc, q, page_ids, n_pages, out, lse, status, ws)
+    ip = _list_address(page_ids, ip, qp)
+    rc = load_library().stc_tree_attn(
+        _shape_bytes(shape, lp), _PACK_CACHE(kp, 0, 0, vp, mp, op, cache.cap_groups), _PACK_TREE(tkp, tvp, tpp, tnp, n, 0), qp, ip, np_,
+        max_pages, sm_scale, _PACK_SCORE(co.softcap, co.window, slp, pop, tdp, qdp), outp, lsep, stp, wsp, ws.numel(),
+        _raw_stream(dev))
+    if rc:
+        raise StcError(rc, "stc_tree_attn")
+
+
+_ACCEPT_NAMES = ("tokens", "parent", "n_nodes", "path", "n_accepted", "next_token")
+
+
+def tree_accept(logits: torch.Tensor, tokens: torch.Tensor, path: torch.Tensor, n_accepted: torch.Tensor,
+                next_token: torch.Tensor, parent: Optional[torch.Tensor] = None, n_nodes: Optional[torch.Tensor] = None) -> None:
+    """Greedy verification: follows argmax(logits) from node 0 through the tree while a child holds the chosen token.
+
+    logits bf16 or f32 [B, n, vocab] (a slice of wider rows allowed); tokens, parent, path i32 [B, n]; n_nodes, n_accepted,
+    next_token i32 [B]."""
+    if logits.dim() != 3 or logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"logits must be bfloat16 or float32 [B, n, vocab], got {logits.dtype} {tuple(logits.shape)}")
+    dev, (B, n, V) = _current_device(), logits.shape
+    if logits.get_device() != dev:
+        raise ValueError(f"logits is on {logits.device}, but the current device is cuda:{dev}")
+    sb, sn, sv = logits.stride()
+    step = sn if n > 1 else sb if B > 1 else V
+    if (V > 1 and sv != 1) or (B > 1 and sb != n * step):
+        raise ValueError(f"logits: a row must be contiguous and rows equally spaced, got strides {logits.stride()}")
+    _sizes(_ACCEPT_NAMES, tokens, (B, n), parent, (B, n), n_nodes, (B,), path, (B, n), n_accepted, (B,), next_token, (B,))
+    tp, pp, np_, hp, ap, xp = _addresses(dev, "iiiiii", _ACCEPT_NAMES, tokens, parent, n_nodes, path, n_accepted, next_token)
+    rc = load_library().stc_tree_accept(B, n, V, logits.data_ptr(), int(logits.dtype is torch.float32), step, tp, pp, np_, hp, ap, xp,
+                                        _raw_stream(dev))
+    if rc:
+        raise StcError(rc, "stc_tree_accept")
+
+
+_COMMIT_NAMES = ("seq_len", *_CACHE_NAMES, "tree.k", "tree.v", "tree.n_nodes", "path", "n_accepted", "new_len", "total_groups", "status")
+
+
+def tree_commit(shape: Shape, cache: Cache, tree: Tree, path: torch.Tensor, n_accepted: torch.Tensor, new_len: torch.Tensor,
+                total_groups: torch.Tensor, status: torch.Tensor) -> None:
+    """The accepted nodes path[b, :n_accepted[b]] become the tokens behind shape.seq_len[b] (the lengths before the call), at full
+    width, in cache.k and the packed store; new_len i32 [B] receives the lengths."""
+    dev, B, H = _current_device(), shape.batch, shape.n_kv_heads
+    n = _check_tree(shape, tree)
+    _check_cache(shape, cache)
+    _sizes(("path", "n_accepted", "new_len", "total_groups", "status"), path, (B, n), n_accepted, (B,), new_len, (B,), total_groups,
+           (B, H), status, (B, H))
+    lp, kp, lo, hi, vp, mp, op, tkp, tvp, tnp, pp, ap, np_, tp, sp = _addresses(
+        dev, "ibbbb**bbiiiili", _COMMIT_NAMES, shape.seq_len, cache.k, cache.kmin, cache.kmax, cache.v_packed, cache.v_mask, cache.v_offs,
+        tree.k, tree.v, tree.n_nodes, path, n_accepted, new_len, total_groups, status)
+    rc = load_library().stc_tree_commit(
+        _shape_bytes(shape, lp), _PACK_CACHE(kp, lo, hi, vp, mp, op, cache.cap_groups), _PACK_TREE(tkp, tvp, 0, tnp, n, 0), pp, ap, np_,
+        tp, sp, _raw_stream(dev))
+    if rc:
+        raise StcError(rc, "stc_tree_commit")
+
+
+_FORK_NAMES = ("seq_len", *("src." + n for n in _CACHE_NAMES), *("dst." + n for n in _CACHE_NAMES), "src_row", "dst_row", "new_len",
+               "total_groups", "status")
+
+
+def cache_fork(src_shape: Shape, src: Cache, dst_shape: Shape, dst: Cache, src_row: torch.Tensor, dst_row: torch.Tensor,
+               new_len: torch.Tensor, total_groups: torch.Tensor, status: torch.Tensor) -> None:
+    """Copies the sequences src_row[i] of src to the rows dst_row[i] of dst (which may be src); pairs of one source next to each
+    other share its reading.  new_len i32 [dst batch], total_groups i64 [dst batch, Hkv], status i32 [pairs, Hkv]."""
+    dev, n, B, H = _current_device(), src_row.shape[0], dst_shape.batch, dst_shape.n_kv_heads
+    _check_cache(src_shape, src, "src")
+    _check_cache(dst_shape, dst, "dst")
+    _sizes(("src_row", "dst_row", "new_len", "total_groups", "status"), src_row, (n,), dst_row, (n,), new_len, (B,), total_groups, (B, H),
+           status, (n, H))
+    at = _addresses(dev, "ibbbb**bbbb**iiili", _FORK_NAMES, src_shape.seq_len, src.k, src.kmin, src.kmax, src.v_packed, src.v_mask,
+                    src.v_offs, dst.k, dst.kmin, dst.kmax, dst.v_packed, dst.v_mask, dst.v_offs, src_row, dst_row, new_len, total_groups,
+                    status)
+    rc = load_library().stc_cache_fork(_shape_bytes(src_shape, at[0]), _PACK_CACHE(*at[1:7], src.cap_groups), _shape_bytes(dst_shape, 0),
+                                       _PACK_CACHE(*at[7:13], dst.cap_groups), n, *at[13:], _raw_stream(dev))
+    if rc:
+        raise StcError(rc, "stc_cache_fork")
+
+
+_COMPACT_NAMES = ("seq_len", *("src." + n for n in _CACHE_NAMES), *("dst." + n for n in _CACHE_NAMES), "page_ids", "n_pages", "new_len",
+                  "total_groups", "status")
+
+
+def cache_compact(shape: Shape, cache: Cache, page_ids: torch.Tensor, n_pages: torch.Tensor, new_len: torch.Tensor,
+                  total_groups: torch.Tensor, status: torch.Tensor, dst_shape: Optional[Shape] = None, dst: Optional[Cache] = None) -> None:
+    """Keeps the listed pages of every KV head, closed up, in dst (None: in place).  page_ids i32 [B, Hkv, max], ascending, n_pages
+    i32 [B, Hkv], new_len i32 [B], total_groups i64 [B, Hkv], status i32 [B, Hkv]."""
+    if (dst is None) != (dst_shape is None):
+        raise ValueError("cache_compact needs both dst_shape and dst, or neither")
+    to_shape, to = (shape, cache) if dst is None else (dst_shape, dst)
+    dev, B, H, most = _current_device(), shape.batch, shape.n_kv_heads, page_ids.shape[-1]
+    _check_cache(shape, cache)
+    if dst is not None:
+        _check_cache(dst_shape, dst, "dst")
+    _sizes(("page_ids", "n_pages", "new_len", "total_groups", "status"), page_ids, (B, H, most), n_pages, (B, H), new_len, (B,),
+           total_groups, (B, H), status, (B, H))
+    at = _addresses(dev, "ibbbb**bbbb**iiili", _COMPACT_NAMES, shape.seq_len, cache.k, cache.kmin, cache.kmax, cache.v_packed, cache.v_mask,
+                    cache.v_offs, to.k, to.kmin, to.kmax, to.v_packed, to.v_mask, to.v_offs, page_ids, n_pages, new_len, total_groups,
+                    status)
+    rc = load_library().stc_cache_compact(_shape_bytes(shape, at[0]), _PACK_CACHE(*at[1:7], cache.cap_groups), at[13], at[14], most,
+                                          _shape_bytes(to_shape, 0), _PACK_CACHE(*at[7:13], to.cap_groups), *at[15:], _raw_stream(dev))
+    if rc:
+        raise StcError(rc, "stc_cache_compact")
 
 
 def decode_step(shape: Shape, cache: Cache, q: torch.Tensor, token_budget: int, page_ids: torch.Tensor,

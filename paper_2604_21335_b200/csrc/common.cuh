@@ -257,6 +257,24 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
                                const int32_t* row_start, float sm_scale, const ScoreArgs* score, const float* own_out,
                                const float* own_lse, float* out, float* lse, void* ws, cudaStream_t st);
 
+size_t tree_attn_ws_bytes(const Geom& g, int n_cap);
+cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tree& tree, const void* q, const int32_t* page_ids,
+                             const int32_t* n_pages, int max_pages, float sm_scale, const ScoreArgs& score, float* out, float* lse,
+                             int32_t* status, void* ws, cudaStream_t st);
+cudaError_t launch_tree_accept(int B, int n_cap, int vocab, const void* logits, bool bf16, int64_t row_stride, const int32_t* tokens,
+                               const int32_t* parent, const int32_t* n_nodes, int32_t* path, int32_t* n_accepted,
+                               int32_t* next_token, cudaStream_t st);
+cudaError_t launch_tree_commit(const Geom& g, const stc_tree& tree, const int32_t* path, const int32_t* n_accepted, void* k,
+                               void* kmin, void* kmax, void* v_packed, uint16_t* v_mask, uint32_t* v_offs, int64_t cap_groups,
+                               int32_t* new_len, int64_t* total_groups, int32_t* status, cudaStream_t st);
+
+cudaError_t launch_cache_fork(const Geom& gs, const stc_cache& src, const Geom& gd, const stc_cache& dst, int n_pairs,
+                              const int32_t* src_row, const int32_t* dst_row, int32_t* new_len, int64_t* total_groups,
+                              int32_t* status, cudaStream_t st);
+cudaError_t launch_cache_compact(const Geom& gs, const stc_cache& src, const int32_t* page_ids, const int32_t* n_pages,
+                                 int max_pages, const Geom& gd, const stc_cache& dst, int32_t* new_len, int64_t* total_groups,
+                                 int32_t* status, cudaStream_t st);
+
 struct AttnPlan { int n_workers, slots_cap; };   // warps that share the pages; partial slots per problem
 AttnPlan attn_plan(const Geom& g, int max_pages);
 size_t attn_ws_bytes(const Geom& g, int max_pages);

@@ -80,6 +80,11 @@ int32_t stc_workspace_bytes(const stc_shape* shape, int32_t op, int64_t arg, siz
         *bytes_host = g.problems == 0 || arg == 0 ? 0 : prefix_ws_bytes(g);
         return STC_OK;
     }
+    if (op == STC_OP_TREE_ATTN) {                   // nodes attend their ancestors even where the cache has no tokens
+        if (arg < 0 || arg > STC_TREE_MAX_NODES) return STC_ERR_INVALID_ARG;
+        *bytes_host = g.problems == 0 || arg == 0 ? 0 : tree_attn_ws_bytes(g, (int)arg);
+        return STC_OK;
+    }
     if (empty(g)) { *bytes_host = 0; return STC_OK; }
     switch (op) {
         case STC_OP_QUEST_SELECT: *bytes_host = select_ws_bytes(g); break;
@@ -425,6 +430,121 @@ int32_t stc_prefix_attn(const stc_shape* shape, const stc_cache* cache, int32_t 
     return cuda_rc(launch_prefix_attn(g, cache->k, cache->v_packed, cache->v_mask, cache->v_offs, cache->cap_groups,
                                       n_rows, q, row_start, sm_scale, plain ? nullptr : &sc, own_out, own_lse, out,
                                       lse_opt, ws, static_cast<cudaStream_t>(stream)));
+}
+
+namespace {
+int32_t check_tree(const stc_tree* t) {
+    if (!t || t->reserved != 0 || t->n_cap < 1 || t->n_cap > STC_TREE_MAX_NODES) return STC_ERR_INVALID_ARG;
+    return STC_OK;
+}
+bool complete(const stc_cache* c) { return c->k && c->v_packed && c->v_mask && c->v_offs && c->cap_groups >= 0 && (!c->kmin) == (!c->kmax); }
+bool aligned(const stc_cache* c) { return aligned16(c->k, c->v_packed, c->kmin, c->kmax); }
+}  // namespace
+
+int32_t stc_tree_attn(const stc_shape* shape, const stc_cache* cache, const stc_tree* tree, const void* q,
+                      const int32_t* page_ids, const int32_t* n_pages, int32_t max_pages, float sm_scale,
+                      const stc_score* score, float* out, float* lse_opt, int32_t* status, void* ws, size_t ws_bytes,
+                      void* stream) {
+    Range nvtx_range("stc_tree_attn");
+    Geom g;
+    int32_t rc = make_geom(shape, &g);
+    if (rc == STC_OK) rc = check_tree(tree);
+    if (rc != STC_OK) return rc;
+    if (!cache || max_pages < 0 || !(sm_scale == sm_scale)) return STC_ERR_INVALID_ARG;
+    ScoreArgs sc;
+    bool plain;
+    rc = score_args(score, sm_scale, &sc, &plain);
+    if (rc != STC_OK) return rc;
+    if ((int64_t)g.problems * g.T > 0x7FFFFFFFLL || (int64_t)g.B * tree->n_cap * g.Hq > 0x7FFFFFFFLL)
+        return STC_ERR_UNSUPPORTED;
+    if (g.problems == 0) return STC_OK;
+    if (!q || !out || !status || !tree->k || !tree->v || (page_ids && !n_pages)) return STC_ERR_INVALID_ARG;
+    if (g.T > 0 && (!cache->k || !cache->v_packed || !cache->v_mask || !cache->v_offs || cache->cap_groups < 0))
+        return STC_ERR_INVALID_ARG;
+    if (!aligned16(cache->k, cache->v_packed, q, out, tree->k, tree->v)) return STC_ERR_INVALID_ARG;
+    rc = check_ws(ws, ws_bytes, tree_attn_ws_bytes(g, tree->n_cap));
+    if (rc != STC_OK) return rc;
+    return cuda_rc(launch_tree_attn(g, *cache, *tree, q, page_ids, n_pages, max_pages, sm_scale, sc, out, lse_opt, status, ws,
+                                    static_cast<cudaStream_t>(stream)));
+}
+
+int32_t stc_tree_accept(int32_t batch, int32_t n_cap, int32_t vocab, const void* logits, int32_t logits_type,
+                        int64_t row_stride, const int32_t* tokens, const int32_t* parent, const int32_t* n_nodes_opt,
+                        int32_t* path, int32_t* n_accepted, int32_t* next_token, void* stream) {
+    Range nvtx_range("stc_tree_accept");
+    if (batch < 0 || n_cap < 1 || n_cap > STC_TREE_MAX_NODES || vocab < 1 || row_stride < vocab ||
+        row_stride >= (int64_t)1 << 40 || (logits_type != STC_LOGITS_BF16 && logits_type != STC_LOGITS_F32))
+        return STC_ERR_INVALID_ARG;
+    if (batch >= 1 << 24) return STC_ERR_UNSUPPORTED;
+    if (batch == 0) return STC_OK;
+    if (!logits || !tokens || !path || !n_accepted || !next_token) return STC_ERR_INVALID_ARG;
+    const bool bf16 = logits_type == STC_LOGITS_BF16;
+    if ((reinterpret_cast<uintptr_t>(logits) & (bf16 ? 1u : 3u)) != 0) return STC_ERR_INVALID_ARG;
+    return cuda_rc(launch_tree_accept(batch, n_cap, vocab, logits, bf16, row_stride, tokens, parent, n_nodes_opt, path, n_accepted,
+                                      next_token, static_cast<cudaStream_t>(stream)));
+}
+
+int32_t stc_tree_commit(const stc_shape* shape, const stc_cache* cache, const stc_tree* tree, const int32_t* path,
+                        const int32_t* n_accepted, int32_t* new_len, int64_t* total_groups, int32_t* status,
+                        void* stream) {
+    Range nvtx_range("stc_tree_commit");
+    Geom g;
+    int32_t rc = make_geom(shape, &g);
+    if (rc == STC_OK) rc = check_tree(tree);
+    if (rc != STC_OK) return rc;
+    if (!cache) return STC_ERR_INVALID_ARG;
+    if (empty(g)) return STC_OK;
+    if (!complete(cache) || !tree->k || !tree->v || !path || !n_accepted || !new_len || !total_groups || !status ||
+        new_len == g.seq_len)
+        return STC_ERR_INVALID_ARG;
+    if (!aligned(cache) || !aligned16(tree->k, tree->v)) return STC_ERR_INVALID_ARG;
+    return cuda_rc(launch_tree_commit(g, *tree, path, n_accepted, const_cast<void*>(cache->k), cache->kmin, cache->kmax,
+                                      cache->v_packed, cache->v_mask, cache->v_offs, cache->cap_groups, new_len, total_groups,
+                                      status, static_cast<cudaStream_t>(stream)));
+}
+
+int32_t stc_cache_fork(const stc_shape* src_shape, const stc_cache* src, const stc_shape* dst_shape, const stc_cache* dst,
+                       int32_t n_pairs, const int32_t* src_row, const int32_t* dst_row, int32_t* new_len,
+                       int64_t* total_groups, int32_t* status, void* stream) {
+    Range nvtx_range("stc_cache_fork");
+    Geom gs, gd;
+    int32_t rc = make_geom(src_shape, &gs);
+    if (rc == STC_OK) rc = make_geom(dst_shape, &gd);
+    if (rc != STC_OK) return rc;
+    if (!src || !dst || n_pairs < 0 || gs.Hkv != gd.Hkv || gs.Hq != gd.Hq || gs.S != gd.S) return STC_ERR_INVALID_ARG;
+    if (n_pairs > 4096 || gs.Hkv > 65535) return STC_ERR_UNSUPPORTED;
+    if (n_pairs == 0 || empty(gs) || empty(gd)) return STC_OK;
+    if (!complete(src) || !complete(dst) || !src_row || !dst_row || !new_len || !total_groups || !status || new_len == gs.seq_len ||
+        (dst->kmin && !src->kmin))
+        return STC_ERR_INVALID_ARG;
+    if (src->k == dst->k && (gs.B != gd.B || gs.T != gd.T || src->v_packed != dst->v_packed || src->v_mask != dst->v_mask ||
+                             src->v_offs != dst->v_offs || src->cap_groups != dst->cap_groups))
+        return STC_ERR_INVALID_ARG;
+    if (!aligned(src) || !aligned(dst)) return STC_ERR_INVALID_ARG;
+    return cuda_rc(launch_cache_fork(gs, *src, gd, *dst, n_pairs, src_row, dst_row, new_len, total_groups, status,
+                                     static_cast<cudaStream_t>(stream)));
+}
+
+int32_t stc_cache_compact(const stc_shape* src_shape, const stc_cache* src, const int32_t* page_ids,
+                          const int32_t* n_pages, int32_t max_pages, const stc_shape* dst_shape, const stc_cache* dst,
+                          int32_t* new_len, int64_t* total_groups, int32_t* status, void* stream) {
+    Range nvtx_range("stc_cache_compact");
+    Geom gs, gd;
+    int32_t rc = make_geom(src_shape, &gs);
+    if (rc == STC_OK) rc = make_geom(dst_shape, &gd);
+    if (rc != STC_OK) return rc;
+    if (!src || !dst || max_pages < 0 || gs.B != gd.B || gs.Hkv != gd.Hkv || gs.Hq != gd.Hq || gs.S != gd.S)
+        return STC_ERR_INVALID_ARG;
+    if (empty(gs) || empty(gd)) return STC_OK;
+    if (!complete(src) || !complete(dst) || (max_pages > 0 && !page_ids) || !n_pages || !new_len || !total_groups || !status ||
+        new_len == gs.seq_len || (dst->kmin && !src->kmin))
+        return STC_ERR_INVALID_ARG;
+    if (src->k == dst->k && (gs.T != gd.T || src->kmin != dst->kmin || src->kmax != dst->kmax || src->v_packed != dst->v_packed ||
+                             src->v_mask != dst->v_mask || src->v_offs != dst->v_offs || src->cap_groups != dst->cap_groups))
+        return STC_ERR_INVALID_ARG;
+    if (!aligned(src) || !aligned(dst)) return STC_ERR_INVALID_ARG;
+    return cuda_rc(launch_cache_compact(gs, *src, page_ids, n_pages, max_pages, gd, *dst, new_len, total_groups, status,
+                                        static_cast<cudaStream_t>(stream)));
 }
 
 int32_t stc_decode_step(const stc_shape* shape, const stc_cache* cache, const void* q, int32_t token_budget,

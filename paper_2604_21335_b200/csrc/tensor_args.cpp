@@ -13,6 +13,7 @@ bool has_type(char code, at::ScalarType t) {
         case 'f': return t == at::kFloat;
         case 'd': return t == at::kDouble;
         case 'i': return t == at::kInt;
+        case 'l': return t == at::kLong;
         case 'u': return t == at::kByte;
         case '*': return true;
         default: return false;
