@@ -497,8 +497,8 @@ int32_t stc_prefix_attn(const stc_shape* shape, const stc_cache* cache, int32_t 
  * n_nodes[b] on are left as they were.  A NaN score of a token that a row sees makes the row NaN; what the row
  * does not see of the keys, and what no node of the sequence sees of the values, may hold anything; other values are to be
  * finite.  status i32 [B]: STC_OK, or STC_ERR_INVALID_ARG for a sequence one of whose parents is not in
- * [-1, node), which is left untouched.  batch * n_cap * n_q_heads and batch * n_kv_heads * t_cap must be below 2^31
- * (else STC_ERR_UNSUPPORTED).  Both products run on the tensor cores with fp32 accumulation, the weights enter
+ * [-1, node); such a parent counts as -1.  batch * n_cap * n_q_heads, batch * n_kv_heads * t_cap and the tiles of eight pages
+ * that the blocks of nodes take together must be below 2^31 (else STC_ERR_UNSUPPORTED).  Both products run on the tensor cores with fp32 accumulation, the weights enter
  * the second as a bf16 pair.  The same call gives the same bits.
  * ws: STC_OP_TREE_ATTN with arg = n_cap; its first int32 is a device status word the call writes: STC_OK, or
  * STC_ERR_TIMEOUT if a bounded wait expired on the device (it never should; out / lse are then unspecified). */

@@ -457,6 +457,9 @@ int32_t stc_tree_attn(const stc_shape* shape, const stc_cache* cache, const stc_
     if (rc != STC_OK) return rc;
     if ((int64_t)g.problems * g.T > 0x7FFFFFFFLL || (int64_t)g.B * tree->n_cap * g.Hq > 0x7FFFFFFFLL)
         return STC_ERR_UNSUPPORTED;
+    // tiles of the call, counted in 32 bits: eight pages each, for every block of at least 32 / 8 nodes
+    const int64_t most_pages = page_ids && max_pages > g.P ? max_pages : g.P;
+    if ((int64_t)g.problems * (most_pages / 8 + 2) > 0x7FFFFFFFLL / ((tree->n_cap + 3) / 4)) return STC_ERR_UNSUPPORTED;
     if (g.problems == 0) return STC_OK;
     if (!q || !out || !status || !tree->k || !tree->v || (page_ids && !n_pages)) return STC_ERR_INVALID_ARG;
     if (g.T > 0 && (!cache->k || !cache->v_packed || !cache->v_mask || !cache->v_offs || cache->cap_groups < 0))

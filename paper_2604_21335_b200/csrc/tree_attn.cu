@@ -1,127 +1,1126 @@
 // Attention for trees of drafted tokens over a routed cache.
 //
-//   Row r = (sequence b, node i, query head h):  softmax over the valid tokens of the listed pages and the nodes N_i (node i and
-//   its ancestors) of s = sm_scale * q.k (+ options of stc_score),  out = sum p v~,  lse = log sum exp s.
+//   Row r = (node i, query head) of a (sequence, KV head):  softmax over the valid tokens of the listed pages and the nodes N_i
+//   (node i and its ancestors) of s = sm_scale * q.k (+ options of stc_score),  out = sum p v~,  lse = log sum exp s.
 //
-// Simplest form: one warp per row, a lane owns four channels, tokens one by one with a running maximum.
-#include "common.cuh"
+// A tree has few rows (a node's query heads times the nodes) and a long cache, so the products are taken transposed: tokens are the 128
+// lanes of tensor memory and rows the columns, as many as there are.
+//   S[token][row] = K . Q^T       A = K tile of 128 tokens (8 pages, or the tree itself), B = Q, M = 128, N = rows, K = 128
+//   O[dim][row]  += V~^T . P^T    A = V~ tile (dims along M, rebuilt from the packed groups), B = P, M = 128, N = 2 rows, K = 128
+// A softmax thread owns a token and walks the rows, so every lane works whatever the number of rows, and a token that is hidden costs
+// a select; the sums of a row stay in the threads' registers until the end.  P enters as a bf16 high part next to a bf16
+// residual, two sets of columns of one product (V~ is read once for both) that are added at the end: one bf16 weight alone would
+// leave the fp32 output 2^-8 off, the pair leaves 2^-16.
+//
+// The running maximum of a row is shared by the tile's 128 threads.  It need not be exact: a tile only moves it when a score exceeds
+// it by more than 2^8 (a vote of the four warps); then the true maxima are taken across lanes, and sums and accumulator follow.
+//
+// Work split.  Unit = (sequence, KV head, block of nodes); its tiles are the tree (tile 0) and then eight listed pages each.  The tiles
+// of all units form one flat sequence that is cut into equal contiguous ranges, one per CTA (one CTA per SM).  A unit within
+// a range is finished in place; of others each CTA leaves (max, sum, accumulator), which a second kernel joins in CTA order:
+// no atomics, the same bits every time.
+//
+// Roles (16 warps): 0 = TMA producer of Q and K (two copies of 16 rows per page); 1 = MMA issuer; 2 = ancestors of the nodes as bit
+// masks (pointer doubling) and the rows' positions; 3 = scheduler; 4..7 and 8..11 = softmax of one half of the rows each; 12..15
+// rebuild the value tiles with 16-byte asynchronous copies straight from the packed store into the swizzled tile.
+//
+// The tensor core truncates when it adds to an accumulator (4e-8 of its value per product), so an accumulator is emptied into
+// fp32 sums every kFlush tiles.
+//
+// Every wait is bounded (about a second); one that expires raises a CTA-wide flag and STC_ERR_TIMEOUT in the status word, the
+// roles leave, the producer waits (bounded) for its copies, tensor memory is freed.
+#include <type_traits>
+
+#include "umma.cuh"
 
 namespace stc {
 namespace {
 
-constexpr int kThreads = 128;
+constexpr int kTok = 128;                         // tokens per tile = tensor-memory lanes
+constexpr int kTilePages = kTok / kPage;
+constexpr int kThreads = 512;
+constexpr int kSegs = 2;                          // segments the scheduler may be ahead
+constexpr int kSegReaders = 15;                   // warps that follow the segments: all but the scheduler
+constexpr uint32_t kHalf = kTok * 128;            // 64 channels of a token tile: 128 rows of 128 bytes
+constexpr uint32_t kTile = 2 * kHalf;             // 32 KiB
+constexpr int kFlush = 16;                        // tiles an accumulator takes: 128 products, at most 5e-6 of it
+constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kSlack = 8.f;                     // log2 units a maximum may be exceeded by
+constexpr float kUnset = -3.0e38f;                // maximum of a row that has seen nothing: every finite score exceeds it
+
+// barriers, in 8-byte words of the control block
+enum { kQFull, kQEmpty, kKFull, kKEmpty = kKFull + 3, kVFull = kKEmpty + 3, kVEmpty = kVFull + 2, kSFull = kVEmpty + 2,
+       kPFull = kSFull + 2, kOFull = kPFull + 2, kGroup = kOFull + 2, kTabFull = kGroup + 2, kTabEmpty, kSegFull,
+       kSegEmpty = kSegFull + kSegs, kBars = kSegEmpty + kSegs };
+constexpr uint32_t kCtlTmem = 256, kCtlAbort = 260, kCtlVotes = 264, kCtlSegs = 288, kCtlMax = 384;
+static_assert(kBars * 8 <= kCtlTmem && kCtlSegs + kSegs * 48 <= kCtlMax, "control block");
+
+// Shared memory of a CTA with N rows.
+template <int N>
+struct Plan {
+    static constexpr int kKStages = N == 32 ? 3 : 2, kVStages = 2, kPBuffers = N == 128 ? 1 : 2;
+    static constexpr uint32_t kQHalf = N * 128, kP = kTok * 2 * N * 2;
+    static constexpr uint32_t kOffK = 2 * kQHalf, kOffV = kOffK + kKStages * kTile, kOffP = kOffV + kVStages * kTile;
+    static constexpr uint32_t kOffCtl = kOffP + kPBuffers * kP;
+    static constexpr uint32_t kCtlKin = kCtlMax + N * 4;                                   // [128 nodes][4 words]
+    static constexpr uint32_t kCtlScratch = kCtlKin + STC_TREE_MAX_NODES * 16;             // [2 groups][4 warps][32], positions, row tables
+    static constexpr uint32_t kCtlPos = kCtlScratch + 1024, kCtlRowPos = kCtlPos + 512, kCtlRowSlope = kCtlRowPos + 256;
+    static constexpr uint32_t kCtlBytes = N == 128 ? kCtlScratch : kCtlRowSlope + 256;
+    static constexpr uint32_t kSmem = kOffCtl + kCtlBytes;
+    static_assert(kSmem <= 232448, "shared memory of a block");
+};
 
 struct TreeArgs {
-    const uint2* q;
-    const uint2* k;
-    const uint2* k_new;
-    const uint2* v_new;
-    const __nv_bfloat16* v_packed;
+    const int32_t* seq_len;
+    const int32_t* n_nodes;
+    const int32_t* parent;       // or nullptr: a chain
+    const int32_t* page_ids;     // or nullptr: all pages
+    const int32_t* n_pages;
     const uint16_t* v_mask;
     const uint32_t* v_offs;
-    const int32_t* seq_len;
-    const int32_t* parent;
-    const int32_t* n_nodes;
-    const int32_t* page_ids;
-    const int32_t* n_pages;
+    const uint4* v_packed;
+    const uint4* v_new;
     float* out;
-    float* lse;
-    int32_t* status;
-    int32_t* word;
+    float* lse;                  // or nullptr
+    int32_t* status;             // [B]
+    int32_t* word;               // the call's status word
+    int32_t* cta_status;         // [grid]
+    int32_t* base;               // [problems + 2]: where each problem begins in the flat sequence; its length; CTAs that share it
+    float2* part_ml;             // [2 * grid][N]
+    float* part_o;               // [2 * grid][N][128]
+    float* flush;                // [grid][N][128]: sums of emptied accumulators
     int64_t cap_groups;
-    int B, Hq, Hkv, Gq, T, P, S, n_cap, max_pages;
-    float scale;
+    int B, Hq, Hkv, Gq, S, T, n_cap, max_pages, problems;
+    int block_nodes;             // nodes per block of rows = N / Gq
+    uint32_t gq_inv;             // row / Gq = row * gq_inv >> 16 for rows below 128
+    float scale_log2, cap_in, cap_log2;
+    uint32_t window;             // tokens a row sees, 0xFFFFFFFF without a window
     ScoreArgs sc;
 };
 
-__global__ void __launch_bounds__(kThreads) tree_attn_kernel(const TreeArgs a) {
-    const long long row = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.word = STC_OK;
-    if (row >= (long long)a.B * a.n_cap * a.Hq) return;
-    const int h = (int)(row % a.Hq), node = (int)(row / a.Hq % a.n_cap), b = (int)(row / a.Hq / a.n_cap);
-    const int len = clamp_len(a.seq_len, b, a.T), n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.n_cap) : a.n_cap;
-    const int32_t* parent = a.parent ? a.parent + (size_t)b * a.n_cap : nullptr;
-    bool bad = false;
-    for (int i = lane; i < n && parent; i += 32) bad |= parent[i] < -1 || parent[i] >= i;
-    bad = __any_sync(0xFFFFFFFFu, bad);
-    if (h == 0 && node == 0 && lane == 0) a.status[b] = bad ? STC_ERR_INVALID_ARG : STC_OK;
-    if (bad || node >= n) return;
-    auto up = [&](int i) { return parent ? parent[i] : i - 1; };
-    auto depth = [&](int i) { int d = 0; for (i = up(i); i >= 0; i = up(i)) ++d; return d; };
-    auto pos_of = [&](int i) { return a.sc.q_pos ? a.sc.q_pos[(size_t)b * a.n_cap + i] : len + depth(i); };
-    const int hk = h / a.Gq, pos = pos_of(node);
-    const size_t problem = (size_t)b * a.Hkv + hk;
-    const float slope = a.sc.slopes ? a.sc.slopes[h] : 0.f;
-    const uint2 qw = a.q[(size_t)row * 32 + lane];
-    float m = -INFINITY, l = 0.f, o[4] = {};
-    auto take = [&](uint2 kw, const float (&v)[4], int t) {
-        float s = bf16lo(qw.x) * bf16lo(kw.x);
-        s = fmaf(bf16hi(qw.x), bf16hi(kw.x), s);
-        s = fmaf(bf16lo(qw.y), bf16lo(kw.y), s);
-        s = fmaf(bf16hi(qw.y), bf16hi(kw.y), s);
+__device__ __forceinline__ int nodes_of(const TreeArgs& a, int b) {
+    return a.n_nodes ? min(max(a.n_nodes[b], 0), a.n_cap) : a.n_cap;
+}
+// Pages that a problem attends: `list` of them, from `first` on where there is no list (nothing before it is in the window).
+__device__ __forceinline__ void pages_of(const TreeArgs& a, int problem, int len, int& list, int& first) {
+    first = 0;
+    if (a.page_ids) {
+        list = min(max(a.n_pages[problem], 0), a.max_pages);
+        return;
+    }
+    if (a.sc.window > 0 && !a.sc.q_pos && len >= a.sc.window) first = (len - a.sc.window + 1) / kPage;
+    list = (len + kPage - 1) / kPage - first;
+}
+struct Unit { int tiles, blocks; };              // tiles of a unit of the problem (the tree's among them), units
+__device__ __forceinline__ Unit unit_of(const TreeArgs& a, int nodes, int list) {
+    return Unit{1 + (list + kTilePages - 1) / kTilePages, (nodes + a.block_nodes - 1) / a.block_nodes};
+}
+__device__ __forceinline__ int problem_length(const TreeArgs& a, int problem) {
+    const int b = problem / a.Hkv, nodes = nodes_of(a, b);
+    int list, first;
+    pages_of(a, problem, clamp_len(a.seq_len, b, a.T), list, first);
+    const Unit u = unit_of(a, nodes, list);
+    return u.tiles * u.blocks;
+}
+// CTA `c` of `n` takes the positions [total * c / n, total * (c + 1) / n) of the flat sequence.
+__device__ __forceinline__ int range_begin(int total, int c, int n) { return (int)((long long)total * c / n); }
+__device__ __forceinline__ int cta_of(int total, int x, int n) { return (int)((((long long)x + 1) * n + total - 1) / total - 1); }
+
+// One segment: tiles [tile0, tile1) of one unit.
+struct Segment {
+    int b, hk, node0, nodes, len, list, first, tile0, tile1;
+    int slot;                    // partial slot, -1 = the whole unit
+};
+
+__device__ __forceinline__ float redux_max(float v) {
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ void sts16(uint32_t addr, const uint32_t (&v)[4]) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+__device__ __forceinline__ float cap_score(float x, float cap_in, float cap_log2) {
+    const float z = x * cap_in, lo = tanh_small(z), hi = tanh_large(z);
+    return cap_log2 * (fabsf(z) <= kTanhSmall ? lo : hi);
+}
+// COLS consecutive columns of the warp's 32 lanes.
+template <int COLS>
+__device__ __forceinline__ void tmem_ld(uint32_t addr, uint32_t (&r)[COLS]) {
+    tmem_ld16<0>(addr, r);
+    if constexpr (COLS > 16) tmem_ld16<16>(addr + 16, r);
+}
+
+// N rows; SCORE: the options of stc_score, positions, or a scale that is not positive.
+template <int N, bool SCORE>
+__global__ void __launch_bounds__(kThreads, 1)
+tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                 const __grid_constant__ CUtensorMap map_new, const TreeArgs a) {
+    using L = Plan<N>;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const uint32_t base = smem_u32(smem);
+    const uint32_t bars = base + L::kOffCtl;
+    unsigned char* const ctl = smem + L::kOffCtl;
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctl + kCtlTmem);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + kCtlAbort);
+    volatile uint32_t* votes = reinterpret_cast<volatile uint32_t*>(ctl + kCtlVotes);       // [2 groups][2]
+    volatile int* segs = reinterpret_cast<volatile int*>(ctl + kCtlSegs);                   // [kSegs][12]
+    float* const row_max = reinterpret_cast<float*>(ctl + kCtlMax);                         // [N], log2 units
+    uint32_t* const kin = reinterpret_cast<uint32_t*>(ctl + L::kCtlKin);
+    int* const node_pos = reinterpret_cast<int*>(ctl + (N == 128 ? 0 : L::kCtlPos));        // (SCORE has N <= 64)
+    int* const row_pos = reinterpret_cast<int*>(ctl + (N == 128 ? 0 : L::kCtlRowPos));
+    float* const row_slope = reinterpret_cast<float*>(ctl + (N == 128 ? 0 : L::kCtlRowSlope));
+    static_assert(!(SCORE && N == 128), "no room for the row tables");
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    asm volatile("griddepcontrol.launch_dependents;");
+
+    // ---- set-up: barriers, tensor memory, and where this CTA's range begins -----------------------------------------------
+    if (warp == 0 && lane < 3)
+        asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_new) : "memory");
+    if (threadIdx.x >= 64 && threadIdx.x < 64 + kBars) {
+        const int i = (int)threadIdx.x - 64;
+        mbar_init(bars + 8 * i, i >= kVFull && i < kVEmpty ? 4 : i >= kPFull && i < kOFull ? 8 : i >= kGroup && i < kTabFull ? 4
+                                : i == kTabEmpty ? 8 : i >= kSegEmpty ? kSegReaders : 1);
+        fence_mbar_init();
+    }
+    if (threadIdx.x < 4) votes[threadIdx.x] = 0;
+    if (threadIdx.x == 4) *abort_flag = (base & 1023u) != 0 ? (int)STC_ERR_CUDA : 0;        // swizzled tiles need 1024-byte aligned bases
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(bars + kCtlTmem), "r"(4u * N) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    const int per = (a.problems + kThreads - 1) / kThreads;
+    const int p_lo = min((int)threadIdx.x * per, a.problems), p_hi = min(p_lo + per, a.problems);
+    int mine = 0;
+    for (int p = p_lo; p < p_hi; ++p) mine += problem_length(a, p);
+    const int incl = (int)warp_incl_scan((uint32_t)mine, lane);
+    volatile int* const sums = reinterpret_cast<volatile int*>(kin);      // [16] of the warps, then problem and offset of the range
+    if (lane == 31) sums[warp] = incl;
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = *tmem_slot;
+    int total = 0, n_cta, x_begin, x_end;
+    {
+        int before = incl - mine;
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
-        s *= a.scale;
-        if (a.sc.softcap > 0.f) s = a.sc.softcap * tanh_f32(s / a.sc.softcap);
-        s += slope * (float)(t - pos);
-        const float top = s > m ? s : m, f = m == -INFINITY ? 0.f : expf(m - top), w = s == -INFINITY ? 0.f : expf(s - top);
-        l = fmaf(l, f, w);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = fmaf(o[e], f, w * v[e]);
-        m = top;
-    };
-    auto hidden = [&](int t) { return t > pos || (a.sc.window > 0 && pos - t >= a.sc.window); };
-    const int pages = (len + kPage - 1) / kPage, listed = a.page_ids ? min(max(a.n_pages[problem], 0), a.max_pages) : pages;
-    for (int i = 0; i < listed; ++i) {
-        const int page = a.page_ids ? a.page_ids[problem * a.max_pages + i] : i;
-        if (page < 0 || page >= pages) continue;
-        for (int t = page * kPage; t < min(len, (page + 1) * kPage); ++t) {
-            if (hidden(t)) continue;
-            if (a.sc.tok_doc) {
-                const int d = a.sc.tok_doc[(size_t)b * a.T + t];
-                if (d >= 0 && d != a.sc.q_doc[b]) continue;
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w < warp) before += sums[w];
+            total += sums[w];
+        }
+        n_cta = min(total, (int)gridDim.x);
+        x_begin = x_end = 0;
+        if ((int)blockIdx.x < n_cta) {
+            x_begin = range_begin(total, (int)blockIdx.x, n_cta);
+            x_end = range_begin(total, (int)blockIdx.x + 1, n_cta);
+        }
+        if ((x_begin < x_end && before <= x_begin && x_begin < before + mine) || blockIdx.x == 0) {
+            int at = before;
+            for (int p = p_lo; p < p_hi; ++p) {
+                const int n = problem_length(a, p);
+                if (x_begin < x_end && at <= x_begin && x_begin < at + n) {
+                    sums[16] = p;
+                    sums[17] = x_begin - at;
+                }
+                if (blockIdx.x == 0) a.base[p] = at;
+                at += n;
             }
-            const uint32_t mask = a.v_mask[problem * a.T + t];
-            const int g = kHeadDim / a.S, grp = 4 * lane / g;
-            const int64_t at = (int64_t)a.v_offs[problem * (a.T + 1) + t] + __popc(mask & ((1u << grp) - 1u));
-            float v[4] = {};
-            if ((mask >> grp & 1u) && at < a.cap_groups)
-                for (int e = 0; e < 4; ++e) v[e] = __bfloat162float(a.v_packed[(problem * a.cap_groups + at) * g + (4 * lane) % g + e]);
-            take(a.k[(problem * a.T + t) * 32 + lane], v, t);
+        }
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            a.base[a.problems] = total;
+            a.base[a.problems + 1] = n_cta;
         }
     }
-    for (int i = node; i >= 0; i = up(i)) {
-        const int t = pos_of(i);
-        if (hidden(t)) continue;
-        const uint2 vw = a.v_new[(problem * a.n_cap + i) * 32 + lane];
-        const float v[4] = {bf16lo(vw.x), bf16hi(vw.x), bf16lo(vw.y), bf16hi(vw.y)};
-        take(a.k_new[(problem * a.n_cap + i) * 32 + lane], v, t);
+    __syncthreads();
+    const int p_first = sums[16], x_first = sums[17];
+    __syncthreads();                                 // (the ancestors' table takes their place)
+
+    auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
+    auto warp_wait = [&](int i, uint32_t phase) { return mbar_warp_wait_or_abort(bar(i), phase & 1u, abort_flag, kWaitNs); };
+    auto give_up = [&]() { atomicCAS(const_cast<int*>(abort_flag), 0, (int)STC_ERR_TIMEOUT); };
+    Segment s;
+    int n_seg = 0;
+    // the next segment, for a whole warp; false at the end
+    auto next = [&](bool& good) -> bool {
+        good = warp_wait(kSegFull + n_seg % kSegs, (uint32_t)(n_seg / kSegs));
+        if (!good) return false;
+        volatile int* e = segs + (n_seg % kSegs) * 12;
+        s.b = e[0]; s.hk = e[1]; s.node0 = e[2]; s.nodes = e[3]; s.len = e[4]; s.list = e[5]; s.first = e[6];
+        s.tile0 = e[7]; s.tile1 = e[8]; s.slot = e[9];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kSegEmpty + n_seg % kSegs));
+        ++n_seg;
+        return s.tile1 >= 0;
+    };
+    // page of list entry j of the segment's problem, -1 where there is none
+    auto page_at = [&](int j) {
+        if (j < 0 || j >= s.list) return -1;
+        const int id = a.page_ids ? __ldg(a.page_ids + (size_t)(s.b * a.Hkv + s.hk) * a.max_pages + j) : s.first + j;
+        return id >= 0 && id < (s.len + kPage - 1) / kPage ? id : -1;
+    };
+
+    if (*abort_flag) {
+        // nothing was started
+    } else if (warp == 0) {
+        // ---- producer of Q and K ---------------------------------------------------------------------------
+        int kc = 0, seg = 0;
+        bool ok = true;
+        const uint32_t q_bytes = 2u * 128u * (uint32_t)(a.Gq * a.block_nodes);
+        while (ok && next(ok)) {
+            const int problem = s.b * a.Hkv + s.hk;
+            auto fetch = [&](int t) { return lane < kTilePages && t > 0 ? page_at((t - 1) * kTilePages + lane) : -1; };
+            int id = fetch(s.tile1 - 1);
+            bool q_due = true;
+#pragma unroll 1
+            for (int t = s.tile1 - 1; t >= s.tile0; --t) {
+                const int id_next = t > s.tile0 ? fetch(t - 1) : -1;
+                const int st = kc % L::kKStages;
+                if (kc >= L::kKStages) ok = warp_wait(kKEmpty + st, (uint32_t)(kc / L::kKStages - 1));
+                if (!ok) break;
+                const bool mine_too = t > 0 ? id >= 0 : lane < (s.nodes + kPage - 1) / kPage;
+                const int boxes = __popc(__ballot_sync(0xFFFFFFFFu, mine_too));
+                if (lane == 0) mbar_expect_tx(bar(kKFull + st), (uint32_t)boxes * kPage * kRowBytes);
+                __syncwarp();
+                if (mine_too) {
+                    const uint32_t dst = base + L::kOffK + st * kTile + (uint32_t)lane * kPage * 128u;
+                    const CUtensorMap* map = t > 0 ? &map_k : &map_new;
+                    const int y = t > 0 ? problem * a.T + id * kPage : problem * a.n_cap + lane * kPage;
+                    tma_2d(dst, map, 0, y, bar(kKFull + st));
+                    tma_2d(dst + kHalf, map, 64, y, bar(kKFull + st));
+                }
+                ++kc;
+                id = id_next;
+                if (q_due) {                         // the queries behind the first keys, which come from farther away
+                    q_due = false;
+                    if (seg > 0) ok = warp_wait(kQEmpty, (uint32_t)(seg - 1));
+                    if (!ok) break;
+                    if (lane == 0) {
+                        mbar_expect_tx(bar(kQFull), q_bytes);
+                        tma_3d(base, &map_q, 0, s.hk * a.Gq, s.b * a.n_cap + s.node0, bar(kQFull));
+                        tma_3d(base + L::kQHalf, &map_q, 64, s.hk * a.Gq, s.b * a.n_cap + s.node0, bar(kQFull));
+                    }
+                    __syncwarp();
+                    ++seg;
+                }
+            }
+        }
+        if (!ok) give_up();
+        if (*abort_flag) {                           // copies still in flight get one more bounded wait each
+            int none = 0;
+            if (seg > 0) mbar_wait_or_abort(bar(kQFull), (uint32_t)(seg - 1) & 1u, &none, kWaitNs);
+            for (int i = max(0, kc - L::kKStages); i < kc; ++i)
+                mbar_wait_or_abort(bar(kKFull + i % L::kKStages), (uint32_t)(i / L::kKStages) & 1u, &none, kWaitNs);
+        }
+    } else if (warp == 1) {
+        // ---- MMA issuer: the warp stays together, an elected lane issues ------------------------------------------
+        constexpr uint32_t id_s = idesc_bf16(kTok, N, false), id_o = idesc_bf16(kHeadDim, 2 * N, true) | 1u << 15;   // (A M-major)
+        const uint32_t sm = uniform(base), ts = uniform(tmem), to = ts + 2 * N;
+        uint32_t tile = 0, seg = 0;                  // tiles of the segments before; segments before
+        bool ok = true;
+        while (ok && next(ok)) {
+            const int tiles = uniform(s.tile1 - s.tile0);
+            ok = warp_wait(kQFull, seg);
+            // iteration n: O += V~^T P^T of tile n - 2, whose S buffer then takes S = K Q^T of tile n
+#pragma unroll 1
+            for (int n = 0; ok && n < tiles + 2; ++n) {
+                if (n >= 2) {
+                    const uint32_t j = tile + (uint32_t)(n - 2), st = j % L::kVStages, buf = j & 1u;
+                    ok = warp_wait(kPFull + buf, j >> 1) && warp_wait(kVFull + st, j / L::kVStages);
+                    if (!ok) break;
+                    tc_after();
+                    const uint64_t dv = smem_desc_128(sm + L::kOffV + st * kTile, kHalf);
+                    const uint64_t dp = smem_desc_128(sm + L::kOffP + (L::kPBuffers > 1 ? buf * L::kP : 0u), kHalf);
+                    const uint32_t more = n > 2 && (n - 2) % kFlush != 0;                  // else O starts anew
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)  // 16 tokens: 16 rows of 128 bytes in both
+                            tc_mma_ss(to, dv + (uint64_t)(k * (2048 >> 4)), dp + (uint64_t)(k * (2048 >> 4)), id_o, k ? 1u : more);
+                        tc_commit_to(bar(kOFull + buf));
+                        tc_commit_to(bar(kVEmpty + st));
+                    }
+                    __syncwarp();
+                }
+                if (n < tiles) {
+                    const uint32_t j = tile + (uint32_t)n, st = j % L::kKStages, buf = j & 1u;
+                    ok = warp_wait(kKFull + st, j / L::kKStages);
+                    if (!ok) break;
+                    tc_after();
+                    const uint64_t dk = smem_desc_128(sm + L::kOffK + st * kTile, 16), dq = smem_desc_128(sm, 16);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)  // 16 dims = 32 bytes = 2 units; 64 dims = one half tile
+                            tc_mma_ss(ts + buf * N, dk + (uint64_t)((k >> 2) * (kHalf >> 4) + (k & 3) * 2),
+                                      dq + (uint64_t)((k >> 2) * (L::kQHalf >> 4) + (k & 3) * 2), id_s, k != 0);
+                        tc_commit_to(bar(kSFull + buf));
+                        tc_commit_to(bar(kKEmpty + st));
+                        if (n == tiles - 1) tc_commit_to(bar(kQEmpty));
+                    }
+                    __syncwarp();
+                }
+            }
+            tile += (uint32_t)tiles;
+            ++seg;
+        }
+        if (!ok) give_up();
+    } else if (warp == 2) {
+        // ---- ancestors of the nodes as bit masks, positions of the rows ---------------------------------------------
+        uint32_t used = 0;
+        bool ok = true;
+        while (ok && next(ok)) {
+            if (!SCORE && s.tile0 > 0) continue;     // nobody asks
+            int up[4];
+            uint32_t m[4][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int node = i * 32 + lane;
+                up[i] = -1;
+                if (node < s.nodes) {
+                    up[i] = a.parent ? a.parent[(size_t)s.b * a.n_cap + node] : node - 1;
+                    if (up[i] < 0 || up[i] >= node) up[i] = -1;
+                }
+#pragma unroll
+                for (int w = 0; w < 4; ++w) m[i][w] = w == i ? 1u << lane : 0u;
+            }
+            if (used > 0) ok = warp_wait(kTabEmpty, used - 1);
+            if (!ok) break;
+            // kin[n]: n and its ancestors up to the one `up` points at, twice as many each time
+            uint4* const table = reinterpret_cast<uint4*>(kin);
+#pragma unroll 1
+            for (;;) {
+                bool going = false;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    table[i * 32 + lane] = make_uint4(m[i][0], m[i][1], m[i][2], m[i][3]);
+                    going |= up[i] >= 0;
+                }
+                __syncwarp();
+                if (!__any_sync(0xFFFFFFFFu, going)) break;
+                int next_up[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    // the node that `up` points at: its mask, and where its pointer goes (held by its lane)
+                    const uint4 t = table[max(up[i], 0)];
+                    int to[4];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) to[w] = __shfl_sync(0xFFFFFFFFu, up[w], max(up[i], 0) & 31);
+                    const int which = max(up[i], 0) >> 5;
+                    next_up[i] = up[i] < 0 ? -1 : which == 0 ? to[0] : which == 1 ? to[1] : which == 2 ? to[2] : to[3];
+                    if (up[i] >= 0) { m[i][0] |= t.x; m[i][1] |= t.y; m[i][2] |= t.z; m[i][3] |= t.w; }
+                }
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) up[i] = next_up[i];
+            }
+            if constexpr (SCORE) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int node = i * 32 + lane;
+                    const int depth = __popc(m[i][0]) + __popc(m[i][1]) + __popc(m[i][2]) + __popc(m[i][3]) - 1;
+                    node_pos[node] = a.sc.q_pos && node < s.nodes ? a.sc.q_pos[(size_t)s.b * a.n_cap + node] : s.len + depth;
+                }
+                __syncwarp();
+                for (int r = lane; r < N; r += 32) {
+                    const int in_block = (int)(((uint32_t)r * a.gq_inv) >> 16), node = min(s.node0 + in_block, STC_TREE_MAX_NODES - 1);
+                    row_pos[r] = node_pos[node];
+                    row_slope[r] = a.sc.slopes ? a.sc.slopes[s.hk * a.Gq + (r - in_block * a.Gq)] * kLog2e : 0.f;
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kTabFull));
+            ++used;
+        }
+        if (!ok) give_up();
+    } else if (warp == 3) {
+        // ---- scheduler: walks the CTA's range, segment by segment -----------------------------------------------------
+        if (lane == 0) {
+            bool ok = true;
+            int x = x_begin, p = p_first, off = x_first;
+            for (int i = 0; ok; ++i) {
+                Segment g = {};
+                g.tile1 = -1;
+                while (x < x_end) {
+                    g.b = p / a.Hkv;
+                    g.hk = p - g.b * a.Hkv;
+                    g.len = clamp_len(a.seq_len, g.b, a.T);
+                    g.nodes = nodes_of(a, g.b);
+                    pages_of(a, p, g.len, g.list, g.first);
+                    const Unit u = unit_of(a, g.nodes, g.list);
+                    if (off >= u.tiles * u.blocks) {
+                        off -= u.tiles * u.blocks;
+                        ++p;
+                        continue;
+                    }
+                    const int blk = off / u.tiles;
+                    g.tile0 = off - blk * u.tiles;
+                    g.tile1 = min(u.tiles, g.tile0 + (x_end - x));
+                    g.node0 = blk * a.block_nodes;
+                    // a CTA continues at most one unit (slot 0) and leaves at most one that it begins (slot 1)
+                    g.slot = g.tile1 - g.tile0 == u.tiles ? -1 : 2 * (int)blockIdx.x + (g.tile0 == 0 ? 1 : 0);
+                    x += g.tile1 - g.tile0;
+                    off += g.tile1 - g.tile0;
+                    break;
+                }
+                if (i >= kSegs) ok = mbar_wait_or_abort(bar(kSegEmpty + i % kSegs), (uint32_t)(i / kSegs - 1) & 1u, abort_flag, kWaitNs);
+                if (!ok) break;
+                volatile int* e = segs + (i % kSegs) * 12;
+                e[0] = g.b; e[1] = g.hk; e[2] = g.node0; e[3] = g.nodes; e[4] = g.len; e[5] = g.list; e[6] = g.first;
+                e[7] = g.tile0; e[8] = g.tile1; e[9] = g.slot;
+                mbar_arrive(bar(kSegFull + i % kSegs));
+                if (g.tile1 < 0) break;
+            }
+            if (!ok) give_up();
+        }
+    } else if (warp < 12) {
+        // ---- softmax: thread = token of the tile, group = half of the rows ------------------------------------------------
+        constexpr int kRows = N / 2, kCols = kRows < 32 ? kRows : 32, kChunks = kRows / kCols;
+        const int grp = (warp - 4) >> 2, quarter = warp & 3, tok = quarter * 32 + lane;
+        const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
+        const uint32_t to = lane_base + 2 * N + grp * kRows;                  // this group's columns of O; the residual's N further on
+        // where the warps of the group meet: maxima and sums of 32 rows each.  With N = 128 that is the group's own part of P.
+        float* const scratch = reinterpret_cast<float*>(N == 128 ? smem + L::kOffP + grp * kHalf : ctl + L::kCtlScratch + grp * 512);
+        float* const my_max = row_max + grp * kRows;
+        float* const my_flush = a.flush + ((size_t)blockIdx.x * N + grp * kRows) * kHeadDim + tok;
+        uint32_t j = 0, meets = 0, tabs = 0;
+        bool ok = true;
+        auto meet = [&]() {                          // the four warps of the group
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kGroup + grp));
+            return warp_wait(kGroup + grp, meets++);
+        };
+
+        auto segment = [&]() {
+            const int live = min(a.block_nodes, s.nodes - s.node0) * a.Gq;    // rows of the block
+            const bool tables = SCORE || s.tile0 == 0;
+            float2 l[kRows / 2];                     // sums of this thread's tokens
+#pragma unroll
+            for (int i = 0; i < kRows / 2; ++i) l[i] = make_float2(0.f, 0.f);
+            if (tok < kRows) my_max[tok] = grp * kRows + tok < live ? kUnset : INFINITY;   // (nothing exceeds it)
+            if (SCORE) {
+                ok = warp_wait(kTabFull, tabs);
+                if (!ok) return;
+            }
+            ok = meet();
+            if (!ok) return;
+            int id = s.tile1 > 1 ? page_at((s.tile1 - 2) * kTilePages + (tok >> 4)) : -1;
+            const int q_doc = SCORE && a.sc.tok_doc ? a.sc.q_doc[s.b] : 0;
+            const int count = s.tile1 - s.tile0;
+#pragma unroll 1
+            for (int n = 0; n < count; ++n, ++j) {
+                const int t = s.tile1 - 1 - n;
+                const uint32_t buf = j & 1u, ts = lane_base + buf * N + grp * kRows;
+                const int id_next = n + 1 < count ? page_at((t - 2) * kTilePages + (tok >> 4)) : -1;
+                // this thread's token
+                int pos = id * kPage + (tok & 15);
+                bool valid = id >= 0 && pos < s.len;
+                if (t == 0) {
+                    valid = tok < s.nodes;
+                    if (!SCORE) {
+                        ok = warp_wait(kTabFull, tabs);
+                        if (!ok) return;
+                    } else {
+                        pos = node_pos[tok];
+                    }
+                }
+                if (SCORE && a.sc.tok_doc && t > 0 && valid) {
+                    const int d = __ldg(a.sc.tok_doc + (size_t)s.b * a.T + pos);
+                    valid = d < 0 || d == q_doc;
+                }
+                const bool all_valid = __all_sync(0xFFFFFFFFu, valid) && t > 0;
+                ok = warp_wait(kSFull + buf, j >> 1);
+                if (!ok) return;
+                tc_after();
+                auto last_product = [&]() {          // the product of the tile before is through
+                    const bool good = warp_wait(kOFull + (buf ^ 1u), (j - 1) >> 1);
+                    tc_after();
+                    return good;
+                };
+                // the accumulator is emptied into fp32 sums; the issuer starts it anew
+                if (n > 0 && n % kFlush == 0) {
+                    ok = last_product();
+                    if (!ok) return;
+#pragma unroll 1
+                    for (int c = 0; c < kRows; c += 16) {
+                        uint32_t hi[16], lo[16];
+                        tmem_ld16(to + c, hi);
+                        tmem_ld16(to + N + c, lo);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float v = __uint_as_float(hi[i]) + __uint_as_float(lo[i]);
+                            float* dst = my_flush + (size_t)(c + i) * kHeadDim;
+                            if (n == kFlush) *dst = v;
+                            else asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(dst), "f"(v) : "memory");
+                        }
+                    }
+                }
+                uint32_t r[kCols];
+                // scores of 32 rows: raw products, or in log2 units with SCORE; -inf where the row does not see the token
+                auto scores = [&](int c) {
+                    tmem_ld<kCols>(ts + c * kCols, r);
+                    tmem_wait_ld();
+                    if constexpr (SCORE) {
+                        const int row0 = grp * kRows + c * kCols;
+#pragma unroll
+                        for (int i = 0; i < kCols; ++i) {
+                            const int p = row_pos[row0 + i];
+                            float y = __uint_as_float(r[i]);
+                            y = a.cap_in != 0.f ? cap_score(y, a.cap_in, a.cap_log2) : y * a.scale_log2;
+                            y = fmaf(row_slope[row0 + i], (float)(pos - p), y);
+                            if (pos > p || (uint32_t)p - (uint32_t)pos >= a.window) y = -INFINITY;
+                            r[i] = __float_as_uint(y);
+                        }
+                    }
+                    if (t == 0) {
+#pragma unroll
+                        for (int i = 0; i < kCols; ++i) {
+                            const uint32_t row = (uint32_t)(grp * kRows + c * kCols + i);
+                            const uint32_t node = min((uint32_t)s.node0 + ((row * a.gq_inv) >> 16), (uint32_t)STC_TREE_MAX_NODES - 1u);
+                            if (!((kin[node * 4 + quarter] >> lane) & 1u)) r[i] = __float_as_uint(-INFINITY);
+                        }
+                    }
+                    if (!all_valid && !valid) {
+#pragma unroll
+                        for (int i = 0; i < kCols; ++i) r[i] = __float_as_uint(-INFINITY);
+                    }
+                };
+                // exponents relative to the rows' maxima, and the largest of them
+                auto relative = [&](int c) {
+                    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    const float4* ref = reinterpret_cast<const float4*>(my_max + c * kCols);
+#pragma unroll
+                    for (int i = 0; i < kCols; i += 4) {
+                        const float4 m = ref[i / 4];
+                        float2 x = make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+                        float2 y = make_float2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+                        if constexpr (SCORE) {
+                            x = add2(x, make_float2(-m.x, -m.y));
+                            y = add2(y, make_float2(-m.z, -m.w));
+                        } else {
+                            x = fma2(x, both(a.scale_log2), make_float2(-m.x, -m.y));
+                            y = fma2(y, both(a.scale_log2), make_float2(-m.z, -m.w));
+                        }
+                        top[(i >> 2) & 3] = fmaxf(fmaxf(fmaxf(top[(i >> 2) & 3], x.x), x.y), fmaxf(y.x, y.y));
+                        r[i] = __float_as_uint(x.x); r[i + 1] = __float_as_uint(x.y);
+                        r[i + 2] = __float_as_uint(y.x); r[i + 3] = __float_as_uint(y.y);
+                    }
+                    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                };
+#pragma unroll 1
+                for (int attempt = 0;; ++attempt) {
+                    float peak = -INFINITY;
+#pragma unroll 1
+                    for (int c = 0; c < kChunks; ++c) {
+                        scores(c);
+                        peak = fmaxf(peak, relative(c));
+                    }
+                    const uint32_t tag = meets + 1u, at = grp * 2u + (meets & 1u);
+                    if (__any_sync(0xFFFFFFFFu, peak > kSlack) && lane == 0) votes[at] = tag;
+                    ok = meet();
+                    if (!ok) return;
+                    if (votes[at] != tag || attempt == 1) break;
+                    if (n > 0 && (L::kPBuffers == 1 || n % kFlush != 0)) {    // the scratch may be P, which the product before reads
+                        ok = last_product();
+                        if (!ok) return;
+                    }
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c) {
+                        // maxima of the tile's tokens: lane i takes column i, then the four warps'
+                        scores(c);
+                        float mine_top = -INFINITY;
+#pragma unroll
+                        for (int i = 0; i < kCols; ++i) {
+                            const float v = redux_max(__uint_as_float(r[i]));
+                            if (lane == i) mine_top = v;
+                        }
+                        if constexpr (!SCORE) mine_top *= a.scale_log2;       // (the scale is positive)
+                        scratch[quarter * 32 + lane] = mine_top;
+                        ok = meet();
+                        if (!ok) return;
+                        float new_max = 0.f, f = 1.f;
+                        if (lane < kCols) {
+                            const float top = fmaxf(fmaxf(scratch[lane], scratch[32 + lane]), fmaxf(scratch[64 + lane], scratch[96 + lane]));
+                            const float old = my_max[c * kCols + lane];
+                            new_max = old;
+                            if (top > old + kSlack) {
+                                new_max = top;
+                                f = old == kUnset ? 0.f : ex2(old - top);
+                            }
+                        }
+                        ok = meet();                 // everybody has read the old maxima
+                        if (!ok) return;
+                        if (quarter == 0 && lane < kCols) my_max[c * kCols + lane] = new_max;
+#pragma unroll
+                        for (int i = 0; i < kCols; i += 2) {
+                            float2& x = l[c * (kCols / 2) + i / 2];
+                            x = mul2(x, make_float2(__shfl_sync(0xFFFFFFFFu, f, i), __shfl_sync(0xFFFFFFFFu, f, i + 1)));
+                        }
+                        if (n > 0 && n % kFlush != 0) {
+#pragma unroll 1
+                            for (int part = 0; part < 2; ++part)              // high, residual
+#pragma unroll 1
+                                for (int e = 0; e < kCols; e += 16) {
+                                    uint32_t q[16];
+                                    tmem_ld16(to + part * N + c * kCols + e, q);
+                                    tmem_wait_ld();
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) {
+                                        const float fi = __shfl_sync(0xFFFFFFFFu, f, e + i);
+                                        q[i] = fi != 1.f ? __float_as_uint(__uint_as_float(q[i]) * fi) : q[i];
+                                    }
+                                    tmem_st16(to + part * N + c * kCols + e, q);
+                                }
+                            tmem_wait_st();
+                        }
+                        if (n >= kFlush) {
+#pragma unroll 1
+                            for (int i = 0; i < kCols; ++i) {
+                                const float fi = __shfl_sync(0xFFFFFFFFu, f, i);
+                                float* dst = my_flush + (size_t)(c * kCols + i) * kHeadDim;
+                                if (fi != 1.f) __stcg(dst, __ldcg(dst) * fi);
+                            }
+                        }
+                    }
+                    ok = meet();                     // the new maxima are there
+                    if (!ok) return;
+                }
+                if (L::kPBuffers == 1 && n > 0) {
+                    ok = last_product();
+                    if (!ok) return;
+                }
+                // weights, their sums, and P: eight rows of a token are 16 bytes of its line
+                const uint32_t line = base + L::kOffP + (L::kPBuffers > 1 ? buf * L::kP : 0u) + (uint32_t)tok * 128u, swz = (uint32_t)tok & 7u;
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    if (kChunks > 1) {
+                        scores(c);
+                        relative(c);
+                    }
+#pragma unroll
+                    for (int e = 0; e < kCols; e += 8) {
+                        uint32_t hi[4], lo[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float2 p = make_float2(ex2(__uint_as_float(r[e + 2 * i])), ex2(__uint_as_float(r[e + 2 * i + 1])));
+                            float2& sum = l[c * (kCols / 2) + e / 2 + i];
+                            sum = add2(sum, p);
+                            const __nv_bfloat162 h2 = __floats2bfloat162_rn(p.x, p.y);
+                            hi[i] = *reinterpret_cast<const uint32_t*>(&h2);
+                            const float2 d = fma2(make_float2(bf16lo(hi[i]), bf16hi(hi[i])), both(-1.f), p);
+                            const __nv_bfloat162 r2 = __floats2bfloat162_rn(d.x, d.y);
+                            lo[i] = *reinterpret_cast<const uint32_t*>(&r2);
+                        }
+                        const uint32_t eh = (uint32_t)(grp * kRows + c * kCols + e), el = eh + N;
+                        sts16(line + (eh >> 6) * kHalf + ((((eh & 63u) >> 3) ^ swz) << 4), hi);
+                        sts16(line + (el >> 6) * kHalf + ((((el & 63u) >> 3) ^ swz) << 4), lo);
+                    }
+                }
+                fence_proxy_async();
+                tc_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kPFull + buf));
+                id = id_next;
+            }
+            // ---- end of the segment -------------------------------------------------------------------------------
+            ok = warp_wait(kOFull + ((j - 1) & 1u), (j - 1) >> 1);
+            if (!ok) return;
+            tc_after();
+            const bool whole = s.slot < 0;
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
+                // sums over the warp's lanes, lane i keeping column i: halves change places, then a quarter of each ...
+                float v[kCols];
+#pragma unroll
+                for (int i = 0; i < kCols / 2; ++i) {
+                    v[2 * i] = l[c * (kCols / 2) + i].x;
+                    v[2 * i + 1] = l[c * (kCols / 2) + i].y;
+                }
+                if constexpr (kCols == 16) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], 16);
+                }
+#pragma unroll
+                for (int w = kCols / 2; w > 0; w >>= 1) {
+                    const bool upper = lane & w;
+#pragma unroll
+                    for (int i = 0; i < w; ++i) {
+                        const float keep = upper ? v[i + w] : v[i], give = upper ? v[i] : v[i + w];
+                        v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, w);
+                    }
+                }
+                scratch[quarter * 32 + lane] = v[0];
+                ok = meet();
+                if (!ok) return;
+                const int col = c * kCols + lane % kCols, row = grp * kRows + col;
+                const float sum = (scratch[lane % kCols] + scratch[32 + lane % kCols]) + (scratch[64 + lane % kCols] + scratch[96 + lane % kCols]);
+                float m = my_max[col];
+                if (m == kUnset) m = -INFINITY;
+                const float inv = sum != 0.f ? 1.f / sum : 0.f;
+                if (quarter == 0 && lane < kCols && row < live) {
+                    if (whole) {
+                        const uint32_t in_block = ((uint32_t)row * a.gq_inv) >> 16;
+                        const size_t at = ((size_t)s.b * a.n_cap + s.node0 + in_block) * a.Hq + s.hk * a.Gq + (row - in_block * a.Gq);
+                        if (a.lse) a.lse[at] = sum != 0.f ? (m + log2f(sum)) * kLn2 : -INFINITY;
+                    } else {
+                        a.part_ml[(size_t)s.slot * N + row] = make_float2(m, sum);
+                    }
+                }
+#pragma unroll 1
+                for (int e = 0; e < kCols; e += 16) {
+                    if (grp * kRows + c * kCols + e >= live) break;
+                    uint32_t hi[16], lo[16];
+                    tmem_ld16(to + c * kCols + e, hi);
+                    tmem_ld16(to + N + c * kCols + e, lo);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int row_i = grp * kRows + c * kCols + e + i;
+                        const float inv_i = __shfl_sync(0xFFFFFFFFu, inv, e + i);
+                        float x = __uint_as_float(hi[i]) + __uint_as_float(lo[i]);
+                        if (row_i < live) {
+                            if (count > kFlush) x += __ldcg(my_flush + (size_t)(c * kCols + e + i) * kHeadDim);
+                            if (whole) {
+                                const uint32_t in_block = ((uint32_t)row_i * a.gq_inv) >> 16;
+                                const size_t at = ((size_t)s.b * a.n_cap + s.node0 + in_block) * a.Hq + s.hk * a.Gq + (row_i - in_block * a.Gq);
+                                a.out[at * kHeadDim + tok] = inv_i != 0.f ? x * inv_i : 0.f;   // (0: nothing seen)
+                            } else {
+                                __stcg(a.part_o + ((size_t)s.slot * N + row_i) * kHeadDim + tok, x);
+                            }
+                        }
+                    }
+                }
+                ok = meet();                         // scratch and maxima are free again
+                if (!ok) return;
+            }
+            tc_before();
+            if (tables) {
+                ++tabs;
+                if (lane == 0) mbar_arrive(bar(kTabEmpty));
+            }
+        };
+        while (ok && next(ok)) segment();
+        if (!ok) give_up();
+    } else {
+        // ---- value tiles: packed groups -> swizzled rows -------------------------------------------------------
+        // A warp takes 32 tokens (two pages) of every tile.  LPT neighbouring lanes copy 16-byte chunks of one token (a whole group of 32
+        // or 64 bytes; two groups of 16), so a token's mask stays with its lanes and the place of a kept group is a running
+        // count.  A kept group is one asynchronous 16-byte copy per chunk, a dropped one a zero-filled copy that
+        // reads nothing.  The copies of a warp's next tile are under way before the last one's are waited for, unless its
+        // stage is still being read.
+        const int tok0 = (warp - 12) * 32;
+        int vc = 0, pending = -1;                    // tiles so far; stage whose copies are not waited for yet
+        bool ok = true;
+        auto publish = [&]() {                       // this warp's copies into `pending` have landed
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kVFull + pending));
+            pending = -1;
+        };
+        auto walk = [&](auto groups) {
+            constexpr int S = decltype(groups)::value, OPG = kOctets / S, LPT = OPG < 2 ? 2 : OPG, GPL = LPT / OPG;
+            const int sub = lane % LPT;
+            while (ok && next(ok)) {
+                const size_t problem = (size_t)s.b * a.Hkv + s.hk;
+                const uint16_t* mask_row = a.v_mask + problem * a.T;
+                const uint32_t* offs = a.v_offs + problem * (a.T + 1);
+                const uint4* packed = a.v_packed + problem * a.cap_groups * OPG;
+                const uint4* fresh = a.v_new + problem * a.n_cap * kOctets;
+                // tokens that no row of the sequence sees are left out: they may hold anything
+                int lo_all = 0, hi_all = s.len, q_doc = 0;
+                if constexpr (SCORE) {
+                    if (a.sc.q_pos) {
+                        int least = 0x7FFFFFFF, most = -1;
+                        for (int i = lane; i < s.nodes; i += 32) {
+                            const int p = a.sc.q_pos[(size_t)s.b * a.n_cap + i];
+                            least = min(least, p);
+                            most = max(most, p);
+                        }
+                        least = __reduce_min_sync(0xFFFFFFFFu, least);
+                        most = __reduce_max_sync(0xFFFFFFFFu, most);
+                        if (a.sc.window > 0 && least >= a.sc.window) lo_all = least - a.sc.window + 1;
+                        if (most < s.len) hi_all = most + 1;
+                    } else if (a.sc.window > 0 && s.len >= a.sc.window) {
+                        lo_all = s.len - a.sc.window + 1;
+                    }
+                    if (a.sc.tok_doc) q_doc = a.sc.q_doc[s.b];
+                }
+                auto page_of = [&](int t) { return t > 0 && t >= s.tile0 ? page_at((t - 1) * kTilePages + (tok0 + lane) / kPage) : -1; };
+                auto fetch = [&](int id, uint32_t& m, uint32_t& first) {          // this lane's mask, its page's first group
+                    m = first = 0;
+                    const int t = id * kPage + (lane & 15);
+                    if (id >= 0 && t < s.len) {
+                        m = mask_row[t];
+                        if (SCORE) {
+                            if (t < lo_all || t >= hi_all) m = 0;
+                            if (a.sc.tok_doc) {
+                                const int d = __ldg(a.sc.tok_doc + (size_t)s.b * a.T + t);
+                                if (d >= 0 && d != q_doc) m = 0;
+                            }
+                        }
+                    }
+                    if (id >= 0) first = offs[id * kPage];
+                    return id >= 0 && t < s.len ? (uint32_t)mask_row[t] : 0u;
+                };
+                uint32_t m_next, first_next, all_next;
+                all_next = fetch(page_of(s.tile1 - 1), m_next, first_next);
+                int id_next = page_of(s.tile1 - 2);
+#pragma unroll 1
+                for (int t = s.tile1 - 1; t >= s.tile0; --t, ++vc) {
+                    const uint32_t m = m_next & ((1u << S) - 1u), first = first_next, cnt = __popc(all_next & ((1u << S) - 1u));
+                    all_next = fetch(id_next, m_next, first_next);
+                    id_next = page_of(t - 2);
+                    // place of the token's first group: its page's, and the groups of the page's tokens before it
+                    const uint32_t incl = warp_incl_scan(cnt, lane), half = __shfl_sync(0xFFFFFFFFu, incl, 15);
+                    const uint32_t place = first + incl - cnt - (lane >= 16 ? half : 0u);
+                    const int st = vc % L::kVStages;
+                    if (vc >= L::kVStages &&
+                        !__all_sync(0xFFFFFFFFu, mbar_try_wait(bar(kVEmpty + st), (uint32_t)(vc / L::kVStages - 1) & 1u))) {
+                        if (pending >= 0) { cp_async_wait<0>(); publish(); }
+                        ok = warp_wait(kVEmpty + st, (uint32_t)(vc / L::kVStages - 1));
+                        if (!ok) break;
+                    }
+                    const uint32_t tile = base + L::kOffV + st * kTile;
+                    if (t == 0) {                    // the tree's own values, full width
+#pragma unroll 4
+                        for (int i = lane; i < 32 * kOctets; i += 32) {
+                            const int tok = tok0 + (i >> 4);
+                            const uint32_t oct = (uint32_t)i & 15u;
+                            const bool there = tok < s.nodes;
+                            cp_async16_zfill(tile + (oct >> 3) * kHalf + (uint32_t)tok * 128u + (((oct & 7u) ^ ((uint32_t)tok & 7u)) << 4),
+                                             there ? fresh + (size_t)tok * kOctets + oct : fresh, there ? 16 : 0);
+                        }
+                    } else {
+                        const uint32_t limit = (uint32_t)min(a.cap_groups, (int64_t)0xFFFFFFFF);   // groups of the store
+#pragma unroll 1
+                        for (int pass = 0; pass < LPT; ++pass) {
+                            const int tok = pass * (32 / LPT) + lane / LPT;       // of the warp's 32
+                            const uint32_t tm = __shfl_sync(0xFFFFFFFFu, m, tok);
+                            uint32_t at = __shfl_sync(0xFFFFFFFFu, place, tok);   // place of the next kept group of the token
+                            const uint32_t row = tile + (uint32_t)(tok0 + tok) * 128u, swz = (uint32_t)(tok & 7);
+#pragma unroll
+                            for (int k = 0; k < 16 / LPT; ++k) {
+                                const uint32_t oct = (uint32_t)(k * LPT + sub);   // chunk of the row: half oct >> 3, swizzled by the token
+                                uint32_t mine_at = at;
+                                bool kept;
+                                if constexpr (GPL == 1) {
+                                    kept = (tm >> k) & 1u;
+                                    at += kept;
+                                } else {
+                                    kept = (tm >> (2 * k + sub)) & 1u;
+                                    if (sub) mine_at += (tm >> (2 * k)) & 1u;
+                                    at += ((tm >> (2 * k)) & 1u) + ((tm >> (2 * k + 1)) & 1u);
+                                }
+                                kept = kept && mine_at < limit;
+                                cp_async16_zfill(row + (oct >> 3) * kHalf + (((oct & 7u) ^ swz) << 4),
+                                                 kept ? packed + (size_t)mine_at * OPG + sub % OPG : a.v_new, kept ? 16 : 0);
+                            }
+                        }
+                    }
+                    cp_async_commit();
+                    if (pending >= 0) { cp_async_wait<1>(); publish(); }
+                    pending = st;
+                }
+            }
+        };
+        if (a.S == 4) walk(std::integral_constant<int, 4>{});
+        else if (a.S == 8) walk(std::integral_constant<int, 8>{});
+        else walk(std::integral_constant<int, 16>{});
+        cp_async_wait<0>();
+        if (ok && pending >= 0) publish();
+        if (!ok) give_up();
     }
-    const float inv = l > 0.f ? 1.f / l : l == l ? 0.f : l;
-    reinterpret_cast<float4*>(a.out)[(size_t)row * 32 + lane] = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-    if (a.lse && lane == 0) a.lse[row] = l == l ? (l > 0.f ? m + logf(l) : -INFINITY) : l;
+    tc_before();
+    __syncthreads();
+    if (threadIdx.x == 0) a.cta_status[blockIdx.x] = *abort_flag;
+    if (warp == 1) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(4u * N) : "memory");
+    }
+}
+
+// Joins the partials of units that more than one CTA worked on, in CTA order; a warp per row, a lane per four channels.  Checks the
+// trees and gathers the CTAs' status on the side.
+__global__ void __launch_bounds__(256)
+tree_join_kernel(const TreeArgs a, int rows, int grid) {
+    // launched while the first kernel still runs: the call's own inputs are read before the wait
+    const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    const int h = (int)(row % a.Hq), node = (int)(row / a.Hq % a.n_cap), b = (int)(row / a.Hq / a.n_cap);
+    int nodes = 0, problem = 0, list = 0, first = 0;
+    if (b < a.B) {
+        nodes = nodes_of(a, b);
+        if (h == 0 && node == 0) {
+            bool bad = false;
+            for (int i = lane; i < nodes && a.parent; i += 32) {
+                const int up = a.parent[(size_t)b * a.n_cap + i];
+                bad |= up < -1 || up >= i;
+            }
+            bad = __any_sync(0xFFFFFFFFu, bad);
+            if (lane == 0) a.status[b] = bad ? STC_ERR_INVALID_ARG : STC_OK;
+        }
+        problem = b * a.Hkv + h / a.Gq;
+        pages_of(a, problem, clamp_len(a.seq_len, b, a.T), list, first);
+    }
+    const Unit u = unit_of(a, nodes, list);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (blockIdx.x == 0 && threadIdx.x < 32) {
+        int st = 0;
+        for (int c = lane; c < grid; c += 32) st = max(st, a.cta_status[c]);
+        st = __reduce_max_sync(0xFFFFFFFFu, st);
+        if (lane == 0) *a.word = st;
+    }
+    if (b >= a.B || node >= nodes) return;
+    const int blk = node / a.block_nodes, total = a.base[a.problems], n_cta = a.base[a.problems + 1];
+    const int x0 = a.base[problem] + blk * u.tiles, c0 = cta_of(total, x0, n_cta), c1 = cta_of(total, x0 + u.tiles - 1, n_cta);
+    if (c0 == c1) return;                            // finished where it was computed
+    const int in_block = (node - blk * a.block_nodes) * a.Gq + h % a.Gq;
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int c = c0; c <= c1; c += 8) {
+        float2 p[8];
+        float4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int e = min(c + i, c1);
+            const size_t at = (size_t)(2 * e + (e == c0 ? 1 : 0)) * rows + in_block;
+            p[i] = __ldcg(a.part_ml + at);
+            v[i] = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * kHeadDim) + lane);
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (c + i > c1) p[i] = make_float2(-INFINITY, 0.f);
+            top = fmaxf(top, p[i].x);
+        }
+        const float fm = m == -INFINITY ? 0.f : ex2(m - top);
+        l *= fm; o.x *= fm; o.y *= fm; o.z *= fm; o.w *= fm;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (p[i].x == -INFINITY) {               // nothing seen: its sum is 0, or NaN
+                l += p[i].y;
+                continue;
+            }
+            const float f = ex2(p[i].x - top);
+            l = fmaf(p[i].y, f, l);
+            o.x = fmaf(v[i].x, f, o.x); o.y = fmaf(v[i].y, f, o.y); o.z = fmaf(v[i].z, f, o.z); o.w = fmaf(v[i].w, f, o.w);
+        }
+        m = top;
+    }
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+    float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (inv != 0.f) r = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    reinterpret_cast<float4*>(a.out)[(size_t)row * 32 + lane] = r;
+    if (a.lse && lane == 0) a.lse[row] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+}
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// The workspace has to be sized without a device, so the partial slots are counted for this many CTAs.
+constexpr int kPlanSms = 148;
+
+// Rows per CTA: the fewest that hold a whole tree, at most 128 (64 with options on the scores).
+int rows_of(const Geom& g, int n_cap, bool score) {
+    const int most = score ? 64 : 128;
+    int n = 32;
+    while (n < most && n / g.Gq < n_cap) n *= 2;
+    return n;
+}
+
+template <int N, bool SCORE>
+cudaError_t launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& fresh, const TreeArgs& a, int n_cta, cudaStream_t st) {
+    cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<N, SCORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan<N>::kSmem);
+    if (e != cudaSuccess) return e;
+    tree_attn_kernel<N, SCORE><<<n_cta, kThreads, Plan<N>::kSmem, st>>>(q, k, fresh, a);
+    return cudaGetLastError();
 }
 
 }  // namespace
 
-size_t tree_attn_ws_bytes(const Geom&, int) { return 256; }
+size_t tree_attn_ws_bytes(const Geom& g, int n_cap) {
+    // (a call with options has no more rows per CTA than one without)
+    const size_t n = (size_t)rows_of(g, n_cap, false);
+    return 256 + align256(kPlanSms * 4) + align256(((size_t)g.problems + 2) * 4) + 2 * (size_t)kPlanSms * n * 8 +
+           3 * (size_t)kPlanSms * n * kHeadDim * 4;
+}
 
 cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tree& tree, const void* q, const int32_t* page_ids,
                              const int32_t* n_pages, int max_pages, float sm_scale, const ScoreArgs& score, float* out, float* lse,
                              int32_t* status, void* ws, cudaStream_t st) {
+    const bool scored = score.softcap > 0.f || score.window > 0 || score.slopes || score.q_pos || score.tok_doc || !(sm_scale > 0.f);
+    const int n = rows_of(g, tree.n_cap, scored);
     TreeArgs a;
-    a.q = static_cast<const uint2*>(q); a.k = static_cast<const uint2*>(cache.k);
-    a.k_new = static_cast<const uint2*>(tree.k); a.v_new = static_cast<const uint2*>(tree.v);
-    a.v_packed = static_cast<const __nv_bfloat16*>(cache.v_packed); a.v_mask = cache.v_mask; a.v_offs = cache.v_offs;
-    a.seq_len = g.seq_len; a.parent = tree.parent; a.n_nodes = tree.n_nodes; a.page_ids = page_ids; a.n_pages = n_pages;
-    a.out = out; a.lse = lse; a.status = status; a.word = static_cast<int32_t*>(ws); a.cap_groups = cache.cap_groups;
-    a.B = g.B; a.Hq = g.Hq; a.Hkv = g.Hkv; a.Gq = g.Gq; a.T = g.T; a.P = g.P; a.S = g.S; a.n_cap = tree.n_cap;
-    a.max_pages = max_pages; a.scale = sm_scale; a.sc = score;
+    a.seq_len = g.seq_len; a.n_nodes = tree.n_nodes; a.parent = tree.parent; a.page_ids = page_ids; a.n_pages = n_pages;
+    a.v_mask = cache.v_mask; a.v_offs = cache.v_offs; a.v_packed = static_cast<const uint4*>(cache.v_packed);
+    a.v_new = static_cast<const uint4*>(tree.v);
+    a.out = out; a.lse = lse; a.status = status;
+    char* w = static_cast<char*>(ws);
+    a.word = reinterpret_cast<int32_t*>(w);
+    w += 256;
+    a.cta_status = reinterpret_cast<int32_t*>(w);
+    w += align256(kPlanSms * 4);
+    a.base = reinterpret_cast<int32_t*>(w);
+    w += align256(((size_t)g.problems + 2) * 4);
+    a.part_ml = reinterpret_cast<float2*>(w);
+    w += 2 * (size_t)kPlanSms * n * 8;
+    a.part_o = reinterpret_cast<float*>(w);
+    w += 2 * (size_t)kPlanSms * n * kHeadDim * 4;
+    a.flush = reinterpret_cast<float*>(w);
+    a.cap_groups = cache.cap_groups;
+    a.B = g.B; a.Hq = g.Hq; a.Hkv = g.Hkv; a.Gq = g.Gq; a.S = g.S; a.T = g.T; a.n_cap = tree.n_cap;
+    a.max_pages = max_pages; a.problems = g.problems;
+    a.block_nodes = n / g.Gq;
+    a.gq_inv = (65536u + (uint32_t)g.Gq - 1u) / (uint32_t)g.Gq;
+    a.sc = score;
+    a.scale_log2 = sm_scale * kLog2e;
+    a.cap_in = score.softcap > 0.f ? sm_scale / score.softcap : 0.f;
+    a.cap_log2 = score.softcap * kLog2e;
+    a.window = score.window > 0 ? (uint32_t)score.window : 0xFFFFFFFFu;
+    int sms = 0;
+    cudaError_t e = device_sm_count(&sms);
+    if (e != cudaSuccess) return e;
+    const int n_cta = sms < kPlanSms ? sms : kPlanSms;
+
+    EncodeTiled enc = tensor_map_encoder();
+    if (!enc) return cudaErrorNotSupported;
+    CUtensorMap map_q, map_k, map_new;
+    {
+        const cuuint64_t dims[3] = {kHeadDim, (cuuint64_t)g.Hq, (cuuint64_t)g.B * (cuuint64_t)tree.n_cap};
+        const cuuint64_t strides[2] = {kRowBytes, (cuuint64_t)g.Hq * kRowBytes};
+        const cuuint32_t box[3] = {64, (cuuint32_t)g.Gq, (cuuint32_t)a.block_nodes}, step[3] = {1, 1, 1};
+        if (enc(&map_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return cudaErrorInvalidValue;
+    }
+    auto rows_map = [&](CUtensorMap* map, const void* p, long long rows) {
+        const cuuint64_t dims[2] = {kHeadDim, (cuuint64_t)rows};
+        const cuuint64_t strides[1] = {kRowBytes};
+        const cuuint32_t box[2] = {64, kPage}, step[2] = {1, 1};
+        return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    const long long new_rows = (long long)g.problems * tree.n_cap;
+    // (a cache without tokens: no page is ever loaded, the map only has to be a valid one)
+    if (!rows_map(&map_new, tree.k, new_rows) ||
+        !(g.T > 0 ? rows_map(&map_k, cache.k, (long long)g.problems * g.T) : rows_map(&map_k, tree.k, new_rows)))
+        return cudaErrorInvalidValue;
+    if (n == 32) e = scored ? launch<32, true>(map_q, map_k, map_new, a, n_cta, st) : launch<32, false>(map_q, map_k, map_new, a, n_cta, st);
+    else if (n == 64) e = scored ? launch<64, true>(map_q, map_k, map_new, a, n_cta, st) : launch<64, false>(map_q, map_k, map_new, a, n_cta, st);
+    else e = launch<128, false>(map_q, map_k, map_new, a, n_cta, st);
+    if (e != cudaSuccess) return e;
     const long long rows = (long long)g.B * tree.n_cap * g.Hq;
-    tree_attn_kernel<<<(unsigned)((rows + kThreads / 32 - 1) / (kThreads / 32)), kThreads, 0, st>>>(a);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((rows + 7) / 8));
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cudaLaunchAttribute early;                       // its blocks wait in place instead of behind a launch
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, tree_join_kernel, a, n, n_cta);
 }
 
 }  // namespace stc
