@@ -12,8 +12,12 @@
 // residual, two sets of columns of one product (V~ is read once for both) that are added at the end: one bf16 weight alone would
 // leave the fp32 output 2^-8 off, the pair leaves 2^-16.
 //
-// The running maximum of a row is shared by the tile's 128 threads.  It need not be exact: a tile only moves it when a score exceeds
-// it by more than 2^8 (a vote of the four warps); then the true maxima are taken across lanes, and sums and accumulator follow.
+// The reference that a row's exponents are taken against is shared by the tile's 128 threads and need not be the maximum: weights may
+// be far above 1 as long as nothing overflows.  It is taken from the first tile (each warp looks at a quarter of the rows over its
+// own 32 tokens) and then stays, so that tiles need no maximum and the warps nothing from each other.  Where a sum comes out
+// above kTooLarge at the end, the CTA walks its range once more in the careful way: a tile moves a reference when a
+// score exceeds it by more than 2^8 (a vote of the four warps); then the true maxima are taken, and sums and accumulator follow.
+// Rows without a reference (first tiles that they do not see) go the careful way until they have one.
 //
 // Work split.  Unit = (sequence, KV head, block of nodes); its tiles are the tree (tile 0) and then eight listed pages each.  The tiles
 // of all units form one flat sequence that is cut into equal contiguous ranges, one per CTA (one CTA per SM).  A unit within
@@ -31,7 +35,7 @@
 // roles leave, the producer waits (bounded) for its copies, tensor memory is freed.
 #include <type_traits>
 
-#include "umma.cuh"
+#include "cap.cuh"
 
 namespace stc {
 namespace {
@@ -47,13 +51,14 @@ constexpr int kFlush = 16;                        // tiles an accumulator takes:
 constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;                     // log2 units a maximum may be exceeded by
-constexpr float kUnset = -3.0e38f;                // maximum of a row that has seen nothing: every finite score exceeds it
+constexpr float kUnset = -3.0e38f;                // reference of a row that has seen nothing: every finite score exceeds it
+constexpr float kTooLarge = 4294967296.f;         // sum of weights that sends a CTA over its range again
 
 // barriers, in 8-byte words of the control block
 enum { kQFull, kQEmpty, kKFull, kKEmpty = kKFull + 3, kVFull = kKEmpty + 3, kVEmpty = kVFull + 2, kSFull = kVEmpty + 2,
        kPFull = kSFull + 2, kOFull = kPFull + 2, kGroup = kOFull + 2, kTabFull = kGroup + 2, kTabEmpty, kSegFull,
        kSegEmpty = kSegFull + kSegs, kBars = kSegEmpty + kSegs };
-constexpr uint32_t kCtlTmem = 256, kCtlAbort = 260, kCtlVotes = 264, kCtlSegs = 288, kCtlMax = 384;
+constexpr uint32_t kCtlTmem = 256, kCtlAbort = 260, kCtlVotes = 264, kCtlRedo = 280, kCtlDone = 284, kCtlSegs = 288, kCtlMax = 384;
 static_assert(kBars * 8 <= kCtlTmem && kCtlSegs + kSegs * 48 <= kCtlMax, "control block");
 
 // Shared memory of a CTA with N rows.
@@ -64,8 +69,8 @@ struct Plan {
     static constexpr uint32_t kOffK = 2 * kQHalf, kOffV = kOffK + kKStages * kTile, kOffP = kOffV + kVStages * kTile;
     static constexpr uint32_t kOffCtl = kOffP + kPBuffers * kP;
     static constexpr uint32_t kCtlKin = kCtlMax + N * 4;                                   // [128 nodes][4 words]
-    static constexpr uint32_t kCtlScratch = kCtlKin + STC_TREE_MAX_NODES * 16;             // [2 groups][4 warps][32], positions, row tables
-    static constexpr uint32_t kCtlPos = kCtlScratch + 1024, kCtlRowPos = kCtlPos + 512, kCtlRowSlope = kCtlRowPos + 256;
+    static constexpr uint32_t kCtlScratch = kCtlKin + STC_TREE_MAX_NODES * 16;             // [2 groups][4 warps][32], positions, slopes
+    static constexpr uint32_t kCtlPos = kCtlScratch + 1024, kCtlRowSlope = kCtlPos + 512;
     static constexpr uint32_t kCtlBytes = N == 128 ? kCtlScratch : kCtlRowSlope + 256;
     static constexpr uint32_t kSmem = kOffCtl + kCtlBytes;
     static_assert(kSmem <= 232448, "shared memory of a block");
@@ -131,6 +136,7 @@ __device__ __forceinline__ int cta_of(int total, int x, int n) { return (int)(((
 struct Segment {
     int b, hk, node0, nodes, len, list, first, tile0, tile1;
     int slot;                    // partial slot, -1 = the whole unit
+    int careful;                 // second walk
 };
 
 __device__ __forceinline__ float redux_max(float v) {
@@ -140,10 +146,6 @@ __device__ __forceinline__ float redux_max(float v) {
 }
 __device__ __forceinline__ void sts16(uint32_t addr, const uint32_t (&v)[4]) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
-}
-__device__ __forceinline__ float cap_score(float x, float cap_in, float cap_log2) {
-    const float z = x * cap_in, lo = tanh_small(z), hi = tanh_large(z);
-    return cap_log2 * (fabsf(z) <= kTanhSmall ? lo : hi);
 }
 // COLS consecutive columns of the warp's 32 lanes.
 template <int COLS>
@@ -165,11 +167,12 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctl + kCtlTmem);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + kCtlAbort);
     volatile uint32_t* votes = reinterpret_cast<volatile uint32_t*>(ctl + kCtlVotes);       // [2 groups][2]
+    volatile int* redo = reinterpret_cast<volatile int*>(ctl + kCtlRedo);                   // a sum came out too large
+    volatile int* done = reinterpret_cast<volatile int*>(ctl + kCtlDone);                   // softmax warps that finished a segment, counted
     volatile int* segs = reinterpret_cast<volatile int*>(ctl + kCtlSegs);                   // [kSegs][12]
     float* const row_max = reinterpret_cast<float*>(ctl + kCtlMax);                         // [N], log2 units
     uint32_t* const kin = reinterpret_cast<uint32_t*>(ctl + L::kCtlKin);
     int* const node_pos = reinterpret_cast<int*>(ctl + (N == 128 ? 0 : L::kCtlPos));        // (SCORE has N <= 64)
-    int* const row_pos = reinterpret_cast<int*>(ctl + (N == 128 ? 0 : L::kCtlRowPos));
     float* const row_slope = reinterpret_cast<float*>(ctl + (N == 128 ? 0 : L::kCtlRowSlope));
     static_assert(!(SCORE && N == 128), "no room for the row tables");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -185,6 +188,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         fence_mbar_init();
     }
     if (threadIdx.x < 4) votes[threadIdx.x] = 0;
+    if (threadIdx.x == 5) *redo = *done = 0;
     if (threadIdx.x == 4) *abort_flag = (base & 1023u) != 0 ? (int)STC_ERR_CUDA : 0;        // swizzled tiles need 1024-byte aligned bases
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
@@ -248,18 +252,18 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         if (!good) return false;
         volatile int* e = segs + (n_seg % kSegs) * 12;
         s.b = e[0]; s.hk = e[1]; s.node0 = e[2]; s.nodes = e[3]; s.len = e[4]; s.list = e[5]; s.first = e[6];
-        s.tile0 = e[7]; s.tile1 = e[8]; s.slot = e[9];
+        s.tile0 = e[7]; s.tile1 = e[8]; s.slot = e[9]; s.careful = e[10];
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(kSegEmpty + n_seg % kSegs));
         ++n_seg;
         return s.tile1 >= 0;
     };
-    // page of list entry j of the segment's problem, -1 where there is none
-    auto page_at = [&](int j) {
+    // entry j of the segment's page list as it stands there, to be asked for ahead of its use; -1 outside the list
+    auto listed = [&](int j) {
         if (j < 0 || j >= s.list) return -1;
-        const int id = a.page_ids ? __ldg(a.page_ids + (size_t)(s.b * a.Hkv + s.hk) * a.max_pages + j) : s.first + j;
-        return id >= 0 && id < (s.len + kPage - 1) / kPage ? id : -1;
+        return a.page_ids ? __ldg(a.page_ids + (size_t)(s.b * a.Hkv + s.hk) * a.max_pages + j) : s.first + j;
     };
+    auto is_page = [&](int id) { return id >= 0 && id < (s.len + kPage - 1) / kPage; };
 
     if (*abort_flag) {
         // nothing was started
@@ -270,7 +274,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         const uint32_t q_bytes = 2u * 128u * (uint32_t)(a.Gq * a.block_nodes);
         while (ok && next(ok)) {
             const int problem = s.b * a.Hkv + s.hk;
-            auto fetch = [&](int t) { return lane < kTilePages && t > 0 ? page_at((t - 1) * kTilePages + lane) : -1; };
+            auto fetch = [&](int t) { return lane < kTilePages && t > 0 ? listed((t - 1) * kTilePages + lane) : -1; };
             int id = fetch(s.tile1 - 1);
             bool q_due = true;
 #pragma unroll 1
@@ -279,7 +283,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 const int st = kc % L::kKStages;
                 if (kc >= L::kKStages) ok = warp_wait(kKEmpty + st, (uint32_t)(kc / L::kKStages - 1));
                 if (!ok) break;
-                const bool mine_too = t > 0 ? id >= 0 : lane < (s.nodes + kPage - 1) / kPage;
+                const bool mine_too = t > 0 ? is_page(id) : lane < (s.nodes + kPage - 1) / kPage;
                 const int boxes = __popc(__ballot_sync(0xFFFFFFFFu, mine_too));
                 if (lane == 0) mbar_expect_tx(bar(kKFull + st), (uint32_t)boxes * kPage * kRowBytes);
                 __syncwarp();
@@ -420,10 +424,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     const int depth = __popc(m[i][0]) + __popc(m[i][1]) + __popc(m[i][2]) + __popc(m[i][3]) - 1;
                     node_pos[node] = a.sc.q_pos && node < s.nodes ? a.sc.q_pos[(size_t)s.b * a.n_cap + node] : s.len + depth;
                 }
-                __syncwarp();
                 for (int r = lane; r < N; r += 32) {
-                    const int in_block = (int)(((uint32_t)r * a.gq_inv) >> 16), node = min(s.node0 + in_block, STC_TREE_MAX_NODES - 1);
-                    row_pos[r] = node_pos[node];
+                    const int in_block = (int)(((uint32_t)r * a.gq_inv) >> 16);
                     row_slope[r] = a.sc.slopes ? a.sc.slopes[s.hk * a.Gq + (r - in_block * a.Gq)] * kLog2e : 0.f;
                 }
             }
@@ -436,8 +438,18 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         // ---- scheduler: walks the CTA's range, segment by segment -----------------------------------------------------
         if (lane == 0) {
             bool ok = true;
-            int x = x_begin, p = p_first, off = x_first;
+            int x = x_begin, p = p_first, off = x_first, careful = 0;
             for (int i = 0; ok; ++i) {
+                if (x >= x_end && !careful && i > 0) {       // all is under way: wait for it, and see how it went
+                    const unsigned long long t0 = global_ns();
+                    while (*done < 8 * i && ok) ok = !*abort_flag && global_ns() - t0 < 4 * kWaitNs;
+                    if (!ok) break;
+                    __threadfence_block();
+                    if (*redo) {
+                        careful = 1;
+                        x = x_begin; p = p_first; off = x_first;
+                    }
+                }
                 Segment g = {};
                 g.tile1 = -1;
                 while (x < x_end) {
@@ -466,7 +478,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 if (!ok) break;
                 volatile int* e = segs + (i % kSegs) * 12;
                 e[0] = g.b; e[1] = g.hk; e[2] = g.node0; e[3] = g.nodes; e[4] = g.len; e[5] = g.list; e[6] = g.first;
-                e[7] = g.tile0; e[8] = g.tile1; e[9] = g.slot;
+                e[7] = g.tile0; e[8] = g.tile1; e[9] = g.slot; e[10] = careful;
                 mbar_arrive(bar(kSegFull + i % kSegs));
                 if (g.tile1 < 0) break;
             }
@@ -492,42 +504,89 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 
         auto segment = [&]() {
             const int live = min(a.block_nodes, s.nodes - s.node0) * a.Gq;    // rows of the block
+            const int mine = live - grp * kRows;                              // of them in this group
             const bool tables = SCORE || s.tile0 == 0;
+            if (mine <= 0) {                         // none: its columns of P and O may be anything
+                for (int n = s.tile1 - s.tile0; n > 0; --n, ++j) {
+                    ok = warp_wait(kSFull + (j & 1u), j >> 1);
+                    if (!ok) return;
+                    if (lane == 0) mbar_arrive(bar(kPFull + (j & 1u)));
+                }
+                if (tables) {
+                    ok = warp_wait(kTabFull, tabs++);
+                    if (ok && lane == 0) mbar_arrive(bar(kTabEmpty));
+                }
+                if (ok && lane == 0) atomicAdd(const_cast<int*>(done), 1);
+                return;
+            }
             float2 l[kRows / 2];                     // sums of this thread's tokens
 #pragma unroll
             for (int i = 0; i < kRows / 2; ++i) l[i] = make_float2(0.f, 0.f);
-            if (tok < kRows) my_max[tok] = grp * kRows + tok < live ? kUnset : INFINITY;   // (nothing exceeds it)
+            if (tok < kRows) my_max[tok] = tok < mine ? kUnset : INFINITY;   // (nothing exceeds it)
+            int p0 = 0, p_least = 0, p_most = 0;     // positions of the block's rows: the first, which distances are taken from
             if (SCORE) {
                 ok = warp_wait(kTabFull, tabs);
                 if (!ok) return;
+                p_least = 0x7FFFFFFF;
+                p_most = -0x7FFFFFFF - 1;
+                p0 = node_pos[s.node0];
+                for (int i = s.node0 + lane; i < min(s.node0 + a.block_nodes, s.nodes); i += 32) {
+                    p_least = min(p_least, node_pos[i]);
+                    p_most = max(p_most, node_pos[i]);
+                }
+                p_least = __reduce_min_sync(0xFFFFFFFFu, p_least);
+                p_most = __reduce_max_sync(0xFFFFFFFFu, p_most);
             }
             ok = meet();
             if (!ok) return;
-            int id = s.tile1 > 1 ? page_at((s.tile1 - 2) * kTilePages + (tok >> 4)) : -1;
+            // page ids are asked for two tiles ahead, documents one
+            auto page_of = [&](int t) { return t > 0 && t >= s.tile0 ? listed((t - 1) * kTilePages + (tok >> 4)) : -1; };
+            auto doc_of = [&](int id) {
+                const int at = id * kPage + (tok & 15);
+                return SCORE && a.sc.tok_doc && is_page(id) && at < s.len ? __ldg(a.sc.tok_doc + (size_t)s.b * a.T + at) : -1;
+            };
+            int id = page_of(s.tile1 - 1), id_next = page_of(s.tile1 - 2), doc = doc_of(id);
             const int q_doc = SCORE && a.sc.tok_doc ? a.sc.q_doc[s.b] : 0;
             const int count = s.tile1 - s.tile0;
+            bool calm = false;                       // every row has a reference
 #pragma unroll 1
             for (int n = 0; n < count; ++n, ++j) {
                 const int t = s.tile1 - 1 - n;
                 const uint32_t buf = j & 1u, ts = lane_base + buf * N + grp * kRows;
-                const int id_next = n + 1 < count ? page_at((t - 2) * kTilePages + (tok >> 4)) : -1;
-                // this thread's token
+                // this thread's token, and the rows of the group that see it
                 int pos = id * kPage + (tok & 15);
-                bool valid = id >= 0 && pos < s.len;
-                if (t == 0) {
-                    valid = tok < s.nodes;
+                bool valid = t > 0 ? is_page(id) && pos < s.len && (!SCORE || doc < 0 || doc == q_doc) : tok < s.nodes;
+                doc = doc_of(id_next);
+                id = id_next;
+                id_next = page_of(t - 2);
+                uint64_t see = valid ? ~0ull : 0ull;
+                bool each = t == 0;                  // row by row
+                if constexpr (SCORE) {
+                    if (t == 0) pos = node_pos[tok];
+                    each = each || __any_sync(0xFFFFFFFFu, valid && (pos > p_least || (uint32_t)p_most - (uint32_t)pos >= a.window));
+                }
+                if (each) {
                     if (!SCORE) {
                         ok = warp_wait(kTabFull, tabs);
                         if (!ok) return;
-                    } else {
-                        pos = node_pos[tok];
                     }
+                    see = 0;
+                    const uint64_t ones = (1ull << a.Gq) - 1ull;
+                    const int from = (int)(((uint32_t)(grp * kRows) * a.gq_inv) >> 16);
+#pragma unroll 4
+                    for (int i = from; i * a.Gq < (grp + 1) * kRows; ++i) {       // nodes of the block
+                        const int node = min(s.node0 + i, STC_TREE_MAX_NODES - 1), at = i * a.Gq - grp * kRows;
+                        bool seen = t > 0 || ((kin[node * 4 + quarter] >> lane) & 1u);
+                        if constexpr (SCORE) {
+                            const int p = node_pos[node];
+                            seen = seen && pos <= p && (uint32_t)p - (uint32_t)pos < a.window;
+                        }
+                        if (seen) see |= at >= 0 ? ones << at : ones >> -at;
+                    }
+                    if (!valid) see = 0;
                 }
-                if (SCORE && a.sc.tok_doc && t > 0 && valid) {
-                    const int d = __ldg(a.sc.tok_doc + (size_t)s.b * a.T + pos);
-                    valid = d < 0 || d == q_doc;
-                }
-                const bool all_valid = __all_sync(0xFFFFFFFFu, valid) && t > 0;
+                const bool open = __all_sync(0xFFFFFFFFu, !each && valid);        // every row sees every token of the warp
+                const float far = SCORE ? (float)(pos - p0) : 0.f;
                 ok = warp_wait(kSFull + buf, j >> 1);
                 if (!ok) return;
                 tc_after();
@@ -555,39 +614,52 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         }
                     }
                 }
-                uint32_t r[kCols];
-                // scores of 32 rows: raw products, or in log2 units with SCORE; -inf where the row does not see the token
-                auto scores = [&](int c) {
-                    tmem_ld<kCols>(ts + c * kCols, r);
-                    tmem_wait_ld();
+                // raw products of the rows from `row` on -> scores: raw ones, or finished ones in log2 units (but for slope times
+                // p0 - p, which is the same for all tokens) with SCORE; -inf where the row does not see the token
+                auto finish = [&](auto& r, int row) {
+                    constexpr int C = sizeof(r) / sizeof(r[0]);
                     if constexpr (SCORE) {
-                        const int row0 = grp * kRows + c * kCols;
+                        if (a.cap_in != 0.f) {
+                            // (what a row does not see, and columns without a row, have no say in how the others are capped)
+                            float most = 0.f;
+                            if (row + C <= mine) {
+                                most = magnitude(r);
+                            } else {
 #pragma unroll
-                        for (int i = 0; i < kCols; ++i) {
-                            const int p = row_pos[row0 + i];
-                            float y = __uint_as_float(r[i]);
-                            y = a.cap_in != 0.f ? cap_score(y, a.cap_in, a.cap_log2) : y * a.scale_log2;
-                            y = fmaf(row_slope[row0 + i], (float)(pos - p), y);
-                            if (pos > p || (uint32_t)p - (uint32_t)pos >= a.window) y = -INFINITY;
-                            r[i] = __float_as_uint(y);
+                                for (int i = 0; i < C; ++i) most = row + i < mine ? fmaxf(most, fabsf(__uint_as_float(r[i]))) : most;
+                            }
+                            if (open && __all_sync(0xFFFFFFFFu, most * fabsf(a.cap_in) <= kCapSmall))
+                                cap_scores_low(r, a.cap_in, a.scale_log2);
+                            else
+                                cap_scores_any(r, a.cap_in, a.cap_log2);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < C; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * a.scale_log2);
+                        }
+                        if (a.sc.slopes) {
+                            const float2* slope = reinterpret_cast<const float2*>(row_slope + grp * kRows + row);
+#pragma unroll
+                            for (int i = 0; i < C; i += 2) {
+                                const float2 y = fma2(slope[i / 2], both(far), make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])));
+                                r[i] = __float_as_uint(y.x);
+                                r[i + 1] = __float_as_uint(y.y);
+                            }
                         }
                     }
-                    if (t == 0) {
+                    if (!open) {
+                        const uint32_t bits = (uint32_t)(see >> row);
 #pragma unroll
-                        for (int i = 0; i < kCols; ++i) {
-                            const uint32_t row = (uint32_t)(grp * kRows + c * kCols + i);
-                            const uint32_t node = min((uint32_t)s.node0 + ((row * a.gq_inv) >> 16), (uint32_t)STC_TREE_MAX_NODES - 1u);
-                            if (!((kin[node * 4 + quarter] >> lane) & 1u)) r[i] = __float_as_uint(-INFINITY);
-                        }
-                    }
-                    if (!all_valid && !valid) {
-#pragma unroll
-                        for (int i = 0; i < kCols; ++i) r[i] = __float_as_uint(-INFINITY);
+                        for (int i = 0; i < C; ++i)
+                            if (!((bits >> i) & 1u)) r[i] = __float_as_uint(-INFINITY);
                     }
                 };
-                // exponents relative to the rows' maxima, and the largest of them
-                auto relative = [&](int c) {
-                    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                auto scores = [&](uint32_t (&r)[kCols], int c) {
+                    tmem_ld<kCols>(ts + c * kCols, r);
+                    tmem_wait_ld();
+                    finish(r, c * kCols);
+                };
+                // exponents relative to the rows' references
+                auto relative = [&](uint32_t (&r)[kCols], int c) {
                     const float4* ref = reinterpret_cast<const float4*>(my_max + c * kCols);
 #pragma unroll
                     for (int i = 0; i < kCols; i += 4) {
@@ -601,89 +673,119 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                             x = fma2(x, both(a.scale_log2), make_float2(-m.x, -m.y));
                             y = fma2(y, both(a.scale_log2), make_float2(-m.z, -m.w));
                         }
-                        top[(i >> 2) & 3] = fmaxf(fmaxf(fmaxf(top[(i >> 2) & 3], x.x), x.y), fmaxf(y.x, y.y));
                         r[i] = __float_as_uint(x.x); r[i + 1] = __float_as_uint(x.y);
                         r[i + 2] = __float_as_uint(y.x); r[i + 3] = __float_as_uint(y.y);
                     }
-                    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
                 };
-#pragma unroll 1
-                for (int attempt = 0;; ++attempt) {
-                    float peak = -INFINITY;
-#pragma unroll 1
-                    for (int c = 0; c < kChunks; ++c) {
-                        scores(c);
-                        peak = fmaxf(peak, relative(c));
+                auto all_set = [&]() {               // (the same answer in the group's four warps)
+                    bool unset = lane < kRows && my_max[lane % kRows] == kUnset;
+                    if (kRows > 32) unset = unset || my_max[32 % kRows + lane % 32] == kUnset;
+                    return !__any_sync(0xFFFFFFFFu, unset);
+                };
+                if (n == 0 && !s.careful) {
+                    // a first reference: this warp's quarter of the rows, over its own tokens
+                    constexpr int kShare = kRows / 4;
+                    uint32_t q[16], r[kShare];
+                    tmem_ld16(ts + quarter * kShare, q);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < kShare; ++i) r[i] = q[i];
+                    finish(r, quarter * kShare);
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < kShare; ++i) {
+                        const float v = redux_max(__uint_as_float(r[i]));
+                        if (lane == i) top = v;
                     }
-                    const uint32_t tag = meets + 1u, at = grp * 2u + (meets & 1u);
-                    if (__any_sync(0xFFFFFFFFu, peak > kSlack) && lane == 0) votes[at] = tag;
+                    if (!SCORE) top *= a.scale_log2;             // (the scale is positive)
+                    if (lane < kShare && my_max[quarter * kShare + lane] == kUnset && top > kUnset) my_max[quarter * kShare + lane] = top;
                     ok = meet();
                     if (!ok) return;
-                    if (votes[at] != tag || attempt == 1) break;
-                    if (n > 0 && (L::kPBuffers == 1 || n % kFlush != 0)) {    // the scratch may be P, which the product before reads
-                        ok = last_product();
-                        if (!ok) return;
-                    }
+                    calm = all_set();
+                }
+                if (__builtin_expect(!calm, 0)) {
+                    uint32_t r[kCols];
+#pragma unroll 1
+                    for (int attempt = 0;; ++attempt) {
+                        bool exceeds = false;
+#pragma unroll 1
+                        for (int c = 0; c < kChunks; ++c) {
+                            scores(r, c);
+                            relative(r, c);
 #pragma unroll
-                    for (int c = 0; c < kChunks; ++c) {
-                        // maxima of the tile's tokens: lane i takes column i, then the four warps'
-                        scores(c);
-                        float mine_top = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < kCols; ++i) {
-                            const float v = redux_max(__uint_as_float(r[i]));
-                            if (lane == i) mine_top = v;
+                            for (int i = 0; i < kCols; ++i) exceeds |= __uint_as_float(r[i]) > kSlack;
                         }
-                        if constexpr (!SCORE) mine_top *= a.scale_log2;       // (the scale is positive)
-                        scratch[quarter * 32 + lane] = mine_top;
+                        const uint32_t tag = meets + 1u, at = grp * 2u + (meets & 1u);
+                        if (__any_sync(0xFFFFFFFFu, exceeds) && lane == 0) votes[at] = tag;
                         ok = meet();
                         if (!ok) return;
-                        float new_max = 0.f, f = 1.f;
-                        if (lane < kCols) {
-                            const float top = fmaxf(fmaxf(scratch[lane], scratch[32 + lane]), fmaxf(scratch[64 + lane], scratch[96 + lane]));
-                            const float old = my_max[c * kCols + lane];
-                            new_max = old;
-                            if (top > old + kSlack) {
-                                new_max = top;
-                                f = old == kUnset ? 0.f : ex2(old - top);
-                            }
+                        if (votes[at] != tag || attempt == 1) break;
+                        if (n > 0 && (L::kPBuffers == 1 || n % kFlush != 0)) {    // the scratch may be P, which the product before reads
+                            ok = last_product();
+                            if (!ok) return;
                         }
-                        ok = meet();                 // everybody has read the old maxima
-                        if (!ok) return;
-                        if (quarter == 0 && lane < kCols) my_max[c * kCols + lane] = new_max;
 #pragma unroll
-                        for (int i = 0; i < kCols; i += 2) {
-                            float2& x = l[c * (kCols / 2) + i / 2];
-                            x = mul2(x, make_float2(__shfl_sync(0xFFFFFFFFu, f, i), __shfl_sync(0xFFFFFFFFu, f, i + 1)));
-                        }
-                        if (n > 0 && n % kFlush != 0) {
-#pragma unroll 1
-                            for (int part = 0; part < 2; ++part)              // high, residual
-#pragma unroll 1
-                                for (int e = 0; e < kCols; e += 16) {
-                                    uint32_t q[16];
-                                    tmem_ld16(to + part * N + c * kCols + e, q);
-                                    tmem_wait_ld();
+                        for (int c = 0; c < kChunks; ++c) {
+                            // maxima of the tile's tokens: lane i takes column i, then the four warps'
+                            scores(r, c);
+                            float mine_top = -INFINITY;
 #pragma unroll
-                                    for (int i = 0; i < 16; ++i) {
-                                        const float fi = __shfl_sync(0xFFFFFFFFu, f, e + i);
-                                        q[i] = fi != 1.f ? __float_as_uint(__uint_as_float(q[i]) * fi) : q[i];
-                                    }
-                                    tmem_st16(to + part * N + c * kCols + e, q);
-                                }
-                            tmem_wait_st();
-                        }
-                        if (n >= kFlush) {
-#pragma unroll 1
                             for (int i = 0; i < kCols; ++i) {
-                                const float fi = __shfl_sync(0xFFFFFFFFu, f, i);
-                                float* dst = my_flush + (size_t)(c * kCols + i) * kHeadDim;
-                                if (fi != 1.f) __stcg(dst, __ldcg(dst) * fi);
+                                const float v = redux_max(__uint_as_float(r[i]));
+                                if (lane == i) mine_top = v;
+                            }
+                            if constexpr (!SCORE) mine_top *= a.scale_log2;
+                            scratch[quarter * 32 + lane] = mine_top;
+                            ok = meet();
+                            if (!ok) return;
+                            float new_max = 0.f, f = 1.f;
+                            if (lane < kCols) {
+                                const float top = fmaxf(fmaxf(scratch[lane], scratch[32 + lane]), fmaxf(scratch[64 + lane], scratch[96 + lane]));
+                                const float old = my_max[c * kCols + lane];
+                                new_max = old;
+                                if (top > old + kSlack) {
+                                    new_max = top;
+                                    f = old == kUnset ? 0.f : ex2(old - top);
+                                }
+                            }
+                            ok = meet();             // everybody has read the old ones
+                            if (!ok) return;
+                            if (quarter == 0 && lane < kCols) my_max[c * kCols + lane] = new_max;
+#pragma unroll
+                            for (int i = 0; i < kCols; i += 2) {
+                                float2& x = l[c * (kCols / 2) + i / 2];
+                                x = mul2(x, make_float2(__shfl_sync(0xFFFFFFFFu, f, i), __shfl_sync(0xFFFFFFFFu, f, i + 1)));
+                            }
+                            if (n > 0 && n % kFlush != 0) {
+#pragma unroll 1
+                                for (int part = 0; part < 2; ++part)          // high, residual
+#pragma unroll 1
+                                    for (int e = 0; e < kCols; e += 16) {
+                                        uint32_t q[16];
+                                        tmem_ld16(to + part * N + c * kCols + e, q);
+                                        tmem_wait_ld();
+#pragma unroll
+                                        for (int i = 0; i < 16; ++i) {
+                                            const float fi = __shfl_sync(0xFFFFFFFFu, f, e + i);
+                                            q[i] = fi != 1.f ? __float_as_uint(__uint_as_float(q[i]) * fi) : q[i];
+                                        }
+                                        tmem_st16(to + part * N + c * kCols + e, q);
+                                    }
+                                tmem_wait_st();
+                            }
+                            if (n >= kFlush) {
+#pragma unroll 1
+                                for (int i = 0; i < kCols; ++i) {
+                                    const float fi = __shfl_sync(0xFFFFFFFFu, f, i);
+                                    float* dst = my_flush + (size_t)(c * kCols + i) * kHeadDim;
+                                    if (fi != 1.f) __stcg(dst, __ldcg(dst) * fi);
+                                }
                             }
                         }
+                        ok = meet();                 // the new ones are there
+                        if (!ok) return;
                     }
-                    ok = meet();                     // the new maxima are there
-                    if (!ok) return;
+                    calm = !s.careful && all_set();
                 }
                 if (L::kPBuffers == 1 && n > 0) {
                     ok = last_product();
@@ -693,10 +795,9 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 const uint32_t line = base + L::kOffP + (L::kPBuffers > 1 ? buf * L::kP : 0u) + (uint32_t)tok * 128u, swz = (uint32_t)tok & 7u;
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c) {
-                    if (kChunks > 1) {
-                        scores(c);
-                        relative(c);
-                    }
+                    uint32_t r[kCols];
+                    scores(r, c);
+                    relative(r, c);
 #pragma unroll
                     for (int e = 0; e < kCols; e += 8) {
                         uint32_t hi[4], lo[4];
@@ -720,7 +821,6 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 tc_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(kPFull + buf));
-                id = id_next;
             }
             // ---- end of the segment -------------------------------------------------------------------------------
             ok = warp_wait(kOFull + ((j - 1) & 1u), (j - 1) >> 1);
@@ -755,7 +855,10 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 const int col = c * kCols + lane % kCols, row = grp * kRows + col;
                 const float sum = (scratch[lane % kCols] + scratch[32 + lane % kCols]) + (scratch[64 + lane % kCols] + scratch[96 + lane % kCols]);
                 float m = my_max[col];
+                if (sum > kTooLarge && row < live) *redo = 1;
                 if (m == kUnset) m = -INFINITY;
+                else if (SCORE && a.sc.slopes)
+                    m = fmaf(row_slope[row], (float)(p0 - node_pos[min(s.node0 + (int)(((uint32_t)row * a.gq_inv) >> 16), STC_TREE_MAX_NODES - 1)]), m);
                 const float inv = sum != 0.f ? 1.f / sum : 0.f;
                 if (quarter == 0 && lane < kCols && row < live) {
                     if (whole) {
@@ -798,6 +901,9 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 ++tabs;
                 if (lane == 0) mbar_arrive(bar(kTabEmpty));
             }
+            __syncwarp();
+            __threadfence_block();
+            if (lane == 0) atomicAdd(const_cast<int*>(done), 1);
         };
         while (ok && next(ok)) segment();
         if (!ok) give_up();
@@ -845,30 +951,28 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     }
                     if (a.sc.tok_doc) q_doc = a.sc.q_doc[s.b];
                 }
-                auto page_of = [&](int t) { return t > 0 && t >= s.tile0 ? page_at((t - 1) * kTilePages + (tok0 + lane) / kPage) : -1; };
-                auto fetch = [&](int id, uint32_t& m, uint32_t& first) {          // this lane's mask, its page's first group
+                auto page_of = [&](int t) { return t > 0 && t >= s.tile0 ? listed((t - 1) * kTilePages + (tok0 + lane) / kPage) : -1; };
+                // of this lane's token: its mask, its page's first group, its document; asked for a tile ahead
+                auto fetch = [&](int id, uint32_t& m, uint32_t& first, int& doc) {
                     m = first = 0;
+                    doc = -1;
                     const int t = id * kPage + (lane & 15);
-                    if (id >= 0 && t < s.len) {
-                        m = mask_row[t];
-                        if (SCORE) {
-                            if (t < lo_all || t >= hi_all) m = 0;
-                            if (a.sc.tok_doc) {
-                                const int d = __ldg(a.sc.tok_doc + (size_t)s.b * a.T + t);
-                                if (d >= 0 && d != q_doc) m = 0;
-                            }
-                        }
-                    }
-                    if (id >= 0) first = offs[id * kPage];
-                    return id >= 0 && t < s.len ? (uint32_t)mask_row[t] : 0u;
+                    if (!is_page(id)) return -1;
+                    first = offs[id * kPage];
+                    if (t >= s.len) return -1;
+                    m = mask_row[t];
+                    if (SCORE && a.sc.tok_doc) doc = __ldg(a.sc.tok_doc + (size_t)s.b * a.T + t);
+                    return t;
                 };
-                uint32_t m_next, first_next, all_next;
-                all_next = fetch(page_of(s.tile1 - 1), m_next, first_next);
+                uint32_t m_next, first_next;
+                int doc_next, at_next = fetch(page_of(s.tile1 - 1), m_next, first_next, doc_next);
                 int id_next = page_of(s.tile1 - 2);
 #pragma unroll 1
                 for (int t = s.tile1 - 1; t >= s.tile0; --t, ++vc) {
-                    const uint32_t m = m_next & ((1u << S) - 1u), first = first_next, cnt = __popc(all_next & ((1u << S) - 1u));
-                    all_next = fetch(id_next, m_next, first_next);
+                    const uint32_t every = m_next & ((1u << S) - 1u), first = first_next, cnt = __popc(every);
+                    uint32_t m = every;
+                    if (SCORE && (at_next < lo_all || at_next >= hi_all || (doc_next >= 0 && doc_next != q_doc))) m = 0;
+                    at_next = fetch(id_next, m_next, first_next, doc_next);
                     id_next = page_of(t - 2);
                     // place of the token's first group: its page's, and the groups of the page's tokens before it
                     const uint32_t incl = warp_incl_scan(cnt, lane), half = __shfl_sync(0xFFFFFFFFu, incl, 15);
@@ -921,13 +1025,14 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     if (pending >= 0) { cp_async_wait<1>(); publish(); }
                     pending = st;
                 }
+                cp_async_wait<0>();                  // (the next segment may only come when this one is done)
+                if (ok && pending >= 0) publish();
             }
         };
         if (a.S == 4) walk(std::integral_constant<int, 4>{});
         else if (a.S == 8) walk(std::integral_constant<int, 8>{});
         else walk(std::integral_constant<int, 16>{});
         cp_async_wait<0>();
-        if (ok && pending >= 0) publish();
         if (!ok) give_up();
     }
     tc_before();
