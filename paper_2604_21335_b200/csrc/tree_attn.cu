@@ -58,7 +58,7 @@ constexpr float kTooLarge = 4294967296.f;         // sum of weights that sends a
 enum { kQFull, kQEmpty, kKFull, kKEmpty = kKFull + 3, kVFull = kKEmpty + 3, kVEmpty = kVFull + 2, kSFull = kVEmpty + 2,
        kPFull = kSFull + 2, kOFull = kPFull + 2, kGroup = kOFull + 2, kTabFull = kGroup + 2, kTabEmpty, kSegFull,
        kSegEmpty = kSegFull + kSegs, kBars = kSegEmpty + kSegs };
-constexpr uint32_t kCtlTmem = 256, kCtlAbort = 260, kCtlVotes = 264, kCtlRedo = 280, kCtlDone = 284, kCtlSegs = 288, kCtlMax = 384;
+constexpr uint32_t kCtlTmem = 256, kCtlAbort = 260, kCtlRedo = 264, kCtlDone = 268, kCtlSegs = 288, kCtlMax = 384;
 static_assert(kBars * 8 <= kCtlTmem && kCtlSegs + kSegs * 48 <= kCtlMax, "control block");
 
 // Shared memory of a CTA with N rows.
@@ -147,6 +147,28 @@ __device__ __forceinline__ float redux_max(float v) {
 __device__ __forceinline__ void sts16(uint32_t addr, const uint32_t (&v)[4]) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
+// Bounded wait of a converged warp for a barrier's phase; false once it expired or another role has given up.  One copy of
+// the instructions that ask (a kernel with fifty waits is bound by fetching its own code otherwise), and the clock, which is read faster
+// than the timer; its limit is a second at the highest clock.
+__device__ __forceinline__ bool warp_wait_clocked(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+    const long long t0 = clock64();
+#pragma unroll 1
+    for (;;) {
+        if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity))) return true;
+        if (__any_sync(0xFFFFFFFFu, *abort_flag != 0 || clock64() - t0 > 2000000000ll)) return false;
+    }
+}
+// 8 consecutive columns of the warp's 32 lanes <-> registers.
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, uint32_t (&r)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
 // COLS consecutive columns of the warp's 32 lanes.
 template <int COLS>
 __device__ __forceinline__ void tmem_ld(uint32_t addr, uint32_t (&r)[COLS]) {
@@ -166,7 +188,6 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     unsigned char* const ctl = smem + L::kOffCtl;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctl + kCtlTmem);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + kCtlAbort);
-    volatile uint32_t* votes = reinterpret_cast<volatile uint32_t*>(ctl + kCtlVotes);       // [2 groups][2]
     volatile int* redo = reinterpret_cast<volatile int*>(ctl + kCtlRedo);                   // a sum came out too large
     volatile int* done = reinterpret_cast<volatile int*>(ctl + kCtlDone);                   // softmax warps that finished a segment, counted
     volatile int* segs = reinterpret_cast<volatile int*>(ctl + kCtlSegs);                   // [kSegs][12]
@@ -187,7 +208,6 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                                 : i == kTabEmpty ? 8 : i >= kSegEmpty ? kSegReaders : 1);
         fence_mbar_init();
     }
-    if (threadIdx.x < 4) votes[threadIdx.x] = 0;
     if (threadIdx.x == 5) *redo = *done = 0;
     if (threadIdx.x == 4) *abort_flag = (base & 1023u) != 0 ? (int)STC_ERR_CUDA : 0;        // swizzled tiles need 1024-byte aligned bases
     if (warp == 1) {
@@ -242,7 +262,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     __syncthreads();                                 // (the ancestors' table takes their place)
 
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
-    auto warp_wait = [&](int i, uint32_t phase) { return mbar_warp_wait_or_abort(bar(i), phase & 1u, abort_flag, kWaitNs); };
+    auto warp_wait = [&](int i, uint32_t phase) { return warp_wait_clocked(bar(i), phase & 1u, abort_flag); };
     auto give_up = [&]() { atomicCAS(const_cast<int*>(abort_flag), 0, (int)STC_ERR_TIMEOUT); };
     Segment s;
     int n_seg = 0;
@@ -331,7 +351,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             for (int n = 0; ok && n < tiles + 2; ++n) {
                 if (n >= 2) {
                     const uint32_t j = tile + (uint32_t)(n - 2), st = j % L::kVStages, buf = j & 1u;
-                    ok = warp_wait(kPFull + buf, j >> 1) && warp_wait(kVFull + st, j / L::kVStages);
+                    ok = warp_wait(kVFull + st, j / L::kVStages) && warp_wait(kPFull + buf, j >> 1);    // (what is late last)
                     if (!ok) break;
                     tc_after();
                     const uint64_t dv = smem_desc_128(sm + L::kOffV + st * kTile, kHalf);
@@ -614,87 +634,44 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         }
                     }
                 }
-                // raw products of the rows from `row` on -> scores: raw ones, or finished ones in log2 units (but for slope times
-                // p0 - p, which is the same for all tokens) with SCORE; -inf where the row does not see the token
-                auto finish = [&](auto& r, int row) {
-                    constexpr int C = sizeof(r) / sizeof(r[0]);
-                    if constexpr (SCORE) {
-                        if (a.cap_in != 0.f) {
-                            // (what a row does not see, and columns without a row, have no say in how the others are capped)
-                            float most = 0.f;
-                            if (row + C <= mine) {
-                                most = magnitude(r);
-                            } else {
+                // Tiles out of the ordinary are finished in place first, eight rows at a time: scores in log2 units with SCORE (but for
+                // slope times p0 - p, which is the same for all tokens of a row), -inf where a row does not see the token.
+                const bool finished = !open || (SCORE && !calm);
+                if (finished) {
+#pragma unroll 1
+                    for (int c = 0; c < kRows; c += 8) {
+                        uint32_t r[8];
+                        tmem_ld8(ts + c, r);
+                        tmem_wait_ld();
+                        const uint32_t bits = (uint32_t)(see >> c);
 #pragma unroll
-                                for (int i = 0; i < C; ++i) most = row + i < mine ? fmaxf(most, fabsf(__uint_as_float(r[i]))) : most;
+                        for (int i = 0; i < 8; ++i) {
+                            float y = __uint_as_float(r[i]);
+                            if constexpr (SCORE) {
+                                y = a.cap_in != 0.f ? cap_any(y, a.cap_in, a.cap_log2) : y * a.scale_log2;
+                                y = fmaf(row_slope[grp * kRows + c + i], far, y);
                             }
-                            if (open && __all_sync(0xFFFFFFFFu, most * fabsf(a.cap_in) <= kCapSmall))
-                                cap_scores_low(r, a.cap_in, a.scale_log2);
-                            else
-                                cap_scores_any(r, a.cap_in, a.cap_log2);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < C; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * a.scale_log2);
+                            r[i] = (bits >> i) & 1u ? __float_as_uint(y) : __float_as_uint(-INFINITY);
                         }
-                        if (a.sc.slopes) {
-                            const float2* slope = reinterpret_cast<const float2*>(row_slope + grp * kRows + row);
-#pragma unroll
-                            for (int i = 0; i < C; i += 2) {
-                                const float2 y = fma2(slope[i / 2], both(far), make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])));
-                                r[i] = __float_as_uint(y.x);
-                                r[i + 1] = __float_as_uint(y.y);
-                            }
-                        }
+                        tmem_st8(ts + c, r);
                     }
-                    if (!open) {
-                        const uint32_t bits = (uint32_t)(see >> row);
-#pragma unroll
-                        for (int i = 0; i < C; ++i)
-                            if (!((bits >> i) & 1u)) r[i] = __float_as_uint(-INFINITY);
-                    }
-                };
-                auto scores = [&](uint32_t (&r)[kCols], int c) {
-                    tmem_ld<kCols>(ts + c * kCols, r);
-                    tmem_wait_ld();
-                    finish(r, c * kCols);
-                };
-                // exponents relative to the rows' references
-                auto relative = [&](uint32_t (&r)[kCols], int c) {
-                    const float4* ref = reinterpret_cast<const float4*>(my_max + c * kCols);
-#pragma unroll
-                    for (int i = 0; i < kCols; i += 4) {
-                        const float4 m = ref[i / 4];
-                        float2 x = make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
-                        float2 y = make_float2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
-                        if constexpr (SCORE) {
-                            x = add2(x, make_float2(-m.x, -m.y));
-                            y = add2(y, make_float2(-m.z, -m.w));
-                        } else {
-                            x = fma2(x, both(a.scale_log2), make_float2(-m.x, -m.y));
-                            y = fma2(y, both(a.scale_log2), make_float2(-m.z, -m.w));
-                        }
-                        r[i] = __float_as_uint(x.x); r[i + 1] = __float_as_uint(x.y);
-                        r[i + 2] = __float_as_uint(y.x); r[i + 3] = __float_as_uint(y.y);
-                    }
-                };
+                    tmem_wait_st();
+                }
                 auto all_set = [&]() {               // (the same answer in the group's four warps)
                     bool unset = lane < kRows && my_max[lane % kRows] == kUnset;
                     if (kRows > 32) unset = unset || my_max[32 % kRows + lane % 32] == kUnset;
                     return !__any_sync(0xFFFFFFFFu, unset);
                 };
-                if (n == 0 && !s.careful) {
-                    // a first reference: this warp's quarter of the rows, over its own tokens
+                if (n == 0 && !s.careful && !(SCORE && a.sc.slopes)) {
+                    // a first reference: this warp's quarter of the rows, over its own tokens (with slopes only the nearest would do)
                     constexpr int kShare = kRows / 4;
-                    uint32_t q[16], r[kShare];
+                    uint32_t q[16];
                     tmem_ld16(ts + quarter * kShare, q);
                     tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < kShare; ++i) r[i] = q[i];
-                    finish(r, quarter * kShare);
                     float top = -INFINITY;
 #pragma unroll
                     for (int i = 0; i < kShare; ++i) {
-                        const float v = redux_max(__uint_as_float(r[i]));
+                        const float v = redux_max(__uint_as_float(q[i]));
                         if (lane == i) top = v;
                     }
                     if (!SCORE) top *= a.scale_log2;             // (the scale is positive)
@@ -704,87 +681,75 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     calm = all_set();
                 }
                 if (__builtin_expect(!calm, 0)) {
-                    uint32_t r[kCols];
-#pragma unroll 1
-                    for (int attempt = 0;; ++attempt) {
-                        bool exceeds = false;
-#pragma unroll 1
-                        for (int c = 0; c < kChunks; ++c) {
-                            scores(r, c);
-                            relative(r, c);
+                    // the true maxima of the tile's tokens against the references; 16 rows at a time: lane i takes row i, then the four warps'
+                    if (L::kPBuffers == 1 && n > 0) {            // the scratch is P, which the product before reads
+                        ok = last_product();
+                        if (!ok) return;
+                    }
+                    float f[kRows / 16];                         // factors of rows 16 i + lane
+                    bool moves = false;
 #pragma unroll
-                            for (int i = 0; i < kCols; ++i) exceeds |= __uint_as_float(r[i]) > kSlack;
+                    for (int c = 0; c < kRows / 16; ++c) {
+                        uint32_t q[16];
+                        tmem_ld16(ts + c * 16, q);
+                        tmem_wait_ld();
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float v = redux_max(__uint_as_float(q[i]));
+                            if (lane == i) top = v;
                         }
-                        const uint32_t tag = meets + 1u, at = grp * 2u + (meets & 1u);
-                        if (__any_sync(0xFFFFFFFFu, exceeds) && lane == 0) votes[at] = tag;
+                        if (!SCORE) top *= a.scale_log2;
+                        scratch[quarter * 32 + lane] = top;
                         ok = meet();
                         if (!ok) return;
-                        if (votes[at] != tag || attempt == 1) break;
-                        if (n > 0 && (L::kPBuffers == 1 || n % kFlush != 0)) {    // the scratch may be P, which the product before reads
+                        top = fmaxf(fmaxf(scratch[lane], scratch[32 + lane]), fmaxf(scratch[64 + lane], scratch[96 + lane]));
+                        const float old = my_max[c * 16 + lane % 16];
+                        const bool move = lane < 16 && top > old + kSlack;
+                        f[c] = !move ? 1.f : old == kUnset ? 0.f : ex2(old - top);
+                        moves |= __any_sync(0xFFFFFFFFu, move) != 0;
+                        ok = meet();                             // everybody has read the old ones
+                        if (!ok) return;
+                        if (quarter == 0 && move) my_max[c * 16 + lane] = top;
+                    }
+                    if (moves) {                                 // sums and accumulator follow
+#pragma unroll
+                        for (int i = 0; i < kRows; i += 2)
+                            l[i / 2] = mul2(l[i / 2], make_float2(__shfl_sync(0xFFFFFFFFu, f[i / 16], i % 16),
+                                                                  __shfl_sync(0xFFFFFFFFu, f[i / 16], i % 16 + 1)));
+                        if (n > 0 && n % kFlush != 0) {
                             ok = last_product();
                             if (!ok) return;
                         }
 #pragma unroll
-                        for (int c = 0; c < kChunks; ++c) {
-                            // maxima of the tile's tokens: lane i takes column i, then the four warps'
-                            scores(r, c);
-                            float mine_top = -INFINITY;
-#pragma unroll
-                            for (int i = 0; i < kCols; ++i) {
-                                const float v = redux_max(__uint_as_float(r[i]));
-                                if (lane == i) mine_top = v;
-                            }
-                            if constexpr (!SCORE) mine_top *= a.scale_log2;
-                            scratch[quarter * 32 + lane] = mine_top;
-                            ok = meet();
-                            if (!ok) return;
-                            float new_max = 0.f, f = 1.f;
-                            if (lane < kCols) {
-                                const float top = fmaxf(fmaxf(scratch[lane], scratch[32 + lane]), fmaxf(scratch[64 + lane], scratch[96 + lane]));
-                                const float old = my_max[c * kCols + lane];
-                                new_max = old;
-                                if (top > old + kSlack) {
-                                    new_max = top;
-                                    f = old == kUnset ? 0.f : ex2(old - top);
-                                }
-                            }
-                            ok = meet();             // everybody has read the old ones
-                            if (!ok) return;
-                            if (quarter == 0 && lane < kCols) my_max[c * kCols + lane] = new_max;
-#pragma unroll
-                            for (int i = 0; i < kCols; i += 2) {
-                                float2& x = l[c * (kCols / 2) + i / 2];
-                                x = mul2(x, make_float2(__shfl_sync(0xFFFFFFFFu, f, i), __shfl_sync(0xFFFFFFFFu, f, i + 1)));
-                            }
+                        for (int c = 0; c < kRows / 16; ++c) {
                             if (n > 0 && n % kFlush != 0) {
 #pragma unroll 1
-                                for (int part = 0; part < 2; ++part)          // high, residual
-#pragma unroll 1
-                                    for (int e = 0; e < kCols; e += 16) {
-                                        uint32_t q[16];
-                                        tmem_ld16(to + part * N + c * kCols + e, q);
-                                        tmem_wait_ld();
+                                for (int part = 0; part < 2; ++part) {        // high, residual
+                                    uint32_t q[16];
+                                    tmem_ld16(to + part * N + c * 16, q);
+                                    tmem_wait_ld();
 #pragma unroll
-                                        for (int i = 0; i < 16; ++i) {
-                                            const float fi = __shfl_sync(0xFFFFFFFFu, f, e + i);
-                                            q[i] = fi != 1.f ? __float_as_uint(__uint_as_float(q[i]) * fi) : q[i];
-                                        }
-                                        tmem_st16(to + part * N + c * kCols + e, q);
+                                    for (int i = 0; i < 16; ++i) {
+                                        const float fi = __shfl_sync(0xFFFFFFFFu, f[c], i);
+                                        q[i] = fi != 1.f ? __float_as_uint(__uint_as_float(q[i]) * fi) : q[i];
                                     }
+                                    tmem_st16(to + part * N + c * 16, q);
+                                }
                                 tmem_wait_st();
                             }
                             if (n >= kFlush) {
 #pragma unroll 1
-                                for (int i = 0; i < kCols; ++i) {
-                                    const float fi = __shfl_sync(0xFFFFFFFFu, f, i);
-                                    float* dst = my_flush + (size_t)(c * kCols + i) * kHeadDim;
+                                for (int i = 0; i < 16; ++i) {
+                                    const float fi = __shfl_sync(0xFFFFFFFFu, f[c], i);
+                                    float* dst = my_flush + (size_t)(c * 16 + i) * kHeadDim;
                                     if (fi != 1.f) __stcg(dst, __ldcg(dst) * fi);
                                 }
                             }
                         }
-                        ok = meet();                 // the new ones are there
-                        if (!ok) return;
                     }
+                    ok = meet();                                 // the new ones are there
+                    if (!ok) return;
                     calm = !s.careful && all_set();
                 }
                 if (L::kPBuffers == 1 && n > 0) {
@@ -794,17 +759,51 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 // weights, their sums, and P: eight rows of a token are 16 bytes of its line
                 const uint32_t line = base + L::kOffP + (L::kPBuffers > 1 ? buf * L::kP : 0u) + (uint32_t)tok * 128u, swz = (uint32_t)tok & 7u;
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c) {
+                for (int c = 0; c < kRows; c += kCols) {
                     uint32_t r[kCols];
-                    scores(r, c);
-                    relative(r, c);
+                    tmem_ld<kCols>(ts + c, r);
+                    tmem_wait_ld();
+                    if (SCORE && !finished) {
+                        if (a.cap_in != 0.f) {
+                            // (what a row does not see, and columns without a row, have no say in how the others are capped)
+                            float most = 0.f;
+                            if (c + kCols <= mine) {
+                                most = magnitude(r);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < kCols; ++i) most = c + i < mine ? fmaxf(most, fabsf(__uint_as_float(r[i]))) : most;
+                            }
+                            if (__all_sync(0xFFFFFFFFu, most * fabsf(a.cap_in) <= kCapSmall))
+                                cap_scores_low(r, a.cap_in, a.scale_log2);
+                            else
+                                cap_scores_any(r, a.cap_in, a.cap_log2);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < kCols; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * a.scale_log2);
+                        }
+                        if (a.sc.slopes) {
+                            const float2* slope = reinterpret_cast<const float2*>(row_slope + grp * kRows + c);
+#pragma unroll
+                            for (int i = 0; i < kCols; i += 2) {
+                                const float2 y = fma2(slope[i / 2], both(far), make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])));
+                                r[i] = __float_as_uint(y.x);
+                                r[i + 1] = __float_as_uint(y.y);
+                            }
+                        }
+                    }
+                    const float4* ref = reinterpret_cast<const float4*>(my_max + c);
 #pragma unroll
                     for (int e = 0; e < kCols; e += 8) {
                         uint32_t hi[4], lo[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const float2 p = make_float2(ex2(__uint_as_float(r[e + 2 * i])), ex2(__uint_as_float(r[e + 2 * i + 1])));
-                            float2& sum = l[c * (kCols / 2) + e / 2 + i];
+                            const float4 m4 = ref[(e + 2 * i) / 4];
+                            const float2 m = i & 1 ? make_float2(-m4.z, -m4.w) : make_float2(-m4.x, -m4.y);
+                            float2 x = make_float2(__uint_as_float(r[e + 2 * i]), __uint_as_float(r[e + 2 * i + 1]));
+                            if constexpr (SCORE) x = add2(x, m);
+                            else x = fma2(x, both(a.scale_log2), m);
+                            const float2 p = make_float2(ex2(x.x), ex2(x.y));
+                            float2& sum = l[(c + e) / 2 + i];
                             sum = add2(sum, p);
                             const __nv_bfloat162 h2 = __floats2bfloat162_rn(p.x, p.y);
                             hi[i] = *reinterpret_cast<const uint32_t*>(&h2);
@@ -812,7 +811,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                             const __nv_bfloat162 r2 = __floats2bfloat162_rn(d.x, d.y);
                             lo[i] = *reinterpret_cast<const uint32_t*>(&r2);
                         }
-                        const uint32_t eh = (uint32_t)(grp * kRows + c * kCols + e), el = eh + N;
+                        const uint32_t eh = (uint32_t)(grp * kRows + c + e), el = eh + N;
                         sts16(line + (eh >> 6) * kHalf + ((((eh & 63u) >> 3) ^ swz) << 4), hi);
                         sts16(line + (el >> 6) * kHalf + ((((el & 63u) >> 3) ^ swz) << 4), lo);
                     }
@@ -827,6 +826,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (!ok) return;
             tc_after();
             const bool whole = s.slot < 0;
+            float inv[kChunks];                      // of row 32 c + lane
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) {
                 // sums over the warp's lanes, lane i keeping column i: halves change places, then a quarter of each ...
@@ -849,53 +849,59 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, w);
                     }
                 }
-                scratch[quarter * 32 + lane] = v[0];
-                ok = meet();
-                if (!ok) return;
+                scratch[(c * 4 + quarter) * 32 + lane] = v[0];
+            }
+            ok = meet();
+            if (!ok) return;
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
                 const int col = c * kCols + lane % kCols, row = grp * kRows + col;
-                const float sum = (scratch[lane % kCols] + scratch[32 + lane % kCols]) + (scratch[64 + lane % kCols] + scratch[96 + lane % kCols]);
+                const float* part = scratch + c * 128 + lane % kCols;
+                const float sum = (part[0] + part[32]) + (part[64] + part[96]);
                 float m = my_max[col];
+                const uint32_t in_block = ((uint32_t)row * a.gq_inv) >> 16;
                 if (sum > kTooLarge && row < live) *redo = 1;
                 if (m == kUnset) m = -INFINITY;
                 else if (SCORE && a.sc.slopes)
-                    m = fmaf(row_slope[row], (float)(p0 - node_pos[min(s.node0 + (int)(((uint32_t)row * a.gq_inv) >> 16), STC_TREE_MAX_NODES - 1)]), m);
-                const float inv = sum != 0.f ? 1.f / sum : 0.f;
+                    m = fmaf(row_slope[row], (float)(p0 - node_pos[min(s.node0 + (int)in_block, STC_TREE_MAX_NODES - 1)]), m);
+                inv[c] = sum != 0.f ? 1.f / sum : 0.f;
                 if (quarter == 0 && lane < kCols && row < live) {
                     if (whole) {
-                        const uint32_t in_block = ((uint32_t)row * a.gq_inv) >> 16;
                         const size_t at = ((size_t)s.b * a.n_cap + s.node0 + in_block) * a.Hq + s.hk * a.Gq + (row - in_block * a.Gq);
                         if (a.lse) a.lse[at] = sum != 0.f ? (m + log2f(sum)) * kLn2 : -INFINITY;
                     } else {
                         a.part_ml[(size_t)s.slot * N + row] = make_float2(m, sum);
                     }
                 }
-#pragma unroll 1
-                for (int e = 0; e < kCols; e += 16) {
-                    if (grp * kRows + c * kCols + e >= live) break;
-                    uint32_t hi[16], lo[16];
-                    tmem_ld16(to + c * kCols + e, hi);
-                    tmem_ld16(to + N + c * kCols + e, lo);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int row_i = grp * kRows + c * kCols + e + i;
-                        const float inv_i = __shfl_sync(0xFFFFFFFFu, inv, e + i);
-                        float x = __uint_as_float(hi[i]) + __uint_as_float(lo[i]);
-                        if (row_i < live) {
-                            if (count > kFlush) x += __ldcg(my_flush + (size_t)(c * kCols + e + i) * kHeadDim);
-                            if (whole) {
-                                const uint32_t in_block = ((uint32_t)row_i * a.gq_inv) >> 16;
-                                const size_t at = ((size_t)s.b * a.n_cap + s.node0 + in_block) * a.Hq + s.hk * a.Gq + (row_i - in_block * a.Gq);
-                                a.out[at * kHeadDim + tok] = inv_i != 0.f ? x * inv_i : 0.f;   // (0: nothing seen)
-                            } else {
-                                __stcg(a.part_o + ((size_t)s.slot * N + row_i) * kHeadDim + tok, x);
-                            }
-                        }
-                    }
-                }
-                ok = meet();                         // scratch and maxima are free again
-                if (!ok) return;
             }
+            // rows of O: the row's place among the outputs (or the partials) moves on by a head at a time
+            const uint32_t node_at = ((uint32_t)(grp * kRows) * a.gq_inv) >> 16;
+            int h = grp * kRows - (int)node_at * a.Gq;
+            float* dst = whole ? a.out + (((size_t)s.b * a.n_cap + s.node0 + node_at) * a.Hq + s.hk * a.Gq + h) * kHeadDim + tok
+                               : a.part_o + ((size_t)s.slot * N + grp * kRows) * kHeadDim + tok;
+            const size_t jump = whole ? (size_t)(a.Hq - a.Gq + 1) * kHeadDim : kHeadDim;      // to the next node's first head
+#pragma unroll 1
+            for (int c = 0; c < kRows && c < mine; c += 8) {
+                uint32_t hi[8], lo[8];
+                float old[8];
+                tmem_ld8(to + c, hi);
+                tmem_ld8(to + N + c, lo);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) old[i] = count > kFlush ? __ldcg(my_flush + (size_t)(c + i) * kHeadDim) : 0.f;
+                tmem_wait_ld();
+                const float inv_c = kChunks == 1 || c < 32 ? inv[0] : inv[kChunks - 1];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float inv_i = __shfl_sync(0xFFFFFFFFu, inv_c, (c + i) & 31);
+                    float x = __uint_as_float(hi[i]) + __uint_as_float(lo[i]) + old[i];
+                    if (whole) x = inv_i != 0.f ? x * inv_i : 0.f;            // (0: nothing seen)
+                    if (c + i < mine) __stcg(dst, x);
+                    dst += ++h == a.Gq ? jump : (size_t)kHeadDim;
+                    if (h == a.Gq) h = 0;
+                }
+            }
+            ok = meet();                             // scratch and references are free again
+            if (!ok) return;
             tc_before();
             if (tables) {
                 ++tabs;
@@ -923,14 +929,14 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (lane == 0) mbar_arrive(bar(kVFull + pending));
             pending = -1;
         };
-        auto walk = [&](auto groups) {
-            constexpr int S = decltype(groups)::value, OPG = kOctets / S, LPT = OPG < 2 ? 2 : OPG, GPL = LPT / OPG;
-            const int sub = lane % LPT;
+        const int opg = kOctets / a.S;               // 16-byte chunks of a group
+        const uint32_t all_groups = (1u << a.S) - 1u, limit = (uint32_t)min(a.cap_groups, (int64_t)0xFFFFFFFF);   // (of the store)
+        {
             while (ok && next(ok)) {
                 const size_t problem = (size_t)s.b * a.Hkv + s.hk;
                 const uint16_t* mask_row = a.v_mask + problem * a.T;
                 const uint32_t* offs = a.v_offs + problem * (a.T + 1);
-                const uint4* packed = a.v_packed + problem * a.cap_groups * OPG;
+                const uint4* packed = a.v_packed + problem * a.cap_groups * opg;
                 const uint4* fresh = a.v_new + problem * a.n_cap * kOctets;
                 // tokens that no row of the sequence sees are left out: they may hold anything
                 int lo_all = 0, hi_all = s.len, q_doc = 0;
@@ -969,7 +975,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 int id_next = page_of(s.tile1 - 2);
 #pragma unroll 1
                 for (int t = s.tile1 - 1; t >= s.tile0; --t, ++vc) {
-                    const uint32_t every = m_next & ((1u << S) - 1u), first = first_next, cnt = __popc(every);
+                    const uint32_t every = m_next & all_groups, first = first_next, cnt = __popc(every);
                     uint32_t m = every;
                     if (SCORE && (at_next < lo_all || at_next >= hi_all || (doc_next >= 0 && doc_next != q_doc))) m = 0;
                     at_next = fetch(id_next, m_next, first_next, doc_next);
@@ -995,31 +1001,37 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                                              there ? fresh + (size_t)tok * kOctets + oct : fresh, there ? 16 : 0);
                         }
                     } else {
-                        const uint32_t limit = (uint32_t)min(a.cap_groups, (int64_t)0xFFFFFFFF);   // groups of the store
+                        auto copy = [&](auto groups) {
+                            constexpr int S = decltype(groups)::value, OPG = kOctets / S, LPT = OPG < 2 ? 2 : OPG, GPL = LPT / OPG;
+                            const int sub = lane % LPT;
 #pragma unroll 1
-                        for (int pass = 0; pass < LPT; ++pass) {
-                            const int tok = pass * (32 / LPT) + lane / LPT;       // of the warp's 32
-                            const uint32_t tm = __shfl_sync(0xFFFFFFFFu, m, tok);
-                            uint32_t at = __shfl_sync(0xFFFFFFFFu, place, tok);   // place of the next kept group of the token
-                            const uint32_t row = tile + (uint32_t)(tok0 + tok) * 128u, swz = (uint32_t)(tok & 7);
+                            for (int pass = 0; pass < LPT; ++pass) {
+                                const int tok = pass * (32 / LPT) + lane / LPT;       // of the warp's 32
+                                const uint32_t tm = __shfl_sync(0xFFFFFFFFu, m, tok);
+                                uint32_t at = __shfl_sync(0xFFFFFFFFu, place, tok);   // place of the next kept group of the token
+                                const uint32_t row = tile + (uint32_t)(tok0 + tok) * 128u, swz = (uint32_t)(tok & 7);
 #pragma unroll
-                            for (int k = 0; k < 16 / LPT; ++k) {
-                                const uint32_t oct = (uint32_t)(k * LPT + sub);   // chunk of the row: half oct >> 3, swizzled by the token
-                                uint32_t mine_at = at;
-                                bool kept;
-                                if constexpr (GPL == 1) {
-                                    kept = (tm >> k) & 1u;
-                                    at += kept;
-                                } else {
-                                    kept = (tm >> (2 * k + sub)) & 1u;
-                                    if (sub) mine_at += (tm >> (2 * k)) & 1u;
-                                    at += ((tm >> (2 * k)) & 1u) + ((tm >> (2 * k + 1)) & 1u);
+                                for (int k = 0; k < 16 / LPT; ++k) {
+                                    const uint32_t oct = (uint32_t)(k * LPT + sub);   // chunk of the row: half oct >> 3, swizzled by the token
+                                    uint32_t mine_at = at;
+                                    bool kept;
+                                    if constexpr (GPL == 1) {
+                                        kept = (tm >> k) & 1u;
+                                        at += kept;
+                                    } else {
+                                        kept = (tm >> (2 * k + sub)) & 1u;
+                                        if (sub) mine_at += (tm >> (2 * k)) & 1u;
+                                        at += ((tm >> (2 * k)) & 1u) + ((tm >> (2 * k + 1)) & 1u);
+                                    }
+                                    kept = kept && mine_at < limit;
+                                    cp_async16_zfill(row + (oct >> 3) * kHalf + (((oct & 7u) ^ swz) << 4),
+                                                     kept ? packed + (size_t)mine_at * OPG + sub % OPG : a.v_new, kept ? 16 : 0);
                                 }
-                                kept = kept && mine_at < limit;
-                                cp_async16_zfill(row + (oct >> 3) * kHalf + (((oct & 7u) ^ swz) << 4),
-                                                 kept ? packed + (size_t)mine_at * OPG + sub % OPG : a.v_new, kept ? 16 : 0);
                             }
-                        }
+                        };
+                        if (a.S == 8) copy(std::integral_constant<int, 8>{});
+                        else if (a.S == 16) copy(std::integral_constant<int, 16>{});
+                        else copy(std::integral_constant<int, 4>{});
                     }
                     cp_async_commit();
                     if (pending >= 0) { cp_async_wait<1>(); publish(); }
@@ -1028,10 +1040,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 cp_async_wait<0>();                  // (the next segment may only come when this one is done)
                 if (ok && pending >= 0) publish();
             }
-        };
-        if (a.S == 4) walk(std::integral_constant<int, 4>{});
-        else if (a.S == 8) walk(std::integral_constant<int, 8>{});
-        else walk(std::integral_constant<int, 16>{});
+        }
         cp_async_wait<0>();
         if (!ok) give_up();
     }
