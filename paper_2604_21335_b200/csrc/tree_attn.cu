@@ -19,7 +19,7 @@
 // score exceeds it by more than 2^8 (a vote of the four warps); then the true maxima are taken, and sums and accumulator follow.
 // Rows without a reference (first tiles that they do not see) go the careful way until they have one.
 //
-// Work split.  Unit = (sequence, KV head, block of nodes); its tiles are the tree (tile 0) and then eight listed pages each.  The tiles
+// Work split.  Unit = (sequence, KV head, block of nodes); its tiles are eight listed pages each and, last, the tree.  The tiles
 // of all units form one flat sequence that is cut into equal contiguous ranges, one per CTA (one CTA per SM).  A unit within
 // a range is finished in place; of others each CTA leaves (max, sum, accumulator), which a second kernel joins in CTA order:
 // no atomics, the same bits every time.
@@ -47,31 +47,35 @@ constexpr int kSegs = 2;                          // segments the scheduler may 
 constexpr int kSegReaders = 15;                   // warps that follow the segments: all but the scheduler
 constexpr uint32_t kHalf = kTok * 128;            // 64 channels of a token tile: 128 rows of 128 bytes
 constexpr uint32_t kTile = 2 * kHalf;             // 32 KiB
+constexpr uint32_t kSlot = kTile / 2;             // values of 64 tokens: two halves of 64 channels
 constexpr int kFlush = 16;                        // tiles an accumulator takes: 128 products, at most 5e-6 of it
 constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;                     // log2 units a maximum may be exceeded by
 constexpr float kUnset = -3.0e38f;                // reference of a row that has seen nothing: every finite score exceeds it
-constexpr float kTooLarge = 4294967296.f;         // sum of weights that sends a CTA over its range again
+constexpr float kTooLarge = 1.8446744e19f;        // 2^64: sum of weights that sends a CTA over its range again
 
 // barriers, in 8-byte words of the control block
-enum { kQFull, kQEmpty, kKFull, kKEmpty = kKFull + 3, kVFull = kKEmpty + 3, kVEmpty = kVFull + 2, kSFull = kVEmpty + 2,
+enum { kQFull, kQEmpty, kKFull, kKEmpty = kKFull + 3, kVFull = kKEmpty + 3, kVEmpty = kVFull + 8, kSFull = kVEmpty + 8,
        kPFull = kSFull + 2, kOFull = kPFull + 2, kGroup = kOFull + 2, kTabFull = kGroup + 2, kTabEmpty, kSegFull,
        kSegEmpty = kSegFull + kSegs, kBars = kSegEmpty + kSegs };
-constexpr uint32_t kCtlTmem = 256, kCtlAbort = 260, kCtlRedo = 264, kCtlDone = 268, kCtlSegs = 288, kCtlMax = 384;
-static_assert(kBars * 8 <= kCtlTmem && kCtlSegs + kSegs * 48 <= kCtlMax, "control block");
+constexpr int kRing = 6;                          // tiles whose valid tokens are kept: K stages, two score buffers and one more are under way
+constexpr uint32_t kCtlTmem = 304, kCtlAbort = 308, kCtlRedo = 312, kCtlDone = 316, kCtlSegs = 320, kCtlValid = 416, kCtlMax = 512;
+static_assert(kBars * 8 <= kCtlTmem && kCtlSegs + kSegs * 48 <= kCtlValid && kCtlValid + kRing * 16 <= kCtlMax, "control block");
 
 // Shared memory of a CTA with N rows.
 template <int N>
 struct Plan {
-    static constexpr int kKStages = N == 32 ? 3 : 2, kVStages = 2, kPBuffers = N == 128 ? 1 : 2;
+    static constexpr int kKStages = N == 32 ? 3 : 2, kVSlots = 4, kPBuffers = N == 128 ? 1 : 2;    // K tiles; half V tiles; P
+    static constexpr int kTurns = kVSlots / 2, kTileWarps = 4 / kTurns;                    // V tiles in flight; warps that fill one
     static constexpr uint32_t kQHalf = N * 128, kP = kTok * 2 * N * 2;
-    static constexpr uint32_t kOffK = 2 * kQHalf, kOffV = kOffK + kKStages * kTile, kOffP = kOffV + kVStages * kTile;
+    static constexpr uint32_t kOffK = 2 * kQHalf, kOffV = kOffK + kKStages * kTile, kOffP = kOffV + kVSlots * kSlot;
     static constexpr uint32_t kOffCtl = kOffP + kPBuffers * kP;
     static constexpr uint32_t kCtlKin = kCtlMax + N * 4;                                   // [128 nodes][4 words]
     static constexpr uint32_t kCtlScratch = kCtlKin + STC_TREE_MAX_NODES * 16;             // [2 groups][4 warps][32], positions, slopes
     static constexpr uint32_t kCtlPos = kCtlScratch + 1024, kCtlRowSlope = kCtlPos + 512;
-    static constexpr uint32_t kCtlBytes = N == 128 ? kCtlScratch : kCtlRowSlope + 256;
+    static constexpr uint32_t kCtlIds = kCtlRowSlope + 256;                                // [ring][8 pages]
+    static constexpr uint32_t kCtlBytes = N == 128 ? kCtlScratch : kCtlIds + kRing * 32;
     static constexpr uint32_t kSmem = kOffCtl + kCtlBytes;
     static_assert(kSmem <= 232448, "shared memory of a block");
 };
@@ -91,7 +95,7 @@ struct TreeArgs {
     int32_t* status;             // [B]
     int32_t* word;               // the call's status word
     int32_t* cta_status;         // [grid]
-    int32_t* base;               // [problems + 2]: where each problem begins in the flat sequence; its length; CTAs that share it
+    int32_t* base;               // [problems + 1]: where each problem begins in the flat sequence, and its length
     float2* part_ml;             // [2 * grid][N]
     float* part_o;               // [2 * grid][N][128]
     float* flush;                // [grid][N][128]: sums of emptied accumulators
@@ -128,9 +132,20 @@ __device__ __forceinline__ int problem_length(const TreeArgs& a, int problem) {
     const Unit u = unit_of(a, nodes, list);
     return u.tiles * u.blocks;
 }
-// CTA `c` of `n` takes the positions [total * c / n, total * (c + 1) / n) of the flat sequence.
-__device__ __forceinline__ int range_begin(int total, int c, int n) { return (int)((long long)total * c / n); }
-__device__ __forceinline__ int cta_of(int total, int x, int n) { return (int)((((long long)x + 1) * n + total - 1) / total - 1); }
+// The flat sequence is cut into `n` ranges of `each` tiles, the first `more` of them one longer.
+struct Cut {
+    int n, each, more;
+    __device__ __forceinline__ Cut(int total, int grid) {
+        n = min(total, grid);
+        each = n > 0 ? (int)((uint32_t)total / (uint32_t)n) : 0;
+        more = total - each * n;
+    }
+    __device__ __forceinline__ int begin(int c) const { return c * each + min(c, more); }
+    __device__ __forceinline__ int owner(int x) const {                       // of position x
+        const int longer = more * (each + 1);
+        return x < longer ? (int)((uint32_t)x / (uint32_t)(each + 1)) : more + (int)((uint32_t)(x - longer) / (uint32_t)each);
+    }
+};
 
 // One segment: tiles [tile0, tile1) of one unit.
 struct Segment {
@@ -151,12 +166,18 @@ __device__ __forceinline__ void sts16(uint32_t addr, const uint32_t (&v)[4]) {
 // the instructions that ask (a kernel with fifty waits is bound by fetching its own code otherwise), and the clock, which is read faster
 // than the timer; its limit is a second at the highest clock.
 __device__ __forceinline__ bool warp_wait_clocked(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+    if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity))) return true;
     const long long t0 = clock64();
 #pragma unroll 1
     for (;;) {
         if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity))) return true;
         if (__any_sync(0xFFFFFFFFu, *abort_flag != 0 || clock64() - t0 > 2000000000ll)) return false;
     }
+}
+// Asynchronous 16-byte copy global -> shared; zeros, and nothing is read, where `take` is 0.
+__device__ __forceinline__ void cp_async16_if(uint32_t dst, const void* src, uint32_t take) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.u32 p, %2, 0;\n\tcp.async.cg.shared.global [%0], [%1], 16, p;\n\t}"
+                 ::"r"(dst), "l"(src), "r"(take) : "memory");
 }
 // 8 consecutive columns of the warp's 32 lanes <-> registers.
 __device__ __forceinline__ void tmem_ld8(uint32_t addr, uint32_t (&r)[8]) {
@@ -176,8 +197,8 @@ __device__ __forceinline__ void tmem_ld(uint32_t addr, uint32_t (&r)[COLS]) {
     if constexpr (COLS > 16) tmem_ld16<16>(addr + 16, r);
 }
 
-// N rows; SCORE: the options of stc_score, positions, or a scale that is not positive.
-template <int N, bool SCORE>
+// N rows; MASK: a window, documents or positions that are given; SCORE: cap, slopes, or a scale that is not positive (with MASK).
+template <int N, bool MASK, bool SCORE>
 __global__ void __launch_bounds__(kThreads, 1)
 tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                  const __grid_constant__ CUtensorMap map_new, const TreeArgs a) {
@@ -193,9 +214,11 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     volatile int* segs = reinterpret_cast<volatile int*>(ctl + kCtlSegs);                   // [kSegs][12]
     float* const row_max = reinterpret_cast<float*>(ctl + kCtlMax);                         // [N], log2 units
     uint32_t* const kin = reinterpret_cast<uint32_t*>(ctl + L::kCtlKin);
-    int* const node_pos = reinterpret_cast<int*>(ctl + (N == 128 ? 0 : L::kCtlPos));        // (SCORE has N <= 64)
+    int* const node_pos = reinterpret_cast<int*>(ctl + (N == 128 ? 0 : L::kCtlPos));        // (MASK has N <= 64)
     float* const row_slope = reinterpret_cast<float*>(ctl + (N == 128 ? 0 : L::kCtlRowSlope));
-    static_assert(!(SCORE && N == 128), "no room for the row tables");
+    static_assert(!(MASK && N == 128) && !(SCORE && !MASK), "no room for the row tables");
+    volatile uint32_t* const valid_tokens = reinterpret_cast<volatile uint32_t*>(ctl + kCtlValid);         // [ring][4 words]
+    volatile int* const tile_pages = reinterpret_cast<volatile int*>(ctl + (N == 128 ? 0 : L::kCtlIds));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     asm volatile("griddepcontrol.launch_dependents;");
 
@@ -204,7 +227,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_new) : "memory");
     if (threadIdx.x >= 64 && threadIdx.x < 64 + kBars) {
         const int i = (int)threadIdx.x - 64;
-        mbar_init(bars + 8 * i, i >= kVFull && i < kVEmpty ? 4 : i >= kPFull && i < kOFull ? 8 : i >= kGroup && i < kTabFull ? 4
+        mbar_init(bars + 8 * i, i >= kPFull && i < kOFull ? 8 : i >= kGroup && i < kTabFull ? 4
                                 : i == kTabEmpty ? 8 : i >= kSegEmpty ? kSegReaders : 1);
         fence_mbar_init();
     }
@@ -215,9 +238,11 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                      ::"r"(bars + kCtlTmem), "r"(4u * N) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    // thread = `per` problems; prefix sums over the block
     const int per = (a.problems + kThreads - 1) / kThreads;
     const int p_lo = min((int)threadIdx.x * per, a.problems), p_hi = min(p_lo + per, a.problems);
     int mine = 0;
+#pragma unroll 1
     for (int p = p_lo; p < p_hi; ++p) mine += problem_length(a, p);
     const int incl = (int)warp_incl_scan((uint32_t)mine, lane);
     volatile int* const sums = reinterpret_cast<volatile int*>(kin);      // [16] of the warps, then problem and offset of the range
@@ -226,25 +251,24 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     __syncthreads();
     tc_after();
     const uint32_t tmem = *tmem_slot;
-    int total = 0, n_cta, x_begin, x_end;
+    int total, x_begin = 0, x_end = 0;
     {
-        int before = incl - mine;
-#pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) {
-            if (w < warp) before += sums[w];
-            total += sums[w];
+        const int of_warp = lane < kThreads / 32 ? sums[lane] : 0;
+        const int upto = (int)warp_incl_scan((uint32_t)of_warp, lane);
+        total = __shfl_sync(0xFFFFFFFFu, upto, 31);
+        const int before = __shfl_sync(0xFFFFFFFFu, upto - of_warp, warp) + incl - mine;
+        const Cut cut(total, (int)gridDim.x);
+        if ((int)blockIdx.x < cut.n) {
+            x_begin = cut.begin((int)blockIdx.x);
+            x_end = cut.begin((int)blockIdx.x + 1);
         }
-        n_cta = min(total, (int)gridDim.x);
-        x_begin = x_end = 0;
-        if ((int)blockIdx.x < n_cta) {
-            x_begin = range_begin(total, (int)blockIdx.x, n_cta);
-            x_end = range_begin(total, (int)blockIdx.x + 1, n_cta);
-        }
-        if ((x_begin < x_end && before <= x_begin && x_begin < before + mine) || blockIdx.x == 0) {
+        const bool holds = x_begin < x_end && before <= x_begin && x_begin < before + mine;
+        if (holds || blockIdx.x == 0) {
             int at = before;
+#pragma unroll 1
             for (int p = p_lo; p < p_hi; ++p) {
-                const int n = problem_length(a, p);
-                if (x_begin < x_end && at <= x_begin && x_begin < at + n) {
+                const int n = per > 1 ? problem_length(a, p) : mine;
+                if (holds && at <= x_begin && x_begin < at + n) {
                     sums[16] = p;
                     sums[17] = x_begin - at;
                 }
@@ -252,10 +276,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 at += n;
             }
         }
-        if (blockIdx.x == 0 && threadIdx.x == 0) {
-            a.base[a.problems] = total;
-            a.base[a.problems + 1] = n_cta;
-        }
+        if (blockIdx.x == 0 && threadIdx.x == 0) a.base[a.problems] = total;
     }
     __syncthreads();
     const int p_first = sums[16], x_first = sums[17];
@@ -278,6 +299,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         ++n_seg;
         return s.tile1 >= 0;
     };
+    // the tree is the last tile of a unit, and the first that is taken; before it stand eight listed pages each
+    auto is_tree = [&](int t) { return t * kTilePages >= s.list; };
     // entry j of the segment's page list as it stands there, to be asked for ahead of its use; -1 outside the list
     auto listed = [&](int j) {
         if (j < 0 || j >= s.list) return -1;
@@ -289,33 +312,78 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         // nothing was started
     } else if (warp == 0) {
         // ---- producer of Q and K ---------------------------------------------------------------------------
-        int kc = 0, seg = 0;
+        int kc = 0, seg = 0, ring = 0;
+        uint32_t st = 0, phase = 1;                  // K stage, and the phase in which it is empty (of the second round on)
         bool ok = true;
         const uint32_t q_bytes = 2u * 128u * (uint32_t)(a.Gq * a.block_nodes);
         while (ok && next(ok)) {
             const int problem = s.b * a.Hkv + s.hk;
-            auto fetch = [&](int t) { return lane < kTilePages && t > 0 ? listed((t - 1) * kTilePages + lane) : -1; };
-            int id = fetch(s.tile1 - 1);
+            const int32_t* const doc_row = MASK && a.sc.tok_doc ? a.sc.tok_doc + (size_t)s.b * a.T : nullptr;
+            const int q_doc = doc_row ? a.sc.q_doc[s.b] : 0;
+            // pages of a tile in lanes 0 .. 7, asked for two tiles ahead; documents of its tokens (32 c + lane) one tile ahead
+            auto ask = [&](int t) { return lane < kTilePages && t >= s.tile0 ? listed(t * kTilePages + lane) : -1; };
+            int doc[4];
+            auto ask_docs = [&](int pages) {
+                if (MASK && doc_row) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int page = __shfl_sync(0xFFFFFFFFu, pages, 2 * c + (lane >> 4)), t = page * kPage + (lane & 15);
+                        doc[c] = is_page(page) && t < s.len ? __ldg(doc_row + t) : -1;
+                    }
+                }
+            };
+            int id = ask(s.tile1 - 1), id_next = ask(s.tile1 - 2);
+            ask_docs(id);
             bool q_due = true;
 #pragma unroll 1
             for (int t = s.tile1 - 1; t >= s.tile0; --t) {
-                const int id_next = t > s.tile0 ? fetch(t - 1) : -1;
-                const int st = kc % L::kKStages;
-                if (kc >= L::kKStages) ok = warp_wait(kKEmpty + st, (uint32_t)(kc / L::kKStages - 1));
-                if (!ok) break;
-                const bool mine_too = t > 0 ? is_page(id) : lane < (s.nodes + kPage - 1) / kPage;
-                const int boxes = __popc(__ballot_sync(0xFFFFFFFFu, mine_too));
-                if (lane == 0) mbar_expect_tx(bar(kKFull + st), (uint32_t)boxes * kPage * kRowBytes);
-                __syncwarp();
-                if (mine_too) {
-                    const uint32_t dst = base + L::kOffK + st * kTile + (uint32_t)lane * kPage * 128u;
-                    const CUtensorMap* map = t > 0 ? &map_k : &map_new;
-                    const int y = t > 0 ? problem * a.T + id * kPage : problem * a.n_cap + lane * kPage;
-                    tma_2d(dst, map, 0, y, bar(kKFull + st));
-                    tma_2d(dst + kHalf, map, 64, y, bar(kKFull + st));
+                // tokens of the tile that there are: 16 bits per page, a word per softmax warp of a group
+                const bool tree = is_tree(t);
+                const int here = !tree ? (is_page(id) ? min(kPage, s.len - id * kPage) : 0) : min(max(s.nodes - lane * kPage, 0), kPage);
+                uint32_t word = (1u << here) - 1u;
+                word = (word | __shfl_down_sync(0xFFFFFFFFu, word, 1) << 16);                // (lanes 0, 2, 4, 6)
+                word = __shfl_sync(0xFFFFFFFFu, word, 2 * lane & 7);
+                if (MASK && doc_row && !tree) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t same = __ballot_sync(0xFFFFFFFFu, doc[c] < 0 || doc[c] == q_doc);
+                        if (lane == c) word &= same;
+                    }
                 }
+                if (kc >= L::kKStages) ok = warp_wait(kKEmpty + st, phase);
+                if (!ok) break;
+                if (lane < 4) valid_tokens[ring * 4 + lane] = word;
+                if (MASK && lane < kTilePages) tile_pages[ring * kTilePages + lane] = id;
+                if (++ring == kRing) ring = 0;
+                __syncwarp();
+                const uint32_t full = bar(kKFull + st), dst = base + L::kOffK + st * kTile;
+                if (tree || !a.page_ids) {           // consecutive rows: two copies of 64 channels
+                    if (elect_one()) {
+                        const CUtensorMap* map = tree ? &map_new : &map_k;
+                        const int y = tree ? problem * a.n_cap : problem * a.T + (s.first + t * kTilePages) * kPage;
+                        mbar_expect_tx(full, (uint32_t)(tree ? a.n_cap : kTok) * kRowBytes);
+                        tma_2d(dst, map, 0, y, full);
+                        tma_2d(dst + kHalf, map, 64, y, full);
+                    }
+                } else {                             // two copies per page.  (From eight lanes at once they take 1300 cycles.)
+                    const uint32_t pages = __ballot_sync(0xFFFFFFFFu, is_page(id));
+                    if (elect_one()) mbar_expect_tx(full, (uint32_t)__popc(pages) * kPage * kRowBytes);
+                    __syncwarp();
+#pragma unroll
+                    for (int p = 0; p < kTilePages; ++p) {
+                        const int y = problem * a.T + __shfl_sync(0xFFFFFFFFu, id, p) * kPage;
+                        if (((pages >> p) & 1u) && elect_one()) {
+                            tma_2d(dst + p * kPage * 128, &map_k, 0, y, full);
+                            tma_2d(dst + kHalf + p * kPage * 128, &map_k, 64, y, full);
+                        }
+                    }
+                }
+                __syncwarp();
                 ++kc;
+                if (++st == (uint32_t)L::kKStages) { st = 0; phase ^= 1u; }
                 id = id_next;
+                id_next = ask(t - 2);
+                ask_docs(id);
                 if (q_due) {                         // the queries behind the first keys, which come from farther away
                     q_due = false;
                     if (seg > 0) ok = warp_wait(kQEmpty, (uint32_t)(seg - 1));
@@ -338,172 +406,188 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 mbar_wait_or_abort(bar(kKFull + i % L::kKStages), (uint32_t)(i / L::kKStages) & 1u, &none, kWaitNs);
         }
     } else if (warp == 1) {
-        // ---- MMA issuer: the warp stays together, an elected lane issues ------------------------------------------
-        constexpr uint32_t id_s = idesc_bf16(kTok, N, false), id_o = idesc_bf16(kHeadDim, 2 * N, true) | 1u << 15;   // (A M-major)
-        const uint32_t sm = uniform(base), ts = uniform(tmem), to = ts + 2 * N;
-        uint32_t tile = 0, seg = 0;                  // tiles of the segments before; segments before
+        // ---- issuer of S = K Q^T: the warp stays together, an elected lane issues ----------------------------------------
+        constexpr uint32_t id_s = idesc_bf16(kTok, N, false);
+        const uint32_t sm = uniform(base), ts = uniform(tmem);
+        const uint64_t dq = smem_desc_128(sm, 16), dk0 = smem_desc_128(sm + L::kOffK, 16);
+        uint32_t j = 0, st = 0, phase = 0, seg = 0;  // tiles so far; K stage and its phase; segments
         bool ok = true;
         while (ok && next(ok)) {
-            const int tiles = uniform(s.tile1 - s.tile0);
+            const int tiles = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)(s.tile1 - s.tile0));
             ok = warp_wait(kQFull, seg);
-            // iteration n: O += V~^T P^T of tile n - 2, whose S buffer then takes S = K Q^T of tile n
 #pragma unroll 1
-            for (int n = 0; ok && n < tiles + 2; ++n) {
-                if (n >= 2) {
-                    const uint32_t j = tile + (uint32_t)(n - 2), st = j % L::kVStages, buf = j & 1u;
-                    ok = warp_wait(kVFull + st, j / L::kVStages) && warp_wait(kPFull + buf, j >> 1);    // (what is late last)
-                    if (!ok) break;
-                    tc_after();
-                    const uint64_t dv = smem_desc_128(sm + L::kOffV + st * kTile, kHalf);
-                    const uint64_t dp = smem_desc_128(sm + L::kOffP + (L::kPBuffers > 1 ? buf * L::kP : 0u), kHalf);
-                    const uint32_t more = n > 2 && (n - 2) % kFlush != 0;                  // else O starts anew
-                    if (elect_one()) {
+            for (int n = 0; ok && n < tiles; ++n, ++j) {
+                const uint32_t buf = j & 1u;
+                // the scores of the tile before last are read when its weights are there
+                ok = warp_wait(kKFull + st, phase) && (j < 2 || warp_wait(kPFull + buf, (j >> 1) - 1u));
+                if (!ok) break;
+                tc_after();
+                const uint64_t dk = dk0 + (uint64_t)(st * (kTile >> 4));
+                if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)  // 16 tokens: 16 rows of 128 bytes in both
-                            tc_mma_ss(to, dv + (uint64_t)(k * (2048 >> 4)), dp + (uint64_t)(k * (2048 >> 4)), id_o, k ? 1u : more);
-                        tc_commit_to(bar(kOFull + buf));
-                        tc_commit_to(bar(kVEmpty + st));
-                    }
-                    __syncwarp();
+                    for (int k = 0; k < 8; ++k)      // 16 dims = 32 bytes = 2 units; 64 dims = one half tile
+                        tc_mma_ss(ts + buf * N, dk + (uint64_t)((k >> 2) * (kHalf >> 4) + (k & 3) * 2),
+                                  dq + (uint64_t)((k >> 2) * (L::kQHalf >> 4) + (k & 3) * 2), id_s, k != 0);
+                    tc_commit_to(bar(kSFull + buf));
+                    tc_commit_to(bar(kKEmpty + st));
+                    if (n == tiles - 1) tc_commit_to(bar(kQEmpty));
                 }
-                if (n < tiles) {
-                    const uint32_t j = tile + (uint32_t)n, st = j % L::kKStages, buf = j & 1u;
-                    ok = warp_wait(kKFull + st, j / L::kKStages);
-                    if (!ok) break;
-                    tc_after();
-                    const uint64_t dk = smem_desc_128(sm + L::kOffK + st * kTile, 16), dq = smem_desc_128(sm, 16);
-                    if (elect_one()) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)  // 16 dims = 32 bytes = 2 units; 64 dims = one half tile
-                            tc_mma_ss(ts + buf * N, dk + (uint64_t)((k >> 2) * (kHalf >> 4) + (k & 3) * 2),
-                                      dq + (uint64_t)((k >> 2) * (L::kQHalf >> 4) + (k & 3) * 2), id_s, k != 0);
-                        tc_commit_to(bar(kSFull + buf));
-                        tc_commit_to(bar(kKEmpty + st));
-                        if (n == tiles - 1) tc_commit_to(bar(kQEmpty));
-                    }
-                    __syncwarp();
-                }
+                __syncwarp();
+                if (++st == (uint32_t)L::kKStages) { st = 0; phase ^= 1u; }
             }
-            tile += (uint32_t)tiles;
             ++seg;
         }
         if (!ok) give_up();
     } else if (warp == 2) {
-        // ---- ancestors of the nodes as bit masks, positions of the rows ---------------------------------------------
-        uint32_t used = 0;
+        // ---- issuer of O += V~^T P^T -------------------------------------------------------------------
+        constexpr uint32_t id_o = idesc_bf16(kHeadDim, 2 * N, true) | 1u << 15;      // (A M-major)
+        const uint32_t sm = uniform(base), to = uniform(tmem) + 2 * N;
+        const uint64_t dv0 = smem_desc_128(sm + L::kOffV, kSlot / 2), dp0 = smem_desc_128(sm + L::kOffP, kHalf);
+        uint32_t j = 0, slot = 0, phase = 0;         // tiles so far; V slot and its phase
         bool ok = true;
         while (ok && next(ok)) {
-            if (!SCORE && s.tile0 > 0) continue;     // nobody asks
+            const int tiles = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)(s.tile1 - s.tile0));
+#pragma unroll 1
+            for (int n = 0; ok && n < tiles; ++n, ++j) {
+                const uint32_t buf = j & 1u, next_slot = slot + 1u;                   // (a tile's two slots are neighbours)
+                ok = warp_wait(kVFull + slot, phase) && warp_wait(kVFull + next_slot, phase) && warp_wait(kPFull + buf, j >> 1);
+                if (!ok) break;
+                tc_after();
+                const uint64_t dv = dv0 + (uint64_t)(slot * (kSlot >> 4)), dp = dp0 + (uint64_t)(L::kPBuffers > 1 ? buf * (L::kP >> 4) : 0u);
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)      // 16 tokens: 16 rows of 128 bytes in both; with every kFlush-th tile O starts anew
+                        tc_mma_ss(to, dv + (uint64_t)((k >> 2) * (kSlot >> 4) + (k & 3) * (2048 >> 4)), dp + (uint64_t)(k * (2048 >> 4)), id_o,
+                                  k ? 1u : (uint32_t)(n % kFlush != 0));
+                    tc_commit_to(bar(kOFull + buf));
+                    tc_commit_to(bar(kVEmpty + slot));
+                    tc_commit_to(bar(kVEmpty + next_slot));
+                }
+                __syncwarp();
+                slot += 2;
+                if (slot == (uint32_t)L::kVSlots) { slot = 0; phase ^= 1u; }
+            }
+        }
+        if (!ok) give_up();
+    } else if (warp == 3) {
+        // ---- scheduler: walks the CTA's range, segment by segment; and, behind each, the ancestors of its nodes as bit masks
+        bool ok = true;
+        int x = x_begin, p = p_first, off = x_first, careful = 0;
+        uint32_t made = 0;                           // tables
+#pragma unroll 1
+        for (int i = 0; ok; ++i) {
+            if (x >= x_end && !careful && i > 0) {   // all is under way: wait for it, and see how it went
+                const long long t0 = clock64();
+#pragma unroll 1
+                while (ok && __any_sync(0xFFFFFFFFu, *done < 8 * i))
+                {
+                    __nanosleep(200);                // (asking all the time takes issue slots from the others)
+                    ok = !__any_sync(0xFFFFFFFFu, *abort_flag != 0 || clock64() - t0 > 8000000000ll);
+                }
+                if (!ok) break;
+                __threadfence_block();
+                if (__any_sync(0xFFFFFFFFu, *redo)) {
+                    careful = 1;
+                    x = x_begin; p = p_first; off = x_first;
+                }
+            }
+            Segment g = {};
+            g.tile1 = -1;
+#pragma unroll 1
+            while (x < x_end) {
+                g.b = (int)((uint32_t)p / (uint32_t)a.Hkv);
+                g.hk = p - g.b * a.Hkv;
+                g.len = clamp_len(a.seq_len, g.b, a.T);
+                g.nodes = nodes_of(a, g.b);
+                pages_of(a, p, g.len, g.list, g.first);
+                const Unit u = unit_of(a, g.nodes, g.list);
+                if (off >= u.tiles * u.blocks) {
+                    off -= u.tiles * u.blocks;
+                    ++p;
+                    continue;
+                }
+                const int blk = (int)((uint32_t)off / (uint32_t)u.tiles);
+                g.tile0 = off - blk * u.tiles;
+                g.tile1 = min(u.tiles, g.tile0 + (x_end - x));
+                g.node0 = blk * a.block_nodes;
+                // a CTA continues at most one unit (slot 0) and leaves at most one that it begins (slot 1)
+                g.slot = g.tile1 - g.tile0 == u.tiles ? -1 : 2 * (int)blockIdx.x + (g.tile0 == 0 ? 1 : 0);
+                x += g.tile1 - g.tile0;
+                off += g.tile1 - g.tile0;
+                break;
+            }
+            if (i >= kSegs) ok = warp_wait(kSegEmpty + i % kSegs, (uint32_t)(i / kSegs - 1));
+            if (!ok) break;
+            if (lane == 0) {
+                volatile int* e = segs + (i % kSegs) * 12;
+                e[0] = g.b; e[1] = g.hk; e[2] = g.node0; e[3] = g.nodes; e[4] = g.len; e[5] = g.list; e[6] = g.first;
+                e[7] = g.tile0; e[8] = g.tile1; e[9] = g.slot; e[10] = careful;
+                mbar_arrive(bar(kSegFull + i % kSegs));
+            }
+            __syncwarp();
+            if (g.tile1 < 0) break;
+            if (!MASK && (g.tile1 - 1) * kTilePages < g.list) continue;      // nobody asks for the tree
             int up[4];
             uint32_t m[4][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int node = i * 32 + lane;
-                up[i] = -1;
-                if (node < s.nodes) {
-                    up[i] = a.parent ? a.parent[(size_t)s.b * a.n_cap + node] : node - 1;
-                    if (up[i] < 0 || up[i] >= node) up[i] = -1;
+            for (int k = 0; k < 4; ++k) {
+                const int node = k * 32 + lane;
+                up[k] = -1;
+                if (node < g.nodes) {
+                    up[k] = a.parent ? a.parent[(size_t)g.b * a.n_cap + node] : node - 1;
+                    if (up[k] < 0 || up[k] >= node) up[k] = -1;
                 }
 #pragma unroll
-                for (int w = 0; w < 4; ++w) m[i][w] = w == i ? 1u << lane : 0u;
+                for (int w = 0; w < 4; ++w) m[k][w] = w == k ? 1u << lane : 0u;
             }
-            if (used > 0) ok = warp_wait(kTabEmpty, used - 1);
+            if (made > 0) ok = warp_wait(kTabEmpty, made - 1);
             if (!ok) break;
-            // kin[n]: n and its ancestors up to the one `up` points at, twice as many each time
+            // each node's mask holds the node and its ancestors up to the one `up` points at, twice as many each time
             uint4* const table = reinterpret_cast<uint4*>(kin);
 #pragma unroll 1
             for (;;) {
                 bool going = false;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    table[i * 32 + lane] = make_uint4(m[i][0], m[i][1], m[i][2], m[i][3]);
-                    going |= up[i] >= 0;
+                for (int k = 0; k < 4; ++k) {
+                    table[k * 32 + lane] = make_uint4(m[k][0], m[k][1], m[k][2], m[k][3]);
+                    going |= up[k] >= 0;
                 }
                 __syncwarp();
                 if (!__any_sync(0xFFFFFFFFu, going)) break;
                 int next_up[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int k = 0; k < 4; ++k) {
                     // the node that `up` points at: its mask, and where its pointer goes (held by its lane)
-                    const uint4 t = table[max(up[i], 0)];
+                    const uint4 t = table[max(up[k], 0)];
                     int to[4];
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) to[w] = __shfl_sync(0xFFFFFFFFu, up[w], max(up[i], 0) & 31);
-                    const int which = max(up[i], 0) >> 5;
-                    next_up[i] = up[i] < 0 ? -1 : which == 0 ? to[0] : which == 1 ? to[1] : which == 2 ? to[2] : to[3];
-                    if (up[i] >= 0) { m[i][0] |= t.x; m[i][1] |= t.y; m[i][2] |= t.z; m[i][3] |= t.w; }
+                    for (int w = 0; w < 4; ++w) to[w] = __shfl_sync(0xFFFFFFFFu, up[w], max(up[k], 0) & 31);
+                    const int which = max(up[k], 0) >> 5;
+                    next_up[k] = up[k] < 0 ? -1 : which == 0 ? to[0] : which == 1 ? to[1] : which == 2 ? to[2] : to[3];
+                    if (up[k] >= 0) { m[k][0] |= t.x; m[k][1] |= t.y; m[k][2] |= t.z; m[k][3] |= t.w; }
                 }
                 __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 4; ++i) up[i] = next_up[i];
+                for (int k = 0; k < 4; ++k) up[k] = next_up[k];
             }
-            if constexpr (SCORE) {
+            if constexpr (MASK) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int node = i * 32 + lane;
-                    const int depth = __popc(m[i][0]) + __popc(m[i][1]) + __popc(m[i][2]) + __popc(m[i][3]) - 1;
-                    node_pos[node] = a.sc.q_pos && node < s.nodes ? a.sc.q_pos[(size_t)s.b * a.n_cap + node] : s.len + depth;
+                for (int k = 0; k < 4; ++k) {
+                    const int node = k * 32 + lane;
+                    const int depth = __popc(m[k][0]) + __popc(m[k][1]) + __popc(m[k][2]) + __popc(m[k][3]) - 1;
+                    node_pos[node] = a.sc.q_pos && node < g.nodes ? a.sc.q_pos[(size_t)g.b * a.n_cap + node] : g.len + depth;
                 }
-                for (int r = lane; r < N; r += 32) {
+#pragma unroll 1
+                for (int r = lane; SCORE && r < N; r += 32) {
                     const int in_block = (int)(((uint32_t)r * a.gq_inv) >> 16);
-                    row_slope[r] = a.sc.slopes ? a.sc.slopes[s.hk * a.Gq + (r - in_block * a.Gq)] * kLog2e : 0.f;
+                    row_slope[r] = a.sc.slopes ? a.sc.slopes[g.hk * a.Gq + (r - in_block * a.Gq)] * kLog2e : 0.f;
                 }
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(kTabFull));
-            ++used;
+            ++made;
         }
         if (!ok) give_up();
-    } else if (warp == 3) {
-        // ---- scheduler: walks the CTA's range, segment by segment -----------------------------------------------------
-        if (lane == 0) {
-            bool ok = true;
-            int x = x_begin, p = p_first, off = x_first, careful = 0;
-            for (int i = 0; ok; ++i) {
-                if (x >= x_end && !careful && i > 0) {       // all is under way: wait for it, and see how it went
-                    const unsigned long long t0 = global_ns();
-                    while (*done < 8 * i && ok) ok = !*abort_flag && global_ns() - t0 < 4 * kWaitNs;
-                    if (!ok) break;
-                    __threadfence_block();
-                    if (*redo) {
-                        careful = 1;
-                        x = x_begin; p = p_first; off = x_first;
-                    }
-                }
-                Segment g = {};
-                g.tile1 = -1;
-                while (x < x_end) {
-                    g.b = p / a.Hkv;
-                    g.hk = p - g.b * a.Hkv;
-                    g.len = clamp_len(a.seq_len, g.b, a.T);
-                    g.nodes = nodes_of(a, g.b);
-                    pages_of(a, p, g.len, g.list, g.first);
-                    const Unit u = unit_of(a, g.nodes, g.list);
-                    if (off >= u.tiles * u.blocks) {
-                        off -= u.tiles * u.blocks;
-                        ++p;
-                        continue;
-                    }
-                    const int blk = off / u.tiles;
-                    g.tile0 = off - blk * u.tiles;
-                    g.tile1 = min(u.tiles, g.tile0 + (x_end - x));
-                    g.node0 = blk * a.block_nodes;
-                    // a CTA continues at most one unit (slot 0) and leaves at most one that it begins (slot 1)
-                    g.slot = g.tile1 - g.tile0 == u.tiles ? -1 : 2 * (int)blockIdx.x + (g.tile0 == 0 ? 1 : 0);
-                    x += g.tile1 - g.tile0;
-                    off += g.tile1 - g.tile0;
-                    break;
-                }
-                if (i >= kSegs) ok = mbar_wait_or_abort(bar(kSegEmpty + i % kSegs), (uint32_t)(i / kSegs - 1) & 1u, abort_flag, kWaitNs);
-                if (!ok) break;
-                volatile int* e = segs + (i % kSegs) * 12;
-                e[0] = g.b; e[1] = g.hk; e[2] = g.node0; e[3] = g.nodes; e[4] = g.len; e[5] = g.list; e[6] = g.first;
-                e[7] = g.tile0; e[8] = g.tile1; e[9] = g.slot; e[10] = careful;
-                mbar_arrive(bar(kSegFull + i % kSegs));
-                if (g.tile1 < 0) break;
-            }
-            if (!ok) give_up();
-        }
     } else if (warp < 12) {
         // ---- softmax: thread = token of the tile, group = half of the rows ------------------------------------------------
         constexpr int kRows = N / 2, kCols = kRows < 32 ? kRows : 32, kChunks = kRows / kCols;
@@ -514,7 +598,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         float* const scratch = reinterpret_cast<float*>(N == 128 ? smem + L::kOffP + grp * kHalf : ctl + L::kCtlScratch + grp * 512);
         float* const my_max = row_max + grp * kRows;
         float* const my_flush = a.flush + ((size_t)blockIdx.x * N + grp * kRows) * kHeadDim + tok;
-        uint32_t j = 0, meets = 0, tabs = 0;
+        uint32_t j = 0, meets = 0, tabs = 0, ring = 0;
         bool ok = true;
         auto meet = [&]() {                          // the four warps of the group
             __syncwarp();
@@ -525,12 +609,13 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         auto segment = [&]() {
             const int live = min(a.block_nodes, s.nodes - s.node0) * a.Gq;    // rows of the block
             const int mine = live - grp * kRows;                              // of them in this group
-            const bool tables = SCORE || s.tile0 == 0;
+            const bool tables = MASK || is_tree(s.tile1 - 1);
             if (mine <= 0) {                         // none: its columns of P and O may be anything
                 for (int n = s.tile1 - s.tile0; n > 0; --n, ++j) {
                     ok = warp_wait(kSFull + (j & 1u), j >> 1);
                     if (!ok) return;
                     if (lane == 0) mbar_arrive(bar(kPFull + (j & 1u)));
+                    if (++ring == kRing) ring = 0;
                 }
                 if (tables) {
                     ok = warp_wait(kTabFull, tabs++);
@@ -544,7 +629,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             for (int i = 0; i < kRows / 2; ++i) l[i] = make_float2(0.f, 0.f);
             if (tok < kRows) my_max[tok] = tok < mine ? kUnset : INFINITY;   // (nothing exceeds it)
             int p0 = 0, p_least = 0, p_most = 0;     // positions of the block's rows: the first, which distances are taken from
-            if (SCORE) {
+            if (MASK) {
                 ok = warp_wait(kTabFull, tabs);
                 if (!ok) return;
                 p_least = 0x7FFFFFFF;
@@ -559,64 +644,53 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             }
             ok = meet();
             if (!ok) return;
-            // page ids are asked for two tiles ahead, documents one
-            auto page_of = [&](int t) { return t > 0 && t >= s.tile0 ? listed((t - 1) * kTilePages + (tok >> 4)) : -1; };
-            auto doc_of = [&](int id) {
-                const int at = id * kPage + (tok & 15);
-                return SCORE && a.sc.tok_doc && is_page(id) && at < s.len ? __ldg(a.sc.tok_doc + (size_t)s.b * a.T + at) : -1;
-            };
-            int id = page_of(s.tile1 - 1), id_next = page_of(s.tile1 - 2), doc = doc_of(id);
-            const int q_doc = SCORE && a.sc.tok_doc ? a.sc.q_doc[s.b] : 0;
             const int count = s.tile1 - s.tile0;
             bool calm = false;                       // every row has a reference
 #pragma unroll 1
             for (int n = 0; n < count; ++n, ++j) {
                 const int t = s.tile1 - 1 - n;
                 const uint32_t buf = j & 1u, ts = lane_base + buf * N + grp * kRows;
-                // this thread's token, and the rows of the group that see it
-                int pos = id * kPage + (tok & 15);
-                bool valid = t > 0 ? is_page(id) && pos < s.len && (!SCORE || doc < 0 || doc == q_doc) : tok < s.nodes;
-                doc = doc_of(id_next);
-                id = id_next;
-                id_next = page_of(t - 2);
-                uint64_t see = valid ? ~0ull : 0ull;
-                bool each = t == 0;                  // row by row
-                if constexpr (SCORE) {
-                    if (t == 0) pos = node_pos[tok];
+                ok = warp_wait(kSFull + buf, j >> 1);
+                if (!ok) return;
+                tc_after();
+                // this thread's token, and the rows of the group that see it where they are not all or none
+                const uint32_t word = valid_tokens[ring * 4 + quarter];
+                const bool valid = (word >> lane) & 1u;
+                int pos = 0;
+                const bool tree = is_tree(t);
+                bool each = tree;                                // row by row
+                if constexpr (MASK) {
+                    pos = tree ? node_pos[tok] : tile_pages[ring * kTilePages + (tok >> 4)] * kPage + (tok & 15);
                     each = each || __any_sync(0xFFFFFFFFu, valid && (pos > p_least || (uint32_t)p_most - (uint32_t)pos >= a.window));
                 }
-                if (each) {
-                    if (!SCORE) {
+                if (++ring == kRing) ring = 0;
+                uint64_t see = 0;
+                if (__builtin_expect(each, 0)) {
+                    if (!MASK) {
                         ok = warp_wait(kTabFull, tabs);
                         if (!ok) return;
                     }
-                    see = 0;
                     const uint64_t ones = (1ull << a.Gq) - 1ull;
                     const int from = (int)(((uint32_t)(grp * kRows) * a.gq_inv) >> 16);
-#pragma unroll 4
+#pragma unroll 1
                     for (int i = from; i * a.Gq < (grp + 1) * kRows; ++i) {       // nodes of the block
                         const int node = min(s.node0 + i, STC_TREE_MAX_NODES - 1), at = i * a.Gq - grp * kRows;
-                        bool seen = t > 0 || ((kin[node * 4 + quarter] >> lane) & 1u);
-                        if constexpr (SCORE) {
+                        bool seen = !tree || ((kin[node * 4 + quarter] >> lane) & 1u);
+                        if constexpr (MASK) {
                             const int p = node_pos[node];
                             seen = seen && pos <= p && (uint32_t)p - (uint32_t)pos < a.window;
                         }
                         if (seen) see |= at >= 0 ? ones << at : ones >> -at;
                     }
-                    if (!valid) see = 0;
                 }
-                const bool open = __all_sync(0xFFFFFFFFu, !each && valid);        // every row sees every token of the warp
                 const float far = SCORE ? (float)(pos - p0) : 0.f;
-                ok = warp_wait(kSFull + buf, j >> 1);
-                if (!ok) return;
-                tc_after();
                 auto last_product = [&]() {          // the product of the tile before is through
                     const bool good = warp_wait(kOFull + (buf ^ 1u), (j - 1) >> 1);
                     tc_after();
                     return good;
                 };
                 // the accumulator is emptied into fp32 sums; the issuer starts it anew
-                if (n > 0 && n % kFlush == 0) {
+                if (__builtin_expect(n > 0 && n % kFlush == 0, 0)) {
                     ok = last_product();
                     if (!ok) return;
 #pragma unroll 1
@@ -635,15 +709,15 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     }
                 }
                 // Tiles out of the ordinary are finished in place first, eight rows at a time: scores in log2 units with SCORE (but for
-                // slope times p0 - p, which is the same for all tokens of a row), -inf where a row does not see the token.
-                const bool finished = !open || (SCORE && !calm);
-                if (finished) {
+                // slope times p0 - p, which is the same for all tokens of a row), -inf where a row does not see a token that others see.
+                const bool finished = each || (SCORE && !calm);
+                if (__builtin_expect(finished, 0)) {
 #pragma unroll 1
                     for (int c = 0; c < kRows; c += 8) {
                         uint32_t r[8];
                         tmem_ld8(ts + c, r);
                         tmem_wait_ld();
-                        const uint32_t bits = (uint32_t)(see >> c);
+                        const uint32_t bits = each ? (uint32_t)(see >> c) : 0xFFu;
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             float y = __uint_as_float(r[i]);
@@ -662,27 +736,32 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     if (kRows > 32) unset = unset || my_max[32 % kRows + lane % 32] == kUnset;
                     return !__any_sync(0xFFFFFFFFu, unset);
                 };
-                if (n == 0 && !s.careful && !(SCORE && a.sc.slopes)) {
-                    // a first reference: this warp's quarter of the rows, over its own tokens (with slopes only the nearest would do)
+                if (__builtin_expect(n == 0 && !s.careful && !(SCORE && a.sc.slopes), 0)) {
+                    // a first reference: this warp's quarter of the rows over its own tokens; in the tree, whose tokens are mostly the
+                    // first warp's, that one all rows.  (With slopes only the nearest tokens would do.)
                     constexpr int kShare = kRows / 4;
-                    uint32_t q[16];
-                    tmem_ld16(ts + quarter * kShare, q);
-                    tmem_wait_ld();
-                    float top = -INFINITY;
+                    const int upto = !tree ? (quarter + 1) * kShare : quarter == 0 ? kRows : 0;
+#pragma unroll 1
+                    for (int c = tree ? 0 : quarter * kShare; c < upto; c += kShare) {
+                        uint32_t q[16];
+                        tmem_ld16(ts + c, q);
+                        tmem_wait_ld();
+                        float top = -INFINITY;
 #pragma unroll
-                    for (int i = 0; i < kShare; ++i) {
-                        const float v = redux_max(__uint_as_float(q[i]));
-                        if (lane == i) top = v;
+                        for (int i = 0; i < kShare; ++i) {
+                            const float v = redux_max(valid ? __uint_as_float(q[i]) : -INFINITY);
+                            if (lane == i) top = v;
+                        }
+                        if (!SCORE) top *= a.scale_log2;         // (the scale is positive)
+                        if (lane < kShare && my_max[c + lane] == kUnset && top > kUnset) my_max[c + lane] = top;
                     }
-                    if (!SCORE) top *= a.scale_log2;             // (the scale is positive)
-                    if (lane < kShare && my_max[quarter * kShare + lane] == kUnset && top > kUnset) my_max[quarter * kShare + lane] = top;
                     ok = meet();
                     if (!ok) return;
                     calm = all_set();
                 }
                 if (__builtin_expect(!calm, 0)) {
                     // the true maxima of the tile's tokens against the references; 16 rows at a time: lane i takes row i, then the four warps'
-                    if (L::kPBuffers == 1 && n > 0) {            // the scratch is P, which the product before reads
+                    if (N == 128 && n > 0) {                     // the scratch is P, which the product before reads
                         ok = last_product();
                         if (!ok) return;
                     }
@@ -696,7 +775,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         float top = -INFINITY;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float v = redux_max(__uint_as_float(q[i]));
+                            const float v = redux_max(valid ? __uint_as_float(q[i]) : -INFINITY);
                             if (lane == i) top = v;
                         }
                         if (!SCORE) top *= a.scale_log2;
@@ -752,10 +831,6 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     if (!ok) return;
                     calm = !s.careful && all_set();
                 }
-                if (L::kPBuffers == 1 && n > 0) {
-                    ok = last_product();
-                    if (!ok) return;
-                }
                 // weights, their sums, and P: eight rows of a token are 16 bytes of its line
                 const uint32_t line = base + L::kOffP + (L::kPBuffers > 1 ? buf * L::kP : 0u) + (uint32_t)tok * 128u, swz = (uint32_t)tok & 7u;
 #pragma unroll
@@ -765,7 +840,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     tmem_wait_ld();
                     if (SCORE && !finished) {
                         if (a.cap_in != 0.f) {
-                            // (what a row does not see, and columns without a row, have no say in how the others are capped)
+                            // (tokens that are not seen, and columns without a row, have no say in how the others are capped)
                             float most = 0.f;
                             if (c + kCols <= mine) {
                                 most = magnitude(r);
@@ -773,7 +848,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 #pragma unroll
                                 for (int i = 0; i < kCols; ++i) most = c + i < mine ? fmaxf(most, fabsf(__uint_as_float(r[i]))) : most;
                             }
-                            if (__all_sync(0xFFFFFFFFu, most * fabsf(a.cap_in) <= kCapSmall))
+                            if (__all_sync(0xFFFFFFFFu, (valid ? most : 0.f) * fabsf(a.cap_in) <= kCapSmall))
                                 cap_scores_low(r, a.cap_in, a.scale_log2);
                             else
                                 cap_scores_any(r, a.cap_in, a.cap_log2);
@@ -791,26 +866,37 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                             }
                         }
                     }
+                    if (word != 0xFFFFFFFFu) {                   // tokens that nobody sees
+#pragma unroll
+                        for (int i = 0; i < kCols; ++i) r[i] = valid ? r[i] : __float_as_uint(-INFINITY);
+                    }
                     const float4* ref = reinterpret_cast<const float4*>(my_max + c);
 #pragma unroll
-                    for (int e = 0; e < kCols; e += 8) {
-                        uint32_t hi[4], lo[4];
+                    for (int i = 0; i < kCols; i += 4) {         // in place: r[i] = high parts of two rows, r[i + 1] = residuals
+                        const float4 m4 = ref[i / 4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float4 m4 = ref[(e + 2 * i) / 4];
-                            const float2 m = i & 1 ? make_float2(-m4.z, -m4.w) : make_float2(-m4.x, -m4.y);
-                            float2 x = make_float2(__uint_as_float(r[e + 2 * i]), __uint_as_float(r[e + 2 * i + 1]));
+                        for (int e = 0; e < 4; e += 2) {
+                            const float2 m = e ? make_float2(-m4.z, -m4.w) : make_float2(-m4.x, -m4.y);
+                            float2 x = make_float2(__uint_as_float(r[i + e]), __uint_as_float(r[i + e + 1]));
                             if constexpr (SCORE) x = add2(x, m);
                             else x = fma2(x, both(a.scale_log2), m);
                             const float2 p = make_float2(ex2(x.x), ex2(x.y));
-                            float2& sum = l[(c + e) / 2 + i];
+                            float2& sum = l[(c + i + e) / 2];
                             sum = add2(sum, p);
                             const __nv_bfloat162 h2 = __floats2bfloat162_rn(p.x, p.y);
-                            hi[i] = *reinterpret_cast<const uint32_t*>(&h2);
-                            const float2 d = fma2(make_float2(bf16lo(hi[i]), bf16hi(hi[i])), both(-1.f), p);
+                            r[i + e] = *reinterpret_cast<const uint32_t*>(&h2);
+                            const float2 d = fma2(make_float2(bf16lo(r[i + e]), bf16hi(r[i + e])), both(-1.f), p);
                             const __nv_bfloat162 r2 = __floats2bfloat162_rn(d.x, d.y);
-                            lo[i] = *reinterpret_cast<const uint32_t*>(&r2);
+                            r[i + e + 1] = *reinterpret_cast<const uint32_t*>(&r2);
                         }
+                    }
+                    if (c == 0 && n >= L::kPBuffers) {           // P is read until its last product is through
+                        ok = L::kPBuffers > 1 ? warp_wait(kOFull + buf, (j >> 1) - 1u) : last_product();
+                        if (!ok) return;
+                    }
+#pragma unroll
+                    for (int e = 0; e < kCols; e += 8) {
+                        const uint32_t hi[4] = {r[e], r[e + 2], r[e + 4], r[e + 6]}, lo[4] = {r[e + 1], r[e + 3], r[e + 5], r[e + 7]};
                         const uint32_t eh = (uint32_t)(grp * kRows + c + e), el = eh + N;
                         sts16(line + (eh >> 6) * kHalf + ((((eh & 63u) >> 3) ^ swz) << 4), hi);
                         sts16(line + (el >> 6) * kHalf + ((((el & 63u) >> 3) ^ swz) << 4), lo);
@@ -915,131 +1001,151 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         if (!ok) give_up();
     } else {
         // ---- value tiles: packed groups -> swizzled rows -------------------------------------------------------
-        // A warp takes 32 tokens (two pages) of every tile.  LPT neighbouring lanes copy 16-byte chunks of one token (a whole group of 32
-        // or 64 bytes; two groups of 16), so a token's mask stays with its lanes and the place of a kept group is a running
-        // count.  A kept group is one asynchronous 16-byte copy per chunk, a dropped one a zero-filled copy that
-        // reads nothing.  The copies of a warp's next tile are under way before the last one's are waited for, unless its
-        // stage is still being read.
-        const int tok0 = (warp - 12) * 32;
-        int vc = 0, pending = -1;                    // tiles so far; stage whose copies are not waited for yet
+        // The warps take the tiles (or, in pairs, halves of tiles) in turn, so that each has the time of several tiles for its chain
+        // list -> masks and offsets -> groups (a round trip to memory each, and one is about as long as a tile).  A warp always
+        // fills the same slots: a barrier's parity only tells neighbouring phases apart.  32 tokens at a time: LPT neighbouring lanes copy
+        // 16-byte chunks of one token (a whole group of 32 or 64 bytes; two groups of 16), so a token's mask stays with its
+        // lanes and the place of a kept group is a running count.  A kept group is one asynchronous 16-byte copy per chunk, a
+        // dropped one a zero-filled copy that reads nothing.
+        constexpr int kHalves = 2 / L::kTileWarps, kParts = 2 * kHalves;     // halves of a tile that a warp fills, in parts of 32 tokens
+        const int turn = (warp - 12) / L::kTileWarps, half0 = L::kTileWarps == 2 ? warp & 1 : 0;
+        int vc = 0;                                  // tiles of the segments before
         bool ok = true;
-        auto publish = [&]() {                       // this warp's copies into `pending` have landed
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kVFull + pending));
-            pending = -1;
-        };
         const int opg = kOctets / a.S;               // 16-byte chunks of a group
         const uint32_t all_groups = (1u << a.S) - 1u, limit = (uint32_t)min(a.cap_groups, (int64_t)0xFFFFFFFF);   // (of the store)
-        {
-            while (ok && next(ok)) {
-                const size_t problem = (size_t)s.b * a.Hkv + s.hk;
-                const uint16_t* mask_row = a.v_mask + problem * a.T;
-                const uint32_t* offs = a.v_offs + problem * (a.T + 1);
-                const uint4* packed = a.v_packed + problem * a.cap_groups * opg;
-                const uint4* fresh = a.v_new + problem * a.n_cap * kOctets;
-                // tokens that no row of the sequence sees are left out: they may hold anything
-                int lo_all = 0, hi_all = s.len, q_doc = 0;
-                if constexpr (SCORE) {
-                    if (a.sc.q_pos) {
-                        int least = 0x7FFFFFFF, most = -1;
-                        for (int i = lane; i < s.nodes; i += 32) {
-                            const int p = a.sc.q_pos[(size_t)s.b * a.n_cap + i];
-                            least = min(least, p);
-                            most = max(most, p);
-                        }
-                        least = __reduce_min_sync(0xFFFFFFFFu, least);
-                        most = __reduce_max_sync(0xFFFFFFFFu, most);
-                        if (a.sc.window > 0 && least >= a.sc.window) lo_all = least - a.sc.window + 1;
-                        if (most < s.len) hi_all = most + 1;
-                    } else if (a.sc.window > 0 && s.len >= a.sc.window) {
-                        lo_all = s.len - a.sc.window + 1;
-                    }
-                    if (a.sc.tok_doc) q_doc = a.sc.q_doc[s.b];
-                }
-                auto page_of = [&](int t) { return t > 0 && t >= s.tile0 ? listed((t - 1) * kTilePages + (tok0 + lane) / kPage) : -1; };
-                // of this lane's token: its mask, its page's first group, its document; asked for a tile ahead
-                auto fetch = [&](int id, uint32_t& m, uint32_t& first, int& doc) {
-                    m = first = 0;
-                    doc = -1;
-                    const int t = id * kPage + (lane & 15);
-                    if (!is_page(id)) return -1;
-                    first = offs[id * kPage];
-                    if (t >= s.len) return -1;
-                    m = mask_row[t];
-                    if (SCORE && a.sc.tok_doc) doc = __ldg(a.sc.tok_doc + (size_t)s.b * a.T + t);
-                    return t;
-                };
-                uint32_t m_next, first_next;
-                int doc_next, at_next = fetch(page_of(s.tile1 - 1), m_next, first_next, doc_next);
-                int id_next = page_of(s.tile1 - 2);
+        while (ok && next(ok)) {
+            const size_t problem = (size_t)s.b * a.Hkv + s.hk;
+            const uint16_t* mask_row = a.v_mask + problem * a.T;
+            const uint32_t* offs = a.v_offs + problem * (a.T + 1);
+            const uint4* packed = a.v_packed + problem * a.cap_groups * opg;
+            const uint4* fresh = a.v_new + problem * a.n_cap * kOctets;
+            // tokens that no row of the sequence sees are left out: they may hold anything
+            int lo_all = 0, hi_all = s.len, q_doc = 0;
+            if constexpr (MASK) {
+                if (a.sc.q_pos) {
+                    int least = 0x7FFFFFFF, most = -1;
 #pragma unroll 1
-                for (int t = s.tile1 - 1; t >= s.tile0; --t, ++vc) {
-                    const uint32_t every = m_next & all_groups, first = first_next, cnt = __popc(every);
-                    uint32_t m = every;
-                    if (SCORE && (at_next < lo_all || at_next >= hi_all || (doc_next >= 0 && doc_next != q_doc))) m = 0;
-                    at_next = fetch(id_next, m_next, first_next, doc_next);
-                    id_next = page_of(t - 2);
-                    // place of the token's first group: its page's, and the groups of the page's tokens before it
-                    const uint32_t incl = warp_incl_scan(cnt, lane), half = __shfl_sync(0xFFFFFFFFu, incl, 15);
-                    const uint32_t place = first + incl - cnt - (lane >= 16 ? half : 0u);
-                    const int st = vc % L::kVStages;
-                    if (vc >= L::kVStages &&
-                        !__all_sync(0xFFFFFFFFu, mbar_try_wait(bar(kVEmpty + st), (uint32_t)(vc / L::kVStages - 1) & 1u))) {
-                        if (pending >= 0) { cp_async_wait<0>(); publish(); }
-                        ok = warp_wait(kVEmpty + st, (uint32_t)(vc / L::kVStages - 1));
-                        if (!ok) break;
+                    for (int i = lane; i < s.nodes; i += 32) {
+                        const int p = a.sc.q_pos[(size_t)s.b * a.n_cap + i];
+                        least = min(least, p);
+                        most = max(most, p);
                     }
-                    const uint32_t tile = base + L::kOffV + st * kTile;
-                    if (t == 0) {                    // the tree's own values, full width
+                    least = __reduce_min_sync(0xFFFFFFFFu, least);
+                    most = __reduce_max_sync(0xFFFFFFFFu, most);
+                    if (a.sc.window > 0 && least >= a.sc.window) lo_all = least - a.sc.window + 1;
+                    if (most < s.len) hi_all = most + 1;
+                } else if (a.sc.window > 0 && s.len >= a.sc.window) {
+                    lo_all = s.len - a.sc.window + 1;
+                }
+                if (a.sc.tok_doc) q_doc = a.sc.q_doc[s.b];
+            }
+            // per 32 tokens: page of this lane's token, its mask, its page's first group, its document; asked for one or two turns ahead
+            int id[kParts], doc[kParts];
+            uint32_t mask[kParts], first[kParts];
+            auto ask_pages = [&](int t) {
+#pragma unroll
+                for (int c = 0; c < kParts; ++c)
+                    id[c] = t >= s.tile0 ? listed(t * kTilePages + 4 * half0 + 2 * c + (lane >> 4)) : -1;
+            };
+            auto ask_masks = [&]() {
+#pragma unroll
+                for (int c = 0; c < kParts; ++c) {
+                    const int t = id[c] * kPage + (lane & 15);
+                    const bool there = is_page(id[c]), token = there && t < s.len;
+                    first[c] = there ? offs[id[c] * kPage] : 0u;
+                    mask[c] = token ? mask_row[t] : 0u;
+                    doc[c] = -1;
+                    if constexpr (MASK) {
+                        if (token && a.sc.tok_doc) doc[c] = __ldg(a.sc.tok_doc + (size_t)s.b * a.T + t);
+                        if (token && (t < lo_all || t >= hi_all)) first[c] |= 1u << 31;      // (groups of a problem are below 2^31)
+                    }
+                }
+            };
+            const int tiles = s.tile1 - s.tile0, n0 = (turn - vc) & (L::kTurns - 1);      // this warp's first tile of the segment
+            ask_pages(s.tile1 - 1 - n0);
+            ask_masks();
+            ask_pages(s.tile1 - 1 - n0 - L::kTurns);
+#pragma unroll 1
+            for (int n = n0; n < tiles; n += L::kTurns) {
+                const int t = s.tile1 - 1 - n;
+#pragma unroll 1
+                for (int h = 0; h < kHalves; ++h) {
+                    const int half = half0 + h;
+                    const int v = 2 * (vc + n) + half, slot = v % L::kVSlots;
+                    if (v >= L::kVSlots) ok = warp_wait(kVEmpty + slot, (uint32_t)(v / L::kVSlots - 1));
+                    if (!ok) break;
+                    const uint32_t rows = base + L::kOffV + slot * kSlot;
+                    if (is_tree(t)) {                // the tree's own values, full width
 #pragma unroll 4
-                        for (int i = lane; i < 32 * kOctets; i += 32) {
-                            const int tok = tok0 + (i >> 4);
+                        for (int i = lane; i < 64 * kOctets; i += 32) {
+                            const int tok = i >> 4;
                             const uint32_t oct = (uint32_t)i & 15u;
-                            const bool there = tok < s.nodes;
-                            cp_async16_zfill(tile + (oct >> 3) * kHalf + (uint32_t)tok * 128u + (((oct & 7u) ^ ((uint32_t)tok & 7u)) << 4),
-                                             there ? fresh + (size_t)tok * kOctets + oct : fresh, there ? 16 : 0);
+                            const bool there = half * 64 + tok < s.nodes;
+                            cp_async16_zfill(rows + (oct >> 3) * (kSlot / 2) + (uint32_t)tok * 128u + (((oct & 7u) ^ ((uint32_t)tok & 7u)) << 4),
+                                             there ? fresh + (size_t)(half * 64 + tok) * kOctets + oct : fresh, there ? 16 : 0);
                         }
                     } else {
-                        auto copy = [&](auto groups) {
-                            constexpr int S = decltype(groups)::value, OPG = kOctets / S, LPT = OPG < 2 ? 2 : OPG, GPL = LPT / OPG;
-                            const int sub = lane % LPT;
-#pragma unroll 1
-                            for (int pass = 0; pass < LPT; ++pass) {
-                                const int tok = pass * (32 / LPT) + lane / LPT;       // of the warp's 32
-                                const uint32_t tm = __shfl_sync(0xFFFFFFFFu, m, tok);
-                                uint32_t at = __shfl_sync(0xFFFFFFFFu, place, tok);   // place of the next kept group of the token
-                                const uint32_t row = tile + (uint32_t)(tok0 + tok) * 128u, swz = (uint32_t)(tok & 7);
 #pragma unroll
-                                for (int k = 0; k < 16 / LPT; ++k) {
-                                    const uint32_t oct = (uint32_t)(k * LPT + sub);   // chunk of the row: half oct >> 3, swizzled by the token
-                                    uint32_t mine_at = at;
-                                    bool kept;
-                                    if constexpr (GPL == 1) {
-                                        kept = (tm >> k) & 1u;
-                                        at += kept;
-                                    } else {
-                                        kept = (tm >> (2 * k + sub)) & 1u;
-                                        if (sub) mine_at += (tm >> (2 * k)) & 1u;
-                                        at += ((tm >> (2 * k)) & 1u) + ((tm >> (2 * k + 1)) & 1u);
-                                    }
-                                    kept = kept && mine_at < limit;
-                                    cp_async16_zfill(row + (oct >> 3) * kHalf + (((oct & 7u) ^ swz) << 4),
-                                                     kept ? packed + (size_t)mine_at * OPG + sub % OPG : a.v_new, kept ? 16 : 0);
-                                }
+                        for (int c = 0; c < 2; ++c) {
+                            const uint32_t every = (h ? mask[kParts - 2 + c] : mask[c]) & all_groups, at0 = h ? first[kParts - 2 + c] : first[c];
+                            uint32_t m = every;
+                            if constexpr (MASK) {
+                                const int d = h ? doc[kParts - 2 + c] : doc[c];
+                                if ((at0 >> 31) || (d >= 0 && d != q_doc)) m = 0;
                             }
-                        };
-                        if (a.S == 8) copy(std::integral_constant<int, 8>{});
-                        else if (a.S == 16) copy(std::integral_constant<int, 16>{});
-                        else copy(std::integral_constant<int, 4>{});
+                            // place of the token's first group: its page's, and the groups of the page's tokens before it
+                            const uint32_t cnt = __popc(every), incl = warp_incl_scan(cnt, lane), page0 = __shfl_sync(0xFFFFFFFFu, incl, 15);
+                            const uint32_t place = (MASK ? at0 & 0x7FFFFFFFu : at0) + incl - cnt - (lane >= 16 ? page0 : 0u);
+                            // groups behind the end of the store are not followed
+                            const uint32_t held = place < limit ? limit - place : 0u;
+                            while (__popc(m) > held) m &= ~(0x80000000u >> __clz(m));
+                            auto copy = [&](auto groups) {
+                                constexpr int S = decltype(groups)::value, OPG = kOctets / S, LPT = OPG < 2 ? 2 : OPG, GPL = LPT / OPG;
+                                const int sub = lane % LPT;
+#pragma unroll 1
+                                for (int pass = 0; pass < LPT; ++pass) {
+                                    const int tok = pass * (32 / LPT) + lane / LPT;       // of the 32
+                                    uint32_t left = __shfl_sync(0xFFFFFFFFu, m, tok);     // groups from this lane's next one on
+                                    const uint32_t at = __shfl_sync(0xFFFFFFFFu, place, tok);
+                                    const uint4* src = packed + (size_t)at * OPG + sub % OPG;
+                                    if constexpr (GPL > 1) {
+                                        src += sub ? left & 1u : 0u;
+                                        left >>= sub;
+                                    }
+                                    // chunk oct of the row: half oct >> 3, place (oct & 7) ^ (tok & 7); oct = k LPT + sub
+                                    const uint32_t row = rows + (uint32_t)(c * 32 + tok) * 128u + (((uint32_t)(tok & 7) ^ (uint32_t)sub) << 4);
+#pragma unroll
+                                    for (int k = 0; k < 16 / LPT; ++k) {
+                                        cp_async16_if(((row ^ (uint32_t)(((k * LPT) & 7) << 4))) + ((k * LPT) >> 3) * (kSlot / 2), src, left & 1u);
+                                        src += (GPL > 1 ? __popc(left & 3u) : (int)(left & 1u)) * OPG;
+                                        left >>= GPL;
+                                    }
+                                }
+                            };
+                            if (a.S == 8) copy(std::integral_constant<int, 8>{});
+                            else if (a.S == 16) copy(std::integral_constant<int, 16>{});
+                            else copy(std::integral_constant<int, 4>{});
+                        }
                     }
                     cp_async_commit();
-                    if (pending >= 0) { cp_async_wait<1>(); publish(); }
-                    pending = st;
                 }
-                cp_async_wait<0>();                  // (the next segment may only come when this one is done)
-                if (ok && pending >= 0) publish();
+                if (!ok) break;
+                ask_masks();
+                ask_pages(t - 2 * L::kTurns);
+                // this warp's copies have landed, the first half's before the second's
+                const int v = 2 * (vc + n) + half0;
+                if constexpr (kHalves == 2) {
+                    cp_async_wait<1>();
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(kVFull + v % L::kVSlots));
+                }
+                cp_async_wait<0>();
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kVFull + (v + kHalves - 1) % L::kVSlots));
             }
+            vc += tiles;
         }
         cp_async_wait<0>();
         if (!ok) give_up();
@@ -1053,50 +1159,51 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     }
 }
 
-// Joins the partials of units that more than one CTA worked on, in CTA order; a warp per row, a lane per four channels.  Checks the
-// trees and gathers the CTAs' status on the side.
+// Joins the partials of units that more than one CTA worked on, in CTA order: block = node of a (sequence, KV head), warp = query head,
+// lane = four channels.  Checks the trees and gathers the CTAs' status on the side.  Short on purpose: it runs once, from
+// cold instruction memory.
 __global__ void __launch_bounds__(256)
 tree_join_kernel(const TreeArgs a, int rows, int grid) {
     // launched while the first kernel still runs: the call's own inputs are read before the wait
-    const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    const int h = (int)(row % a.Hq), node = (int)(row / a.Hq % a.n_cap), b = (int)(row / a.Hq / a.n_cap);
-    int nodes = 0, problem = 0, list = 0, first = 0;
-    if (b < a.B) {
-        nodes = nodes_of(a, b);
-        if (h == 0 && node == 0) {
-            bool bad = false;
-            for (int i = lane; i < nodes && a.parent; i += 32) {
-                const int up = a.parent[(size_t)b * a.n_cap + i];
-                bad |= up < -1 || up >= i;
-            }
-            bad = __any_sync(0xFFFFFFFFu, bad);
-            if (lane == 0) a.status[b] = bad ? STC_ERR_INVALID_ARG : STC_OK;
-        }
-        problem = b * a.Hkv + h / a.Gq;
-        pages_of(a, problem, clamp_len(a.seq_len, b, a.T), list, first);
-    }
+    const int problem = blockIdx.x, node = blockIdx.y, h = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int b = (int)((uint32_t)problem / (uint32_t)a.Hkv), hk = problem - b * a.Hkv;
+    const int nodes = nodes_of(a, b);
+    int list, first;
+    pages_of(a, problem, clamp_len(a.seq_len, b, a.T), list, first);
     const Unit u = unit_of(a, nodes, list);
+    if (node == 0 && hk == 0 && h == 0) {
+        bool bad = false;
+#pragma unroll 1
+        for (int i = lane; i < nodes && a.parent; i += 32) {
+            const int up = a.parent[(size_t)b * a.n_cap + i];
+            bad |= up < -1 || up >= i;
+        }
+        bad = __any_sync(0xFFFFFFFFu, bad);
+        if (lane == 0) a.status[b] = bad ? STC_ERR_INVALID_ARG : STC_OK;
+    }
+    const int blk = (int)((uint32_t)node / (uint32_t)a.block_nodes);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (blockIdx.x == 0 && threadIdx.x < 32) {
+    if (problem == 0 && node == 0 && h == 0) {
         int st = 0;
+#pragma unroll 1
         for (int c = lane; c < grid; c += 32) st = max(st, a.cta_status[c]);
         st = __reduce_max_sync(0xFFFFFFFFu, st);
         if (lane == 0) *a.word = st;
     }
-    if (b >= a.B || node >= nodes) return;
-    const int blk = node / a.block_nodes, total = a.base[a.problems], n_cta = a.base[a.problems + 1];
-    const int x0 = a.base[problem] + blk * u.tiles, c0 = cta_of(total, x0, n_cta), c1 = cta_of(total, x0 + u.tiles - 1, n_cta);
+    if (node >= nodes) return;
+    const Cut cut(a.base[a.problems], grid);
+    const int x0 = a.base[problem] + blk * u.tiles, c0 = cut.owner(x0), c1 = cut.owner(x0 + u.tiles - 1);
     if (c0 == c1) return;                            // finished where it was computed
-    const int in_block = (node - blk * a.block_nodes) * a.Gq + h % a.Gq;
+    const int in_block = (node - blk * a.block_nodes) * a.Gq + h;
+    const size_t row = ((size_t)b * a.n_cap + node) * a.Hq + hk * a.Gq + h;
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-    for (int c = c0; c <= c1; c += 8) {
-        float2 p[8];
-        float4 v[8];
+    for (int c = c0; c <= c1; c += 4) {              // four loads in flight
+        float2 p[4];
+        float4 v[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             const int e = min(c + i, c1);
             const size_t at = (size_t)(2 * e + (e == c0 ? 1 : 0)) * rows + in_block;
             p[i] = __ldcg(a.part_ml + at);
@@ -1104,14 +1211,14 @@ tree_join_kernel(const TreeArgs a, int rows, int grid) {
         }
         float top = m;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             if (c + i > c1) p[i] = make_float2(-INFINITY, 0.f);
             top = fmaxf(top, p[i].x);
         }
         const float fm = m == -INFINITY ? 0.f : ex2(m - top);
         l *= fm; o.x *= fm; o.y *= fm; o.z *= fm; o.w *= fm;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             if (p[i].x == -INFINITY) {               // nothing seen: its sum is 0, or NaN
                 l += p[i].y;
                 continue;
@@ -1125,7 +1232,7 @@ tree_join_kernel(const TreeArgs a, int rows, int grid) {
     const float inv = l != 0.f ? 1.f / l : 0.f;
     float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
     if (inv != 0.f) r = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    reinterpret_cast<float4*>(a.out)[(size_t)row * 32 + lane] = r;
+    reinterpret_cast<float4*>(a.out)[row * 32 + lane] = r;
     if (a.lse && lane == 0) a.lse[row] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
@@ -1142,11 +1249,11 @@ int rows_of(const Geom& g, int n_cap, bool score) {
     return n;
 }
 
-template <int N, bool SCORE>
+template <int N, bool MASK, bool SCORE>
 cudaError_t launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& fresh, const TreeArgs& a, int n_cta, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<N, SCORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan<N>::kSmem);
+    cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<N, MASK, SCORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan<N>::kSmem);
     if (e != cudaSuccess) return e;
-    tree_attn_kernel<N, SCORE><<<n_cta, kThreads, Plan<N>::kSmem, st>>>(q, k, fresh, a);
+    tree_attn_kernel<N, MASK, SCORE><<<n_cta, kThreads, Plan<N>::kSmem, st>>>(q, k, fresh, a);
     return cudaGetLastError();
 }
 
@@ -1155,15 +1262,16 @@ cudaError_t launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap
 size_t tree_attn_ws_bytes(const Geom& g, int n_cap) {
     // (a call with options has no more rows per CTA than one without)
     const size_t n = (size_t)rows_of(g, n_cap, false);
-    return 256 + align256(kPlanSms * 4) + align256(((size_t)g.problems + 2) * 4) + 2 * (size_t)kPlanSms * n * 8 +
+    return 256 + align256(kPlanSms * 4) + align256(((size_t)g.problems + 1) * 4) + 2 * (size_t)kPlanSms * n * 8 +
            3 * (size_t)kPlanSms * n * kHeadDim * 4;
 }
 
 cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tree& tree, const void* q, const int32_t* page_ids,
                              const int32_t* n_pages, int max_pages, float sm_scale, const ScoreArgs& score, float* out, float* lse,
                              int32_t* status, void* ws, cudaStream_t st) {
-    const bool scored = score.softcap > 0.f || score.window > 0 || score.slopes || score.q_pos || score.tok_doc || !(sm_scale > 0.f);
-    const int n = rows_of(g, tree.n_cap, scored);
+    const bool scored = score.softcap > 0.f || score.slopes || !(sm_scale > 0.f);
+    const bool masked = scored || score.window > 0 || score.q_pos || score.tok_doc;
+    const int n = rows_of(g, tree.n_cap, masked);
     TreeArgs a;
     a.seq_len = g.seq_len; a.n_nodes = tree.n_nodes; a.parent = tree.parent; a.page_ids = page_ids; a.n_pages = n_pages;
     a.v_mask = cache.v_mask; a.v_offs = cache.v_offs; a.v_packed = static_cast<const uint4*>(cache.v_packed);
@@ -1175,7 +1283,7 @@ cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tr
     a.cta_status = reinterpret_cast<int32_t*>(w);
     w += align256(kPlanSms * 4);
     a.base = reinterpret_cast<int32_t*>(w);
-    w += align256(((size_t)g.problems + 2) * 4);
+    w += align256(((size_t)g.problems + 1) * 4);
     a.part_ml = reinterpret_cast<float2*>(w);
     w += 2 * (size_t)kPlanSms * n * 8;
     a.part_o = reinterpret_cast<float*>(w);
@@ -1208,26 +1316,28 @@ cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tr
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return cudaErrorInvalidValue;
     }
-    auto rows_map = [&](CUtensorMap* map, const void* p, long long rows) {
+    auto rows_map = [&](CUtensorMap* map, const void* p, long long rows, int at_once) {
         const cuuint64_t dims[2] = {kHeadDim, (cuuint64_t)rows};
         const cuuint64_t strides[1] = {kRowBytes};
-        const cuuint32_t box[2] = {64, kPage}, step[2] = {1, 1};
+        const cuuint32_t box[2] = {64, (cuuint32_t)at_once}, step[2] = {1, 1};
         return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     };
     const long long new_rows = (long long)g.problems * tree.n_cap;
     // (a cache without tokens: no page is ever loaded, the map only has to be a valid one)
-    if (!rows_map(&map_new, tree.k, new_rows) ||
-        !(g.T > 0 ? rows_map(&map_k, cache.k, (long long)g.problems * g.T) : rows_map(&map_k, tree.k, new_rows)))
+    const int at_once = page_ids ? kPage : kTok;     // rows of a copy of K
+    if (!rows_map(&map_new, tree.k, new_rows, tree.n_cap) ||
+        !(g.T > 0 ? rows_map(&map_k, cache.k, (long long)g.problems * g.T, at_once) : rows_map(&map_k, tree.k, new_rows, at_once)))
         return cudaErrorInvalidValue;
-    if (n == 32) e = scored ? launch<32, true>(map_q, map_k, map_new, a, n_cta, st) : launch<32, false>(map_q, map_k, map_new, a, n_cta, st);
-    else if (n == 64) e = scored ? launch<64, true>(map_q, map_k, map_new, a, n_cta, st) : launch<64, false>(map_q, map_k, map_new, a, n_cta, st);
-    else e = launch<128, false>(map_q, map_k, map_new, a, n_cta, st);
+    if (n == 32) e = scored ? launch<32, true, true>(map_q, map_k, map_new, a, n_cta, st)
+                     : masked ? launch<32, true, false>(map_q, map_k, map_new, a, n_cta, st) : launch<32, false, false>(map_q, map_k, map_new, a, n_cta, st);
+    else if (n == 64) e = scored ? launch<64, true, true>(map_q, map_k, map_new, a, n_cta, st)
+                          : masked ? launch<64, true, false>(map_q, map_k, map_new, a, n_cta, st) : launch<64, false, false>(map_q, map_k, map_new, a, n_cta, st);
+    else e = launch<128, false, false>(map_q, map_k, map_new, a, n_cta, st);
     if (e != cudaSuccess) return e;
-    const long long rows = (long long)g.B * tree.n_cap * g.Hq;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((rows + 7) / 8));
-    cfg.blockDim = dim3(256);
+    cfg.gridDim = dim3((unsigned)g.problems, (unsigned)tree.n_cap);
+    cfg.blockDim = dim3(32u * (unsigned)g.Gq);
     cfg.stream = st;
     cudaLaunchAttribute early;                       // its blocks wait in place instead of behind a launch
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
