@@ -67,7 +67,6 @@ static_assert(kBars * 8 <= kCtlTmem && kCtlSegs + kSegs * 48 <= kCtlValid && kCt
 template <int N>
 struct Plan {
     static constexpr int kKStages = N == 32 ? 3 : 2, kVSlots = 4, kPBuffers = N == 128 ? 1 : 2;    // K tiles; half V tiles; P
-    static constexpr int kTurns = kVSlots / 2, kTileWarps = 4 / kTurns;                    // V tiles in flight; warps that fill one
     static constexpr uint32_t kQHalf = N * 128, kP = kTok * 2 * N * 2;
     static constexpr uint32_t kOffK = 2 * kQHalf, kOffV = kOffK + kKStages * kTile, kOffP = kOffV + kVSlots * kSlot;
     static constexpr uint32_t kOffCtl = kOffP + kPBuffers * kP;
@@ -227,7 +226,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_new) : "memory");
     if (threadIdx.x >= 64 && threadIdx.x < 64 + kBars) {
         const int i = (int)threadIdx.x - 64;
-        mbar_init(bars + 8 * i, i >= kPFull && i < kOFull ? 8 : i >= kGroup && i < kTabFull ? 4
+        mbar_init(bars + 8 * i, i >= kVFull && i < kVEmpty ? 2 : i >= kPFull && i < kOFull ? 8 : i >= kGroup && i < kTabFull ? 4
                                 : i == kTabEmpty ? 8 : i >= kSegEmpty ? kSegReaders : 1);
         fence_mbar_init();
     }
@@ -1001,16 +1000,20 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         if (!ok) give_up();
     } else {
         // ---- value tiles: packed groups -> swizzled rows -------------------------------------------------------
-        // The warps take the tiles (or, in pairs, halves of tiles) in turn, so that each has the time of several tiles for its chain
-        // list -> masks and offsets -> groups (a round trip to memory each, and one is about as long as a tile).  A warp always
-        // fills the same slots: a barrier's parity only tells neighbouring phases apart.  32 tokens at a time: LPT neighbouring lanes copy
-        // 16-byte chunks of one token (a whole group of 32 or 64 bytes; two groups of 16), so a token's mask stays with its
-        // lanes and the place of a kept group is a running count.  A kept group is one asynchronous 16-byte copy per chunk, a
-        // dropped one a zero-filled copy that reads nothing.
-        constexpr int kHalves = 2 / L::kTileWarps, kParts = 2 * kHalves;     // halves of a tile that a warp fills, in parts of 32 tokens
-        const int turn = (warp - 12) / L::kTileWarps, half0 = L::kTileWarps == 2 ? warp & 1 : 0;
-        int vc = 0;                                  // tiles of the segments before
+        // A warp takes 32 tokens (two pages) of every tile.  LPT neighbouring lanes copy 16-byte chunks of one token (a whole group of
+        // 32 or 64 bytes; two groups of 16), so a token's mask stays with its lanes and the place of a kept group is a
+        // running count.  A kept group is one asynchronous 16-byte copy per chunk, a dropped one a copy that writes zeros and
+        // reads nothing.  The copies of a warp's next tile are under way before the last one's are waited for, unless its slot is
+        // still being read.  Page ids are asked for two tiles ahead, masks and offsets one.
+        const int tok0 = (warp - 12) * 32, half = (warp - 12) >> 1;
+        int vc = 0, pending = -1;                    // tiles so far; slot whose copies are not waited for yet
         bool ok = true;
+        auto publish = [&]() {                       // this warp's copies into `pending` have landed
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kVFull + pending));
+            pending = -1;
+        };
         const int opg = kOctets / a.S;               // 16-byte chunks of a group
         const uint32_t all_groups = (1u << a.S) - 1u, limit = (uint32_t)min(a.cap_groups, (int64_t)0xFFFFFFFF);   // (of the store)
         while (ok && next(ok)) {
@@ -1039,113 +1042,86 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 }
                 if (a.sc.tok_doc) q_doc = a.sc.q_doc[s.b];
             }
-            // per 32 tokens: page of this lane's token, its mask, its page's first group, its document; asked for one or two turns ahead
-            int id[kParts], doc[kParts];
-            uint32_t mask[kParts], first[kParts];
-            auto ask_pages = [&](int t) {
-#pragma unroll
-                for (int c = 0; c < kParts; ++c)
-                    id[c] = t >= s.tile0 ? listed(t * kTilePages + 4 * half0 + 2 * c + (lane >> 4)) : -1;
+            // of this lane's token: its mask, its page's first group, its document; -1 or the token
+            auto ask_page = [&](int t) { return t >= s.tile0 ? listed(t * kTilePages + (tok0 + lane) / kPage) : -1; };
+            auto ask_mask = [&](int id, uint32_t& m, uint32_t& first, int& doc) {
+                m = first = 0;
+                doc = -1;
+                if (!is_page(id)) return -1;
+                const int at = id * kPage + (lane & 15);
+                first = offs[id * kPage];
+                if (at >= s.len) return -1;
+                m = mask_row[at];
+                if (MASK && a.sc.tok_doc) doc = __ldg(a.sc.tok_doc + (size_t)s.b * a.T + at);
+                return at;
             };
-            auto ask_masks = [&]() {
-#pragma unroll
-                for (int c = 0; c < kParts; ++c) {
-                    const int t = id[c] * kPage + (lane & 15);
-                    const bool there = is_page(id[c]), token = there && t < s.len;
-                    first[c] = there ? offs[id[c] * kPage] : 0u;
-                    mask[c] = token ? mask_row[t] : 0u;
-                    doc[c] = -1;
-                    if constexpr (MASK) {
-                        if (token && a.sc.tok_doc) doc[c] = __ldg(a.sc.tok_doc + (size_t)s.b * a.T + t);
-                        if (token && (t < lo_all || t >= hi_all)) first[c] |= 1u << 31;      // (groups of a problem are below 2^31)
-                    }
-                }
-            };
-            const int tiles = s.tile1 - s.tile0, n0 = (turn - vc) & (L::kTurns - 1);      // this warp's first tile of the segment
-            ask_pages(s.tile1 - 1 - n0);
-            ask_masks();
-            ask_pages(s.tile1 - 1 - n0 - L::kTurns);
+            uint32_t m_next, first_next;
+            int doc_next, at_next = ask_mask(ask_page(s.tile1 - 1), m_next, first_next, doc_next);
+            int id_next = ask_page(s.tile1 - 2);
 #pragma unroll 1
-            for (int n = n0; n < tiles; n += L::kTurns) {
-                const int t = s.tile1 - 1 - n;
-#pragma unroll 1
-                for (int h = 0; h < kHalves; ++h) {
-                    const int half = half0 + h;
-                    const int v = 2 * (vc + n) + half, slot = v % L::kVSlots;
-                    if (v >= L::kVSlots) ok = warp_wait(kVEmpty + slot, (uint32_t)(v / L::kVSlots - 1));
+            for (int t = s.tile1 - 1; t >= s.tile0; --t, ++vc) {
+                const uint32_t every = m_next & all_groups, first = first_next;
+                uint32_t m = every;
+                if (MASK && (at_next < lo_all || at_next >= hi_all || (doc_next >= 0 && doc_next != q_doc))) m = 0;
+                at_next = ask_mask(id_next, m_next, first_next, doc_next);
+                id_next = ask_page(t - 2);
+                const int v = 2 * vc + half, slot = v % L::kVSlots;
+                if (v >= L::kVSlots &&
+                    !__all_sync(0xFFFFFFFFu, mbar_try_wait(bar(kVEmpty + slot), (uint32_t)(v / L::kVSlots - 1) & 1u))) {
+                    if (pending >= 0) { cp_async_wait<0>(); publish(); }
+                    ok = warp_wait(kVEmpty + slot, (uint32_t)(v / L::kVSlots - 1));
                     if (!ok) break;
-                    const uint32_t rows = base + L::kOffV + slot * kSlot;
-                    if (is_tree(t)) {                // the tree's own values, full width
+                }
+                const uint32_t rows = base + L::kOffV + slot * kSlot + (uint32_t)(tok0 & 63) * 128u;     // of the warp's tokens
+                if (is_tree(t)) {                    // the tree's own values, full width
 #pragma unroll 4
-                        for (int i = lane; i < 64 * kOctets; i += 32) {
-                            const int tok = i >> 4;
-                            const uint32_t oct = (uint32_t)i & 15u;
-                            const bool there = half * 64 + tok < s.nodes;
-                            cp_async16_zfill(rows + (oct >> 3) * (kSlot / 2) + (uint32_t)tok * 128u + (((oct & 7u) ^ ((uint32_t)tok & 7u)) << 4),
-                                             there ? fresh + (size_t)(half * 64 + tok) * kOctets + oct : fresh, there ? 16 : 0);
-                        }
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            const uint32_t every = (h ? mask[kParts - 2 + c] : mask[c]) & all_groups, at0 = h ? first[kParts - 2 + c] : first[c];
-                            uint32_t m = every;
-                            if constexpr (MASK) {
-                                const int d = h ? doc[kParts - 2 + c] : doc[c];
-                                if ((at0 >> 31) || (d >= 0 && d != q_doc)) m = 0;
-                            }
-                            // place of the token's first group: its page's, and the groups of the page's tokens before it
-                            const uint32_t cnt = __popc(every), incl = warp_incl_scan(cnt, lane), page0 = __shfl_sync(0xFFFFFFFFu, incl, 15);
-                            const uint32_t place = (MASK ? at0 & 0x7FFFFFFFu : at0) + incl - cnt - (lane >= 16 ? page0 : 0u);
-                            // groups behind the end of the store are not followed
-                            const uint32_t held = place < limit ? limit - place : 0u;
-                            while (__popc(m) > held) m &= ~(0x80000000u >> __clz(m));
-                            auto copy = [&](auto groups) {
-                                constexpr int S = decltype(groups)::value, OPG = kOctets / S, LPT = OPG < 2 ? 2 : OPG, GPL = LPT / OPG;
-                                const int sub = lane % LPT;
-#pragma unroll 1
-                                for (int pass = 0; pass < LPT; ++pass) {
-                                    const int tok = pass * (32 / LPT) + lane / LPT;       // of the 32
-                                    uint32_t left = __shfl_sync(0xFFFFFFFFu, m, tok);     // groups from this lane's next one on
-                                    const uint32_t at = __shfl_sync(0xFFFFFFFFu, place, tok);
-                                    const uint4* src = packed + (size_t)at * OPG + sub % OPG;
-                                    if constexpr (GPL > 1) {
-                                        src += sub ? left & 1u : 0u;
-                                        left >>= sub;
-                                    }
-                                    // chunk oct of the row: half oct >> 3, place (oct & 7) ^ (tok & 7); oct = k LPT + sub
-                                    const uint32_t row = rows + (uint32_t)(c * 32 + tok) * 128u + (((uint32_t)(tok & 7) ^ (uint32_t)sub) << 4);
-#pragma unroll
-                                    for (int k = 0; k < 16 / LPT; ++k) {
-                                        cp_async16_if(((row ^ (uint32_t)(((k * LPT) & 7) << 4))) + ((k * LPT) >> 3) * (kSlot / 2), src, left & 1u);
-                                        src += (GPL > 1 ? __popc(left & 3u) : (int)(left & 1u)) * OPG;
-                                        left >>= GPL;
-                                    }
-                                }
-                            };
-                            if (a.S == 8) copy(std::integral_constant<int, 8>{});
-                            else if (a.S == 16) copy(std::integral_constant<int, 16>{});
-                            else copy(std::integral_constant<int, 4>{});
-                        }
+                    for (int i = lane; i < 32 * kOctets; i += 32) {
+                        const int tok = i >> 4;
+                        const uint32_t oct = (uint32_t)i & 15u;
+                        const bool there = tok0 + tok < s.nodes;
+                        cp_async16_if(rows + (oct >> 3) * (kSlot / 2) + (uint32_t)tok * 128u + (((oct & 7u) ^ ((uint32_t)tok & 7u)) << 4),
+                                      there ? fresh + (size_t)(tok0 + tok) * kOctets + oct : fresh, there);
                     }
-                    cp_async_commit();
+                } else {
+                    // place of the token's first group: its page's, and the groups of the page's tokens before it
+                    const uint32_t cnt = __popc(every), incl = warp_incl_scan(cnt, lane), page0 = __shfl_sync(0xFFFFFFFFu, incl, 15);
+                    const uint32_t place = first + incl - cnt - (lane >= 16 ? page0 : 0u);
+                                                // groups behind the end of the store are not followed
+                                                const uint32_t held = place < limit ? limit - place : 0u;
+                                                while (__popc(m) > held) m &= ~(0x80000000u >> __clz(m));
+                                                auto copy = [&](auto groups) {
+                                                    constexpr int S = decltype(groups)::value, OPG = kOctets / S, LPT = OPG < 2 ? 2 : OPG, GPL = LPT / OPG;
+                                                    const int sub = lane % LPT;
+                    #pragma unroll 1
+                                                    for (int pass = 0; pass < LPT; ++pass) {
+                                                        const int tok = pass * (32 / LPT) + lane / LPT;       // of the 32
+                                                        uint32_t left = __shfl_sync(0xFFFFFFFFu, m, tok);     // groups from this lane's next one on
+                                                        const uint32_t at = __shfl_sync(0xFFFFFFFFu, place, tok);
+                                                        const uint4* src = packed + (size_t)at * OPG + sub % OPG;
+                                                        if constexpr (GPL > 1) {
+                                                            src += sub ? left & 1u : 0u;
+                                                            left >>= sub;
+                                                        }
+                                                        // chunk oct of the row: half oct >> 3, place (oct & 7) ^ (tok & 7); oct = k LPT + sub
+                                                        const uint32_t row = rows + (uint32_t)tok * 128u + (((uint32_t)(tok & 7) ^ (uint32_t)sub) << 4);
+                    #pragma unroll
+                                                        for (int k = 0; k < 16 / LPT; ++k) {
+                                                            cp_async16_if(((row ^ (uint32_t)(((k * LPT) & 7) << 4))) + ((k * LPT) >> 3) * (kSlot / 2), src, left & 1u);
+                                                            src += (GPL > 1 ? __popc(left & 3u) : (int)(left & 1u)) * OPG;
+                                                            left >>= GPL;
+                                                        }
+                                                    }
+                                                };
+                    if (a.S == 8) copy(std::integral_constant<int, 8>{});
+                    else if (a.S == 16) copy(std::integral_constant<int, 16>{});
+                    else copy(std::integral_constant<int, 4>{});
                 }
-                if (!ok) break;
-                ask_masks();
-                ask_pages(t - 2 * L::kTurns);
-                // this warp's copies have landed, the first half's before the second's
-                const int v = 2 * (vc + n) + half0;
-                if constexpr (kHalves == 2) {
-                    cp_async_wait<1>();
-                    fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(kVFull + v % L::kVSlots));
-                }
-                cp_async_wait<0>();
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(kVFull + (v + kHalves - 1) % L::kVSlots));
+                cp_async_commit();
+                if (pending >= 0) { cp_async_wait<1>(); publish(); }
+                pending = slot;
             }
-            vc += tiles;
+            cp_async_wait<0>();                      // (the next segment may only come when this one is done)
+            if (ok && pending >= 0) publish();
         }
         cp_async_wait<0>();
         if (!ok) give_up();
