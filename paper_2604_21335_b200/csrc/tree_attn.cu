@@ -3,33 +3,32 @@
 //   Row r = (node i, query head) of a (sequence, KV head):  softmax over the valid tokens of the listed pages and the nodes N_i
 //   (node i and its ancestors) of s = sm_scale * q.k (+ options of stc_score),  out = sum p v~,  lse = log sum exp s.
 //
-// A tree has few rows (a node's query heads times the nodes) and a long cache, so the products are taken transposed: tokens are the 128
-// lanes of tensor memory and rows the columns, as many as there are.
-//   S[token][row] = K . Q^T       A = K tile of 128 tokens (8 pages, or the tree itself), B = Q, M = 128, N = rows, K = 128
-//   O[dim][row]  += V~^T . P^T    A = V~ tile (dims along M, rebuilt from the packed groups), B = P, M = 128, N = 2 rows, K = 128
-// A softmax thread owns a token and walks the rows, so every lane works whatever the number of rows, and a token that is hidden costs
-// a select; the sums of a row stay in the threads' registers until the end.  P enters as a bf16 high part next to a bf16
-// residual, two sets of columns of one product (V~ is read once for both) that are added at the end: one bf16 weight alone would
-// leave the fp32 output 2^-8 off, the pair leaves 2^-16.
-//
-// The reference that a row's exponents are taken against is shared by the tile's 128 threads and need not be the maximum: weights may
-// be far above 1 as long as nothing overflows.  It is taken from the first tile (each warp looks at a quarter of the rows over its
-// own 32 tokens) and then stays, so that tiles need no maximum and the warps nothing from each other.  Where a sum comes out
-// above kTooLarge at the end, the CTA walks its range once more in the careful way: a tile moves a reference when a
-// score exceeds it by more than 2^8 (a vote of the four warps); then the true maxima are taken, and sums and accumulator follow.
-// Rows without a reference (first tiles that they do not see) go the careful way until they have one.
+// Rows (up to 128: whole nodes with their query heads) are the lanes of tensor memory, 128 tokens (8 pages, or the tree itself) a tile:
+//   S[row][token] = Q . K^T       Q, K tiles by TMA (128-byte swizzle), M = 128, N = 128, K = 128
+//   O[row][dim]  += P . V~        P from tensor memory, written over S by the softmax; V~ rebuilt from the packed groups
+//                                 in shared memory, token rows of 128 dims = N-major operand
+// A softmax thread owns a row.  With few rows most lanes idle, but the time of a tile hardly depends on them: the products take
+// 1600 cycles of the tensor pipe, the 128 exponentials of a thread 1024 of its quarter of the SM, and the tile's bytes (K 32 KiB, V
+// up to 32 KiB) 2100 to 2800 cycles of an SM's share of HBM.  (Tried first: tokens as lanes and rows as columns, which leaves no lane
+// idle.  Weights then pass through shared memory, sums take a register per row, maxima need the other warps, and the
+// unrolled columns do not fit the instruction cache: 3200 cycles per tile with 16 rows, 5000 with 128.)
+// P enters as a bf16 high part plus a bf16 residual (two MMAs): the output is fp32, and one bf16 weight alone would leave it 2^-8 off;
+// the pair leaves 2^-16.
 //
 // Work split.  Unit = (sequence, KV head, block of nodes); its tiles are eight listed pages each and, last, the tree.  The tiles
 // of all units form one flat sequence that is cut into equal contiguous ranges, one per CTA (one CTA per SM).  A unit within
 // a range is finished in place; of others each CTA leaves (max, sum, accumulator), which a second kernel joins in CTA order:
 // no atomics, the same bits every time.
 //
-// Roles (16 warps): 0 = TMA producer of Q and K (two copies of 16 rows per page); 1 = MMA issuer; 2 = ancestors of the nodes as bit
-// masks (pointer doubling) and the rows' positions; 3 = scheduler; 4..7 and 8..11 = softmax of one half of the rows each; 12..15
-// rebuild the value tiles with 16-byte asynchronous copies straight from the packed store into the swizzled tile.
+// Roles (16 warps): 0 = TMA producer of Q and K, which also tells which tokens of a tile there are; 1 = issuer of S, 2 = issuer of O;
+// 3 = scheduler, and the ancestors of a tree's nodes as bit masks (pointer doubling); 4..7 and 8..11 = softmax of the two groups,
+// which take the tiles in turn, each with its own S, O, maxima and sums, joined at the end of a segment; 12..15 rebuild the value tiles
+// with 16-byte asynchronous copies straight from the packed store into the swizzled tile.
 //
-// The tensor core truncates when it adds to an accumulator (4e-8 of its value per product), so an accumulator is emptied into
-// fp32 sums every kFlush tiles.
+// The running maximum only moves when a tile exceeds it by more than 2^8, so the accumulator in tensor memory is rescaled a few times
+// per segment and not per tile.  The tensor core truncates when it adds to an accumulator (4e-8 of its value per product, 16
+// products per tile), so an accumulator is emptied into fp32 sums every kFlush tiles.  A unit's tree comes first, then its pages from
+// the last to the first: with a distance bias the largest scores come first.
 //
 // Every wait is bounded (about a second); one that expires raises a CTA-wide flag and STC_ERR_TIMEOUT in the status word, the
 // roles leave, the producer waits (bounded) for its copies, tensor memory is freed.
@@ -48,36 +47,26 @@ constexpr int kSegReaders = 15;                   // warps that follow the segme
 constexpr uint32_t kHalf = kTok * 128;            // 64 channels of a token tile: 128 rows of 128 bytes
 constexpr uint32_t kTile = 2 * kHalf;             // 32 KiB
 constexpr uint32_t kSlot = kTile / 2;             // values of 64 tokens: two halves of 64 channels
-constexpr int kFlush = 16;                        // tiles an accumulator takes: 128 products, at most 5e-6 of it
+constexpr int kRows = 128;                        // rows of a block = tensor-memory lanes
+constexpr int kFlush = 8;                         // tiles of a group that an accumulator takes: 128 products, at most 5e-6 of it
 constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;                     // log2 units a maximum may be exceeded by
-constexpr float kUnset = -3.0e38f;                // reference of a row that has seen nothing: every finite score exceeds it
-constexpr float kTooLarge = 1.8446744e19f;        // 2^64: sum of weights that sends a CTA over its range again
+constexpr int kKStages = 2, kVSlots = 6;          // K tiles; half V tiles
 
-// barriers, in 8-byte words of the control block
-enum { kQFull, kQEmpty, kKFull, kKEmpty = kKFull + 3, kVFull = kKEmpty + 3, kVEmpty = kVFull + 8, kSFull = kVEmpty + 8,
-       kPFull = kSFull + 2, kOFull = kPFull + 2, kGroup = kOFull + 2, kTabFull = kGroup + 2, kTabEmpty, kSegFull,
+// barriers, in 8-byte words of the control block; [2] = per group
+enum { kQFull, kQEmpty, kKFull, kKEmpty = kKFull + kKStages, kVFull = kKEmpty + kKStages, kVEmpty = kVFull + kVSlots,
+       kSFull = kVEmpty + kVSlots, kPFull = kSFull + 2, kOFull = kPFull + 2, kXchg = kOFull + 2, kTabFull, kTabEmpty, kSegFull,
        kSegEmpty = kSegFull + kSegs, kBars = kSegEmpty + kSegs };
-constexpr int kRing = 6;                          // tiles whose valid tokens are kept: K stages, two score buffers and one more are under way
-constexpr uint32_t kCtlTmem = 304, kCtlAbort = 308, kCtlRedo = 312, kCtlDone = 316, kCtlSegs = 320, kCtlValid = 416, kCtlMax = 512;
-static_assert(kBars * 8 <= kCtlTmem && kCtlSegs + kSegs * 48 <= kCtlValid && kCtlValid + kRing * 16 <= kCtlMax, "control block");
-
-// Shared memory of a CTA with N rows.
-template <int N>
-struct Plan {
-    static constexpr int kKStages = N == 32 ? 3 : 2, kVSlots = 4, kPBuffers = N == 128 ? 1 : 2;    // K tiles; half V tiles; P
-    static constexpr uint32_t kQHalf = N * 128, kP = kTok * 2 * N * 2;
-    static constexpr uint32_t kOffK = 2 * kQHalf, kOffV = kOffK + kKStages * kTile, kOffP = kOffV + kVSlots * kSlot;
-    static constexpr uint32_t kOffCtl = kOffP + kPBuffers * kP;
-    static constexpr uint32_t kCtlKin = kCtlMax + N * 4;                                   // [128 nodes][4 words]
-    static constexpr uint32_t kCtlScratch = kCtlKin + STC_TREE_MAX_NODES * 16;             // [2 groups][4 warps][32], positions, slopes
-    static constexpr uint32_t kCtlPos = kCtlScratch + 1024, kCtlRowSlope = kCtlPos + 512;
-    static constexpr uint32_t kCtlIds = kCtlRowSlope + 256;                                // [ring][8 pages]
-    static constexpr uint32_t kCtlBytes = N == 128 ? kCtlScratch : kCtlIds + kRing * 32;
-    static constexpr uint32_t kSmem = kOffCtl + kCtlBytes;
-    static_assert(kSmem <= 232448, "shared memory of a block");
-};
+constexpr int kRing = 6;                          // tiles whose valid tokens are kept: K stages, the groups' tiles and one more
+constexpr uint32_t kQHalf = kRows * 128;
+constexpr uint32_t kOffK = 2 * kQHalf, kOffV = kOffK + kKStages * kTile, kOffCtl = kOffV + kVSlots * kSlot;
+constexpr uint32_t kCtlTmem = 256, kCtlAbort = 260, kCtlSegs = 272, kCtlValid = kCtlSegs + kSegs * 48,            // [ring][4 words]
+                   kCtlIds = kCtlValid + kRing * 16, kCtlPos = kCtlIds + kRing * 32,                              // [ring][8 pages], [128]
+                   kCtlKin = (kCtlPos + 512 + 15) / 16 * 16,                                                      // [128 nodes][4 words]
+                   kCtlMl = kCtlKin + STC_TREE_MAX_NODES * 16, kCtlBytes = kCtlMl + 2 * kRows * 8;                // [2 groups][128]
+constexpr uint32_t kSmem = kOffCtl + kCtlBytes;
+static_assert(kBars * 8 <= kCtlTmem && kSmem <= 232448, "shared memory of a block");
 
 struct TreeArgs {
     const int32_t* seq_len;
@@ -95,12 +84,12 @@ struct TreeArgs {
     int32_t* word;               // the call's status word
     int32_t* cta_status;         // [grid]
     int32_t* base;               // [problems + 1]: where each problem begins in the flat sequence, and its length
-    float2* part_ml;             // [2 * grid][N]
-    float* part_o;               // [2 * grid][N][128]
-    float* flush;                // [grid][N][128]: sums of emptied accumulators
+    float2* part_ml;             // [2 * grid][128 rows]
+    float* part_o;               // [2 * grid][128 rows][128]
+    float4* flush;               // [grid][2 groups][32][128 rows]: sums of emptied accumulators
     int64_t cap_groups;
     int B, Hq, Hkv, Gq, S, T, n_cap, max_pages, problems;
-    int block_nodes;             // nodes per block of rows = N / Gq
+    int block_nodes;             // nodes per block of rows = 128 / Gq
     uint32_t gq_inv;             // row / Gq = row * gq_inv >> 16 for rows below 128
     float scale_log2, cap_in, cap_log2;
     uint32_t window;             // tokens a row sees, 0xFFFFFFFF without a window
@@ -150,17 +139,8 @@ struct Cut {
 struct Segment {
     int b, hk, node0, nodes, len, list, first, tile0, tile1;
     int slot;                    // partial slot, -1 = the whole unit
-    int careful;                 // second walk
 };
 
-__device__ __forceinline__ float redux_max(float v) {
-    float r;
-    asm("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(r) : "f"(v));
-    return r;
-}
-__device__ __forceinline__ void sts16(uint32_t addr, const uint32_t (&v)[4]) {
-    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
-}
 // Bounded wait of a converged warp for a barrier's phase; false once it expired or another role has given up.  One copy of
 // the instructions that ask (a kernel with fifty waits is bound by fetching its own code otherwise), and the clock, which is read faster
 // than the timer; its limit is a second at the highest clock.
@@ -178,46 +158,24 @@ __device__ __forceinline__ void cp_async16_if(uint32_t dst, const void* src, uin
     asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.u32 p, %2, 0;\n\tcp.async.cg.shared.global [%0], [%1], 16, p;\n\t}"
                  ::"r"(dst), "l"(src), "r"(take) : "memory");
 }
-// 8 consecutive columns of the warp's 32 lanes <-> registers.
-__device__ __forceinline__ void tmem_ld8(uint32_t addr, uint32_t (&r)[8]) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "r"(addr));
-}
-__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&r)[8]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-                 : "memory");
-}
-// COLS consecutive columns of the warp's 32 lanes.
-template <int COLS>
-__device__ __forceinline__ void tmem_ld(uint32_t addr, uint32_t (&r)[COLS]) {
-    tmem_ld16<0>(addr, r);
-    if constexpr (COLS > 16) tmem_ld16<16>(addr + 16, r);
-}
-
-// N rows; MASK: a window, documents or positions that are given; SCORE: cap, slopes, or a scale that is not positive (with MASK).
-template <int N, bool MASK, bool SCORE>
+// MASK: a window, documents or positions that are given; SCORE: cap, slopes, or a scale that is not positive (with MASK).
+template <bool MASK, bool SCORE>
 __global__ void __launch_bounds__(kThreads, 1)
 tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                  const __grid_constant__ CUtensorMap map_new, const TreeArgs a) {
-    using L = Plan<N>;
+    static_assert(MASK || !SCORE, "SCORE needs the positions");
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = smem_u32(smem);
-    const uint32_t bars = base + L::kOffCtl;
-    unsigned char* const ctl = smem + L::kOffCtl;
+    const uint32_t bars = base + kOffCtl;
+    unsigned char* const ctl = smem + kOffCtl;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctl + kCtlTmem);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(ctl + kCtlAbort);
-    volatile int* redo = reinterpret_cast<volatile int*>(ctl + kCtlRedo);                   // a sum came out too large
-    volatile int* done = reinterpret_cast<volatile int*>(ctl + kCtlDone);                   // softmax warps that finished a segment, counted
     volatile int* segs = reinterpret_cast<volatile int*>(ctl + kCtlSegs);                   // [kSegs][12]
-    float* const row_max = reinterpret_cast<float*>(ctl + kCtlMax);                         // [N], log2 units
-    uint32_t* const kin = reinterpret_cast<uint32_t*>(ctl + L::kCtlKin);
-    int* const node_pos = reinterpret_cast<int*>(ctl + (N == 128 ? 0 : L::kCtlPos));        // (MASK has N <= 64)
-    float* const row_slope = reinterpret_cast<float*>(ctl + (N == 128 ? 0 : L::kCtlRowSlope));
-    static_assert(!(MASK && N == 128) && !(SCORE && !MASK), "no room for the row tables");
-    volatile uint32_t* const valid_tokens = reinterpret_cast<volatile uint32_t*>(ctl + kCtlValid);         // [ring][4 words]
-    volatile int* const tile_pages = reinterpret_cast<volatile int*>(ctl + (N == 128 ? 0 : L::kCtlIds));
+    uint32_t* const kin = reinterpret_cast<uint32_t*>(ctl + kCtlKin);
+    int* const node_pos = reinterpret_cast<int*>(ctl + kCtlPos);
+    float2* const ml = reinterpret_cast<float2*>(ctl + kCtlMl);
+    volatile uint32_t* const valid_tokens = reinterpret_cast<volatile uint32_t*>(ctl + kCtlValid);
+    volatile int* const tile_pages = reinterpret_cast<volatile int*>(ctl + kCtlIds);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     asm volatile("griddepcontrol.launch_dependents;");
 
@@ -226,15 +184,14 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_new) : "memory");
     if (threadIdx.x >= 64 && threadIdx.x < 64 + kBars) {
         const int i = (int)threadIdx.x - 64;
-        mbar_init(bars + 8 * i, i >= kVFull && i < kVEmpty ? 2 : i >= kPFull && i < kOFull ? 8 : i >= kGroup && i < kTabFull ? 4
-                                : i == kTabEmpty ? 8 : i >= kSegEmpty ? kSegReaders : 1);
+        mbar_init(bars + 8 * i, i >= kVFull && i < kVEmpty ? 2 : i >= kPFull && i < kOFull ? 4 : i == kXchg || i == kTabEmpty ? 8
+                                : i >= kSegEmpty ? kSegReaders : 1);
         fence_mbar_init();
     }
-    if (threadIdx.x == 5) *redo = *done = 0;
     if (threadIdx.x == 4) *abort_flag = (base & 1023u) != 0 ? (int)STC_ERR_CUDA : 0;        // swizzled tiles need 1024-byte aligned bases
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     ::"r"(bars + kCtlTmem), "r"(4u * N) : "memory");
+                     ::"r"(bars + kCtlTmem), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     // thread = `per` problems; prefix sums over the block
@@ -292,7 +249,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         if (!good) return false;
         volatile int* e = segs + (n_seg % kSegs) * 12;
         s.b = e[0]; s.hk = e[1]; s.node0 = e[2]; s.nodes = e[3]; s.len = e[4]; s.list = e[5]; s.first = e[6];
-        s.tile0 = e[7]; s.tile1 = e[8]; s.slot = e[9]; s.careful = e[10];
+        s.tile0 = e[7]; s.tile1 = e[8]; s.slot = e[9];
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(kSegEmpty + n_seg % kSegs));
         ++n_seg;
@@ -349,13 +306,13 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         if (lane == c) word &= same;
                     }
                 }
-                if (kc >= L::kKStages) ok = warp_wait(kKEmpty + st, phase);
+                if (kc >= kKStages) ok = warp_wait(kKEmpty + st, phase);
                 if (!ok) break;
                 if (lane < 4) valid_tokens[ring * 4 + lane] = word;
                 if (MASK && lane < kTilePages) tile_pages[ring * kTilePages + lane] = id;
                 if (++ring == kRing) ring = 0;
                 __syncwarp();
-                const uint32_t full = bar(kKFull + st), dst = base + L::kOffK + st * kTile;
+                const uint32_t full = bar(kKFull + st), dst = base + kOffK + st * kTile;
                 if (tree || !a.page_ids) {           // consecutive rows: two copies of 64 channels
                     if (elect_one()) {
                         const CUtensorMap* map = tree ? &map_new : &map_k;
@@ -379,7 +336,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 }
                 __syncwarp();
                 ++kc;
-                if (++st == (uint32_t)L::kKStages) { st = 0; phase ^= 1u; }
+                if (++st == (uint32_t)kKStages) { st = 0; phase ^= 1u; }
                 id = id_next;
                 id_next = ask(t - 2);
                 ask_docs(id);
@@ -390,7 +347,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     if (lane == 0) {
                         mbar_expect_tx(bar(kQFull), q_bytes);
                         tma_3d(base, &map_q, 0, s.hk * a.Gq, s.b * a.n_cap + s.node0, bar(kQFull));
-                        tma_3d(base + L::kQHalf, &map_q, 64, s.hk * a.Gq, s.b * a.n_cap + s.node0, bar(kQFull));
+                        tma_3d(base + kQHalf, &map_q, 64, s.hk * a.Gq, s.b * a.n_cap + s.node0, bar(kQFull));
                     }
                     __syncwarp();
                     ++seg;
@@ -401,95 +358,85 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         if (*abort_flag) {                           // copies still in flight get one more bounded wait each
             int none = 0;
             if (seg > 0) mbar_wait_or_abort(bar(kQFull), (uint32_t)(seg - 1) & 1u, &none, kWaitNs);
-            for (int i = max(0, kc - L::kKStages); i < kc; ++i)
-                mbar_wait_or_abort(bar(kKFull + i % L::kKStages), (uint32_t)(i / L::kKStages) & 1u, &none, kWaitNs);
+            for (int i = max(0, kc - kKStages); i < kc; ++i)
+                mbar_wait_or_abort(bar(kKFull + i % kKStages), (uint32_t)(i / kKStages) & 1u, &none, kWaitNs);
         }
     } else if (warp == 1) {
-        // ---- issuer of S = K Q^T: the warp stays together, an elected lane issues ----------------------------------------
-        constexpr uint32_t id_s = idesc_bf16(kTok, N, false);
+        // ---- issuer of S = Q K^T: the warp stays together, an elected lane issues ----------------------------------------
+        constexpr uint32_t id_s = idesc_bf16(kRows, kTok, false);
         const uint32_t sm = uniform(base), ts = uniform(tmem);
-        const uint64_t dq = smem_desc_128(sm, 16), dk0 = smem_desc_128(sm + L::kOffK, 16);
-        uint32_t j = 0, st = 0, phase = 0, seg = 0;  // tiles so far; K stage and its phase; segments
+        const uint64_t dq = smem_desc_128(sm, 16), dk0 = smem_desc_128(sm + kOffK, 16);
+        uint32_t st = 0, phase = 0, seg = 0, before[2] = {0u, 0u};   // K stage and its phase; segments; tiles of each group so far
         bool ok = true;
         while (ok && next(ok)) {
             const int tiles = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)(s.tile1 - s.tile0));
             ok = warp_wait(kQFull, seg);
 #pragma unroll 1
-            for (int n = 0; ok && n < tiles; ++n, ++j) {
-                const uint32_t buf = j & 1u;
-                // the scores of the tile before last are read when its weights are there
-                ok = warp_wait(kKFull + st, phase) && (j < 2 || warp_wait(kPFull + buf, (j >> 1) - 1u));
+            for (int n = 0; ok && n < tiles; ++n) {
+                const uint32_t g = (uint32_t)n & 1u, j = g ? before[1] : before[0];
+                // the group's S holds the weights of its last tile until their product is through
+                ok = warp_wait(kKFull + st, phase) && (j == 0 || warp_wait(kOFull + g, j - 1u));
                 if (!ok) break;
                 tc_after();
                 const uint64_t dk = dk0 + (uint64_t)(st * (kTile >> 4));
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k)      // 16 dims = 32 bytes = 2 units; 64 dims = one half tile
-                        tc_mma_ss(ts + buf * N, dk + (uint64_t)((k >> 2) * (kHalf >> 4) + (k & 3) * 2),
-                                  dq + (uint64_t)((k >> 2) * (L::kQHalf >> 4) + (k & 3) * 2), id_s, k != 0);
-                    tc_commit_to(bar(kSFull + buf));
+                        tc_mma_ss(ts + g * 256u, dq + (uint64_t)((k >> 2) * (kQHalf >> 4) + (k & 3) * 2),
+                                  dk + (uint64_t)((k >> 2) * (kHalf >> 4) + (k & 3) * 2), id_s, k != 0);
+                    tc_commit_to(bar(kSFull + g));
                     tc_commit_to(bar(kKEmpty + st));
                     if (n == tiles - 1) tc_commit_to(bar(kQEmpty));
                 }
                 __syncwarp();
-                if (++st == (uint32_t)L::kKStages) { st = 0; phase ^= 1u; }
+                if (g) ++before[1]; else ++before[0];
+                if (++st == (uint32_t)kKStages) { st = 0; phase ^= 1u; }
             }
             ++seg;
         }
         if (!ok) give_up();
     } else if (warp == 2) {
-        // ---- issuer of O += V~^T P^T -------------------------------------------------------------------
-        constexpr uint32_t id_o = idesc_bf16(kHeadDim, 2 * N, true) | 1u << 15;      // (A M-major)
-        const uint32_t sm = uniform(base), to = uniform(tmem) + 2 * N;
-        const uint64_t dv0 = smem_desc_128(sm + L::kOffV, kSlot / 2), dp0 = smem_desc_128(sm + L::kOffP, kHalf);
-        uint32_t j = 0, slot = 0, phase = 0;         // tiles so far; V slot and its phase
+        // ---- issuer of O += P V~ ----------------------------------------------------------------------------------------
+        constexpr uint32_t id_o = idesc_bf16(kRows, kHeadDim, true);
+        const uint32_t sm = uniform(base), ts = uniform(tmem);
+        const uint64_t dv0 = smem_desc_128(sm + kOffV, kSlot / 2);
+        uint32_t slot = 0, phase = 0, before[2] = {0u, 0u};
         bool ok = true;
         while (ok && next(ok)) {
             const int tiles = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)(s.tile1 - s.tile0));
 #pragma unroll 1
-            for (int n = 0; ok && n < tiles; ++n, ++j) {
-                const uint32_t buf = j & 1u, next_slot = slot + 1u;                   // (a tile's two slots are neighbours)
-                ok = warp_wait(kVFull + slot, phase) && warp_wait(kVFull + next_slot, phase) && warp_wait(kPFull + buf, j >> 1);
+            for (int n = 0; ok && n < tiles; ++n) {
+                const uint32_t g = (uint32_t)n & 1u, j = g ? before[1] : before[0], next_slot = slot + 1u;    // (a tile's slots are neighbours)
+                ok = warp_wait(kVFull + slot, phase) && warp_wait(kVFull + next_slot, phase) && warp_wait(kPFull + g, j);
                 if (!ok) break;
                 tc_after();
-                const uint64_t dv = dv0 + (uint64_t)(slot * (kSlot >> 4)), dp = dp0 + (uint64_t)(L::kPBuffers > 1 ? buf * (L::kP >> 4) : 0u);
+                const uint64_t dv = dv0 + (uint64_t)(slot * (kSlot >> 4));
+                const uint32_t p = ts + g * 256u, more = (uint32_t)((n >> 1) % kFlush != 0);          // else O starts anew
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)      // 16 tokens: 16 rows of 128 bytes in both; with every kFlush-th tile O starts anew
-                        tc_mma_ss(to, dv + (uint64_t)((k >> 2) * (kSlot >> 4) + (k & 3) * (2048 >> 4)), dp + (uint64_t)(k * (2048 >> 4)), id_o,
-                                  k ? 1u : (uint32_t)(n % kFlush != 0));
-                    tc_commit_to(bar(kOFull + buf));
+                    for (int k = 0; k < 8; ++k) {    // 16 tokens: 16 rows of 128 bytes; P: 8 columns high, 8 residual
+                        const uint64_t d = dv + (uint64_t)((k >> 2) * (kSlot >> 4) + (k & 3) * (2048 >> 4));
+                        tc_mma_ts(p + 128, p + 16 * k, d, id_o, k ? 1u : more);
+                        tc_mma_ts(p + 128, p + 16 * k + 8, d, id_o, 1);
+                    }
+                    tc_commit_to(bar(kOFull + g));
                     tc_commit_to(bar(kVEmpty + slot));
                     tc_commit_to(bar(kVEmpty + next_slot));
                 }
                 __syncwarp();
+                if (g) ++before[1]; else ++before[0];
                 slot += 2;
-                if (slot == (uint32_t)L::kVSlots) { slot = 0; phase ^= 1u; }
+                if (slot == (uint32_t)kVSlots) { slot = 0; phase ^= 1u; }
             }
         }
         if (!ok) give_up();
     } else if (warp == 3) {
         // ---- scheduler: walks the CTA's range, segment by segment; and, behind each, the ancestors of its nodes as bit masks
         bool ok = true;
-        int x = x_begin, p = p_first, off = x_first, careful = 0;
+        int x = x_begin, p = p_first, off = x_first;
         uint32_t made = 0;                           // tables
 #pragma unroll 1
         for (int i = 0; ok; ++i) {
-            if (x >= x_end && !careful && i > 0) {   // all is under way: wait for it, and see how it went
-                const long long t0 = clock64();
-#pragma unroll 1
-                while (ok && __any_sync(0xFFFFFFFFu, *done < 8 * i))
-                {
-                    __nanosleep(200);                // (asking all the time takes issue slots from the others)
-                    ok = !__any_sync(0xFFFFFFFFu, *abort_flag != 0 || clock64() - t0 > 8000000000ll);
-                }
-                if (!ok) break;
-                __threadfence_block();
-                if (__any_sync(0xFFFFFFFFu, *redo)) {
-                    careful = 1;
-                    x = x_begin; p = p_first; off = x_first;
-                }
-            }
             Segment g = {};
             g.tile1 = -1;
 #pragma unroll 1
@@ -520,7 +467,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (lane == 0) {
                 volatile int* e = segs + (i % kSegs) * 12;
                 e[0] = g.b; e[1] = g.hk; e[2] = g.node0; e[3] = g.nodes; e[4] = g.len; e[5] = g.list; e[6] = g.first;
-                e[7] = g.tile0; e[8] = g.tile1; e[9] = g.slot; e[10] = careful;
+                e[7] = g.tile0; e[8] = g.tile1; e[9] = g.slot;
                 mbar_arrive(bar(kSegFull + i % kSegs));
             }
             __syncwarp();
@@ -576,11 +523,6 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     const int depth = __popc(m[k][0]) + __popc(m[k][1]) + __popc(m[k][2]) + __popc(m[k][3]) - 1;
                     node_pos[node] = a.sc.q_pos && node < g.nodes ? a.sc.q_pos[(size_t)g.b * a.n_cap + node] : g.len + depth;
                 }
-#pragma unroll 1
-                for (int r = lane; SCORE && r < N; r += 32) {
-                    const int in_block = (int)(((uint32_t)r * a.gq_inv) >> 16);
-                    row_slope[r] = a.sc.slopes ? a.sc.slopes[g.hk * a.Gq + (r - in_block * a.Gq)] * kLog2e : 0.f;
-                }
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(kTabFull));
@@ -588,413 +530,293 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         }
         if (!ok) give_up();
     } else if (warp < 12) {
-        // ---- softmax: thread = token of the tile, group = half of the rows ------------------------------------------------
-        constexpr int kRows = N / 2, kCols = kRows < 32 ? kRows : 32, kChunks = kRows / kCols;
-        const int grp = (warp - 4) >> 2, quarter = warp & 3, tok = quarter * 32 + lane;
-        const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
-        const uint32_t to = lane_base + 2 * N + grp * kRows;                  // this group's columns of O; the residual's N further on
-        // where the warps of the group meet: maxima and sums of 32 rows each.  With N = 128 that is the group's own part of P.
-        float* const scratch = reinterpret_cast<float*>(N == 128 ? smem + L::kOffP + grp * kHalf : ctl + L::kCtlScratch + grp * 512);
-        float* const my_max = row_max + grp * kRows;
-        float* const my_flush = a.flush + ((size_t)blockIdx.x * N + grp * kRows) * kHeadDim + tok;
-        uint32_t j = 0, meets = 0, tabs = 0, ring = 0;
+        // ---- softmax: thread = row ---------------------------------------------------------------------------------------
+        const int grp = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), ts = lanes + (uint32_t)grp * 256u, to = ts + 128;
+        float4* const my_flush = a.flush + ((size_t)blockIdx.x * 2 + grp) * 32 * kRows + row;
+        uint32_t j = 0, joins = 0, tabs = 0, tile0 = 0;      // this group's tiles so far; joins; tables; tiles of the segments before
         bool ok = true;
-        auto meet = [&]() {                          // the four warps of the group
+        auto join = [&]() {                          // both groups
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kGroup + grp));
-            return warp_wait(kGroup + grp, meets++);
+            if (lane == 0) mbar_arrive(bar(kXchg));
+            return warp_wait(kXchg, joins++);
         };
 
         auto segment = [&]() {
             const int live = min(a.block_nodes, s.nodes - s.node0) * a.Gq;    // rows of the block
-            const int mine = live - grp * kRows;                              // of them in this group
+            const bool mine = row < live, warp_live = quarter * 32 < live;
+            const int tiles = s.tile1 - s.tile0, count = (tiles + 1 - grp) >> 1;
             const bool tables = MASK || is_tree(s.tile1 - 1);
-            if (mine <= 0) {                         // none: its columns of P and O may be anything
-                for (int n = s.tile1 - s.tile0; n > 0; --n, ++j) {
-                    ok = warp_wait(kSFull + (j & 1u), j >> 1);
-                    if (!ok) return;
-                    if (lane == 0) mbar_arrive(bar(kPFull + (j & 1u)));
-                    if (++ring == kRing) ring = 0;
-                }
-                if (tables) {
-                    ok = warp_wait(kTabFull, tabs++);
-                    if (ok && lane == 0) mbar_arrive(bar(kTabEmpty));
-                }
-                if (ok && lane == 0) atomicAdd(const_cast<int*>(done), 1);
-                return;
-            }
-            float2 l[kRows / 2];                     // sums of this thread's tokens
-#pragma unroll
-            for (int i = 0; i < kRows / 2; ++i) l[i] = make_float2(0.f, 0.f);
-            if (tok < kRows) my_max[tok] = tok < mine ? kUnset : INFINITY;   // (nothing exceeds it)
-            int p0 = 0, p_least = 0, p_most = 0;     // positions of the block's rows: the first, which distances are taken from
+            const uint32_t in_block = ((uint32_t)row * a.gq_inv) >> 16;
+            const int node = min(s.node0 + (int)in_block, STC_TREE_MAX_NODES - 1), h = row - (int)in_block * a.Gq;
+            int p = 0;
+            float slope2 = 0.f;
             if (MASK) {
                 ok = warp_wait(kTabFull, tabs);
                 if (!ok) return;
-                p_least = 0x7FFFFFFF;
-                p_most = -0x7FFFFFFF - 1;
-                p0 = node_pos[s.node0];
-                for (int i = s.node0 + lane; i < min(s.node0 + a.block_nodes, s.nodes); i += 32) {
-                    p_least = min(p_least, node_pos[i]);
-                    p_most = max(p_most, node_pos[i]);
-                }
-                p_least = __reduce_min_sync(0xFFFFFFFFu, p_least);
-                p_most = __reduce_max_sync(0xFFFFFFFFu, p_most);
+                p = node_pos[node];
+                if (SCORE && a.sc.slopes && mine) slope2 = a.sc.slopes[s.hk * a.Gq + h] * kLog2e;
             }
-            ok = meet();
-            if (!ok) return;
-            const int count = s.tile1 - s.tile0;
-            bool calm = false;                       // every row has a reference
+            float m = -INFINITY, l = 0.f, m_flush = -INFINITY;
 #pragma unroll 1
             for (int n = 0; n < count; ++n, ++j) {
-                const int t = s.tile1 - 1 - n;
-                const uint32_t buf = j & 1u, ts = lane_base + buf * N + grp * kRows;
-                ok = warp_wait(kSFull + buf, j >> 1);
+                const int t = s.tile1 - 1 - 2 * n - grp;
+                ok = warp_wait(kSFull + grp, j);
                 if (!ok) return;
-                tc_after();
-                // this thread's token, and the rows of the group that see it where they are not all or none
-                const uint32_t word = valid_tokens[ring * 4 + quarter];
-                const bool valid = (word >> lane) & 1u;
-                int pos = 0;
-                const bool tree = is_tree(t);
-                bool each = tree;                                // row by row
-                if constexpr (MASK) {
-                    pos = tree ? node_pos[tok] : tile_pages[ring * kTilePages + (tok >> 4)] * kPage + (tok & 15);
-                    each = each || __any_sync(0xFFFFFFFFu, valid && (pos > p_least || (uint32_t)p_most - (uint32_t)pos >= a.window));
+                if (!warp_live) {                    // a quarter without rows: its P may be anything
+                    if (lane == 0) mbar_arrive(bar(kPFull + grp));
+                    continue;
                 }
-                if (++ring == kRing) ring = 0;
-                uint64_t see = 0;
-                if (__builtin_expect(each, 0)) {
+                tc_after();
+                // tokens that the row sees: those that there are, in the tree its ancestors, and the window's
+                const int at = (int)((tile0 + 2u * (uint32_t)n + (uint32_t)grp) % kRing);
+                uint32_t see[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) see[i] = valid_tokens[at * 4 + i];
+                const bool tree = is_tree(t);
+                if (tree) {
                     if (!MASK) {
                         ok = warp_wait(kTabFull, tabs);
                         if (!ok) return;
                     }
-                    const uint64_t ones = (1ull << a.Gq) - 1ull;
-                    const int from = (int)(((uint32_t)(grp * kRows) * a.gq_inv) >> 16);
-#pragma unroll 1
-                    for (int i = from; i * a.Gq < (grp + 1) * kRows; ++i) {       // nodes of the block
-                        const int node = min(s.node0 + i, STC_TREE_MAX_NODES - 1), at = i * a.Gq - grp * kRows;
-                        bool seen = !tree || ((kin[node * 4 + quarter] >> lane) & 1u);
-                        if constexpr (MASK) {
-                            const int p = node_pos[node];
-                            seen = seen && pos <= p && (uint32_t)p - (uint32_t)pos < a.window;
-                        }
-                        if (seen) see |= at >= 0 ? ones << at : ones >> -at;
-                    }
+                    const uint4 k = reinterpret_cast<const uint4*>(kin)[node];
+                    see[0] &= k.x; see[1] &= k.y; see[2] &= k.z; see[3] &= k.w;
                 }
-                const float far = SCORE ? (float)(pos - p0) : 0.f;
-                auto last_product = [&]() {          // the product of the tile before is through
-                    const bool good = warp_wait(kOFull + (buf ^ 1u), (j - 1) >> 1);
-                    tc_after();
-                    return good;
-                };
-                // the accumulator is emptied into fp32 sums; the issuer starts it anew
-                if (__builtin_expect(n > 0 && n % kFlush == 0, 0)) {
-                    ok = last_product();
-                    if (!ok) return;
+                if constexpr (MASK) {
+                    if (tree) {
 #pragma unroll 1
-                    for (int c = 0; c < kRows; c += 16) {
-                        uint32_t hi[16], lo[16];
-                        tmem_ld16(to + c, hi);
-                        tmem_ld16(to + N + c, lo);
-                        tmem_wait_ld();
+                        for (int i = 0; i < s.nodes; ++i) {
+                            const int at_i = node_pos[i];
+                            if (at_i > p || (uint32_t)p - (uint32_t)at_i >= a.window) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float v = __uint_as_float(hi[i]) + __uint_as_float(lo[i]);
-                            float* dst = my_flush + (size_t)(c + i) * kHeadDim;
-                            if (n == kFlush) *dst = v;
-                            else asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(dst), "f"(v) : "memory");
-                        }
-                    }
-                }
-                // Tiles out of the ordinary are finished in place first, eight rows at a time: scores in log2 units with SCORE (but for
-                // slope times p0 - p, which is the same for all tokens of a row), -inf where a row does not see a token that others see.
-                const bool finished = each || (SCORE && !calm);
-                if (__builtin_expect(finished, 0)) {
-#pragma unroll 1
-                    for (int c = 0; c < kRows; c += 8) {
-                        uint32_t r[8];
-                        tmem_ld8(ts + c, r);
-                        tmem_wait_ld();
-                        const uint32_t bits = each ? (uint32_t)(see >> c) : 0xFFu;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            float y = __uint_as_float(r[i]);
-                            if constexpr (SCORE) {
-                                y = a.cap_in != 0.f ? cap_any(y, a.cap_in, a.cap_log2) : y * a.scale_log2;
-                                y = fmaf(row_slope[grp * kRows + c + i], far, y);
-                            }
-                            r[i] = (bits >> i) & 1u ? __float_as_uint(y) : __float_as_uint(-INFINITY);
-                        }
-                        tmem_st8(ts + c, r);
-                    }
-                    tmem_wait_st();
-                }
-                auto all_set = [&]() {               // (the same answer in the group's four warps)
-                    bool unset = lane < kRows && my_max[lane % kRows] == kUnset;
-                    if (kRows > 32) unset = unset || my_max[32 % kRows + lane % 32] == kUnset;
-                    return !__any_sync(0xFFFFFFFFu, unset);
-                };
-                if (__builtin_expect(n == 0 && !s.careful && !(SCORE && a.sc.slopes), 0)) {
-                    // a first reference: this warp's quarter of the rows over its own tokens; in the tree, whose tokens are mostly the
-                    // first warp's, that one all rows.  (With slopes only the nearest tokens would do.)
-                    constexpr int kShare = kRows / 4;
-                    const int upto = !tree ? (quarter + 1) * kShare : quarter == 0 ? kRows : 0;
-#pragma unroll 1
-                    for (int c = tree ? 0 : quarter * kShare; c < upto; c += kShare) {
-                        uint32_t q[16];
-                        tmem_ld16(ts + c, q);
-                        tmem_wait_ld();
-                        float top = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < kShare; ++i) {
-                            const float v = redux_max(valid ? __uint_as_float(q[i]) : -INFINITY);
-                            if (lane == i) top = v;
-                        }
-                        if (!SCORE) top *= a.scale_log2;         // (the scale is positive)
-                        if (lane < kShare && my_max[c + lane] == kUnset && top > kUnset) my_max[c + lane] = top;
-                    }
-                    ok = meet();
-                    if (!ok) return;
-                    calm = all_set();
-                }
-                if (__builtin_expect(!calm, 0)) {
-                    // the true maxima of the tile's tokens against the references; 16 rows at a time: lane i takes row i, then the four warps'
-                    if (N == 128 && n > 0) {                     // the scratch is P, which the product before reads
-                        ok = last_product();
-                        if (!ok) return;
-                    }
-                    float f[kRows / 16];                         // factors of rows 16 i + lane
-                    bool moves = false;
-#pragma unroll
-                    for (int c = 0; c < kRows / 16; ++c) {
-                        uint32_t q[16];
-                        tmem_ld16(ts + c * 16, q);
-                        tmem_wait_ld();
-                        float top = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float v = redux_max(valid ? __uint_as_float(q[i]) : -INFINITY);
-                            if (lane == i) top = v;
-                        }
-                        if (!SCORE) top *= a.scale_log2;
-                        scratch[quarter * 32 + lane] = top;
-                        ok = meet();
-                        if (!ok) return;
-                        top = fmaxf(fmaxf(scratch[lane], scratch[32 + lane]), fmaxf(scratch[64 + lane], scratch[96 + lane]));
-                        const float old = my_max[c * 16 + lane % 16];
-                        const bool move = lane < 16 && top > old + kSlack;
-                        f[c] = !move ? 1.f : old == kUnset ? 0.f : ex2(old - top);
-                        moves |= __any_sync(0xFFFFFFFFu, move) != 0;
-                        ok = meet();                             // everybody has read the old ones
-                        if (!ok) return;
-                        if (quarter == 0 && move) my_max[c * 16 + lane] = top;
-                    }
-                    if (moves) {                                 // sums and accumulator follow
-#pragma unroll
-                        for (int i = 0; i < kRows; i += 2)
-                            l[i / 2] = mul2(l[i / 2], make_float2(__shfl_sync(0xFFFFFFFFu, f[i / 16], i % 16),
-                                                                  __shfl_sync(0xFFFFFFFFu, f[i / 16], i % 16 + 1)));
-                        if (n > 0 && n % kFlush != 0) {
-                            ok = last_product();
-                            if (!ok) return;
-                        }
-#pragma unroll
-                        for (int c = 0; c < kRows / 16; ++c) {
-                            if (n > 0 && n % kFlush != 0) {
-#pragma unroll 1
-                                for (int part = 0; part < 2; ++part) {        // high, residual
-                                    uint32_t q[16];
-                                    tmem_ld16(to + part * N + c * 16, q);
-                                    tmem_wait_ld();
-#pragma unroll
-                                    for (int i = 0; i < 16; ++i) {
-                                        const float fi = __shfl_sync(0xFFFFFFFFu, f[c], i);
-                                        q[i] = fi != 1.f ? __float_as_uint(__uint_as_float(q[i]) * fi) : q[i];
-                                    }
-                                    tmem_st16(to + part * N + c * 16, q);
-                                }
-                                tmem_wait_st();
-                            }
-                            if (n >= kFlush) {
-#pragma unroll 1
-                                for (int i = 0; i < 16; ++i) {
-                                    const float fi = __shfl_sync(0xFFFFFFFFu, f[c], i);
-                                    float* dst = my_flush + (size_t)(c * 16 + i) * kHeadDim;
-                                    if (fi != 1.f) __stcg(dst, __ldcg(dst) * fi);
-                                }
+                                for (int w = 0; w < 4; ++w) see[w] &= ~(i >> 5 == w ? 1u << (i & 31) : 0u);
                             }
                         }
-                    }
-                    ok = meet();                                 // the new ones are there
-                    if (!ok) return;
-                    calm = !s.careful && all_set();
-                }
-                // weights, their sums, and P: eight rows of a token are 16 bytes of its line
-                const uint32_t line = base + L::kOffP + (L::kPBuffers > 1 ? buf * L::kP : 0u) + (uint32_t)tok * 128u, swz = (uint32_t)tok & 7u;
+                    } else if (a.sc.q_pos || a.sc.window > 0) {
 #pragma unroll
-                for (int c = 0; c < kRows; c += kCols) {
-                    uint32_t r[kCols];
-                    tmem_ld<kCols>(ts + c, r);
+                        for (int i = 0; i < kTilePages; ++i) {                // of a page's 16 tokens the bits [lo, hi)
+                            const int t0 = tile_pages[at * kTilePages + i] * kPage;
+                            const long long ahead = (long long)p - t0;        // distance of its first token
+                            const int hi = (int)min(max(ahead + 1, 0LL), 16LL), lo = (int)min(max(ahead + 1 - (long long)a.window, 0LL), 16LL);
+                            const uint32_t bits = ((1u << hi) - 1u) & ~((1u << lo) - 1u);
+                            see[i >> 1] &= i & 1 ? bits << 16 | 0xFFFFu : bits | 0xFFFF0000u;
+                        }
+                    }
+                }
+                const bool open = __all_sync(0xFFFFFFFFu, !mine || (see[0] & see[1] & see[2] & see[3]) == 0xFFFFFFFFu);
+                const bool empty_now = n > 0 && n % kFlush == 0;
+                const float m_acc = m;               // maximum the accumulator was built with
+                // maximum of the tile; scores that are not raw products times a positive scale, or hidden, are written back
+                float top = -INFINITY;
+#pragma unroll 1
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t r[32];
+                    tmem_ld16<0>(ts + 32 * c, r);
+                    tmem_ld16<16>(ts + 32 * c + 16, r);
                     tmem_wait_ld();
-                    if (SCORE && !finished) {
+                    const uint32_t bits = c & 2 ? (c & 1 ? see[3] : see[2]) : (c & 1 ? see[1] : see[0]);
+                    if constexpr (SCORE) {
                         if (a.cap_in != 0.f) {
-                            // (tokens that are not seen, and columns without a row, have no say in how the others are capped)
-                            float most = 0.f;
-                            if (c + kCols <= mine) {
-                                most = magnitude(r);
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < kCols; ++i) most = c + i < mine ? fmaxf(most, fabsf(__uint_as_float(r[i]))) : most;
-                            }
-                            if (__all_sync(0xFFFFFFFFu, (valid ? most : 0.f) * fabsf(a.cap_in) <= kCapSmall))
+                            // (what a row does not see, and lanes without a row, have no say in how the others are capped)
+                            const bool all = __all_sync(0xFFFFFFFFu, bits == 0xFFFFFFFFu || !mine);
+                            if (all && __all_sync(0xFFFFFFFFu, (mine ? magnitude(r) : 0.f) * fabsf(a.cap_in) <= kCapSmall))
                                 cap_scores_low(r, a.cap_in, a.scale_log2);
                             else
                                 cap_scores_any(r, a.cap_in, a.cap_log2);
                         } else {
 #pragma unroll
-                            for (int i = 0; i < kCols; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * a.scale_log2);
+                            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * a.scale_log2);
                         }
                         if (a.sc.slopes) {
-                            const float2* slope = reinterpret_cast<const float2*>(row_slope + grp * kRows + c);
+                            if (tree) {
 #pragma unroll
-                            for (int i = 0; i < kCols; i += 2) {
-                                const float2 y = fma2(slope[i / 2], both(far), make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])));
-                                r[i] = __float_as_uint(y.x);
-                                r[i + 1] = __float_as_uint(y.y);
+                                for (int i = 0; i < 32; ++i)
+                                    r[i] = __float_as_uint(fmaf(slope2, (float)(node_pos[32 * c + i] - p), __uint_as_float(r[i])));
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    const float far = (float)(tile_pages[at * kTilePages + 2 * c + e] * kPage - p);
+#pragma unroll
+                                    for (int i = 0; i < 16; i += 2) {
+                                        const float2 x = fma2(both(slope2), add2(both(far), make_float2((float)i, (float)(i + 1))),
+                                                              make_float2(__uint_as_float(r[16 * e + i]), __uint_as_float(r[16 * e + i + 1])));
+                                        r[16 * e + i] = __float_as_uint(x.x);
+                                        r[16 * e + i + 1] = __float_as_uint(x.y);
+                                    }
+                                }
                             }
                         }
                     }
-                    if (word != 0xFFFFFFFFu) {                   // tokens that nobody sees
+                    if (!open) {
 #pragma unroll
-                        for (int i = 0; i < kCols; ++i) r[i] = valid ? r[i] : __float_as_uint(-INFINITY);
+                        for (int i = 0; i < 32; ++i)
+                            if (!((bits >> i) & 1u)) r[i] = __float_as_uint(-INFINITY);
                     }
-                    const float4* ref = reinterpret_cast<const float4*>(my_max + c);
+                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int i = 0; i < kCols; i += 4) {         // in place: r[i] = high parts of two rows, r[i + 1] = residuals
-                        const float4 m4 = ref[i / 4];
+                    for (int i = 0; i < 32; i += 2)
+                        t4[(i >> 1) & 3] = fmaxf(fmaxf(t4[(i >> 1) & 3], __uint_as_float(r[i])), __uint_as_float(r[i + 1]));
+                    top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
+                    if (SCORE || !open) {
+                        uint32_t lo[16], hi[16];
 #pragma unroll
-                        for (int e = 0; e < 4; e += 2) {
-                            const float2 m = e ? make_float2(-m4.z, -m4.w) : make_float2(-m4.x, -m4.y);
-                            float2 x = make_float2(__uint_as_float(r[i + e]), __uint_as_float(r[i + e + 1]));
-                            if constexpr (SCORE) x = add2(x, m);
-                            else x = fma2(x, both(a.scale_log2), m);
-                            const float2 p = make_float2(ex2(x.x), ex2(x.y));
-                            float2& sum = l[(c + i + e) / 2];
-                            sum = add2(sum, p);
-                            const __nv_bfloat162 h2 = __floats2bfloat162_rn(p.x, p.y);
-                            r[i + e] = *reinterpret_cast<const uint32_t*>(&h2);
-                            const float2 d = fma2(make_float2(bf16lo(r[i + e]), bf16hi(r[i + e])), both(-1.f), p);
-                            const __nv_bfloat162 r2 = __floats2bfloat162_rn(d.x, d.y);
-                            r[i + e + 1] = *reinterpret_cast<const uint32_t*>(&r2);
+                        for (int i = 0; i < 16; ++i) { lo[i] = r[i]; hi[i] = r[16 + i]; }
+                        tmem_st16(ts + 32 * c, lo);
+                        tmem_st16(ts + 32 * c + 16, hi);
+                    }
+                }
+                if (SCORE || !open) tmem_wait_st();
+                if (!SCORE) top *= a.scale_log2;     // (-inf stays -inf: the scale is positive)
+                // move the maximum only if it is exceeded by much; the accumulator follows.  (S was only issued when the product
+                // of the group's last tile was through.)
+                const bool move = mine && (top > m + kSlack || (m == -INFINITY && top > -INFINITY));
+                if (__any_sync(0xFFFFFFFFu, move)) {
+                    const float to_m = move ? top : m, f = m == -INFINITY ? 0.f : ex2(m - to_m);
+                    l *= f;
+                    if (n > 0 && !empty_now) {
+#pragma unroll 1
+                        for (int c = 0; c < kHeadDim; c += 16) {
+                            uint32_t q[16];
+                            tmem_ld16(to + c, q);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) q[i] = move ? __float_as_uint(__uint_as_float(q[i]) * f) : q[i];
+                            tmem_st16(to + c, q);
                         }
                     }
-                    if (c == 0 && n >= L::kPBuffers) {           // P is read until its last product is through
-                        ok = L::kPBuffers > 1 ? warp_wait(kOFull + buf, (j >> 1) - 1u) : last_product();
-                        if (!ok) return;
-                    }
+                    m = to_m;
+                }
+                // the accumulator is emptied into fp32 sums, relative to m_flush; the issuer starts it anew
+                if (empty_now) {
+                    const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m_acc);
+#pragma unroll 1
+                    for (int c = 0; c < kHeadDim; c += 16) {
+                        float4 old[4];
 #pragma unroll
-                    for (int e = 0; e < kCols; e += 8) {
-                        const uint32_t hi[4] = {r[e], r[e + 2], r[e + 4], r[e + 6]}, lo[4] = {r[e + 1], r[e + 3], r[e + 5], r[e + 7]};
-                        const uint32_t eh = (uint32_t)(grp * kRows + c + e), el = eh + N;
-                        sts16(line + (eh >> 6) * kHalf + ((((eh & 63u) >> 3) ^ swz) << 4), hi);
-                        sts16(line + (el >> 6) * kHalf + ((((el & 63u) >> 3) ^ swz) << 4), lo);
+                        for (int i = 0; i < 4; ++i)
+                            old[i] = n > kFlush ? __ldcg(my_flush + (size_t)(c / 4 + i) * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
+                        uint32_t q[16];
+                        tmem_ld16(to + c, q);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            __stcg(my_flush + (size_t)(c / 4 + i) * kRows,
+                                   make_float4(fmaf(old[i].x, keep, __uint_as_float(q[4 * i])), fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1])),
+                                               fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2])), fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3]))));
+                    }
+                    m_flush = m_acc;
+                }
+                // weights, their sum, and P over S: per 16 tokens 8 columns of bf16 pairs high, 8 residual
+                const float ref = m == -INFINITY ? 0.f : m;
+                float2 la = make_float2(0.f, 0.f), lb = la;
+#pragma unroll 1
+                for (int c = 0; c < 128; c += 32) {
+                    uint32_t r[32];
+                    tmem_ld16<0>(ts + c, r);
+                    tmem_ld16<16>(ts + c + 16, r);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; e += 16) {
+                        uint32_t o[16];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            float2 x = make_float2(__uint_as_float(r[e + 2 * i]), __uint_as_float(r[e + 2 * i + 1]));
+                            if constexpr (SCORE) x = add2(x, both(-ref));
+                            else x = fma2(x, both(a.scale_log2), both(-ref));
+                            x.x = ex2(x.x);
+                            x.y = ex2(x.y);
+                            if (i & 1) lb = add2(lb, x); else la = add2(la, x);
+                            const __nv_bfloat162 h2 = __floats2bfloat162_rn(x.x, x.y);
+                            o[i] = *reinterpret_cast<const uint32_t*>(&h2);
+                            const float2 d = fma2(make_float2(bf16lo(o[i]), bf16hi(o[i])), both(-1.f), x);
+                            const __nv_bfloat162 r2 = __floats2bfloat162_rn(d.x, d.y);
+                            o[8 + i] = *reinterpret_cast<const uint32_t*>(&r2);
+                        }
+                        tmem_st16(ts + c + e, o);
                     }
                 }
-                fence_proxy_async();
+                l += (la.x + lb.x) + (la.y + lb.y);
+                tmem_wait_st();
                 tc_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(kPFull + buf));
+                if (lane == 0) mbar_arrive(bar(kPFull + grp));
             }
-            // ---- end of the segment -------------------------------------------------------------------------------
-            ok = warp_wait(kOFull + ((j - 1) & 1u), (j - 1) >> 1);
+            // ---- end of the segment: both groups hold part of the rows; each joins them for half of the channels ----------
+            if (count > 0) {
+                ok = warp_wait(kOFull + grp, j - 1);
+                if (!ok) return;
+                tc_after();
+                if (count > kFlush && warp_live) {   // take back what the accumulator was emptied of
+                    const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
+#pragma unroll 1
+                    for (int c = 0; c < kHeadDim; c += 16) {
+                        float4 old[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) old[i] = __ldcg(my_flush + (size_t)(c / 4 + i) * kRows);
+                        uint32_t q[16];
+                        tmem_ld16(to + c, q);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            q[4 * i] = __float_as_uint(fmaf(old[i].x, keep, __uint_as_float(q[4 * i])));
+                            q[4 * i + 1] = __float_as_uint(fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1])));
+                            q[4 * i + 2] = __float_as_uint(fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2])));
+                            q[4 * i + 3] = __float_as_uint(fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3])));
+                        }
+                        tmem_st16(to + c, q);
+                    }
+                    tmem_wait_st();
+                }
+            }
+            tile0 += (uint32_t)tiles;
+            ml[grp * kRows + row] = make_float2(m, l);
+            tc_before();
+            ok = join();
             if (!ok) return;
             tc_after();
-            const bool whole = s.slot < 0;
-            float inv[kChunks];                      // of row 32 c + lane
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
-                // sums over the warp's lanes, lane i keeping column i: halves change places, then a quarter of each ...
-                float v[kCols];
-#pragma unroll
-                for (int i = 0; i < kCols / 2; ++i) {
-                    v[2 * i] = l[c * (kCols / 2) + i].x;
-                    v[2 * i + 1] = l[c * (kCols / 2) + i].y;
+            if (warp_live) {
+                const float2 a0 = ml[row], a1 = ml[kRows + row];
+                m = fmaxf(a0.x, a1.x);
+                float f0 = a0.x == -INFINITY ? 0.f : ex2(a0.x - m), f1 = a1.x == -INFINITY ? 0.f : ex2(a1.x - m);
+                l = (a0.x == -INFINITY ? a0.y : a0.y * f0) + (a1.x == -INFINITY ? a1.y : a1.y * f1);      // (nothing seen: 0, or NaN)
+                const bool whole = s.slot < 0;
+                const size_t at = ((size_t)s.b * a.n_cap + node) * a.Hq + s.hk * a.Gq + h;
+                if (whole) {
+                    const float inv = l != 0.f ? 1.f / l : 0.f;
+                    f0 *= inv;
+                    f1 *= inv;
                 }
-                if constexpr (kCols == 16) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], 16);
+                if (grp == 0 && mine) {
+                    if (!whole) a.part_ml[(size_t)s.slot * kRows + row] = make_float2(m, l);
+                    else if (a.lse) a.lse[at] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
                 }
-#pragma unroll
-                for (int w = kCols / 2; w > 0; w >>= 1) {
-                    const bool upper = lane & w;
-#pragma unroll
-                    for (int i = 0; i < w; ++i) {
-                        const float keep = upper ? v[i + w] : v[i], give = upper ? v[i] : v[i + w];
-                        v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, w);
-                    }
-                }
-                scratch[(c * 4 + quarter) * 32 + lane] = v[0];
-            }
-            ok = meet();
-            if (!ok) return;
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
-                const int col = c * kCols + lane % kCols, row = grp * kRows + col;
-                const float* part = scratch + c * 128 + lane % kCols;
-                const float sum = (part[0] + part[32]) + (part[64] + part[96]);
-                float m = my_max[col];
-                const uint32_t in_block = ((uint32_t)row * a.gq_inv) >> 16;
-                if (sum > kTooLarge && row < live) *redo = 1;
-                if (m == kUnset) m = -INFINITY;
-                else if (SCORE && a.sc.slopes)
-                    m = fmaf(row_slope[row], (float)(p0 - node_pos[min(s.node0 + (int)in_block, STC_TREE_MAX_NODES - 1)]), m);
-                inv[c] = sum != 0.f ? 1.f / sum : 0.f;
-                if (quarter == 0 && lane < kCols && row < live) {
-                    if (whole) {
-                        const size_t at = ((size_t)s.b * a.n_cap + s.node0 + in_block) * a.Hq + s.hk * a.Gq + (row - in_block * a.Gq);
-                        if (a.lse) a.lse[at] = sum != 0.f ? (m + log2f(sum)) * kLn2 : -INFINITY;
-                    } else {
-                        a.part_ml[(size_t)s.slot * N + row] = make_float2(m, sum);
-                    }
-                }
-            }
-            // rows of O: the row's place among the outputs (or the partials) moves on by a head at a time
-            const uint32_t node_at = ((uint32_t)(grp * kRows) * a.gq_inv) >> 16;
-            int h = grp * kRows - (int)node_at * a.Gq;
-            float* dst = whole ? a.out + (((size_t)s.b * a.n_cap + s.node0 + node_at) * a.Hq + s.hk * a.Gq + h) * kHeadDim + tok
-                               : a.part_o + ((size_t)s.slot * N + grp * kRows) * kHeadDim + tok;
-            const size_t jump = whole ? (size_t)(a.Hq - a.Gq + 1) * kHeadDim : kHeadDim;      // to the next node's first head
+                float4* dst = reinterpret_cast<float4*>(whole ? a.out + at * kHeadDim : a.part_o + ((size_t)s.slot * kRows + row) * kHeadDim);
 #pragma unroll 1
-            for (int c = 0; c < kRows && c < mine; c += 8) {
-                uint32_t hi[8], lo[8];
-                float old[8];
-                tmem_ld8(to + c, hi);
-                tmem_ld8(to + N + c, lo);
+                for (int c = 64 * grp; c < 64 * grp + 64; c += 16) {
+                    uint32_t q0[16], q1[16];
+                    tmem_ld16(lanes + 128 + c, q0);
+                    tmem_ld16(lanes + 384 + c, q1);
+                    tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) old[i] = count > kFlush ? __ldcg(my_flush + (size_t)(c + i) * kHeadDim) : 0.f;
-                tmem_wait_ld();
-                const float inv_c = kChunks == 1 || c < 32 ? inv[0] : inv[kChunks - 1];
+                    for (int i = 0; i < 4; ++i) {
+                        float v[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float inv_i = __shfl_sync(0xFFFFFFFFu, inv_c, (c + i) & 31);
-                    float x = __uint_as_float(hi[i]) + __uint_as_float(lo[i]) + old[i];
-                    if (whole) x = inv_i != 0.f ? x * inv_i : 0.f;            // (0: nothing seen)
-                    if (c + i < mine) __stcg(dst, x);
-                    dst += ++h == a.Gq ? jump : (size_t)kHeadDim;
-                    if (h == a.Gq) h = 0;
+                        for (int e = 0; e < 4; ++e) {        // (a factor 0 stands for "nothing seen", whatever was summed)
+                            v[e] = f0 != 0.f ? __uint_as_float(q0[4 * i + e]) * f0 : 0.f;
+                            if (f1 != 0.f) v[e] = fmaf(__uint_as_float(q1[4 * i + e]), f1, v[e]);
+                        }
+                        if (mine) __stcg(dst + c / 4 + i, make_float4(v[0], v[1], v[2], v[3]));
+                    }
                 }
+                tc_before();
             }
-            ok = meet();                             // scratch and references are free again
+            ok = join();                             // accumulators and the exchange are free again
             if (!ok) return;
-            tc_before();
+            tc_after();
             if (tables) {
                 ++tabs;
                 if (lane == 0) mbar_arrive(bar(kTabEmpty));
             }
-            __syncwarp();
-            __threadfence_block();
-            if (lane == 0) atomicAdd(const_cast<int*>(done), 1);
         };
         while (ok && next(ok)) segment();
         if (!ok) give_up();
@@ -1065,14 +887,14 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 if (MASK && (at_next < lo_all || at_next >= hi_all || (doc_next >= 0 && doc_next != q_doc))) m = 0;
                 at_next = ask_mask(id_next, m_next, first_next, doc_next);
                 id_next = ask_page(t - 2);
-                const int v = 2 * vc + half, slot = v % L::kVSlots;
-                if (v >= L::kVSlots &&
-                    !__all_sync(0xFFFFFFFFu, mbar_try_wait(bar(kVEmpty + slot), (uint32_t)(v / L::kVSlots - 1) & 1u))) {
+                const int v = 2 * vc + half, slot = v % kVSlots;
+                if (v >= kVSlots &&
+                    !__all_sync(0xFFFFFFFFu, mbar_try_wait(bar(kVEmpty + slot), (uint32_t)(v / kVSlots - 1) & 1u))) {
                     if (pending >= 0) { cp_async_wait<0>(); publish(); }
-                    ok = warp_wait(kVEmpty + slot, (uint32_t)(v / L::kVSlots - 1));
+                    ok = warp_wait(kVEmpty + slot, (uint32_t)(v / kVSlots - 1));
                     if (!ok) break;
                 }
-                const uint32_t rows = base + L::kOffV + slot * kSlot + (uint32_t)(tok0 & 63) * 128u;     // of the warp's tokens
+                const uint32_t rows = base + kOffV + slot * kSlot + (uint32_t)(tok0 & 63) * 128u;     // of the warp's tokens
                 if (is_tree(t)) {                    // the tree's own values, full width
 #pragma unroll 4
                     for (int i = lane; i < 32 * kOctets; i += 32) {
@@ -1131,7 +953,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     if (threadIdx.x == 0) a.cta_status[blockIdx.x] = *abort_flag;
     if (warp == 1) {
         tc_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(4u * N) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
 }
 
@@ -1217,29 +1039,19 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // The workspace has to be sized without a device, so the partial slots are counted for this many CTAs.
 constexpr int kPlanSms = 148;
 
-// Rows per CTA: the fewest that hold a whole tree, at most 128 (64 with options on the scores).
-int rows_of(const Geom& g, int n_cap, bool score) {
-    const int most = score ? 64 : 128;
-    int n = 32;
-    while (n < most && n / g.Gq < n_cap) n *= 2;
-    return n;
-}
-
-template <int N, bool MASK, bool SCORE>
+template <bool MASK, bool SCORE>
 cudaError_t launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& fresh, const TreeArgs& a, int n_cta, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<N, MASK, SCORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Plan<N>::kSmem);
+    cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<MASK, SCORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
     if (e != cudaSuccess) return e;
-    tree_attn_kernel<N, MASK, SCORE><<<n_cta, kThreads, Plan<N>::kSmem, st>>>(q, k, fresh, a);
+    tree_attn_kernel<MASK, SCORE><<<n_cta, kThreads, kSmem, st>>>(q, k, fresh, a);
     return cudaGetLastError();
 }
 
 }  // namespace
 
-size_t tree_attn_ws_bytes(const Geom& g, int n_cap) {
-    // (a call with options has no more rows per CTA than one without)
-    const size_t n = (size_t)rows_of(g, n_cap, false);
-    return 256 + align256(kPlanSms * 4) + align256(((size_t)g.problems + 1) * 4) + 2 * (size_t)kPlanSms * n * 8 +
-           3 * (size_t)kPlanSms * n * kHeadDim * 4;
+size_t tree_attn_ws_bytes(const Geom& g, int) {
+    return 256 + align256(kPlanSms * 4) + align256(((size_t)g.problems + 1) * 4) + 2 * (size_t)kPlanSms * kRows * 8 +
+           4 * (size_t)kPlanSms * kRows * kHeadDim * 4;
 }
 
 cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tree& tree, const void* q, const int32_t* page_ids,
@@ -1247,7 +1059,6 @@ cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tr
                              int32_t* status, void* ws, cudaStream_t st) {
     const bool scored = score.softcap > 0.f || score.slopes || !(sm_scale > 0.f);
     const bool masked = scored || score.window > 0 || score.q_pos || score.tok_doc;
-    const int n = rows_of(g, tree.n_cap, masked);
     TreeArgs a;
     a.seq_len = g.seq_len; a.n_nodes = tree.n_nodes; a.parent = tree.parent; a.page_ids = page_ids; a.n_pages = n_pages;
     a.v_mask = cache.v_mask; a.v_offs = cache.v_offs; a.v_packed = static_cast<const uint4*>(cache.v_packed);
@@ -1261,14 +1072,14 @@ cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tr
     a.base = reinterpret_cast<int32_t*>(w);
     w += align256(((size_t)g.problems + 1) * 4);
     a.part_ml = reinterpret_cast<float2*>(w);
-    w += 2 * (size_t)kPlanSms * n * 8;
+    w += 2 * (size_t)kPlanSms * kRows * 8;
     a.part_o = reinterpret_cast<float*>(w);
-    w += 2 * (size_t)kPlanSms * n * kHeadDim * 4;
-    a.flush = reinterpret_cast<float*>(w);
+    w += 2 * (size_t)kPlanSms * kRows * kHeadDim * 4;
+    a.flush = reinterpret_cast<float4*>(w);
     a.cap_groups = cache.cap_groups;
     a.B = g.B; a.Hq = g.Hq; a.Hkv = g.Hkv; a.Gq = g.Gq; a.S = g.S; a.T = g.T; a.n_cap = tree.n_cap;
     a.max_pages = max_pages; a.problems = g.problems;
-    a.block_nodes = n / g.Gq;
+    a.block_nodes = kRows / g.Gq;
     a.gq_inv = (65536u + (uint32_t)g.Gq - 1u) / (uint32_t)g.Gq;
     a.sc = score;
     a.scale_log2 = sm_scale * kLog2e;
@@ -1305,11 +1116,8 @@ cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tr
     if (!rows_map(&map_new, tree.k, new_rows, tree.n_cap) ||
         !(g.T > 0 ? rows_map(&map_k, cache.k, (long long)g.problems * g.T, at_once) : rows_map(&map_k, tree.k, new_rows, at_once)))
         return cudaErrorInvalidValue;
-    if (n == 32) e = scored ? launch<32, true, true>(map_q, map_k, map_new, a, n_cta, st)
-                     : masked ? launch<32, true, false>(map_q, map_k, map_new, a, n_cta, st) : launch<32, false, false>(map_q, map_k, map_new, a, n_cta, st);
-    else if (n == 64) e = scored ? launch<64, true, true>(map_q, map_k, map_new, a, n_cta, st)
-                          : masked ? launch<64, true, false>(map_q, map_k, map_new, a, n_cta, st) : launch<64, false, false>(map_q, map_k, map_new, a, n_cta, st);
-    else e = launch<128, false, false>(map_q, map_k, map_new, a, n_cta, st);
+    e = scored ? launch<true, true>(map_q, map_k, map_new, a, n_cta, st)
+        : masked ? launch<true, false>(map_q, map_k, map_new, a, n_cta, st) : launch<false, false>(map_q, map_k, map_new, a, n_cta, st);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)g.problems, (unsigned)tree.n_cap);
@@ -1320,7 +1128,7 @@ cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tr
     early.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &early;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, tree_join_kernel, a, n, n_cta);
+    return cudaLaunchKernelEx(&cfg, tree_join_kernel, a, kRows, n_cta);
 }
 
 }  // namespace stc
