@@ -25,7 +25,7 @@
 // which take the tiles in turn, each with its own S, O, maxima and sums, joined at the end of a segment; 12..15 rebuild the value tiles
 // with 16-byte asynchronous copies straight from the packed store into the swizzled tile.
 //
-// The running maximum only moves when a tile exceeds it by more than 2^8, so the accumulator in tensor memory is rescaled a few times
+// The running maximum only moves when a tile exceeds it by more than 2^24, so the accumulator in tensor memory is rescaled a few times
 // per segment and not per tile.  The tensor core truncates when it adds to an accumulator (4e-8 of its value per product, 16
 // products per tile), so an accumulator is emptied into fp32 sums every kFlush tiles.  A unit's tree comes first, then its pages from
 // the last to the first: with a distance bias the largest scores come first.
@@ -48,23 +48,24 @@ constexpr uint32_t kHalf = kTok * 128;            // 64 channels of a token tile
 constexpr uint32_t kTile = 2 * kHalf;             // 32 KiB
 constexpr uint32_t kSlot = kTile / 2;             // values of 64 tokens: two halves of 64 channels
 constexpr int kRows = 128;                        // rows of a block = tensor-memory lanes
-constexpr int kFlush = 8;                         // tiles of a group that an accumulator takes: 128 products, at most 5e-6 of it
+constexpr int kFlush = 8;                         // tiles that an accumulator takes: 128 products, at most 5e-6 of it
+constexpr int kBufs = 3;                          // score buffers: 128 columns each, and 128 for O
 constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kSlack = 8.f;                     // log2 units a maximum may be exceeded by
+constexpr float kSlack = 24.f;                    // log2 units a maximum may be exceeded by: weights up to 2^24 are as exact as others
 constexpr int kKStages = 2, kVSlots = 6;          // K tiles; half V tiles
 
-// barriers, in 8-byte words of the control block; [2] = per group
+// barriers, in 8-byte words of the control block; S, P, O per score buffer
 enum { kQFull, kQEmpty, kKFull, kKEmpty = kKFull + kKStages, kVFull = kKEmpty + kKStages, kVEmpty = kVFull + kVSlots,
-       kSFull = kVEmpty + kVSlots, kPFull = kSFull + 2, kOFull = kPFull + 2, kXchg = kOFull + 2, kTabFull, kTabEmpty, kSegFull,
+       kSFull = kVEmpty + kVSlots, kPFull = kSFull + kBufs, kOFull = kPFull + kBufs, kPair = kOFull + kBufs, kTabFull = kPair + 4, kTabEmpty, kSegFull,
        kSegEmpty = kSegFull + kSegs, kBars = kSegEmpty + kSegs };
-constexpr int kRing = 6;                          // tiles whose valid tokens are kept: K stages, the groups' tiles and one more
+constexpr int kRing = 6;                          // tiles whose valid tokens are kept: K stages, score buffers and one more
 constexpr uint32_t kQHalf = kRows * 128;
 constexpr uint32_t kOffK = 2 * kQHalf, kOffV = kOffK + kKStages * kTile, kOffCtl = kOffV + kVSlots * kSlot;
-constexpr uint32_t kCtlTmem = 256, kCtlAbort = 260, kCtlSegs = 272, kCtlValid = kCtlSegs + kSegs * 48,            // [ring][4 words]
+constexpr uint32_t kCtlTmem = 304, kCtlAbort = 308, kCtlSegs = 320, kCtlValid = kCtlSegs + kSegs * 48,            // [ring][4 words]
                    kCtlIds = kCtlValid + kRing * 16, kCtlPos = kCtlIds + kRing * 32,                              // [ring][8 pages], [128]
                    kCtlKin = (kCtlPos + 512 + 15) / 16 * 16,                                                      // [128 nodes][4 words]
-                   kCtlMl = kCtlKin + STC_TREE_MAX_NODES * 16, kCtlBytes = kCtlMl + 2 * kRows * 8;                // [2 groups][128]
+                   kCtlMl = kCtlKin + STC_TREE_MAX_NODES * 16, kCtlBytes = kCtlMl + 2 * kRows * 8;                // [2][2 groups][128]
 constexpr uint32_t kSmem = kOffCtl + kCtlBytes;
 static_assert(kBars * 8 <= kCtlTmem && kSmem <= 232448, "shared memory of a block");
 
@@ -86,7 +87,7 @@ struct TreeArgs {
     int32_t* base;               // [problems + 1]: where each problem begins in the flat sequence, and its length
     float2* part_ml;             // [2 * grid][128 rows]
     float* part_o;               // [2 * grid][128 rows][128]
-    float4* flush;               // [grid][2 groups][32][128 rows]: sums of emptied accumulators
+    float4* flush;               // [grid][32][128 rows]: sums of emptied accumulators
     int64_t cap_groups;
     int B, Hq, Hkv, Gq, S, T, n_cap, max_pages, problems;
     int block_nodes;             // nodes per block of rows = 128 / Gq
@@ -173,7 +174,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     volatile int* segs = reinterpret_cast<volatile int*>(ctl + kCtlSegs);                   // [kSegs][12]
     uint32_t* const kin = reinterpret_cast<uint32_t*>(ctl + kCtlKin);
     int* const node_pos = reinterpret_cast<int*>(ctl + kCtlPos);
-    float2* const ml = reinterpret_cast<float2*>(ctl + kCtlMl);
+    float* const told = reinterpret_cast<float*>(ctl + kCtlMl);
     volatile uint32_t* const valid_tokens = reinterpret_cast<volatile uint32_t*>(ctl + kCtlValid);
     volatile int* const tile_pages = reinterpret_cast<volatile int*>(ctl + kCtlIds);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -184,7 +185,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_new) : "memory");
     if (threadIdx.x >= 64 && threadIdx.x < 64 + kBars) {
         const int i = (int)threadIdx.x - 64;
-        mbar_init(bars + 8 * i, i >= kVFull && i < kVEmpty ? 2 : i >= kPFull && i < kOFull ? 4 : i == kXchg || i == kTabEmpty ? 8
+        mbar_init(bars + 8 * i, i >= kVFull && i < kVEmpty ? 2 : i >= kPFull && i < kOFull ? 8 : i >= kPair && i < kTabFull ? 2 : i == kTabEmpty ? 8
                                 : i >= kSegEmpty ? kSegReaders : 1);
         fence_mbar_init();
     }
@@ -366,30 +367,29 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         constexpr uint32_t id_s = idesc_bf16(kRows, kTok, false);
         const uint32_t sm = uniform(base), ts = uniform(tmem);
         const uint64_t dq = smem_desc_128(sm, 16), dk0 = smem_desc_128(sm + kOffK, 16);
-        uint32_t st = 0, phase = 0, seg = 0, before[2] = {0u, 0u};   // K stage and its phase; segments; tiles of each group so far
+        uint32_t st = 0, phase = 0, seg = 0, buf = 0, turn = 0;      // K stage and its phase; segments; score buffer, its uses so far
         bool ok = true;
         while (ok && next(ok)) {
             const int tiles = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)(s.tile1 - s.tile0));
             ok = warp_wait(kQFull, seg);
 #pragma unroll 1
             for (int n = 0; ok && n < tiles; ++n) {
-                const uint32_t g = (uint32_t)n & 1u, j = g ? before[1] : before[0];
-                // the group's S holds the weights of its last tile until their product is through
-                ok = warp_wait(kKFull + st, phase) && (j == 0 || warp_wait(kOFull + g, j - 1u));
+                // the buffer holds the weights of an earlier tile until their product is through
+                ok = warp_wait(kKFull + st, phase) && (turn == 0 || warp_wait(kOFull + buf, turn - 1u));
                 if (!ok) break;
                 tc_after();
                 const uint64_t dk = dk0 + (uint64_t)(st * (kTile >> 4));
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k)      // 16 dims = 32 bytes = 2 units; 64 dims = one half tile
-                        tc_mma_ss(ts + g * 256u, dq + (uint64_t)((k >> 2) * (kQHalf >> 4) + (k & 3) * 2),
+                        tc_mma_ss(ts + buf * kTok, dq + (uint64_t)((k >> 2) * (kQHalf >> 4) + (k & 3) * 2),
                                   dk + (uint64_t)((k >> 2) * (kHalf >> 4) + (k & 3) * 2), id_s, k != 0);
-                    tc_commit_to(bar(kSFull + g));
+                    tc_commit_to(bar(kSFull + buf));
                     tc_commit_to(bar(kKEmpty + st));
                     if (n == tiles - 1) tc_commit_to(bar(kQEmpty));
                 }
                 __syncwarp();
-                if (g) ++before[1]; else ++before[0];
+                if (++buf == (uint32_t)kBufs) { buf = 0; ++turn; }
                 if (++st == (uint32_t)kKStages) { st = 0; phase ^= 1u; }
             }
             ++seg;
@@ -398,33 +398,33 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     } else if (warp == 2) {
         // ---- issuer of O += P V~ ----------------------------------------------------------------------------------------
         constexpr uint32_t id_o = idesc_bf16(kRows, kHeadDim, true);
-        const uint32_t sm = uniform(base), ts = uniform(tmem);
+        const uint32_t sm = uniform(base), ts = uniform(tmem), to = ts + kBufs * kTok;
         const uint64_t dv0 = smem_desc_128(sm + kOffV, kSlot / 2);
-        uint32_t slot = 0, phase = 0, before[2] = {0u, 0u};
+        uint32_t slot = 0, phase = 0, buf = 0, turn = 0;
         bool ok = true;
         while (ok && next(ok)) {
             const int tiles = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)(s.tile1 - s.tile0));
 #pragma unroll 1
             for (int n = 0; ok && n < tiles; ++n) {
-                const uint32_t g = (uint32_t)n & 1u, j = g ? before[1] : before[0], next_slot = slot + 1u;    // (a tile's slots are neighbours)
-                ok = warp_wait(kVFull + slot, phase) && warp_wait(kVFull + next_slot, phase) && warp_wait(kPFull + g, j);
+                const uint32_t next_slot = slot + 1u;                        // (a tile's slots are neighbours)
+                ok = warp_wait(kVFull + slot, phase) && warp_wait(kVFull + next_slot, phase) && warp_wait(kPFull + buf, turn);
                 if (!ok) break;
                 tc_after();
                 const uint64_t dv = dv0 + (uint64_t)(slot * (kSlot >> 4));
-                const uint32_t p = ts + g * 256u, more = (uint32_t)((n >> 1) % kFlush != 0);          // else O starts anew
+                const uint32_t p = ts + buf * kTok, more = (uint32_t)(n % kFlush != 0);               // else O starts anew
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {    // 16 tokens: 16 rows of 128 bytes; P: 8 columns high, 8 residual
                         const uint64_t d = dv + (uint64_t)((k >> 2) * (kSlot >> 4) + (k & 3) * (2048 >> 4));
-                        tc_mma_ts(p + 128, p + 16 * k, d, id_o, k ? 1u : more);
-                        tc_mma_ts(p + 128, p + 16 * k + 8, d, id_o, 1);
+                        tc_mma_ts(to, p + 16 * k, d, id_o, k ? 1u : more);
+                        tc_mma_ts(to, p + 16 * k + 8, d, id_o, 1);
                     }
-                    tc_commit_to(bar(kOFull + g));
+                    tc_commit_to(bar(kOFull + buf));
                     tc_commit_to(bar(kVEmpty + slot));
                     tc_commit_to(bar(kVEmpty + next_slot));
                 }
                 __syncwarp();
-                if (g) ++before[1]; else ++before[0];
+                if (++buf == (uint32_t)kBufs) { buf = 0; ++turn; }
                 slot += 2;
                 if (slot == (uint32_t)kVSlots) { slot = 0; phase ^= 1u; }
             }
@@ -530,22 +530,33 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         }
         if (!ok) give_up();
     } else if (warp < 12) {
-        // ---- softmax: thread = row ---------------------------------------------------------------------------------------
-        const int grp = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
-        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), ts = lanes + (uint32_t)grp * 256u, to = ts + 128;
-        float4* const my_flush = a.flush + ((size_t)blockIdx.x * 2 + grp) * 32 * kRows + row;
-        uint32_t j = 0, joins = 0, tabs = 0, tile0 = 0;      // this group's tiles so far; joins; tables; tiles of the segments before
+        // ---- softmax: thread = row; the two warps of a quarter have 64 of a tile's 128 tokens each ------------------------
+        const int grp = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane, c0 = 64 * grp;
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), to = lanes + kBufs * kTok;
+        float4* const my_flush = a.flush + (size_t)blockIdx.x * 32 * kRows + row;
+        uint32_t buf = 0, turn = 0, last_buf = 0, last_turn = 0, ring = 0;   // score buffer and its uses so far, of the tile before too
+        uint32_t pairs = 0, tabs = 0;
         bool ok = true;
-        auto join = [&]() {                          // both groups
+        // what the warps of a quarter tell each other, a number per row
+        auto exchange = [&](float mine, float& other) {
+            float* const place = told + (pairs & 1u) * 2 * kRows;
+            place[grp * kRows + row] = mine;
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kXchg));
-            return warp_wait(kXchg, joins++);
+            if (lane == 0) mbar_arrive(bar(kPair + quarter));
+            if (!warp_wait(kPair + quarter, pairs++)) return false;
+            other = place[(grp ^ 1) * kRows + row];
+            return true;
+        };
+        auto step = [&]() {
+            last_buf = buf; last_turn = turn;
+            if (++buf == (uint32_t)kBufs) { buf = 0; ++turn; }
+            if (++ring == (uint32_t)kRing) ring = 0;
         };
 
         auto segment = [&]() {
             const int live = min(a.block_nodes, s.nodes - s.node0) * a.Gq;    // rows of the block
             const bool mine = row < live, warp_live = quarter * 32 < live;
-            const int tiles = s.tile1 - s.tile0, count = (tiles + 1 - grp) >> 1;
+            const int tiles = s.tile1 - s.tile0;
             const bool tables = MASK || is_tree(s.tile1 - 1);
             const uint32_t in_block = ((uint32_t)row * a.gq_inv) >> 16;
             const int node = min(s.node0 + (int)in_block, STC_TREE_MAX_NODES - 1), h = row - (int)in_block * a.Gq;
@@ -559,43 +570,48 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             }
             float m = -INFINITY, l = 0.f, m_flush = -INFINITY;
 #pragma unroll 1
-            for (int n = 0; n < count; ++n, ++j) {
-                const int t = s.tile1 - 1 - 2 * n - grp;
-                ok = warp_wait(kSFull + grp, j);
+            for (int n = 0; n < tiles; ++n, step()) {
+                const int t = s.tile1 - 1 - n;
+                ok = warp_wait(kSFull + buf, turn);
                 if (!ok) return;
                 if (!warp_live) {                    // a quarter without rows: its P may be anything
-                    if (lane == 0) mbar_arrive(bar(kPFull + grp));
+                    if (lane == 0) mbar_arrive(bar(kPFull + buf));
                     continue;
                 }
+                const uint32_t ts = lanes + buf * kTok + c0;
+                auto last_product = [&]() {          // the product of the tile before is through
+                    const bool good = warp_wait(kOFull + last_buf, last_turn);
+                    tc_after();
+                    return good;
+                };
                 tc_after();
                 // tokens that the row sees: those that there are, in the tree its ancestors, and the window's
-                const int at = (int)((tile0 + 2u * (uint32_t)n + (uint32_t)grp) % kRing);
-                uint32_t see[4];
+                uint32_t see[2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) see[i] = valid_tokens[at * 4 + i];
+                for (int i = 0; i < 2; ++i) see[i] = valid_tokens[ring * 4 + 2 * grp + i];
                 const bool tree = is_tree(t);
                 if (tree) {
                     if (!MASK) {
                         ok = warp_wait(kTabFull, tabs);
                         if (!ok) return;
                     }
-                    const uint4 k = reinterpret_cast<const uint4*>(kin)[node];
-                    see[0] &= k.x; see[1] &= k.y; see[2] &= k.z; see[3] &= k.w;
+                    const uint2 k = reinterpret_cast<const uint2*>(kin)[node * 2 + grp];
+                    see[0] &= k.x; see[1] &= k.y;
                 }
                 if constexpr (MASK) {
                     if (tree) {
 #pragma unroll 1
-                        for (int i = 0; i < s.nodes; ++i) {
-                            const int at_i = node_pos[i];
+                        for (int i = 0; i < min(64, s.nodes - c0); ++i) {
+                            const int at_i = node_pos[c0 + i];
                             if (at_i > p || (uint32_t)p - (uint32_t)at_i >= a.window) {
-#pragma unroll
-                                for (int w = 0; w < 4; ++w) see[w] &= ~(i >> 5 == w ? 1u << (i & 31) : 0u);
+                                if (i < 32) see[0] &= ~(1u << i);
+                                else see[1] &= ~(1u << (i - 32));
                             }
                         }
                     } else if (a.sc.q_pos || a.sc.window > 0) {
 #pragma unroll
-                        for (int i = 0; i < kTilePages; ++i) {                // of a page's 16 tokens the bits [lo, hi)
-                            const int t0 = tile_pages[at * kTilePages + i] * kPage;
+                        for (int i = 0; i < kTilePages / 2; ++i) {            // of a page's 16 tokens the bits [lo, hi)
+                            const int t0 = tile_pages[ring * kTilePages + kTilePages / 2 * grp + i] * kPage;
                             const long long ahead = (long long)p - t0;        // distance of its first token
                             const int hi = (int)min(max(ahead + 1, 0LL), 16LL), lo = (int)min(max(ahead + 1 - (long long)a.window, 0LL), 16LL);
                             const uint32_t bits = ((1u << hi) - 1u) & ~((1u << lo) - 1u);
@@ -603,18 +619,18 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         }
                     }
                 }
-                const bool open = __all_sync(0xFFFFFFFFu, !mine || (see[0] & see[1] & see[2] & see[3]) == 0xFFFFFFFFu);
+                const bool open = __all_sync(0xFFFFFFFFu, !mine || (see[0] & see[1]) == 0xFFFFFFFFu);
                 const bool empty_now = n > 0 && n % kFlush == 0;
                 const float m_acc = m;               // maximum the accumulator was built with
                 // maximum of the tile; scores that are not raw products times a positive scale, or hidden, are written back
                 float top = -INFINITY;
 #pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 0; c < 2; ++c) {
                     uint32_t r[32];
                     tmem_ld16<0>(ts + 32 * c, r);
                     tmem_ld16<16>(ts + 32 * c + 16, r);
                     tmem_wait_ld();
-                    const uint32_t bits = c & 2 ? (c & 1 ? see[3] : see[2]) : (c & 1 ? see[1] : see[0]);
+                    const uint32_t bits = c ? see[1] : see[0];
                     if constexpr (SCORE) {
                         if (a.cap_in != 0.f) {
                             // (what a row does not see, and lanes without a row, have no say in how the others are capped)
@@ -631,11 +647,11 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                             if (tree) {
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
-                                    r[i] = __float_as_uint(fmaf(slope2, (float)(node_pos[32 * c + i] - p), __uint_as_float(r[i])));
+                                    r[i] = __float_as_uint(fmaf(slope2, (float)(node_pos[c0 + 32 * c + i] - p), __uint_as_float(r[i])));
                             } else {
 #pragma unroll
                                 for (int e = 0; e < 2; ++e) {
-                                    const float far = (float)(tile_pages[at * kTilePages + 2 * c + e] * kPage - p);
+                                    const float far = (float)(tile_pages[ring * kTilePages + kTilePages / 2 * grp + 2 * c + e] * kPage - p);
 #pragma unroll
                                     for (int i = 0; i < 16; i += 2) {
                                         const float2 x = fma2(both(slope2), add2(both(far), make_float2((float)i, (float)(i + 1))),
@@ -667,15 +683,20 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 }
                 if (SCORE || !open) tmem_wait_st();
                 if (!SCORE) top *= a.scale_log2;     // (-inf stays -inf: the scale is positive)
-                // move the maximum only if it is exceeded by much; the accumulator follows.  (S was only issued when the product
-                // of the group's last tile was through.)
+                float other = -INFINITY;
+                ok = exchange(top, other);
+                if (!ok) return;
+                top = fmaxf(top, other);
+                // move the maximum only if it is exceeded by much; the accumulator follows (half of its channels here, half there)
                 const bool move = mine && (top > m + kSlack || (m == -INFINITY && top > -INFINITY));
                 if (__any_sync(0xFFFFFFFFu, move)) {
                     const float to_m = move ? top : m, f = m == -INFINITY ? 0.f : ex2(m - to_m);
                     l *= f;
                     if (n > 0 && !empty_now) {
+                        ok = last_product();
+                        if (!ok) return;
 #pragma unroll 1
-                        for (int c = 0; c < kHeadDim; c += 16) {
+                        for (int c = c0; c < c0 + 64; c += 16) {
                             uint32_t q[16];
                             tmem_ld16(to + c, q);
                             tmem_wait_ld();
@@ -688,9 +709,11 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 }
                 // the accumulator is emptied into fp32 sums, relative to m_flush; the issuer starts it anew
                 if (empty_now) {
+                    ok = last_product();
+                    if (!ok) return;
                     const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m_acc);
 #pragma unroll 1
-                    for (int c = 0; c < kHeadDim; c += 16) {
+                    for (int c = c0; c < c0 + 64; c += 16) {
                         float4 old[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
@@ -710,7 +733,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 const float ref = m == -INFINITY ? 0.f : m;
                 float2 la = make_float2(0.f, 0.f), lb = la;
 #pragma unroll 1
-                for (int c = 0; c < 128; c += 32) {
+                for (int c = 0; c < 64; c += 32) {
                     uint32_t r[32];
                     tmem_ld16<0>(ts + c, r);
                     tmem_ld16<16>(ts + c + 16, r);
@@ -739,80 +762,44 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 tmem_wait_st();
                 tc_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(kPFull + grp));
+                if (lane == 0) mbar_arrive(bar(kPFull + buf));
             }
-            // ---- end of the segment: both groups hold part of the rows; each joins them for half of the channels ----------
-            if (count > 0) {
-                ok = warp_wait(kOFull + grp, j - 1);
-                if (!ok) return;
-                tc_after();
-                if (count > kFlush && warp_live) {   // take back what the accumulator was emptied of
-                    const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m);
-#pragma unroll 1
-                    for (int c = 0; c < kHeadDim; c += 16) {
-                        float4 old[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) old[i] = __ldcg(my_flush + (size_t)(c / 4 + i) * kRows);
-                        uint32_t q[16];
-                        tmem_ld16(to + c, q);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            q[4 * i] = __float_as_uint(fmaf(old[i].x, keep, __uint_as_float(q[4 * i])));
-                            q[4 * i + 1] = __float_as_uint(fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1])));
-                            q[4 * i + 2] = __float_as_uint(fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2])));
-                            q[4 * i + 3] = __float_as_uint(fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3])));
-                        }
-                        tmem_st16(to + c, q);
-                    }
-                    tmem_wait_st();
-                }
-            }
-            tile0 += (uint32_t)tiles;
-            ml[grp * kRows + row] = make_float2(m, l);
-            tc_before();
-            ok = join();
+            // ---- end of the segment: each warp of a quarter writes half of its rows' channels --------------------------------
+            ok = warp_wait(kOFull + last_buf, last_turn);
             if (!ok) return;
             tc_after();
             if (warp_live) {
-                const float2 a0 = ml[row], a1 = ml[kRows + row];
-                m = fmaxf(a0.x, a1.x);
-                float f0 = a0.x == -INFINITY ? 0.f : ex2(a0.x - m), f1 = a1.x == -INFINITY ? 0.f : ex2(a1.x - m);
-                l = (a0.x == -INFINITY ? a0.y : a0.y * f0) + (a1.x == -INFINITY ? a1.y : a1.y * f1);      // (nothing seen: 0, or NaN)
+                float other = 0.f;
+                ok = exchange(l, other);
+                if (!ok) return;
+                l += other;
                 const bool whole = s.slot < 0;
                 const size_t at = ((size_t)s.b * a.n_cap + node) * a.Hq + s.hk * a.Gq + h;
-                if (whole) {
-                    const float inv = l != 0.f ? 1.f / l : 0.f;
-                    f0 *= inv;
-                    f1 *= inv;
-                }
                 if (grp == 0 && mine) {
                     if (!whole) a.part_ml[(size_t)s.slot * kRows + row] = make_float2(m, l);
                     else if (a.lse) a.lse[at] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
                 }
+                const float f = !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;     // (0: nothing seen, whatever was summed)
+                const float keep = f * (m_flush == -INFINITY ? 0.f : ex2(m_flush - m));
                 float4* dst = reinterpret_cast<float4*>(whole ? a.out + at * kHeadDim : a.part_o + ((size_t)s.slot * kRows + row) * kHeadDim);
 #pragma unroll 1
-                for (int c = 64 * grp; c < 64 * grp + 64; c += 16) {
-                    uint32_t q0[16], q1[16];
-                    tmem_ld16(lanes + 128 + c, q0);
-                    tmem_ld16(lanes + 384 + c, q1);
+                for (int c = c0; c < c0 + 64; c += 16) {
+                    float4 old[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        old[i] = tiles > kFlush ? __ldcg(my_flush + (size_t)(c / 4 + i) * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    uint32_t q[16];
+                    tmem_ld16(to + c, q);
                     tmem_wait_ld();
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float v[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {        // (a factor 0 stands for "nothing seen", whatever was summed)
-                            v[e] = f0 != 0.f ? __uint_as_float(q0[4 * i + e]) * f0 : 0.f;
-                            if (f1 != 0.f) v[e] = fmaf(__uint_as_float(q1[4 * i + e]), f1, v[e]);
-                        }
-                        if (mine) __stcg(dst + c / 4 + i, make_float4(v[0], v[1], v[2], v[3]));
+                        const float4 v = make_float4(fmaf(old[i].x, keep, __uint_as_float(q[4 * i]) * f), fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1]) * f),
+                                                     fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2]) * f), fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3]) * f));
+                        if (mine) __stcg(dst + c / 4 + i, f != 0.f ? v : make_float4(0.f, 0.f, 0.f, 0.f));
                     }
                 }
                 tc_before();
             }
-            ok = join();                             // accumulators and the exchange are free again
-            if (!ok) return;
-            tc_after();
             if (tables) {
                 ++tabs;
                 if (lane == 0) mbar_arrive(bar(kTabEmpty));
@@ -1051,7 +1038,7 @@ cudaError_t launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap
 
 size_t tree_attn_ws_bytes(const Geom& g, int) {
     return 256 + align256(kPlanSms * 4) + align256(((size_t)g.problems + 1) * 4) + 2 * (size_t)kPlanSms * kRows * 8 +
-           4 * (size_t)kPlanSms * kRows * kHeadDim * 4;
+           3 * (size_t)kPlanSms * kRows * kHeadDim * 4;
 }
 
 cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tree& tree, const void* q, const int32_t* page_ids,
