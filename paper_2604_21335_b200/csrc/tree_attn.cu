@@ -47,12 +47,14 @@ constexpr int kSegReaders = 15;                   // warps that follow the segme
 constexpr uint32_t kHalf = kTok * 128;            // 64 channels of a token tile: 128 rows of 128 bytes
 constexpr uint32_t kTile = 2 * kHalf;             // 32 KiB
 constexpr uint32_t kSlot = kTile / 2;             // values of 64 tokens: two halves of 64 channels
-constexpr int kRows = 128;                        // rows of a block = tensor-memory lanes
+constexpr int kRows = 128;                        // tensor-memory lanes
 constexpr int kFlush = 8;                         // tiles that an accumulator takes: 128 products, at most 5e-6 of it
 constexpr int kBufs = 3;                          // score buffers: 128 columns each, and 128 for O
 constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 24.f;                    // log2 units a maximum may be exceeded by: weights up to 2^24 are as exact as others
+constexpr int kSoftmaxRegs = 176, kOtherRegs = 80;           // of the 128 per thread of the launch
+static_assert(256 * kSoftmaxRegs + 256 * kOtherRegs <= 128 * kThreads, "registers of a block");
 constexpr int kKStages = 2, kVSlots = 6;          // K tiles; half V tiles
 
 // barriers, in 8-byte words of the control block; S, P, O per score buffer
@@ -85,12 +87,12 @@ struct TreeArgs {
     int32_t* word;               // the call's status word
     int32_t* cta_status;         // [grid]
     int32_t* base;               // [problems + 1]: where each problem begins in the flat sequence, and its length
-    float2* part_ml;             // [2 * grid][128 rows]
-    float* part_o;               // [2 * grid][128 rows][128]
-    float4* flush;               // [grid][32][128 rows]: sums of emptied accumulators
+    float2* part_ml;             // [2 * grid][128 lanes]
+    float4* part_o;              // [3 * grid][32][128 lanes]: first and last partial of a CTA, and a place to add copies up
     int64_t cap_groups;
     int B, Hq, Hkv, Gq, S, T, n_cap, max_pages, problems;
-    int block_nodes;             // nodes per block of rows = 128 / Gq
+    int rows;                    // rows of a block: 32, 64 or 128
+    int block_nodes;             // nodes of a block = rows / Gq
     uint32_t gq_inv;             // row / Gq = row * gq_inv >> 16 for rows below 128
     float scale_log2, cap_in, cap_log2;
     uint32_t window;             // tokens a row sees, 0xFFFFFFFF without a window
@@ -160,11 +162,13 @@ __device__ __forceinline__ void cp_async16_if(uint32_t dst, const void* src, uin
                  ::"r"(dst), "l"(src), "r"(take) : "memory");
 }
 // MASK: a window, documents or positions that are given; SCORE: cap, slopes, or a scale that is not positive (with MASK).
-template <bool MASK, bool SCORE>
+// R rows of a block; the lanes hold 128 / R copies of them.
+template <int R, bool MASK, bool SCORE>
 __global__ void __launch_bounds__(kThreads, 1)
 tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                  const __grid_constant__ CUtensorMap map_new, const TreeArgs a) {
     static_assert(MASK || !SCORE, "SCORE needs the positions");
+    constexpr int kCopies = kRows / R, kCols = R / 2;         // tokens of a tile that a thread weighs
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = smem_u32(smem);
     const uint32_t bars = base + kOffCtl;
@@ -185,7 +189,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_new) : "memory");
     if (threadIdx.x >= 64 && threadIdx.x < 64 + kBars) {
         const int i = (int)threadIdx.x - 64;
-        mbar_init(bars + 8 * i, i >= kVFull && i < kVEmpty ? 2 : i >= kPFull && i < kOFull ? 8 : i >= kPair && i < kTabFull ? 2 : i == kTabEmpty ? 8
+        mbar_init(bars + 8 * i, i >= kVFull && i < kVEmpty ? 2 : i >= kPFull && i < kOFull ? 8 : i >= kPair && i < kTabFull ? 2 * kCopies : i == kTabEmpty ? 8
                                 : i >= kSegEmpty ? kSegReaders : 1);
         fence_mbar_init();
     }
@@ -265,286 +269,299 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     };
     auto is_page = [&](int id) { return id >= 0 && id < (s.len + kPage - 1) / kPage; };
 
+    // the softmax warps hold 64 channels of their rows besides a tile's scores; the registers are moved within each role, where ptxas
+    // sees how many there are
+    auto fewer_registers = [] { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs)); };
     if (*abort_flag) {
         // nothing was started
-    } else if (warp == 0) {
-        // ---- producer of Q and K ---------------------------------------------------------------------------
-        int kc = 0, seg = 0, ring = 0;
-        uint32_t st = 0, phase = 1;                  // K stage, and the phase in which it is empty (of the second round on)
-        bool ok = true;
-        const uint32_t q_bytes = 2u * 128u * (uint32_t)(a.Gq * a.block_nodes);
-        while (ok && next(ok)) {
-            const int problem = s.b * a.Hkv + s.hk;
-            const int32_t* const doc_row = MASK && a.sc.tok_doc ? a.sc.tok_doc + (size_t)s.b * a.T : nullptr;
-            const int q_doc = doc_row ? a.sc.q_doc[s.b] : 0;
-            // pages of a tile in lanes 0 .. 7, asked for two tiles ahead; documents of its tokens (32 c + lane) one tile ahead
-            auto ask = [&](int t) { return lane < kTilePages && t >= s.tile0 ? listed(t * kTilePages + lane) : -1; };
-            int doc[4];
-            auto ask_docs = [&](int pages) {
-                if (MASK && doc_row) {
+    } else if (warp < 4) {
+        fewer_registers();
+        if (warp == 0) {
+            // ---- producer of Q and K ---------------------------------------------------------------------------
+            int kc = 0, seg = 0, ring = 0;
+            uint32_t st = 0, phase = 1;                  // K stage, and the phase in which it is empty (of the second round on)
+            bool ok = true;
+            const uint32_t q_bytes = 2u * 128u * (uint32_t)(a.Gq * a.block_nodes * kCopies);
+            while (ok && next(ok)) {
+                const int problem = s.b * a.Hkv + s.hk;
+                const int32_t* const doc_row = MASK && a.sc.tok_doc ? a.sc.tok_doc + (size_t)s.b * a.T : nullptr;
+                const int q_doc = doc_row ? a.sc.q_doc[s.b] : 0;
+                // pages of a tile in lanes 0 .. 7, asked for two tiles ahead; documents of its tokens (32 c + lane) one tile ahead
+                auto ask = [&](int t) { return lane < kTilePages && t >= s.tile0 ? listed(t * kTilePages + lane) : -1; };
+                int doc[4];
+                auto ask_docs = [&](int pages) {
+                    if (MASK && doc_row) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const int page = __shfl_sync(0xFFFFFFFFu, pages, 2 * c + (lane >> 4)), t = page * kPage + (lane & 15);
-                        doc[c] = is_page(page) && t < s.len ? __ldg(doc_row + t) : -1;
-                    }
-                }
-            };
-            int id = ask(s.tile1 - 1), id_next = ask(s.tile1 - 2);
-            ask_docs(id);
-            bool q_due = true;
-#pragma unroll 1
-            for (int t = s.tile1 - 1; t >= s.tile0; --t) {
-                // tokens of the tile that there are: 16 bits per page, a word per softmax warp of a group
-                const bool tree = is_tree(t);
-                const int here = !tree ? (is_page(id) ? min(kPage, s.len - id * kPage) : 0) : min(max(s.nodes - lane * kPage, 0), kPage);
-                uint32_t word = (1u << here) - 1u;
-                word = (word | __shfl_down_sync(0xFFFFFFFFu, word, 1) << 16);                // (lanes 0, 2, 4, 6)
-                word = __shfl_sync(0xFFFFFFFFu, word, 2 * lane & 7);
-                if (MASK && doc_row && !tree) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const uint32_t same = __ballot_sync(0xFFFFFFFFu, doc[c] < 0 || doc[c] == q_doc);
-                        if (lane == c) word &= same;
-                    }
-                }
-                if (kc >= kKStages) ok = warp_wait(kKEmpty + st, phase);
-                if (!ok) break;
-                if (lane < 4) valid_tokens[ring * 4 + lane] = word;
-                if (MASK && lane < kTilePages) tile_pages[ring * kTilePages + lane] = id;
-                if (++ring == kRing) ring = 0;
-                __syncwarp();
-                const uint32_t full = bar(kKFull + st), dst = base + kOffK + st * kTile;
-                if (tree || !a.page_ids) {           // consecutive rows: two copies of 64 channels
-                    if (elect_one()) {
-                        const CUtensorMap* map = tree ? &map_new : &map_k;
-                        const int y = tree ? problem * a.n_cap : problem * a.T + (s.first + t * kTilePages) * kPage;
-                        mbar_expect_tx(full, (uint32_t)(tree ? a.n_cap : kTok) * kRowBytes);
-                        tma_2d(dst, map, 0, y, full);
-                        tma_2d(dst + kHalf, map, 64, y, full);
-                    }
-                } else {                             // two copies per page.  (From eight lanes at once they take 1300 cycles.)
-                    const uint32_t pages = __ballot_sync(0xFFFFFFFFu, is_page(id));
-                    if (elect_one()) mbar_expect_tx(full, (uint32_t)__popc(pages) * kPage * kRowBytes);
-                    __syncwarp();
-#pragma unroll
-                    for (int p = 0; p < kTilePages; ++p) {
-                        const int y = problem * a.T + __shfl_sync(0xFFFFFFFFu, id, p) * kPage;
-                        if (((pages >> p) & 1u) && elect_one()) {
-                            tma_2d(dst + p * kPage * 128, &map_k, 0, y, full);
-                            tma_2d(dst + kHalf + p * kPage * 128, &map_k, 64, y, full);
+                        for (int c = 0; c < 4; ++c) {
+                            const int page = __shfl_sync(0xFFFFFFFFu, pages, 2 * c + (lane >> 4)), t = page * kPage + (lane & 15);
+                            doc[c] = is_page(page) && t < s.len ? __ldg(doc_row + t) : -1;
                         }
                     }
-                }
-                __syncwarp();
-                ++kc;
-                if (++st == (uint32_t)kKStages) { st = 0; phase ^= 1u; }
-                id = id_next;
-                id_next = ask(t - 2);
+                };
+                int id = ask(s.tile1 - 1), id_next = ask(s.tile1 - 2);
                 ask_docs(id);
-                if (q_due) {                         // the queries behind the first keys, which come from farther away
-                    q_due = false;
-                    if (seg > 0) ok = warp_wait(kQEmpty, (uint32_t)(seg - 1));
+                bool q_due = true;
+#pragma unroll 1
+                for (int t = s.tile1 - 1; t >= s.tile0; --t) {
+                    // tokens of the tile that there are: 16 bits per page, a word per softmax warp of a group
+                    const bool tree = is_tree(t);
+                    const int here = !tree ? (is_page(id) ? min(kPage, s.len - id * kPage) : 0) : min(max(s.nodes - lane * kPage, 0), kPage);
+                    uint32_t word = (1u << here) - 1u;
+                    word = (word | __shfl_down_sync(0xFFFFFFFFu, word, 1) << 16);                // (lanes 0, 2, 4, 6)
+                    word = __shfl_sync(0xFFFFFFFFu, word, 2 * lane & 7);
+                    if (MASK && doc_row && !tree) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const uint32_t same = __ballot_sync(0xFFFFFFFFu, doc[c] < 0 || doc[c] == q_doc);
+                            if (lane == c) word &= same;
+                        }
+                    }
+                    if (kc >= kKStages) ok = warp_wait(kKEmpty + st, phase);
                     if (!ok) break;
-                    if (lane == 0) {
-                        mbar_expect_tx(bar(kQFull), q_bytes);
-                        tma_3d(base, &map_q, 0, s.hk * a.Gq, s.b * a.n_cap + s.node0, bar(kQFull));
-                        tma_3d(base + kQHalf, &map_q, 64, s.hk * a.Gq, s.b * a.n_cap + s.node0, bar(kQFull));
+                    if (lane < 4) valid_tokens[ring * 4 + lane] = word;
+                    if (MASK && lane < kTilePages) tile_pages[ring * kTilePages + lane] = id;
+                    if (++ring == kRing) ring = 0;
+                    __syncwarp();
+                    const uint32_t full = bar(kKFull + st), dst = base + kOffK + st * kTile;
+                    if (tree || !a.page_ids) {           // consecutive rows: two copies of 64 channels
+                        if (elect_one()) {
+                            const CUtensorMap* map = tree ? &map_new : &map_k;
+                            const int y = tree ? problem * a.n_cap : problem * a.T + (s.first + t * kTilePages) * kPage;
+                            mbar_expect_tx(full, (uint32_t)(tree ? a.n_cap : kTok) * kRowBytes);
+                            tma_2d(dst, map, 0, y, full);
+                            tma_2d(dst + kHalf, map, 64, y, full);
+                        }
+                    } else {                             // two copies per page.  (From eight lanes at once they take 1300 cycles.)
+                        const uint32_t pages = __ballot_sync(0xFFFFFFFFu, is_page(id));
+                        if (elect_one()) mbar_expect_tx(full, (uint32_t)__popc(pages) * kPage * kRowBytes);
+                        __syncwarp();
+#pragma unroll
+                        for (int p = 0; p < kTilePages; ++p) {
+                            const int y = problem * a.T + __shfl_sync(0xFFFFFFFFu, id, p) * kPage;
+                            if (((pages >> p) & 1u) && elect_one()) {
+                                tma_2d(dst + p * kPage * 128, &map_k, 0, y, full);
+                                tma_2d(dst + kHalf + p * kPage * 128, &map_k, 64, y, full);
+                            }
+                        }
                     }
                     __syncwarp();
-                    ++seg;
-                }
-            }
-        }
-        if (!ok) give_up();
-        if (*abort_flag) {                           // copies still in flight get one more bounded wait each
-            int none = 0;
-            if (seg > 0) mbar_wait_or_abort(bar(kQFull), (uint32_t)(seg - 1) & 1u, &none, kWaitNs);
-            for (int i = max(0, kc - kKStages); i < kc; ++i)
-                mbar_wait_or_abort(bar(kKFull + i % kKStages), (uint32_t)(i / kKStages) & 1u, &none, kWaitNs);
-        }
-    } else if (warp == 1) {
-        // ---- issuer of S = Q K^T: the warp stays together, an elected lane issues ----------------------------------------
-        constexpr uint32_t id_s = idesc_bf16(kRows, kTok, false);
-        const uint32_t sm = uniform(base), ts = uniform(tmem);
-        const uint64_t dq = smem_desc_128(sm, 16), dk0 = smem_desc_128(sm + kOffK, 16);
-        uint32_t st = 0, phase = 0, seg = 0, buf = 0, turn = 0;      // K stage and its phase; segments; score buffer, its uses so far
-        bool ok = true;
-        while (ok && next(ok)) {
-            const int tiles = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)(s.tile1 - s.tile0));
-            ok = warp_wait(kQFull, seg);
-#pragma unroll 1
-            for (int n = 0; ok && n < tiles; ++n) {
-                // the buffer holds the weights of an earlier tile until their product is through
-                ok = warp_wait(kKFull + st, phase) && (turn == 0 || warp_wait(kOFull + buf, turn - 1u));
-                if (!ok) break;
-                tc_after();
-                const uint64_t dk = dk0 + (uint64_t)(st * (kTile >> 4));
-                if (elect_one()) {
+                    ++kc;
+                    if (++st == (uint32_t)kKStages) { st = 0; phase ^= 1u; }
+                    id = id_next;
+                    id_next = ask(t - 2);
+                    ask_docs(id);
+                    if (q_due) {                         // the queries behind the first keys, which come from farther away
+                        q_due = false;
+                        if (seg > 0) ok = warp_wait(kQEmpty, (uint32_t)(seg - 1));
+                        if (!ok) break;
+                        if (lane == 0) {
+                            mbar_expect_tx(bar(kQFull), q_bytes);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)      // 16 dims = 32 bytes = 2 units; 64 dims = one half tile
-                        tc_mma_ss(ts + buf * kTok, dq + (uint64_t)((k >> 2) * (kQHalf >> 4) + (k & 3) * 2),
-                                  dk + (uint64_t)((k >> 2) * (kHalf >> 4) + (k & 3) * 2), id_s, k != 0);
-                    tc_commit_to(bar(kSFull + buf));
-                    tc_commit_to(bar(kKEmpty + st));
-                    if (n == tiles - 1) tc_commit_to(bar(kQEmpty));
-                }
-                __syncwarp();
-                if (++buf == (uint32_t)kBufs) { buf = 0; ++turn; }
-                if (++st == (uint32_t)kKStages) { st = 0; phase ^= 1u; }
-            }
-            ++seg;
-        }
-        if (!ok) give_up();
-    } else if (warp == 2) {
-        // ---- issuer of O += P V~ ----------------------------------------------------------------------------------------
-        constexpr uint32_t id_o = idesc_bf16(kRows, kHeadDim, true);
-        const uint32_t sm = uniform(base), ts = uniform(tmem), to = ts + kBufs * kTok;
-        const uint64_t dv0 = smem_desc_128(sm + kOffV, kSlot / 2);
-        uint32_t slot = 0, phase = 0, buf = 0, turn = 0;
-        bool ok = true;
-        while (ok && next(ok)) {
-            const int tiles = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)(s.tile1 - s.tile0));
-#pragma unroll 1
-            for (int n = 0; ok && n < tiles; ++n) {
-                const uint32_t next_slot = slot + 1u;                        // (a tile's slots are neighbours)
-                ok = warp_wait(kVFull + slot, phase) && warp_wait(kVFull + next_slot, phase) && warp_wait(kPFull + buf, turn);
-                if (!ok) break;
-                tc_after();
-                const uint64_t dv = dv0 + (uint64_t)(slot * (kSlot >> 4));
-                const uint32_t p = ts + buf * kTok, more = (uint32_t)(n % kFlush != 0);               // else O starts anew
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {    // 16 tokens: 16 rows of 128 bytes; P: 8 columns high, 8 residual
-                        const uint64_t d = dv + (uint64_t)((k >> 2) * (kSlot >> 4) + (k & 3) * (2048 >> 4));
-                        tc_mma_ts(to, p + 16 * k, d, id_o, k ? 1u : more);
-                        tc_mma_ts(to, p + 16 * k + 8, d, id_o, 1);
+                            for (int i = 0; i < kCopies; ++i) {
+                                tma_3d(base + i * R * 128, &map_q, 0, s.hk * a.Gq, s.b * a.n_cap + s.node0, bar(kQFull));
+                                tma_3d(base + kQHalf + i * R * 128, &map_q, 64, s.hk * a.Gq, s.b * a.n_cap + s.node0, bar(kQFull));
+                            }
+                        }
+                        __syncwarp();
+                        ++seg;
                     }
-                    tc_commit_to(bar(kOFull + buf));
-                    tc_commit_to(bar(kVEmpty + slot));
-                    tc_commit_to(bar(kVEmpty + next_slot));
+                }
+            }
+            if (!ok) give_up();
+            if (*abort_flag) {                           // copies still in flight get one more bounded wait each
+                int none = 0;
+                if (seg > 0) mbar_wait_or_abort(bar(kQFull), (uint32_t)(seg - 1) & 1u, &none, kWaitNs);
+                for (int i = max(0, kc - kKStages); i < kc; ++i)
+                    mbar_wait_or_abort(bar(kKFull + i % kKStages), (uint32_t)(i / kKStages) & 1u, &none, kWaitNs);
+            }
+        } else if (warp == 1) {
+            // ---- issuer of S = Q K^T: the warp stays together, an elected lane issues ----------------------------------------
+            constexpr uint32_t id_s = idesc_bf16(kRows, kTok, false);
+            const uint32_t sm = uniform(base), ts = uniform(tmem);
+            const uint64_t dq = smem_desc_128(sm, 16), dk0 = smem_desc_128(sm + kOffK, 16);
+            uint32_t st = 0, phase = 0, seg = 0, buf = 0, turn = 0;      // K stage and its phase; segments; score buffer, its uses so far
+            bool ok = true;
+            while (ok && next(ok)) {
+                const int tiles = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)(s.tile1 - s.tile0));
+                ok = warp_wait(kQFull, seg);
+#pragma unroll 1
+                for (int n = 0; ok && n < tiles; ++n) {
+                    // the buffer holds the weights of an earlier tile until their product is through
+                    ok = warp_wait(kKFull + st, phase) && (turn == 0 || warp_wait(kOFull + buf, turn - 1u));
+                    if (!ok) break;
+                    tc_after();
+                    const uint64_t dk = dk0 + (uint64_t)(st * (kTile >> 4));
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)      // 16 dims = 32 bytes = 2 units; 64 dims = one half tile
+                            tc_mma_ss(ts + buf * kTok, dq + (uint64_t)((k >> 2) * (kQHalf >> 4) + (k & 3) * 2),
+                                      dk + (uint64_t)((k >> 2) * (kHalf >> 4) + (k & 3) * 2), id_s, k != 0);
+                        tc_commit_to(bar(kSFull + buf));
+                        tc_commit_to(bar(kKEmpty + st));
+                        if (n == tiles - 1) tc_commit_to(bar(kQEmpty));
+                    }
+                    __syncwarp();
+                    if (++buf == (uint32_t)kBufs) { buf = 0; ++turn; }
+                    if (++st == (uint32_t)kKStages) { st = 0; phase ^= 1u; }
+                }
+                ++seg;
+            }
+            if (!ok) give_up();
+        } else if (warp == 2) {
+            // ---- issuer of O += P V~ ----------------------------------------------------------------------------------------
+            constexpr uint32_t id_o = idesc_bf16(kRows, kHeadDim, true);
+            const uint32_t sm = uniform(base), ts = uniform(tmem), to = ts + kBufs * kTok;
+            const uint64_t dv0 = smem_desc_128(sm + kOffV, kSlot / 2);
+            uint32_t slot = 0, phase = 0, buf = 0, turn = 0;
+            bool ok = true;
+            while (ok && next(ok)) {
+                const int tiles = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)(s.tile1 - s.tile0));
+#pragma unroll 1
+                for (int n = 0; ok && n < tiles; ++n) {
+                    const uint32_t next_slot = slot + 1u;                        // (a tile's slots are neighbours)
+                    ok = warp_wait(kVFull + slot, phase) && warp_wait(kVFull + next_slot, phase) && warp_wait(kPFull + buf, turn);
+                    if (!ok) break;
+                    tc_after();
+                    const uint64_t dv = dv0 + (uint64_t)(slot * (kSlot >> 4));
+                    const uint32_t p = ts + buf * kTok, more = (uint32_t)(n % kFlush != 0);               // else O starts anew
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {    // 16 tokens: 16 rows of 128 bytes; P: 8 columns high, 8 residual
+                            const uint64_t d = dv + (uint64_t)((k >> 2) * (kSlot >> 4) + (k & 3) * (2048 >> 4));
+                            tc_mma_ts(to, p + 16 * k, d, id_o, k ? 1u : more);
+                            tc_mma_ts(to, p + 16 * k + 8, d, id_o, 1);
+                        }
+                        tc_commit_to(bar(kOFull + buf));
+                        tc_commit_to(bar(kVEmpty + slot));
+                        tc_commit_to(bar(kVEmpty + next_slot));
+                    }
+                    __syncwarp();
+                    if (++buf == (uint32_t)kBufs) { buf = 0; ++turn; }
+                    slot += 2;
+                    if (slot == (uint32_t)kVSlots) { slot = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok) give_up();
+        } else if (warp == 3) {
+            // ---- scheduler: walks the CTA's range, segment by segment; and, behind each, the ancestors of its nodes as bit masks
+            bool ok = true;
+            int x = x_begin, p = p_first, off = x_first;
+            uint32_t made = 0;                           // tables
+#pragma unroll 1
+            for (int i = 0; ok; ++i) {
+                Segment g = {};
+                g.tile1 = -1;
+#pragma unroll 1
+                while (x < x_end) {
+                    g.b = (int)((uint32_t)p / (uint32_t)a.Hkv);
+                    g.hk = p - g.b * a.Hkv;
+                    g.len = clamp_len(a.seq_len, g.b, a.T);
+                    g.nodes = nodes_of(a, g.b);
+                    pages_of(a, p, g.len, g.list, g.first);
+                    const Unit u = unit_of(a, g.nodes, g.list);
+                    if (off >= u.tiles * u.blocks) {
+                        off -= u.tiles * u.blocks;
+                        ++p;
+                        continue;
+                    }
+                    const int blk = (int)((uint32_t)off / (uint32_t)u.tiles);
+                    g.tile0 = off - blk * u.tiles;
+                    g.tile1 = min(u.tiles, g.tile0 + (x_end - x));
+                    g.node0 = blk * a.block_nodes;
+                    // a CTA continues at most one unit (slot 0) and leaves at most one that it begins (slot 1)
+                    g.slot = g.tile1 - g.tile0 == u.tiles ? -1 : 2 * (int)blockIdx.x + (g.tile0 == 0 ? 1 : 0);
+                    x += g.tile1 - g.tile0;
+                    off += g.tile1 - g.tile0;
+                    break;
+                }
+                if (i >= kSegs) ok = warp_wait(kSegEmpty + i % kSegs, (uint32_t)(i / kSegs - 1));
+                if (!ok) break;
+                if (lane == 0) {
+                    volatile int* e = segs + (i % kSegs) * 12;
+                    e[0] = g.b; e[1] = g.hk; e[2] = g.node0; e[3] = g.nodes; e[4] = g.len; e[5] = g.list; e[6] = g.first;
+                    e[7] = g.tile0; e[8] = g.tile1; e[9] = g.slot;
+                    mbar_arrive(bar(kSegFull + i % kSegs));
                 }
                 __syncwarp();
-                if (++buf == (uint32_t)kBufs) { buf = 0; ++turn; }
-                slot += 2;
-                if (slot == (uint32_t)kVSlots) { slot = 0; phase ^= 1u; }
-            }
-        }
-        if (!ok) give_up();
-    } else if (warp == 3) {
-        // ---- scheduler: walks the CTA's range, segment by segment; and, behind each, the ancestors of its nodes as bit masks
-        bool ok = true;
-        int x = x_begin, p = p_first, off = x_first;
-        uint32_t made = 0;                           // tables
-#pragma unroll 1
-        for (int i = 0; ok; ++i) {
-            Segment g = {};
-            g.tile1 = -1;
-#pragma unroll 1
-            while (x < x_end) {
-                g.b = (int)((uint32_t)p / (uint32_t)a.Hkv);
-                g.hk = p - g.b * a.Hkv;
-                g.len = clamp_len(a.seq_len, g.b, a.T);
-                g.nodes = nodes_of(a, g.b);
-                pages_of(a, p, g.len, g.list, g.first);
-                const Unit u = unit_of(a, g.nodes, g.list);
-                if (off >= u.tiles * u.blocks) {
-                    off -= u.tiles * u.blocks;
-                    ++p;
-                    continue;
-                }
-                const int blk = (int)((uint32_t)off / (uint32_t)u.tiles);
-                g.tile0 = off - blk * u.tiles;
-                g.tile1 = min(u.tiles, g.tile0 + (x_end - x));
-                g.node0 = blk * a.block_nodes;
-                // a CTA continues at most one unit (slot 0) and leaves at most one that it begins (slot 1)
-                g.slot = g.tile1 - g.tile0 == u.tiles ? -1 : 2 * (int)blockIdx.x + (g.tile0 == 0 ? 1 : 0);
-                x += g.tile1 - g.tile0;
-                off += g.tile1 - g.tile0;
-                break;
-            }
-            if (i >= kSegs) ok = warp_wait(kSegEmpty + i % kSegs, (uint32_t)(i / kSegs - 1));
-            if (!ok) break;
-            if (lane == 0) {
-                volatile int* e = segs + (i % kSegs) * 12;
-                e[0] = g.b; e[1] = g.hk; e[2] = g.node0; e[3] = g.nodes; e[4] = g.len; e[5] = g.list; e[6] = g.first;
-                e[7] = g.tile0; e[8] = g.tile1; e[9] = g.slot;
-                mbar_arrive(bar(kSegFull + i % kSegs));
-            }
-            __syncwarp();
-            if (g.tile1 < 0) break;
-            if (!MASK && (g.tile1 - 1) * kTilePages < g.list) continue;      // nobody asks for the tree
-            int up[4];
-            uint32_t m[4][4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int node = k * 32 + lane;
-                up[k] = -1;
-                if (node < g.nodes) {
-                    up[k] = a.parent ? a.parent[(size_t)g.b * a.n_cap + node] : node - 1;
-                    if (up[k] < 0 || up[k] >= node) up[k] = -1;
-                }
-#pragma unroll
-                for (int w = 0; w < 4; ++w) m[k][w] = w == k ? 1u << lane : 0u;
-            }
-            if (made > 0) ok = warp_wait(kTabEmpty, made - 1);
-            if (!ok) break;
-            // each node's mask holds the node and its ancestors up to the one `up` points at, twice as many each time
-            uint4* const table = reinterpret_cast<uint4*>(kin);
-#pragma unroll 1
-            for (;;) {
-                bool going = false;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    table[k * 32 + lane] = make_uint4(m[k][0], m[k][1], m[k][2], m[k][3]);
-                    going |= up[k] >= 0;
-                }
-                __syncwarp();
-                if (!__any_sync(0xFFFFFFFFu, going)) break;
-                int next_up[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    // the node that `up` points at: its mask, and where its pointer goes (held by its lane)
-                    const uint4 t = table[max(up[k], 0)];
-                    int to[4];
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) to[w] = __shfl_sync(0xFFFFFFFFu, up[w], max(up[k], 0) & 31);
-                    const int which = max(up[k], 0) >> 5;
-                    next_up[k] = up[k] < 0 ? -1 : which == 0 ? to[0] : which == 1 ? to[1] : which == 2 ? to[2] : to[3];
-                    if (up[k] >= 0) { m[k][0] |= t.x; m[k][1] |= t.y; m[k][2] |= t.z; m[k][3] |= t.w; }
-                }
-                __syncwarp();
-#pragma unroll
-                for (int k = 0; k < 4; ++k) up[k] = next_up[k];
-            }
-            if constexpr (MASK) {
+                if (g.tile1 < 0) break;
+                if (!MASK && (g.tile1 - 1) * kTilePages < g.list) continue;      // nobody asks for the tree
+                int up[4];
+                uint32_t m[4][4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int node = k * 32 + lane;
-                    const int depth = __popc(m[k][0]) + __popc(m[k][1]) + __popc(m[k][2]) + __popc(m[k][3]) - 1;
-                    node_pos[node] = a.sc.q_pos && node < g.nodes ? a.sc.q_pos[(size_t)g.b * a.n_cap + node] : g.len + depth;
+                    up[k] = -1;
+                    if (node < g.nodes) {
+                        up[k] = a.parent ? a.parent[(size_t)g.b * a.n_cap + node] : node - 1;
+                        if (up[k] < 0 || up[k] >= node) up[k] = -1;
+                    }
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) m[k][w] = w == k ? 1u << lane : 0u;
                 }
+                if (made > 0) ok = warp_wait(kTabEmpty, made - 1);
+                if (!ok) break;
+                // each node's mask holds the node and its ancestors up to the one `up` points at, twice as many each time
+                uint4* const table = reinterpret_cast<uint4*>(kin);
+#pragma unroll 1
+                for (;;) {
+                    bool going = false;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        table[k * 32 + lane] = make_uint4(m[k][0], m[k][1], m[k][2], m[k][3]);
+                        going |= up[k] >= 0;
+                    }
+                    __syncwarp();
+                    if (!__any_sync(0xFFFFFFFFu, going)) break;
+                    int next_up[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        // the node that `up` points at: its mask, and where its pointer goes (held by its lane)
+                        const uint4 t = table[max(up[k], 0)];
+                        int to[4];
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) to[w] = __shfl_sync(0xFFFFFFFFu, up[w], max(up[k], 0) & 31);
+                        const int which = max(up[k], 0) >> 5;
+                        next_up[k] = up[k] < 0 ? -1 : which == 0 ? to[0] : which == 1 ? to[1] : which == 2 ? to[2] : to[3];
+                        if (up[k] >= 0) { m[k][0] |= t.x; m[k][1] |= t.y; m[k][2] |= t.z; m[k][3] |= t.w; }
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) up[k] = next_up[k];
+                }
+                if constexpr (MASK) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int node = k * 32 + lane;
+                        const int depth = __popc(m[k][0]) + __popc(m[k][1]) + __popc(m[k][2]) + __popc(m[k][3]) - 1;
+                        node_pos[node] = a.sc.q_pos && node < g.nodes ? a.sc.q_pos[(size_t)g.b * a.n_cap + node] : g.len + depth;
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kTabFull));
+                ++made;
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kTabFull));
-            ++made;
+            if (!ok) give_up();
         }
-        if (!ok) give_up();
     } else if (warp < 12) {
-        // ---- softmax: thread = row; the two warps of a quarter have 64 of a tile's 128 tokens each ------------------------
-        const int grp = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane, c0 = 64 * grp;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        // ---- softmax: thread = a row and kCols of a tile's 128 tokens: a lane has 64 of them in each of its two warps, a copy its
+        // part of those and zeros elsewhere -----------------------------------------------------------------------------
+        const int grp = (warp - 4) >> 2, quarter = warp & 3, place = quarter * 32 + lane, row = place % R, copy = place / R;
+        const int half = 64 * grp, c0 = half + copy * kCols;     // first token; half: first channel of those that this warp looks after
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), to = lanes + kBufs * kTok;
-        float4* const my_flush = a.flush + (size_t)blockIdx.x * 32 * kRows + row;
         uint32_t buf = 0, turn = 0, last_buf = 0, last_turn = 0, ring = 0;   // score buffer and its uses so far, of the tile before too
         uint32_t pairs = 0, tabs = 0;
         bool ok = true;
-        // what the warps of a quarter tell each other, a number per row
-        auto exchange = [&](float mine, float& other) {
-            float* const place = told + (pairs & 1u) * 2 * kRows;
-            place[grp * kRows + row] = mine;
+        // what the warps that share rows tell each other, a number per row
+        constexpr int kTold = 2 * kCopies;
+        auto exchange = [&](float mine, float (&all)[kTold]) {
+            float* const board = told + (pairs & 1u) * 2 * kRows;
+            board[(grp * kCopies + copy) * R + row] = mine;
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kPair + quarter));
-            if (!warp_wait(kPair + quarter, pairs++)) return false;
-            other = place[(grp ^ 1) * kRows + row];
+            if (lane == 0) mbar_arrive(bar(kPair + quarter % (R / 32)));
+            if (!warp_wait(kPair + quarter % (R / 32), pairs++)) return false;
+#pragma unroll
+            for (int i = 0; i < kTold; ++i) all[i] = board[i * R + row];
             return true;
         };
         auto step = [&]() {
@@ -555,7 +572,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 
         auto segment = [&]() {
             const int live = min(a.block_nodes, s.nodes - s.node0) * a.Gq;    // rows of the block
-            const bool mine = row < live, warp_live = quarter * 32 < live;
+            const bool mine = row < live, warp_live = quarter * 32 % R < live;
             const int tiles = s.tile1 - s.tile0;
             const bool tables = MASK || is_tree(s.tile1 - 1);
             const uint32_t in_block = ((uint32_t)row * a.gq_inv) >> 16;
@@ -568,7 +585,10 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 p = node_pos[node];
                 if (SCORE && a.sc.slopes && mine) slope2 = a.sc.slopes[s.hk * a.Gq + h] * kLog2e;
             }
-            float m = -INFINITY, l = 0.f, m_flush = -INFINITY;
+            float m = -INFINITY, l = 0.f, m_sums = -INFINITY;
+            float sums[64];                          // the channels of half: sums of emptied accumulators, relative to m_sums
+#pragma unroll
+            for (int i = 0; i < 64; ++i) sums[i] = 0.f;
 #pragma unroll 1
             for (int n = 0; n < tiles; ++n, step()) {
                 const int t = s.tile1 - 1 - n;
@@ -578,7 +598,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     if (lane == 0) mbar_arrive(bar(kPFull + buf));
                     continue;
                 }
-                const uint32_t ts = lanes + buf * kTok + c0;
+                const uint32_t ts = lanes + buf * kTok + c0, word0 = (uint32_t)c0 >> 5, shift = (uint32_t)c0 & 31u;
                 auto last_product = [&]() {          // the product of the tile before is through
                     const bool good = warp_wait(kOFull + last_buf, last_turn);
                     tc_after();
@@ -586,32 +606,33 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 };
                 tc_after();
                 // tokens that the row sees: those that there are, in the tree its ancestors, and the window's
-                uint32_t see[2];
+                constexpr int kWords = kCols == 64 ? 2 : 1;
+                uint32_t see[kWords];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) see[i] = valid_tokens[ring * 4 + 2 * grp + i];
+                for (int i = 0; i < kWords; ++i) see[i] = valid_tokens[ring * 4 + word0 + i] >> shift;
                 const bool tree = is_tree(t);
                 if (tree) {
                     if (!MASK) {
                         ok = warp_wait(kTabFull, tabs);
                         if (!ok) return;
                     }
-                    const uint2 k = reinterpret_cast<const uint2*>(kin)[node * 2 + grp];
-                    see[0] &= k.x; see[1] &= k.y;
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) see[i] &= kin[node * 4 + word0 + i] >> shift;
                 }
                 if constexpr (MASK) {
                     if (tree) {
 #pragma unroll 1
-                        for (int i = 0; i < min(64, s.nodes - c0); ++i) {
+                        for (int i = 0; i < min(kCols, s.nodes - c0); ++i) {
                             const int at_i = node_pos[c0 + i];
                             if (at_i > p || (uint32_t)p - (uint32_t)at_i >= a.window) {
                                 if (i < 32) see[0] &= ~(1u << i);
-                                else see[1] &= ~(1u << (i - 32));
+                                else see[kWords - 1] &= ~(1u << (i - 32));
                             }
                         }
                     } else if (a.sc.q_pos || a.sc.window > 0) {
 #pragma unroll
-                        for (int i = 0; i < kTilePages / 2; ++i) {            // of a page's 16 tokens the bits [lo, hi)
-                            const int t0 = tile_pages[ring * kTilePages + kTilePages / 2 * grp + i] * kPage;
+                        for (int i = 0; i < kCols / kPage; ++i) {             // of a page's 16 tokens the bits [lo, hi)
+                            const int t0 = tile_pages[ring * kTilePages + c0 / kPage + i] * kPage;
                             const long long ahead = (long long)p - t0;        // distance of its first token
                             const int hi = (int)min(max(ahead + 1, 0LL), 16LL), lo = (int)min(max(ahead + 1 - (long long)a.window, 0LL), 16LL);
                             const uint32_t bits = ((1u << hi) - 1u) & ~((1u << lo) - 1u);
@@ -619,39 +640,41 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         }
                     }
                 }
-                const bool open = __all_sync(0xFFFFFFFFu, !mine || (see[0] & see[1]) == 0xFFFFFFFFu);
+                constexpr uint32_t kAll = kCols >= 32 ? 0xFFFFFFFFu : (1u << kCols % 32) - 1u;       // the tokens of a word
+                const bool open = __all_sync(0xFFFFFFFFu, !mine || (see[0] & see[kWords - 1] & kAll) == kAll);
                 const bool empty_now = n > 0 && n % kFlush == 0;
                 const float m_acc = m;               // maximum the accumulator was built with
                 // maximum of the tile; scores that are not raw products times a positive scale, or hidden, are written back
                 float top = -INFINITY;
+                constexpr int kStep = kCols < 32 ? kCols : 32;
 #pragma unroll 1
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t r[32];
-                    tmem_ld16<0>(ts + 32 * c, r);
-                    tmem_ld16<16>(ts + 32 * c + 16, r);
+                for (int c = 0; c < kCols; c += kStep) {
+                    uint32_t r[kStep];
+                    tmem_ld16<0>(ts + c, r);
+                    if constexpr (kStep > 16) tmem_ld16<16>(ts + c + 16, r);
                     tmem_wait_ld();
-                    const uint32_t bits = c ? see[1] : see[0];
+                    const uint32_t bits = c ? see[kWords - 1] : see[0];
                     if constexpr (SCORE) {
                         if (a.cap_in != 0.f) {
                             // (what a row does not see, and lanes without a row, have no say in how the others are capped)
-                            const bool all = __all_sync(0xFFFFFFFFu, bits == 0xFFFFFFFFu || !mine);
+                            const bool all = __all_sync(0xFFFFFFFFu, (bits & kAll) == kAll || !mine);
                             if (all && __all_sync(0xFFFFFFFFu, (mine ? magnitude(r) : 0.f) * fabsf(a.cap_in) <= kCapSmall))
                                 cap_scores_low(r, a.cap_in, a.scale_log2);
                             else
                                 cap_scores_any(r, a.cap_in, a.cap_log2);
                         } else {
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * a.scale_log2);
+                            for (int i = 0; i < kStep; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * a.scale_log2);
                         }
                         if (a.sc.slopes) {
                             if (tree) {
 #pragma unroll
-                                for (int i = 0; i < 32; ++i)
-                                    r[i] = __float_as_uint(fmaf(slope2, (float)(node_pos[c0 + 32 * c + i] - p), __uint_as_float(r[i])));
+                                for (int i = 0; i < kStep; ++i)
+                                    r[i] = __float_as_uint(fmaf(slope2, (float)(node_pos[c0 + c + i] - p), __uint_as_float(r[i])));
                             } else {
 #pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    const float far = (float)(tile_pages[ring * kTilePages + kTilePages / 2 * grp + 2 * c + e] * kPage - p);
+                                for (int e = 0; e < kStep / kPage; ++e) {
+                                    const float far = (float)(tile_pages[ring * kTilePages + (c0 + c) / kPage + e] * kPage - p);
 #pragma unroll
                                     for (int i = 0; i < 16; i += 2) {
                                         const float2 x = fma2(both(slope2), add2(both(far), make_float2((float)i, (float)(i + 1))),
@@ -665,28 +688,32 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     }
                     if (!open) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
+                        for (int i = 0; i < kStep; ++i)
                             if (!((bits >> i) & 1u)) r[i] = __float_as_uint(-INFINITY);
                     }
                     float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2)
+                    for (int i = 0; i < kStep; i += 2)
                         t4[(i >> 1) & 3] = fmaxf(fmaxf(t4[(i >> 1) & 3], __uint_as_float(r[i])), __uint_as_float(r[i + 1]));
+                    __syncwarp();
                     top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
                     if (SCORE || !open) {
-                        uint32_t lo[16], hi[16];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) { lo[i] = r[i]; hi[i] = r[16 + i]; }
-                        tmem_st16(ts + 32 * c, lo);
-                        tmem_st16(ts + 32 * c + 16, hi);
+                        for (int e = 0; e < kStep; e += 16) {
+                            uint32_t o[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = r[e + i];
+                            tmem_st16(ts + c + e, o);
+                        }
                     }
                 }
                 if (SCORE || !open) tmem_wait_st();
                 if (!SCORE) top *= a.scale_log2;     // (-inf stays -inf: the scale is positive)
-                float other = -INFINITY;
-                ok = exchange(top, other);
+                float all_tops[kTold];
+                ok = exchange(top, all_tops);
                 if (!ok) return;
-                top = fmaxf(top, other);
+#pragma unroll
+                for (int i = 0; i < kTold; ++i) top = fmaxf(top, all_tops[i]);
                 // move the maximum only if it is exceeded by much; the accumulator follows (half of its channels here, half there)
                 const bool move = mine && (top > m + kSlack || (m == -INFINITY && top > -INFINITY));
                 if (__any_sync(0xFFFFFFFFu, move)) {
@@ -696,7 +723,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         ok = last_product();
                         if (!ok) return;
 #pragma unroll 1
-                        for (int c = c0; c < c0 + 64; c += 16) {
+                        for (int c = half; c < half + 64; c += 16) {
                             uint32_t q[16];
                             tmem_ld16(to + c, q);
                             tmem_wait_ld();
@@ -707,39 +734,32 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     }
                     m = to_m;
                 }
-                // the accumulator is emptied into fp32 sums, relative to m_flush; the issuer starts it anew
+                // the accumulator is emptied into the sums; the issuer starts it anew
                 if (empty_now) {
                     ok = last_product();
                     if (!ok) return;
-                    const float keep = m_flush == -INFINITY ? 0.f : ex2(m_flush - m_acc);
-#pragma unroll 1
-                    for (int c = c0; c < c0 + 64; c += 16) {
-                        float4 old[4];
+                    const float keep = m_sums == -INFINITY ? 0.f : ex2(m_sums - m_acc);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            old[i] = n > kFlush ? __ldcg(my_flush + (size_t)(c / 4 + i) * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int c = 0; c < 64; c += 16) {
                         uint32_t q[16];
-                        tmem_ld16(to + c, q);
+                        tmem_ld16(to + half + c, q);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            __stcg(my_flush + (size_t)(c / 4 + i) * kRows,
-                                   make_float4(fmaf(old[i].x, keep, __uint_as_float(q[4 * i])), fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1])),
-                                               fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2])), fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3]))));
+                        for (int i = 0; i < 16; ++i) sums[c + i] = fmaf(sums[c + i], keep, __uint_as_float(q[i]));
                     }
-                    m_flush = m_acc;
+                    m_sums = m_acc;
                 }
                 // weights, their sum, and P over S: per 16 tokens 8 columns of bf16 pairs high, 8 residual
                 const float ref = m == -INFINITY ? 0.f : m;
                 float2 la = make_float2(0.f, 0.f), lb = la;
 #pragma unroll 1
-                for (int c = 0; c < 64; c += 32) {
-                    uint32_t r[32];
+                for (int c = 0; c < kCols; c += kStep) {
+                    uint32_t r[kStep];
                     tmem_ld16<0>(ts + c, r);
-                    tmem_ld16<16>(ts + c + 16, r);
+                    if constexpr (kStep > 16) tmem_ld16<16>(ts + c + 16, r);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int e = 0; e < 32; e += 16) {
+                    for (int e = 0; e < kStep; e += 16) {
                         uint32_t o[16];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
@@ -758,6 +778,13 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         tmem_st16(ts + c + e, o);
                     }
                 }
+                if constexpr (kCopies > 1) {         // the tokens of the other copies
+                    uint32_t zero[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) zero[i] = 0u;
+#pragma unroll
+                    for (int c = kCols; c < 64; c += 16) tmem_st16(lanes + buf * kTok + half + ((copy * kCols + c) & 63), zero);
+                }
                 l += (la.x + lb.x) + (la.y + lb.y);
                 tmem_wait_st();
                 tc_before();
@@ -769,33 +796,56 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (!ok) return;
             tc_after();
             if (warp_live) {
-                float other = 0.f;
-                ok = exchange(l, other);
+                float told_sums[kTold];
+                ok = exchange(l, told_sums);
                 if (!ok) return;
-                l += other;
+                l = 0.f;
+#pragma unroll
+                for (int i = 0; i < kTold; ++i) l += told_sums[i];
                 const bool whole = s.slot < 0;
                 const size_t at = ((size_t)s.b * a.n_cap + node) * a.Hq + s.hk * a.Gq + h;
-                if (grp == 0 && mine) {
+                if (grp == 0 && copy == 0 && mine) {
                     if (!whole) a.part_ml[(size_t)s.slot * kRows + row] = make_float2(m, l);
                     else if (a.lse) a.lse[at] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
                 }
+                __syncwarp();
                 const float f = !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;     // (0: nothing seen, whatever was summed)
-                const float keep = f * (m_flush == -INFINITY ? 0.f : ex2(m_flush - m));
-                float4* dst = reinterpret_cast<float4*>(whole ? a.out + at * kHeadDim : a.part_o + ((size_t)s.slot * kRows + row) * kHeadDim);
+                const float keep = f * (m_sums == -INFINITY ? 0.f : ex2(m_sums - m));
+                // the copies of a row are added up where their CTA finishes it, or by the second kernel
+                const bool aside = whole && copy > 0;
+                float4* const to_lane = a.part_o + (size_t)(whole ? 2 * (int)gridDim.x + (int)blockIdx.x : s.slot) * 32 * kRows + row;
+                float4* const to_row = reinterpret_cast<float4*>(a.out + at * kHeadDim);
 #pragma unroll 1
-                for (int c = c0; c < c0 + 64; c += 16) {
-                    float4 old[4];
+                for (int pass = 0; pass < (kCopies > 1 && whole ? 2 : 1); ++pass) {
+                    if (pass == (kCopies > 1 && whole && !aside ? 1 : 0)) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        old[i] = tiles > kFlush ? __ldcg(my_flush + (size_t)(c / 4 + i) * kRows) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    uint32_t q[16];
-                    tmem_ld16(to + c, q);
-                    tmem_wait_ld();
+                        for (int c = 0; c < 64; c += 16) {
+                            uint32_t q[16];
+                            __syncwarp();
+                            tmem_ld16(to + half + c, q);
+                            tmem_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float4 v = make_float4(fmaf(old[i].x, keep, __uint_as_float(q[4 * i]) * f), fmaf(old[i].y, keep, __uint_as_float(q[4 * i + 1]) * f),
-                                                     fmaf(old[i].z, keep, __uint_as_float(q[4 * i + 2]) * f), fmaf(old[i].w, keep, __uint_as_float(q[4 * i + 3]) * f));
-                        if (mine) __stcg(dst + c / 4 + i, f != 0.f ? v : make_float4(0.f, 0.f, 0.f, 0.f));
+                            for (int i = 0; i < 4; ++i) {
+                                const int at4 = half / 4 + c / 4 + i;
+                                float* const x = sums + c + 4 * i;
+                                float4 v = make_float4(fmaf(__uint_as_float(q[4 * i]), f, x[0] * keep), fmaf(__uint_as_float(q[4 * i + 1]), f, x[1] * keep),
+                                                       fmaf(__uint_as_float(q[4 * i + 2]), f, x[2] * keep), fmaf(__uint_as_float(q[4 * i + 3]), f, x[3] * keep));
+                                if (kCopies > 1 && whole && !aside) {
+#pragma unroll
+                                    for (int k = 1; k < kCopies; ++k) {
+                                        const float4 w = __ldcg(to_lane + (size_t)at4 * kRows + k * R);
+                                        v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+                                    }
+                                }
+                                if (f == 0.f) v = make_float4(0.f, 0.f, 0.f, 0.f);
+                                if (mine) __stcg(whole && !aside ? to_row + at4 : to_lane + (size_t)at4 * kRows + copy * R, v);
+                            }
+                        }
+                    }
+                    if (kCopies > 1 && whole) {      // the other copies' parts are there; later, they may be written anew
+                        __threadfence();
+                        ok = exchange(0.f, told_sums);
+                        if (!ok) return;
                     }
                 }
                 tc_before();
@@ -808,6 +858,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         while (ok && next(ok)) segment();
         if (!ok) give_up();
     } else {
+        fewer_registers();
         // ---- value tiles: packed groups -> swizzled rows -------------------------------------------------------
         // A warp takes 32 tokens (two pages) of every tile.  LPT neighbouring lanes copy 16-byte chunks of one token (a whole group of
         // 32 or 64 bytes; two groups of 16), so a token's mask stays with its lanes and the place of a kept group is a
@@ -944,19 +995,19 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     }
 }
 
-// Joins the partials of units that more than one CTA worked on, in CTA order: block = node of a (sequence, KV head), warp = query head,
-// lane = four channels.  Checks the trees and gathers the CTAs' status on the side.  Short on purpose: it runs once, from
+// Joins the partials of units that more than one CTA worked on, in CTA order: block = 8 rows of a block of a (sequence, KV head).
+// Checks the trees and gathers the CTAs' status on the side.  Short on purpose: it runs once, from
 // cold instruction memory.
 __global__ void __launch_bounds__(256)
-tree_join_kernel(const TreeArgs a, int rows, int grid) {
+tree_join_kernel(const TreeArgs a, int grid) {
     // launched while the first kernel still runs: the call's own inputs are read before the wait
-    const int problem = blockIdx.x, node = blockIdx.y, h = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int problem = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int b = (int)((uint32_t)problem / (uint32_t)a.Hkv), hk = problem - b * a.Hkv;
     const int nodes = nodes_of(a, b);
-    int list, first;
-    pages_of(a, problem, clamp_len(a.seq_len, b, a.T), list, first);
+    int list, first_page;
+    pages_of(a, problem, clamp_len(a.seq_len, b, a.T), list, first_page);
     const Unit u = unit_of(a, nodes, list);
-    if (node == 0 && hk == 0 && h == 0) {
+    if (blockIdx.y == 0 && hk == 0 && warp == 0) {
         bool bad = false;
 #pragma unroll 1
         for (int i = lane; i < nodes && a.parent; i += 32) {
@@ -966,44 +1017,49 @@ tree_join_kernel(const TreeArgs a, int rows, int grid) {
         bad = __any_sync(0xFFFFFFFFu, bad);
         if (lane == 0) a.status[b] = bad ? STC_ERR_INVALID_ARG : STC_OK;
     }
-    const int blk = (int)((uint32_t)node / (uint32_t)a.block_nodes);
+    // warp = 8 rows of a block and 4 chunks of 4 channels: the partials are read in 128 bytes, the rows written in 64
+    const int eights = a.rows / 8, blk = (int)((uint32_t)blockIdx.y / (uint32_t)eights);
+    const int in_block = ((int)blockIdx.y - blk * eights) * 8 + (lane & 7), chunk = warp * 4 + (lane >> 3);
+    const int node_in = (int)(((uint32_t)in_block * a.gq_inv) >> 16), node = blk * a.block_nodes + node_in, h = in_block - node_in * a.Gq;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (problem == 0 && node == 0 && h == 0) {
+    if (problem == 0 && blockIdx.y == 0 && warp == 0) {
         int st = 0;
 #pragma unroll 1
         for (int c = lane; c < grid; c += 32) st = max(st, a.cta_status[c]);
         st = __reduce_max_sync(0xFFFFFFFFu, st);
         if (lane == 0) *a.word = st;
     }
-    if (node >= nodes) return;
+    if (node_in >= a.block_nodes || node >= nodes) return;
     const Cut cut(a.base[a.problems], grid);
     const int x0 = a.base[problem] + blk * u.tiles, c0 = cut.owner(x0), c1 = cut.owner(x0 + u.tiles - 1);
     if (c0 == c1) return;                            // finished where it was computed
-    const int in_block = (node - blk * a.block_nodes) * a.Gq + h;
     const size_t row = ((size_t)b * a.n_cap + node) * a.Hq + hk * a.Gq + h;
+    constexpr int kAtOnce = 8;                       // loads in flight
+    const int copies_log2 = __ffs(kRows / a.rows) - 1, parts = (c1 - c0 + 1) << copies_log2;
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-    for (int c = c0; c <= c1; c += 4) {              // four loads in flight
-        float2 p[4];
-        float4 v[4];
+    for (int first = 0; first < parts; first += kAtOnce) {
+        float2 p[kAtOnce];
+        float4 v[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int e = min(c + i, c1);
-            const size_t at = (size_t)(2 * e + (e == c0 ? 1 : 0)) * rows + in_block;
-            p[i] = __ldcg(a.part_ml + at);
-            v[i] = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * kHeadDim) + lane);
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int j = min(first + i, parts - 1), e = c0 + (j >> copies_log2), copy = j & ((1 << copies_log2) - 1);
+            const size_t at = (size_t)(2 * e + (e == c0 ? 1 : 0));
+            p[i] = __ldcg(a.part_ml + at * kRows + in_block);
+            if (copy) p[i].y = 0.f;                  // the row's sum is told once
+            v[i] = __ldcg(a.part_o + (at * 32 + chunk) * kRows + copy * a.rows + in_block);
         }
         float top = m;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (c + i > c1) p[i] = make_float2(-INFINITY, 0.f);
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (first + i >= parts) p[i] = make_float2(-INFINITY, 0.f);
             top = fmaxf(top, p[i].x);
         }
         const float fm = m == -INFINITY ? 0.f : ex2(m - top);
         l *= fm; o.x *= fm; o.y *= fm; o.z *= fm; o.w *= fm;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kAtOnce; ++i) {
             if (p[i].x == -INFINITY) {               // nothing seen: its sum is 0, or NaN
                 l += p[i].y;
                 continue;
@@ -1017,8 +1073,8 @@ tree_join_kernel(const TreeArgs a, int rows, int grid) {
     const float inv = l != 0.f ? 1.f / l : 0.f;
     float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
     if (inv != 0.f) r = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    reinterpret_cast<float4*>(a.out)[row * 32 + lane] = r;
-    if (a.lse && lane == 0) a.lse[row] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+    reinterpret_cast<float4*>(a.out)[row * 32 + chunk] = r;
+    if (a.lse && chunk == 0) a.lse[row] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -1026,12 +1082,23 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // The workspace has to be sized without a device, so the partial slots are counted for this many CTAs.
 constexpr int kPlanSms = 148;
 
-template <bool MASK, bool SCORE>
+template <int R, bool MASK, bool SCORE>
 cudaError_t launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& fresh, const TreeArgs& a, int n_cta, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<MASK, SCORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<R, MASK, SCORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
     if (e != cudaSuccess) return e;
-    tree_attn_kernel<MASK, SCORE><<<n_cta, kThreads, kSmem, st>>>(q, k, fresh, a);
+    cudaFuncAttributes f;                            // (a launch with fewer registers would wait for them without end)
+    e = cudaFuncGetAttributes(&f, tree_attn_kernel<R, MASK, SCORE>);
+    if (e != cudaSuccess) return e;
+    if (f.numRegs * kThreads < 256 * kSoftmaxRegs + 256 * kOtherRegs) return cudaErrorInvalidConfiguration;
+    tree_attn_kernel<R, MASK, SCORE><<<n_cta, kThreads, kSmem, st>>>(q, k, fresh, a);
     return cudaGetLastError();
+}
+
+template <int R>
+cudaError_t launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& fresh, const TreeArgs& a, int n_cta, bool masked, bool scored,
+                   cudaStream_t st) {
+    return scored ? launch<R, true, true>(q, k, fresh, a, n_cta, st)
+           : masked ? launch<R, true, false>(q, k, fresh, a, n_cta, st) : launch<R, false, false>(q, k, fresh, a, n_cta, st);
 }
 
 }  // namespace
@@ -1060,23 +1127,27 @@ cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tr
     w += align256(((size_t)g.problems + 1) * 4);
     a.part_ml = reinterpret_cast<float2*>(w);
     w += 2 * (size_t)kPlanSms * kRows * 8;
-    a.part_o = reinterpret_cast<float*>(w);
-    w += 2 * (size_t)kPlanSms * kRows * kHeadDim * 4;
-    a.flush = reinterpret_cast<float4*>(w);
+    a.part_o = reinterpret_cast<float4*>(w);
     a.cap_groups = cache.cap_groups;
     a.B = g.B; a.Hq = g.Hq; a.Hkv = g.Hkv; a.Gq = g.Gq; a.S = g.S; a.T = g.T; a.n_cap = tree.n_cap;
     a.max_pages = max_pages; a.problems = g.problems;
-    a.block_nodes = kRows / g.Gq;
+    // The fewest rows that hold a whole tree: the time of a tile goes with the tokens that a thread weighs (8x28/4 heads, 5 nodes, capped
+    // scores: 99 -> 77 us with 64 rows, 16x32/8, 16 nodes: 78 -> 77).  Copies have to be added up at the end, so not where a CTA gets few
+    // tiles (1x8 heads, 8 nodes, 64 pages: 18 us, 25 with copies).
+    int sms = 0;
+    cudaError_t e = device_sm_count(&sms);
+    if (e != cudaSuccess) return e;
+    const int n_cta = sms < kPlanSms ? sms : kPlanSms;
+    const int64_t most_tiles = (int64_t)g.problems * ((page_ids ? max_pages : g.P) / kTilePages + 1);
+    a.rows = most_tiles <= 4 * n_cta ? kRows : 32;
+    while (a.rows < kRows && a.rows / g.Gq < tree.n_cap) a.rows *= 2;
+    a.block_nodes = a.rows / g.Gq;
     a.gq_inv = (65536u + (uint32_t)g.Gq - 1u) / (uint32_t)g.Gq;
     a.sc = score;
     a.scale_log2 = sm_scale * kLog2e;
     a.cap_in = score.softcap > 0.f ? sm_scale / score.softcap : 0.f;
     a.cap_log2 = score.softcap * kLog2e;
     a.window = score.window > 0 ? (uint32_t)score.window : 0xFFFFFFFFu;
-    int sms = 0;
-    cudaError_t e = device_sm_count(&sms);
-    if (e != cudaSuccess) return e;
-    const int n_cta = sms < kPlanSms ? sms : kPlanSms;
 
     EncodeTiled enc = tensor_map_encoder();
     if (!enc) return cudaErrorNotSupported;
@@ -1103,19 +1174,19 @@ cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tr
     if (!rows_map(&map_new, tree.k, new_rows, tree.n_cap) ||
         !(g.T > 0 ? rows_map(&map_k, cache.k, (long long)g.problems * g.T, at_once) : rows_map(&map_k, tree.k, new_rows, at_once)))
         return cudaErrorInvalidValue;
-    e = scored ? launch<true, true>(map_q, map_k, map_new, a, n_cta, st)
-        : masked ? launch<true, false>(map_q, map_k, map_new, a, n_cta, st) : launch<false, false>(map_q, map_k, map_new, a, n_cta, st);
+    e = a.rows == 32 ? launch<32>(map_q, map_k, map_new, a, n_cta, masked, scored, st)
+        : a.rows == 64 ? launch<64>(map_q, map_k, map_new, a, n_cta, masked, scored, st) : launch<128>(map_q, map_k, map_new, a, n_cta, masked, scored, st);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)g.problems, (unsigned)tree.n_cap);
-    cfg.blockDim = dim3(32u * (unsigned)g.Gq);
+    cfg.gridDim = dim3((unsigned)g.problems, (unsigned)((tree.n_cap + a.block_nodes - 1) / a.block_nodes * (a.rows / 8)));
+    cfg.blockDim = dim3(256);
     cfg.stream = st;
     cudaLaunchAttribute early;                       // its blocks wait in place instead of behind a launch
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &early;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, tree_join_kernel, a, kRows, n_cta);
+    return cudaLaunchKernelEx(&cfg, tree_join_kernel, a, n_cta);
 }
 
 }  // namespace stc
