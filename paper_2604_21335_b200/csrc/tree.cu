@@ -15,19 +15,49 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kAcceptThreads = 512, kAcceptCtas = 8;
+constexpr int kAcceptThreads = 512, kAcceptCtas = 8, kAcceptWarps = kAcceptThreads / 32;
 
-// Larger logit first, lower index among equals; NaN above everything.  0 is below every candidate.
-__device__ __forceinline__ unsigned long long candidate(float x, uint32_t index) {
-    const uint32_t key = x != x ? 0xFFFFFFFFu : float_key(x);
-    return (unsigned long long)key << 32 | (0xFFFFFFFFu - index);
-}
-__device__ __forceinline__ unsigned long long later(unsigned long long a, unsigned long long b) { return a > b ? a : b; }
+// The best of a set of logits: the largest key (NaN above everything), the lowest index among equals.
+struct Best {
+    uint32_t key = 0, index = 0xFFFFFFFFu;                   // (key 0: none; of a logit it is at least float_key(-inf) > 0)
+    __device__ __forceinline__ void take(float x, uint32_t i) { take(x != x ? 0xFFFFFFFFu : float_key(x + 0.f), i); }    // (-0 is 0)
+    __device__ __forceinline__ void take(uint32_t k, uint32_t i) {
+        if (k > key || (k == key && i < index)) {
+            key = k;
+            index = i;
+        }
+    }
+    __device__ __forceinline__ void over_warp() {
+        const uint32_t top = __reduce_max_sync(0xFFFFFFFFu, key);
+        index = __reduce_min_sync(0xFFFFFFFFu, key == top ? index : 0xFFFFFFFFu);
+        key = top;
+    }
+};
 
 template <bool BF16>
 __device__ __forceinline__ float logit_at(const void* row, uint32_t i) {
     if constexpr (BF16) return __uint_as_float((uint32_t)static_cast<const uint16_t*>(row)[i] << 16);
     else return static_cast<const float*>(row)[i];
+}
+// Maximum of the logits of 16 bytes; NaN if there is one.
+template <bool BF16>
+__device__ __forceinline__ float top_of(const uint4& w) {
+    if constexpr (BF16) {
+        auto top2 = [](uint32_t a, uint32_t b) {
+            uint32_t r;
+            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+            return r;
+        };
+        const uint32_t t = top2(top2(w.x, w.y), top2(w.z, w.w)), u = top2(t, t >> 16 | t << 16);
+        return bf16lo(u);
+    } else {
+        auto top = [](float a, float b) {
+            float r;
+            asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+            return r;
+        };
+        return top(top(__uint_as_float(w.x), __uint_as_float(w.y)), top(__uint_as_float(w.z), __uint_as_float(w.w)));
+    }
 }
 
 template <bool BF16>
@@ -35,9 +65,8 @@ __global__ void __launch_bounds__(kAcceptThreads)
 tree_accept_kernel(const void* __restrict__ logits, int n_cap, int vocab, int64_t row_stride, const int32_t* __restrict__ tokens,
                    const int32_t* __restrict__ parent, const int32_t* __restrict__ n_nodes, int32_t* __restrict__ path,
                    int32_t* __restrict__ n_accepted, int32_t* __restrict__ next_token) {
-    constexpr int kPer = BF16 ? 8 : 4;                       // logits per 16 bytes
-    __shared__ unsigned long long sh_best[2][kAcceptCtas];   // per step parity and CTA of the cluster
-    __shared__ unsigned long long sh_warp[kAcceptThreads / 32];
+    constexpr int kPer = BF16 ? 8 : 4, kAtOnce = 8;          // logits per 16 bytes; loads in flight
+    __shared__ uint2 sh_best[2][kAcceptCtas * kAcceptWarps]; // (key, index) per step parity and warp of the cluster
     __shared__ int sh_token[STC_TREE_MAX_NODES], sh_parent[STC_TREE_MAX_NODES];
     cg::cluster_group cluster = cg::this_cluster();
     const int b = blockIdx.x / kAcceptCtas, rank = (int)cluster.block_rank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -54,45 +83,55 @@ tree_accept_kernel(const void* __restrict__ logits, int n_cap, int vocab, int64_
         // the row from its first 16-byte boundary on, in 16-byte pieces dealt out in turn; the ends one by one
         const uint32_t head = min((uint32_t)vocab, (uint32_t)((16u - (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u)) & 15u) / (BF16 ? 2u : 4u));
         const uint32_t pieces = ((uint32_t)vocab - head) / kPer, tail = head + pieces * kPer;
-        unsigned long long best = 0;
         const uint32_t me = (uint32_t)rank * kAcceptThreads + threadIdx.x;
-        if (me < head) best = candidate(logit_at<BF16>(row, me), me);
-        if (tail + me < (uint32_t)vocab) best = later(best, candidate(logit_at<BF16>(row, tail + me), tail + me));
         const uint4* src = reinterpret_cast<const uint4*>(row + head * (BF16 ? 2 : 4));
-        // per thread ascending: of equal values the first stays
-        float top = -INFINITY;
+        // the piece with the thread's largest logit, the first of equal ones; within it the place is looked for once, at the end
+        float top = 0.f;
         uint32_t top_at = 0xFFFFFFFFu;
-        bool nan = false;
-#pragma unroll 4
-        for (uint32_t i = me; i < pieces; i += kAcceptCtas * kAcceptThreads) {
-            const uint4 w = ldg_nc16(src + i);
-            const uint32_t r[4] = {w.x, w.y, w.z, w.w};
+        uint4 top_piece = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 1
+        for (uint32_t i0 = me; i0 < pieces; i0 += kAtOnce * kAcceptCtas * kAcceptThreads) {
+            uint4 w[kAtOnce];
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) {
-                const float x = BF16 ? (e & 1 ? bf16hi(r[e / 2]) : bf16lo(r[e / 2])) : __uint_as_float(r[e % 4]);
-                if (!nan && (x > top || x != x || top_at == 0xFFFFFFFFu)) {
+            for (int u = 0; u < kAtOnce; ++u) {
+                const uint32_t i = i0 + (uint32_t)u * kAcceptCtas * kAcceptThreads;
+                w[u] = ldg_nc16(src + (i < pieces ? i : i0));
+            }
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const uint32_t i = i0 + (uint32_t)u * kAcceptCtas * kAcceptThreads;
+                const float x = top_of<BF16>(w[u]);
+                if (i < pieces && (top_at == 0xFFFFFFFFu || x > top || (x != x && top == top))) {
                     top = x;
-                    top_at = head + i * kPer + e;
-                    nan = x != x;
+                    top_at = i;
+                    top_piece = w[u];
                 }
             }
         }
-        if (top_at != 0xFFFFFFFFu) best = later(best, candidate(top, top_at));
+        Best best;
+        if (me < head) best.take(logit_at<BF16>(row, me), me);
+        if (tail + me < (uint32_t)vocab) best.take(logit_at<BF16>(row, tail + me), tail + me);
+        if (top_at != 0xFFFFFFFFu) {
+            const uint32_t r[4] = {top_piece.x, top_piece.y, top_piece.z, top_piece.w};
+            int at = kPer - 1;
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) best = later(best, __shfl_xor_sync(0xFFFFFFFFu, best, d));
-        if (lane == 0) sh_warp[warp] = best;
-        __syncthreads();
-        if (warp == 0) {
-            best = lane < kAcceptThreads / 32 ? sh_warp[lane] : 0;
-#pragma unroll
-            for (int d = 8; d > 0; d >>= 1) best = later(best, __shfl_xor_sync(0xFFFFFFFFu, best, d));
-            if (lane < kAcceptCtas) *cluster.map_shared_rank(&sh_best[count & 1][rank], lane) = best;
+            for (int e = kPer - 2; e >= 0; --e) {
+                const float x = BF16 ? (e & 1 ? bf16hi(r[e / 2]) : bf16lo(r[e / 2])) : __uint_as_float(r[e % 4]);
+                if (x == top || (x != x && top != top)) at = e;
+            }
+            best.take(top, head + top_at * kPer + at);
         }
+        best.over_warp();
+        if (lane < kAcceptCtas) *cluster.map_shared_rank(&sh_best[count & 1][rank * kAcceptWarps + warp], lane) = make_uint2(best.key, best.index);
         cluster.sync();
-        best = 0;
+        best = Best();
 #pragma unroll
-        for (int i = 0; i < kAcceptCtas; ++i) best = later(best, sh_best[count & 1][i]);
-        choice = (int)(0xFFFFFFFFu - (uint32_t)best);
+        for (int i = 0; i < kAcceptCtas * kAcceptWarps / 32; ++i) {
+            const uint2 of_warp = sh_best[count & 1][i * 32 + lane];
+            best.take(of_warp.x, of_warp.y);
+        }
+        best.over_warp();
+        choice = (int)best.index;
         ++count;
         // the lowest child with that token; every warp looks for itself
         int child = STC_TREE_MAX_NODES;
