@@ -152,6 +152,164 @@ fork_copy_kernel(int n_pairs, const int32_t* __restrict__ src_row, const int32_t
 
 constexpr int kCompactThreads = 256, kCompactCtas = 8, kCompactPages = 4;    // pages a CTA moves per round
 
+// For a cluster per (sequence, KV head): tokens that are kept, or -1, with its status, if a list of the sequence is not as it has to be.
+// Every CTA checks a share of all lists of the sequence: every head drops the same number of tokens or nothing is moved.
+__device__ __forceinline__ int kept_tokens(int problem, int len, int n, int Hkv, const int32_t* __restrict__ page_ids,
+                                           const int32_t* __restrict__ n_pages, int max_pages, int dst_T,
+                                           int32_t* __restrict__ new_len, int32_t* __restrict__ status) {
+    __shared__ int sh_bad[kCompactCtas];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = (int)cluster.block_rank(), tid = threadIdx.x, b = problem / Hkv;
+    const int pages = (len + kPage - 1) / kPage, rest = pages * kPage - len;
+    bool bad = n < 0 || n > max_pages || n > pages;
+    bool ends = false;                                                       // the last page is listed
+    if (!bad && n > 0) ends = page_ids[(size_t)b * Hkv * max_pages + n - 1] == pages - 1;
+    const int kept = bad ? 0 : n * kPage - (ends ? rest : 0);
+    bad = bad || kept > dst_T;
+    for (int h = tid; h < Hkv && !bad; h += kCompactThreads) bad = n_pages[(size_t)b * Hkv + h] != n;
+    bad = __syncthreads_or(bad);
+    if (!bad) {
+        // entry i of all lists at once: i = e mod n of list e / n
+        for (int64_t e = rank * kCompactThreads + tid; e < (int64_t)n * Hkv; e += kCompactCtas * kCompactThreads) {
+            const int h = (int)(e / n), i = (int)(e - (int64_t)h * n);
+            const int32_t* list = page_ids + ((size_t)b * Hkv + h) * max_pages;
+            const int p = list[i];
+            bad |= p < 0 || p >= pages || (i > 0 && list[i - 1] >= p);
+            if (i == n - 1 && rest > 0) bad |= (p == pages - 1) != ends;
+        }
+    }
+    bad = __syncthreads_or(bad);
+    cluster.sync();
+    if (tid < kCompactCtas) *cluster.map_shared_rank(&sh_bad[rank], tid) = bad;
+    cluster.sync();
+#pragma unroll
+    for (int i = 0; i < kCompactCtas; ++i) bad |= sh_bad[i] != 0;
+    if (rank == 0 && tid == 0) {
+        if (problem == b * Hkv) new_len[b] = bad ? len : kept;
+        if (bad) status[problem] = STC_ERR_INVALID_ARG;
+    }
+    return bad ? -1 : kept;
+}
+
+// Between two caches the pages are independent once their new offsets are known: a CTA takes a share of the list, the CTAs meet
+// once to tell each other the groups of their shares, and every warp moves pages by itself.
+template <int S>
+__global__ void __launch_bounds__(kCompactThreads, 2)
+compact_apart_kernel(const int32_t* __restrict__ seq_len, int Hkv, const int32_t* __restrict__ page_ids,
+                     const int32_t* __restrict__ n_pages, int max_pages, View src, View dst, int32_t* __restrict__ new_len,
+                     int64_t* __restrict__ total_groups, int32_t* __restrict__ status) {
+    constexpr int OPG = kOctets / S, kWarps = kCompactThreads / 32, kPer = kPage * kOctets / 32;
+    __shared__ uint32_t sh_count[kCompactCtas], sh_sum[kWarps], sh_first[kCompactThreads], sh_to[kCompactThreads], sh_size[kCompactThreads];
+    __shared__ int sh_page[kCompactThreads];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int problem = blockIdx.x / kCompactCtas, rank = (int)cluster.block_rank(), b = problem / Hkv, tid = threadIdx.x;
+    const int len = clamp_len(seq_len, b, src.T), n = n_pages[(size_t)b * Hkv], warp = tid >> 5, lane = tid & 31;
+    const int kept = kept_tokens(problem, len, n, Hkv, page_ids, n_pages, max_pages, dst.T, new_len, status);
+    if (kept < 0) return;                                                    // (the whole cluster)
+    const int32_t* list = page_ids + (size_t)problem * max_pages;
+    const uint32_t* offs = src.v_offs + (size_t)problem * (src.T + 1);
+    const int share = (n + kCompactCtas - 1) / kCompactCtas, first = min(rank * share, n), last = min(first + share, n);
+    // of entry i: its page, where its groups are, how many
+    auto entry = [&](int i, int& page, uint32_t& o0) -> uint32_t {
+        page = -1;
+        o0 = 0;
+        if (i >= last) return 0;
+        page = list[i];
+        const int t0 = page * kPage, tokens = min(kPage, len - t0);
+        o0 = offs[t0];
+        return min(offs[t0 + tokens] - o0, (uint32_t)(tokens * S));
+    };
+    // sum over the block of what each thread has, and the sum before it
+    auto scan = [&](uint32_t x, uint32_t& total) -> uint32_t {
+        const uint32_t incl = warp_incl_scan(x, lane);
+        __syncthreads();
+        if (lane == 31) sh_sum[warp] = incl;
+        __syncthreads();
+        uint32_t before = 0;
+        total = 0;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) {
+            if (i < warp) before += sh_sum[i];
+            total += sh_sum[i];
+        }
+        return before + incl - x;
+    };
+    int page;
+    uint32_t o0, sum = 0, mine;
+    const bool once = share <= kCompactThreads;
+    uint32_t size = entry(first + tid, page, o0), before = scan(size, mine);
+    if (!once) {
+        sum = size;
+        for (int i = first + kCompactThreads + tid; i < last; i += kCompactThreads) {
+            int p;
+            uint32_t o;
+            sum += entry(i, p, o);
+        }
+        scan(sum, mine);
+    }
+    if (tid < kCompactCtas) *cluster.map_shared_rank(&sh_count[rank], tid) = mine;
+    cluster.sync();                                                          // (the last write to another CTA is through)
+    uint32_t base = 0, all = 0;                                              // (offsets are 32-bit numbers in the cache itself)
+#pragma unroll
+    for (int c = 0; c < kCompactCtas; ++c) {
+        if (c < rank) base += sh_count[c];
+        all += sh_count[c];
+    }
+    const uint4* ks = src.k + (size_t)problem * src.T * kOctets;
+    const uint4* vs = src.v_packed + (size_t)problem * src.cap_groups * OPG;
+    uint4* kd = dst.k + (size_t)problem * dst.T * kOctets;
+    uint4* vd = dst.v_packed + (size_t)problem * dst.cap_groups * OPG;
+    for (int i0 = first; i0 < last; i0 += kCompactThreads) {
+        if (i0 > first) size = entry(i0 + tid, page, o0);
+        uint32_t total;
+        if (i0 > first || !once) before = scan(size, total);
+        else total = mine;
+        __syncthreads();
+        sh_page[tid] = page; sh_first[tid] = o0; sh_size[tid] = size; sh_to[tid] = base + before;
+        __syncthreads();
+        base += total;
+        const int m = min(kCompactThreads, last - i0);
+#pragma unroll 1
+        for (int j = warp; j < m; j += kWarps) {
+            const int i = i0 + j, t0 = sh_page[j] * kPage, tokens = min(kPage, len - t0);
+            const uint32_t from = sh_first[j], to = sh_to[j];
+            const int64_t room = src.cap_groups - (int64_t)from;             // (offsets that do not fit the store are not followed)
+            const int chunks = (int)min((int64_t)sh_size[j], max(room, (int64_t)0)) * OPG;
+            uint4 key[kPer], val[kPer], meta = {};
+            uint32_t word = 0, off = 0;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (lane + e * 32 < tokens * kOctets) key[e] = ldg_nc16(ks + (size_t)t0 * kOctets + lane + e * 32);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (lane + e * 32 < chunks) val[e] = ldg_nc16(vs + (size_t)from * OPG + lane + e * 32);
+            if (dst.kmin) meta = ldg_nc16((lane < kOctets ? src.kmin : src.kmax) + ((size_t)problem * src.P + t0 / kPage) * kOctets + (lane & 15));
+            if (lane < tokens) {
+                word = src.v_mask[(size_t)problem * src.T + t0 + lane];
+                off = offs[t0 + lane] - from;
+            }
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (lane + e * 32 < tokens * kOctets) kd[(size_t)i * kPage * kOctets + lane + e * 32] = key[e];
+            const int64_t fits = (dst.cap_groups - (int64_t)to) * OPG;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (lane + e * 32 < chunks && lane + e * 32 < fits) vd[(size_t)to * OPG + lane + e * 32] = val[e];
+            if (dst.kmin) ((lane < kOctets ? dst.kmin : dst.kmax) + ((size_t)problem * dst.P + i) * kOctets)[lane & 15] = meta;
+            if (lane < tokens) {
+                dst.v_mask[(size_t)problem * dst.T + i * kPage + lane] = (uint16_t)word;
+                dst.v_offs[(size_t)problem * (dst.T + 1) + i * kPage + lane] = to + off;
+            }
+        }
+    }
+    if (rank == 0 && tid == 0) {                                             // (every token wrote where it begins; this is where the last ends)
+        dst.v_offs[(size_t)problem * (dst.T + 1) + kept] = all;
+        total_groups[problem] = all;
+        status[problem] = (int64_t)all > dst.cap_groups ? STC_ERR_CAPACITY : STC_OK;
+    }
+}
+
+// Within one cache the order matters.
 // One cluster per (sequence, KV head) moves 32 listed pages per round.  A round is read into registers, the CTAs meet (which also
 // tells each how many groups those before it hold), and the round is written.  In place that order is enough: the
 // i-th listed page is at i or above, so what a round writes lies below everything that later rounds read, and everything that
@@ -163,41 +321,12 @@ compact_kernel(const int32_t* __restrict__ seq_len, int Hkv, const int32_t* __re
                const int32_t* __restrict__ n_pages, int max_pages, View src, View dst, int32_t* __restrict__ new_len,
                int64_t* __restrict__ total_groups, int32_t* __restrict__ status) {
     constexpr int OPG = kOctets / S, kPer = kPage * kOctets / 64;            // 64 threads per page, 16-byte pieces of each
-    __shared__ int sh_bad[kCompactCtas];
     __shared__ uint32_t sh_count[2][kCompactCtas];                           // groups of each CTA's pages, per round parity
     cg::cluster_group cluster = cg::this_cluster();
     const int problem = blockIdx.x / kCompactCtas, rank = (int)cluster.block_rank(), b = problem / Hkv, tid = threadIdx.x;
-    const int len = clamp_len(seq_len, b, src.T), pages = (len + kPage - 1) / kPage, rest = pages * kPage - len;
-    const int n = n_pages[(size_t)b * Hkv];
-    // all lists of the sequence, a share per CTA: every head drops the same number of tokens or nothing is moved
-    bool bad = n < 0 || n > max_pages || n > pages;
-    bool ends = false;                                                       // the last page is listed
-    if (!bad && n > 0) ends = page_ids[(size_t)b * Hkv * max_pages + n - 1] == pages - 1;
-    const int kept = bad ? 0 : n * kPage - (ends ? rest : 0);
-    bad = bad || kept > dst.T;
-    for (int h = tid; h < Hkv && !bad; h += kCompactThreads) bad = n_pages[(size_t)b * Hkv + h] != n;
-    bad = __syncthreads_or(bad);
-    if (!bad) {
-        for (int h = 0; h < Hkv; ++h) {
-            const int32_t* list = page_ids + ((size_t)b * Hkv + h) * max_pages;
-            for (int i = rank * kCompactThreads + tid; i < n; i += kCompactCtas * kCompactThreads) {
-                const int p = list[i];
-                bad |= p < 0 || p >= pages || (i > 0 && list[i - 1] >= p);
-                if (i == n - 1 && rest > 0) bad |= (p == pages - 1) != ends;
-            }
-        }
-    }
-    bad = __syncthreads_or(bad);
-    cluster.sync();
-    if (tid < kCompactCtas) *cluster.map_shared_rank(&sh_bad[rank], tid) = bad;
-    cluster.sync();
-#pragma unroll
-    for (int i = 0; i < kCompactCtas; ++i) bad |= sh_bad[i] != 0;
-    if (rank == 0 && tid == 0 && problem == b * Hkv) new_len[b] = bad ? len : kept;
-    if (bad) {
-        if (rank == 0 && tid == 0) status[problem] = STC_ERR_INVALID_ARG;
-        return;                                                              // (the whole cluster: nobody writes to a CTA that left)
-    }
+    const int len = clamp_len(seq_len, b, src.T), n = n_pages[(size_t)b * Hkv];
+    const int kept = kept_tokens(problem, len, n, Hkv, page_ids, n_pages, max_pages, dst.T, new_len, status);
+    if (kept < 0) return;                                                    // (the whole cluster: nobody writes to a CTA that left)
     const int32_t* list = page_ids + (size_t)problem * max_pages;
     const uint32_t* offs = src.v_offs + (size_t)problem * (src.T + 1);
     const uint16_t* mask = src.v_mask + (size_t)problem * src.T;
@@ -360,9 +489,10 @@ cudaError_t launch_cache_compact(const Geom& gs, const stc_cache& src, const int
     cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
     cfg.attrs = &cluster;
     cfg.numAttrs = 1;
+    // (a share of the list per CTA and one meeting, against a meeting per 32 pages)
 #define STC_COMPACT(S_) \
-    case S_: return cudaLaunchKernelEx(&cfg, compact_kernel<S_>, gs.seq_len, gs.Hkv, page_ids, n_pages, max_pages, vs, vd, new_len, \
-                                       total_groups, status);
+    case S_: return cudaLaunchKernelEx(&cfg, src.k == dst.k ? compact_kernel<S_> : compact_apart_kernel<S_>, gs.seq_len, gs.Hkv, page_ids, \
+                                       n_pages, max_pages, vs, vd, new_len, total_groups, status);
     switch (gs.S) {
         STC_COMPACT(4) STC_COMPACT(8) STC_COMPACT(16)
         default: return cudaErrorInvalidValue;
