@@ -325,6 +325,28 @@ def test_compact_long_lists_in_place_again_and_again():
         length = new_len
 
 
+def test_compact_long_lists_into_another_cache():
+    """More pages per CTA than it has threads, and a store that ends in the middle of them."""
+    S, H, T, lens = 4, 2, 34000, [34000, 301]
+    c, r = full(12, 2, H, T, S, lens, keep=1), TR.rng(2)
+    lists = []
+    for n in lens:
+        pages = (n + 15) // 16
+        m = pages - 9
+        lists.append([sorted(r.sample(range(pages - 1), m - 1)) + [pages - 1] for _ in range(H)])
+    ids, n = pack_lists(lists, 2125)
+    for cap in (c["cap"], c["cap"] // 2):
+        d = blank(3, 2, H, 2125 * 16, S, cap)
+        src, dst = device(c), device(d)
+        new_len, total, status = outputs(2, H, 2)
+        P.cache_compact(P.Shape(2, H, H, S, T, i32(lens)), src, ids, n, new_len, total, status, dst_shape=P.Shape(2, H, H, S, 2125 * 16), dst=dst)
+        w, ln, tot = compact_on_host(c, d, S, lists)
+        same(dst, w)
+        same(src, c)
+        assert new_len.tolist() == ln and total.flatten().tolist() == tot
+        assert status.flatten().tolist() == [0 if x <= cap else 4 for x in tot]
+
+
 def test_compact_dropping_the_last_page_that_is_not_full():
     S, H, T, lens = 8, 2, 200, [185, 200]
     c = full(2, 2, H, T, S, lens)

@@ -321,3 +321,37 @@ def test_offsets_beyond_32_bits():
         o, l, to, tl = TR.tree_rows(q[-1, :, 2 * h:2 * h + 2].cpu(), k[-1, h][at.cuda()].cpu(), dense.reshape(-1, 128), at, kn[-1, h].cpu(),
                                     vn[-1, h].cpu(), [-1, 0, 1, 2, 3], n, T + torch.arange(n), SCALE)
         R.assert_rows(out[-1, :, 2 * h:2 * h + 2], lse[-1, :, 2 * h:2 * h + 2], o, l, to, tl)
+
+
+# rows of a block (32, 64, 128), copied over the tensor-memory lanes once the call may have more than four tiles per SM
+FEW_ROWS = [((8, 8), 8, 32), ((8, 8), 4, 3), ((32, 8), 16, 16), ((28, 4), 8, 5), ((8, 2), 8, 1), ((16, 8), 8, 33)]
+
+
+@pytest.mark.parametrize("heads,S,nodes", FEW_ROWS)
+def test_few_rows_long_caches(heads, S, nodes):
+    T = 128 * (600 // (3 * heads[1]) + 1) + 3
+    c = make(nodes, heads, S, T, [min(T, 3400), 1500, 129], nodes, [nodes, max(1, nodes - 1), nodes])
+    check(c, *call(c))
+
+
+@pytest.mark.parametrize("heads,S,nodes", FEW_ROWS)
+def test_few_rows_many_short_caches(heads, S, nodes):
+    """Units that a CTA finishes by itself, several per CTA."""
+    r, B, T = TR.rng(nodes), 192 // heads[1], 700
+    lens = [r.choice([0, 1, 16, 127, 128, 500, 699, 700]) for _ in range(B)]
+    c = make(nodes + 1, heads, S, T, lens, nodes, [r.randint(0, nodes) for _ in range(B)])
+    check(c, *call(c))
+
+
+@pytest.mark.parametrize("heads,nodes", [((8, 8), 20), ((28, 4), 5)])
+@pytest.mark.parametrize("softcap,alibi,window,docs", [(30.0, False, 0, False), (0.0, True, 0, False), (0.0, False, 150, True), (5.0, True, 400, True)])
+def test_few_rows_with_options(heads, nodes, softcap, alibi, window, docs):
+    r, B, T = TR.rng(nodes), 192 // heads[1], 700
+    lens = [r.choice([1, 130, 500, 700]) for _ in range(B)]
+    c = make(nodes + 2, heads, 8, T, lens, nodes, [r.randint(1, nodes) for _ in range(B)])
+    slopes = torch.tensor([2.0 ** (-8.0 * (h + 1) / heads[0]) for h in range(heads[0])]) if alibi else None
+    doc = (torch.arange(T)[None, :] // 37 % 4 - 1).expand(B, T).contiguous().int() if docs else None
+    q_doc = torch.tensor([r.choice([1, 2, 9]) for _ in range(B)], dtype=torch.int32) if docs else None
+    dev = lambda x: None if x is None else x.cuda()  # noqa: E731
+    score = P.Score(softcap=softcap, slopes=dev(slopes), window=window, tok_doc=dev(doc), q_doc=dev(q_doc))
+    check(c, *call(c, score=score), softcap=softcap, slopes=slopes, window=window, doc=doc, q_doc=q_doc)
