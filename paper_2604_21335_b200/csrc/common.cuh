@@ -257,7 +257,7 @@ cudaError_t launch_prefix_attn(const Geom& g, const void* k, const void* v_packe
                                const int32_t* row_start, float sm_scale, const ScoreArgs* score, const float* own_out,
                                const float* own_lse, float* out, float* lse, void* ws, cudaStream_t st);
 
-size_t tree_attn_ws_bytes(const Geom& g, int n_cap);
+size_t tree_attn_ws_bytes();
 cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tree& tree, const void* q, const int32_t* page_ids,
                              const int32_t* n_pages, int max_pages, float sm_scale, const ScoreArgs& score, float* out, float* lse,
                              int32_t* status, void* ws, cudaStream_t st);

@@ -82,7 +82,7 @@ int32_t stc_workspace_bytes(const stc_shape* shape, int32_t op, int64_t arg, siz
     }
     if (op == STC_OP_TREE_ATTN) {                   // nodes attend their ancestors even where the cache has no tokens
         if (arg < 0 || arg > STC_TREE_MAX_NODES) return STC_ERR_INVALID_ARG;
-        *bytes_host = g.problems == 0 || arg == 0 ? 0 : tree_attn_ws_bytes(g, (int)arg);
+        *bytes_host = g.problems == 0 || arg == 0 ? 0 : tree_attn_ws_bytes();
         return STC_OK;
     }
     if (empty(g)) { *bytes_host = 0; return STC_OK; }
@@ -465,7 +465,7 @@ int32_t stc_tree_attn(const stc_shape* shape, const stc_cache* cache, const stc_
     if (g.T > 0 && (!cache->k || !cache->v_packed || !cache->v_mask || !cache->v_offs || cache->cap_groups < 0))
         return STC_ERR_INVALID_ARG;
     if (!aligned16(cache->k, cache->v_packed, q, out, tree->k, tree->v)) return STC_ERR_INVALID_ARG;
-    rc = check_ws(ws, ws_bytes, tree_attn_ws_bytes(g, tree->n_cap));
+    rc = check_ws(ws, ws_bytes, tree_attn_ws_bytes());
     if (rc != STC_OK) return rc;
     return cuda_rc(launch_tree_attn(g, *cache, *tree, q, page_ids, n_pages, max_pages, sm_scale, sc, out, lse_opt, status, ws,
                                     static_cast<cudaStream_t>(stream)));

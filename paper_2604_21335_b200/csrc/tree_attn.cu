@@ -48,7 +48,7 @@ constexpr uint32_t kHalf = kTok * 128;            // 64 channels of a token tile
 constexpr uint32_t kTile = 2 * kHalf;             // 32 KiB
 constexpr uint32_t kSlot = kTile / 2;             // values of 64 tokens: two halves of 64 channels
 constexpr int kRows = 128;                        // tensor-memory lanes
-constexpr int kFlush = 8;                         // tiles that an accumulator takes: 128 products, at most 5e-6 of it
+constexpr int kFlush = 4;                         // tiles that an accumulator takes: 64 products, at most 2.6e-6 of it
 constexpr int kBufs = 3;                          // score buffers: 128 columns each, and 128 for O
 constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -86,7 +86,7 @@ struct TreeArgs {
     int32_t* status;             // [B]
     int32_t* word;               // the call's status word
     int32_t* cta_status;         // [grid]
-    int32_t* base;               // [problems + 1]: where each problem begins in the flat sequence, and its length
+    int4* split;                 // [grid] the unit that a CTA begins and leaves to others: problem (-1: none), block, last CTA, nodes
     float2* part_ml;             // [2 * grid][128 lanes]
     float4* part_o;              // [3 * grid][32][128 lanes]: first and last partial of a CTA, and a place to add copies up
     int64_t cap_groups;
@@ -224,24 +224,23 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             x_end = cut.begin((int)blockIdx.x + 1);
         }
         const bool holds = x_begin < x_end && before <= x_begin && x_begin < before + mine;
-        if (holds || blockIdx.x == 0) {
+        if (holds) {
             int at = before;
 #pragma unroll 1
             for (int p = p_lo; p < p_hi; ++p) {
                 const int n = per > 1 ? problem_length(a, p) : mine;
-                if (holds && at <= x_begin && x_begin < at + n) {
+                if (at <= x_begin && x_begin < at + n) {
                     sums[16] = p;
                     sums[17] = x_begin - at;
                 }
-                if (blockIdx.x == 0) a.base[p] = at;
                 at += n;
             }
         }
-        if (blockIdx.x == 0 && threadIdx.x == 0) a.base[a.problems] = total;
     }
     __syncthreads();
     const int p_first = sums[16], x_first = sums[17];
     __syncthreads();                                 // (the ancestors' table takes their place)
+    if (threadIdx.x == 96) a.split[blockIdx.x] = make_int4(-1, 0, 0, 0);         // (the scheduler's)
 
     auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
     auto warp_wait = [&](int i, uint32_t phase) { return warp_wait_clocked(bar(i), phase & 1u, abort_flag); };
@@ -470,6 +469,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     g.node0 = blk * a.block_nodes;
                     // a CTA continues at most one unit (slot 0) and leaves at most one that it begins (slot 1)
                     g.slot = g.tile1 - g.tile0 == u.tiles ? -1 : 2 * (int)blockIdx.x + (g.tile0 == 0 ? 1 : 0);
+                    if (lane == 0 && g.slot > 0 && (g.slot & 1))
+                        a.split[blockIdx.x] = make_int4(p, blk, Cut(total, (int)gridDim.x).owner(x + u.tiles - 1), g.nodes);
                     x += g.tile1 - g.tile0;
                     off += g.tile1 - g.tile0;
                     break;
@@ -995,46 +996,46 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     }
 }
 
-// Joins the partials of units that more than one CTA worked on, in CTA order: block = 8 rows of a block of a (sequence, KV head).
-// Checks the trees and gathers the CTAs' status on the side.  Short on purpose: it runs once, from
-// cold instruction memory.
-__global__ void __launch_bounds__(256)
+// Joins the partials of units that more than one CTA worked on, in CTA order: blockIdx.x = the CTA that begins the unit, blockIdx.y =
+// 8 rows of it; behind them blocks that check the trees and gather the CTAs' status.  Few dependent loads on purpose: nothing
+// hides this kernel's latency (with the units looked up by problem it took 24 us at 16x32/8 heads and 64 nodes).
+__global__ void __launch_bounds__(256, 6)
 tree_join_kernel(const TreeArgs a, int grid) {
-    // launched while the first kernel still runs: the call's own inputs are read before the wait
-    const int problem = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int b = (int)((uint32_t)problem / (uint32_t)a.Hkv), hk = problem - b * a.Hkv;
-    const int nodes = nodes_of(a, b);
-    int list, first_page;
-    pages_of(a, problem, clamp_len(a.seq_len, b, a.T), list, first_page);
-    const Unit u = unit_of(a, nodes, list);
-    if (blockIdx.y == 0 && hk == 0 && warp == 0) {
-        bool bad = false;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if ((int)blockIdx.x >= grid) {
+        if (blockIdx.y > 0) return;
+        const int b = ((int)blockIdx.x - grid) * 8 + warp;
+        if (b < a.B) {
+            const int nodes = nodes_of(a, b);
+            bool bad = false;
 #pragma unroll 1
-        for (int i = lane; i < nodes && a.parent; i += 32) {
-            const int up = a.parent[(size_t)b * a.n_cap + i];
-            bad |= up < -1 || up >= i;
+            for (int i = lane; i < nodes && a.parent; i += 32) {
+                const int up = a.parent[(size_t)b * a.n_cap + i];
+                bad |= up < -1 || up >= i;
+            }
+            bad = __any_sync(0xFFFFFFFFu, bad);
+            if (lane == 0) a.status[b] = bad ? STC_ERR_INVALID_ARG : STC_OK;
         }
-        bad = __any_sync(0xFFFFFFFFu, bad);
-        if (lane == 0) a.status[b] = bad ? STC_ERR_INVALID_ARG : STC_OK;
-    }
-    // warp = 8 rows of a block and 4 chunks of 4 channels: the partials are read in 128 bytes, the rows written in 64
-    const int eights = a.rows / 8, blk = (int)((uint32_t)blockIdx.y / (uint32_t)eights);
-    const int in_block = ((int)blockIdx.y - blk * eights) * 8 + (lane & 7), chunk = warp * 4 + (lane >> 3);
-    const int node_in = (int)(((uint32_t)in_block * a.gq_inv) >> 16), node = blk * a.block_nodes + node_in, h = in_block - node_in * a.Gq;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (problem == 0 && blockIdx.y == 0 && warp == 0) {
-        int st = 0;
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (b == 0) {
+            int st = 0;
 #pragma unroll 1
-        for (int c = lane; c < grid; c += 32) st = max(st, a.cta_status[c]);
-        st = __reduce_max_sync(0xFFFFFFFFu, st);
-        if (lane == 0) *a.word = st;
+            for (int c = lane; c < grid; c += 32) st = max(st, __ldcg(a.cta_status + c));
+            st = __reduce_max_sync(0xFFFFFFFFu, st);
+            if (lane == 0) *a.word = st;
+        }
+        return;
     }
-    if (node_in >= a.block_nodes || node >= nodes) return;
-    const Cut cut(a.base[a.problems], grid);
-    const int x0 = a.base[problem] + blk * u.tiles, c0 = cut.owner(x0), c1 = cut.owner(x0 + u.tiles - 1);
-    if (c0 == c1) return;                            // finished where it was computed
+    // warp = 8 rows and 4 chunks of 4 channels: the partials are read in 128 bytes, the rows written in 64
+    const int in_block = (int)blockIdx.y * 8 + (lane & 7), chunk = warp * 4 + (lane >> 3);
+    const int node_in = (int)(((uint32_t)in_block * a.gq_inv) >> 16), h = in_block - node_in * a.Gq;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int4 split = __ldcg(a.split + blockIdx.x);
+    const int node = split.y * a.block_nodes + node_in, c0 = (int)blockIdx.x, c1 = split.z;
+    if (split.x < 0 || node_in >= a.block_nodes || node >= split.w) return;
+    const int b = (int)((uint32_t)split.x / (uint32_t)a.Hkv), hk = split.x - b * a.Hkv;
     const size_t row = ((size_t)b * a.n_cap + node) * a.Hq + hk * a.Gq + h;
-    constexpr int kAtOnce = 8;                       // loads in flight
+    constexpr int kAtOnce = 4;                       // loads in flight
     const int copies_log2 = __ffs(kRows / a.rows) - 1, parts = (c1 - c0 + 1) << copies_log2;
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1044,18 +1045,18 @@ tree_join_kernel(const TreeArgs a, int grid) {
         float4 v[kAtOnce];
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
-            const int j = min(first + i, parts - 1), e = c0 + (j >> copies_log2), copy = j & ((1 << copies_log2) - 1);
+            const int e = c0 + ((first + i) >> copies_log2), copy = (first + i) & ((1 << copies_log2) - 1);
             const size_t at = (size_t)(2 * e + (e == c0 ? 1 : 0));
+            p[i] = make_float2(-INFINITY, 0.f);
+            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (first + i >= parts) continue;
             p[i] = __ldcg(a.part_ml + at * kRows + in_block);
             if (copy) p[i].y = 0.f;                  // the row's sum is told once
             v[i] = __ldcg(a.part_o + (at * 32 + chunk) * kRows + copy * a.rows + in_block);
         }
         float top = m;
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            if (first + i >= parts) p[i] = make_float2(-INFINITY, 0.f);
-            top = fmaxf(top, p[i].x);
-        }
+        for (int i = 0; i < kAtOnce; ++i) top = fmaxf(top, p[i].x);
         const float fm = m == -INFINITY ? 0.f : ex2(m - top);
         l *= fm; o.x *= fm; o.y *= fm; o.z *= fm; o.w *= fm;
 #pragma unroll
@@ -1103,8 +1104,8 @@ cudaError_t launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap
 
 }  // namespace
 
-size_t tree_attn_ws_bytes(const Geom& g, int) {
-    return 256 + align256(kPlanSms * 4) + align256(((size_t)g.problems + 1) * 4) + 2 * (size_t)kPlanSms * kRows * 8 +
+size_t tree_attn_ws_bytes() {
+    return 256 + align256(kPlanSms * 4) + align256(kPlanSms * 16) + 2 * (size_t)kPlanSms * kRows * 8 +
            3 * (size_t)kPlanSms * kRows * kHeadDim * 4;
 }
 
@@ -1123,8 +1124,8 @@ cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tr
     w += 256;
     a.cta_status = reinterpret_cast<int32_t*>(w);
     w += align256(kPlanSms * 4);
-    a.base = reinterpret_cast<int32_t*>(w);
-    w += align256(((size_t)g.problems + 1) * 4);
+    a.split = reinterpret_cast<int4*>(w);
+    w += align256(kPlanSms * 16);
     a.part_ml = reinterpret_cast<float2*>(w);
     w += 2 * (size_t)kPlanSms * kRows * 8;
     a.part_o = reinterpret_cast<float4*>(w);
@@ -1178,7 +1179,7 @@ cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tr
         : a.rows == 64 ? launch<64>(map_q, map_k, map_new, a, n_cta, masked, scored, st) : launch<128>(map_q, map_k, map_new, a, n_cta, masked, scored, st);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)g.problems, (unsigned)((tree.n_cap + a.block_nodes - 1) / a.block_nodes * (a.rows / 8)));
+    cfg.gridDim = dim3((unsigned)(n_cta + (g.B + 7) / 8), (unsigned)(a.rows / 8));
     cfg.blockDim = dim3(256);
     cfg.stream = st;
     cudaLaunchAttribute early;                       // its blocks wait in place instead of behind a launch
