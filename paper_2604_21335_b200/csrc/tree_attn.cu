@@ -3,32 +3,41 @@
 //   Row r = (node i, query head) of a (sequence, KV head):  softmax over the valid tokens of the listed pages and the nodes N_i
 //   (node i and its ancestors) of s = sm_scale * q.k (+ options of stc_score),  out = sum p v~,  lse = log sum exp s.
 //
-// Rows (up to 128: whole nodes with their query heads) are the lanes of tensor memory, 128 tokens (8 pages, or the tree itself) a tile:
+// Rows (32, 64 or 128: whole nodes with their query heads) are the lanes of tensor memory, 128 tokens (8 pages, or the tree itself) a tile:
 //   S[row][token] = Q . K^T       Q, K tiles by TMA (128-byte swizzle), M = 128, N = 128, K = 128
 //   O[row][dim]  += P . V~        P from tensor memory, written over S by the softmax; V~ rebuilt from the packed groups
 //                                 in shared memory, token rows of 128 dims = N-major operand
-// A softmax thread owns a row.  With few rows most lanes idle, but the time of a tile hardly depends on them: the products take
-// 1600 cycles of the tensor pipe, the 128 exponentials of a thread 1024 of its quarter of the SM, and the tile's bytes (K 32 KiB, V
-// up to 32 KiB) 2100 to 2800 cycles of an SM's share of HBM.  (Tried first: tokens as lanes and rows as columns, which leaves no lane
-// idle.  Weights then pass through shared memory, sums take a register per row, maxima need the other warps, and the
-// unrolled columns do not fit the instruction cache: 3200 cycles per tile with 16 rows, 5000 with 128.)
+// Fewer than 128 rows are loaded several times.  The products cost the same, every copy of a row has all its scores; a copy weighs its share
+// of the tile's tokens, writes zeros for the others, and the copies' outputs add up at the end.  So the exponentials of a tile, 1024
+// cycles of an SM with 128 rows, go with the rows.
+// (Tried first: tokens as lanes and rows as columns, which leaves no lane idle.  Weights then pass through shared memory, sums take a
+// register per row, maxima need the other warps, and the unrolled columns do not fit the instruction cache: 3200 cycles per tile
+// with 16 rows, 5000 with 128; now 2600 and 3100.)
 // P enters as a bf16 high part plus a bf16 residual (two MMAs): the output is fp32, and one bf16 weight alone would leave it 2^-8 off;
 // the pair leaves 2^-16.
 //
 // Work split.  Unit = (sequence, KV head, block of nodes); its tiles are eight listed pages each and, last, the tree.  The tiles
 // of all units form one flat sequence that is cut into equal contiguous ranges, one per CTA (one CTA per SM).  A unit within
 // a range is finished in place; of others each CTA leaves (max, sum, accumulator), which a second kernel joins in CTA order:
-// no atomics, the same bits every time.
+// no atomics, the same bits every time.  (Joining in the CTA that is through last, with a counter per unit: 1x8 heads 19 -> 25 us, 8x28/4
+// 78 -> 89: cold instructions and dependent loads at the end of every segment.)
 //
 // Roles (16 warps): 0 = TMA producer of Q and K, which also tells which tokens of a tile there are; 1 = issuer of S, 2 = issuer of O;
-// 3 = scheduler, and the ancestors of a tree's nodes as bit masks (pointer doubling); 4..7 and 8..11 = softmax of the two groups,
-// which take the tiles in turn, each with its own S, O, maxima and sums, joined at the end of a segment; 12..15 rebuild the value tiles
-// with 16-byte asynchronous copies straight from the packed store into the swizzled tile.
+// 3 = scheduler, and the ancestors of a tree's nodes as bit masks (pointer doubling); 4..7 and 8..11 = softmax, two warps for each 32
+// lanes, which have 64 tokens of a tile and later 64 channels of the output each and tell each other their maxima; 12..15 rebuild the value
+// tiles with 16-byte asynchronous copies straight from the packed store into the swizzled tile, 32 tokens of every tile each.
+// Three score buffers of 128 columns and O fill the tensor memory.
 //
 // The running maximum only moves when a tile exceeds it by more than 2^24, so the accumulator in tensor memory is rescaled a few times
 // per segment and not per tile.  The tensor core truncates when it adds to an accumulator (4e-8 of its value per product, 16
-// products per tile), so an accumulator is emptied into fp32 sums every kFlush tiles.  A unit's tree comes first, then its pages from
-// the last to the first: with a distance bias the largest scores come first.
+// products per tile), so an accumulator is emptied every kFlush tiles into fp32 sums, which the softmax warps hold in registers (176 a
+// thread, the other warps 80).  A unit's tree comes first, then its pages from the last to the first: with a distance bias the
+// largest scores come first.
+//
+// What bounds it (16x32/8 heads, 256 pages of 128 tokens in 16; measured by leaving parts out): with 64 nodes, 149 us, the softmax (132
+// without it) and the value copies (148 without them); with 16 nodes, 76 us, neither (74 and 75): the way of a tile from its page ids
+// over TMA, S, softmax and O, two tiles of K and three of S deep.  Three K stages, prefetching K into L2, one copy per page instead of
+// two, finding the next maximum before the weights of this tile: no gain.
 //
 // Every wait is bounded (about a second); one that expires raises a CTA-wide flag and STC_ERR_TIMEOUT in the status word, the
 // roles leave, the producer waits (bounded) for its copies, tensor memory is freed.
@@ -59,8 +68,8 @@ constexpr int kKStages = 2, kVSlots = 6;          // K tiles; half V tiles
 
 // barriers, in 8-byte words of the control block; S, P, O per score buffer
 enum { kQFull, kQEmpty, kKFull, kKEmpty = kKFull + kKStages, kVFull = kKEmpty + kKStages, kVEmpty = kVFull + kVSlots,
-       kSFull = kVEmpty + kVSlots, kPFull = kSFull + kBufs, kOFull = kPFull + kBufs, kPair = kOFull + kBufs, kTabFull = kPair + 4, kTabEmpty, kSegFull,
-       kSegEmpty = kSegFull + kSegs, kBars = kSegEmpty + kSegs };
+       kSFull = kVEmpty + kVSlots, kPFull = kSFull + kBufs, kOFull = kPFull + kBufs, kPair = kOFull + kBufs, kTabFull = kPair + 4,
+       kTabEmpty, kSegFull, kSegEmpty = kSegFull + kSegs, kBars = kSegEmpty + kSegs };
 constexpr int kRing = 6;                          // tiles whose valid tokens are kept: K stages, score buffers and one more
 constexpr uint32_t kQHalf = kRows * 128;
 constexpr uint32_t kOffK = 2 * kQHalf, kOffV = kOffK + kKStages * kTile, kOffCtl = kOffV + kVSlots * kSlot;
@@ -189,7 +198,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_new) : "memory");
     if (threadIdx.x >= 64 && threadIdx.x < 64 + kBars) {
         const int i = (int)threadIdx.x - 64;
-        mbar_init(bars + 8 * i, i >= kVFull && i < kVEmpty ? 2 : i >= kPFull && i < kOFull ? 8 : i >= kPair && i < kTabFull ? 2 * kCopies : i == kTabEmpty ? 8
+        mbar_init(bars + 8 * i, i >= kVFull && i < kVEmpty ? 2 : i >= kPFull && i < kOFull ? 8
+                                : i >= kPair && i < kTabFull ? 2 * kCopies : i == kTabEmpty ? 8
                                 : i >= kSegEmpty ? kSegReaders : 1);
         fence_mbar_init();
     }
@@ -828,9 +838,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 const int at4 = half / 4 + c / 4 + i;
-                                float* const x = sums + c + 4 * i;
-                                float4 v = make_float4(fmaf(__uint_as_float(q[4 * i]), f, x[0] * keep), fmaf(__uint_as_float(q[4 * i + 1]), f, x[1] * keep),
-                                                       fmaf(__uint_as_float(q[4 * i + 2]), f, x[2] * keep), fmaf(__uint_as_float(q[4 * i + 3]), f, x[3] * keep));
+                                auto sum = [&](int e) { return fmaf(__uint_as_float(q[4 * i + e]), f, sums[c + 4 * i + e] * keep); };
+                                float4 v = make_float4(sum(0), sum(1), sum(2), sum(3));
                                 if (kCopies > 1 && whole && !aside) {
 #pragma unroll
                                     for (int k = 1; k < kCopies; ++k) {
@@ -947,32 +956,32 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     // place of the token's first group: its page's, and the groups of the page's tokens before it
                     const uint32_t cnt = __popc(every), incl = warp_incl_scan(cnt, lane), page0 = __shfl_sync(0xFFFFFFFFu, incl, 15);
                     const uint32_t place = first + incl - cnt - (lane >= 16 ? page0 : 0u);
-                                                // groups behind the end of the store are not followed
-                                                const uint32_t held = place < limit ? limit - place : 0u;
-                                                while (__popc(m) > held) m &= ~(0x80000000u >> __clz(m));
-                                                auto copy = [&](auto groups) {
-                                                    constexpr int S = decltype(groups)::value, OPG = kOctets / S, LPT = OPG < 2 ? 2 : OPG, GPL = LPT / OPG;
-                                                    const int sub = lane % LPT;
-                    #pragma unroll 1
-                                                    for (int pass = 0; pass < LPT; ++pass) {
-                                                        const int tok = pass * (32 / LPT) + lane / LPT;       // of the 32
-                                                        uint32_t left = __shfl_sync(0xFFFFFFFFu, m, tok);     // groups from this lane's next one on
-                                                        const uint32_t at = __shfl_sync(0xFFFFFFFFu, place, tok);
-                                                        const uint4* src = packed + (size_t)at * OPG + sub % OPG;
-                                                        if constexpr (GPL > 1) {
-                                                            src += sub ? left & 1u : 0u;
-                                                            left >>= sub;
-                                                        }
-                                                        // chunk oct of the row: half oct >> 3, place (oct & 7) ^ (tok & 7); oct = k LPT + sub
-                                                        const uint32_t row = rows + (uint32_t)tok * 128u + (((uint32_t)(tok & 7) ^ (uint32_t)sub) << 4);
-                    #pragma unroll
-                                                        for (int k = 0; k < 16 / LPT; ++k) {
-                                                            cp_async16_if(((row ^ (uint32_t)(((k * LPT) & 7) << 4))) + ((k * LPT) >> 3) * (kSlot / 2), src, left & 1u);
-                                                            src += (GPL > 1 ? __popc(left & 3u) : (int)(left & 1u)) * OPG;
-                                                            left >>= GPL;
-                                                        }
-                                                    }
-                                                };
+                    // groups behind the end of the store are not followed
+                    const uint32_t held = place < limit ? limit - place : 0u;
+                    while (__popc(m) > held) m &= ~(0x80000000u >> __clz(m));
+                    auto copy = [&](auto groups) {
+                        constexpr int S = decltype(groups)::value, OPG = kOctets / S, LPT = OPG < 2 ? 2 : OPG, GPL = LPT / OPG;
+                        const int sub = lane % LPT;
+#pragma unroll 1
+                        for (int pass = 0; pass < LPT; ++pass) {
+                            const int tok = pass * (32 / LPT) + lane / LPT;       // of the 32
+                            uint32_t left = __shfl_sync(0xFFFFFFFFu, m, tok);     // groups from this lane's next one on
+                            const uint32_t at = __shfl_sync(0xFFFFFFFFu, place, tok);
+                            const uint4* src = packed + (size_t)at * OPG + sub % OPG;
+                            if constexpr (GPL > 1) {
+                                src += sub ? left & 1u : 0u;
+                                left >>= sub;
+                            }
+                            // chunk oct of the row: half oct >> 3, place (oct & 7) ^ (tok & 7); oct = k LPT + sub
+                            const uint32_t row = rows + (uint32_t)tok * 128u + (((uint32_t)(tok & 7) ^ (uint32_t)sub) << 4);
+#pragma unroll
+                            for (int k = 0; k < 16 / LPT; ++k) {
+                                cp_async16_if(((row ^ (uint32_t)(((k * LPT) & 7) << 4))) + ((k * LPT) >> 3) * (kSlot / 2), src, left & 1u);
+                                src += (GPL > 1 ? __popc(left & 3u) : (int)(left & 1u)) * OPG;
+                                left >>= GPL;
+                            }
+                        }
+                    };
                     if (a.S == 8) copy(std::integral_constant<int, 8>{});
                     else if (a.S == 16) copy(std::integral_constant<int, 16>{});
                     else copy(std::integral_constant<int, 4>{});
@@ -999,7 +1008,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 // Joins the partials of units that more than one CTA worked on, in CTA order: blockIdx.x = the CTA that begins the unit, blockIdx.y =
 // 8 rows of it; behind them blocks that check the trees and gather the CTAs' status.  Few dependent loads on purpose: nothing
 // hides this kernel's latency (with the units looked up by problem it took 24 us at 16x32/8 heads and 64 nodes).
-__global__ void __launch_bounds__(256, 6)
+__global__ void __launch_bounds__(256, 3)
 tree_join_kernel(const TreeArgs a, int grid) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((int)blockIdx.x >= grid) {
@@ -1035,7 +1044,7 @@ tree_join_kernel(const TreeArgs a, int grid) {
     if (split.x < 0 || node_in >= a.block_nodes || node >= split.w) return;
     const int b = (int)((uint32_t)split.x / (uint32_t)a.Hkv), hk = split.x - b * a.Hkv;
     const size_t row = ((size_t)b * a.n_cap + node) * a.Hq + hk * a.Gq + h;
-    constexpr int kAtOnce = 4;                       // loads in flight
+    constexpr int kAtOnce = 8;                       // loads in flight
     const int copies_log2 = __ffs(kRows / a.rows) - 1, parts = (c1 - c0 + 1) << copies_log2;
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1176,7 +1185,8 @@ cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tr
         !(g.T > 0 ? rows_map(&map_k, cache.k, (long long)g.problems * g.T, at_once) : rows_map(&map_k, tree.k, new_rows, at_once)))
         return cudaErrorInvalidValue;
     e = a.rows == 32 ? launch<32>(map_q, map_k, map_new, a, n_cta, masked, scored, st)
-        : a.rows == 64 ? launch<64>(map_q, map_k, map_new, a, n_cta, masked, scored, st) : launch<128>(map_q, map_k, map_new, a, n_cta, masked, scored, st);
+        : a.rows == 64 ? launch<64>(map_q, map_k, map_new, a, n_cta, masked, scored, st)
+                       : launch<128>(map_q, map_k, map_new, a, n_cta, masked, scored, st);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(n_cta + (g.B + 7) / 8), (unsigned)(a.rows / 8));
