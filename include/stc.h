@@ -498,10 +498,13 @@ int32_t stc_prefix_attn(const stc_shape* shape, const stc_cache* cache, int32_t 
  * does not see of the keys, and what no node of the sequence sees of the values, may hold anything; other values are to be
  * finite.  status i32 [B]: STC_OK, or STC_ERR_INVALID_ARG for a sequence one of whose parents is not in
  * [-1, node); such a parent counts as -1.  batch * n_cap * n_q_heads, batch * n_kv_heads * t_cap and the tiles of eight pages
- * that the blocks of nodes take together must be below 2^31 (else STC_ERR_UNSUPPORTED).  Both products run on the tensor cores with fp32 accumulation, the weights enter
- * the second as a bf16 pair.  The same call gives the same bits.
+ * that the blocks of nodes take together must be below 2^31 (else STC_ERR_UNSUPPORTED).  Both products run on the tensor
+ * cores with fp32 accumulation, the weights enter the second as a bf16 pair.  The same call gives the same bits.  The last bits
+ * of a row may depend on the other rows of the call, by which the work is split, and the rows of one KV head choose
+ * together between two forms of the cap that agree to fp32 accuracy.
  * ws: STC_OP_TREE_ATTN with arg = n_cap; its first int32 is a device status word the call writes: STC_OK, or
- * STC_ERR_TIMEOUT if a bounded wait expired on the device (it never should; out / lse are then unspecified). */
+ * STC_ERR_TIMEOUT if a bounded wait expired on the device (it never should; out / lse are then unspecified).  The workspace is
+ * 30 MB for any n_cap (partial results of every SM); calls that may overlap need one each. */
 int32_t stc_tree_attn(const stc_shape* shape, const stc_cache* cache, const stc_tree* tree, const void* q,
                       const int32_t* page_ids, const int32_t* n_pages, int32_t max_pages, float sm_scale,
                       const stc_score* score, float* out, float* lse_opt, int32_t* status, void* ws, size_t ws_bytes,

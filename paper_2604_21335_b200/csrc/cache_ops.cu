@@ -1,5 +1,6 @@
 // Copying whole cached sequences and closing the gaps that dropped pages leave.  No arithmetic but prefix sums: both calls move
-// bytes and are bound by HBM (one read of each source, one write of each destination).
+// bytes and are bound by HBM (one read of each source, one write of each destination): 16 copies of two prompts of 16384 tokens
+// 181 us, 4.6 TB/s; 16x8 lists of 256 pages into another cache 94 us, 4.7 TB/s, where a plain copy reaches 6.6.
 #include <cooperative_groups.h>
 
 #include "common.cuh"
@@ -489,7 +490,8 @@ cudaError_t launch_cache_compact(const Geom& gs, const stc_cache& src, const int
     cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
     cfg.attrs = &cluster;
     cfg.numAttrs = 1;
-    // (a share of the list per CTA and one meeting, against a meeting per 32 pages)
+    // (between two caches a share of the list per CTA and one meeting; within one, in order, a meeting per 32 pages.  16x8 lists of 256
+    // pages: 94 and 140 us)
 #define STC_COMPACT(S_) \
     case S_: return cudaLaunchKernelEx(&cfg, src.k == dst.k ? compact_kernel<S_> : compact_apart_kernel<S_>, gs.seq_len, gs.Hkv, page_ids, \
                                        n_pages, max_pages, vs, vd, new_len, total_groups, status);

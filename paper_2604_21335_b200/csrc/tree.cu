@@ -2,10 +2,13 @@
 //
 // stc_tree_accept.  Only the logits of accepted nodes matter, and which they are is known step by step: the root's row
 // gives a token, the token a child, the child's row the next token.  So a cluster of CTAs walks one sequence: each CTA
-// takes a slice of the row, the slices' maxima meet in distributed shared memory, every CTA finds the child by itself.
+// takes a slice of the row, every warp tells all CTAs its best through distributed shared memory, every warp finds the child by
+// itself.  Bound by that chain: a row from HBM, one meeting, the child, eight times over for 16 trees of 64 over 152064 words in
+// bf16 (25 us, 3.3 us of bytes).  A thread keeps the 16 bytes with its largest logit and looks for the place in them once, at the
+// end of the row; key and index reduce as two 32-bit words (place by place, 64-bit words and a stage per CTA: 49 us).
 //
 // stc_tree_commit.  One CTA per (sequence, KV head): rows of 256 bytes from the draft buffers to the cache, a few kilobytes
-// per problem; the time is one launch and two dependent round trips (path, rows).
+// per problem; the time is one launch and two dependent round trips (path, rows): 6 us on the device for 64x8 problems.
 #include <cooperative_groups.h>
 
 #include "common.cuh"

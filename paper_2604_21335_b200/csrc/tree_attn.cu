@@ -34,10 +34,10 @@
 // thread, the other warps 80).  A unit's tree comes first, then its pages from the last to the first: with a distance bias the
 // largest scores come first.
 //
-// What bounds it (16x32/8 heads, 256 pages of 128 tokens in 16; measured by leaving parts out): with 64 nodes, 149 us, the softmax (132
-// without it) and the value copies (148 without them); with 16 nodes, 76 us, neither (74 and 75): the way of a tile from its page ids
-// over TMA, S, softmax and O, two tiles of K and three of S deep.  Three K stages, prefetching K into L2, one copy per page instead of
-// two, finding the next maximum before the weights of this tile: no gain.
+// What bounds it (16x32/8 heads, 256 listed pages; measured by leaving parts out): with 64 nodes the softmax (162 us, 132 without it) and
+// the value copies (148 without them); with 16 nodes (78 us) neither (74 and 75), but the way of a tile from its page ids over TMA, S,
+// softmax and O, two tiles of K and three of S deep.  Three K stages, keys prefetched into L2, one copy per page instead of two, the next
+// tile's maximum before the weights of this one: no gain.  Since then the joining kernel is faster (147 and 77 us).
 //
 // Every wait is bounded (about a second); one that expires raises a CTA-wide flag and STC_ERR_TIMEOUT in the status word, the
 // roles leave, the producer waits (bounded) for its copies, tensor memory is freed.
