@@ -1,6 +1,8 @@
 // Copying whole cached sequences and closing the gaps that dropped pages leave.  No arithmetic but prefix sums: both calls move
 // bytes and are bound by HBM (one read of each source, one write of each destination): 16 copies of two prompts of 16384 tokens
-// 181 us, 4.6 TB/s; 16x8 lists of 256 pages into another cache 94 us, 4.7 TB/s, where a plain copy reaches 6.6.
+// 181 us, 4.6 TB/s; 16x8 lists of 256 pages into another cache 91 us, 4.9 TB/s, where a plain copy reaches 6.6.  The copies are bound
+// by what is written: 4.1 TB/s, where the plain copy writes 3.3.  (A list of destinations in shared memory in place of two dependent
+// reads per copy: 188 us.)
 #include <cooperative_groups.h>
 
 #include "common.cuh"
@@ -195,11 +197,11 @@ __device__ __forceinline__ int kept_tokens(int problem, int len, int n, int Hkv,
 // Between two caches the pages are independent once their new offsets are known: a CTA takes a share of the list, the CTAs meet
 // once to tell each other the groups of their shares, and every warp moves pages by itself.
 template <int S>
-__global__ void __launch_bounds__(kCompactThreads, 2)
+__global__ void __launch_bounds__(kCompactThreads, 3)
 compact_apart_kernel(const int32_t* __restrict__ seq_len, int Hkv, const int32_t* __restrict__ page_ids,
                      const int32_t* __restrict__ n_pages, int max_pages, View src, View dst, int32_t* __restrict__ new_len,
                      int64_t* __restrict__ total_groups, int32_t* __restrict__ status) {
-    constexpr int OPG = kOctets / S, kWarps = kCompactThreads / 32, kPer = kPage * kOctets / 32;
+    constexpr int OPG = kOctets / S, kWarps = kCompactThreads / 32, kPer = kPage * kOctets / 64;        // (half a page at a time)
     __shared__ uint32_t sh_count[kCompactCtas], sh_sum[kWarps], sh_first[kCompactThreads], sh_to[kCompactThreads], sh_size[kCompactThreads];
     __shared__ int sh_page[kCompactThreads];
     cg::cluster_group cluster = cg::this_cluster();
@@ -276,26 +278,30 @@ compact_apart_kernel(const int32_t* __restrict__ seq_len, int Hkv, const int32_t
             const uint32_t from = sh_first[j], to = sh_to[j];
             const int64_t room = src.cap_groups - (int64_t)from;             // (offsets that do not fit the store are not followed)
             const int chunks = (int)min((int64_t)sh_size[j], max(room, (int64_t)0)) * OPG;
-            uint4 key[kPer], val[kPer], meta = {};
+            const int64_t fits = (dst.cap_groups - (int64_t)to) * OPG;
+            uint4 meta = {};
             uint32_t word = 0, off = 0;
-#pragma unroll
-            for (int e = 0; e < kPer; ++e)
-                if (lane + e * 32 < tokens * kOctets) key[e] = ldg_nc16(ks + (size_t)t0 * kOctets + lane + e * 32);
-#pragma unroll
-            for (int e = 0; e < kPer; ++e)
-                if (lane + e * 32 < chunks) val[e] = ldg_nc16(vs + (size_t)from * OPG + lane + e * 32);
             if (dst.kmin) meta = ldg_nc16((lane < kOctets ? src.kmin : src.kmax) + ((size_t)problem * src.P + t0 / kPage) * kOctets + (lane & 15));
             if (lane < tokens) {
                 word = src.v_mask[(size_t)problem * src.T + t0 + lane];
                 off = offs[t0 + lane] - from;
             }
+#pragma unroll 1
+            for (int at = lane; at < kPage * kOctets; at += 32 * kPer) {
+                uint4 key[kPer], val[kPer];
 #pragma unroll
-            for (int e = 0; e < kPer; ++e)
-                if (lane + e * 32 < tokens * kOctets) kd[(size_t)i * kPage * kOctets + lane + e * 32] = key[e];
-            const int64_t fits = (dst.cap_groups - (int64_t)to) * OPG;
+                for (int e = 0; e < kPer; ++e)
+                    if (at + e * 32 < tokens * kOctets) key[e] = ldg_nc16(ks + (size_t)t0 * kOctets + at + e * 32);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e)
-                if (lane + e * 32 < chunks && lane + e * 32 < fits) vd[(size_t)to * OPG + lane + e * 32] = val[e];
+                for (int e = 0; e < kPer; ++e)
+                    if (at + e * 32 < chunks) val[e] = ldg_nc16(vs + (size_t)from * OPG + at + e * 32);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e)
+                    if (at + e * 32 < tokens * kOctets) kd[(size_t)i * kPage * kOctets + at + e * 32] = key[e];
+#pragma unroll
+                for (int e = 0; e < kPer; ++e)
+                    if (at + e * 32 < chunks && at + e * 32 < fits) vd[(size_t)to * OPG + at + e * 32] = val[e];
+            }
             if (dst.kmin) ((lane < kOctets ? dst.kmin : dst.kmax) + ((size_t)problem * dst.P + i) * kOctets)[lane & 15] = meta;
             if (lane < tokens) {
                 dst.v_mask[(size_t)problem * dst.T + i * kPage + lane] = (uint16_t)word;
@@ -491,7 +497,7 @@ cudaError_t launch_cache_compact(const Geom& gs, const stc_cache& src, const int
     cfg.attrs = &cluster;
     cfg.numAttrs = 1;
     // (between two caches a share of the list per CTA and one meeting; within one, in order, a meeting per 32 pages.  16x8 lists of 256
-    // pages: 94 and 140 us)
+    // pages: 91 and 140 us)
 #define STC_COMPACT(S_) \
     case S_: return cudaLaunchKernelEx(&cfg, src.k == dst.k ? compact_kernel<S_> : compact_apart_kernel<S_>, gs.seq_len, gs.Hkv, page_ids, \
                                        n_pages, max_pages, vs, vd, new_len, total_groups, status);
