@@ -557,6 +557,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         // ---- softmax: thread = a row and kCols of a tile's 128 tokens: a lane has 64 of them in each of its two warps, a copy its
         // part of those and zeros elsewhere -----------------------------------------------------------------------------
+        constexpr int kStep = kCols < 32 ? kCols : 32;           // of them at a time
+        constexpr bool kHeld = kCols == kStep;                   // a tile's scores stay in registers from the maximum to the weights
         const int grp = (warp - 4) >> 2, quarter = warp & 3, place = quarter * 32 + lane, row = place % R, copy = place / R;
         const int half = 64 * grp, c0 = half + copy * kCols;     // first token; half: first channel of those that this warp looks after
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), to = lanes + kBufs * kTok;
@@ -655,12 +657,12 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 const bool open = __all_sync(0xFFFFFFFFu, !mine || (see[0] & see[kWords - 1] & kAll) == kAll);
                 const bool empty_now = n > 0 && n % kFlush == 0;
                 const float m_acc = m;               // maximum the accumulator was built with
-                // maximum of the tile; scores that are not raw products times a positive scale, or hidden, are written back
+                // maximum of the tile; scores that are not raw products times a positive scale, or hidden, are written back (where a
+                // thread has up to 32 they stay in its registers instead: 8x28/4 heads, 5 nodes, capped, 78 -> 73 us)
                 float top = -INFINITY;
-                constexpr int kStep = kCols < 32 ? kCols : 32;
+                uint32_t r[kStep];
 #pragma unroll 1
                 for (int c = 0; c < kCols; c += kStep) {
-                    uint32_t r[kStep];
                     tmem_ld16<0>(ts + c, r);
                     if constexpr (kStep > 16) tmem_ld16<16>(ts + c + 16, r);
                     tmem_wait_ld();
@@ -708,7 +710,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         t4[(i >> 1) & 3] = fmaxf(fmaxf(t4[(i >> 1) & 3], __uint_as_float(r[i])), __uint_as_float(r[i + 1]));
                     __syncwarp();
                     top = fmaxf(top, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
-                    if (SCORE || !open) {
+                    if (!kHeld && (SCORE || !open)) {
 #pragma unroll
                         for (int e = 0; e < kStep; e += 16) {
                             uint32_t o[16];
@@ -718,7 +720,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         }
                     }
                 }
-                if (SCORE || !open) tmem_wait_st();
+                if (!kHeld && (SCORE || !open)) tmem_wait_st();
                 if (!SCORE) top *= a.scale_log2;     // (-inf stays -inf: the scale is positive)
                 float all_tops[kTold];
                 ok = exchange(top, all_tops);
@@ -765,10 +767,11 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 float2 la = make_float2(0.f, 0.f), lb = la;
 #pragma unroll 1
                 for (int c = 0; c < kCols; c += kStep) {
-                    uint32_t r[kStep];
-                    tmem_ld16<0>(ts + c, r);
-                    if constexpr (kStep > 16) tmem_ld16<16>(ts + c + 16, r);
-                    tmem_wait_ld();
+                    if constexpr (!kHeld) {
+                        tmem_ld16<0>(ts + c, r);
+                        if constexpr (kStep > 16) tmem_ld16<16>(ts + c + 16, r);
+                        tmem_wait_ld();
+                    }
 #pragma unroll
                     for (int e = 0; e < kStep; e += 16) {
                         uint32_t o[16];
@@ -1008,7 +1011,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 // Joins the partials of units that more than one CTA worked on, in CTA order: blockIdx.x = the CTA that begins the unit, blockIdx.y =
 // 8 rows of it; behind them blocks that check the trees and gather the CTAs' status.  Few dependent loads on purpose: nothing
 // hides this kernel's latency (with the units looked up by problem it took 24 us at 16x32/8 heads and 64 nodes).
-__global__ void __launch_bounds__(256, 3)
+__global__ void __launch_bounds__(256, 4)
 tree_join_kernel(const TreeArgs a, int grid) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((int)blockIdx.x >= grid) {
@@ -1044,7 +1047,7 @@ tree_join_kernel(const TreeArgs a, int grid) {
     if (split.x < 0 || node_in >= a.block_nodes || node >= split.w) return;
     const int b = (int)((uint32_t)split.x / (uint32_t)a.Hkv), hk = split.x - b * a.Hkv;
     const size_t row = ((size_t)b * a.n_cap + node) * a.Hq + hk * a.Gq + h;
-    constexpr int kAtOnce = 8;                       // loads in flight
+    constexpr int kAtOnce = 4;                       // loads in flight
     const int copies_log2 = __ffs(kRows / a.rows) - 1, parts = (c1 - c0 + 1) << copies_log2;
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1142,8 +1145,8 @@ cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tr
     a.B = g.B; a.Hq = g.Hq; a.Hkv = g.Hkv; a.Gq = g.Gq; a.S = g.S; a.T = g.T; a.n_cap = tree.n_cap;
     a.max_pages = max_pages; a.problems = g.problems;
     // The fewest rows that hold a whole tree: the time of a tile goes with the tokens that a thread weighs (8x28/4 heads, 5 nodes, capped
-    // scores: 99 -> 77 us with 64 rows, 16x32/8, 16 nodes: 78 -> 77).  Copies have to be added up at the end, so not where a CTA gets few
-    // tiles (1x8 heads, 8 nodes, 64 pages: 18 us, 25 with copies).
+    // scores: 99 -> 77 us with 64 rows; 16x32/8, 16 nodes: 78 -> 77).  Copies have to be added up at the end, so not where a CTA gets
+    // few tiles (1x8 heads, 8 nodes, 64 pages: 18 us, 25 with copies).
     int sms = 0;
     cudaError_t e = device_sm_count(&sms);
     if (e != cudaSuccess) return e;
