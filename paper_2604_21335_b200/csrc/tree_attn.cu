@@ -30,8 +30,8 @@
 //
 // The running maximum only moves when a tile exceeds it by more than 2^24, so the accumulator in tensor memory is rescaled a few times
 // per segment and not per tile.  The tensor core truncates when it adds to an accumulator (4e-8 of its value per product, 16
-// products per tile), so an accumulator is emptied every kFlush tiles into fp32 sums, which the softmax warps hold in registers (176 a
-// thread, the other warps 80).  A unit's tree comes first, then its pages from the last to the first: with a distance bias the
+// products per tile), so an accumulator is emptied every kFlush tiles into fp32 sums, which the softmax warps hold in registers (184 a
+// thread, the other warps 72).  A unit's tree comes first, then its pages from the last to the first: with a distance bias the
 // largest scores come first.
 //
 // What bounds it (16x32/8 heads, 256 listed pages; measured by leaving parts out): with 64 nodes the softmax (162 us, 132 without it) and
@@ -62,7 +62,7 @@ constexpr int kBufs = 3;                          // score buffers: 128 columns 
 constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 24.f;                    // log2 units a maximum may be exceeded by: weights up to 2^24 are as exact as others
-constexpr int kSoftmaxRegs = 176, kOtherRegs = 80;           // of the 128 per thread of the launch
+constexpr int kSoftmaxRegs = 184, kOtherRegs = 72;           // of the 128 per thread of the launch; 168, 176, 184: 8x28/4 chain 73.9, 73.2, 71.8 us
 static_assert(256 * kSoftmaxRegs + 256 * kOtherRegs <= 128 * kThreads, "registers of a block");
 constexpr int kKStages = 2, kVSlots = 6;          // K tiles; half V tiles
 
