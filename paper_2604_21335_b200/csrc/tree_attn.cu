@@ -171,12 +171,13 @@ __device__ __forceinline__ void cp_async16_if(uint32_t dst, const void* src, uin
                  ::"r"(dst), "l"(src), "r"(take) : "memory");
 }
 // MASK: a window, documents or positions that are given; SCORE: cap, slopes, or a scale that is not positive (with MASK).
-// R rows of a block; the lanes hold 128 / R copies of them.
-template <int R, bool MASK, bool SCORE>
+// R rows of a block; the lanes hold 128 / R copies of them.  APART: a window and given positions, whose windows may lie apart (a variant
+// of its own: with the look-up in all of them 16x32/8 heads, 16 nodes, documents took 78 us, now 73, the 8x28/4 chain 78, now 70).
+template <int R, bool MASK, bool SCORE, bool APART>
 __global__ void __launch_bounds__(kThreads, 1)
 tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                  const __grid_constant__ CUtensorMap map_new, const TreeArgs a) {
-    static_assert(MASK || !SCORE, "SCORE needs the positions");
+    static_assert(MASK || !(SCORE || APART), "SCORE and APART need the positions");
     constexpr int kCopies = kRows / R, kCols = R / 2;         // tokens of a tile that a thread weighs
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = smem_u32(smem);
@@ -895,8 +896,11 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             const uint32_t* offs = a.v_offs + problem * (a.T + 1);
             const uint4* packed = a.v_packed + problem * a.cap_groups * opg;
             const uint4* fresh = a.v_new + problem * a.n_cap * kOctets;
-            // tokens that no row of the sequence sees are left out: they may hold anything
+            // tokens that no row of the sequence sees are left out: they may hold anything.  All that are seen lie in [lo_all, hi_all);
+            // with given positions farther apart than the window there may be others between them, and each token is looked up
+            // (16x32/8 heads, 256 listed pages, window 64: 16 nodes 71 -> 77 us, 4x32/8 with 128 nodes 90 -> 138)
             int lo_all = 0, hi_all = s.len, q_doc = 0;
+            bool gaps = false;
             if constexpr (MASK) {
                 if (a.sc.q_pos) {
                     int least = 0x7FFFFFFF, most = -1;
@@ -910,11 +914,22 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     most = __reduce_max_sync(0xFFFFFFFFu, most);
                     if (a.sc.window > 0 && least >= a.sc.window) lo_all = least - a.sc.window + 1;
                     if (most < s.len) hi_all = most + 1;
+                    gaps = (long long)most - least > a.sc.window;
                 } else if (a.sc.window > 0 && s.len >= a.sc.window) {
                     lo_all = s.len - a.sc.window + 1;
                 }
                 if (a.sc.tok_doc) q_doc = a.sc.q_doc[s.b];
             }
+            auto seen_by_a_node = [&](int at) {
+                const int32_t* const pos = a.sc.q_pos + (size_t)s.b * a.n_cap;
+                bool seen = false;
+#pragma unroll 4
+                for (int i = 0; i < s.nodes; ++i) {
+                    const int p = __ldg(pos + i);
+                    seen |= at <= p && (uint32_t)p - (uint32_t)at < a.window;
+                }
+                return seen;
+            };
             // of this lane's token: its mask, its page's first group, its document; -1 or the token
             auto ask_page = [&](int t) { return t >= s.tile0 ? listed(t * kTilePages + (tok0 + lane) / kPage) : -1; };
             auto ask_mask = [&](int id, uint32_t& m, uint32_t& first, int& doc) {
@@ -936,6 +951,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 const uint32_t every = m_next & all_groups, first = first_next;
                 uint32_t m = every;
                 if (MASK && (at_next < lo_all || at_next >= hi_all || (doc_next >= 0 && doc_next != q_doc))) m = 0;
+                if (APART && gaps && !seen_by_a_node(at_next)) m = 0;
                 at_next = ask_mask(id_next, m_next, first_next, doc_next);
                 id_next = ask_page(t - 2);
                 const int v = 2 * vc + half, slot = v % kVSlots;
@@ -1095,23 +1111,25 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // The workspace has to be sized without a device, so the partial slots are counted for this many CTAs.
 constexpr int kPlanSms = 148;
 
-template <int R, bool MASK, bool SCORE>
+template <int R, bool MASK, bool SCORE, bool APART>
 cudaError_t launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& fresh, const TreeArgs& a, int n_cta, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<R, MASK, SCORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<R, MASK, SCORE, APART>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
     if (e != cudaSuccess) return e;
     cudaFuncAttributes f;                            // (a launch with fewer registers would wait for them without end)
-    e = cudaFuncGetAttributes(&f, tree_attn_kernel<R, MASK, SCORE>);
+    e = cudaFuncGetAttributes(&f, tree_attn_kernel<R, MASK, SCORE, APART>);
     if (e != cudaSuccess) return e;
     if (f.numRegs * kThreads < 256 * kSoftmaxRegs + 256 * kOtherRegs) return cudaErrorInvalidConfiguration;
-    tree_attn_kernel<R, MASK, SCORE><<<n_cta, kThreads, kSmem, st>>>(q, k, fresh, a);
+    tree_attn_kernel<R, MASK, SCORE, APART><<<n_cta, kThreads, kSmem, st>>>(q, k, fresh, a);
     return cudaGetLastError();
 }
 
 template <int R>
 cudaError_t launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& fresh, const TreeArgs& a, int n_cta, bool masked, bool scored,
                    cudaStream_t st) {
-    return scored ? launch<R, true, true>(q, k, fresh, a, n_cta, st)
-           : masked ? launch<R, true, false>(q, k, fresh, a, n_cta, st) : launch<R, false, false>(q, k, fresh, a, n_cta, st);
+    if (a.sc.q_pos && a.sc.window > 0)
+        return scored ? launch<R, true, true, true>(q, k, fresh, a, n_cta, st) : launch<R, true, false, true>(q, k, fresh, a, n_cta, st);
+    return scored ? launch<R, true, true, false>(q, k, fresh, a, n_cta, st)
+           : masked ? launch<R, true, false, false>(q, k, fresh, a, n_cta, st) : launch<R, false, false, false>(q, k, fresh, a, n_cta, st);
 }
 
 }  // namespace
