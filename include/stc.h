@@ -535,7 +535,8 @@ int32_t stc_tree_accept(int32_t batch, int32_t n_cap, int32_t vocab, const void*
  *   total_groups  i64 [B][Hkv], status i32 [B][Hkv] as in stc_append_tokens (STC_ERR_CAPACITY: groups past cap_groups were
  *                 not stored).  A sequence with n_accepted outside [0, n_cap], a path entry outside [0, n_nodes[b])
  *                 or more tokens than t_cap is left untouched, total_groups too, with new_len = len and STC_ERR_INVALID_ARG.
- * tree->parent is not read.  Needs no workspace. */
+ * t_cap = 0: STC_OK, but nothing is enqueued and no output is written, new_len and status among them; a caller whose cache may have no room
+ * looks at t_cap first.  tree->parent is not read.  Needs no workspace. */
 int32_t stc_tree_commit(const stc_shape* shape, const stc_cache* cache, const stc_tree* tree, const int32_t* path,
                         const int32_t* n_accepted, int32_t* new_len, int64_t* total_groups, int32_t* status,
                         void* stream);
@@ -552,7 +553,8 @@ int32_t stc_tree_commit(const stc_shape* shape, const stc_cache* cache, const st
  *                     earlier pair has, more tokens than dst's t_cap, or, within one cache, a dst_row that is
  *                     the src_row of a pair (a pair of a row with itself is fine and moves nothing)
  * dst->kmin and kmax may be NULL (metadata is not copied), and are NULL where src's are.  Buffers of different caches must not
- * overlap.  n_pairs <= 4096, n_kv_heads <= 65535.  Needs no workspace. */
+ * overlap.  t_cap = 0 of either cache: STC_OK, nothing is enqueued and no output is written, as in stc_tree_commit.
+ * n_pairs <= 4096, n_kv_heads <= 65535.  Needs no workspace. */
 int32_t stc_cache_fork(const stc_shape* src_shape, const stc_cache* src, const stc_shape* dst_shape, const stc_cache* dst,
                        int32_t n_pairs, const int32_t* src_row, const int32_t* dst_row, int32_t* new_len,
                        int64_t* total_groups, int32_t* status, void* stream);
@@ -570,7 +572,7 @@ int32_t stc_cache_fork(const stc_shape* src_shape, const stc_cache* src, const s
  *   total_groups       i64 [B][Hkv];   status i32 [B][Hkv]: STC_OK; STC_ERR_CAPACITY (groups past dst's cap_groups were not
  *                      stored); STC_ERR_INVALID_ARG in all heads of a sequence whose lists are not as above or do
  *                      not fit dst's t_cap: new_len = len, nothing else is written
- * kmin / kmax as in stc_cache_fork.  Needs no workspace. */
+ * kmin / kmax and t_cap = 0 as in stc_cache_fork.  Needs no workspace. */
 int32_t stc_cache_compact(const stc_shape* src_shape, const stc_cache* src, const int32_t* page_ids,
                           const int32_t* n_pages, int32_t max_pages, const stc_shape* dst_shape, const stc_cache* dst,
                           int32_t* new_len, int64_t* total_groups, int32_t* status, void* stream);

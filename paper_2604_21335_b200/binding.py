@@ -632,6 +632,12 @@ def _check_cache(shape: Shape, cache: Cache, what: str = "") -> None:
         raise ValueError("v_mask must hold 16-bit and v_offs 32-bit integers")
 
 
+def _check_room(what: str, *shapes: Shape) -> None:
+    """The library does nothing for a cache of t_cap 0, and says STC_OK: outputs that a caller reads next would be left as they were."""
+    if any(s.t_cap == 0 and s.batch > 0 for s in shapes):
+        raise ValueError(f"{what} needs caches with room for tokens, got t_cap 0")
+
+
 def _check_tree(shape: Shape, tree: Tree) -> int:
     n = tree.k.shape[2] if tree.k.dim() == 4 else -1
     rows = (shape.batch, shape.n_kv_heads, n, shape.head_dim)
@@ -699,9 +705,10 @@ _COMMIT_NAMES = ("seq_len", *_CACHE_NAMES, "tree.k", "tree.v", "tree.n_nodes", "
 def tree_commit(shape: Shape, cache: Cache, tree: Tree, path: torch.Tensor, n_accepted: torch.Tensor, new_len: torch.Tensor,
                 total_groups: torch.Tensor, status: torch.Tensor) -> None:
     """The accepted nodes path[b, :n_accepted[b]] become the tokens behind shape.seq_len[b] (the lengths before the call), at full
-    width, in cache.k and the packed store; new_len i32 [B] receives the lengths."""
+    width, in cache.k and the packed store; new_len i32 [B] receives the lengths.  A cache of t_cap 0 is refused."""
     dev, B, H = _current_device(), shape.batch, shape.n_kv_heads
     n = _check_tree(shape, tree)
+    _check_room("tree_commit", shape)
     _check_cache(shape, cache)
     _sizes(("path", "n_accepted", "new_len", "total_groups", "status"), path, (B, n), n_accepted, (B,), new_len, (B,), total_groups,
            (B, H), status, (B, H))
@@ -722,8 +729,11 @@ _FORK_NAMES = ("seq_len", *("src." + n for n in _CACHE_NAMES), *("dst." + n for 
 def cache_fork(src_shape: Shape, src: Cache, dst_shape: Shape, dst: Cache, src_row: torch.Tensor, dst_row: torch.Tensor,
                new_len: torch.Tensor, total_groups: torch.Tensor, status: torch.Tensor) -> None:
     """Copies the sequences src_row[i] of src to the rows dst_row[i] of dst (which may be src); pairs of one source next to each
-    other share its reading.  new_len i32 [dst batch], total_groups i64 [dst batch, Hkv], status i32 [pairs, Hkv]."""
+    other share its reading.  new_len i32 [dst batch], total_groups i64 [dst batch, Hkv], status i32 [pairs, Hkv].  Caches of t_cap 0
+    are refused."""
     dev, n, B, H = _current_device(), src_row.shape[0], dst_shape.batch, dst_shape.n_kv_heads
+    if n > 0:
+        _check_room("cache_fork", src_shape, dst_shape)
     _check_cache(src_shape, src, "src")
     _check_cache(dst_shape, dst, "dst")
     _sizes(("src_row", "dst_row", "new_len", "total_groups", "status"), src_row, (n,), dst_row, (n,), new_len, (B,), total_groups, (B, H),
@@ -744,11 +754,12 @@ _COMPACT_NAMES = ("seq_len", *("src." + n for n in _CACHE_NAMES), *("dst." + n f
 def cache_compact(shape: Shape, cache: Cache, page_ids: torch.Tensor, n_pages: torch.Tensor, new_len: torch.Tensor,
                   total_groups: torch.Tensor, status: torch.Tensor, dst_shape: Optional[Shape] = None, dst: Optional[Cache] = None) -> None:
     """Keeps the listed pages of every KV head, closed up, in dst (None: in place).  page_ids i32 [B, Hkv, max], ascending, n_pages
-    i32 [B, Hkv], new_len i32 [B], total_groups i64 [B, Hkv], status i32 [B, Hkv]."""
+    i32 [B, Hkv], new_len i32 [B], total_groups i64 [B, Hkv], status i32 [B, Hkv].  Caches of t_cap 0 are refused."""
     if (dst is None) != (dst_shape is None):
         raise ValueError("cache_compact needs both dst_shape and dst, or neither")
     to_shape, to = (shape, cache) if dst is None else (dst_shape, dst)
     dev, B, H, most = _current_device(), shape.batch, shape.n_kv_heads, page_ids.shape[-1]
+    _check_room("cache_compact", shape, to_shape)
     _check_cache(shape, cache)
     if dst is not None:
         _check_cache(dst_shape, dst, "dst")
