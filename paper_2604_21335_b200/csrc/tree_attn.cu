@@ -48,7 +48,7 @@
 namespace stc {
 namespace {
 
-constexpr int kTok = 128;                         // tokens per tile = tensor-memory lanes
+constexpr int kTok = 128;                         // tokens per tile = tensor-memory columns of its scores
 constexpr int kTilePages = kTok / kPage;
 constexpr int kThreads = 512;
 constexpr int kSegs = 2;                          // segments the scheduler may be ahead
