@@ -1162,16 +1162,21 @@ cudaError_t launch_tree_attn(const Geom& g, const stc_cache& cache, const stc_tr
     a.cap_groups = cache.cap_groups;
     a.B = g.B; a.Hq = g.Hq; a.Hkv = g.Hkv; a.Gq = g.Gq; a.S = g.S; a.T = g.T; a.n_cap = tree.n_cap;
     a.max_pages = max_pages; a.problems = g.problems;
-    // The fewest rows that hold a whole tree: the time of a tile goes with the tokens that a thread weighs (8x28/4 heads, 5 nodes, capped
-    // scores: 99 -> 77 us with 64 rows; 16x32/8, 16 nodes: 78 -> 77).  Copies have to be added up at the end, so not where a CTA gets
-    // few tiles (1x8 heads, 8 nodes, 64 pages: 18 us, 25 with copies).
+    // The fewest rows that hold a whole tree, copied over the other lanes: the time of a tile goes with the tokens that a thread weighs.  The
+    // copies of a row have to be added up at the end, by the second kernel copies * CTAs per unit parts of a row, so they pay from some
+    // tiles per CTA on that grow with the parts.  Measured with 1 to 16 sequences of 4 or 8 KV heads, 2 to 48 tiles per CTA; with 5, 9, 18,
+    // 37 and 74 parts they pay from 7, 6, 11, 16, 30 tiles on without options, 6, 4, 9, 12, 21 with masks, 3, 2, 3, 6, 10 with a cap, 5, 3,
+    // 7, 8, 15 with slopes.  1x32/8 heads, 16 nodes (37 parts), no options: 6 tiles per CTA 31 us without copies and 35 with them, 28 tiles
+    // 68 and 62; 8x28/4, 5 nodes, cap (9 parts): 2 tiles 27 and 27, 24 tiles 91 and 66.
     int sms = 0;
     cudaError_t e = device_sm_count(&sms);
     if (e != cudaSuccess) return e;
     const int n_cta = sms < kPlanSms ? sms : kPlanSms;
     const int64_t most_tiles = (int64_t)g.problems * ((page_ids ? max_pages : g.P) / kTilePages + 1);
-    a.rows = most_tiles <= 4 * n_cta ? kRows : 32;
+    a.rows = 32;
     while (a.rows < kRows && a.rows / g.Gq < tree.n_cap) a.rows *= 2;
+    const double parts = (double)(kRows / a.rows) * n_cta / g.problems;
+    if ((double)most_tiles <= n_cta * (scored ? 1.5 + parts / 7 : masked ? 3.5 + parts / 4 : 4 + parts / 3)) a.rows = kRows;
     a.block_nodes = a.rows / g.Gq;
     a.gq_inv = (65536u + (uint32_t)g.Gq - 1u) / (uint32_t)g.Gq;
     a.sc = score;
