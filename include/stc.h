@@ -482,7 +482,9 @@ int32_t stc_prefix_attn(const stc_shape* shape, const stc_cache* cache, int32_t 
 
 /* Attention for trees of drafted tokens over a routed cache (the attention equation of Section 3.3 for the verification
  * step of speculative decoding, which the paper does not have): every node of a sequence's tree attends the valid tokens
- * of the sequence's listed pages -- read once for all nodes and query heads of a KV head -- and its own ancestors:
+ * of the sequence's listed pages and its own ancestors.  Pages are read once per block of nodes, whose nodes times query heads per KV
+ * head are at most 128 rows: once for all nodes of a KV head up to there, eight times for 128 nodes and 8 heads.  Listed pages of which an
+ * option hides every token are read all the same.
  *   N_i = node i, its parent, the parent's parent, ...;   position of node i: p_i = score->q_pos[b][i], or
  *         len + |N_i| - 1 where q_pos is NULL (cached token t stands at t, the tree continues the sequence)
  *     s_t = sm_scale * q_i.k_t over the listed tokens t and, over j in N_i, s_j = sm_scale * q_i.k_j (k_j: tree->k),
@@ -544,8 +546,8 @@ int32_t stc_tree_commit(const stc_shape* shape, const stc_cache* cache, const st
 /* Copies of whole cached sequences (several answers to one prompt, beams, hand-over to another cache; not in the paper).
  * For every pair i the sequence src_row[i] of `src` becomes the sequence dst_row[i] of `dst`: keys, page metadata, masks,
  * offsets and packed groups up to its length.  The shapes agree in everything but batch, t_cap and seq_len
- * (dst_shape->seq_len is not read); `dst` may be `src` (the same k), whose rows that are not a dst_row are left alone.
- *   src_row, dst_row  device i32 [n_pairs]; pairs of one source next to each other share its reading
+ * (dst_shape->seq_len is not read; new_len must not be src_shape->seq_len); `dst` may be `src` (the same k), whose rows that are not a dst_row are left alone.
+ *   src_row, dst_row  device i32 [n_pairs]; pairs of one source next to each other share its reading (up to 16 of them)
  *   new_len           i32 [dst batch]: entry dst_row[i] receives the length
  *   total_groups      i64 [dst batch][Hkv]: row dst_row[i] receives the groups
  *   status            i32 [n_pairs][Hkv]: STC_OK; STC_ERR_CAPACITY (groups past dst's cap_groups were not stored);

@@ -1,8 +1,8 @@
 // Copying whole cached sequences and closing the gaps that dropped pages leave.  No arithmetic but prefix sums: both calls move
-// bytes and are bound by HBM (one read of each source, one write of each destination): 16 copies of two prompts of 16384 tokens
-// 181 us, 4.6 TB/s; 16x8 lists of 256 pages into another cache 91 us, 4.9 TB/s, where a plain copy reaches 6.6.  The copies are bound
-// by what is written: 4.1 TB/s, where the plain copy writes 3.3.  (A list of destinations in shared memory in place of two dependent
-// reads per copy: 188 us.)
+// bytes (one read of each source, one write of each destination): 16 copies of two prompts of 16384 tokens 180 us, 4.6 TB/s; 16x8 lists
+// of 256 pages into another cache 91 us, 4.9 TB/s, in place 138 us, where a plain copy reaches 6.6.  The copies write 4.1 TB/s, which is
+// not the most that the chip writes: a kernel that only stores, in the same order, reaches 6.0 to 6.8.  (A list of destinations in shared
+// memory in place of two dependent reads per copy: 188 us.)
 #include <cooperative_groups.h>
 
 #include "common.cuh"
@@ -501,7 +501,7 @@ cudaError_t launch_cache_compact(const Geom& gs, const stc_cache& src, const int
     cfg.attrs = &cluster;
     cfg.numAttrs = 1;
     // (between two caches a share of the list per CTA and one meeting; within one, in order, a meeting per 32 pages.  16x8 lists of 256
-    // pages: 91 and 140 us)
+    // pages: 91 and 138 us)
 #define STC_COMPACT(S_) \
     case S_: return cudaLaunchKernelEx(&cfg, src.k == dst.k ? compact_kernel<S_> : compact_apart_kernel<S_>, gs.seq_len, gs.Hkv, page_ids, \
                                        n_pages, max_pages, vs, vd, new_len, total_groups, status);

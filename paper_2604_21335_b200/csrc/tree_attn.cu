@@ -12,7 +12,7 @@
 // cycles of an SM with 128 rows, go with the rows.
 // (Tried first: tokens as lanes and rows as columns, which leaves no lane idle.  Weights then pass through shared memory, sums take a
 // register per row, maxima need the other warps, and the unrolled columns do not fit the instruction cache: 3200 cycles per tile
-// with 16 rows, 5000 with 128; now 2600 and 3100.)
+// with 16 rows, 5000 with 128; in this form 2600 and 3100.)
 // P enters as a bf16 high part plus a bf16 residual (two MMAs): the output is fp32, and one bf16 weight alone would leave it 2^-8 off;
 // the pair leaves 2^-16.
 //
@@ -34,10 +34,11 @@
 // thread, the other warps 72).  A unit's tree comes first, then its pages from the last to the first: with a distance bias the
 // largest scores come first.
 //
-// What bounds it (16x32/8 heads, 256 listed pages; measured by leaving parts out): with 64 nodes the softmax (162 us, 132 without it) and
-// the value copies (148 without them); with 16 nodes (78 us) neither (74 and 75), but the way of a tile from its page ids over TMA, S,
-// softmax and O, two tiles of K and three of S deep.  Three K stages, keys prefetched into L2, one copy per page instead of two, the next
-// tile's maximum before the weights of this one: no gain.  Since then the joining kernel is faster (147 and 77 us).
+// What bounds it (16x32/8 heads, 256 listed pages; measured by leaving parts out): with 64 nodes (two blocks, 127 us) the softmax, 102
+// without it, and a little the value copies, 123 without them; with 16 nodes and documents (74 us) not the softmax (75 without it), but the
+// way of a tile from its page ids over TMA, S, softmax and O, two tiles of K and three of S deep; half of its pages are hidden and go the
+// same way.  8x28/4 chain, cap and window (72 us): 62 without the softmax, 66 without the value copies.  Three K stages, keys prefetched
+// into L2, one copy per page instead of two, the next tile's maximum before the weights of this one: no gain.
 //
 // Every wait is bounded (about a second); one that expires raises a CTA-wide flag and STC_ERR_TIMEOUT in the status word, the
 // roles leave, the producer waits (bounded) for its copies, tensor memory is freed.
